@@ -387,6 +387,33 @@ tt_status tt_verify_sharded(const tt_batch* batch, const float* q_hat, const tt_
                             int32_t* accepted, int32_t* next_token, float* p_hat, float* lse,
                             float* summaries, int32_t* status, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Operators around a verification step (no counterpart in the paper): what a
+ * serving loop asks of the rows the step reads.
+ */
+
+/* Outputs of tt_logprobs, per row r; status is required, the rest may be NULL. */
+typedef struct {
+  float* logprob;      /* [R] log p of the row's given column */
+  int32_t* rank;       /* [R] columns before it: larger logit, or equal and smaller column */
+  float* entropy;      /* [R] -sum p log p, nats */
+  float* lse;          /* [R] natural log-normaliser of z / T */
+  int32_t* top_ids;    /* [R * top_n] the best columns, larger logit first, then smaller column */
+  float* top_logprobs; /* [R * top_n] their log p */
+  int32_t* status;     /* [R] TT_REQ_* bits */
+} tt_logprobs_out;
+
+/* Log probabilities of R = rows->n_rows logits rows, p = softmax(z / T): of the
+ * given columns ids [R] (device; needed for logprob and rank; -1: no column,
+ * logprob 0 and rank -1; any other column outside the row: NaN, -1 and
+ * ID_OUT_OF_RANGE), the entropy, and the top_n best columns (0 ..
+ * TT_MAX_TOP_K). Columns of -inf have log p = -inf and are never among the best:
+ * where a row has fewer, the rest is (-1, -inf). A row that has no normaliser
+ * (nothing but -inf, or +inf or NaN anywhere) gets NaN, -1 and NOT_FINITE.
+ * Sums are kept in fp32. Needs no workspace. */
+tt_status tt_logprobs(const tt_logits* rows, const int32_t* ids, float temp, int32_t top_n,
+                      const tt_logprobs_out* out, void* stream);
+
 /* Static text for a tt_status. */
 const char* tt_status_string(tt_status s);
 

@@ -68,12 +68,17 @@ class _StepOut(ctypes.Structure):
                 ("lse", c_p)]
 
 
+class _LogprobsOut(ctypes.Structure):
+    _fields_ = [("logprob", c_p), ("rank", c_p), ("entropy", c_p), ("lse", c_p), ("top_ids", c_p),
+                ("top_logprobs", c_p), ("status", c_p)]
+
+
 _lib = None
 EXPORTS = ("tt_workspace_bytes", "tt_workspace_bytes_for", "tt_align", "tt_transfer", "tt_verify", "tt_step",
            "tt_step_noalloc", "tt_status_string", "tt_last_cuda_error", "tt_version",
            "tt_vocab_index_bytes", "tt_vocab_index_build", "tt_encode_workspace_bytes",
            "tt_encode", "tt_consistency", "tt_dpos_hist", "tt_sharded_workspace_bytes",
-           "tt_verify_sharded")
+           "tt_verify_sharded", "tt_logprobs")
 TT_MAX_SHARDS = 8
 TT_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -138,6 +143,8 @@ def load(build_if_missing: bool = False):
     L.tt_consistency.restype = c_i32
     L.tt_dpos_hist.argtypes = [P(_Batch), c_p, c_p, c_p, c_i32, c_i32, c_p, c_p]
     L.tt_dpos_hist.restype = c_i32
+    L.tt_logprobs.argtypes = [P(_Logits), c_p, c_f32, c_i32, P(_LogprobsOut), c_p]
+    L.tt_logprobs.restype = c_i32
     _lib = L
     return L
 
@@ -641,3 +648,38 @@ def tt_dpos_hist(batch: Batch, path: torch.Tensor, path_len: torch.Tensor,
                                int(mode), int(n_bins), _ptr(h), _stream(stream))
     _check("tt_dpos_hist", code)
     return h
+
+
+# --------------------------------------- operators around a verification step
+
+def _given(t, name, dtype, numel):
+    """A contiguous tensor argument of a type and at least a size (None passes)."""
+    if t is not None and (t.dtype != dtype or not t.is_contiguous() or t.numel() < numel):
+        raise ValueError("%s must be a contiguous %s tensor of %d elements or more"
+                         % (name, str(dtype).replace("torch.", ""), numel))
+    return _ptr(t)
+
+
+def tt_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, *, temp: float = 1.0,
+                top_n: int = 0, out=None, stream=None) -> dict:
+    """Log probabilities of logits rows [R, V], p = softmax(z / temp): lse and
+    entropy [R], with ids (int32 [R], -1: none) the logprob and the rank of each
+    row's column, and the top_n best columns as top_ids and top_logprobs
+    [R, top_n]; status [R]. Tensors given in ``out`` are written in place."""
+    L = _logits(logits)
+    R, dev = logits.shape[0], logits.device
+    o = dict(out or {})
+    for key in ("lse", "entropy") + (("logprob",) if ids is not None else ()):
+        _need(o, key, R, torch.float32, dev)
+    for key in ("status",) + (("rank",) if ids is not None else ()):
+        _need(o, key, R, torch.int32, dev)
+    if "top_ids" not in o:
+        o["top_ids"] = torch.empty((R, top_n), dtype=torch.int32, device=dev)
+    if "top_logprobs" not in o:
+        o["top_logprobs"] = torch.empty((R, top_n), dtype=torch.float32, device=dev)
+    c_out = _LogprobsOut(*[_ptr(o.get(k)) for k in ("logprob", "rank", "entropy", "lse", "top_ids",
+                                                    "top_logprobs", "status")])
+    code = load().tt_logprobs(ctypes.byref(L), _given(ids, "ids", torch.int32, R), float(temp),
+                              int(top_n), ctypes.byref(c_out), _stream(stream))
+    _check("tt_logprobs", code)
+    return o

@@ -9,6 +9,7 @@
 
 #include "tt_device.cuh"
 #include "tt_launch.h"
+#include "tt_ops.h"
 #include "tt_shard.h"
 
 namespace {
@@ -42,6 +43,7 @@ cudaError_t ensure_loaded() {
   if ((e = preload_nucleus_rows()) != cudaSuccess) return e;
   if ((e = preload_pen()) != cudaSuccess) return e;
   if ((e = preload_shard()) != cudaSuccess) return e;
+  if ((e = preload_logprobs()) != cudaSuccess) return e;
   if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
   return cudaSuccess;
 }
@@ -375,6 +377,9 @@ tt_status fill_align_args(const tt_batch* bt, const tt_vocab* vd, const tt_vocab
 
 namespace tt {
 tt_status record_cuda_error(cudaError_t e) { return cuda_fail(e); }
+cudaError_t load_kernels() { return ensure_loaded(); }
+int device_sms() { return sm_count_current(); }
+bool rows_usable(const tt_logits* L, int64_t rows) { return logits_ok(L, rows); }
 
 tt_status step_check(const tt_batch* batch, const tt_vocab* vd, const tt_vocab* vt,
                      const tt_logits* draft, const float* draft_probs, const tt_logits* target,
@@ -973,6 +978,6 @@ const char* tt_status_string(tt_status s) {
 
 int32_t tt_last_cuda_error(void) { return g_last_cuda_error.load(); }
 
-int32_t tt_version(void) { return 110; }
+int32_t tt_version(void) { return 120; }
 
 }  // extern "C"

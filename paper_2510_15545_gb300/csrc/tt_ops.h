@@ -1,0 +1,33 @@
+// tt_ops.h -- arguments and launchers of the operators around a verification
+// step: log probabilities of logits rows (logprob.cu).
+#pragma once
+
+#include <cstdint>
+#include <cuda_runtime.h>
+
+#include "tt.h"
+
+namespace tt {
+
+// What the entry points share (api.cu): every kernel loaded on the current
+// device, its SM count, logits rows that the kernels take, a failed call's code.
+cudaError_t load_kernels();
+int device_sms();
+bool rows_usable(const tt_logits* L, int64_t rows);
+tt_status record_cuda_error(cudaError_t e);
+
+struct LogprobArgs {
+  const char* data;
+  int64_t stride_bytes;
+  int64_t rows;
+  int V;
+  float temp, scale;  // T, log2(e) / T
+  int top_n;
+  const int32_t* ids;
+  tt_logprobs_out out;
+};
+
+cudaError_t launch_logprobs(const LogprobArgs& args, int dt, cudaStream_t stream, int sm_count);
+cudaError_t preload_logprobs();
+
+}  // namespace tt
