@@ -414,6 +414,46 @@ typedef struct {
 tt_status tt_logprobs(const tt_logits* rows, const int32_t* ids, float temp, int32_t top_n,
                       const tt_logprobs_out* out, void* stream);
 
+#define TT_MAX_DISTILL_K 128 /* longest teacher list per row */
+
+/* A teacher's top log probabilities per row (tt_logprobs' top_ids and
+ * top_logprobs are one): k entries (column, natural log probability); column -1
+ * marks an unused entry, entries of one column add up, entries of -inf add nothing. */
+typedef struct {
+  const int32_t* ids; /* device, [R * k] */
+  const float* logp;  /* device, [R * k] */
+  int32_t k;          /* 0 .. TT_MAX_DISTILL_K */
+} tt_teacher;
+
+/* Distillation: the loss of R = student->n_rows logits rows, q = softmax(z / T),
+ * against the teacher's lists, and its gradient to the logits.
+ *   tail = 0: the list is normalised, p = softmax(logp), and the loss is
+ *     sum p (ln p - ln q) over it;
+ *   tail = 1: p = exp(logp) as given, and the teacher's remaining mass
+ *     r = max(0, 1 - sum p) is compared with the student's mass t outside the
+ *     list: the loss gets r (ln r - ln t).
+ * loss [R] (optional) is not weighted; grad (optional; the student's type, width
+ * and row count; may be the student's own memory) = weight[r] dloss[r] / dz, with
+ * weight [R] fp32 or NULL for 1. stats [R * 4] (optional, 16-byte aligned) is what
+ * tt_distill_grad takes for a gradient in a later call, when the weights are
+ * known then. status [R] is required. A row without any usable entry has loss
+ * and gradient 0 and EMPTY; one with a list column outside the row loses that
+ * entry and gets ID_OUT_OF_RANGE; one without a normaliser, or with a NaN or
+ * +inf in its list, has loss NaN, gradient 0 and NOT_FINITE (TIMEOUT if a wait
+ * inside the kernel gave up). A list column whose student logit is -inf makes
+ * the loss +inf. Sums are kept in fp32 or more, the gradient is rounded once.
+ * Rows of more than 1,638,400 bf16 or 819,200 fp32 columns are TT_ERR_UNSUPPORTED.
+ * Needs no workspace. */
+tt_status tt_distill(const tt_logits* student, const tt_teacher* teacher, float temp,
+                     int32_t tail, const float* weight, float* loss, float* stats,
+                     const tt_logits* grad, int32_t* status, void* stream);
+
+/* The gradient of tt_distill alone, from its stats and the same student,
+ * teacher, temp and tail. */
+tt_status tt_distill_grad(const tt_logits* student, const tt_teacher* teacher, float temp,
+                          int32_t tail, const float* weight, const float* stats,
+                          const tt_logits* grad, void* stream);
+
 /* Static text for a tt_status. */
 const char* tt_status_string(tt_status s);
 

@@ -73,12 +73,16 @@ class _LogprobsOut(ctypes.Structure):
                 ("top_logprobs", c_p), ("status", c_p)]
 
 
+class _Teacher(ctypes.Structure):
+    _fields_ = [("ids", c_p), ("logp", c_p), ("k", c_i32)]
+
+
 _lib = None
 EXPORTS = ("tt_workspace_bytes", "tt_workspace_bytes_for", "tt_align", "tt_transfer", "tt_verify", "tt_step",
            "tt_step_noalloc", "tt_status_string", "tt_last_cuda_error", "tt_version",
            "tt_vocab_index_bytes", "tt_vocab_index_build", "tt_encode_workspace_bytes",
            "tt_encode", "tt_consistency", "tt_dpos_hist", "tt_sharded_workspace_bytes",
-           "tt_verify_sharded", "tt_logprobs")
+           "tt_verify_sharded", "tt_logprobs", "tt_distill", "tt_distill_grad")
 TT_MAX_SHARDS = 8
 TT_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -145,6 +149,11 @@ def load(build_if_missing: bool = False):
     L.tt_dpos_hist.restype = c_i32
     L.tt_logprobs.argtypes = [P(_Logits), c_p, c_f32, c_i32, P(_LogprobsOut), c_p]
     L.tt_logprobs.restype = c_i32
+    L.tt_distill.argtypes = [P(_Logits), P(_Teacher), c_f32, c_i32, c_p, c_p, c_p, P(_Logits), c_p,
+                             c_p]
+    L.tt_distill.restype = c_i32
+    L.tt_distill_grad.argtypes = [P(_Logits), P(_Teacher), c_f32, c_i32, c_p, c_p, P(_Logits), c_p]
+    L.tt_distill_grad.restype = c_i32
     _lib = L
     return L
 
@@ -683,3 +692,84 @@ def tt_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, *, tem
                               int(top_n), ctypes.byref(c_out), _stream(stream))
     _check("tt_logprobs", code)
     return o
+
+
+def _teacher(ids: torch.Tensor, logp: torch.Tensor, R: int) -> _Teacher:
+    if ids.dim() != 2 or ids.shape != logp.shape or ids.shape[0] != R:
+        raise ValueError("teacher ids and logp must be [rows, k] of the student's rows")
+    return _Teacher(_given(ids, "teacher ids", torch.int32, 0),
+                    _given(logp, "teacher logp", torch.float32, 0), ids.shape[1])
+
+
+def _like_rows(logits: torch.Tensor) -> torch.Tensor:
+    """Rows like `logits`, each starting on 16 bytes."""
+    R, V = logits.shape
+    return torch.empty((R, (V + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :V]
+
+
+def tt_distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: torch.Tensor, *,
+               temp: float = 1.0, tail: bool = False, weight: Optional[torch.Tensor] = None,
+               grad=True, out=None, stream=None) -> dict:
+    """Loss [R] of student logits rows [R, V] (softmax(z / temp)) against a
+    teacher's top log probabilities (int32 and fp32 [R, k], as tt_logprobs gives
+    them), with ``tail`` the teacher's mass outside the list too; the gradient to
+    the logits, weight[r] times each row's (grad: True, False, or the tensor to
+    write, which may be the logits); stats for a later tt_distill_grad; status."""
+    L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, logits.shape[0])
+    R, dev = logits.shape[0], logits.device
+    o = dict(out or {})
+    _need(o, "loss", R, torch.float32, dev)
+    _need(o, "status", R, torch.int32, dev)
+    if "stats" not in o:
+        o["stats"] = torch.empty((R, 4), dtype=torch.float32, device=dev)
+    G = None
+    if grad is not False:
+        o["grad"] = _like_rows(logits) if grad is True else grad
+        G = _logits(o["grad"])
+    code = load().tt_distill(ctypes.byref(L), ctypes.byref(T), float(temp), int(bool(tail)),
+                             _given(weight, "weight", torch.float32, R), _ptr(o["loss"]),
+                             _ptr(o["stats"]), None if G is None else ctypes.byref(G),
+                             _ptr(o["status"]), _stream(stream))
+    _check("tt_distill", code)
+    return o
+
+
+def tt_distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: torch.Tensor,
+                    stats: torch.Tensor, *, temp: float = 1.0, tail: bool = False,
+                    weight: Optional[torch.Tensor] = None, grad: Optional[torch.Tensor] = None,
+                    stream=None) -> torch.Tensor:
+    """The gradient of tt_distill from its stats (same arguments otherwise)."""
+    L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, logits.shape[0])
+    g = _like_rows(logits) if grad is None else grad
+    G = _logits(g)
+    R = logits.shape[0]
+    code = load().tt_distill_grad(ctypes.byref(L), ctypes.byref(T), float(temp), int(bool(tail)),
+                                  _given(weight, "weight", torch.float32, R),
+                                  _given(stats, "stats", torch.float32, 4 * R), ctypes.byref(G),
+                                  _stream(stream))
+    _check("tt_distill_grad", code)
+    return g
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, teacher_ids, teacher_logp, temp, tail):
+        o = tt_distill(logits, teacher_ids, teacher_logp, temp=temp, tail=tail, grad=False)
+        ctx.save_for_backward(logits, teacher_ids, teacher_logp, o["stats"])
+        ctx.args = temp, tail
+        return o["loss"][:logits.shape[0]]
+
+    @staticmethod
+    def backward(ctx, up):
+        logits, ids, logp, stats = ctx.saved_tensors
+        temp, tail = ctx.args
+        g = tt_distill_grad(logits, ids, logp, stats, temp=temp, tail=tail,
+                            weight=up.float().contiguous())
+        return g, None, None, None, None
+
+
+def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: torch.Tensor, *,
+                 temp: float = 1.0, tail: bool = False) -> torch.Tensor:
+    """tt_distill as a differentiable loss per row [R]; gradients flow to the
+    logits only."""
+    return _DistillLoss.apply(logits, teacher_ids, teacher_logp, float(temp), bool(tail))

@@ -1,5 +1,6 @@
 // tt_ops.h -- arguments and launchers of the operators around a verification
-// step: log probabilities of logits rows (logprob.cu).
+// step: log probabilities of logits rows (logprob.cu), a student's loss against a
+// teacher's top log probabilities (distill.cu).
 #pragma once
 
 #include <cstdint>
@@ -29,5 +30,27 @@ struct LogprobArgs {
 
 cudaError_t launch_logprobs(const LogprobArgs& args, int dt, cudaStream_t stream, int sm_count);
 cudaError_t preload_logprobs();
+
+struct DistillArgs {
+  const char* data;  // student logits
+  int64_t stride_bytes;
+  int64_t rows;
+  int V, K, tail;
+  float temp, scale;  // T, log2(e) / T
+  const int32_t* ids;   // [rows * K]
+  const float* logp;    // [rows * K]
+  const float* weight;  // [rows] or NULL
+  float* loss;
+  float* stats;  // [rows * 4]: max z, sum of 2^((z - max) scale) over all columns and outside the list
+  int32_t* status;
+  char* grad;  // NULL: the forward call alone
+  int64_t grad_stride_bytes;
+  int split, share;  // CTAs per row and columns of each (filled in by the launcher)
+};
+
+int distill_max_cols(int dt);
+cudaError_t launch_distill(const DistillArgs& args, int dt, cudaStream_t stream);
+cudaError_t launch_distill_grad(const DistillArgs& args, int dt, cudaStream_t stream);
+cudaError_t preload_distill();
 
 }  // namespace tt
