@@ -81,7 +81,7 @@ typedef enum {
 #define TT_MAX_DPOS_BINS 4096    /* most bins of tt_dpos_hist */
 #define TT_MAX_HISTORY 3072      /* longest repetition-penalty history per request */
 
-typedef enum { TT_F32 = 0, TT_BF16 = 1 } tt_dtype;
+typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 /* tt_tree_attn only */ } tt_dtype;
 
 /* A token byte-string table: token id v spells bytes[offsets[v] .. offsets[v+1]). */
 typedef struct {
@@ -453,6 +453,70 @@ tt_status tt_distill(const tt_logits* student, const tt_teacher* teacher, float 
 tt_status tt_distill_grad(const tt_logits* student, const tt_teacher* teacher, float temp,
                           int32_t tail, const float* weight, const float* stats,
                           const tt_logits* grad, void* stream);
+
+#define TT_MAX_TREE 512 /* most drafted tokens of a request */
+
+/* Heads of tokens: element d of head h of token i is data[i * token_stride +
+ * h * head_stride + d]. data must be 16-byte aligned and the strides multiples of
+ * 8 elements. */
+typedef struct {
+  const void* data; /* device */
+  int64_t token_stride;
+  int64_t head_stride;
+} tt_heads;
+
+/* Pages of a cache: element d of head h in slot x of page p is data[p *
+ * page_stride + x * slot_stride + h * head_stride + d]; alignment as tt_heads. */
+typedef struct {
+  const void* data; /* device */
+  int64_t page_stride;
+  int64_t slot_stride;
+  int64_t head_stride;
+} tt_pages;
+
+/* Drafted tokens of B requests over their paged caches. Request b owns the nodes
+ * tree_off[b] .. tree_off[b+1]-1 of q, k and v: the tokens a target model scores
+ * at once, a chain or a tree of alternatives, whose keys and values are not in
+ * the cache yet. Slot x of its cache is slot x % page_size of page
+ * page_table[b * table_stride + x / page_size]. */
+typedef struct {
+  int32_t B;
+  int32_t n_nodes;    /* tokens of q, k, v; tree_off[B] */
+  int32_t max_nodes;  /* bound on a request's nodes (<= TT_MAX_TREE) */
+  int32_t dtype;      /* TT_BF16 or TT_F16: of q, k, v, the caches and the output */
+  int32_t n_q_heads;  /* a multiple of n_kv_heads, at most 128 times it */
+  int32_t n_kv_heads; /* query head h reads the keys of head h / (n_q_heads / n_kv_heads) */
+  int32_t head_dim;   /* 64 or 128 */
+  int32_t page_size;  /* slots of a page, a multiple of 16 */
+  const int32_t* tree_off; /* device, [B+1] */
+  const int32_t* parents;  /* device, [n_nodes] parent of a node within its request (less
+                              than the node's own number; -1: the cache's last token), or
+                              NULL for chains */
+  tt_heads q, k, v;
+  tt_pages k_cache, v_cache;
+  int64_t n_pages;            /* pages at k_cache and v_cache */
+  const int32_t* page_table;  /* device */
+  int64_t table_stride;       /* elements between its rows */
+  const int32_t* cache_len;   /* device, [B] slots in use */
+  int32_t max_len;            /* bound on cache_len; the table's rows hold its pages */
+  float scale;                /* of the scores, > 0 (commonly head_dim ** -0.5) */
+} tt_tree;
+
+/* Scratch bytes of tt_tree_attn for these sizes (0: none needed, or invalid sizes). */
+size_t tt_tree_workspace_bytes(const tt_tree* tree);
+
+/* Attention of every node over its request's cache, its ancestors and itself:
+ * out [n_nodes, n_q_heads, head_dim] (contiguous, 16-byte aligned) and lse
+ * [n_nodes, n_q_heads] (optional: natural log of the sum of exp(scale q.k)).
+ * Slots past cache_len are never used, whatever they hold, and other requests'
+ * nodes neither. Scores, statistics and sums are fp32; the softmax's weights are
+ * rounded to the inputs' type for their product with the values, the output once.
+ * status [B]: BAD_OFFSETS and TOO_LONG (more nodes than max_nodes, a length that
+ * is negative or above max_len) leave the request's outputs unwritten;
+ * ID_OUT_OF_RANGE reports a parent or a page out of range (the node then counts
+ * as a root, the page's slots are left out). Lengths of zero are fine. */
+tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_bytes, void* out,
+                       float* lse, int32_t* status, void* stream);
 
 /* Static text for a tt_status. */
 const char* tt_status_string(tt_status s);

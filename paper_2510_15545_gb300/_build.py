@@ -17,7 +17,7 @@ OUT_DIR = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libtt.so")
 SOURCES = ["api.cu", "align.cu", "rowpass.cu", "decide.cu", "noalloc.cu", "encode.cu", "shard.cu",
            "filter.cu", "nucleus.cu", "nucrow.cu", "pen.cu", "ops.cu", "logprob.cu",
-           "distill.cu"]
+           "distill.cu", "tree.cu"]
 HEADERS = ["tt_device.cuh", "tt_launch.h", "tt_shard.h", "tt_f2.cuh",
            "tt_ring.cuh", "tt_ops.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

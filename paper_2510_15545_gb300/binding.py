@@ -23,7 +23,8 @@ TT_REQ_ID_OUT_OF_RANGE, TT_REQ_TOO_LONG, TT_REQ_EMPTY, TT_REQ_BAD_OFFSETS, TT_RE
     1, 2, 4, 8, 16)
 TT_REQ_NO_MATCH, TT_REQ_INCONSISTENT = 128, 256
 TT_MAX_ENCODE_BYTES, TT_MAX_DPOS_BINS = 2048, 4096
-TT_F32, TT_BF16 = 0, 1
+TT_F32, TT_BF16, TT_F16 = 0, 1, 2
+TT_MAX_TOP_K, TT_MAX_DISTILL_K, TT_MAX_TREE = 32, 128, 512
 TT_MAX_K, TT_MAX_M, TT_MAX_TOKEN_BYTES = 256, 512, 256
 
 
@@ -77,12 +78,31 @@ class _Teacher(ctypes.Structure):
     _fields_ = [("ids", c_p), ("logp", c_p), ("k", c_i32)]
 
 
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", c_p), ("token_stride", c_i64), ("head_stride", c_i64)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("data", c_p), ("page_stride", c_i64), ("slot_stride", c_i64),
+                ("head_stride", c_i64)]
+
+
+class _Tree(ctypes.Structure):
+    _fields_ = [("B", c_i32), ("n_nodes", c_i32), ("max_nodes", c_i32), ("dtype", c_i32),
+                ("n_q_heads", c_i32), ("n_kv_heads", c_i32), ("head_dim", c_i32),
+                ("page_size", c_i32), ("tree_off", c_p), ("parents", c_p), ("q", _Heads),
+                ("k", _Heads), ("v", _Heads), ("k_cache", _Pages), ("v_cache", _Pages),
+                ("n_pages", c_i64), ("page_table", c_p), ("table_stride", c_i64),
+                ("cache_len", c_p), ("max_len", c_i32), ("scale", c_f32)]
+
+
 _lib = None
 EXPORTS = ("tt_workspace_bytes", "tt_workspace_bytes_for", "tt_align", "tt_transfer", "tt_verify", "tt_step",
            "tt_step_noalloc", "tt_status_string", "tt_last_cuda_error", "tt_version",
            "tt_vocab_index_bytes", "tt_vocab_index_build", "tt_encode_workspace_bytes",
            "tt_encode", "tt_consistency", "tt_dpos_hist", "tt_sharded_workspace_bytes",
-           "tt_verify_sharded", "tt_logprobs", "tt_distill", "tt_distill_grad")
+           "tt_verify_sharded", "tt_logprobs", "tt_distill", "tt_distill_grad",
+           "tt_tree_workspace_bytes", "tt_tree_attn")
 TT_MAX_SHARDS = 8
 TT_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -154,6 +174,10 @@ def load(build_if_missing: bool = False):
     L.tt_distill.restype = c_i32
     L.tt_distill_grad.argtypes = [P(_Logits), P(_Teacher), c_f32, c_i32, c_p, c_p, P(_Logits), c_p]
     L.tt_distill_grad.restype = c_i32
+    L.tt_tree_workspace_bytes.argtypes = [P(_Tree)]
+    L.tt_tree_workspace_bytes.restype = ctypes.c_size_t
+    L.tt_tree_attn.argtypes = [P(_Tree), c_p, ctypes.c_size_t, c_p, c_p, c_p, c_p]
+    L.tt_tree_attn.restype = c_i32
     _lib = L
     return L
 
@@ -773,3 +797,87 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: 
     """tt_distill as a differentiable loss per row [R]; gradients flow to the
     logits only."""
     return _DistillLoss.apply(logits, teacher_ids, teacher_logp, float(temp), bool(tail))
+
+
+_TREE_DTYPES = {torch.bfloat16: TT_BF16, torch.float16: TT_F16}
+
+
+def _heads(t: torch.Tensor, name: str, like: torch.Tensor, dims: int):
+    """Strides of a tensor [..., heads, head_dim] of the queries' type."""
+    if t.dim() != dims or t.dtype != like.dtype or t.shape[-1] != like.shape[-1]:
+        raise ValueError("%s must be a %d-D %s tensor of the queries' head size"
+                         % (name, dims, str(like.dtype).replace("torch.", "")))
+    if t.stride(-1) != 1:
+        raise ValueError("%s must have unit stride within a head" % name)
+    return t.data_ptr(), *t.stride()[:-1]
+
+
+def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
+          max_nodes) -> _Tree:
+    if q.dtype not in _TREE_DTYPES:
+        raise TypeError("queries must be bfloat16 or float16")
+    B, (N, Hq, D) = cache_len.numel(), q.shape
+    if k.shape != v.shape or k.shape[0] != N or k_cache.shape != v_cache.shape \
+            or k_cache.shape[2] != k.shape[1]:
+        raise ValueError("keys and values must be of the same tokens, pages and heads")
+    if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.shape[0] != B \
+            or (page_table.numel() and page_table.stride(1) != 1):
+        raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
+    pages, page, _, _ = k_cache.shape
+    room = page_table.shape[1] * page
+    max_len = room if max_len is None else int(max_len)
+    if max_len > room:
+        raise ValueError("max_len is more than the page table's rows hold")
+    return _Tree(B, N, min(TT_MAX_TREE, max(N, 1)) if max_nodes is None else int(max_nodes),
+                 _TREE_DTYPES[q.dtype], Hq, k.shape[1], D, page,
+                 _given(tree_off, "tree_off", torch.int32, B + 1),
+                 _given(parents, "parents", torch.int32, N), _Heads(*_heads(q, "q", q, 3)),
+                 _Heads(*_heads(k, "k", q, 3)), _Heads(*_heads(v, "v", q, 3)),
+                 _Pages(*_heads(k_cache, "k_cache", q, 4)),
+                 _Pages(*_heads(v_cache, "v_cache", q, 4)), pages, _ptr(page_table),
+                 max(page_table.stride(0), page_table.shape[1]),
+                 _given(cache_len, "cache_len", torch.int32, B), max_len,
+                 float(D ** -0.5 if scale is None else scale))
+
+
+def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
+                 v_cache: torch.Tensor, page_table: torch.Tensor, cache_len: torch.Tensor,
+                 tree_off: torch.Tensor, parents: Optional[torch.Tensor] = None, *,
+                 scale: Optional[float] = None, max_len: Optional[int] = None,
+                 max_nodes: Optional[int] = None, ws: Optional[torch.Tensor] = None, out=None,
+                 stream=None) -> dict:
+    """Attention of the drafted tokens q [N, q heads, head_dim] of B requests
+    (nodes tree_off[b] .. tree_off[b+1]-1, k and v [N, kv heads, head_dim] their own
+    keys and values, parents [N] numbered within the request, None for chains) over
+    the requests' paged caches k_cache, v_cache [pages, page_size, kv heads,
+    head_dim] (any strides with unit innermost), page_table int32 [B, pages per
+    request], cache_len int32 [B]. Returns out [N, q heads, head_dim], lse
+    [N, q heads] and status [B]. max_len and max_nodes bound the lengths and the
+    nodes of a request and size the launch (default: what the table and N allow)."""
+    T = _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
+              max_nodes)
+    dev, L = q.device, load()
+    o = dict(out or {})
+    if "out" not in o:
+        o["out"] = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if "lse" not in o:
+        o["lse"] = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
+    _need(o, "status", T.B, torch.int32, dev)
+    if ws is None:
+        n = int(L.tt_tree_workspace_bytes(ctypes.byref(T)))
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
+    code = L.tt_tree_attn(ctypes.byref(T), _ptr(ws), 0 if ws is None else ws.numel(),
+                          _given(o["out"], "out", q.dtype, q.numel()),
+                          _given(o["lse"], "lse", torch.float32, q.shape[0] * q.shape[1]),
+                          _ptr(o["status"]), _stream(stream))
+    _check("tt_tree_attn", code)
+    return o
+
+
+def tt_tree_workspace(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents=None, *,
+                      max_len=None, max_nodes=None) -> torch.Tensor:
+    """Scratch that tt_tree_attn calls of these sizes can share, one at a time."""
+    T = _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, None, max_len,
+              max_nodes)
+    return torch.empty(max(int(load().tt_tree_workspace_bytes(ctypes.byref(T))), 256),
+                       dtype=torch.uint8, device=q.device)

@@ -45,6 +45,7 @@ cudaError_t ensure_loaded() {
   if ((e = preload_shard()) != cudaSuccess) return e;
   if ((e = preload_logprobs()) != cudaSuccess) return e;
   if ((e = preload_distill()) != cudaSuccess) return e;
+  if ((e = preload_tree()) != cudaSuccess) return e;
   if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
   return cudaSuccess;
 }

@@ -50,6 +50,65 @@ bool distill_ok(const tt_logits* student, const tt_teacher* teacher, float temp,
          teacher->k <= TT_MAX_DISTILL_K && temp_ok(temp) && (tail == 0 || tail == 1);
 }
 
+bool aligned16(const void* p) { return p && (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0; }
+bool heads_ok(const tt_heads& h) {
+  return aligned16(h.data) && stride_ok(h.token_stride) && stride_ok(h.head_stride);
+}
+bool pages_ok(const tt_pages& p) {
+  return aligned16(p.data) && stride_ok(p.page_stride) && stride_ok(p.slot_stride) &&
+         stride_ok(p.head_stride);
+}
+
+// The sizes of a tree call, on which its workspace depends.
+bool tree_sizes_ok(const tt_tree* t) {
+  if (!t || t->B < 0 || t->n_nodes < 0 || t->max_nodes < 1 || t->max_nodes > TT_MAX_TREE)
+    return false;
+  if (t->n_kv_heads < 1 || t->n_q_heads < 1 || t->n_q_heads % t->n_kv_heads != 0 ||
+      t->n_q_heads / t->n_kv_heads > 128)
+    return false;
+  return (t->head_dim == 64 || t->head_dim == 128) && t->page_size >= 16 &&
+         t->page_size % 16 == 0 && t->max_len >= 0;
+}
+
+TreeArgs tree_args(const tt_tree* t) {
+  TreeArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.B = t->B;
+  a.n_nodes = t->n_nodes;
+  a.max_nodes = t->max_nodes;
+  a.Hq = t->n_q_heads;
+  a.Hkv = t->n_kv_heads;
+  a.D = t->head_dim;
+  a.tree_off = t->tree_off;
+  a.parents = t->parents;
+  a.q = static_cast<const char*>(t->q.data);
+  a.q_token = t->q.token_stride;
+  a.q_head = t->q.head_stride;
+  a.k = static_cast<const char*>(t->k.data);
+  a.k_token = t->k.token_stride;
+  a.k_head = t->k.head_stride;
+  a.v = static_cast<const char*>(t->v.data);
+  a.v_token = t->v.token_stride;
+  a.v_head = t->v.head_stride;
+  a.kc = static_cast<const char*>(t->k_cache.data);
+  a.kc_page = t->k_cache.page_stride;
+  a.kc_slot = t->k_cache.slot_stride;
+  a.kc_head = t->k_cache.head_stride;
+  a.vc = static_cast<const char*>(t->v_cache.data);
+  a.vc_page = t->v_cache.page_stride;
+  a.vc_slot = t->v_cache.slot_stride;
+  a.vc_head = t->v_cache.head_stride;
+  a.n_pages = t->n_pages;
+  a.page_size = t->page_size;
+  a.page_table = t->page_table;
+  a.table_stride = t->table_stride;
+  a.cache_len = t->cache_len;
+  a.max_len = t->max_len;
+  a.scale = t->scale;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -109,6 +168,41 @@ tt_status tt_distill_grad(const tt_logits* student, const tt_teacher* teacher, f
   cudaError_t e = load_kernels();
   if (e == cudaSuccess)
     e = launch_distill_grad(a, student->dtype, static_cast<cudaStream_t>(stream));
+  return e == cudaSuccess ? TT_OK : record_cuda_error(e);
+}
+
+size_t tt_tree_workspace_bytes(const tt_tree* tree) {
+  return tree_sizes_ok(tree) ? tree_workspace_bytes(tree_args(tree), device_sms()) : 0;
+}
+
+tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_bytes, void* out,
+                       float* lse, int32_t* status, void* stream) {
+  if (!tree_sizes_ok(tree)) return TT_ERR_INVALID_ARG;
+  if (tree->dtype != TT_BF16 && tree->dtype != TT_F16) return TT_ERR_INVALID_ARG;
+  if (!(tree->scale > 0.f) || !std::isfinite(tree->scale)) return TT_ERR_INVALID_ARG;
+  if (tree->B == 0) return TT_OK;
+  if (!tree->tree_off || !tree->cache_len || !status) return TT_ERR_INVALID_ARG;
+  if (tree->n_nodes > 0 && (!heads_ok(tree->q) || !heads_ok(tree->k) || !heads_ok(tree->v) ||
+                            !aligned16(out)))
+    return TT_ERR_INVALID_ARG;
+  const int64_t pages = (int64_t(tree->max_len) + tree->page_size - 1) / tree->page_size;
+  if (tree->max_len > 0 &&
+      (!pages_ok(tree->k_cache) || !pages_ok(tree->v_cache) || tree->n_pages < 1 ||
+       tree->n_pages > INT32_MAX || !tree->page_table || tree->table_stride < pages))
+    return TT_ERR_INVALID_ARG;
+  TreeArgs a = tree_args(tree);
+  const size_t need = tree_workspace_bytes(a, device_sms());
+  if (need > 0 && (!workspace || workspace_bytes < need ||
+                   (reinterpret_cast<uintptr_t>(workspace) & 255) != 0))
+    return TT_ERR_INVALID_ARG;
+  if (tree->B > 65535) return TT_ERR_UNSUPPORTED;
+  a.ws = static_cast<char*>(workspace);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.status = status;
+  cudaError_t e = load_kernels();
+  if (e == cudaSuccess)
+    e = launch_tree(a, tree->dtype, static_cast<cudaStream_t>(stream), device_sms());
   return e == cudaSuccess ? TT_OK : record_cuda_error(e);
 }
 

@@ -1,6 +1,7 @@
 // tt_ops.h -- arguments and launchers of the operators around a verification
 // step: log probabilities of logits rows (logprob.cu), a student's loss against a
-// teacher's top log probabilities (distill.cu).
+// teacher's top log probabilities (distill.cu), attention of drafted tokens over a
+// paged cache (tree.cu).
 #pragma once
 
 #include <cstdint>
@@ -52,5 +53,30 @@ int distill_max_cols(int dt);
 cudaError_t launch_distill(const DistillArgs& args, int dt, cudaStream_t stream);
 cudaError_t launch_distill_grad(const DistillArgs& args, int dt, cudaStream_t stream);
 cudaError_t preload_distill();
+
+struct TreeArgs {
+  int B, n_nodes, max_nodes, Hq, Hkv, D;
+  const int32_t* tree_off;
+  const int32_t* parents;  // NULL: chains
+  const char *q, *k, *v;   // strides below in elements
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+  const char *kc, *vc;
+  int64_t kc_page, kc_slot, kc_head, vc_page, vc_slot, vc_head;
+  int64_t n_pages;
+  int page_size;
+  const int32_t* page_table;
+  int64_t table_stride;
+  const int32_t* cache_len;
+  int max_len;
+  float scale;
+  char* ws;
+  char* out;
+  float* lse;
+  int32_t* status;
+};
+
+size_t tree_workspace_bytes(const TreeArgs& args, int sm_count);
+cudaError_t launch_tree(const TreeArgs& args, int dt, cudaStream_t stream, int sm_count);
+cudaError_t preload_tree();
 
 }  // namespace tt
