@@ -68,7 +68,8 @@ bool tree_sizes_ok(const tt_tree* t) {
       t->n_q_heads / t->n_kv_heads > 128)
     return false;
   return (t->head_dim == 64 || t->head_dim == 128) && t->page_size >= 16 &&
-         t->page_size % 16 == 0 && t->max_len >= 0;
+         t->page_size % 16 == 0 && t->page_size <= 1 << 20 && t->max_len >= 0 &&
+         t->max_len <= 1 << 30;
 }
 
 TreeArgs tree_args(const tt_tree* t) {

@@ -5,19 +5,65 @@
 // i, parent(i), parent(parent(i)), ... and nothing else; its output in a head is
 // sum_x softmax_x(scale q.k_x) v_x over them, held in the running form: with
 // m = max s_x and l = sum 2^(s_x - m), a larger m scales what was summed before.
+//
+// The bound is the cache: each key and value is read once for all tokens and all
+// query heads that share its head, G = Hq / Hkv. Their products are matrix
+// products: 128 rows (token, head of the group) against tiles of 128 keys. A CTA
+// takes the rows of one request and key head (more than 128: several CTAs read
+// the tiles through L2) over a run of tiles, the request's cache first, then its
+// own drafted tokens, on which each row's ancestors are a bit mask. One warp
+// copies tiles in (a page at a time), one issues the two products per tile, and
+// four hold one row per thread: scores come from tensor memory, the weights go
+// back over them in the inputs' type as the second product's operand. Two CTAs
+// share an SM, so that one's softmax runs beside the other's products and copies.
+// Long caches are split into runs, whose results a second kernel joins.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <atomic>
 #include <cstdint>
+#include <cstring>
+#include <numeric>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include "tt_device.cuh"
+#include "tt_f2.cuh"
 #include "tt_ops.h"
+#include "tt_ring.cuh"
+#include "tt_umma.cuh"
 
 namespace tt {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kTile = 128;               // keys of a tile, rows of a CTA
+constexpr int kRowWarps = 4;
+constexpr int kThreads = (kRowWarps + 2) * 32;
+constexpr int kTmemColumns = 256;        // scores and weights: 128, output: up to 128
+constexpr int kWords = TT_MAX_TREE / 32;
+constexpr int kOut = 128;                // tensor memory column of the output
+constexpr float kLn2 = 0.693147180559945f;
+// A row's reference maximum follows its maximum once that is 2^kSlack above it:
+// weights stay below 2^(kSlack + offset), and the output is scaled rarely.
+constexpr float kSlack = 8.f;
+
+struct TreeKernelArgs {
+  CUtensorMap q, k, v, kc, vc;
+  TreeArgs a;
+  float scale2;       // scale * log2(e)
+  int group;          // G
+  int per_tile;       // tokens of a 128-row tile
+  int row_tiles;      // CTAs of a request's rows, at most
+  int run;            // tiles of a run, at most
+  int runs;           // runs of a request, at most
+  int box;            // slots of one copy: they lie within a page
+  int slots_inner;    // the cache maps' second dimension is the slot, the third the head
+  float* part;        // [runs * n_nodes * Hq * D] outputs of runs, not normalised
+  float2* part_ml;    // [runs * n_nodes * Hq] their reference maximum (log2) and sum
+};
 
 // A request's usable range: its nodes and cache length, or why it has none.
 struct Request {
@@ -38,102 +84,608 @@ __device__ __forceinline__ Request request(const TreeArgs& a, int b) {
   return r;
 }
 
-// Whether every parent and page of the request is in range.
-__device__ int check_request(const TreeArgs& a, int b, const Request& r) {
+// The tiles that the rows of tokens first .. end - 1 see: the cache's, then
+// those of drafted tokens up to end - 1; and the runs they are cut into.
+__host__ __device__ inline int cache_tiles(int len) { return len / kTile + (len % kTile != 0); }
+__host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / kTile; }
+__host__ __device__ inline int run_count(int tiles, int run) { return (tiles + run - 1) / run; }
+
+// Whether every parent and page of the request is in range (threads 0 .. 127).
+__device__ bool out_of_range(const TreeArgs& a, int b, const Request& r, int t) {
   bool bad = false;
   if (a.parents)
-    for (int i = threadIdx.x; i < r.nodes; i += blockDim.x) {
+    for (int i = t; i < r.nodes; i += kTile) {
       const int p = a.parents[r.first + i];
       bad |= p < -1 || p >= i;
     }
-  for (int x = threadIdx.x; int64_t(x) * a.page_size < r.len; x += blockDim.x) {
+  const int pages = r.len / a.page_size + (r.len % a.page_size != 0);
+  for (int x = t; x < pages; x += kTile) {
     const int p = a.page_table[b * a.table_stride + x];
     bad |= p < 0 || p >= a.n_pages;
   }
-  return __syncthreads_or(bad) ? TT_REQ_ID_OUT_OF_RANGE : 0;
+  return bad;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) tree_kernel(const __grid_constant__ TreeArgs a) {
-  __shared__ uint32_t seen[TT_MAX_TREE / 32];
-  const int i = blockIdx.x, b = blockIdx.y, t = threadIdx.x, lane = t & 31;
+template <int D>
+struct Smem {
+  static constexpr int kStages = D == 128 ? 1 : 2;  // two CTAs of an SM fit
+  char q[kTile * D * 2];
+  char k[kStages][kTile * D * 2];
+  char v[kStages][kTile * D * 2];
+  uint32_t seen[kTile][kWords];  // a token's ancestors and itself
+  int16_t up[TT_MAX_TREE];       // parents, -1 for roots
+  uint32_t odd[kWords];          // drafted tokens with a value that is not finite
+  uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t s_full, p_full, o_full;
+  uint32_t tmem;
+  int failed;
+};
+
+template <bool F16>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  uint32_t r;
+  if constexpr (F16)
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  else
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+template <bool F16>
+__device__ __forceinline__ float unpack(uint16_t x) {
+  if constexpr (F16)
+    return __half2float(__ushort_as_half(x));
+  else
+    return bf16_to_f32(x);
+}
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(kThreads, 2)
+    tree_kernel(const __grid_constant__ TreeKernelArgs p) {
+  using S = Smem<D>;
+  constexpr int kHalves = D / 64;              // 128-byte column blocks of a tile
+  constexpr int kBlock = kTile * 128;          // their distance in bytes
+  constexpr float kOffset = F16 ? 7.f : 0.f;   // fp16 weights: away from its small end
+  extern __shared__ char raw[];
+  S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+  const TreeArgs& a = p.a;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  int x = blockIdx.x;
+  const int mt = x % p.row_tiles;
+  x /= p.row_tiles;
+  const int hk = x % a.Hkv;
+  x /= a.Hkv;
+  const int run = x % p.runs, b = x / p.runs;
+  grid_launch_dependents();
   const Request r = request(a, b);
-  if (i == 0) {
-    const int bad = r.status ? r.status : check_request(a, b, r);
-    if (t == 0) a.status[b] = bad;
+  const int node0 = mt * p.per_tile, node1 = min(r.nodes, node0 + p.per_tile);
+  const int rows = max(0, node1 - node0) * p.group;
+  const int n_cache = cache_tiles(r.len);
+  const int tiles = rows > 0 ? n_cache + tree_tiles(node1) : 0;
+  const int runs = run_count(tiles, p.run);
+  const bool reports = run == 0 && hk == 0 && mt == 0;
+  if (run >= runs) {  // nothing here, but perhaps the request's status
+    if (reports) {
+      const bool bad = !r.status && t < kTile && out_of_range(a, b, r, t);
+      const int any = __syncthreads_or(bad);
+      if (t == 0) a.status[b] = r.status | (any ? TT_REQ_ID_OUT_OF_RANGE : 0);
+    }
+    return;
   }
-  if (i >= r.nodes) return;
-  if (t < TT_MAX_TREE / 32) seen[t] = 0;
-  __syncthreads();
+  const int tile0 = int(int64_t(run) * tiles / runs), tile1 = int(int64_t(run + 1) * tiles / runs);
+  const uint64_t limit = kWaitLimitNs;
+
   if (t == 0) {
-    for (int j = i;;) {
-      seen[j >> 5] |= 1u << (j & 31);
-      const int p = a.parents ? a.parents[r.first + j] : j - 1;
-      if (p < 0 || p >= j) break;
-      j = p;
+    mbar_init(&s.q_full, 1);
+    for (int i = 0; i < S::kStages; ++i) {
+      mbar_init(&s.k_full[i], 1);
+      mbar_init(&s.k_empty[i], 1);
+      mbar_init(&s.v_full[i], 1);
+      mbar_init(&s.v_empty[i], 1);
+    }
+    mbar_init(&s.s_full, 1);
+    mbar_init(&s.p_full, kRowWarps * 32);
+    mbar_init(&s.o_full, 1);
+    s.failed = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kRowWarps + 1) tmem_alloc(&s.tmem, kTmemColumns);
+  const bool has_tree = tile1 > n_cache;
+  if (has_tree) {
+    if (t < kWords) s.odd[t] = 0;
+    for (int i = t; i < node1; i += kThreads) {
+      const int up = a.parents ? a.parents[r.first + i] : i - 1;
+      s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
     }
   }
+  tc_fence_before();
   __syncthreads();
-  const int G = a.Hq / a.Hkv;
-  const float scale = a.scale * 1.4426950408889634f;
-  const int64_t node = int64_t(r.first) + i;
-  for (int h = t >> 5; h < a.Hq; h += kThreads / 32) {
-    const int hk = h / G;
-    const T* q = reinterpret_cast<const T*>(a.q) + node * a.q_token + h * a.q_head;
-    float qf[4], acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < 4; ++c) qf[c] = c * 32 < a.D ? float(q[c * 32 + lane]) * scale : 0.f;
-    float m = -INFINITY, l = 0.f;
-    auto take = [&](const T* k, const T* v) {
-      float s = 0.f;
-      for (int c = 0; c * 32 < a.D; ++c) s = fmaf(qf[c], float(k[c * 32 + lane]), s);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      const float top = fmaxf(m, s);
-      if (top == -INFINITY && s == s) return;
-      const float f = ex2_approx(m - top), e = ex2_approx(s - top);
-      m = top;
-      l = fmaf(l, f, e);
-      for (int c = 0; c * 32 < a.D; ++c) acc[c] = fmaf(acc[c], f, e * float(v[c * 32 + lane]));
+  tc_fence_after();
+  const uint32_t tmem = s.tmem;
+  bool ok = true;
+
+  if (warp == kRowWarps) {
+    // ------------------------------------------------------------ copies
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&s.q_full, kHalves * p.per_tile * p.group * 128);
+      for (int h = 0; h < kHalves; ++h)
+        tma_load_3d(smem_u32(s.q) + h * kBlock, &p.q, smem_u32(&s.q_full), 64 * h, hk * p.group,
+                    r.first + node0);
+    }
+    // lane i copies the tile's i-th box of slots
+    const int per = kTile / p.box;
+    auto page_of = [&](int tile) {
+      const int slot = tile * kTile + lane * p.box;
+      return tile < min(tile1, n_cache) && lane < per && slot < r.len
+                 ? a.page_table[b * a.table_stride + slot / a.page_size]
+                 : -1;
     };
-    for (int x0 = 0; x0 < r.len; x0 += a.page_size) {
-      const int page = a.page_table[b * a.table_stride + x0 / a.page_size];
-      if (page < 0 || page >= a.n_pages) continue;
-      const T* k = reinterpret_cast<const T*>(a.kc) + page * a.kc_page + hk * a.kc_head;
-      const T* v = reinterpret_cast<const T*>(a.vc) + page * a.vc_page + hk * a.vc_head;
-      for (int x = 0; x < a.page_size && x0 + x < r.len; ++x)
-        take(k + x * a.kc_slot, v + x * a.vc_slot);
+    int page = page_of(tile0);
+    for (int j = tile0; j < tile1 && ok; ++j) {
+      const int it = j - tile0, st = it % S::kStages;
+      const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
+      const int next = page_of(j + 1);
+      const bool cache = j < n_cache;
+      bool mine;
+      int bytes, at;
+      if (cache) {
+        mine = page >= 0 && page < a.n_pages;
+        bytes = p.box * 128;
+        at = lane * p.box;
+      } else {
+        at = lane * 16;
+        mine = lane < kTile / 16 && (j - n_cache) * kTile + at < node1;
+        bytes = 16 * 128;
+      }
+      const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
+      auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* paged, const CUtensorMap* own) {
+        if (lane == 0) mbar_arrive_expect_tx(bar, boxes * bytes * kHalves);
+        __syncwarp();
+        if (!mine) return;
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h) {
+          const uint32_t to = smem_u32(dst) + h * kBlock + at * 128;
+          if (cache) {
+            const int slot = (j * kTile + at) % a.page_size;
+            tma_load_4d(to, paged, smem_u32(bar), 64 * h, p.slots_inner ? slot : hk,
+                        p.slots_inner ? hk : slot, page);
+          } else {
+            tma_load_3d(to, own, smem_u32(bar), 64 * h, hk, r.first + (j - n_cache) * kTile + at);
+          }
+        }
+      };
+      ok = mbar_wait(&s.k_empty[st], parity, limit);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
+      ok = mbar_wait(&s.v_empty[st], parity, limit);
+      if (!__all_sync(0xffffffffu, ok)) break;
+      copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
+      page = next;
     }
-    for (int j = 0; j <= i; ++j) {
-      if (!(seen[j >> 5] >> (j & 31) & 1)) continue;
-      const int64_t n = int64_t(r.first) + j;
-      take(reinterpret_cast<const T*>(a.k) + n * a.k_token + hk * a.k_head,
-           reinterpret_cast<const T*>(a.v) + n * a.v_token + hk * a.v_head);
+  } else if (warp == kRowWarps + 1) {
+    // ---------------------------------------------------------- products
+    if (lane == 0) {
+      const uint32_t idesc_o = umma_idesc(F16, D, true);
+      ok = mbar_wait(&s.q_full, 0, limit);
+      for (int j = tile0; j < tile1 && ok; ++j) {
+        const int it = j - tile0, st = it % S::kStages;
+        const uint32_t parity = (it / S::kStages) & 1;
+        // keys of the tile in use, up to a multiple of 32
+        const int left = j < n_cache ? r.len - j * kTile : node1 - (j - n_cache) * kTile;
+        const int n = min(kTile, (left + 31) & ~31);
+        ok = mbar_wait(&s.k_full[st], parity, limit);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t idesc_s = umma_idesc(F16, n, false);
+        const uint32_t qa = smem_u32(s.q), ka = smem_u32(s.k[st]), va = smem_u32(s.v[st]);
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          const uint32_t at = (c / 4) * kBlock + (c % 4) * 32;
+          umma_ss(tmem, umma_desc(qa + at, 16), umma_desc(ka + at, 16), idesc_s, c > 0);
+        }
+        umma_commit(&s.s_full);
+        umma_commit(&s.k_empty[st]);
+        ok = mbar_wait(&s.v_full[st], parity, limit) && mbar_wait(&s.p_full, it & 1, limit);
+        if (!ok) break;
+        tc_fence_after();
+        for (int c = 0; c < n / 16; ++c)
+          umma_ts(tmem + kOut, tmem + 8 * c, umma_desc(va + c * 2048, kBlock), idesc_o,
+                  it > 0 || c > 0);
+        umma_commit(&s.v_empty[st]);
+      }
+      if (ok) umma_commit(&s.o_full);
     }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-    T* out = reinterpret_cast<T*>(a.out) + (node * a.Hq + h) * a.D;
-    for (int c = 0; c * 32 < a.D; ++c) out[c * 32 + lane] = T(acc[c] * inv);
-    if (a.lse && lane == 0)
-      a.lse[node * a.Hq + h] = l > 0.f || l != l ? 0.693147180559945f * m + logf(l) : -INFINITY;
+  } else {
+    // -------------------------------------------------------------- rows
+    const uint32_t mine = tmem + (uint32_t(warp * 32) << 16);  // this warp's lanes
+    const bool some = warp * 32 < rows;                        // (others only keep step)
+    const int local = t / p.group;                             // token of the row's tile
+    if (has_tree) {
+      // a token's ancestors: one thread walks up from each token
+      if (t < node1 - node0) {
+        const int w1 = tree_tiles(node1) * (kTile / 32);
+        for (int w = 0; w < w1; ++w) s.seen[t][w] = 0;
+        for (int i = node0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+    }
+    const int per = kTile / p.box;
+    auto box_ok = [&](int tile) {  // whether box `lane` of a cache tile is in range
+      const int slot = tile * kTile + lane * p.box;
+      if (tile >= min(tile1, n_cache) || lane >= per || slot >= r.len) return true;
+      const int page = a.page_table[b * a.table_stride + slot / a.page_size];
+      return page >= 0 && page < a.n_pages;
+    };
+    bool good = box_ok(tile0);
+    float m = -INFINITY, l = 0.f;  // the reference maximum (of scores) and the sum
+    for (int j = tile0; j < tile1; ++j) {
+      const int it = j - tile0, st = it % S::kStages;
+      const uint32_t parity = (it / S::kStages) & 1;
+      const bool cache = j < n_cache;
+      const int base = (j - n_cache) * kTile;  // first drafted token of a tree tile
+      const int left = cache ? r.len - j * kTile : node1 - base;
+      const int n = min(kTile, (left + 31) & ~31);
+      const uint32_t bad_boxes = ~__ballot_sync(0xffffffffu, good);
+      good = box_ok(j + 1);
+      // which of 32 keys from c on the row sees; `there`: which hold anything
+      auto there = [&](int c) {
+        uint32_t w = left - c >= 32 ? 0xffffffffu : (1u << max(0, left - c)) - 1;
+        if (bad_boxes)
+          for (int i = 0; i < 32; i += 16)
+            if (bad_boxes >> ((c + i) / p.box) & 1) w &= ~(0xffffu << i);
+        return w;
+      };
+      auto sees = [&](int c) {
+        return cache ? there(c) : local < node1 - node0 ? s.seen[local][(base + c) >> 5] : 0u;
+      };
+      // (the warp goes on, or gives up, as one)
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
+      tc_fence_after();
+      if (some) {
+        uint32_t v[32];
+        float top = -INFINITY;
+        for (int c = 0; c < n; c += 32) {
+          tmem_ld32(mine + c, v);
+          tmem_wait_ld(v);
+          const uint32_t w = sees(c);
+          if (w == 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+          } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (w >> i & 1) top = fmaxf(top, __uint_as_float(v[i]));
+          }
+          __syncwarp();
+        }
+        // the reference follows the maximum, and with it the sums
+        const bool raise = (top - m) * p.scale2 > kSlack || (m == -INFINITY && top > -INFINITY);
+        if (__any_sync(0xffffffffu, raise)) {
+          const float to = fmaxf(m, top);
+          const float f = m == -INFINITY ? 0.f : ex2_approx((m - to) * p.scale2);
+          m = to;
+          l *= f;
+          if (it > 0) {
+#pragma unroll
+            for (int c = 0; c < D; c += 32) {
+              tmem_ld32(mine + kOut + c, v);
+              tmem_wait_ld(v);
+#pragma unroll
+              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+              tmem_st32(mine + kOut + c, v);
+            }
+          }
+        }
+        const float shift = (m == -INFINITY ? 0.f : -m * p.scale2) + kOffset;
+        for (int c = 0; c < n; c += 32) {
+          tmem_ld32(mine + c, v);
+          tmem_wait_ld(v);
+          const uint32_t w = sees(c);
+          if (w != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+              if (!(w >> i & 1)) v[i] = 0xff800000u;
+          }
+          __syncwarp();
+          uint32_t o[16];
+          float l0 = 0.f, l1 = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const float e0 = ex2_approx(fmaf(__uint_as_float(v[2 * i]), p.scale2, shift));
+            const float e1 = ex2_approx(fmaf(__uint_as_float(v[2 * i + 1]), p.scale2, shift));
+            l0 += e0;
+            l1 += e1;
+            o[i] = pack2<F16>(e0, e1);
+          }
+          l += l0 + l1;
+          tmem_st16(mine + c / 2, o);
+        }
+        tmem_wait_st();
+      }
+      // Values that no row may touch: slots past the end (0 times what is there
+      // could be NaN), and of drafted tokens, what is not finite: a token outside
+      // its branch would get NaN from it. (Its own branch gets it at the end.)
+      uint32_t gaps = 0;
+      for (int c = 0; c < n; c += 32) gaps |= there(c) != 0xffffffffu;
+      if (gaps || !cache) {
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.v_full[st], parity, limit)))) break;
+        for (int i = t; i < n * kHalves * 8; i += kTile) {
+          const int row = (i >> 3) % n, half = (i >> 3) / n;
+          uint4* at = reinterpret_cast<uint4*>(s.v[st] + half * kBlock + row * 128 + (i & 7) * 16);
+          if (!(there(row & ~31) >> (row & 31) & 1)) {
+            *at = make_uint4(0, 0, 0, 0);
+          } else if (!cache) {
+            constexpr uint16_t kExp = F16 ? 0x7c00 : 0x7f80;
+            uint4 w = *at;
+            uint16_t* e = reinterpret_cast<uint16_t*>(&w);
+            bool odd = false;
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+              if ((e[q] & kExp) == kExp) {
+                e[q] = 0;
+                odd = true;
+              }
+            if (odd) {
+              *at = w;
+              atomicOr(&s.odd[(base + row) >> 5], 1u << ((base + row) & 31));
+            }
+          }
+        }
+        fence_proxy_async();
+      }
+      tc_fence_before();
+      mbar_arrive(&s.p_full);
+    }
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s.o_full, 0, limit));
+    tc_fence_after();
+    if (has_tree) asm volatile("bar.sync 1, 128;" ::: "memory");  // (s.odd is whole)
+    if (ok && some) {
+      const bool valid = t < rows;
+      const int node = r.first + node0 + local, h = hk * p.group + t % p.group;
+      const int64_t row = int64_t(node) * a.Hq + h;
+      const bool whole = runs == 1;
+      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+      const int64_t at = (int64_t(run) * a.n_nodes * a.Hq + row) * D;
+      for (int c = 0; c < D; c += 32) {
+        uint32_t v[32];
+        tmem_ld32(mine + kOut + c, v);
+        tmem_wait_ld(v);
+        if (valid) {
+          if (has_tree) {
+            for (int w = 0; w * 32 < node1; ++w)
+              for (uint32_t odd = s.odd[w] & s.seen[local][w]; odd; odd &= odd - 1) {
+                const int64_t other = int64_t(r.first) + w * 32 + __ffs(odd) - 1;
+                const uint16_t* e = reinterpret_cast<const uint16_t*>(a.v) + other * a.v_token +
+                                    hk * a.v_head + c;
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                  const float y = unpack<F16>(e[i]);
+                  if (!(fabsf(y) < INFINITY)) v[i] = __float_as_uint(__uint_as_float(v[i]) + y);
+                }
+              }
+          }
+          if (whole) {
+            uint4* out = reinterpret_cast<uint4*>(a.out + (row * D + c) * 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t o[4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q)
+                o[q] = pack2<F16>(__uint_as_float(v[8 * i + 2 * q]) * inv,
+                                  __uint_as_float(v[8 * i + 2 * q + 1]) * inv);
+              out[i] = make_uint4(o[0], o[1], o[2], o[3]);
+            }
+          } else {
+            uint4* out = reinterpret_cast<uint4*>(p.part + at + c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              out[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          }
+        }
+        __syncwarp();
+      }
+      if (valid) {
+        const float m2 = m == -INFINITY ? -INFINITY : m * p.scale2 - kOffset;
+        if (!whole)
+          p.part_ml[int64_t(run) * a.n_nodes * a.Hq + row] = make_float2(m2, l);
+        else if (a.lse)
+          a.lse[row] = l > 0.f || l != l ? fmaf(m2, kLn2, logf(l)) : -INFINITY;
+      }
+    }
+    if (reports) {
+      bool bad = out_of_range(a, b, r, t);
+      bad = __any_sync(0xffffffffu, bad);
+      if (bad && lane == 0) atomicOr(&s.failed, 2);
+    }
   }
+  if (!ok) atomicOr(&s.failed, 1);
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kRowWarps + 1) tmem_free(tmem, kTmemColumns);
+  if (t == 0 && (reports || (s.failed & 1)))
+    a.status[b] = (s.failed & 1 ? TT_REQ_TIMEOUT : 0) | (s.failed & 2 ? TT_REQ_ID_OUT_OF_RANGE : 0);
+}
+
+// Joins the runs of every row that has more than one: with M the largest of the
+// runs' references, out = sum 2^(m - M) o / sum 2^(m - M) l. A warp per row.
+template <int D, bool F16>
+__global__ void __launch_bounds__(256) tree_join_kernel(const __grid_constant__ TreeKernelArgs p) {
+  const TreeArgs& a = p.a;
+  const int lane = threadIdx.x & 31;
+  const int64_t w = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  grid_dependency_wait();
+  // row w of the B * max_nodes * Hq that there may be
+  const int h = int(w % a.Hq);
+  const int i = int(w / a.Hq % a.max_nodes);
+  const int64_t b = w / a.Hq / a.max_nodes;
+  if (b >= a.B) return;
+  const Request r = request(a, int(b));
+  if (i >= r.nodes) return;
+  const int end = min(r.nodes, (i / p.per_tile + 1) * p.per_tile);
+  const int runs = run_count(cache_tiles(r.len) + tree_tiles(end), p.run);
+  if (runs < 2) return;
+  const int64_t row = (int64_t(r.first) + i) * a.Hq + h, rows = int64_t(a.n_nodes) * a.Hq;
+  float M = -INFINITY;
+  for (int s = lane; s < runs; s += 32) M = fmaxf(M, p.part_ml[s * rows + row].x);
+  M = warp_max_f(M);
+  constexpr int N = D / 32;
+  float acc[N] = {};
+  float l = 0.f;
+  for (int s = 0; s < runs; ++s) {
+    const float2 ml = p.part_ml[s * rows + row];
+    const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
+    if (f == 0.f && ml.y == ml.y) continue;
+    l = fmaf(ml.y, f, l);
+    const float* o = p.part + (s * rows + row) * D + lane * N;
+#pragma unroll
+    for (int c = 0; c < N; ++c) acc[c] = fmaf(o[c], f, acc[c]);
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  uint32_t o[N / 2];
+#pragma unroll
+  for (int c = 0; c < N / 2; ++c) o[c] = pack2<F16>(acc[2 * c] * inv, acc[2 * c + 1] * inv);
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
+#pragma unroll
+  for (int c = 0; c < N / 2; ++c) out[c] = o[c];
+  if (a.lse && lane == 0) a.lse[row] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
+}
+
+// ------------------------------------------------------------------- host
+
+// How a call is cut: tokens per tile of rows, tiles per run, runs.
+struct Cut {
+  int group, per_tile, row_tiles, run, runs;
+  size_t part_bytes, bytes;
+};
+Cut cut(const TreeArgs& a, int sm_count) {
+  Cut c;
+  c.group = a.Hq / a.Hkv;
+  c.per_tile = kTile / c.group;
+  c.row_tiles = (a.max_nodes + c.per_tile - 1) / c.per_tile;
+  const int tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);
+  const int64_t items = int64_t(a.B) * a.Hkv * c.row_tiles, slots = 2 * int64_t(sm_count);
+  c.run = int(std::max<int64_t>(1, std::min<int64_t>(tiles, items * tiles / (slots * 4))));
+  c.runs = run_count(tiles, c.run);
+  const size_t rows = size_t(c.runs) * a.n_nodes * a.Hq;
+  c.part_bytes = c.runs > 1 ? align256(rows * a.D * sizeof(float)) : 0;
+  c.bytes = c.part_bytes + (c.runs > 1 ? align256(rows * sizeof(float2)) : 0);
+  return c;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+  static std::atomic<void*> found{nullptr};
+  void* f = found.load(std::memory_order_acquire);
+  if (!f) {
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return nullptr;
+    found.store(f, std::memory_order_release);
+  }
+  return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+}
+
+// A map of 16-bit elements, 128-byte swizzled boxes of 64 innermost ones.
+// Strides in elements; a dimension of one entry takes any valid stride.
+bool encode(CUtensorMap* map, bool f16, const char* data, int rank, const int64_t* size,
+            const int64_t* stride, const int* box) {
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t boxes[4], ones[4] = {1, 1, 1, 1};
+  for (int i = 0; i < rank; ++i) {
+    dims[i] = cuuint64_t(size[i]);
+    boxes[i] = cuuint32_t(box[i]);
+    if (i > 0) strides[i - 1] = cuuint64_t(size[i] > 1 ? stride[i] : size[0]) * 2;
+  }
+  const auto f = encoder();
+  return f && f(map, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                cuuint32_t(rank), const_cast<char*>(data), dims, strides, boxes, ones,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool F16>
+cudaError_t launch(const TreeKernelArgs& p, cudaStream_t stream) {
+  const TreeArgs& a = p.a;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(int64_t(a.B) * p.runs * a.Hkv * p.row_tiles));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem<D>) + 1024;
+  cfg.stream = stream;
+  cudaError_t e = cudaLaunchKernelEx(&cfg, tree_kernel<D, F16>, p);
+  if (e != cudaSuccess || p.runs == 1) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.gridDim = dim3(unsigned((int64_t(a.B) * a.max_nodes * a.Hq + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.dynamicSmemBytes = 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16>, p);
+}
+
+template <int D, bool F16>
+cudaError_t preload() {
+  cudaFuncAttributes fa;
+  const cudaError_t e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16>);
+  if (e != cudaSuccess) return e;
+  return cudaFuncSetAttribute(tree_kernel<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              int(sizeof(Smem<D>)) + 1024);
 }
 
 }  // namespace
 
-size_t tree_workspace_bytes(const TreeArgs&, int) { return 0; }
+size_t tree_workspace_bytes(const TreeArgs& a, int sm_count) { return cut(a, sm_count).bytes; }
 
-cudaError_t launch_tree(const TreeArgs& a, int dt, cudaStream_t stream, int) {
-  const dim3 grid(unsigned(a.max_nodes), unsigned(a.B));
-  if (dt == TT_BF16)
-    tree_kernel<__nv_bfloat16><<<grid, kThreads, 0, stream>>>(a);
-  else
-    tree_kernel<__half><<<grid, kThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+cudaError_t launch_tree(const TreeArgs& a, int dt, cudaStream_t stream, int sm_count) {
+  const Cut c = cut(a, sm_count);
+  if (int64_t(a.B) * c.runs * a.Hkv * c.row_tiles > INT32_MAX ||
+      int64_t(a.B) * a.max_nodes * a.Hq > INT32_MAX)
+    return cudaErrorInvalidConfiguration;
+  TreeKernelArgs p;
+  std::memset(&p, 0, sizeof p);
+  p.a = a;
+  p.scale2 = float(double(a.scale) * 1.4426950408889634);
+  p.group = c.group;
+  p.per_tile = c.per_tile;
+  p.row_tiles = c.row_tiles;
+  p.run = c.run;
+  p.runs = c.runs;
+  p.box = std::gcd(a.page_size, kTile);
+  p.part = reinterpret_cast<float*>(a.ws);
+  p.part_ml = reinterpret_cast<float2*>(a.ws + c.part_bytes);
+  const bool f16 = dt == TT_F16;
+  bool ok = true;
+  if (a.n_nodes > 0) {
+    const int64_t nq[3] = {a.D, a.Hq, a.n_nodes}, nk[3] = {a.D, a.Hkv, a.n_nodes};
+    const int64_t sq[3] = {1, a.q_head, a.q_token}, sk[3] = {1, a.k_head, a.k_token},
+                  sv[3] = {1, a.v_head, a.v_token};
+    const int bq[3] = {64, c.group, c.per_tile}, bk[3] = {64, 1, 16};
+    ok = encode(&p.q, f16, a.q, 3, nq, sq, bq) && encode(&p.k, f16, a.k, 3, nk, sk, bk) &&
+         encode(&p.v, f16, a.v, 3, nk, sv, bk);
+  }
+  if (a.max_len > 0) {
+    // (dimensions by rising stride: heads within slots, or slots within heads)
+    p.slots_inner = a.kc_slot < a.kc_head && a.page_size > 1 && a.Hkv > 1;
+    const bool si = p.slots_inner;
+    const int64_t n[4] = {a.D, si ? a.page_size : a.Hkv, si ? a.Hkv : a.page_size, a.n_pages};
+    const int64_t sk[4] = {1, si ? a.kc_slot : a.kc_head, si ? a.kc_head : a.kc_slot, a.kc_page};
+    const int64_t sv[4] = {1, si ? a.vc_slot : a.vc_head, si ? a.vc_head : a.vc_slot, a.vc_page};
+    const int box[4] = {64, si ? p.box : 1, si ? 1 : p.box, 1};
+    ok = ok && encode(&p.kc, f16, a.kc, 4, n, sk, box) && encode(&p.vc, f16, a.vc, 4, n, sv, box);
+  }
+  if (!ok) return cudaErrorInvalidValue;
+  if (a.D == 128) return f16 ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+  return f16 ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
 }
 
 cudaError_t preload_tree() {
-  cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, tree_kernel<__nv_bfloat16>);
-  return e == cudaSuccess ? cudaFuncGetAttributes(&fa, tree_kernel<__half>) : e;
+  cudaError_t e = preload<128, true>();
+  if (e == cudaSuccess) e = preload<128, false>();
+  if (e == cudaSuccess) e = preload<64, true>();
+  if (e == cudaSuccess) e = preload<64, false>();
+  return e;
 }
 
 }  // namespace tt
