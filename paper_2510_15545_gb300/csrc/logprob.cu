@@ -7,6 +7,19 @@
 // -sum p ln p = ln S - ln 2 E / S. The difference z_x - M is taken first: in the
 // product z_x log2(e) / T the rounding of a large z would be an error of the
 // whole row. A column of -inf adds nothing (d is held at -256, 2^d is 0).
+//
+// One pass over the logits: each thread keeps its own M (sums are scaled when it
+// rises), S, E and the columns that come before the given one. The best columns
+// need a bar that the n best of the row reach: each warp posts the k-th largest
+// of its lanes' maxima, k = ceil(n / warps), and since those are k different
+// columns of each warp, at least n columns reach the least of the posts. What
+// reaches the bar as it stands is gathered; a few hundred of 200,000 columns do.
+// Rows for which more than the buffer holds do (long runs of equal logits at the
+// bar) are searched digit by digit, reading them again. When there are few rows, a
+// cluster of CTAs shares each and joins its parts through distributed shared
+// memory.
+#include <algorithm>
+#include <cooperative_groups.h>
 #include <cstdint>
 
 #include "tt_device.cuh"
@@ -19,7 +32,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
+constexpr int kBatch = 4;           // vectors of a thread between two looks at the bar
+constexpr int kCandidates = 2048;   // room for what reaches the bar
+constexpr int kMaxSplit = 16;
 constexpr float kLn2 = 0.693147180559945f;
+
+namespace cg = cooperative_groups;
 
 // Order of a logit as an unsigned number (-0 as 0); above 0 for every logit.
 __device__ __forceinline__ uint32_t order_key(float z) {
@@ -30,46 +48,26 @@ __device__ __forceinline__ float key_value(uint32_t k) {
   return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
 }
 
-// The row's columns c0 .. c1 - 1 in steps of one per thread.
+// The columns c0 .. c1 - 1 in steps of one per thread.
 template <int DT, typename F>
-__device__ __forceinline__ void each_logit(const char* row, int V, F&& f) {
-  for (int x = threadIdx.x; x < V; x += kThreads) f(load_logit<DT>(row, x), x);
+__device__ __forceinline__ void each_logit(const char* row, int c0, int c1, F&& f) {
+  for (int x = c0 + threadIdx.x; x < c1; x += kThreads) f(load_logit<DT>(row, x), x);
 }
 
-__device__ __forceinline__ float block_max(float v, float* red) {
-  v = warp_max_f(v);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-  for (int w = 1; w < kWarps; ++w) v = fmaxf(v, red[w]);
-  return v;
-}
-
-template <typename T>
-__device__ __forceinline__ T block_sum(T v, T* red) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-  for (int w = 1; w < kWarps; ++w) v += red[w];
-  return v;
-}
-
-// The n best of the row's columns above -inf, in order, into best (keys: order
-// of the logit above the complement of the column; 0 where there are fewer): a
-// radix search for the n-th largest logit, the columns above it, and the first
-// of those equal to it.
+// The n best of the columns c0 .. c1 - 1 above -inf, in order, into best (keys:
+// order of the logit above the complement of the column; 0 where there are
+// fewer): a radix search for the n-th largest logit, the columns above it, and
+// the first of those equal to it.
 template <int DT>
-__device__ void select_best(const char* row, int V, int n, unsigned long long* best) {
+__device__ __noinline__ void select_best(const char* row, int c0, int c1, int n,
+                                         unsigned long long* best) {
   __shared__ unsigned int hist[256];
   __shared__ unsigned int s_prefix, s_want, s_count;
   __shared__ unsigned int s_warp[kWarps];
   __shared__ unsigned long long found[TT_MAX_TOP_K];
   const int t = threadIdx.x;
   const uint32_t empty = order_key(-INFINITY);
+  __syncthreads();
   if (t == 0) {
     s_prefix = 0;
     s_want = n;
@@ -78,7 +76,7 @@ __device__ void select_best(const char* row, int V, int n, unsigned long long* b
     hist[t] = 0;
     __syncthreads();
     const uint32_t prefix = s_prefix;
-    each_logit<DT>(row, V, [&](float z, int) {
+    each_logit<DT>(row, c0, c1, [&](float z, int) {
       const uint32_t k = order_key(z);
       if (k > empty && (shift == 24 || (k >> (shift + 8)) == prefix >> (shift + 8)))
         atomicAdd(&hist[(k >> shift) & 255], 1u);
@@ -98,7 +96,7 @@ __device__ void select_best(const char* row, int V, int n, unsigned long long* b
   const unsigned int equal = s_want;  // how many of its equals are taken, in column order
   if (t == 0) s_count = 0;
   __syncthreads();
-  each_logit<DT>(row, V, [&](float z, int x) {
+  each_logit<DT>(row, c0, c1, [&](float z, int x) {
     const uint32_t k = order_key(z);
     if (k > tau && k > empty) {
       const unsigned int p = atomicAdd(&s_count, 1u);
@@ -108,9 +106,9 @@ __device__ void select_best(const char* row, int V, int n, unsigned long long* b
   __syncthreads();
   const unsigned int above = min(s_count, unsigned(n));
   unsigned int taken = 0;
-  for (int x0 = 0; x0 < V && taken < equal; x0 += kThreads) {
+  for (int x0 = c0; x0 < c1 && taken < equal; x0 += kThreads) {
     const int x = x0 + t;
-    const uint32_t k = x < V ? order_key(load_logit<DT>(row, x)) : 0u;
+    const uint32_t k = x < c1 ? order_key(load_logit<DT>(row, x)) : 0u;
     const bool eq = k == tau && k > empty;
     const unsigned int bits = __ballot_sync(0xffffffffu, eq);
     __syncthreads();
@@ -138,69 +136,319 @@ __device__ void select_best(const char* row, int V, int n, unsigned long long* b
   __syncthreads();
 }
 
+// The sums of some columns: their maximum z, sum of 2^d and of 2^d d with
+// d = (z - max) log2(e) / T, and how many come before the given column.
+struct Sums {
+  float m, s, e;
+  int before;
+};
+__device__ __forceinline__ void join(Sums& a, const Sums& b, float scale) {
+  const float m = fmaxf(a.m, b.m);
+  // (d of -inf, or of the type's whole range: the factor is 0)
+  const float da = a.m == m ? 0.f : fmaxf((a.m - m) * scale, -256.f);
+  const float db = b.m == m ? 0.f : fmaxf((b.m - m) * scale, -256.f);
+  const float fa = ex2_approx(da), fb = ex2_approx(db);
+  a.e = fa * fmaf(a.s, da, a.e) + fb * fmaf(b.s, db, b.e);
+  a.s = fa * a.s + fb * b.s;
+  a.m = m;
+  a.before += b.before;
+}
+
 template <int DT>
-__global__ void __launch_bounds__(kThreads) logprob_kernel(const __grid_constant__ LogprobArgs a) {
-  __shared__ float red[kWarps];
-  __shared__ int redi[kWarps];
-  __shared__ unsigned long long best[TT_MAX_TOP_K];
-  const int64_t r = blockIdx.x;
+struct Logit;
+template <>
+struct Logit<TT_F32> {
+  static constexpr uint32_t kMinusInf = 0xff800000u;
+};
+template <>
+struct Logit<TT_BF16> {
+  static constexpr uint32_t kMinusInf = 0xff80ff80u;
+};
+
+// Columns of one vector, the first of them `col`, that come before column id
+// with logit zt.
+template <int DT>
+__device__ __forceinline__ int count_before(const uint4& w, int col, int id, float zt) {
+  constexpr int VEC = DT == TT_F32 ? 4 : 8;
+  int n = 0;
+  if (col + VEC <= id) {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) n += lane_elem<DT>(w, q) >= zt;
+  } else if (col > id) {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) n += lane_elem<DT>(w, q) > zt;
+  } else {
+#pragma unroll
+    for (int q = 0; q < VEC; ++q) {
+      const float z = lane_elem<DT>(w, q);
+      n += z > zt || (z == zt && col + q < id);
+    }
+  }
+  return n;
+}
+
+struct Shared {
+  Sums sums[kWarps];
+  Sums mine;  // the CTA's share
+  float post[kWarps];
+  unsigned int count;     // columns that reached the bar
+  unsigned int kept;
+  unsigned long long best[TT_MAX_TOP_K];
+  unsigned long long found[kCandidates];
+};
+
+// The n best of `count` keys (n <= TT_MAX_TOP_K; 0 where there are fewer), by
+// counting those above each one: keys are distinct.
+__device__ __forceinline__ void rank_keys(const unsigned long long* key, int count, int n,
+                                          unsigned long long* best) {
+  if (threadIdx.x < n) best[threadIdx.x] = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < count; i += kThreads) {
+    const unsigned long long k = key[i];
+    int r = 0;
+    for (int j = 0; j < count; ++j) r += key[j] > k;
+    if (r < n) best[r] = k;
+  }
+  __syncthreads();
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kThreads, 4)
+    logprob_kernel(const __grid_constant__ LogprobArgs a) {
+  constexpr int VEC = DT == TT_F32 ? 4 : 8;
+  constexpr int ESZ = 16 / VEC;
+  __shared__ Shared s;
+  const cg::cluster_group cluster = cg::this_cluster();
+  const int S = a.split, rank = S > 1 ? int(cluster.block_rank()) : 0;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const int64_t r = blockIdx.x / S;
   const char* row = a.data + r * a.stride_bytes;
+  const int c0 = min(a.V, rank * a.share), c1 = min(a.V, c0 + a.share);
   const int id = a.ids ? a.ids[r] : -1;
   const bool given = id >= 0 && id < a.V;
   const float zt = given ? load_logit<DT>(row, id) : 0.f;
-  float m = -INFINITY;
-  each_logit<DT>(row, a.V, [&](float z, int) { m = fmaxf(m, z); });
-  m = block_max(m, red);
-  float S = 0.f, E = 0.f;
-  int before = 0;
-  each_logit<DT>(row, a.V, [&](float z, int x) {
-    const float d = (z - m) * a.scale, e = ex2_approx(d);
-    S += e;
-    E = fmaf(e, fmaxf(d, -256.f), E);
-    before += z > zt || (z == zt && x < id);
-  });
-  S = block_sum(S, red);
-  E = block_sum(E, red);
-  before = block_sum(before, redi);
-  const bool ok = S > 0.f && S < INFINITY;  // neither empty nor NaN or +inf
-  if (a.top_n > 0 && ok) select_best<DT>(row, a.V, a.top_n, best);
-  const float nan = __int_as_float(0x7fffffff), ln_s = logf(S), lse = m / a.temp + ln_s;
-  if (threadIdx.x == 0) {
+  const int n = a.top_n, k = (n + kWarps - 1) / kWarps;
+  const char* base = row + int64_t(c0) * ESZ;
+  const int whole = (c1 - c0) / VEC, nvec = (c1 - c0 + VEC - 1) / VEC;
+
+  auto load = [&](int v) {
+    if (v < whole) return ld_stream_v4(base + int64_t(v) * 16);
+    constexpr uint32_t e = Logit<DT>::kMinusInf;
+    uint4 w = make_uint4(e, e, e, e);
+    if (v < nvec) {  // the row's last columns
+      const int c = c0 + whole * VEC;
+      uint32_t bits[VEC];
+#pragma unroll
+      for (int q = 0; q < VEC; ++q)
+        bits[q] = __float_as_uint(c + q < c1 ? load_logit<DT>(row, c + q) : -INFINITY);
+      if constexpr (DT == TT_F32)
+        w = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+      else
+        w = make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5],
+                       bits[6] >> 16 | bits[7]);
+    }
+    return w;
+  };
+
+  Sums x{-INFINITY, 0.f, 0.f, 0};
+  float bar = -INFINITY;
+  if (t == 0) s.count = s.kept = 0;
+  uint4 w[kBatch];
+#pragma unroll
+  for (int u = 0; u < kBatch; ++u) w[u] = load(u * kThreads + t);
+  int it = 0;
+  for (int v0 = 0; v0 < nvec; v0 += kBatch * kThreads, ++it) {
+    uint4 next[kBatch];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) next[u] = load(v0 + (kBatch + u) * kThreads + t);
+    float vm[kBatch], top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      vm[u] = vec_max<DT>(w[u]);
+      top = fmaxf(top, vm[u]);
+    }
+    if (top > x.m) {
+      const float d = fmaxf((x.m - top) * a.scale, -256.f), f = ex2_approx(d);
+      x.e = f * fmaf(x.s, d, x.e);
+      x.s *= f;
+      x.m = top;
+    }
+    const float ref = x.m > -INFINITY ? x.m : 0.f;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) {
+        const float d = (lane_elem<DT>(w[u], q) - ref) * a.scale, e = ex2_approx(d);
+        x.s += e;
+        x.e = fmaf(e, fmaxf(d, -256.f), x.e);
+      }
+    }
+    if (given) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        x.before += count_before<DT>(w[u], c0 + (v0 + u * kThreads + t) * VEC, id, zt);
+    }
+    if (n > 0) {
+      if (it < 4 || (it & 3) == 0) {
+        // the k-th largest of the lanes' maxima, for all warps to see
+        uint32_t key = order_key(x.m), kth = 0;
+        for (int j = 0; j < k; ++j) {
+          kth = __reduce_max_sync(0xffffffffu, key);
+          const unsigned int who = __ballot_sync(0xffffffffu, key == kth);
+          if (lane == __ffs(who) - 1) key = 0;
+        }
+        volatile float* post = s.post;
+        if (lane == 0) post[warp] = kth ? key_value(kth) : -INFINITY;
+        if (it == 0)
+          __syncthreads();
+        else
+          __syncwarp();
+        bar = post[0];
+#pragma unroll
+        for (int j = 1; j < kWarps; ++j) bar = fminf(bar, post[j]);
+      }
+      if (top >= bar && top > -INFINITY) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          if (!(vm[u] >= bar)) continue;
+#pragma unroll
+          for (int q = 0; q < VEC; ++q) {
+            const float z = lane_elem<DT>(w[u], q);
+            if (z >= bar && z > -INFINITY) {
+              const unsigned int p = atomicAdd(&s.count, 1u);
+              const uint32_t col = c0 + (v0 + u * kThreads + t) * VEC + q;
+              if (p < kCandidates) s.found[p] = uint64_t(order_key(z)) << 32 | uint32_t(~col);
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) w[u] = next[u];
+  }
+
+  // the CTA's sums
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    Sums y;
+    y.m = __shfl_xor_sync(0xffffffffu, x.m, o);
+    y.s = __shfl_xor_sync(0xffffffffu, x.s, o);
+    y.e = __shfl_xor_sync(0xffffffffu, x.e, o);
+    y.before = __shfl_xor_sync(0xffffffffu, x.before, o);
+    join(x, y, a.scale);
+  }
+  if (lane == 0) s.sums[warp] = x;
+  __syncthreads();
+  if (t == 0) {
+    Sums y = s.sums[0];
+    for (int j = 1; j < kWarps; ++j) join(y, s.sums[j], a.scale);
+    s.mine = y;
+  }
+  // and its best columns: the last bar leaves little more than them
+  if (n > 0) {
+    const unsigned int count = s.count;
+    if (count > kCandidates) {
+      select_best<DT>(row, c0, c1, n, s.best);
+    } else {
+      bar = nvec > 0 ? s.post[0] : -INFINITY;
+      for (int j = 1; j < kWarps; ++j) bar = fminf(bar, s.post[j]);
+      const uint32_t low = nvec > 0 ? order_key(bar) : 0;
+      unsigned long long key[kCandidates / kThreads];
+#pragma unroll
+      for (int j = 0; j < kCandidates / kThreads; ++j) {
+        const unsigned int i = j * kThreads + t;
+        key[j] = i < count ? s.found[i] : 0;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < kCandidates / kThreads; ++j)
+        if (key[j] && uint32_t(key[j] >> 32) >= low) s.found[atomicAdd(&s.kept, 1u)] = key[j];
+      __syncthreads();
+      rank_keys(s.found, s.kept, n, s.best);
+    }
+  }
+  // the row's, by its first CTA
+  if (S > 1) {
+    cluster.sync();
+    if (rank > 0) {
+      cluster.sync();  // (its shared memory is read until here)
+      return;
+    }
+    if (n > 0) {
+      for (int i = t; i < S * n; i += kThreads) s.found[i] = cluster.map_shared_rank(s.best, i / n)[i % n];
+    }
+    if (t == 0) {
+      Sums y = s.mine;
+      for (int j = 1; j < S; ++j) join(y, *cluster.map_shared_rank(&s.mine, j), a.scale);
+      s.sums[0] = y;
+      s.kept = 0;
+    }
+    cluster.sync();
+    if (n > 0) rank_keys(s.found, S * n, n, s.best);
+    if (t == 0) s.mine = s.sums[0];
+  }
+  __syncthreads();
+  const Sums y = s.mine;
+  const bool ok = y.s > 0.f && y.s < INFINITY;  // neither empty nor NaN or +inf
+  const float nan = __int_as_float(0x7fffffff), ln_s = logf(y.s);
+  if (t == 0) {
     a.out.status[r] = (ok ? 0 : TT_REQ_NOT_FINITE) |
                       (given || id == -1 ? 0 : TT_REQ_ID_OUT_OF_RANGE);
-    if (a.out.lse) a.out.lse[r] = ok ? lse : nan;
-    if (a.out.entropy) a.out.entropy[r] = ok ? ln_s - kLn2 * (E / S) : nan;
+    if (a.out.lse) a.out.lse[r] = ok ? y.m / a.temp + ln_s : nan;
+    if (a.out.entropy) a.out.entropy[r] = ok ? ln_s - kLn2 * (y.e / y.s) : nan;
     if (a.out.logprob)
-      a.out.logprob[r] = !ok || (!given && id != -1) ? nan : given ? (zt - m) / a.temp - ln_s : 0.f;
-    if (a.out.rank) a.out.rank[r] = ok && given ? before : -1;
+      a.out.logprob[r] =
+          !ok || (!given && id != -1) ? nan : given ? (zt - y.m) / a.temp - ln_s : 0.f;
+    if (a.out.rank) a.out.rank[r] = ok && given ? y.before : -1;
   }
-  if (threadIdx.x < a.top_n) {
-    const unsigned long long k = ok ? best[threadIdx.x] : 0;
-    const int64_t at = r * a.top_n + threadIdx.x;
-    if (a.out.top_ids) a.out.top_ids[at] = k ? int32_t(~uint32_t(k)) : -1;
+  if (t < n) {
+    const unsigned long long key = ok ? s.best[t] : 0;
+    const int64_t at = r * n + t;
+    if (a.out.top_ids) a.out.top_ids[at] = key ? int32_t(~uint32_t(key)) : -1;
     if (a.out.top_logprobs)
-      a.out.top_logprobs[at] = !ok ? nan
-                               : k ? (key_value(uint32_t(k >> 32)) - m) / a.temp - ln_s
-                                   : -INFINITY;
+      a.out.top_logprobs[at] =
+          !ok ? nan : key ? (key_value(uint32_t(key >> 32)) - y.m) / a.temp - ln_s : -INFINITY;
   }
+}
+
+template <int DT>
+cudaError_t launch(LogprobArgs a, cudaStream_t stream, int sm_count) {
+  constexpr int VEC = DT == TT_F32 ? 4 : 8;
+  // CTAs of a row: enough to fill the SMs, each with a batch of vectors at least
+  int S = 1;
+  while (S < kMaxSplit && a.rows * S < 2 * sm_count &&
+         a.V / (2 * S) >= kBatch * kThreads * VEC)
+    S *= 2;
+  a.split = S;
+  a.share = ((a.V + S - 1) / S + VEC - 1) / VEC * VEC;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(unsigned(a.rows * S));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = S;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = S > 1 ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<DT>, a);
+}
+
+template <int DT>
+cudaError_t preload() {
+  return cudaFuncSetAttribute(logprob_kernel<DT>, cudaFuncAttributeNonPortableClusterSizeAllowed,
+                              1);
 }
 
 }  // namespace
 
-cudaError_t launch_logprobs(const LogprobArgs& a, int dt, cudaStream_t stream, int) {
-  const dim3 grid{unsigned(a.rows)};
-  if (dt == TT_F32)
-    logprob_kernel<TT_F32><<<grid, kThreads, 0, stream>>>(a);
-  else
-    logprob_kernel<TT_BF16><<<grid, kThreads, 0, stream>>>(a);
-  return cudaGetLastError();
+cudaError_t launch_logprobs(const LogprobArgs& a, int dt, cudaStream_t stream, int sm_count) {
+  return dt == TT_F32 ? launch<TT_F32>(a, stream, sm_count) : launch<TT_BF16>(a, stream, sm_count);
 }
 
 cudaError_t preload_logprobs() {
-  cudaFuncAttributes attr;
-  cudaError_t e = cudaFuncGetAttributes(&attr, logprob_kernel<TT_F32>);
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&attr, logprob_kernel<TT_BF16>);
-  return e;
+  const cudaError_t e = preload<TT_F32>();
+  return e == cudaSuccess ? preload<TT_BF16>() : e;
 }
 
 }  // namespace tt

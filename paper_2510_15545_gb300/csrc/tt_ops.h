@@ -27,6 +27,7 @@ struct LogprobArgs {
   int top_n;
   const int32_t* ids;
   tt_logprobs_out out;
+  int split, share;  // CTAs per row and columns of each (filled in by the launcher)
 };
 
 cudaError_t launch_logprobs(const LogprobArgs& args, int dt, cudaStream_t stream, int sm_count);
