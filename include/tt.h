@@ -410,7 +410,7 @@ typedef struct {
  * TT_MAX_TOP_K). Columns of -inf have log p = -inf and are never among the best:
  * where a row has fewer, the rest is (-1, -inf). A row that has no normaliser
  * (nothing but -inf, or +inf or NaN anywhere) gets NaN, -1 and NOT_FINITE.
- * Sums are kept in fp32. Needs no workspace. */
+ * temp from 1e-36 to 1e36. Sums are kept in fp32. Needs no workspace. */
 tt_status tt_logprobs(const tt_logits* rows, const int32_t* ids, float temp, int32_t top_n,
                       const tt_logprobs_out* out, void* stream);
 

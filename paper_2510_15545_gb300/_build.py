@@ -19,7 +19,7 @@ SOURCES = ["api.cu", "align.cu", "rowpass.cu", "decide.cu", "noalloc.cu", "encod
            "filter.cu", "nucleus.cu", "nucrow.cu", "pen.cu", "ops.cu", "logprob.cu",
            "distill.cu", "tree.cu"]
 HEADERS = ["tt_device.cuh", "tt_launch.h", "tt_shard.h", "tt_f2.cuh",
-           "tt_ring.cuh", "tt_ops.h", "tt_umma.cuh"]
+           "tt_ring.cuh", "tt_ops.h", "tt_umma.cuh", "tt_x2.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -6,7 +6,8 @@
 // lse = M / T + ln S, log p_t = (z_t - M) / T - ln S, and the entropy
 // -sum p ln p = ln S - ln 2 E / S. The difference z_x - M is taken first: in the
 // product z_x log2(e) / T the rounding of a large z would be an error of the
-// whole row. A column of -inf adds nothing (d is held at -256, 2^d is 0).
+// whole row. A column of -inf adds nothing: it counts as one so low that its 2^d
+// is 0, with a finite d.
 //
 // One pass over the logits: each thread keeps its own M (sums are scaled when it
 // rises), S, E and the columns that come before the given one. The best columns
@@ -25,6 +26,7 @@
 #include "tt_device.cuh"
 #include "tt_ops.h"
 #include "tt_ring.cuh"
+#include "tt_x2.cuh"
 
 namespace tt {
 
@@ -33,8 +35,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
 constexpr int kBatch = 4;           // vectors of a thread between two looks at the bar
-constexpr int kCandidates = 2048;   // room for what reaches the bar
+constexpr int kVectors = 2048;      // room for vectors that reach the bar
+constexpr int kCandidates = 1024;   // and for columns that reach the last one
 constexpr int kMaxSplit = 16;
+constexpr float kLeast = -3.402823466e38f;  // -inf never reaches a bar
 constexpr float kLn2 = 0.693147180559945f;
 
 namespace cg = cooperative_groups;
@@ -165,35 +169,72 @@ struct Logit<TT_BF16> {
   static constexpr uint32_t kMinusInf = 0xff80ff80u;
 };
 
-// Columns of one vector, the first of them `col`, that come before column id
-// with logit zt.
+// A logit so far below `top` that its 2^d is 0, but whose d is finite, which the
+// d of -inf would not be: taken in place of everything below it. Rounded down to
+// a bf16; below the type's lowest value that is -inf (see number).
 template <int DT>
-__device__ __forceinline__ int count_before(const uint4& w, int col, int id, float zt) {
-  constexpr int VEC = DT == TT_F32 ? 4 : 8;
-  int n = 0;
-  if (col + VEC <= id) {
+__device__ __forceinline__ uint32_t lowest(float top, float reach) {
+  float z = top - reach;
+  if (!(z < top)) z = fmaf(fabsf(top), -1.2e-7f, top);
+  const uint32_t u = __float_as_uint(z);
+  if constexpr (DT == TT_F32) return u;
+  const uint32_t h = (z < 0.f ? u + 0xffffu : u) >> 16;
+  return h << 16 | h;
+}
+
+// A thread's E, 0 in place of NaN: it is NaN where a d was -inf, which next to a
+// maximum at the end of the type's range is every column but its equals, whose d
+// is 0. (A logit that is NaN makes S NaN too.)
+__device__ __forceinline__ f32x2 number(f32x2 e) {
+  float lo, hi;
+  split(e, lo, hi);
+  return pair(lo == lo ? lo : 0.f, hi == hi ? hi : 0.f);
+}
+
+// How many of a vector's logits are at or above a threshold, added to `n` (two
+// counts of up to 256 in bf16, or one in fp32, as a number of the logits' type).
+template <int DT>
+__device__ __forceinline__ void count_at_least(const uint4& w, uint32_t threshold, uint32_t& n) {
+  const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) n += lane_elem<DT>(w, q) >= zt;
-  } else if (col > id) {
-#pragma unroll
-    for (int q = 0; q < VEC; ++q) n += lane_elem<DT>(w, q) > zt;
-  } else {
-#pragma unroll
-    for (int q = 0; q < VEC; ++q) {
-      const float z = lane_elem<DT>(w, q);
-      n += z > zt || (z == zt && col + q < id);
+  for (int q = 0; q < 4; ++q) {
+    uint32_t one;
+    if constexpr (DT == TT_F32) {
+      asm("set.ge.f32.f32 %0, %1, %2;" : "=r"(one) : "r"(x[q]), "r"(threshold));
+      asm("add.f32 %0, %0, %1;" : "+r"(n) : "r"(one));
+    } else {
+      asm("set.ge.bf16x2.bf16x2 %0, %1, %2;" : "=r"(one) : "r"(x[q]), "r"(threshold));
+      asm("add.bf16x2 %0, %0, %1;" : "+r"(n) : "r"(one));
     }
   }
-  return n;
+}
+template <int DT>
+__device__ __forceinline__ int count_of(uint32_t n) {
+  if constexpr (DT == TT_F32) return int(__uint_as_float(n));
+  return int(__uint_as_float(n << 16)) + int(__uint_as_float(n & 0xffff0000u));
+}
+// The thresholds of the columns before the given one (its equals come first) and
+// behind it (they do not: the next logit of the type).
+template <int DT>
+__device__ __forceinline__ uint32_t logit_bits(float z) {
+  const uint32_t u = __float_as_uint(z);
+  return DT == TT_F32 ? u : (u & 0xffff0000u) | u >> 16;
+}
+template <int DT>
+__device__ __forceinline__ float logit_above(float z) {
+  constexpr int step = DT == TT_F32 ? 1 : 1 << 16;
+  const int u = __float_as_int(z + 0.f);
+  return __int_as_float(z == 0.f ? step : u > 0 ? u + step : u - step);
 }
 
 struct Shared {
   Sums sums[kWarps];
   Sums mine;  // the CTA's share
   float post[kWarps];
-  unsigned int count;     // columns that reached the bar
-  unsigned int kept;
+  unsigned int count;  // vectors that reached the bar
+  unsigned int kept;   // columns that reach the last one
   unsigned long long best[TT_MAX_TOP_K];
+  int vecs[kVectors];
   unsigned long long found[kCandidates];
 };
 
@@ -231,27 +272,36 @@ __global__ void __launch_bounds__(kThreads, 4)
   const char* base = row + int64_t(c0) * ESZ;
   const int whole = (c1 - c0) / VEC, nvec = (c1 - c0 + VEC - 1) / VEC;
 
+  constexpr uint32_t kNone = Logit<DT>::kMinusInf;
+  const uint4 none = make_uint4(kNone, kNone, kNone, kNone);
+  uint4 tail = none;  // the row's last columns
+  if (nvec > whole && t == whole % kThreads) {
+    const int c = c0 + whole * VEC;
+    uint32_t bits[VEC];
+#pragma unroll
+    for (int q = 0; q < VEC; ++q)
+      bits[q] = __float_as_uint(c + q < c1 ? load_logit<DT>(row, c + q) : -INFINITY);
+    if constexpr (DT == TT_F32)
+      tail = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+    else
+      tail = make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5],
+                        bits[6] >> 16 | bits[7]);
+  }
   auto load = [&](int v) {
     if (v < whole) return ld_stream_v4(base + int64_t(v) * 16);
-    constexpr uint32_t e = Logit<DT>::kMinusInf;
-    uint4 w = make_uint4(e, e, e, e);
-    if (v < nvec) {  // the row's last columns
-      const int c = c0 + whole * VEC;
-      uint32_t bits[VEC];
-#pragma unroll
-      for (int q = 0; q < VEC; ++q)
-        bits[q] = __float_as_uint(c + q < c1 ? load_logit<DT>(row, c + q) : -INFINITY);
-      if constexpr (DT == TT_F32)
-        w = make_uint4(bits[0], bits[1], bits[2], bits[3]);
-      else
-        w = make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5],
-                       bits[6] >> 16 | bits[7]);
-    }
-    return w;
+    return v == whole ? tail : none;
   };
 
   Sums x{-INFINITY, 0.f, 0.f, 0};
-  float bar = -INFINITY;
+  // (pairs of sums, even and odd columns; of a thread that has seen nothing but
+  // -inf: sums of 0 relative to 0)
+  f32x2 s2 = 0, e2 = 0, minus = 0;
+  const f32x2 scale2 = pair(a.scale, a.scale);
+  uint32_t low = lowest<DT>(0.f, a.reach);
+  // the vector that holds the given column, and the thresholds around it
+  const int v_id = id >= c0 ? (id - c0) / VEC : -1;
+  const uint32_t from = logit_bits<DT>(zt), above = logit_bits<DT>(logit_above<DT>(zt));
+  float bar = kLeast;
   if (t == 0) s.count = s.kept = 0;
   uint4 w[kBatch];
 #pragma unroll
@@ -269,24 +319,32 @@ __global__ void __launch_bounds__(kThreads, 4)
     }
     if (top > x.m) {
       const float d = fmaxf((x.m - top) * a.scale, -256.f), f = ex2_approx(d);
-      x.e = f * fmaf(x.s, d, x.e);
-      x.s *= f;
+      const f32x2 d2 = pair(d, d), f2 = pair(f, f);
+      e2 = mul2(f2, fma2(s2, d2, number(e2)));
+      s2 = mul2(s2, f2);
       x.m = top;
+      minus = pair(-top, -top);
+      low = lowest<DT>(top, a.reach);
     }
-    const float ref = x.m > -INFINITY ? x.m : 0.f;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
+      const uint4 y = at_least<DT>(w[u], low);
 #pragma unroll
-      for (int q = 0; q < VEC; ++q) {
-        const float d = (lane_elem<DT>(w[u], q) - ref) * a.scale, e = ex2_approx(d);
-        x.s += e;
-        x.e = fmaf(e, fmaxf(d, -256.f), x.e);
+      for (int q = 0; q < VEC / 2; ++q) {
+        const f32x2 d = mul2(add2(logit_pair<DT>(y, q), minus), scale2), e = exp2_pair(d);
+        s2 = add2(s2, e);
+        e2 = fma2(e, d, e2);
       }
     }
-    if (given) {
+    if (given && top >= zt) {
+      uint32_t n_before = 0;
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u)
-        x.before += count_before<DT>(w[u], c0 + (v0 + u * kThreads + t) * VEC, id, zt);
+      for (int u = 0; u < kBatch; ++u) {
+        const int v = v0 + u * kThreads + t;
+        if (vm[u] >= zt && v != v_id && v < nvec)
+          count_at_least<DT>(w[u], v < v_id ? from : above, n_before);
+      }
+      x.before += count_of<DT>(n_before);
     }
     if (n > 0) {
       if (it < 4 || (it & 3) == 0) {
@@ -306,19 +364,14 @@ __global__ void __launch_bounds__(kThreads, 4)
         bar = post[0];
 #pragma unroll
         for (int j = 1; j < kWarps; ++j) bar = fminf(bar, post[j]);
+        bar = fmaxf(bar, kLeast);
       }
-      if (top >= bar && top > -INFINITY) {
+      if (top >= bar) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-          if (!(vm[u] >= bar)) continue;
-#pragma unroll
-          for (int q = 0; q < VEC; ++q) {
-            const float z = lane_elem<DT>(w[u], q);
-            if (z >= bar && z > -INFINITY) {
-              const unsigned int p = atomicAdd(&s.count, 1u);
-              const uint32_t col = c0 + (v0 + u * kThreads + t) * VEC + q;
-              if (p < kCandidates) s.found[p] = uint64_t(order_key(z)) << 32 | uint32_t(~col);
-            }
+          if (vm[u] >= bar) {
+            const unsigned int p = atomicAdd(&s.count, 1u);
+            if (p < kVectors) s.vecs[p] = v0 + u * kThreads + t;
           }
         }
       }
@@ -328,6 +381,8 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 
   // the CTA's sums
+  x.s = sum_pair(s2);
+  x.e = sum_pair(number(e2));
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     Sums y;
@@ -338,34 +393,45 @@ __global__ void __launch_bounds__(kThreads, 4)
     join(x, y, a.scale);
   }
   if (lane == 0) s.sums[warp] = x;
+  // (the columns around the given one within its vector)
+  int close = 0;
+  if (warp == 0 && given && v_id >= 0 && v_id < nvec && lane < VEC) {
+    const int col = c0 + v_id * VEC + lane;
+    if (col < c1) {
+      const float z = load_logit<DT>(row, col);
+      close = z > zt || (z == zt && col < id);
+    }
+  }
+  close = __popc(__ballot_sync(0xffffffffu, close));
   __syncthreads();
   if (t == 0) {
     Sums y = s.sums[0];
+    y.before += close;
     for (int j = 1; j < kWarps; ++j) join(y, s.sums[j], a.scale);
     s.mine = y;
   }
   // and its best columns: the last bar leaves little more than them
   if (n > 0) {
-    const unsigned int count = s.count;
-    if (count > kCandidates) {
-      select_best<DT>(row, c0, c1, n, s.best);
-    } else {
-      bar = nvec > 0 ? s.post[0] : -INFINITY;
+    const int count = int(s.count);
+    if (count <= kVectors && nvec > 0) {
+      bar = s.post[0];
       for (int j = 1; j < kWarps; ++j) bar = fminf(bar, s.post[j]);
-      const uint32_t low = nvec > 0 ? order_key(bar) : 0;
-      unsigned long long key[kCandidates / kThreads];
-#pragma unroll
-      for (int j = 0; j < kCandidates / kThreads; ++j) {
-        const unsigned int i = j * kThreads + t;
-        key[j] = i < count ? s.found[i] : 0;
+      bar = fmaxf(bar, kLeast);
+      for (int i = t; i < count * VEC; i += kThreads) {
+        const int col = c0 + s.vecs[i / VEC] * VEC + i % VEC;
+        const float z = col < c1 ? load_logit<DT>(row, col) : -INFINITY;
+        if (z >= bar) {
+          const unsigned int p = atomicAdd(&s.kept, 1u);
+          if (p < kCandidates) s.found[p] = uint64_t(order_key(z)) << 32 | uint32_t(~col);
+        }
       }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kCandidates / kThreads; ++j)
-        if (key[j] && uint32_t(key[j] >> 32) >= low) s.found[atomicAdd(&s.kept, 1u)] = key[j];
-      __syncthreads();
-      rank_keys(s.found, s.kept, n, s.best);
     }
+    __syncthreads();
+    const int kept = int(s.kept);
+    if (count > kVectors || kept > kCandidates)
+      select_best<DT>(row, c0, c1, n, s.best);
+    else
+      rank_keys(s.found, kept, n, s.best);
   }
   // the row's, by its first CTA
   if (S > 1) {
@@ -421,6 +487,7 @@ cudaError_t launch(LogprobArgs a, cudaStream_t stream, int sm_count) {
     S *= 2;
   a.split = S;
   a.share = ((a.V + S - 1) / S + VEC - 1) / VEC * VEC;
+  a.reach = 300.f / a.scale;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(a.rows * S));
   cfg.blockDim = dim3(kThreads);

@@ -11,7 +11,8 @@ namespace {
 
 using namespace tt;
 
-bool temp_ok(float t) { return t > 0.f && std::isfinite(t); }
+// (log2(e) / T and what it scales stay within fp32)
+bool temp_ok(float t) { return t >= 1e-36f && t <= 1e36f; }
 float log2e_over(float t) { return float(1.4426950408889634 / double(t)); }
 
 int elem_size(const tt_logits* L) { return L->dtype == TT_F32 ? 4 : 2; }

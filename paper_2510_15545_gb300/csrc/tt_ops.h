@@ -27,7 +27,8 @@ struct LogprobArgs {
   int top_n;
   const int32_t* ids;
   tt_logprobs_out out;
-  int split, share;  // CTAs per row and columns of each (filled in by the launcher)
+  int split, share;  // CTAs per row and columns of each, and
+  float reach;       // 300 in the units of z (filled in by the launcher)
 };
 
 cudaError_t launch_logprobs(const LogprobArgs& args, int dt, cudaStream_t stream, int sm_count);

@@ -159,6 +159,28 @@ def test_masks(V, dtype, low):
     torch.testing.assert_close(g["lse"].cpu().double()[:5], o["lse"][:5], rtol=REL, atol=ABS)
 
 
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("temp", [1e-30, 1e-4, 0.01, 100.0, 1e30])
+@pytest.mark.parametrize("size", [1e-3, 1.0, 1e4, 1e30])
+def test_temperatures_and_sizes(dtype, temp, size):
+    """Far temperatures and logits, with and without masked columns. (The
+    entropy's terms have the rounding of d, 2^-23 |d|, where |d| < 100.)"""
+    gen = torch.Generator().manual_seed(21)
+    V = 9000
+    z = torch.randn((4, V), generator=gen) * size
+    z[1, torch.rand(V, generator=gen) < 0.5] = -math.inf
+    z[2] -= 50 * size
+    z[3, ::2] = torch.finfo(dtype).min
+    rows = rows_of(z, dtype)
+    ids = rows.float().argmax(1).int()
+    g = tt.tt_logprobs(rows, ids, temp=temp, top_n=4)
+    o = expected(rows, ids, temp, 4)
+    assert g["status"].tolist() == [0] * 4
+    assert torch.equal(g["top_ids"].cpu().long(), o["top_ids"])
+    torch.testing.assert_close(g["logprob"].cpu().double(), o["logprob"], rtol=REL, atol=ABS)
+    torch.testing.assert_close(g["entropy"].cpu().double(), o["entropy"], rtol=1e-5, atol=2e-5)
+
+
 @pytest.mark.parametrize("V", [40, 5000, 70001])
 @pytest.mark.parametrize("dtype", [F, H])
 def test_rows_that_are_not_finite(V, dtype):
