@@ -34,7 +34,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kBatch = 4;           // vectors of a thread between two looks at the bar
+constexpr int kBatch = 8;           // vectors of a thread between two looks at the bar
 constexpr int kVectors = 2048;      // room for vectors that reach the bar
 constexpr int kCandidates = 1024;   // and for columns that reach the last one
 constexpr int kMaxSplit = 16;
@@ -287,9 +287,20 @@ __global__ void __launch_bounds__(kThreads, 4)
       tail = make_uint4(bits[0] >> 16 | bits[1], bits[2] >> 16 | bits[3], bits[4] >> 16 | bits[5],
                         bits[6] >> 16 | bits[7]);
   }
-  auto load = [&](int v) {
-    if (v < whole) return ld_stream_v4(base + int64_t(v) * 16);
-    return v == whole ? tail : none;
+  // this thread's vectors of the batch at v0
+  auto load = [&](uint4 (&w)[kBatch], int v0) {
+    const char* p = base + (uint32_t(v0 + t) << 4);
+    if (v0 + kBatch * kThreads <= whole) {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) w[u] = ld_stream_v4(p + u * kThreads * 16);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int v = v0 + u * kThreads + t;
+        w[u] = v == whole ? tail : none;
+        if (v < whole) w[u] = ld_stream_v4(p + u * kThreads * 16);
+      }
+    }
   };
 
   Sums x{-INFINITY, 0.f, 0.f, 0};
@@ -303,14 +314,10 @@ __global__ void __launch_bounds__(kThreads, 4)
   const uint32_t from = logit_bits<DT>(zt), above = logit_bits<DT>(logit_above<DT>(zt));
   float bar = kLeast;
   if (t == 0) s.count = s.kept = 0;
-  uint4 w[kBatch];
-#pragma unroll
-  for (int u = 0; u < kBatch; ++u) w[u] = load(u * kThreads + t);
   int it = 0;
   for (int v0 = 0; v0 < nvec; v0 += kBatch * kThreads, ++it) {
-    uint4 next[kBatch];
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) next[u] = load(v0 + (kBatch + u) * kThreads + t);
+    uint4 w[kBatch];
+    load(w, v0);
     float vm[kBatch], top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < kBatch; ++u) {
@@ -376,8 +383,6 @@ __global__ void __launch_bounds__(kThreads, 4)
         }
       }
     }
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) w[u] = next[u];
   }
 
   // the CTA's sums
