@@ -11,16 +11,22 @@
 //
 // A row is held on chip between the two readings that the softmax needs: a
 // cluster of S CTAs takes a row, each copies its share of the columns into
-// shared memory in one bulk copy, takes the list's columns out of it, and sums
-// what is left; the CTAs give each other their sums and the list's logits
-// through distributed shared memory, and each writes its share of the gradient.
-// Logits are read from memory once, the gradient written once.
+// shared memory in bulk copies, takes the list's columns out of it, and sums
+// what is left; the CTAs give each other their sums through distributed shared
+// memory, and each writes its share of the gradient. Logits are read from memory
+// once, the gradient written once. Several CTAs share an SM, so that one's copies
+// run beside another's sums and stores; a CTA's own steps are kept few (three
+// barriers), since thousands of rows make tens of thousands of CTAs: one warp
+// reads the list while the copies are on their way, a thread takes out, and later
+// patches, the listed columns of its own vectors.
 #include <cooperative_groups.h>
 #include <cstdint>
 
 #include "tt_device.cuh"
+#include "tt_f2.cuh"
 #include "tt_ops.h"
 #include "tt_ring.cuh"
+#include "tt_x2.cuh"
 
 namespace tt {
 
@@ -28,116 +34,142 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
 constexpr int kMaxSplit = 16;
+constexpr int kSegmentGoal = 52 * 1024;
 constexpr int kSegmentMax = 200 * 1024;  // bytes of a row that a CTA holds
+constexpr int kPerLane = TT_MAX_DISTILL_K / 32;
 
-// The teacher's list of a row as every CTA of the row sees it: entries of one
-// column added up in the first of them, unusable ones dropped (col -1).
+// The list's entries within a CTA's columns, those of one column added up in the
+// first of them (the others have column -1), and the whole list's mass.
 struct List {
+  int count;
   int32_t col[TT_MAX_DISTILL_K];
   float p[TT_MAX_DISTILL_K];
   float z[TT_MAX_DISTILL_K];  // the student's logit of the column
-  float raw[TT_MAX_DISTILL_K];
-  float red[kWarps];
-  double redd[kWarps];
-  double mass;  // P
-  float rest;   // r
+  float mass, rest;           // P, r
   int status;
 };
 
-template <typename T, typename Op>
-__device__ __forceinline__ T block_reduce(T v, T* red, Op op) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
-  __syncthreads();
-  v = red[0];
-#pragma unroll
-  for (int w = 1; w < kWarps; ++w) v = op(v, red[w]);
-  return v;
-}
-struct Max {
-  __device__ float operator()(float a, float b) const { return fmaxf(a, b); }
-};
-struct Sum {
-  template <typename T>
-  __device__ T operator()(T a, T b) const { return a + b; }
+// What the CTAs of a row tell each other: sums relative to `base` (a share of
+// nothing but -inf: 0).
+struct Share {
+  float base;
+  float out;     // sum of 2^((z - base) scale) outside the list
+  float listed;  // the same on the list
+  float mass;    // sum of p on the list,
+  float cross;   // and of p (ln p - (z - base) / T)
 };
 
-// Reads the list of row r: p_i = exp(logp_i), scaled to sum 1 without tail mode.
-__device__ void read_list(const DistillArgs& a, int64_t r, List& L) {
-  const int t = threadIdx.x;
-  int id = -1;
-  float lp = -INFINITY;
-  bool off = false, odd = false;
-  if (t < a.K) {
-    id = a.ids[r * a.K + t];
-    lp = a.logp[r * a.K + t];
-    off = id < -1 || id >= a.V;
-    if (off) id = -1;
-    odd = id >= 0 && !(lp < INFINITY);  // NaN or +inf
-    if (id >= 0 && lp == -INFINITY) id = -1;
-  }
-  const float top = block_reduce(id >= 0 ? lp : -INFINITY, L.red, Max());
-  const float lead = a.tail || !(top > -INFINITY) ? 0.f : top;
-  float p = id >= 0 ? expf(lp - lead) : 0.f;
-  if (t < a.K) {
-    L.col[t] = id;
-    L.raw[t] = p;
-  }
-  double mass = block_reduce(double(p), L.redd, Sum());
-  if (!a.tail && mass > 0.0) {
-    p = float(double(p) / mass);
-    mass = 1.0;
-  }
-  const int any = __syncthreads_or(id >= 0);
-  const int bad = __syncthreads_or(odd), wrong = __syncthreads_or(off);
-  const float scale = float(p > 0.f && t < a.K ? p / L.raw[t] : 0.f);
-  bool first = id >= 0;
-  float sum = 0.f;
-  if (id >= 0) {
-    for (int j = 0; j < a.K; ++j) {
-      if (L.col[j] != id) continue;
-      if (j < t) first = false;
-      sum += L.raw[j];
+// One warp reads the list of row r for columns c0 .. c1 - 1: p = exp(logp),
+// scaled to sum 1 without tail mode.
+__device__ __forceinline__ void read_list(const DistillArgs& a, int64_t r, int c0, int c1, List& L,
+                                          int lane) {
+  int id[kPerLane];
+  float p[kPerLane];
+  bool off = false, odd = false, any = false;
+  float top = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int j = i * 32 + lane;
+    id[i] = -1;
+    p[i] = -INFINITY;
+    if (j < a.K) {
+      id[i] = a.ids[r * a.K + j];
+      p[i] = a.logp[r * a.K + j];
     }
   }
-  __syncthreads();
-  if (t < a.K) {
-    L.col[t] = first ? id : -1;
-    L.p[t] = first ? sum * scale : 0.f;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    if (id[i] < -1 || id[i] >= a.V) {
+      off = true;
+      id[i] = -1;
+    }
+    odd |= id[i] >= 0 && !(p[i] < INFINITY);  // NaN or +inf
+    if (p[i] == -INFINITY) id[i] = -1;
+    any |= id[i] >= 0;
+    if (id[i] >= 0) top = fmaxf(top, p[i]);
   }
-  if (t == 0) {
-    L.mass = mass;
-    L.rest = a.tail && any ? float(fmax(0.0, 1.0 - mass)) : 0.f;
-    L.status = (any ? 0 : TT_REQ_EMPTY) | (bad ? TT_REQ_NOT_FINITE : 0) |
-               (wrong ? TT_REQ_ID_OUT_OF_RANGE : 0);
+  const float lead = a.tail ? 0.f : warp_max_f(top);
+  F2 mass = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    p[i] = id[i] >= 0 ? expf(p[i] - lead) : 0.f;
+    mass = f2_add(mass, F2{p[i], 0.f});
   }
-  __syncthreads();
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1)
+    mass = f2_add(mass, F2{__shfl_xor_sync(0xffffffffu, mass.hi, o),
+                           __shfl_xor_sync(0xffffffffu, mass.lo, o)});
+  const float inv = a.tail || !(mass.hi > 0.f) ? 1.f : 1.f / mass.hi;
+  int n = 0;
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    if (i * 32 >= a.K) break;
+    const bool mine = id[i] >= c0 && id[i] < c1;
+    const unsigned int who = __ballot_sync(0xffffffffu, mine);
+    if (mine) {
+      const int at = n + __popc(who & ((1u << lane) - 1));
+      L.col[at] = id[i];
+      L.p[at] = p[i] * inv;
+    }
+    n += __popc(who);
+  }
+  __syncwarp();
+  // entries of one column
+  bool first[kPerLane];
+  float sum[kPerLane];
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int e = i * 32 + lane;
+    first[i] = e < n;
+    sum[i] = 0.f;
+    if (i * 32 >= n) break;
+    const int col = e < n ? L.col[e] : -1;
+    for (int j = 0; j < n; ++j) {
+      if (L.col[j] != col) continue;
+      first[i] &= j >= e;
+      sum[i] += L.p[j];
+    }
+  }
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kPerLane; ++i) {
+    const int e = i * 32 + lane;
+    if (e >= n) break;
+    L.col[e] = first[i] ? L.col[e] : -1;
+    L.p[e] = first[i] ? sum[i] : 0.f;
+  }
+  any = __any_sync(0xffffffffu, any);
+  odd = __any_sync(0xffffffffu, odd);
+  off = __any_sync(0xffffffffu, off);
+  if (lane == 0) {
+    L.count = n;
+    L.mass = a.tail ? mass.hi : any ? 1.f : 0.f;
+    L.rest = a.tail && any ? fmaxf(0.f, (1.f - mass.hi) - mass.lo) : 0.f;
+    L.status = (any ? 0 : TT_REQ_EMPTY) | (odd ? TT_REQ_NOT_FINITE : 0) |
+               (off ? TT_REQ_ID_OUT_OF_RANGE : 0);
+  }
 }
 
+// coef 2^((z - M) scale) of a vector's logits, in their type.
 template <int DT>
 __device__ __forceinline__ uint4 scaled_exp(const uint4& w, float M, float scale, float coef) {
-  if constexpr (DT == TT_F32) {
-    uint4 o;
-    o.x = __float_as_uint(coef * ex2_approx((__uint_as_float(w.x) - M) * scale));
-    o.y = __float_as_uint(coef * ex2_approx((__uint_as_float(w.y) - M) * scale));
-    o.z = __float_as_uint(coef * ex2_approx((__uint_as_float(w.z) - M) * scale));
-    o.w = __float_as_uint(coef * ex2_approx((__uint_as_float(w.w) - M) * scale));
-    return o;
-  } else {
-    uint32_t o[4];
+  const f32x2 minus = pair(-M, -M), scale2 = pair(scale, scale), coef2 = pair(coef, coef);
+  uint32_t o[4];
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-      const float lo = coef * ex2_approx((lane_elem<DT>(w, 2 * h) - M) * scale);
-      const float hi = coef * ex2_approx((lane_elem<DT>(w, 2 * h + 1) - M) * scale);
-      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[h]) : "f"(hi), "f"(lo));
+  for (int q = 0; q < (DT == TT_F32 ? 2 : 4); ++q) {
+    float lo, hi;
+    split(mul2(coef2, exp2_pair(mul2(add2(logit_pair<DT>(w, q), minus), scale2))), lo, hi);
+    if constexpr (DT == TT_F32) {
+      o[2 * q] = __float_as_uint(lo);
+      o[2 * q + 1] = __float_as_uint(hi);
+    } else {
+      asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(o[q]) : "f"(hi), "f"(lo));
     }
-    return make_uint4(o[0], o[1], o[2], o[3]);
   }
+  return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
 template <int DT>
@@ -157,32 +189,39 @@ struct Factors {
   float outside;  // (W - r / t) w / (T S): times 2^((z - M) scale), outside the list
   float listed;   // W / S
   float wt;       // w / T
+  bool none;      // gradient 0
 };
 __device__ __forceinline__ Factors factors(const DistillArgs& a, const List& L, int64_t r, float M,
                                            float S, float S_out) {
   Factors f;
   f.wt = (a.weight ? a.weight[r] : 1.f) / a.temp;
-  const float W = float(L.mass + double(L.rest));
+  const float W = L.mass + L.rest;
   f.M = M;
   f.listed = W / S;
   // (no mass outside the list: nothing there has a gradient)
   f.outside = f.wt * (S_out > 0.f ? W / S - L.rest / S_out : 0.f);
-  if (!(S > 0.f && S < INFINITY) || (L.status & (TT_REQ_EMPTY | TT_REQ_NOT_FINITE))) {
-    f.outside = f.listed = f.wt = 0.f;
-    f.M = INFINITY;  // (2^-inf for whatever the row holds)
-  }
+  f.none = f.wt == 0.f || !(S > 0.f && S < INFINITY) ||
+           (L.status & (TT_REQ_EMPTY | TT_REQ_NOT_FINITE)) != 0;
   return f;
 }
+__device__ __forceinline__ float listed_grad(const DistillArgs& a, const Factors& f, float z,
+                                             float p) {
+  return f.none ? 0.f : f.wt * (f.listed * ex2_approx((z - f.M) * a.scale) - p);
+}
 
-// The gradient of the listed columns of [c0, c1), whose logits are in L.z.
 template <int DT>
-__device__ __forceinline__ void store_listed(const DistillArgs& a, const List& L, const Factors& f,
-                                             char* grow, int c0, int c1) {
-  const int t = threadIdx.x;
-  if (t < a.K && L.col[t] >= c0 && L.col[t] < c1)
-    store_elem<DT>(grow, L.col[t],
-                   f.wt == 0.f ? 0.f
-                               : f.wt * (f.listed * ex2_approx((L.z[t] - f.M) * a.scale) - L.p[t]));
+__device__ __forceinline__ float smem_logit(const char* seg, int x) {
+  if constexpr (DT == TT_F32)
+    return reinterpret_cast<const float*>(seg)[x];
+  else
+    return bf16_to_f32(reinterpret_cast<const uint16_t*>(seg)[x]);
+}
+template <int DT>
+__device__ __forceinline__ void set_smem_logit(char* seg, int x, float z) {
+  if constexpr (DT == TT_F32)
+    reinterpret_cast<float*>(seg)[x] = z;
+  else
+    reinterpret_cast<uint16_t*>(seg)[x] = uint16_t(__float_as_uint(z) >> 16);
 }
 
 template <int DT>
@@ -192,9 +231,11 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   extern __shared__ __align__(128) char seg[];
   __shared__ List L;
   __shared__ uint64_t full;
-  __shared__ float s_max[kMaxSplit], s_sum[kMaxSplit];
+  __shared__ float2 s_ms[kWarps];
+  __shared__ Share s_share[kMaxSplit];
   const cg::cluster_group cluster = cg::this_cluster();
-  const int S = a.split, rank = S > 1 ? int(cluster.block_rank()) : 0, t = threadIdx.x;
+  const int S = a.split, rank = S > 1 ? int(cluster.block_rank()) : 0;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
   // (a CTA's shared memory is written by the others only once it runs)
   if (S > 1) cluster.barrier_arrive();
   const int64_t r = blockIdx.x / S;
@@ -202,7 +243,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   const int c0 = min(a.V, rank * a.share), c1 = min(a.V, c0 + a.share);
   const int whole = (c1 - c0) / VEC, nvec = (c1 - c0 + VEC - 1) / VEC;
   uint4* sv = reinterpret_cast<uint4*>(seg);
-  if (t == 0) {
+  if (t == kThreads - 1) {
     mbar_init(&full, 1);
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (whole > 0) {
@@ -214,102 +255,134 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   // the ragged tail (the row's last columns) with -inf behind it
   if (nvec > whole && t >= 32 && t < 32 + VEC) {
     const int x = whole * VEC + t - 32;
-    const float z = c0 + x < c1 ? load_logit<DT>(row, c0 + x) : -INFINITY;
-    if constexpr (DT == TT_F32)
-      reinterpret_cast<float*>(seg)[x] = z;
-    else
-      reinterpret_cast<uint16_t*>(seg)[x] = uint16_t(__float_as_uint(z) >> 16);
+    set_smem_logit<DT>(seg, x, c0 + x < c1 ? load_logit<DT>(row, c0 + x) : -INFINITY);
   }
-  read_list(a, r, L);
-  const uint64_t limit = kWaitLimitNs;
-  bool ok = whole == 0 || mbar_wait(&full, 0, limit);
-  ok = !__syncthreads_or(!ok);
-  if (S > 1) cluster.barrier_wait();
-  // take the list's columns out
-  float zi = -INFINITY;
-  if (t < a.K && L.col[t] >= c0 && L.col[t] < c1) {
-    const int x = L.col[t] - c0;
-    if constexpr (DT == TT_F32) {
-      float* p = reinterpret_cast<float*>(seg) + x;
-      zi = *p;
-      *p = -INFINITY;
-    } else {
-      uint16_t* p = reinterpret_cast<uint16_t*>(seg) + x;
-      zi = bf16_to_f32(*p);
-      *p = 0xff80u;
-    }
-    for (int k = 0; k < S; ++k)
-      (S > 1 ? cluster.map_shared_rank(L.z, k) : L.z)[t] = zi;
-  }
+  if (warp == 0) read_list(a, r, c0, c1, L, lane);
   __syncthreads();
+  const uint64_t limit = kWaitLimitNs;
+  const bool ok = whole == 0 || mbar_wait(&full, 0, limit);
+  // take the list's columns out of this thread's vectors
+  const int n = L.count;
+  for (int e = 0; e < n; ++e) {
+    const int x = L.col[e] - c0;
+    if (x >= 0 && (x / VEC) % kThreads == t) {
+      L.z[e] = smem_logit<DT>(seg, x);
+      set_smem_logit<DT>(seg, x, -INFINITY);
+    }
+  }
+  // their maximum, then their sum
   float m = -INFINITY;
   for (int v = t; v < nvec; v += kThreads) m = fmaxf(m, vec_max<DT>(sv[v]));
-  m = block_reduce(m, L.red, Max());
-  const float base = m > -INFINITY ? m : 0.f;
-  float sum = 0.f;
-  for (int v = t; v < nvec; v += kThreads) {
-    const uint4 w = sv[v];
+  const f32x2 scale2 = pair(a.scale, a.scale);
+  f32x2 s2 = 0;
+  {
+    const float base = m > -INFINITY ? m : 0.f;
+    const f32x2 minus = pair(-base, -base);
+    for (int v = t; v < nvec; v += kThreads) {
+      const uint4 w = sv[v];
 #pragma unroll
-    for (int q = 0; q < VEC; ++q) sum += ex2_approx((lane_elem<DT>(w, q) - base) * a.scale);
+      for (int q = 0; q < VEC / 2; ++q)
+        s2 = add2(s2, exp2_pair(mul2(add2(logit_pair<DT>(w, q), minus), scale2)));
+    }
   }
-  sum = block_reduce(sum, L.red, Sum());
-  if (!ok) sum = __int_as_float(0x7fffffff);
-  if (t < S) {
-    (S > 1 ? cluster.map_shared_rank(s_max, t) : s_max)[rank] = m;
-    (S > 1 ? cluster.map_shared_rank(s_sum, t) : s_sum)[rank] = sum;
+  float sum = ok ? sum_pair(s2) : __int_as_float(0x7fffffff);
+  {
+    const float mw = warp_max_f(m);
+    if (m > -INFINITY) sum *= ex2_approx((m - mw) * a.scale);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) s_ms[warp] = make_float2(mw, sum);
+  }
+  __syncthreads();
+  if (warp == 0) {
+    // the CTA's share, with the list's columns
+    float top = lane < kWarps ? s_ms[lane].x : -INFINITY;
+    for (int e = lane; e < n; e += 32)
+      if (L.col[e] >= 0) top = fmaxf(top, L.z[e]);
+    top = warp_max_f(top);
+    Share x;
+    x.base = top > -INFINITY ? top : 0.f;
+    x.out = x.listed = x.mass = x.cross = 0.f;
+    if (lane < kWarps) {
+      const float2 ms = s_ms[lane];
+      x.out = ms.x > -INFINITY ? ms.y * ex2_approx((ms.x - x.base) * a.scale) : ms.y;
+    }
+    for (int e = lane; e < n; e += 32) {
+      if (L.col[e] < 0) continue;
+      const float d = L.z[e] - x.base, p = L.p[e];
+      x.listed += ex2_approx(d * a.scale);
+      x.mass += p;
+      if (p > 0.f) x.cross += p * (logf(p) - d / a.temp);
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      x.out += __shfl_xor_sync(0xffffffffu, x.out, o);
+      x.listed += __shfl_xor_sync(0xffffffffu, x.listed, o);
+      x.mass += __shfl_xor_sync(0xffffffffu, x.mass, o);
+      x.cross += __shfl_xor_sync(0xffffffffu, x.cross, o);
+    }
+    if (S > 1) cluster.barrier_wait();
+    if (lane < S) (S > 1 ? cluster.map_shared_rank(s_share, lane) : s_share)[rank] = x;
+  } else if (S > 1) {
+    cluster.barrier_wait();
   }
   if (S > 1)
     cluster.sync();
   else
     __syncthreads();
   // the row's maximum and sums, the same in every CTA
-  const float zl = t < a.K && L.col[t] >= 0 ? L.z[t] : -INFINITY;
-  float M = zl;
-  if (t < S) M = fmaxf(M, s_max[t]);
-  M = block_reduce(M, L.red, Max());
-  float S_out = 0.f;
-  for (int k = 0; k < S; ++k)
-    S_out += s_max[k] > -INFINITY ? s_sum[k] * ex2_approx((s_max[k] - M) * a.scale) : s_sum[k];
-  const float S_all =
-      S_out + block_reduce(zl > -INFINITY || zl != zl ? ex2_approx((zl - M) * a.scale) : 0.f, L.red,
-                           Sum());
-  const bool finite = S_all > 0.f && S_all < INFINITY;
-  if (rank == 0) {
+  float M = s_share[0].base;
+  for (int k = 1; k < S; ++k) M = fmaxf(M, s_share[k].base);
+  float S_out = 0.f, S_all = 0.f;
+  for (int k = 0; k < S; ++k) {
+    const float f = ex2_approx((s_share[k].base - M) * a.scale);
+    S_out += s_share[k].out * f;
+    S_all += s_share[k].listed * f;
+  }
+  S_all += S_out;
+  if (rank == 0 && t == 0) {
     const float ln_s = logf(S_all);
-    float term = 0.f;
-    if (t < a.K && L.p[t] > 0.f) term = L.p[t] * (logf(L.p[t]) - ((zl - M) / a.temp - ln_s));
-    float loss = block_reduce(term, L.red, Sum());
-    if (L.rest > 0.f) loss += L.rest * (logf(L.rest) - (logf(S_out) - ln_s));
-    if (t == 0) {
-      const int st = L.status | (finite ? 0 : TT_REQ_NOT_FINITE) | (ok ? 0 : TT_REQ_TIMEOUT);
-      a.status[r] = st;
-      if (a.loss)
-        a.loss[r] = st & (TT_REQ_NOT_FINITE | TT_REQ_TIMEOUT) ? __int_as_float(0x7fffffff)
-                    : st & TT_REQ_EMPTY                       ? 0.f
-                                                              : loss;
-      if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(M, S_all, S_out, 0.f);
+    float loss = 0.f, mass = 0.f;
+    for (int k = 0; k < S; ++k) {
+      mass += s_share[k].mass;
+      loss += s_share[k].cross + s_share[k].mass * ((M - s_share[k].base) / a.temp);
     }
+    loss += mass * ln_s;
+    if (L.rest > 0.f) loss += L.rest * (logf(L.rest) - (logf(S_out) - ln_s));
+    const bool finite = S_all > 0.f && S_all < INFINITY;
+    const int st = L.status | (finite ? 0 : TT_REQ_NOT_FINITE) | (ok ? 0 : TT_REQ_TIMEOUT);
+    a.status[r] = st;
+    if (a.loss)
+      a.loss[r] = st & (TT_REQ_NOT_FINITE | TT_REQ_TIMEOUT) ? __int_as_float(0x7fffffff)
+                  : st & TT_REQ_EMPTY                       ? 0.f
+                                                            : loss;
+    if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(M, S_all, S_out, 0.f);
   }
   if (!a.grad) return;
   const Factors f = factors(a, L, r, M, S_all, S_out);
   char* grow = a.grad + r * a.grad_stride_bytes;
   uint4* out = reinterpret_cast<uint4*>(grow + int64_t(c0) * ESZ);
   for (int v = t; v < whole; v += kThreads)
-    out[v] = f.wt == 0.f ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(sv[v], f.M, a.scale, f.outside);
-  if (nvec > whole && t < c1 - c0 - whole * VEC) {
-    const int x = whole * VEC + t;
-    const float z = DT == TT_F32 ? reinterpret_cast<float*>(seg)[x]
-                                 : bf16_to_f32(reinterpret_cast<uint16_t*>(seg)[x]);
-    store_elem<DT>(grow, c0 + x, f.wt == 0.f ? 0.f : f.outside * ex2_approx((z - f.M) * a.scale));
+    out[v] = f.none ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(sv[v], f.M, a.scale, f.outside);
+  if (nvec > whole && t == whole % kThreads) {
+    for (int x = whole * VEC; x < c1 - c0; ++x)
+      store_elem<DT>(grow, c0 + x,
+                     f.none ? 0.f
+                            : f.outside * ex2_approx((smem_logit<DT>(seg, x) - f.M) * a.scale));
   }
-  __syncthreads();  // the listed columns' stores come last
-  store_listed<DT>(a, L, f, grow, c0, c1);
+  // the listed columns of this thread's vectors, after them
+  for (int e = 0; e < n; ++e) {
+    const int x = L.col[e] - c0;
+    if (x >= 0 && (x / VEC) % kThreads == t)
+      store_elem<DT>(grow, c0 + x, listed_grad(a, f, L.z[e], L.p[e]));
+  }
 }
 
 // The gradient alone, from the forward call's statistics: a CTA takes kGradVecs
-// vectors of a row, reads the listed logits among them first (the gradient may
-// take the logits' place), and streams the rest.
-constexpr int kGradVecs = 8 * kThreads;
+// vectors of a row, all of them loaded before the first is written (the gradient
+// may take the logits' place).
+constexpr int kPerThread = 8;
+constexpr int kGradVecs = kPerThread * kThreads;
 
 template <int DT>
 __global__ void __launch_bounds__(kThreads) distill_grad_kernel(
@@ -323,32 +396,54 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(
   const int c0 = int(blockIdx.x % parts) * kGradVecs * VEC, c1 = min(a.V, c0 + kGradVecs * VEC);
   const char* row = a.data + r * a.stride_bytes;
   char* grow = a.grad + r * a.grad_stride_bytes;
-  read_list(a, r, L);
-  const float4 st = reinterpret_cast<const float4*>(a.stats)[r];
-  if (t < a.K && L.col[t] >= c0 && L.col[t] < c1) L.z[t] = load_logit<DT>(row, L.col[t]);
   const int whole = (c1 - c0) / VEC;
-  const int x = whole * VEC + t;
-  const float z = c0 + x < c1 ? load_logit<DT>(row, c0 + x) : 0.f;  // (t < VEC: the tail)
+  const char* in = row + int64_t(c0) * ESZ;
+  uint4 w[kPerThread];
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const int v = u * kThreads + t;
+    w[u] = v < whole ? ld_stream_v4(in + v * 16) : make_uint4(0, 0, 0, 0);
+  }
+  const bool ragged = t == whole % kThreads;  // the thread of the row's last columns
+  float z_tail[VEC];
+  if (ragged)
+    for (int q = 0; q < VEC; ++q)
+      z_tail[q] = c0 + whole * VEC + q < c1 ? load_logit<DT>(row, c0 + whole * VEC + q) : 0.f;
+  const float4 st = reinterpret_cast<const float4*>(a.stats)[r];
+  if (t < 32) {
+    read_list(a, r, c0, c1, L, t);
+    __syncwarp();
+    for (int e = t; e < L.count; e += 32)
+      if (L.col[e] >= 0) L.z[e] = load_logit<DT>(row, L.col[e]);
+  }
   __syncthreads();
   const Factors f = factors(a, L, r, st.x, st.y, st.z);
-  const uint4* in = reinterpret_cast<const uint4*>(row + int64_t(c0) * ESZ);
   uint4* out = reinterpret_cast<uint4*>(grow + int64_t(c0) * ESZ);
-  for (int v = t; v < whole; v += kThreads)
-    out[v] = f.wt == 0.f ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(in[v], f.M, a.scale, f.outside);
-  if (t < VEC && c0 + x < c1)
-    store_elem<DT>(grow, c0 + x, f.wt == 0.f ? 0.f : f.outside * ex2_approx((z - f.M) * a.scale));
-  __syncthreads();
-  store_listed<DT>(a, L, f, grow, c0, c1);
+#pragma unroll
+  for (int u = 0; u < kPerThread; ++u) {
+    const int v = u * kThreads + t;
+    if (v < whole)
+      out[v] = f.none ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(w[u], f.M, a.scale, f.outside);
+  }
+  if (ragged)
+    for (int q = 0; q < VEC; ++q)
+      if (c0 + whole * VEC + q < c1)
+        store_elem<DT>(grow, c0 + whole * VEC + q,
+                       f.none ? 0.f : f.outside * ex2_approx((z_tail[q] - f.M) * a.scale));
+  for (int e = 0; e < L.count; ++e) {
+    const int x = L.col[e] - c0;
+    if (x >= 0 && (x / VEC) % kThreads == t)
+      store_elem<DT>(grow, c0 + x, listed_grad(a, f, L.z[e], L.p[e]));
+  }
 }
 
 template <int DT>
 cudaError_t launch(DistillArgs a, cudaStream_t stream) {
   constexpr int VEC = DT == TT_F32 ? 4 : 8;
   constexpr int ESZ = 16 / VEC;
-  // the fewest CTAs whose shares fit
   int S = 1;
   auto share = [&](int s) { return ((a.V + s - 1) / s + VEC - 1) / VEC * VEC; };
-  while (S < kMaxSplit && share(S) * ESZ > kSegmentMax) S *= 2;
+  while (S < kMaxSplit && share(S) * ESZ > kSegmentGoal) S *= 2;
   a.split = S;
   a.share = share(S);
   cudaLaunchConfig_t cfg = {};
