@@ -39,6 +39,7 @@ constexpr int kWarps = kThreads / 32;
 constexpr int kMaxSplit = 16;
 constexpr int kSegmentGoal = 52 * 1024;
 constexpr int kSegmentMax = 200 * 1024;  // bytes of a row that a CTA holds
+constexpr int kStep = 4;  // vectors of a thread summed at once
 constexpr int kPerLane = TT_MAX_DISTILL_K / 32;
 
 // The list's entries within a CTA's columns, those of one column added up in the
@@ -270,19 +271,31 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
       set_smem_logit<DT>(seg, x, -INFINITY);
     }
   }
-  // their maximum, then their sum
+  // their maximum and, relative to it, their sum
   float m = -INFINITY;
-  for (int v = t; v < nvec; v += kThreads) m = fmaxf(m, vec_max<DT>(sv[v]));
   const f32x2 scale2 = pair(a.scale, a.scale);
-  f32x2 s2 = 0;
-  {
-    const float base = m > -INFINITY ? m : 0.f;
-    const f32x2 minus = pair(-base, -base);
-    for (int v = t; v < nvec; v += kThreads) {
-      const uint4 w = sv[v];
+  f32x2 s2 = 0, minus = 0;
+  constexpr uint32_t kNone = DT == TT_F32 ? 0xff800000u : 0xff80ff80u;
+  for (int v0 = t; v0 < nvec; v0 += kStep * kThreads) {
+    uint4 w[kStep];
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
+      w[u] = v0 + u * kThreads < nvec ? sv[v0 + u * kThreads]
+                                      : make_uint4(kNone, kNone, kNone, kNone);
+      top = fmaxf(top, vec_max<DT>(w[u]));
+    }
+    if (top > m) {
+      const float f = ex2_approx((m - top) * a.scale);
+      s2 = mul2(s2, pair(f, f));
+      m = top;
+      minus = pair(-top, -top);
+    }
+#pragma unroll
+    for (int u = 0; u < kStep; ++u) {
 #pragma unroll
       for (int q = 0; q < VEC / 2; ++q)
-        s2 = add2(s2, exp2_pair(mul2(add2(logit_pair<DT>(w, q), minus), scale2)));
+        s2 = add2(s2, exp2_pair(mul2(add2(logit_pair<DT>(w[u], q), minus), scale2)));
     }
   }
   float sum = ok ? sum_pair(s2) : __int_as_float(0x7fffffff);
@@ -362,8 +375,13 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   const Factors f = factors(a, L, r, M, S_all, S_out);
   char* grow = a.grad + r * a.grad_stride_bytes;
   uint4* out = reinterpret_cast<uint4*>(grow + int64_t(c0) * ESZ);
-  for (int v = t; v < whole; v += kThreads)
-    out[v] = f.none ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(sv[v], f.M, a.scale, f.outside);
+  if (f.none) {
+    for (int v = t; v < whole; v += kThreads) out[v] = make_uint4(0, 0, 0, 0);
+  } else {
+#pragma unroll 4
+    for (int v = t; v < whole; v += kThreads)
+      out[v] = scaled_exp<DT>(sv[v], f.M, a.scale, f.outside);
+  }
   if (nvec > whole && t == whole % kThreads) {
     for (int x = whole * VEC; x < c1 - c0; ++x)
       store_elem<DT>(grow, c0 + x,
