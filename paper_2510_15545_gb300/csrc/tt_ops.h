@@ -52,7 +52,7 @@ struct DistillArgs {
 };
 
 int distill_max_cols(int dt);
-cudaError_t launch_distill(const DistillArgs& args, int dt, cudaStream_t stream);
+cudaError_t launch_distill(const DistillArgs& args, int dt, cudaStream_t stream, int sm_count);
 cudaError_t launch_distill_grad(const DistillArgs& args, int dt, cudaStream_t stream);
 cudaError_t preload_distill();
 
