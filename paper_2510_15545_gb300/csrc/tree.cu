@@ -25,6 +25,7 @@
 #include <cstdint>
 #include <cstring>
 #include <numeric>
+#include <type_traits>
 
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -34,6 +35,7 @@
 #include "tt_ops.h"
 #include "tt_ring.cuh"
 #include "tt_umma.cuh"
+#include "tt_x2.cuh"
 
 namespace tt {
 
@@ -42,9 +44,8 @@ namespace {
 constexpr int kTile = 128;               // keys of a tile, rows of a CTA
 constexpr int kRowWarps = 4;
 constexpr int kThreads = (kRowWarps + 2) * 32;
-constexpr int kTmemColumns = 256;        // scores and weights: 128, output: up to 128
+constexpr int kTmemColumns = 256;        // of tensor memory: two CTAs of an SM fit
 constexpr int kWords = TT_MAX_TREE / 32;
-constexpr int kOut = 128;                // tensor memory column of the output
 constexpr float kLn2 = 0.693147180559945f;
 // A row's reference maximum follows its maximum once that is 2^kSlack above it:
 // weights stay below 2^(kSlack + offset), and the output is scaled rarely.
@@ -109,6 +110,11 @@ __device__ bool out_of_range(const TreeArgs& a, int b, const Request& r, int t) 
 template <int D>
 struct Smem {
   static constexpr int kStages = D == 128 ? 1 : 2;  // two CTAs of an SM fit
+  // Tensor memory: scores in columns 0 .. 127, weights, output. Narrow heads leave
+  // room for weights of their own, and the next tile's scores are computed while
+  // this one's weights are; else the weights take the scores' place.
+  static constexpr bool kOwn = D == 64;
+  static constexpr int kWeights = kOwn ? 128 : 0, kOut = kOwn ? 192 : 128;
   char q[kTile * D * 2];
   char k[kStages][kTile * D * 2];
   char v[kStages][kTile * D * 2];
@@ -116,7 +122,7 @@ struct Smem {
   int16_t up[TT_MAX_TREE];       // parents, -1 for roots
   uint32_t odd[kWords];          // drafted tokens with a value that is not finite
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  uint64_t s_full, p_full, o_full;
+  uint64_t s_full, s_free, p_full, o_done;
   uint32_t tmem;
   int failed;
 };
@@ -183,8 +189,9 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_init(&s.v_empty[i], 1);
     }
     mbar_init(&s.s_full, 1);
+    mbar_init(&s.s_free, kRowWarps * 32);
     mbar_init(&s.p_full, kRowWarps * 32);
-    mbar_init(&s.o_full, 1);
+    mbar_init(&s.o_done, 1);
     s.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
@@ -265,18 +272,17 @@ __global__ void __launch_bounds__(kThreads, 2)
     // ---------------------------------------------------------- products
     if (lane == 0) {
       const uint32_t idesc_o = umma_idesc(F16, D, true);
-      ok = mbar_wait(&s.q_full, 0, limit);
-      for (int j = tile0; j < tile1 && ok; ++j) {
-        const int it = j - tile0, st = it % S::kStages;
-        const uint32_t parity = (it / S::kStages) & 1;
-        // keys of the tile in use, up to a multiple of 32
+      // keys of tile j in use, up to a multiple of 32
+      auto keys = [&](int j) {
         const int left = j < n_cache ? r.len - j * kTile : node1 - (j - n_cache) * kTile;
-        const int n = min(kTile, (left + 31) & ~31);
-        ok = mbar_wait(&s.k_full[st], parity, limit);
-        if (!ok) break;
+        return min(kTile, (left + 31) & ~31);
+      };
+      auto scores = [&](int j) {
+        const int it = j - tile0, st = it % S::kStages;
+        if (!mbar_wait(&s.k_full[st], (it / S::kStages) & 1, limit)) return false;
         tc_fence_after();
-        const uint32_t idesc_s = umma_idesc(F16, n, false);
-        const uint32_t qa = smem_u32(s.q), ka = smem_u32(s.k[st]), va = smem_u32(s.v[st]);
+        const uint32_t idesc_s = umma_idesc(F16, keys(j), false);
+        const uint32_t qa = smem_u32(s.q), ka = smem_u32(s.k[st]);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           const uint32_t at = (c / 4) * kBlock + (c % 4) * 32;
@@ -284,15 +290,29 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         umma_commit(&s.s_full);
         umma_commit(&s.k_empty[st]);
-        ok = mbar_wait(&s.v_full[st], parity, limit) && mbar_wait(&s.p_full, it & 1, limit);
+        return true;
+      };
+      ok = mbar_wait(&s.q_full, 0, limit) && scores(tile0);
+      for (int j = tile0; j < tile1 && ok; ++j) {
+        const int it = j - tile0, st = it % S::kStages;
+        // (scores read by all rows: the next ones may take their place)
+        if (S::kOwn && j + 1 < tile1) {
+          ok = mbar_wait(&s.s_free, it & 1, limit) && scores(j + 1);
+          if (!ok) break;
+        }
+        ok = mbar_wait(&s.v_full[st], (it / S::kStages) & 1, limit) &&
+             mbar_wait(&s.p_full, it & 1, limit);
         if (!ok) break;
         tc_fence_after();
-        for (int c = 0; c < n / 16; ++c)
-          umma_ts(tmem + kOut, tmem + 8 * c, umma_desc(va + c * 2048, kBlock), idesc_o,
-                  it > 0 || c > 0);
+        const uint32_t va = smem_u32(s.v[st]);
+        const int steps = keys(j) / 16;
+        for (int c = 0; c < steps; ++c)
+          umma_ts(tmem + S::kOut, tmem + S::kWeights + 8 * c, umma_desc(va + c * 2048, kBlock),
+                  idesc_o, it > 0 || c > 0);
+        umma_commit(&s.o_done);
         umma_commit(&s.v_empty[st]);
+        if (!S::kOwn && j + 1 < tile1) ok = scores(j + 1);
       }
-      if (ok) umma_commit(&s.o_full);
     }
   } else {
     // -------------------------------------------------------------- rows
@@ -340,67 +360,87 @@ __global__ void __launch_bounds__(kThreads, 2)
       // (the warp goes on, or gives up, as one)
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
       tc_fence_after();
+      // (Rolled loops: unrolled over the tile, this code no longer fits the
+      // instruction cache beside the other warps', and a call takes half as long again.)
+      bool raised = false;
+      float f = 1.f;
       if (some) {
-        uint32_t v[32];
-        float top = -INFINITY;
+        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll 1
         for (int c = 0; c < n; c += 32) {
+          uint32_t v[32];
           tmem_ld32(mine + c, v);
+          const uint32_t see = sees(c);
           tmem_wait_ld(v);
-          const uint32_t w = sees(c);
-          if (w == 0xffffffffu) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
-          } else {
+          if (see != 0xffffffffu) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (w >> i & 1) top = fmaxf(top, __uint_as_float(v[i]));
+              if (!(see >> i & 1)) v[i] = 0xff800000u;
           }
           __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i]));
         }
+        const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         // the reference follows the maximum, and with it the sums
-        const bool raise = (top - m) * p.scale2 > kSlack || (m == -INFINITY && top > -INFINITY);
-        if (__any_sync(0xffffffffu, raise)) {
-          const float to = fmaxf(m, top);
-          const float f = m == -INFINITY ? 0.f : ex2_approx((m - to) * p.scale2);
+        const bool raise = (high - m) * p.scale2 > kSlack || (m == -INFINITY && high > -INFINITY);
+        raised = __any_sync(0xffffffffu, raise);
+        if (raised) {
+          const float to = fmaxf(m, high);
+          f = m == -INFINITY ? 0.f : ex2_approx((m - to) * p.scale2);
           m = to;
           l *= f;
-          if (it > 0) {
+        }
+      }
+      // The last tile's product is in the output and done with its weights. (Every
+      // warp waits for it, or one without rows would be a tile ahead on p_full.)
+      if (S::kOwn && it > 0) {
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
+        tc_fence_after();
+      }
+      if (some) {
+        if (raised && it > 0) {
+#pragma unroll 1
+          for (int c = 0; c < D; c += 32) {
+            uint32_t o[32];
+            tmem_ld32(mine + S::kOut + c, o);
+            tmem_wait_ld(o);
 #pragma unroll
-            for (int c = 0; c < D; c += 32) {
-              tmem_ld32(mine + kOut + c, v);
-              tmem_wait_ld(v);
-#pragma unroll
-              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-              tmem_st32(mine + kOut + c, v);
-            }
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st32(mine + S::kOut + c, o);
           }
         }
         const float shift = (m == -INFINITY ? 0.f : -m * p.scale2) + kOffset;
+        const f32x2 scale2 = pair(p.scale2, p.scale2), shift2 = pair(shift, shift);
+        f32x2 sum2 = 0;
+#pragma unroll 1
         for (int c = 0; c < n; c += 32) {
+          uint32_t v[32], w[16];
           tmem_ld32(mine + c, v);
+          const uint32_t see = sees(c);
           tmem_wait_ld(v);
-          const uint32_t w = sees(c);
-          if (w != 0xffffffffu) {
+          if (see != 0xffffffffu) {
 #pragma unroll
             for (int i = 0; i < 32; ++i)
-              if (!(w >> i & 1)) v[i] = 0xff800000u;
+              if (!(see >> i & 1)) v[i] = 0xff800000u;
           }
           __syncwarp();
-          uint32_t o[16];
-          float l0 = 0.f, l1 = 0.f;
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
-            const float e0 = ex2_approx(fmaf(__uint_as_float(v[2 * i]), p.scale2, shift));
-            const float e1 = ex2_approx(fmaf(__uint_as_float(v[2 * i + 1]), p.scale2, shift));
-            l0 += e0;
-            l1 += e1;
-            o[i] = pack2<F16>(e0, e1);
+            const f32x2 e = exp2_pair(
+                fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale2, shift2));
+            sum2 = add2(sum2, e);
+            float lo, hi;
+            split(e, lo, hi);
+            w[i] = pack2<F16>(lo, hi);
           }
-          l += l0 + l1;
-          tmem_st16(mine + c / 2, o);
+          tmem_st16(mine + S::kWeights + c / 2, w);
         }
+        l += sum_pair(sum2);
         tmem_wait_st();
+        tc_fence_before();
       }
+      if (S::kOwn) mbar_arrive(&s.s_free);
       // Values that no row may touch: slots past the end (0 times what is there
       // could be NaN), and of drafted tokens, what is not finite: a token outside
       // its branch would get NaN from it. (Its own branch gets it at the end.)
@@ -435,7 +475,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       tc_fence_before();
       mbar_arrive(&s.p_full);
     }
-    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s.o_full, 0, limit));
+    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (tile1 - tile0 - 1) & 1, limit));
     tc_fence_after();
     if (has_tree) asm volatile("bar.sync 1, 128;" ::: "memory");  // (s.odd is whole)
     if (ok && some) {
@@ -447,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       const int64_t at = (int64_t(run) * a.n_nodes * a.Hq + row) * D;
       for (int c = 0; c < D; c += 32) {
         uint32_t v[32];
-        tmem_ld32(mine + kOut + c, v);
+        tmem_ld32(mine + S::kOut + c, v);
         tmem_wait_ld(v);
         if (valid) {
           if (has_tree) {
@@ -506,19 +546,24 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Joins the runs of every row that has more than one: with M the largest of the
-// runs' references, out = sum 2^(m - M) o / sum 2^(m - M) l. A warp per row.
+// runs' references, out = sum 2^(m - M) o / sum 2^(m - M) l. A CTA per row, its
+// warps take the runs in turn; each warp reads a run's output in one go.
+constexpr int kJoinWarps = 4;
+
 template <int D, bool F16>
-__global__ void __launch_bounds__(256) tree_join_kernel(const __grid_constant__ TreeKernelArgs p) {
+__global__ void __launch_bounds__(kJoinWarps * 32)
+    tree_join_kernel(const __grid_constant__ TreeKernelArgs p) {
+  constexpr int N = D / 32;
+  using Vec = typename std::conditional<N == 4, float4, float2>::type;
+  __shared__ float s_acc[kJoinWarps][D];
+  __shared__ float s_l[kJoinWarps];
   const TreeArgs& a = p.a;
-  const int lane = threadIdx.x & 31;
-  const int64_t w = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   grid_dependency_wait();
-  // row w of the B * max_nodes * Hq that there may be
-  const int h = int(w % a.Hq);
-  const int i = int(w / a.Hq % a.max_nodes);
-  const int64_t b = w / a.Hq / a.max_nodes;
-  if (b >= a.B) return;
-  const Request r = request(a, int(b));
+  // row blockIdx.x of the B * max_nodes * Hq that there may be
+  const int h = int(blockIdx.x % a.Hq), i = int(blockIdx.x / a.Hq % a.max_nodes);
+  const int b = int(blockIdx.x / a.Hq / a.max_nodes);
+  const Request r = request(a, b);
   if (i >= r.nodes) return;
   const int end = min(r.nodes, (i / p.per_tile + 1) * p.per_tile);
   const int runs = run_count(cache_tiles(r.len) + tree_tiles(end), p.run);
@@ -527,30 +572,46 @@ __global__ void __launch_bounds__(256) tree_join_kernel(const __grid_constant__ 
   float M = -INFINITY;
   for (int s = lane; s < runs; s += 32) M = fmaxf(M, p.part_ml[s * rows + row].x);
   M = warp_max_f(M);
-  constexpr int N = D / 32;
   float acc[N] = {};
   float l = 0.f;
-  for (int s = 0; s < runs; ++s) {
+#pragma unroll 4
+  for (int s = warp; s < runs; s += kJoinWarps) {
     const float2 ml = p.part_ml[s * rows + row];
+    const Vec o = reinterpret_cast<const Vec*>(p.part + (s * rows + row) * D)[lane];
+    // (a run of nothing but -inf scores: 0, whatever the maximum is)
     const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
-    if (f == 0.f && ml.y == ml.y) continue;
     l = fmaf(ml.y, f, l);
-    const float* o = p.part + (s * rows + row) * D + lane * N;
-#pragma unroll
-    for (int c = 0; c < N; ++c) acc[c] = fmaf(o[c], f, acc[c]);
+    acc[0] = fmaf(o.x, f, acc[0]);
+    acc[1] = fmaf(o.y, f, acc[1]);
+    if constexpr (N == 4) {
+      acc[2] = fmaf(o.z, f, acc[2]);
+      acc[3] = fmaf(o.w, f, acc[3]);
+    }
   }
+#pragma unroll
+  for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[c];
+  if (lane == 0) s_l[warp] = l;
+  __syncthreads();
+  l = s_l[0];
+#pragma unroll
+  for (int w = 1; w < kJoinWarps; ++w) l += s_l[w];
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-  uint32_t o[N / 2];
+  for (int c = threadIdx.x; c < D / 2; c += kJoinWarps * 32) {
+    float lo = s_acc[0][2 * c], hi = s_acc[0][2 * c + 1];
 #pragma unroll
-  for (int c = 0; c < N / 2; ++c) o[c] = pack2<F16>(acc[2 * c] * inv, acc[2 * c + 1] * inv);
-  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
-#pragma unroll
-  for (int c = 0; c < N / 2; ++c) out[c] = o[c];
-  if (a.lse && lane == 0) a.lse[row] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
+    for (int w = 1; w < kJoinWarps; ++w) {
+      lo += s_acc[w][2 * c];
+      hi += s_acc[w][2 * c + 1];
+    }
+    reinterpret_cast<uint32_t*>(a.out + row * D * 2)[c] = pack2<F16>(lo * inv, hi * inv);
+  }
+  if (a.lse && threadIdx.x == 0)
+    a.lse[row] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
 }
 
 // ------------------------------------------------------------------- host
 
+constexpr int kMinRun = 4, kWaves = 2;
 // How a call is cut: tokens per tile of rows, tiles per run, runs.
 struct Cut {
   int group, per_tile, row_tiles, run, runs;
@@ -563,7 +624,7 @@ Cut cut(const TreeArgs& a, int sm_count) {
   c.row_tiles = (a.max_nodes + c.per_tile - 1) / c.per_tile;
   const int tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);
   const int64_t items = int64_t(a.B) * a.Hkv * c.row_tiles, slots = 2 * int64_t(sm_count);
-  c.run = int(std::max<int64_t>(1, std::min<int64_t>(tiles, items * tiles / (slots * 4))));
+  c.run = int(std::max<int64_t>(kMinRun, (items * tiles + slots * kWaves - 1) / (slots * kWaves)));
   c.runs = run_count(tiles, c.run);
   const size_t rows = size_t(c.runs) * a.n_nodes * a.Hq;
   c.part_bytes = c.runs > 1 ? align256(rows * a.D * sizeof(float)) : 0;
@@ -617,8 +678,8 @@ cudaError_t launch(const TreeKernelArgs& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(unsigned((int64_t(a.B) * a.max_nodes * a.Hq + 7) / 8));
-  cfg.blockDim = dim3(256);
+  cfg.gridDim = dim3(unsigned(int64_t(a.B) * a.max_nodes * a.Hq));
+  cfg.blockDim = dim3(kJoinWarps * 32);
   cfg.dynamicSmemBytes = 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
