@@ -13,10 +13,13 @@
 // the tiles through L2) over a run of tiles, the request's cache first, then its
 // own drafted tokens, on which each row's ancestors are a bit mask. One warp
 // copies tiles in (a page at a time), one issues the two products per tile, and
-// four hold one row per thread: scores come from tensor memory, the weights go
+// eight hold the rows: scores come from tensor memory, the weights go
 // back over them in the inputs' type as the second product's operand. Two CTAs
 // share an SM, so that one's softmax runs beside the other's products and copies.
-// Long caches are split into runs, whose results a second kernel joins.
+// A tile's way from scores to weights is mostly waiting (for tensor memory, for
+// the special function unit): two threads share a row, one for each half of the
+// tile's keys, read their scores once, and agree on the maximum through shared
+// memory. Long caches are split into runs, whose results a second kernel joins.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -42,7 +45,8 @@ namespace tt {
 namespace {
 
 constexpr int kTile = 128;               // keys of a tile, rows of a CTA
-constexpr int kRowWarps = 4;
+constexpr int kRowWarps = 8;              // two for each 32 rows
+constexpr int kRowThreads = kRowWarps * 32;
 constexpr int kThreads = (kRowWarps + 2) * 32;
 constexpr int kTmemColumns = 256;        // of tensor memory: two CTAs of an SM fit
 constexpr int kWords = TT_MAX_TREE / 32;
@@ -91,16 +95,16 @@ __host__ __device__ inline int cache_tiles(int len) { return len / kTile + (len 
 __host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / kTile; }
 __host__ __device__ inline int run_count(int tiles, int run) { return (tiles + run - 1) / run; }
 
-// Whether every parent and page of the request is in range (threads 0 .. 127).
+// Whether every parent and page of the request is in range (the row threads).
 __device__ bool out_of_range(const TreeArgs& a, int b, const Request& r, int t) {
   bool bad = false;
   if (a.parents)
-    for (int i = t; i < r.nodes; i += kTile) {
+    for (int i = t; i < r.nodes; i += kRowThreads) {
       const int p = a.parents[r.first + i];
       bad |= p < -1 || p >= i;
     }
   const int pages = r.len / a.page_size + (r.len % a.page_size != 0);
-  for (int x = t; x < pages; x += kTile) {
+  for (int x = t; x < pages; x += kRowThreads) {
     const int p = a.page_table[b * a.table_stride + x];
     bad |= p < 0 || p >= a.n_pages;
   }
@@ -114,12 +118,18 @@ struct Smem {
   // room for weights of their own, and the next tile's scores are computed while
   // this one's weights are; else the weights take the scores' place.
   static constexpr bool kOwn = D == 64;
-  static constexpr int kWeights = kOwn ? 128 : 0, kOut = kOwn ? 192 : 128;
+  static constexpr int kOut = kOwn ? 192 : 128;
+  // the column of the weights of key c, two keys to a column (in the scores' place:
+  // each half of the tile where its own scores are)
+  static __device__ __forceinline__ int weights(int c) {
+    return kOwn ? 128 + c / 2 : (c & 64) + (c & 63) / 2;
+  }
   char q[kTile * D * 2];
   char k[kStages][kTile * D * 2];
   char v[kStages][kTile * D * 2];
   uint32_t seen[kTile][kWords];  // a token's ancestors and itself
   int16_t up[TT_MAX_TREE];       // parents, -1 for roots
+  float half[2][2][kTile];       // what the two threads of a row tell each other
   uint32_t odd[kWords];          // drafted tokens with a value that is not finite
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t s_full, s_free, p_full, o_done;
@@ -142,6 +152,27 @@ __device__ __forceinline__ float unpack(uint16_t x) {
     return __half2float(__ushort_as_half(x));
   else
     return bf16_to_f32(x);
+}
+
+// -inf in place of the scores whose bit is not set.
+__device__ __forceinline__ void hide(uint32_t (&v)[32], uint32_t see) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (!(see >> i & 1)) v[i] = 0xff800000u;
+}
+
+// 32 bytes to memory: one store where they are known to start on 32 bytes (the
+// runs' outputs), two of 16 for the caller's output.
+template <bool TWO>
+__device__ __forceinline__ void store_sector(char* to, const uint32_t (&o)[8]) {
+  if constexpr (TWO) {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  } else {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(o[0]),
+                 "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
+                 : "memory");
+  }
 }
 
 template <int D, bool F16>
@@ -171,7 +202,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   const bool reports = run == 0 && hk == 0 && mt == 0;
   if (run >= runs) {  // nothing here, but perhaps the request's status
     if (reports) {
-      const bool bad = !r.status && t < kTile && out_of_range(a, b, r, t);
+      const bool bad = !r.status && t < kRowThreads && out_of_range(a, b, r, t);
       const int any = __syncthreads_or(bad);
       if (t == 0) a.status[b] = r.status | (any ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
@@ -180,7 +211,60 @@ __global__ void __launch_bounds__(kThreads, 2)
   const int tile0 = int(int64_t(run) * tiles / runs), tile1 = int(int64_t(run + 1) * tiles / runs);
   const uint64_t limit = kWaitLimitNs;
 
-  if (t == 0) {
+  // The copying warp's part: lane i copies a tile's i-th box of slots. The first
+  // tile is on its way before the CTA has its tensor memory.
+  int page = -1;
+  const int per = kTile / p.box;
+  auto page_of = [&](int tile) {
+    const int slot = tile * kTile + lane * p.box;
+    return tile < min(tile1, n_cache) && lane < per && slot < r.len
+               ? a.page_table[b * a.table_stride + slot / a.page_size]
+               : -1;
+  };
+  auto copy_tile = [&](int j) {
+    const int it = j - tile0, st = it % S::kStages;
+    const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
+    const int next = page_of(j + 1);
+    const bool cache = j < n_cache;
+    bool mine;
+    int bytes, at;
+    if (cache) {
+      mine = page >= 0 && page < a.n_pages;
+      bytes = p.box * 128;
+      at = lane * p.box;
+    } else {
+      at = lane * 16;
+      mine = lane < kTile / 16 && (j - n_cache) * kTile + at < node1;
+      bytes = 16 * 128;
+    }
+    const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
+    auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* paged, const CUtensorMap* own) {
+      if (lane == 0) mbar_arrive_expect_tx(bar, boxes * bytes * kHalves);
+      __syncwarp();
+      if (!mine) return;
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        const uint32_t to = smem_u32(dst) + h * kBlock + at * 128;
+        if (cache) {
+          const int slot = (j * kTile + at) % a.page_size;
+          tma_load_4d(to, paged, smem_u32(bar), 64 * h, p.slots_inner ? slot : hk,
+                      p.slots_inner ? hk : slot, page);
+        } else {
+          tma_load_3d(to, own, smem_u32(bar), 64 * h, hk, r.first + (j - n_cache) * kTile + at);
+        }
+      }
+    };
+    if (!__all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit))) return false;
+    copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
+    __syncwarp();
+    if (!__all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit))) return false;
+    copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
+    __syncwarp();
+    page = next;
+    return true;
+  };
+
+  if (t == kRowThreads) {
     mbar_init(&s.q_full, 1);
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&s.k_full[i], 1);
@@ -189,11 +273,23 @@ __global__ void __launch_bounds__(kThreads, 2)
       mbar_init(&s.v_empty[i], 1);
     }
     mbar_init(&s.s_full, 1);
-    mbar_init(&s.s_free, kRowWarps * 32);
-    mbar_init(&s.p_full, kRowWarps * 32);
+    mbar_init(&s.s_free, kRowThreads);
+    mbar_init(&s.p_full, kRowThreads);
     mbar_init(&s.o_done, 1);
     s.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  bool ok = true;
+  if (warp == kRowWarps) {
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&s.q_full, kHalves * p.per_tile * p.group * 128);
+      for (int h = 0; h < kHalves; ++h)
+        tma_load_3d(smem_u32(s.q) + h * kBlock, &p.q, smem_u32(&s.q_full), 64 * h, hk * p.group,
+                    r.first + node0);
+    }
+    page = page_of(tile0);
+    ok = copy_tile(tile0);
   }
   if (warp == kRowWarps + 1) tmem_alloc(&s.tmem, kTmemColumns);
   const bool has_tree = tile1 > n_cache;
@@ -208,66 +304,10 @@ __global__ void __launch_bounds__(kThreads, 2)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s.tmem;
-  bool ok = true;
 
   if (warp == kRowWarps) {
     // ------------------------------------------------------------ copies
-    if (lane == 0) {
-      mbar_arrive_expect_tx(&s.q_full, kHalves * p.per_tile * p.group * 128);
-      for (int h = 0; h < kHalves; ++h)
-        tma_load_3d(smem_u32(s.q) + h * kBlock, &p.q, smem_u32(&s.q_full), 64 * h, hk * p.group,
-                    r.first + node0);
-    }
-    // lane i copies the tile's i-th box of slots
-    const int per = kTile / p.box;
-    auto page_of = [&](int tile) {
-      const int slot = tile * kTile + lane * p.box;
-      return tile < min(tile1, n_cache) && lane < per && slot < r.len
-                 ? a.page_table[b * a.table_stride + slot / a.page_size]
-                 : -1;
-    };
-    int page = page_of(tile0);
-    for (int j = tile0; j < tile1 && ok; ++j) {
-      const int it = j - tile0, st = it % S::kStages;
-      const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
-      const int next = page_of(j + 1);
-      const bool cache = j < n_cache;
-      bool mine;
-      int bytes, at;
-      if (cache) {
-        mine = page >= 0 && page < a.n_pages;
-        bytes = p.box * 128;
-        at = lane * p.box;
-      } else {
-        at = lane * 16;
-        mine = lane < kTile / 16 && (j - n_cache) * kTile + at < node1;
-        bytes = 16 * 128;
-      }
-      const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
-      auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* paged, const CUtensorMap* own) {
-        if (lane == 0) mbar_arrive_expect_tx(bar, boxes * bytes * kHalves);
-        __syncwarp();
-        if (!mine) return;
-#pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
-          const uint32_t to = smem_u32(dst) + h * kBlock + at * 128;
-          if (cache) {
-            const int slot = (j * kTile + at) % a.page_size;
-            tma_load_4d(to, paged, smem_u32(bar), 64 * h, p.slots_inner ? slot : hk,
-                        p.slots_inner ? hk : slot, page);
-          } else {
-            tma_load_3d(to, own, smem_u32(bar), 64 * h, hk, r.first + (j - n_cache) * kTile + at);
-          }
-        }
-      };
-      ok = mbar_wait(&s.k_empty[st], parity, limit);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
-      ok = mbar_wait(&s.v_empty[st], parity, limit);
-      if (!__all_sync(0xffffffffu, ok)) break;
-      copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
-      page = next;
-    }
+    for (int j = tile0 + 1; j < tile1 && ok; ++j) ok = copy_tile(j);
   } else if (warp == kRowWarps + 1) {
     // ---------------------------------------------------------- products
     if (lane == 0) {
@@ -307,7 +347,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         const uint32_t va = smem_u32(s.v[st]);
         const int steps = keys(j) / 16;
         for (int c = 0; c < steps; ++c)
-          umma_ts(tmem + S::kOut, tmem + S::kWeights + 8 * c, umma_desc(va + c * 2048, kBlock),
+          umma_ts(tmem + S::kOut, tmem + S::weights(16 * c), umma_desc(va + c * 2048, kBlock),
                   idesc_o, it > 0 || c > 0);
         umma_commit(&s.o_done);
         umma_commit(&s.v_empty[st]);
@@ -316,9 +356,16 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
   } else {
     // -------------------------------------------------------------- rows
-    const uint32_t mine = tmem + (uint32_t(warp * 32) << 16);  // this warp's lanes
-    const bool some = warp * 32 < rows;                        // (others only keep step)
-    const int local = t / p.group;                             // token of the row's tile
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
+    const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
+    const bool some = quarter * 32 < rows;                        // (others only keep step)
+    const int local = row / p.group;                              // token of the row
+    // tells the row's other thread x, and returns what that told (turn: of two)
+    auto other = [&](float x, int turn) {
+      s.half[turn][half][row] = x;
+      asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
+      return s.half[turn][half ^ 1][row];
+    };
     if (has_tree) {
       // a token's ancestors: one thread walks up from each token
       if (t < node1 - node0) {
@@ -326,9 +373,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         for (int w = 0; w < w1; ++w) s.seen[t][w] = 0;
         for (int i = node0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
       }
-      asm volatile("bar.sync 1, 128;" ::: "memory");
+      asm volatile("bar.sync 5, 256;" ::: "memory");
     }
-    const int per = kTile / p.box;
     auto box_ok = [&](int tile) {  // whether box `lane` of a cache tile is in range
       const int slot = tile * kTile + lane * p.box;
       if (tile >= min(tile1, n_cache) || lane >= per || slot >= r.len) return true;
@@ -360,28 +406,25 @@ __global__ void __launch_bounds__(kThreads, 2)
       // (the warp goes on, or gives up, as one)
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
       tc_fence_after();
-      // (Rolled loops: unrolled over the tile, this code no longer fits the
-      // instruction cache beside the other warps', and a call takes half as long again.)
-      bool raised = false;
+      // this thread's half of the row's scores, 32 at a time
+      const int c0 = 64 * half, c1 = min(n, c0 + 64);
       float f = 1.f;
+      bool raised = false;
       if (some) {
         float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-        for (int c = 0; c < n; c += 32) {
+        for (int c = c0; c < c1; c += 32) {
           uint32_t v[32];
           tmem_ld32(mine + c, v);
           const uint32_t see = sees(c);
           tmem_wait_ld(v);
-          if (see != 0xffffffffu) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(see >> i & 1)) v[i] = 0xff800000u;
-          }
+          if (see != 0xffffffffu) hide(v, see);
           __syncwarp();
 #pragma unroll
           for (int i = 0; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i]));
         }
-        const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        high = fmaxf(high, other(high, it & 1));
         // the reference follows the maximum, and with it the sums
         const bool raise = (high - m) * p.scale2 > kSlack || (m == -INFINITY && high > -INFINITY);
         raised = __any_sync(0xffffffffu, raise);
@@ -392,38 +435,20 @@ __global__ void __launch_bounds__(kThreads, 2)
           l *= f;
         }
       }
-      // The last tile's product is in the output and done with its weights. (Every
-      // warp waits for it, or one without rows would be a tile ahead on p_full.)
-      if (S::kOwn && it > 0) {
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
-        tc_fence_after();
-      }
+      uint32_t w[32];  // the weights, two to a word
       if (some) {
-        if (raised && it > 0) {
-#pragma unroll 1
-          for (int c = 0; c < D; c += 32) {
-            uint32_t o[32];
-            tmem_ld32(mine + S::kOut + c, o);
-            tmem_wait_ld(o);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(mine + S::kOut + c, o);
-          }
-        }
         const float shift = (m == -INFINITY ? 0.f : -m * p.scale2) + kOffset;
         const f32x2 scale2 = pair(p.scale2, p.scale2), shift2 = pair(shift, shift);
         f32x2 sum2 = 0;
-#pragma unroll 1
-        for (int c = 0; c < n; c += 32) {
-          uint32_t v[32], w[16];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int c = c0 + 32 * h;
+          if (c >= c1) break;
+          uint32_t v[32];
           tmem_ld32(mine + c, v);
           const uint32_t see = sees(c);
           tmem_wait_ld(v);
-          if (see != 0xffffffffu) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!(see >> i & 1)) v[i] = 0xff800000u;
-          }
+          if (see != 0xffffffffu) hide(v, see);
           __syncwarp();
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -432,26 +457,50 @@ __global__ void __launch_bounds__(kThreads, 2)
             sum2 = add2(sum2, e);
             float lo, hi;
             split(e, lo, hi);
-            w[i] = pack2<F16>(lo, hi);
+            w[16 * h + i] = pack2<F16>(lo, hi);
           }
-          tmem_st16(mine + S::kWeights + c / 2, w);
         }
         l += sum_pair(sum2);
-        tmem_wait_st();
         tc_fence_before();
       }
-      if (S::kOwn) mbar_arrive(&s.s_free);
+      // Weights of their own: the scores' place is free, and the last tile's product
+      // has to be done with the weights' place and in the output. (Every warp waits
+      // for that, or one without rows would be a tile ahead on p_full.)
+      if (S::kOwn) {
+        mbar_arrive(&s.s_free);
+        if (it > 0) {
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
+          tc_fence_after();
+        }
+      }
+      if (some) {
+        const uint32_t to = mine + S::weights(c0);
+        if (c0 + 32 < c1)
+          tmem_st32(to, w);
+        else if (c0 < c1)
+          tmem_st16(to, w);
+        if (raised && it > 0) {
+#pragma unroll 1
+          for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+            uint32_t o[32];
+            tmem_ld32(mine + S::kOut + c, o);
+            tmem_wait_ld(o);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st32(mine + S::kOut + c, o);
+          }
+        }
+        tmem_wait_st();
+      }
       // Values that no row may touch: slots past the end (0 times what is there
       // could be NaN), and of drafted tokens, what is not finite: a token outside
       // its branch would get NaN from it. (Its own branch gets it at the end.)
-      uint32_t gaps = 0;
-      for (int c = 0; c < n; c += 32) gaps |= there(c) != 0xffffffffu;
-      if (gaps || !cache) {
+      if (left < n || bad_boxes || !cache) {
         if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.v_full[st], parity, limit)))) break;
-        for (int i = t; i < n * kHalves * 8; i += kTile) {
-          const int row = (i >> 3) % n, half = (i >> 3) / n;
-          uint4* at = reinterpret_cast<uint4*>(s.v[st] + half * kBlock + row * 128 + (i & 7) * 16);
-          if (!(there(row & ~31) >> (row & 31) & 1)) {
+        for (int i = t; i < n * kHalves * 8; i += kRowThreads) {
+          const int key = (i >> 3) % n, block = (i >> 3) / n;
+          uint4* at = reinterpret_cast<uint4*>(s.v[st] + block * kBlock + key * 128 + (i & 7) * 16);
+          if (!(there(key & ~31) >> (key & 31) & 1)) {
             *at = make_uint4(0, 0, 0, 0);
           } else if (!cache) {
             constexpr uint16_t kExp = F16 ? 0x7c00 : 0x7f80;
@@ -466,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 2)
               }
             if (odd) {
               *at = w;
-              atomicOr(&s.odd[(base + row) >> 5], 1u << ((base + row) & 31));
+              atomicOr(&s.odd[(base + key) >> 5], 1u << ((base + key) & 31));
             }
           }
         }
@@ -477,15 +526,17 @@ __global__ void __launch_bounds__(kThreads, 2)
     }
     if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (tile1 - tile0 - 1) & 1, limit));
     tc_fence_after();
-    if (has_tree) asm volatile("bar.sync 1, 128;" ::: "memory");  // (s.odd is whole)
+    if (has_tree) asm volatile("bar.sync 5, 256;" ::: "memory");  // (s.odd is whole)
     if (ok && some) {
-      const bool valid = t < rows;
-      const int node = r.first + node0 + local, h = hk * p.group + t % p.group;
-      const int64_t row = int64_t(node) * a.Hq + h;
+      l += other(l, (tile1 - tile0) & 1);
+      const bool valid = row < rows;
+      const int node = r.first + node0 + local, h = hk * p.group + row % p.group;
+      const int64_t to = int64_t(node) * a.Hq + h;  // row of the outputs
       const bool whole = runs == 1;
       const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-      const int64_t at = (int64_t(run) * a.n_nodes * a.Hq + row) * D;
-      for (int c = 0; c < D; c += 32) {
+      const int64_t at = (int64_t(run) * a.n_nodes * a.Hq + to) * D;
+#pragma unroll 1
+      for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
         uint32_t v[32];
         tmem_ld32(mine + S::kOut + c, v);
         tmem_wait_ld(v);
@@ -493,8 +544,8 @@ __global__ void __launch_bounds__(kThreads, 2)
           if (has_tree) {
             for (int w = 0; w * 32 < node1; ++w)
               for (uint32_t odd = s.odd[w] & s.seen[local][w]; odd; odd &= odd - 1) {
-                const int64_t other = int64_t(r.first) + w * 32 + __ffs(odd) - 1;
-                const uint16_t* e = reinterpret_cast<const uint16_t*>(a.v) + other * a.v_token +
+                const int64_t peer = int64_t(r.first) + w * 32 + __ffs(odd) - 1;
+                const uint16_t* e = reinterpret_cast<const uint16_t*>(a.v) + peer * a.v_token +
                                     hk * a.v_head + c;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
@@ -504,31 +555,35 @@ __global__ void __launch_bounds__(kThreads, 2)
               }
           }
           if (whole) {
-            uint4* out = reinterpret_cast<uint4*>(a.out + (row * D + c) * 2);
+            char* out = a.out + (to * D + c) * 2;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t o[4];
+            for (int i = 0; i < 2; ++i) {
+              uint32_t o[8];
 #pragma unroll
-              for (int q = 0; q < 4; ++q)
-                o[q] = pack2<F16>(__uint_as_float(v[8 * i + 2 * q]) * inv,
-                                  __uint_as_float(v[8 * i + 2 * q + 1]) * inv);
-              out[i] = make_uint4(o[0], o[1], o[2], o[3]);
+              for (int q = 0; q < 8; ++q)
+                o[q] = pack2<F16>(__uint_as_float(v[16 * i + 2 * q]) * inv,
+                                  __uint_as_float(v[16 * i + 2 * q + 1]) * inv);
+              store_sector<true>(out + 32 * i, o);
             }
           } else {
-            uint4* out = reinterpret_cast<uint4*>(p.part + at + c);
+            char* out = reinterpret_cast<char*>(p.part + at + c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              out[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 4; ++i) {
+              uint32_t o[8];
+#pragma unroll
+              for (int q = 0; q < 8; ++q) o[q] = v[8 * i + q];
+              store_sector<false>(out + 32 * i, o);
+            }
           }
         }
         __syncwarp();
       }
-      if (valid) {
+      if (valid && half == 0) {
         const float m2 = m == -INFINITY ? -INFINITY : m * p.scale2 - kOffset;
         if (!whole)
-          p.part_ml[int64_t(run) * a.n_nodes * a.Hq + row] = make_float2(m2, l);
+          p.part_ml[int64_t(run) * a.n_nodes * a.Hq + to] = make_float2(m2, l);
         else if (a.lse)
-          a.lse[row] = l > 0.f || l != l ? fmaf(m2, kLn2, logf(l)) : -INFINITY;
+          a.lse[to] = l > 0.f || l != l ? fmaf(m2, kLn2, logf(l)) : -INFINITY;
       }
     }
     if (reports) {
@@ -546,28 +601,31 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Joins the runs of every row that has more than one: with M the largest of the
-// runs' references, out = sum 2^(m - M) o / sum 2^(m - M) l. A CTA per row, its
-// warps take the runs in turn; each warp reads a run's output in one go.
+// runs' references, out = sum 2^(m - M) o / sum 2^(m - M) l. W warps take a row's
+// runs in turn, each reads a run's output in one go: one warp for a few runs
+// (rows are many then: a CTA for each of 32,768 rows with two runs took 50 us more
+// than a warp), four for more.
 constexpr int kJoinWarps = 4;
 
-template <int D, bool F16>
+template <int D, bool F16, int W>
 __global__ void __launch_bounds__(kJoinWarps * 32)
     tree_join_kernel(const __grid_constant__ TreeKernelArgs p) {
   constexpr int N = D / 32;
   using Vec = typename std::conditional<N == 4, float4, float2>::type;
-  __shared__ float s_acc[kJoinWarps][D];
-  __shared__ float s_l[kJoinWarps];
+  __shared__ float s_acc[W == 1 ? 1 : W][D];
+  __shared__ float s_l[W];
   const TreeArgs& a = p.a;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  grid_dependency_wait();
-  // row blockIdx.x of the B * max_nodes * Hq that there may be
-  const int h = int(blockIdx.x % a.Hq), i = int(blockIdx.x / a.Hq % a.max_nodes);
-  const int b = int(blockIdx.x / a.Hq / a.max_nodes);
+  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // row x of the B * max_nodes * Hq that there may be
+  const unsigned int x = W == 1 ? blockIdx.x * kJoinWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const int h = int(x % a.Hq), i = int(x / a.Hq % a.max_nodes), b = int(x / a.Hq / a.max_nodes);
+  if (b >= a.B) return;
   const Request r = request(a, b);
   if (i >= r.nodes) return;
   const int end = min(r.nodes, (i / p.per_tile + 1) * p.per_tile);
   const int runs = run_count(cache_tiles(r.len) + tree_tiles(end), p.run);
   if (runs < 2) return;
+  grid_dependency_wait();
   const int64_t row = (int64_t(r.first) + i) * a.Hq + h, rows = int64_t(a.n_nodes) * a.Hq;
   float M = -INFINITY;
   for (int s = lane; s < runs; s += 32) M = fmaxf(M, p.part_ml[s * rows + row].x);
@@ -575,7 +633,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   float acc[N] = {};
   float l = 0.f;
 #pragma unroll 4
-  for (int s = warp; s < runs; s += kJoinWarps) {
+  for (int s = warp; s < runs; s += W) {
     const float2 ml = p.part_ml[s * rows + row];
     const Vec o = reinterpret_cast<const Vec*>(p.part + (s * rows + row) * D)[lane];
     // (a run of nothing but -inf scores: 0, whatever the maximum is)
@@ -588,30 +646,29 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
       acc[3] = fmaf(o.w, f, acc[3]);
     }
   }
+  if constexpr (W > 1) {
 #pragma unroll
-  for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[c];
-  if (lane == 0) s_l[warp] = l;
-  __syncthreads();
-  l = s_l[0];
+    for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[c];
+    if (lane == 0) s_l[warp] = l;
+    __syncthreads();
+    if (warp > 0) return;
 #pragma unroll
-  for (int w = 1; w < kJoinWarps; ++w) l += s_l[w];
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-  for (int c = threadIdx.x; c < D / 2; c += kJoinWarps * 32) {
-    float lo = s_acc[0][2 * c], hi = s_acc[0][2 * c + 1];
+    for (int w = 1; w < W; ++w) {
+      l += s_l[w];
 #pragma unroll
-    for (int w = 1; w < kJoinWarps; ++w) {
-      lo += s_acc[w][2 * c];
-      hi += s_acc[w][2 * c + 1];
+      for (int c = 0; c < N; ++c) acc[c] += s_acc[w][lane * N + c];
     }
-    reinterpret_cast<uint32_t*>(a.out + row * D * 2)[c] = pack2<F16>(lo * inv, hi * inv);
   }
-  if (a.lse && threadIdx.x == 0)
-    a.lse[row] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
+  out[0] = pack2<F16>(acc[0] * inv, acc[1] * inv);
+  if constexpr (N == 4) out[1] = pack2<F16>(acc[2] * inv, acc[3] * inv);
+  if (a.lse && lane == 0) a.lse[row] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
 }
 
 // ------------------------------------------------------------------- host
 
-constexpr int kMinRun = 4, kWaves = 2;
+constexpr int kMinRun = 2, kWaves = 1;
 // How a call is cut: tokens per tile of rows, tiles per run, runs.
 struct Cut {
   int group, per_tile, row_tiles, run, runs;
@@ -678,18 +735,22 @@ cudaError_t launch(const TreeKernelArgs& p, cudaStream_t stream) {
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.gridDim = dim3(unsigned(int64_t(a.B) * a.max_nodes * a.Hq));
+  const bool few = p.runs <= 8;
+  const int64_t rows = int64_t(a.B) * a.max_nodes * a.Hq;
+  cfg.gridDim = dim3(unsigned(few ? (rows + kJoinWarps - 1) / kJoinWarps : rows));
   cfg.blockDim = dim3(kJoinWarps * 32);
   cfg.dynamicSmemBytes = 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16>, p);
+  return few ? cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16, 1>, p)
+             : cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16, kJoinWarps>, p);
 }
 
 template <int D, bool F16>
 cudaError_t preload() {
   cudaFuncAttributes fa;
-  const cudaError_t e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16>);
+  cudaError_t e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16, 1>);
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16, kJoinWarps>);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(tree_kernel<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               int(sizeof(Smem<D>)) + 1024);
