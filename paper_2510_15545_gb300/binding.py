@@ -685,6 +685,15 @@ def tt_dpos_hist(batch: Batch, path: torch.Tensor, path_len: torch.Tensor,
 
 # --------------------------------------- operators around a verification step
 
+def _on(stream):
+    """Makes `stream` the current one, so that what a call allocates belongs to the
+    stream it runs on."""
+    if hasattr(stream, "cuda_stream"):
+        return torch.cuda.stream(stream)
+    return torch.cuda.stream(torch.cuda.ExternalStream(int(stream)) if int(stream)
+                             else torch.cuda.default_stream())
+
+
 def _given(t, name, dtype, numel):
     """A contiguous tensor argument of a type and at least a size (None passes)."""
     if t is not None and (t.dtype != dtype or not t.is_contiguous() or t.numel() < numel):
@@ -699,22 +708,44 @@ def tt_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, *, tem
     entropy [R], with ids (int32 [R], -1: none) the logprob and the rank of each
     row's column, and the top_n best columns as top_ids and top_logprobs
     [R, top_n]; status [R]. Tensors given in ``out`` are written in place."""
+    if stream is not None:
+        with _on(stream):
+            return tt_logprobs(logits, ids, temp=temp, top_n=top_n, out=out)
     L = _logits(logits)
-    R, dev = logits.shape[0], logits.device
-    o = dict(out or {})
-    for key in ("lse", "entropy") + (("logprob",) if ids is not None else ()):
-        _need(o, key, R, torch.float32, dev)
-    for key in ("status",) + (("rank",) if ids is not None else ()):
-        _need(o, key, R, torch.int32, dev)
-    if "top_ids" not in o:
-        o["top_ids"] = torch.empty((R, top_n), dtype=torch.int32, device=dev)
-    if "top_logprobs" not in o:
-        o["top_logprobs"] = torch.empty((R, top_n), dtype=torch.float32, device=dev)
-    c_out = _LogprobsOut(*[_ptr(o.get(k)) for k in ("logprob", "rank", "entropy", "lse", "top_ids",
-                                                    "top_logprobs", "status")])
-    code = load().tt_logprobs(ctypes.byref(L), _given(ids, "ids", torch.int32, R), float(temp),
-                              int(top_n), ctypes.byref(c_out), _stream(stream))
-    _check("tt_logprobs", code)
+    R, n = logits.shape[0], int(top_n)
+    ids_p = _given(ids, "ids", torch.int32, R)
+    if out:
+        o, dev = dict(out), logits.device
+        f32, i32 = torch.float32, torch.int32
+        for key, dtype, size in (("lse", f32, (R,)), ("entropy", f32, (R,)), ("status", i32, (R,)),
+                                 ("top_ids", i32, (R, n)), ("top_logprobs", f32, (R, n))) + (
+                () if ids is None else (("logprob", f32, (R,)), ("rank", i32, (R,)))):
+            if key not in o:
+                o[key] = torch.empty(size, dtype=dtype, device=dev)
+        ptrs = [_given(o.get(k), k, t, m) for k, t, m in (
+            ("logprob", f32, R), ("rank", i32, R), ("entropy", f32, R), ("lse", f32, R),
+            ("top_ids", i32, R * n), ("top_logprobs", f32, R * n), ("status", i32, R))]
+    else:
+        # (an allocation for each output cost a call 12 us on the Grace host)
+        buf = torch.empty(5 * R + 2 * R * max(n, 0), dtype=torch.float32, device=logits.device)
+        whole = buf.view(torch.int32)
+        row, top = ((R,), (1,)), ((R, n), (n, 1))
+        o = {"lse": buf.as_strided(*row, 0), "entropy": buf.as_strided(*row, R),
+             "status": whole.as_strided(*row, 2 * R),
+             "top_ids": whole.as_strided(*top, 5 * R),
+             "top_logprobs": buf.as_strided(*top, 5 * R + R * n)}
+        if ids is not None:
+            o["logprob"] = buf.as_strided(*row, 3 * R)
+            o["rank"] = whole.as_strided(*row, 4 * R)
+        p = buf.data_ptr()
+        given = ids is not None
+        ptrs = [p + 12 * R if given else None, p + 16 * R if given else None, p + 4 * R, p,
+                p + 20 * R, p + 20 * R + 4 * R * n, p + 8 * R]
+    c_out = _LogprobsOut(*ptrs)
+    code = load().tt_logprobs(ctypes.byref(L), ids_p, float(temp), n, ctypes.byref(c_out),
+                              _stream(stream))
+    if code:
+        _check("tt_logprobs", code)
     return o
 
 
@@ -728,6 +759,8 @@ def _teacher(ids: torch.Tensor, logp: torch.Tensor, R: int) -> _Teacher:
 def _like_rows(logits: torch.Tensor) -> torch.Tensor:
     """Rows like `logits`, each starting on 16 bytes."""
     R, V = logits.shape
+    if V % 8 == 0:
+        return torch.empty((R, V), dtype=logits.dtype, device=logits.device)
     return torch.empty((R, (V + 7) // 8 * 8), dtype=logits.dtype, device=logits.device)[:, :V]
 
 
@@ -738,23 +771,39 @@ def tt_distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: to
     teacher's top log probabilities (int32 and fp32 [R, k], as tt_logprobs gives
     them), with ``tail`` the teacher's mass outside the list too; the gradient to
     the logits, weight[r] times each row's (grad: True, False, or the tensor to
-    write, which may be the logits); stats for a later tt_distill_grad; status."""
-    L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, logits.shape[0])
-    R, dev = logits.shape[0], logits.device
-    o = dict(out or {})
-    _need(o, "loss", R, torch.float32, dev)
-    _need(o, "status", R, torch.int32, dev)
-    if "stats" not in o:
-        o["stats"] = torch.empty((R, 4), dtype=torch.float32, device=dev)
+    write, which may be the logits); stats [R, 4] for a later tt_distill_grad;
+    status [R]. Tensors given in ``out`` are written in place."""
+    if stream is not None:
+        with _on(stream):
+            return tt_distill(logits, teacher_ids, teacher_logp, temp=temp, tail=tail,
+                              weight=weight, grad=grad, out=out)
+    R = logits.shape[0]
+    L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, R)
+    weight_p = _given(weight, "weight", torch.float32, R)
+    if out:
+        o, dev = dict(out), logits.device
+        _need(o, "loss", R, torch.float32, dev)
+        _need(o, "status", R, torch.int32, dev)
+        if "stats" not in o:
+            o["stats"] = torch.empty((R, 4), dtype=torch.float32, device=dev)
+        loss_p = _given(o["loss"], "loss", torch.float32, R)
+        stats_p = _given(o["stats"], "stats", torch.float32, 4 * R)
+        status_p = _given(o["status"], "status", torch.int32, R)
+    else:
+        buf = torch.empty(6 * R, dtype=torch.float32, device=logits.device)
+        o = {"stats": buf.as_strided((R, 4), (4, 1), 0), "loss": buf.as_strided((R,), (1,), 4 * R),
+             "status": buf.view(torch.int32).as_strided((R,), (1,), 5 * R)}
+        stats_p = buf.data_ptr()
+        loss_p, status_p = stats_p + 16 * R, stats_p + 20 * R
     G = None
     if grad is not False:
         o["grad"] = _like_rows(logits) if grad is True else grad
         G = _logits(o["grad"])
     code = load().tt_distill(ctypes.byref(L), ctypes.byref(T), float(temp), int(bool(tail)),
-                             _given(weight, "weight", torch.float32, R), _ptr(o["loss"]),
-                             _ptr(o["stats"]), None if G is None else ctypes.byref(G),
-                             _ptr(o["status"]), _stream(stream))
-    _check("tt_distill", code)
+                             weight_p, loss_p, stats_p, None if G is None else ctypes.byref(G),
+                             status_p, _stream(stream))
+    if code:
+        _check("tt_distill", code)
     return o
 
 
@@ -763,6 +812,10 @@ def tt_distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
                     weight: Optional[torch.Tensor] = None, grad: Optional[torch.Tensor] = None,
                     stream=None) -> torch.Tensor:
     """The gradient of tt_distill from its stats (same arguments otherwise)."""
+    if stream is not None:
+        with _on(stream):
+            return tt_distill_grad(logits, teacher_ids, teacher_logp, stats, temp=temp, tail=tail,
+                                   weight=weight, grad=grad)
     L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, logits.shape[0])
     g = _like_rows(logits) if grad is None else grad
     G = _logits(g)
@@ -771,7 +824,8 @@ def tt_distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
                                   _given(weight, "weight", torch.float32, R),
                                   _given(stats, "stats", torch.float32, 4 * R), ctypes.byref(G),
                                   _stream(stream))
-    _check("tt_distill_grad", code)
+    if code:
+        _check("tt_distill_grad", code)
     return g
 
 
@@ -852,25 +906,42 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
     the requests' paged caches k_cache, v_cache [pages, page_size, kv heads,
     head_dim] (any strides with unit innermost), page_table int32 [B, pages per
     request], cache_len int32 [B]. Returns out [N, q heads, head_dim], lse
-    [N, q heads] and status [B]. max_len and max_nodes bound the lengths and the
-    nodes of a request and size the launch (default: what the table and N allow)."""
+    [N, q heads] and status [B]; tensors given in ``out`` are written in place.
+    max_len and max_nodes bound the lengths and the nodes of a request and size the
+    launch (default: what the table and N allow)."""
+    if stream is not None:
+        with _on(stream):
+            return tt_tree_attn(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents,
+                                scale=scale, max_len=max_len, max_nodes=max_nodes, ws=ws, out=out)
     T = _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
               max_nodes)
-    dev, L = q.device, load()
-    o = dict(out or {})
+    L = load()
+    N, Hq, D = q.shape
+    rows, B = N * Hq, T.B
+    n = int(L.tt_tree_workspace_bytes(ctypes.byref(T))) if ws is None else 0
+    if out:
+        o = dict(out)
+        if "lse" not in o:
+            o["lse"] = torch.empty((N, Hq), dtype=torch.float32, device=q.device)
+        _need(o, "status", B, torch.int32, q.device)
+        if n:
+            ws = torch.empty(n, dtype=torch.uint8, device=q.device)
+        ws_p, n = (_ptr(ws), ws.numel()) if ws is not None else (None, 0)
+    else:
+        # (one allocation: scratch, then lse and status)
+        buf = torch.empty(n // 4 + rows + B, dtype=torch.float32, device=q.device)
+        o = {"lse": buf.as_strided((N, Hq), (Hq, 1), n // 4),
+             "status": buf.view(torch.int32).as_strided((B,), (1,), n // 4 + rows)}
+        ws_p = buf.data_ptr()
+        if ws is not None:
+            ws_p, n = ws.data_ptr(), ws.numel()
     if "out" not in o:
-        o["out"] = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    if "lse" not in o:
-        o["lse"] = torch.empty(q.shape[:2], dtype=torch.float32, device=dev)
-    _need(o, "status", T.B, torch.int32, dev)
-    if ws is None:
-        n = int(L.tt_tree_workspace_bytes(ctypes.byref(T)))
-        ws = torch.empty(n, dtype=torch.uint8, device=dev) if n else None
-    code = L.tt_tree_attn(ctypes.byref(T), _ptr(ws), 0 if ws is None else ws.numel(),
-                          _given(o["out"], "out", q.dtype, q.numel()),
-                          _given(o["lse"], "lse", torch.float32, q.shape[0] * q.shape[1]),
-                          _ptr(o["status"]), _stream(stream))
-    _check("tt_tree_attn", code)
+        o["out"] = torch.empty((N, Hq, D), dtype=q.dtype, device=q.device)
+    code = L.tt_tree_attn(ctypes.byref(T), ws_p, n, _given(o["out"], "out", q.dtype, rows * D),
+                          _given(o["lse"], "lse", torch.float32, rows),
+                          _given(o["status"], "status", torch.int32, B), _stream(None))
+    if code:
+        _check("tt_tree_attn", code)
     return o
 
 
