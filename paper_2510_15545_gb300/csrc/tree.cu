@@ -19,7 +19,15 @@
 // A tile's way from scores to weights is mostly waiting (for tensor memory, for
 // the special function unit): two threads share a row, one for each half of the
 // tile's keys, read their scores once, and agree on the maximum through shared
-// memory. Long caches are split into runs, whose results a second kernel joins.
+// memory.
+//
+// The tiles of all requests, key heads and row tiles form one list, which the
+// CTAs, two per SM, share evenly: lengths are known on the device alone, and a
+// grid over the longest one would leave SMs idle beside ragged batches. A CTA
+// finds its part from the requests' sizes, and takes it item by item (an item:
+// one request, key head and row tile); the copies of an item begin while the one
+// before it is finished. Items cut by a CTA's end leave unnormalised pieces, which
+// a second kernel joins.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -54,6 +62,7 @@ constexpr float kLn2 = 0.693147180559945f;
 // A row's reference maximum follows its maximum once that is 2^kSlack above it:
 // weights stay below 2^(kSlack + offset), and the output is scaled rarely.
 constexpr float kSlack = 8.f;
+constexpr int kMinShare = 2;  // tiles of a CTA, where there are few
 
 struct TreeKernelArgs {
   CUtensorMap q, k, v, kc, vc;
@@ -61,13 +70,15 @@ struct TreeKernelArgs {
   float scale2;       // scale * log2(e)
   int group;          // G
   int per_tile;       // tokens of a 128-row tile
-  int row_tiles;      // CTAs of a request's rows, at most
-  int run;            // tiles of a run, at most
-  int runs;           // runs of a request, at most
+  int ctas;           // of the launch
+  int rows;           // rows of an item, at most
   int box;            // slots of one copy: they lie within a page
   int slots_inner;    // the cache maps' second dimension is the slot, the third the head
-  float* part;        // [runs * n_nodes * Hq * D] outputs of runs, not normalised
-  float2* part_ml;    // [runs * n_nodes * Hq] their reference maximum (log2) and sum
+  // pieces: CTA c leaves that of an item that began before its tiles at 2 c, that
+  // of one that begins in them at 2 c + 1
+  float* part;        // [2 ctas * rows * D] outputs, not normalised
+  float2* part_ml;    // [2 ctas * rows] their reference maximum (log2) and sum
+  int32_t* first;     // [B + 1] tiles before each request's, then the tiles per CTA
 };
 
 // A request's usable range: its nodes and cache length, or why it has none.
@@ -89,11 +100,44 @@ __device__ __forceinline__ Request request(const TreeArgs& a, int b) {
   return r;
 }
 
-// The tiles that the rows of tokens first .. end - 1 see: the cache's, then
-// those of drafted tokens up to end - 1; and the runs they are cut into.
+// The tiles that the rows of tokens up to end - 1 see: the cache's, then those of
+// drafted tokens.
 __host__ __device__ inline int cache_tiles(int len) { return len / kTile + (len % kTile != 0); }
 __host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / kTile; }
-__host__ __device__ inline int run_count(int tiles, int run) { return (tiles + run - 1) / run; }
+__device__ __forceinline__ int item_tiles(const TreeKernelArgs& p, const Request& r, int mt) {
+  return cache_tiles(r.len) + tree_tiles(min(r.nodes, (mt + 1) * p.per_tile));
+}
+// The tiles of one key head of a request.
+__device__ __forceinline__ int head_tiles(const TreeKernelArgs& p, const Request& r) {
+  int n = 0;
+  for (int mt = 0; mt * p.per_tile < r.nodes; ++mt) n += item_tiles(p, r, mt);
+  return n;
+}
+// A place in the list of tiles.
+struct Place {
+  int b, hk, mt, tile;
+  Request r;
+  __device__ __forceinline__ void find(const TreeKernelArgs& p, int request_b, int offset) {
+    b = request_b;
+    r = request(p.a, b);
+    const int per_head = head_tiles(p, r);
+    hk = offset / per_head;
+    tile = offset % per_head;
+    mt = 0;
+    for (int n; tile >= (n = item_tiles(p, r, mt)); ++mt) tile -= n;
+  }
+  __device__ __forceinline__ void next_item(const TreeKernelArgs& p) {
+    tile = 0;
+    if (++mt * p.per_tile < r.nodes) return;
+    mt = 0;
+    if (++hk < p.a.Hkv) return;
+    hk = 0;
+    do {
+      if (++b >= p.a.B) return;
+      r = request(p.a, b);
+    } while (r.nodes == 0);
+  }
+};
 
 // Whether every parent and page of the request is in range (the row threads).
 __device__ bool out_of_range(const TreeArgs& a, int b, const Request& r, int t) {
@@ -132,7 +176,9 @@ struct Smem {
   float half[2][2][kTile];       // what the two threads of a row tell each other
   uint32_t odd[kWords];          // drafted tokens with a value that is not finite
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  uint64_t s_full, s_free, p_full, o_done;
+  uint64_t q_empty, s_full, s_free, p_full, o_done;
+  long long sums[kThreads / 32];  // tiles of the requests, by warps
+  int start_b, start_offset;      // where this CTA's tiles begin
   uint32_t tmem;
   int failed;
 };
@@ -186,86 +232,12 @@ __global__ void __launch_bounds__(kThreads, 2)
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
   const TreeArgs& a = p.a;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  int x = blockIdx.x;
-  const int mt = x % p.row_tiles;
-  x /= p.row_tiles;
-  const int hk = x % a.Hkv;
-  x /= a.Hkv;
-  const int run = x % p.runs, b = x / p.runs;
-  grid_launch_dependents();
-  const Request r = request(a, b);
-  const int node0 = mt * p.per_tile, node1 = min(r.nodes, node0 + p.per_tile);
-  const int rows = max(0, node1 - node0) * p.group;
-  const int n_cache = cache_tiles(r.len);
-  const int tiles = rows > 0 ? n_cache + tree_tiles(node1) : 0;
-  const int runs = run_count(tiles, p.run);
-  const bool reports = run == 0 && hk == 0 && mt == 0;
-  if (run >= runs) {  // nothing here, but perhaps the request's status
-    if (reports) {
-      const bool bad = !r.status && t < kRowThreads && out_of_range(a, b, r, t);
-      const int any = __syncthreads_or(bad);
-      if (t == 0) a.status[b] = r.status | (any ? TT_REQ_ID_OUT_OF_RANGE : 0);
-    }
-    return;
-  }
-  const int tile0 = int(int64_t(run) * tiles / runs), tile1 = int(int64_t(run + 1) * tiles / runs);
   const uint64_t limit = kWaitLimitNs;
-
-  // The copying warp's part: lane i copies a tile's i-th box of slots. The first
-  // tile is on its way before the CTA has its tensor memory.
-  int page = -1;
-  const int per = kTile / p.box;
-  auto page_of = [&](int tile) {
-    const int slot = tile * kTile + lane * p.box;
-    return tile < min(tile1, n_cache) && lane < per && slot < r.len
-               ? a.page_table[b * a.table_stride + slot / a.page_size]
-               : -1;
-  };
-  auto copy_tile = [&](int j) {
-    const int it = j - tile0, st = it % S::kStages;
-    const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
-    const int next = page_of(j + 1);
-    const bool cache = j < n_cache;
-    bool mine;
-    int bytes, at;
-    if (cache) {
-      mine = page >= 0 && page < a.n_pages;
-      bytes = p.box * 128;
-      at = lane * p.box;
-    } else {
-      at = lane * 16;
-      mine = lane < kTile / 16 && (j - n_cache) * kTile + at < node1;
-      bytes = 16 * 128;
-    }
-    const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
-    auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* paged, const CUtensorMap* own) {
-      if (lane == 0) mbar_arrive_expect_tx(bar, boxes * bytes * kHalves);
-      __syncwarp();
-      if (!mine) return;
-#pragma unroll
-      for (int h = 0; h < kHalves; ++h) {
-        const uint32_t to = smem_u32(dst) + h * kBlock + at * 128;
-        if (cache) {
-          const int slot = (j * kTile + at) % a.page_size;
-          tma_load_4d(to, paged, smem_u32(bar), 64 * h, p.slots_inner ? slot : hk,
-                      p.slots_inner ? hk : slot, page);
-        } else {
-          tma_load_3d(to, own, smem_u32(bar), 64 * h, hk, r.first + (j - n_cache) * kTile + at);
-        }
-      }
-    };
-    if (!__all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit))) return false;
-    copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
-    __syncwarp();
-    if (!__all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit))) return false;
-    copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
-    __syncwarp();
-    page = next;
-    return true;
-  };
+  grid_launch_dependents();
 
   if (t == kRowThreads) {
     mbar_init(&s.q_full, 1);
+    mbar_init(&s.q_empty, 1);
     for (int i = 0; i < S::kStages; ++i) {
       mbar_init(&s.k_full[i], 1);
       mbar_init(&s.k_empty[i], 1);
@@ -279,331 +251,469 @@ __global__ void __launch_bounds__(kThreads, 2)
     s.failed = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  bool ok = true;
-  if (warp == kRowWarps) {
-    __syncwarp();
-    if (lane == 0) {
-      mbar_arrive_expect_tx(&s.q_full, kHalves * p.per_tile * p.group * 128);
-      for (int h = 0; h < kHalves; ++h)
-        tma_load_3d(smem_u32(s.q) + h * kBlock, &p.q, smem_u32(&s.q_full), 64 * h, hk * p.group,
-                    r.first + node0);
-    }
-    page = page_of(tile0);
-    ok = copy_tile(tile0);
-  }
   if (warp == kRowWarps + 1) tmem_alloc(&s.tmem, kTmemColumns);
-  const bool has_tree = tile1 > n_cache;
-  if (has_tree) {
-    if (t < kWords) s.odd[t] = 0;
-    for (int i = t; i < node1; i += kThreads) {
-      const int up = a.parents ? a.parents[r.first + i] : i - 1;
-      s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
+  // The list: each thread adds up a run of requests, and the one whose run holds
+  // this CTA's first tile tells the request.
+  int todo;
+  {
+    const int each = (a.B + kThreads - 1) / kThreads, b0 = min(a.B, t * each),
+              b1 = min(a.B, b0 + each);
+    long long mine = 0;
+    for (int b = b0; b < b1; ++b) mine += (long long)(head_tiles(p, request(a, b))) * a.Hkv;
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 31) s.sums[warp] = upto;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    long long all = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) upto += s.sums[w];
+      all += s.sums[w];
+    }
+    const long long share = max((long long)(kMinShare), (all + p.ctas - 1) / p.ctas);
+    const long long from = share * blockIdx.x;
+    todo = int(max(0ll, min(share, all - from)));
+    long long at = upto - mine;
+    if (todo > 0 && from >= at && from < upto) {
+      for (int b = b0; b < b1; ++b) {
+        const long long n = (long long)(head_tiles(p, request(a, b))) * a.Hkv;
+        if (from < at + n) {
+          s.start_b = b;
+          s.start_offset = int(from - at);
+          break;
+        }
+        at += n;
+      }
+    }
+    if (blockIdx.x == 0) {  // for the join
+      at = upto - mine;
+      for (int b = b0; b < b1; ++b) {
+        p.first[b] = int(at);
+        at += (long long)(head_tiles(p, request(a, b))) * a.Hkv;
+      }
+      if (t == 0) p.first[a.B] = int(share);
     }
   }
-  tc_fence_before();
   __syncthreads();
-  tc_fence_after();
   const uint32_t tmem = s.tmem;
+  bool ok = true;
+  Place x;
+  if (todo > 0) x.find(p, s.start_b, s.start_offset);
 
   if (warp == kRowWarps) {
     // ------------------------------------------------------------ copies
-    for (int j = tile0 + 1; j < tile1 && ok; ++j) ok = copy_tile(j);
+    // lane i copies a tile's i-th box of slots
+    const int per = kTile / p.box;
+    int it = 0;
+    for (int seg = 0; todo > 0 && ok; ++seg) {
+      const int n_cache = cache_tiles(x.r.len);
+      const int node0 = x.mt * p.per_tile, node1 = min(x.r.nodes, node0 + p.per_tile);
+      const int tile1 = min(n_cache + tree_tiles(node1), x.tile + todo);
+      auto page_of = [&](int tile) {
+        const int slot = tile * kTile + lane * p.box;
+        return tile < min(tile1, n_cache) && lane < per && slot < x.r.len
+                   ? a.page_table[x.b * a.table_stride + slot / a.page_size]
+                   : -1;
+      };
+      int page = page_of(x.tile);
+      // the queries, once the item before has been done with its own
+      ok = __all_sync(0xffffffffu, mbar_wait(&s.q_empty, (seg & 1) ^ 1, limit));
+      if (!ok) break;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(&s.q_full, kHalves * p.per_tile * p.group * 128);
+        for (int h = 0; h < kHalves; ++h)
+          tma_load_3d(smem_u32(s.q) + h * kBlock, &p.q, smem_u32(&s.q_full), 64 * h,
+                      x.hk * p.group, x.r.first + node0);
+      }
+      __syncwarp();
+      for (int j = x.tile; j < tile1; ++j, ++it) {
+        const int st = it % S::kStages;
+        const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
+        const int next = page_of(j + 1);
+        const bool cache = j < n_cache;
+        bool mine;
+        int bytes, at;
+        if (cache) {
+          mine = page >= 0 && page < a.n_pages;
+          bytes = p.box * 128;
+          at = lane * p.box;
+        } else {
+          at = lane * 16;
+          mine = lane < kTile / 16 && (j - n_cache) * kTile + at < node1;
+          bytes = 16 * 128;
+        }
+        const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
+        auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* paged,
+                        const CUtensorMap* own) {
+          if (lane == 0) mbar_arrive_expect_tx(bar, boxes * bytes * kHalves);
+          __syncwarp();
+          if (mine) {
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+              const uint32_t to = smem_u32(dst) + h * kBlock + at * 128;
+              if (cache) {
+                const int slot = (j * kTile + at) % a.page_size;
+                tma_load_4d(to, paged, smem_u32(bar), 64 * h, p.slots_inner ? slot : x.hk,
+                            p.slots_inner ? x.hk : slot, page);
+              } else {
+                tma_load_3d(to, own, smem_u32(bar), 64 * h, x.hk,
+                            x.r.first + (j - n_cache) * kTile + at);
+              }
+            }
+          }
+          __syncwarp();
+        };
+        ok = __all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit));
+        if (!ok) break;
+        copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
+        ok = __all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit));
+        if (!ok) break;
+        copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
+        page = next;
+      }
+      todo -= tile1 - x.tile;
+      x.next_item(p);
+    }
   } else if (warp == kRowWarps + 1) {
     // ---------------------------------------------------------- products
     if (lane == 0) {
       const uint32_t idesc_o = umma_idesc(F16, D, true);
-      // keys of tile j in use, up to a multiple of 32
-      auto keys = [&](int j) {
-        const int left = j < n_cache ? r.len - j * kTile : node1 - (j - n_cache) * kTile;
-        return min(kTile, (left + 31) & ~31);
-      };
-      auto scores = [&](int j) {
-        const int it = j - tile0, st = it % S::kStages;
-        if (!mbar_wait(&s.k_full[st], (it / S::kStages) & 1, limit)) return false;
-        tc_fence_after();
-        const uint32_t idesc_s = umma_idesc(F16, keys(j), false);
-        const uint32_t qa = smem_u32(s.q), ka = smem_u32(s.k[st]);
+      int it = 0;
+      for (int seg = 0; todo > 0 && ok; ++seg) {
+        const int n_cache = cache_tiles(x.r.len);
+        const int node1 = min(x.r.nodes, (x.mt + 1) * p.per_tile);
+        const int tile1 = min(n_cache + tree_tiles(node1), x.tile + todo);
+        // keys of tile j in use, up to a multiple of 32
+        auto keys = [&](int j) {
+          const int left = j < n_cache ? x.r.len - j * kTile : node1 - (j - n_cache) * kTile;
+          return min(kTile, (left + 31) & ~31);
+        };
+        auto scores = [&](int j, int i) {
+          const int st = i % S::kStages;
+          if (!mbar_wait(&s.k_full[st], (i / S::kStages) & 1, limit)) return false;
+          tc_fence_after();
+          const uint32_t idesc_s = umma_idesc(F16, keys(j), false);
+          const uint32_t qa = smem_u32(s.q), ka = smem_u32(s.k[st]);
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {
-          const uint32_t at = (c / 4) * kBlock + (c % 4) * 32;
-          umma_ss(tmem, umma_desc(qa + at, 16), umma_desc(ka + at, 16), idesc_s, c > 0);
-        }
-        umma_commit(&s.s_full);
-        umma_commit(&s.k_empty[st]);
-        return true;
-      };
-      ok = mbar_wait(&s.q_full, 0, limit) && scores(tile0);
-      for (int j = tile0; j < tile1 && ok; ++j) {
-        const int it = j - tile0, st = it % S::kStages;
+          for (int c = 0; c < D / 16; ++c) {
+            const uint32_t at = (c / 4) * kBlock + (c % 4) * 32;
+            umma_ss(tmem, umma_desc(qa + at, 16), umma_desc(ka + at, 16), idesc_s, c > 0);
+          }
+          umma_commit(&s.s_full);
+          umma_commit(&s.k_empty[st]);
+          if (j + 1 == tile1) umma_commit(&s.q_empty);
+          return true;
+        };
+        ok = mbar_wait(&s.q_full, seg & 1, limit);
         // (scores read by all rows: the next ones may take their place)
-        if (S::kOwn && j + 1 < tile1) {
-          ok = mbar_wait(&s.s_free, it & 1, limit) && scores(j + 1);
+        if (ok && S::kOwn && it > 0) ok = mbar_wait(&s.s_free, (it - 1) & 1, limit);
+        ok = ok && scores(x.tile, it);
+        for (int j = x.tile; j < tile1 && ok; ++j, ++it) {
+          const int st = it % S::kStages;
+          if (S::kOwn && j + 1 < tile1) {
+            ok = mbar_wait(&s.s_free, it & 1, limit) && scores(j + 1, it + 1);
+            if (!ok) break;
+          }
+          ok = mbar_wait(&s.v_full[st], (it / S::kStages) & 1, limit) &&
+               mbar_wait(&s.p_full, it & 1, limit);
           if (!ok) break;
+          tc_fence_after();
+          const uint32_t va = smem_u32(s.v[st]);
+          const int steps = keys(j) / 16;
+          for (int c = 0; c < steps; ++c)
+            umma_ts(tmem + S::kOut, tmem + S::weights(16 * c), umma_desc(va + c * 2048, kBlock),
+                    idesc_o, j > x.tile || c > 0);
+          umma_commit(&s.o_done);
+          umma_commit(&s.v_empty[st]);
+          if (!S::kOwn && j + 1 < tile1) ok = scores(j + 1, it + 1);
         }
-        ok = mbar_wait(&s.v_full[st], (it / S::kStages) & 1, limit) &&
-             mbar_wait(&s.p_full, it & 1, limit);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t va = smem_u32(s.v[st]);
-        const int steps = keys(j) / 16;
-        for (int c = 0; c < steps; ++c)
-          umma_ts(tmem + S::kOut, tmem + S::weights(16 * c), umma_desc(va + c * 2048, kBlock),
-                  idesc_o, it > 0 || c > 0);
-        umma_commit(&s.o_done);
-        umma_commit(&s.v_empty[st]);
-        if (!S::kOwn && j + 1 < tile1) ok = scores(j + 1);
+        todo -= tile1 - x.tile;
+        x.next_item(p);
       }
     }
   } else {
     // -------------------------------------------------------------- rows
+    // (while the first copies are on their way: the requests' statuses)
+    for (int b = blockIdx.x; b < a.B; b += p.ctas) {
+      const Request r = request(a, b);
+      const bool bad = __any_sync(0xffffffffu, !r.status && out_of_range(a, b, r, t));
+      if (t == 0) s.up[0] = 0;
+      asm volatile("bar.sync 5, 256;" ::: "memory");
+      if (bad && lane == 0) s.up[0] = 1;
+      asm volatile("bar.sync 5, 256;" ::: "memory");
+      if (t == 0) a.status[b] = r.status | (s.up[0] ? TT_REQ_ID_OUT_OF_RANGE : 0);
+      asm volatile("bar.sync 5, 256;" ::: "memory");
+    }
     const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-    const bool some = quarter * 32 < rows;                        // (others only keep step)
     const int local = row / p.group;                              // token of the row
+    const int per = kTile / p.box;
     // tells the row's other thread x, and returns what that told (turn: of two)
-    auto other = [&](float x, int turn) {
-      s.half[turn][half][row] = x;
+    auto other = [&](float y, int turn) {
+      s.half[turn][half][row] = y;
       asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
       return s.half[turn][half ^ 1][row];
     };
-    if (has_tree) {
-      // a token's ancestors: one thread walks up from each token
-      if (t < node1 - node0) {
-        const int w1 = tree_tiles(node1) * (kTile / 32);
-        for (int w = 0; w < w1; ++w) s.seen[t][w] = 0;
-        for (int i = node0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
+    int it = 0;
+    while (todo > 0) {
+      const int n_cache = cache_tiles(x.r.len);
+      const int node0 = x.mt * p.per_tile, node1 = min(x.r.nodes, node0 + p.per_tile);
+      const int rows = (node1 - node0) * p.group;
+      const int tiles = n_cache + tree_tiles(node1), tile1 = min(tiles, x.tile + todo);
+      const bool some = quarter * 32 < rows;  // (others only keep step)
+      const bool has_tree = tile1 > n_cache;
+      if (has_tree) {
+        // a token's ancestors: one thread walks up from each token
+        asm volatile("bar.sync 5, 256;" ::: "memory");  // (done with the last ones)
+        if (t < kWords) s.odd[t] = 0;
+        for (int i = t; i < node1; i += kRowThreads) {
+          const int up = a.parents ? a.parents[x.r.first + i] : i - 1;
+          s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
+        }
+        asm volatile("bar.sync 5, 256;" ::: "memory");
+        if (t < node1 - node0) {
+          const int w1 = tree_tiles(node1) * (kTile / 32);
+          for (int w = 0; w < w1; ++w) s.seen[t][w] = 0;
+          for (int i = node0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
+        }
+        asm volatile("bar.sync 5, 256;" ::: "memory");
       }
-      asm volatile("bar.sync 5, 256;" ::: "memory");
-    }
-    auto box_ok = [&](int tile) {  // whether box `lane` of a cache tile is in range
-      const int slot = tile * kTile + lane * p.box;
-      if (tile >= min(tile1, n_cache) || lane >= per || slot >= r.len) return true;
-      const int page = a.page_table[b * a.table_stride + slot / a.page_size];
-      return page >= 0 && page < a.n_pages;
-    };
-    bool good = box_ok(tile0);
-    float m = -INFINITY, l = 0.f;  // the reference maximum (of scores) and the sum
-    for (int j = tile0; j < tile1; ++j) {
-      const int it = j - tile0, st = it % S::kStages;
-      const uint32_t parity = (it / S::kStages) & 1;
-      const bool cache = j < n_cache;
-      const int base = (j - n_cache) * kTile;  // first drafted token of a tree tile
-      const int left = cache ? r.len - j * kTile : node1 - base;
-      const int n = min(kTile, (left + 31) & ~31);
-      const uint32_t bad_boxes = ~__ballot_sync(0xffffffffu, good);
-      good = box_ok(j + 1);
-      // which of 32 keys from c on the row sees; `there`: which hold anything
-      auto there = [&](int c) {
-        uint32_t w = left - c >= 32 ? 0xffffffffu : (1u << max(0, left - c)) - 1;
-        if (bad_boxes)
-          for (int i = 0; i < 32; i += 16)
-            if (bad_boxes >> ((c + i) / p.box) & 1) w &= ~(0xffffu << i);
-        return w;
+      auto box_ok = [&](int tile) {  // whether box `lane` of a cache tile is in range
+        const int slot = tile * kTile + lane * p.box;
+        if (tile >= min(tile1, n_cache) || lane >= per || slot >= x.r.len) return true;
+        const int page = a.page_table[x.b * a.table_stride + slot / a.page_size];
+        return page >= 0 && page < a.n_pages;
       };
-      auto sees = [&](int c) {
-        return cache ? there(c) : local < node1 - node0 ? s.seen[local][(base + c) >> 5] : 0u;
-      };
-      // (the warp goes on, or gives up, as one)
-      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
-      tc_fence_after();
-      // this thread's half of the row's scores, 32 at a time
-      const int c0 = 64 * half, c1 = min(n, c0 + 64);
-      float f = 1.f;
-      bool raised = false;
-      if (some) {
-        float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      bool good = box_ok(x.tile);
+      float m = -INFINITY, l = 0.f;  // the reference maximum (of scores) and the sum
+      for (int j = x.tile; j < tile1; ++j, ++it) {
+        const int st = it % S::kStages;
+        const uint32_t parity = (it / S::kStages) & 1;
+        const bool cache = j < n_cache;
+        const int base = (j - n_cache) * kTile;  // first drafted token of a tree tile
+        const int left = cache ? x.r.len - j * kTile : node1 - base;
+        const int n = min(kTile, (left + 31) & ~31);
+        const uint32_t bad_boxes = ~__ballot_sync(0xffffffffu, good);
+        good = box_ok(j + 1);
+        // which of 32 keys from c on the row sees; `there`: which hold anything
+        auto there = [&](int c) {
+          uint32_t w = left - c >= 32 ? 0xffffffffu : (1u << max(0, left - c)) - 1;
+          if (bad_boxes)
+            for (int i = 0; i < 32; i += 16)
+              if (bad_boxes >> ((c + i) / p.box) & 1) w &= ~(0xffffu << i);
+          return w;
+        };
+        auto sees = [&](int c) {
+          return cache ? there(c) : local < node1 - node0 ? s.seen[local][(base + c) >> 5] : 0u;
+        };
+        // (the warp goes on, or gives up, as one)
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
+        tc_fence_after();
+        // this thread's half of the row's scores, 32 at a time
+        const int c0 = 64 * half, c1 = min(n, c0 + 64);
+        float f = 1.f;
+        bool raised = false;
+        if (some) {
+          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll 1
-        for (int c = c0; c < c1; c += 32) {
-          uint32_t v[32];
-          tmem_ld32(mine + c, v);
-          const uint32_t see = sees(c);
-          tmem_wait_ld(v);
-          if (see != 0xffffffffu) hide(v, see);
-          __syncwarp();
+          for (int c = c0; c < c1; c += 32) {
+            uint32_t v[32];
+            tmem_ld32(mine + c, v);
+            const uint32_t see = sees(c);
+            tmem_wait_ld(v);
+            if (see != 0xffffffffu) hide(v, see);
+            __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i]));
-        }
-        float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-        high = fmaxf(high, other(high, it & 1));
-        // the reference follows the maximum, and with it the sums
-        const bool raise = (high - m) * p.scale2 > kSlack || (m == -INFINITY && high > -INFINITY);
-        raised = __any_sync(0xffffffffu, raise);
-        if (raised) {
-          const float to = fmaxf(m, high);
-          f = m == -INFINITY ? 0.f : ex2_approx((m - to) * p.scale2);
-          m = to;
-          l *= f;
-        }
-      }
-      uint32_t w[32];  // the weights, two to a word
-      if (some) {
-        const float shift = (m == -INFINITY ? 0.f : -m * p.scale2) + kOffset;
-        const f32x2 scale2 = pair(p.scale2, p.scale2), shift2 = pair(shift, shift);
-        f32x2 sum2 = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int c = c0 + 32 * h;
-          if (c >= c1) break;
-          uint32_t v[32];
-          tmem_ld32(mine + c, v);
-          const uint32_t see = sees(c);
-          tmem_wait_ld(v);
-          if (see != 0xffffffffu) hide(v, see);
-          __syncwarp();
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const f32x2 e = exp2_pair(
-                fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale2, shift2));
-            sum2 = add2(sum2, e);
-            float lo, hi;
-            split(e, lo, hi);
-            w[16 * h + i] = pack2<F16>(lo, hi);
+            for (int i = 0; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i]));
+          }
+          float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          high = fmaxf(high, other(high, it & 1));
+          // the reference follows the maximum, and with it the sums
+          const bool raise = (high - m) * p.scale2 > kSlack || (m == -INFINITY && high > -INFINITY);
+          raised = __any_sync(0xffffffffu, raise);
+          if (raised) {
+            const float to = fmaxf(m, high);
+            f = m == -INFINITY ? 0.f : ex2_approx((m - to) * p.scale2);
+            m = to;
+            l *= f;
           }
         }
-        l += sum_pair(sum2);
-        tc_fence_before();
-      }
-      // Weights of their own: the scores' place is free, and the last tile's product
-      // has to be done with the weights' place and in the output. (Every warp waits
-      // for that, or one without rows would be a tile ahead on p_full.)
-      if (S::kOwn) {
-        mbar_arrive(&s.s_free);
-        if (it > 0) {
-          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
-          tc_fence_after();
-        }
-      }
-      if (some) {
-        const uint32_t to = mine + S::weights(c0);
-        if (c0 + 32 < c1)
-          tmem_st32(to, w);
-        else if (c0 < c1)
-          tmem_st16(to, w);
-        if (raised && it > 0) {
-#pragma unroll 1
-          for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
-            uint32_t o[32];
-            tmem_ld32(mine + S::kOut + c, o);
-            tmem_wait_ld(o);
+        uint32_t w[32];  // the weights, two to a word
+        if (some) {
+          const float shift = (m == -INFINITY ? 0.f : -m * p.scale2) + kOffset;
+          const f32x2 scale2 = pair(p.scale2, p.scale2), shift2 = pair(shift, shift);
+          f32x2 sum2 = 0;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st32(mine + S::kOut + c, o);
-          }
-        }
-        tmem_wait_st();
-      }
-      // Values that no row may touch: slots past the end (0 times what is there
-      // could be NaN), and of drafted tokens, what is not finite: a token outside
-      // its branch would get NaN from it. (Its own branch gets it at the end.)
-      if (left < n || bad_boxes || !cache) {
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.v_full[st], parity, limit)))) break;
-        for (int i = t; i < n * kHalves * 8; i += kRowThreads) {
-          const int key = (i >> 3) % n, block = (i >> 3) / n;
-          uint4* at = reinterpret_cast<uint4*>(s.v[st] + block * kBlock + key * 128 + (i & 7) * 16);
-          if (!(there(key & ~31) >> (key & 31) & 1)) {
-            *at = make_uint4(0, 0, 0, 0);
-          } else if (!cache) {
-            constexpr uint16_t kExp = F16 ? 0x7c00 : 0x7f80;
-            uint4 w = *at;
-            uint16_t* e = reinterpret_cast<uint16_t*>(&w);
-            bool odd = false;
+          for (int h = 0; h < 2; ++h) {
+            const int c = c0 + 32 * h;
+            if (c >= c1) break;
+            uint32_t v[32];
+            tmem_ld32(mine + c, v);
+            const uint32_t see = sees(c);
+            tmem_wait_ld(v);
+            if (see != 0xffffffffu) hide(v, see);
+            __syncwarp();
 #pragma unroll
-            for (int q = 0; q < 8; ++q)
-              if ((e[q] & kExp) == kExp) {
-                e[q] = 0;
-                odd = true;
-              }
-            if (odd) {
-              *at = w;
-              atomicOr(&s.odd[(base + key) >> 5], 1u << ((base + key) & 31));
+            for (int i = 0; i < 16; ++i) {
+              const f32x2 e = exp2_pair(
+                  fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale2, shift2));
+              sum2 = add2(sum2, e);
+              float lo, hi;
+              split(e, lo, hi);
+              w[16 * h + i] = pack2<F16>(lo, hi);
             }
           }
+          l += sum_pair(sum2);
+          tc_fence_before();
         }
-        fence_proxy_async();
-      }
-      tc_fence_before();
-      mbar_arrive(&s.p_full);
-    }
-    if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (tile1 - tile0 - 1) & 1, limit));
-    tc_fence_after();
-    if (has_tree) asm volatile("bar.sync 5, 256;" ::: "memory");  // (s.odd is whole)
-    if (ok && some) {
-      l += other(l, (tile1 - tile0) & 1);
-      const bool valid = row < rows;
-      const int node = r.first + node0 + local, h = hk * p.group + row % p.group;
-      const int64_t to = int64_t(node) * a.Hq + h;  // row of the outputs
-      const bool whole = runs == 1;
-      const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-      const int64_t at = (int64_t(run) * a.n_nodes * a.Hq + to) * D;
-#pragma unroll 1
-      for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
-        uint32_t v[32];
-        tmem_ld32(mine + S::kOut + c, v);
-        tmem_wait_ld(v);
-        if (valid) {
-          if (has_tree) {
-            for (int w = 0; w * 32 < node1; ++w)
-              for (uint32_t odd = s.odd[w] & s.seen[local][w]; odd; odd &= odd - 1) {
-                const int64_t peer = int64_t(r.first) + w * 32 + __ffs(odd) - 1;
-                const uint16_t* e = reinterpret_cast<const uint16_t*>(a.v) + peer * a.v_token +
-                                    hk * a.v_head + c;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  const float y = unpack<F16>(e[i]);
-                  if (!(fabsf(y) < INFINITY)) v[i] = __float_as_uint(__uint_as_float(v[i]) + y);
-                }
-              }
+        // Weights of their own: the scores' place is free, and the last tile's product
+        // has to be done with the weights' place and in the output. (Every warp waits
+        // for that, or one without rows would be a tile ahead on p_full.)
+        if (S::kOwn) {
+          mbar_arrive(&s.s_free);
+          if (it > 0) {
+            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
+            tc_fence_after();
           }
-          if (whole) {
-            char* out = a.out + (to * D + c) * 2;
+        }
+        if (some) {
+          const uint32_t to = mine + S::weights(c0);
+          if (c0 + 32 < c1)
+            tmem_st32(to, w);
+          else if (c0 < c1)
+            tmem_st16(to, w);
+          if (raised && j > x.tile) {
+#pragma unroll 1
+            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+              uint32_t o[32];
+              tmem_ld32(mine + S::kOut + c, o);
+              tmem_wait_ld(o);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              uint32_t o[8];
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st32(mine + S::kOut + c, o);
+            }
+          }
+          tmem_wait_st();
+        }
+        // Values that no row may touch: slots past the end (0 times what is there
+        // could be NaN), and of drafted tokens, what is not finite: a token outside
+        // its branch would get NaN from it. (Its own branch gets it at the end.)
+        if (left < n || bad_boxes || !cache) {
+          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.v_full[st], parity, limit)))) break;
+          for (int i = t; i < n * kHalves * 8; i += kRowThreads) {
+            const int key = (i >> 3) % n, block = (i >> 3) / n;
+            uint4* at = reinterpret_cast<uint4*>(s.v[st] + block * kBlock + key * 128 + (i & 7) * 16);
+            if (!(there(key & ~31) >> (key & 31) & 1)) {
+              *at = make_uint4(0, 0, 0, 0);
+            } else if (!cache) {
+              constexpr uint16_t kExp = F16 ? 0x7c00 : 0x7f80;
+              uint4 w = *at;
+              uint16_t* e = reinterpret_cast<uint16_t*>(&w);
+              bool odd = false;
 #pragma unroll
               for (int q = 0; q < 8; ++q)
-                o[q] = pack2<F16>(__uint_as_float(v[16 * i + 2 * q]) * inv,
-                                  __uint_as_float(v[16 * i + 2 * q + 1]) * inv);
-              store_sector<true>(out + 32 * i, o);
-            }
-          } else {
-            char* out = reinterpret_cast<char*>(p.part + at + c);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              uint32_t o[8];
-#pragma unroll
-              for (int q = 0; q < 8; ++q) o[q] = v[8 * i + q];
-              store_sector<false>(out + 32 * i, o);
+                if ((e[q] & kExp) == kExp) {
+                  e[q] = 0;
+                  odd = true;
+                }
+              if (odd) {
+                *at = w;
+                atomicOr(&s.odd[(base + key) >> 5], 1u << ((base + key) & 31));
+              }
             }
           }
+          fence_proxy_async();
         }
-        __syncwarp();
+        tc_fence_before();
+        mbar_arrive(&s.p_full);
       }
-      if (valid && half == 0) {
-        const float m2 = m == -INFINITY ? -INFINITY : m * p.scale2 - kOffset;
-        if (!whole)
-          p.part_ml[int64_t(run) * a.n_nodes * a.Hq + to] = make_float2(m2, l);
-        else if (a.lse)
-          a.lse[to] = l > 0.f || l != l ? fmaf(m2, kLn2, logf(l)) : -INFINITY;
+      if (!ok) {
+        if (t == 0) a.status[x.b] = TT_REQ_TIMEOUT;
+        break;
       }
-    }
-    if (reports) {
-      bool bad = out_of_range(a, b, r, t);
-      bad = __any_sync(0xffffffffu, bad);
-      if (bad && lane == 0) atomicOr(&s.failed, 2);
+      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
+      tc_fence_after();
+      if (has_tree) asm volatile("bar.sync 5, 256;" ::: "memory");  // (s.odd is whole)
+      if (some) {
+        l += other(l, it & 1);
+        const bool valid = row < rows, whole = x.tile == 0 && tile1 == tiles;
+        // where the row goes: to the output, or to its place in the CTA's piece
+        const int64_t to =
+            whole ? (int64_t(x.r.first) + node0 + local) * a.Hq + x.hk * p.group + row % p.group
+                  : (2 * int64_t(blockIdx.x) + (x.tile == 0)) * p.rows + row;
+        const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+#pragma unroll 1
+        for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+          uint32_t v[32];
+          tmem_ld32(mine + S::kOut + c, v);
+          tmem_wait_ld(v);
+          if (valid) {
+            if (has_tree) {
+              for (int w = 0; w * 32 < node1; ++w)
+                for (uint32_t odd = s.odd[w] & s.seen[local][w]; odd; odd &= odd - 1) {
+                  const int64_t peer = int64_t(x.r.first) + w * 32 + __ffs(odd) - 1;
+                  const uint16_t* e = reinterpret_cast<const uint16_t*>(a.v) + peer * a.v_token +
+                                      x.hk * a.v_head + c;
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) {
+                    const float y = unpack<F16>(e[i]);
+                    if (!(fabsf(y) < INFINITY)) v[i] = __float_as_uint(__uint_as_float(v[i]) + y);
+                  }
+                }
+            }
+            if (whole) {
+              char* out = a.out + (to * D + c) * 2;
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                uint32_t o[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                  o[q] = pack2<F16>(__uint_as_float(v[16 * i + 2 * q]) * inv,
+                                    __uint_as_float(v[16 * i + 2 * q + 1]) * inv);
+                store_sector<true>(out + 32 * i, o);
+              }
+            } else {
+              char* out = reinterpret_cast<char*>(p.part + to * D + c);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t o[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) o[q] = v[8 * i + q];
+                store_sector<false>(out + 32 * i, o);
+              }
+            }
+          }
+          __syncwarp();
+        }
+        if (valid && half == 0) {
+          const float m2 = m == -INFINITY ? -INFINITY : m * p.scale2 - kOffset;
+          if (!whole)
+            p.part_ml[to] = make_float2(m2, l);
+          else if (a.lse)
+            a.lse[to] = l > 0.f || l != l ? fmaf(m2, kLn2, logf(l)) : -INFINITY;
+        }
+        tc_fence_before();
+      }
+      todo -= tile1 - x.tile;
+      x.next_item(p);
     }
   }
   if (!ok) atomicOr(&s.failed, 1);
   tc_fence_before();
   __syncthreads();
   if (warp == kRowWarps + 1) tmem_free(tmem, kTmemColumns);
-  if (t == 0 && (reports || (s.failed & 1)))
-    a.status[b] = (s.failed & 1 ? TT_REQ_TIMEOUT : 0) | (s.failed & 2 ? TT_REQ_ID_OUT_OF_RANGE : 0);
+  if (t == 0 && s.failed && todo > 0) a.status[x.b] = TT_REQ_TIMEOUT;
 }
 
-// Joins the runs of every row that has more than one: with M the largest of the
-// runs' references, out = sum 2^(m - M) o / sum 2^(m - M) l. W warps take a row's
-// runs in turn, each reads a run's output in one go: one warp for a few runs
-// (rows are many then: a CTA for each of 32,768 rows with two runs took 50 us more
+// Joins the pieces of every row whose item was cut: with M the largest of their
+// references, out = sum 2^(m - M) o / sum 2^(m - M) l. W warps take a row's pieces
+// in turn, each reads a piece's output in one go: one warp for a few pieces (rows
+// are many then: a CTA for each of 32,768 rows with two pieces took 50 us more
 // than a warp), four for more.
 constexpr int kJoinWarps = 4;
 
@@ -622,21 +732,29 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   if (b >= a.B) return;
   const Request r = request(a, b);
   if (i >= r.nodes) return;
-  const int end = min(r.nodes, (i / p.per_tile + 1) * p.per_tile);
-  const int runs = run_count(cache_tiles(r.len) + tree_tiles(end), p.run);
-  if (runs < 2) return;
   grid_dependency_wait();
-  const int64_t row = (int64_t(r.first) + i) * a.Hq + h, rows = int64_t(a.n_nodes) * a.Hq;
+  // the CTAs that the row's item lies in, c0 .. c1
+  const int mt = i / p.per_tile, hk = h / p.group;
+  int before = p.first[b] + hk * head_tiles(p, r);
+  for (int k = 0; k < mt; ++k) before += item_tiles(p, r, k);
+  const int share = p.first[a.B];
+  const int c0 = before / share, c1 = (before + item_tiles(p, r, mt) - 1) / share;
+  if (c0 == c1) return;
+  const int pieces = c1 - c0 + 1;
+  const int in_item = (i - mt * p.per_tile) * p.group + h % p.group;
+  auto place = [&](int s) {  // of the row in piece s
+    return (2 * (int64_t(c0) + s) + (s == 0)) * p.rows + in_item;
+  };
   float M = -INFINITY;
-  for (int s = lane; s < runs; s += 32) M = fmaxf(M, p.part_ml[s * rows + row].x);
+  for (int s = lane; s < pieces; s += 32) M = fmaxf(M, p.part_ml[place(s)].x);
   M = warp_max_f(M);
   float acc[N] = {};
   float l = 0.f;
 #pragma unroll 4
-  for (int s = warp; s < runs; s += W) {
-    const float2 ml = p.part_ml[s * rows + row];
-    const Vec o = reinterpret_cast<const Vec*>(p.part + (s * rows + row) * D)[lane];
-    // (a run of nothing but -inf scores: 0, whatever the maximum is)
+  for (int s = warp; s < pieces; s += W) {
+    const float2 ml = p.part_ml[place(s)];
+    const Vec o = reinterpret_cast<const Vec*>(p.part + place(s) * D)[lane];
+    // (a piece of nothing but -inf scores: 0, whatever the maximum is)
     const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
     l = fmaf(ml.y, f, l);
     acc[0] = fmaf(o.x, f, acc[0]);
@@ -660,6 +778,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
     }
   }
   const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const int64_t row = (int64_t(r.first) + i) * a.Hq + h;
   uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
   out[0] = pack2<F16>(acc[0] * inv, acc[1] * inv);
   if constexpr (N == 4) out[1] = pack2<F16>(acc[2] * inv, acc[3] * inv);
@@ -668,24 +787,29 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
 
 // ------------------------------------------------------------------- host
 
-constexpr int kMinRun = 2, kWaves = 1;
-// How a call is cut: tokens per tile of rows, tiles per run, runs.
+// How a call is cut: tokens per tile of rows, CTAs, and the workspace.
 struct Cut {
-  int group, per_tile, row_tiles, run, runs;
-  size_t part_bytes, bytes;
+  int group, per_tile, ctas, rows;
+  int64_t pieces;  // of one item, about
+  size_t part_bytes, ml_bytes, bytes;
 };
 Cut cut(const TreeArgs& a, int sm_count) {
   Cut c;
   c.group = a.Hq / a.Hkv;
   c.per_tile = kTile / c.group;
-  c.row_tiles = (a.max_nodes + c.per_tile - 1) / c.per_tile;
-  const int tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);
-  const int64_t items = int64_t(a.B) * a.Hkv * c.row_tiles, slots = 2 * int64_t(sm_count);
-  c.run = int(std::max<int64_t>(kMinRun, (items * tiles + slots * kWaves - 1) / (slots * kWaves)));
-  c.runs = run_count(tiles, c.run);
-  const size_t rows = size_t(c.runs) * a.n_nodes * a.Hq;
-  c.part_bytes = c.runs > 1 ? align256(rows * a.D * sizeof(float)) : 0;
-  c.bytes = c.part_bytes + (c.runs > 1 ? align256(rows * sizeof(float2)) : 0);
+  const int64_t row_tiles = (a.max_nodes + c.per_tile - 1) / c.per_tile;
+  const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
+  const int64_t all = int64_t(a.B) * a.Hkv * row_tiles * tiles;
+  c.ctas = int(std::max<int64_t>(1, std::min<int64_t>(2 * int64_t(sm_count),
+                                                      (all + kMinShare - 1) / kMinShare)));
+  // (were all lengths the longest; fewer tiles make shares smaller and pieces more)
+  const int64_t share = std::max<int64_t>(kMinShare, (all + c.ctas - 1) / c.ctas);
+  c.pieces = tiles / share + 2;
+  c.rows = std::min(a.max_nodes, c.per_tile) * c.group;
+  const size_t rows = 2 * size_t(c.ctas) * c.rows;
+  c.part_bytes = align256(rows * a.D * sizeof(float));
+  c.ml_bytes = align256(rows * sizeof(float2));
+  c.bytes = c.part_bytes + c.ml_bytes + align256((size_t(a.B) + 1) * sizeof(int32_t));
   return c;
 }
 
@@ -723,19 +847,19 @@ bool encode(CUtensorMap* map, bool f16, const char* data, int rank, const int64_
 }
 
 template <int D, bool F16>
-cudaError_t launch(const TreeKernelArgs& p, cudaStream_t stream) {
+cudaError_t launch(const TreeKernelArgs& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(int64_t(a.B) * p.runs * a.Hkv * p.row_tiles));
+  cfg.gridDim = dim3(unsigned(p.ctas));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = sizeof(Smem<D>) + 1024;
   cfg.stream = stream;
   cudaError_t e = cudaLaunchKernelEx(&cfg, tree_kernel<D, F16>, p);
-  if (e != cudaSuccess || p.runs == 1) return e;
+  if (e != cudaSuccess || p.ctas == 1) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  const bool few = p.runs <= 8;
+  const bool few = pieces <= 8;
   const int64_t rows = int64_t(a.B) * a.max_nodes * a.Hq;
   cfg.gridDim = dim3(unsigned(few ? (rows + kJoinWarps - 1) / kJoinWarps : rows));
   cfg.blockDim = dim3(kJoinWarps * 32);
@@ -762,21 +886,19 @@ size_t tree_workspace_bytes(const TreeArgs& a, int sm_count) { return cut(a, sm_
 
 cudaError_t launch_tree(const TreeArgs& a, int dt, cudaStream_t stream, int sm_count) {
   const Cut c = cut(a, sm_count);
-  if (int64_t(a.B) * c.runs * a.Hkv * c.row_tiles > INT32_MAX ||
-      int64_t(a.B) * a.max_nodes * a.Hq > INT32_MAX)
-    return cudaErrorInvalidConfiguration;
+  if (int64_t(a.B) * a.max_nodes * a.Hq > INT32_MAX) return cudaErrorInvalidConfiguration;
   TreeKernelArgs p;
   std::memset(&p, 0, sizeof p);
   p.a = a;
   p.scale2 = float(double(a.scale) * 1.4426950408889634);
   p.group = c.group;
   p.per_tile = c.per_tile;
-  p.row_tiles = c.row_tiles;
-  p.run = c.run;
-  p.runs = c.runs;
+  p.ctas = c.ctas;
+  p.rows = c.rows;
   p.box = std::gcd(a.page_size, kTile);
   p.part = reinterpret_cast<float*>(a.ws);
   p.part_ml = reinterpret_cast<float2*>(a.ws + c.part_bytes);
+  p.first = reinterpret_cast<int32_t*>(a.ws + c.part_bytes + c.ml_bytes);
   const bool f16 = dt == TT_F16;
   bool ok = true;
   if (a.n_nodes > 0) {
@@ -798,8 +920,8 @@ cudaError_t launch_tree(const TreeArgs& a, int dt, cudaStream_t stream, int sm_c
     ok = ok && encode(&p.kc, f16, a.kc, 4, n, sk, box) && encode(&p.vc, f16, a.vc, 4, n, sv, box);
   }
   if (!ok) return cudaErrorInvalidValue;
-  if (a.D == 128) return f16 ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
-  return f16 ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
+  if (a.D == 128) return f16 ? launch<128, true>(p, c.pieces, stream) : launch<128, false>(p, c.pieces, stream);
+  return f16 ? launch<64, true>(p, c.pieces, stream) : launch<64, false>(p, c.pieces, stream);
 }
 
 cudaError_t preload_tree() {
