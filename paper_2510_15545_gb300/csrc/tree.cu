@@ -174,11 +174,13 @@ struct Smem {
   uint32_t seen[kTile][kWords];  // a token's ancestors and itself
   int16_t up[TT_MAX_TREE];       // parents, -1 for roots
   float half[2][2][kTile];       // what the two threads of a row tell each other
+  uint32_t left_out[4];          // boxes of the last tiles that were not copied
   uint32_t odd[kWords];          // drafted tokens with a value that is not finite
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t q_empty, s_full, s_free, p_full, o_done;
   long long sums[kThreads / 32];  // tiles of the requests, by warps
   int start_b, start_offset;      // where this CTA's tiles begin
+  Place place[kRowWarps];         // where the row warps are (their registers are dear)
   uint32_t tmem;
   int failed;
 };
@@ -302,11 +304,11 @@ __global__ void __launch_bounds__(kThreads, 2)
   __syncthreads();
   const uint32_t tmem = s.tmem;
   bool ok = true;
-  Place x;
-  if (todo > 0) x.find(p, s.start_b, s.start_offset);
 
   if (warp == kRowWarps) {
     // ------------------------------------------------------------ copies
+    Place x;
+    if (todo > 0) x.find(p, s.start_b, s.start_offset);
     // lane i copies a tile's i-th box of slots
     const int per = kTile / p.box;
     int it = 0;
@@ -347,7 +349,8 @@ __global__ void __launch_bounds__(kThreads, 2)
           mine = lane < kTile / 16 && (j - n_cache) * kTile + at < node1;
           bytes = 16 * 128;
         }
-        const int boxes = __popc(__ballot_sync(0xffffffffu, mine));
+        const unsigned int copied = __ballot_sync(0xffffffffu, mine);
+        const int boxes = __popc(copied);
         auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* paged,
                         const CUtensorMap* own) {
           if (lane == 0) mbar_arrive_expect_tx(bar, boxes * bytes * kHalves);
@@ -370,6 +373,11 @@ __global__ void __launch_bounds__(kThreads, 2)
         };
         ok = __all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit));
         if (!ok) break;
+        // boxes of slots in use whose page is out of range (told before the copy is)
+        if (lane == 0)
+          s.left_out[it & 3] =
+              cache ? ~copied & ((1u << (min(kTile, x.r.len - j * kTile) + p.box - 1) / p.box) - 1)
+                    : 0u;
         copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
         ok = __all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit));
         if (!ok) break;
@@ -382,6 +390,8 @@ __global__ void __launch_bounds__(kThreads, 2)
   } else if (warp == kRowWarps + 1) {
     // ---------------------------------------------------------- products
     if (lane == 0) {
+      Place x;
+      if (todo > 0) x.find(p, s.start_b, s.start_offset);
       const uint32_t idesc_o = umma_idesc(F16, D, true);
       int it = 0;
       for (int seg = 0; todo > 0 && ok; ++seg) {
@@ -452,22 +462,25 @@ __global__ void __launch_bounds__(kThreads, 2)
     const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
     const int local = row / p.group;                              // token of the row
-    const int per = kTile / p.box;
     // tells the row's other thread x, and returns what that told (turn: of two)
     auto other = [&](float y, int turn) {
       s.half[turn][half][row] = y;
       asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
       return s.half[turn][half ^ 1][row];
     };
+    Place& x = s.place[warp];
+    if (todo > 0 && lane == 0) x.find(p, s.start_b, s.start_offset);
+    __syncwarp();
     int it = 0;
     while (todo > 0) {
       const int n_cache = cache_tiles(x.r.len);
-      const int node0 = x.mt * p.per_tile, node1 = min(x.r.nodes, node0 + p.per_tile);
-      const int rows = (node1 - node0) * p.group;
-      const int tiles = n_cache + tree_tiles(node1), tile1 = min(tiles, x.tile + todo);
-      const bool some = quarter * 32 < rows;  // (others only keep step)
-      const bool has_tree = tile1 > n_cache;
-      if (has_tree) {
+      const int node1 = min(x.r.nodes, (x.mt + 1) * p.per_tile);
+      const int tile1 = min(n_cache + tree_tiles(node1), x.tile + todo);
+      auto first_node = [&] { return x.mt * p.per_tile; };
+      const bool valid = row < (node1 - first_node()) * p.group;
+      const bool some = __any_sync(0xffffffffu, valid);  // (others only keep step)
+      if (tile1 > n_cache) {
+        const int node0 = first_node();
         // a token's ancestors: one thread walks up from each token
         asm volatile("bar.sync 5, 256;" ::: "memory");  // (done with the last ones)
         if (t < kWords) s.odd[t] = 0;
@@ -483,13 +496,6 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         asm volatile("bar.sync 5, 256;" ::: "memory");
       }
-      auto box_ok = [&](int tile) {  // whether box `lane` of a cache tile is in range
-        const int slot = tile * kTile + lane * p.box;
-        if (tile >= min(tile1, n_cache) || lane >= per || slot >= x.r.len) return true;
-        const int page = a.page_table[x.b * a.table_stride + slot / a.page_size];
-        return page >= 0 && page < a.n_pages;
-      };
-      bool good = box_ok(x.tile);
       float m = -INFINITY, l = 0.f;  // the reference maximum (of scores) and the sum
       for (int j = x.tile; j < tile1; ++j, ++it) {
         const int st = it % S::kStages;
@@ -498,8 +504,10 @@ __global__ void __launch_bounds__(kThreads, 2)
         const int base = (j - n_cache) * kTile;  // first drafted token of a tree tile
         const int left = cache ? x.r.len - j * kTile : node1 - base;
         const int n = min(kTile, (left + 31) & ~31);
-        const uint32_t bad_boxes = ~__ballot_sync(0xffffffffu, good);
-        good = box_ok(j + 1);
+        // (the warp goes on, or gives up, as one)
+        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
+        tc_fence_after();
+        const uint32_t bad_boxes = s.left_out[it & 3];
         // which of 32 keys from c on the row sees; `there`: which hold anything
         auto there = [&](int c) {
           uint32_t w = left - c >= 32 ? 0xffffffffu : (1u << max(0, left - c)) - 1;
@@ -509,11 +517,8 @@ __global__ void __launch_bounds__(kThreads, 2)
           return w;
         };
         auto sees = [&](int c) {
-          return cache ? there(c) : local < node1 - node0 ? s.seen[local][(base + c) >> 5] : 0u;
+          return cache ? there(c) : valid ? s.seen[local][(base + c) >> 5] : 0u;
         };
-        // (the warp goes on, or gives up, as one)
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
-        tc_fence_after();
         // this thread's half of the row's scores, 32 at a time
         const int c0 = 64 * half, c1 = min(n, c0 + 64);
         float f = 1.f;
@@ -638,13 +643,14 @@ __global__ void __launch_bounds__(kThreads, 2)
       }
       if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
       tc_fence_after();
+      const bool has_tree = tile1 > n_cache;
       if (has_tree) asm volatile("bar.sync 5, 256;" ::: "memory");  // (s.odd is whole)
       if (some) {
         l += other(l, it & 1);
-        const bool valid = row < rows, whole = x.tile == 0 && tile1 == tiles;
+        const bool whole = x.tile == 0 && tile1 == n_cache + tree_tiles(node1);
         // where the row goes: to the output, or to its place in the CTA's piece
         const int64_t to =
-            whole ? (int64_t(x.r.first) + node0 + local) * a.Hq + x.hk * p.group + row % p.group
+            whole ? (int64_t(x.r.first) + first_node() + local) * a.Hq + x.hk * p.group + row % p.group
                   : (2 * int64_t(blockIdx.x) + (x.tile == 0)) * p.rows + row;
         const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
 #pragma unroll 1
@@ -700,89 +706,113 @@ __global__ void __launch_bounds__(kThreads, 2)
         tc_fence_before();
       }
       todo -= tile1 - x.tile;
-      x.next_item(p);
+      __syncwarp();
+      if (lane == 0) x.next_item(p);
+      __syncwarp();
     }
   }
   if (!ok) atomicOr(&s.failed, 1);
   tc_fence_before();
   __syncthreads();
   if (warp == kRowWarps + 1) tmem_free(tmem, kTmemColumns);
-  if (t == 0 && s.failed && todo > 0) a.status[x.b] = TT_REQ_TIMEOUT;
+  if (t == 0 && s.failed && todo > 0) a.status[s.place[0].b] = TT_REQ_TIMEOUT;
 }
 
 // Joins the pieces of every row whose item was cut: with M the largest of their
-// references, out = sum 2^(m - M) o / sum 2^(m - M) l. W warps take a row's pieces
-// in turn, each reads a piece's output in one go: one warp for a few pieces (rows
-// are many then: a CTA for each of 32,768 rows with two pieces took 50 us more
-// than a warp), four for more.
-constexpr int kJoinWarps = 4;
+// references, out = sum 2^(m - M) o / sum 2^(m - M) l. A few pieces: a warp takes
+// a token's rows of a key head, kJoinRows at once (rows are many then, and what
+// they wait for is the way to their pieces). More: the CTA's warps take a row's
+// pieces in turn.
+constexpr int kJoinWarps = 4, kJoinRows = 4;
 
-template <int D, bool F16, int W>
+template <int D, bool F16, bool FEW>
 __global__ void __launch_bounds__(kJoinWarps * 32)
     tree_join_kernel(const __grid_constant__ TreeKernelArgs p) {
-  constexpr int N = D / 32;
+  constexpr int N = D / 32, R = FEW ? kJoinRows : 1, W = FEW ? 1 : kJoinWarps;
   using Vec = typename std::conditional<N == 4, float4, float2>::type;
-  __shared__ float s_acc[W == 1 ? 1 : W][D];
+  __shared__ float s_acc[W][D];
   __shared__ float s_l[W];
   const TreeArgs& a = p.a;
-  const int warp = W == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // row x of the B * max_nodes * Hq that there may be
-  const unsigned int x = W == 1 ? blockIdx.x * kJoinWarps + (threadIdx.x >> 5) : blockIdx.x;
-  const int h = int(x % a.Hq), i = int(x / a.Hq % a.max_nodes), b = int(x / a.Hq / a.max_nodes);
+  const int warp = FEW ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+  // token i of request b and key head hk (FEW), or the head h too
+  const unsigned int x = FEW ? blockIdx.x * kJoinWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const unsigned int heads = FEW ? a.Hkv : a.Hq;
+  const int head = int(x % heads), i = int(x / heads % a.max_nodes);
+  const int b = int(x / heads / a.max_nodes);
   if (b >= a.B) return;
   const Request r = request(a, b);
   if (i >= r.nodes) return;
-  grid_dependency_wait();
-  // the CTAs that the row's item lies in, c0 .. c1
-  const int mt = i / p.per_tile, hk = h / p.group;
-  int before = p.first[b] + hk * head_tiles(p, r);
+  const int hk = FEW ? head : head / p.group;
+  const int mt = i / p.per_tile;
+  int before = hk * head_tiles(p, r);
   for (int k = 0; k < mt; ++k) before += item_tiles(p, r, k);
-  const int share = p.first[a.B];
-  const int c0 = before / share, c1 = (before + item_tiles(p, r, mt) - 1) / share;
-  if (c0 == c1) return;
-  const int pieces = c1 - c0 + 1;
-  const int in_item = (i - mt * p.per_tile) * p.group + h % p.group;
-  auto place = [&](int s) {  // of the row in piece s
-    return (2 * (int64_t(c0) + s) + (s == 0)) * p.rows + in_item;
-  };
-  float M = -INFINITY;
-  for (int s = lane; s < pieces; s += 32) M = fmaxf(M, p.part_ml[place(s)].x);
-  M = warp_max_f(M);
-  float acc[N] = {};
-  float l = 0.f;
-#pragma unroll 4
-  for (int s = warp; s < pieces; s += W) {
-    const float2 ml = p.part_ml[place(s)];
-    const Vec o = reinterpret_cast<const Vec*>(p.part + place(s) * D)[lane];
-    // (a piece of nothing but -inf scores: 0, whatever the maximum is)
-    const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M);
-    l = fmaf(ml.y, f, l);
-    acc[0] = fmaf(o.x, f, acc[0]);
-    acc[1] = fmaf(o.y, f, acc[1]);
-    if constexpr (N == 4) {
-      acc[2] = fmaf(o.z, f, acc[2]);
-      acc[3] = fmaf(o.w, f, acc[3]);
+  const int last = before + item_tiles(p, r, mt) - 1;
+  grid_dependency_wait();
+  // the CTAs that the item lies in
+  const int share = p.first[a.B], first = p.first[b];
+  const int c0 = (first + before) / share, pieces = (first + last) / share - c0 + 1;
+  if (pieces < 2) return;
+  for (int g0 = FEW ? 0 : head % p.group; g0 < (FEW ? p.group : head % p.group + 1); g0 += R) {
+    const int in_item = (i - mt * p.per_tile) * p.group + g0;
+    auto place = [&](int s, int q) {  // of row q in piece s (past the group: the last)
+      return (2 * (int64_t(c0) + s) + (s == 0)) * p.rows + in_item + min(q, p.group - 1 - g0);
+    };
+    float M[R], l[R], acc[R][N];
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      M[q] = -INFINITY;
+      l[q] = 0.f;
+#pragma unroll
+      for (int c = 0; c < N; ++c) acc[q][c] = 0.f;
+    }
+    for (int s = lane; s < pieces; s += 32) {
+#pragma unroll
+      for (int q = 0; q < R; ++q) M[q] = fmaxf(M[q], p.part_ml[place(s, q)].x);
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) M[q] = warp_max_f(M[q]);
+#pragma unroll 2
+    for (int s = warp; s < pieces; s += W) {
+#pragma unroll
+      for (int q = 0; q < R; ++q) {
+        const float2 ml = p.part_ml[place(s, q)];
+        const Vec o = reinterpret_cast<const Vec*>(p.part + place(s, q) * D)[lane];
+        // (a piece of nothing but -inf scores: 0, whatever the maximum is)
+        const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M[q]);
+        l[q] = fmaf(ml.y, f, l[q]);
+        acc[q][0] = fmaf(o.x, f, acc[q][0]);
+        acc[q][1] = fmaf(o.y, f, acc[q][1]);
+        if constexpr (N == 4) {
+          acc[q][2] = fmaf(o.z, f, acc[q][2]);
+          acc[q][3] = fmaf(o.w, f, acc[q][3]);
+        }
+      }
+    }
+    if constexpr (!FEW) {
+#pragma unroll
+      for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[0][c];
+      if (lane == 0) s_l[warp] = l[0];
+      __syncthreads();
+      if (warp > 0) return;
+#pragma unroll
+      for (int w = 1; w < W; ++w) {
+        l[0] += s_l[w];
+#pragma unroll
+        for (int c = 0; c < N; ++c) acc[0][c] += s_acc[w][lane * N + c];
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      if (g0 + q >= p.group) break;
+      const float inv = l[q] > 0.f || l[q] != l[q] ? 1.f / l[q] : 0.f;
+      const int64_t row = (int64_t(r.first) + i) * a.Hq + hk * p.group + g0 + q;
+      uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
+      out[0] = pack2<F16>(acc[q][0] * inv, acc[q][1] * inv);
+      if constexpr (N == 4) out[1] = pack2<F16>(acc[q][2] * inv, acc[q][3] * inv);
+      if (a.lse && lane == 0)
+        a.lse[row] = l[q] > 0.f || l[q] != l[q] ? fmaf(M[q], kLn2, logf(l[q])) : -INFINITY;
     }
   }
-  if constexpr (W > 1) {
-#pragma unroll
-    for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[c];
-    if (lane == 0) s_l[warp] = l;
-    __syncthreads();
-    if (warp > 0) return;
-#pragma unroll
-    for (int w = 1; w < W; ++w) {
-      l += s_l[w];
-#pragma unroll
-      for (int c = 0; c < N; ++c) acc[c] += s_acc[w][lane * N + c];
-    }
-  }
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
-  const int64_t row = (int64_t(r.first) + i) * a.Hq + h;
-  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
-  out[0] = pack2<F16>(acc[0] * inv, acc[1] * inv);
-  if constexpr (N == 4) out[1] = pack2<F16>(acc[2] * inv, acc[3] * inv);
-  if (a.lse && lane == 0) a.lse[row] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
 }
 
 // ------------------------------------------------------------------- host
@@ -860,21 +890,22 @@ cudaError_t launch(const TreeKernelArgs& p, int64_t pieces, cudaStream_t stream)
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   const bool few = pieces <= 8;
-  const int64_t rows = int64_t(a.B) * a.max_nodes * a.Hq;
-  cfg.gridDim = dim3(unsigned(few ? (rows + kJoinWarps - 1) / kJoinWarps : rows));
+  const int64_t tokens = int64_t(a.B) * a.max_nodes;
+  cfg.gridDim =
+      dim3(unsigned(few ? (tokens * a.Hkv + kJoinWarps - 1) / kJoinWarps : tokens * a.Hq));
   cfg.blockDim = dim3(kJoinWarps * 32);
   cfg.dynamicSmemBytes = 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return few ? cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16, 1>, p)
-             : cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16, kJoinWarps>, p);
+  return few ? cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16, true>, p)
+             : cudaLaunchKernelEx(&cfg, tree_join_kernel<D, F16, false>, p);
 }
 
 template <int D, bool F16>
 cudaError_t preload() {
   cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16, 1>);
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16, kJoinWarps>);
+  cudaError_t e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16, true>);
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree_join_kernel<D, F16, false>);
   if (e != cudaSuccess) return e;
   return cudaFuncSetAttribute(tree_kernel<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               int(sizeof(Smem<D>)) + 1024);
