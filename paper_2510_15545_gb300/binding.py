@@ -696,10 +696,27 @@ def _on(stream):
 
 def _given(t, name, dtype, numel):
     """A contiguous tensor argument of a type and at least a size (None passes)."""
-    if t is not None and (t.dtype != dtype or not t.is_contiguous() or t.numel() < numel):
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < numel or not t.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of %d elements or more"
                          % (name, str(dtype).replace("torch.", ""), numel))
-    return _ptr(t)
+    return t.data_ptr()
+
+
+_LOGITS_DTYPES = {torch.float32: TT_F32, torch.bfloat16: TT_BF16}
+
+
+def _rows(t: torch.Tensor) -> _Logits:
+    """_logits, for calls whose time is the host's."""
+    dt = _LOGITS_DTYPES.get(t.dtype)
+    if dt is None or t.dim() != 2:
+        return _logits(t)
+    stride, col = t.stride()
+    if col != 1:
+        return _logits(t)
+    R, V = t.shape
+    return _Logits(t.data_ptr(), dt, V, stride, R)
 
 
 def tt_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, *, temp: float = 1.0,
@@ -711,8 +728,8 @@ def tt_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, *, tem
     if stream is not None:
         with _on(stream):
             return tt_logprobs(logits, ids, temp=temp, top_n=top_n, out=out)
-    L = _logits(logits)
-    R, n = logits.shape[0], int(top_n)
+    L = _rows(logits)
+    R, n = L.n_rows, int(top_n)
     ids_p = _given(ids, "ids", torch.int32, R)
     if out:
         o, dev = dict(out), logits.device
@@ -777,8 +794,9 @@ def tt_distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: to
         with _on(stream):
             return tt_distill(logits, teacher_ids, teacher_logp, temp=temp, tail=tail,
                               weight=weight, grad=grad, out=out)
-    R = logits.shape[0]
-    L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, R)
+    L = _rows(logits)
+    R = L.n_rows
+    T = _teacher(teacher_ids, teacher_logp, R)
     weight_p = _given(weight, "weight", torch.float32, R)
     if out:
         o, dev = dict(out), logits.device
@@ -798,7 +816,7 @@ def tt_distill(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: to
     G = None
     if grad is not False:
         o["grad"] = _like_rows(logits) if grad is True else grad
-        G = _logits(o["grad"])
+        G = _rows(o["grad"])
     code = load().tt_distill(ctypes.byref(L), ctypes.byref(T), float(temp), int(bool(tail)),
                              weight_p, loss_p, stats_p, None if G is None else ctypes.byref(G),
                              status_p, _stream(stream))
@@ -816,9 +834,9 @@ def tt_distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
         with _on(stream):
             return tt_distill_grad(logits, teacher_ids, teacher_logp, stats, temp=temp, tail=tail,
                                    weight=weight, grad=grad)
-    L, T = _logits(logits), _teacher(teacher_ids, teacher_logp, logits.shape[0])
+    L, T = _rows(logits), _teacher(teacher_ids, teacher_logp, logits.shape[0])
     g = _like_rows(logits) if grad is None else grad
-    G = _logits(g)
+    G = _rows(g)
     R = logits.shape[0]
     code = load().tt_distill_grad(ctypes.byref(L), ctypes.byref(T), float(temp), int(bool(tail)),
                                   _given(weight, "weight", torch.float32, R),
@@ -856,42 +874,46 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: 
 _TREE_DTYPES = {torch.bfloat16: TT_BF16, torch.float16: TT_F16}
 
 
-def _heads(t: torch.Tensor, name: str, like: torch.Tensor, dims: int):
-    """Strides of a tensor [..., heads, head_dim] of the queries' type."""
-    if t.dim() != dims or t.dtype != like.dtype or t.shape[-1] != like.shape[-1]:
+def _heads(t: torch.Tensor, name: str, dtype, D: int, dims: int, C):
+    """Pointer and strides of a tensor [..., heads, head_dim] of the queries' type."""
+    stride = t.stride()
+    if t.dtype is not dtype or len(stride) != dims or t.shape[-1] != D:
         raise ValueError("%s must be a %d-D %s tensor of the queries' head size"
-                         % (name, dims, str(like.dtype).replace("torch.", "")))
-    if t.stride(-1) != 1:
+                         % (name, dims, str(dtype).replace("torch.", "")))
+    if stride[-1] != 1:
         raise ValueError("%s must have unit stride within a head" % name)
-    return t.data_ptr(), *t.stride()[:-1]
+    return C(t.data_ptr(), *stride[:-1])
 
 
 def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
           max_nodes) -> _Tree:
-    if q.dtype not in _TREE_DTYPES:
+    dtype = q.dtype
+    code = _TREE_DTYPES.get(dtype)
+    if code is None:
         raise TypeError("queries must be bfloat16 or float16")
     B, (N, Hq, D) = cache_len.numel(), q.shape
-    if k.shape != v.shape or k.shape[0] != N or k_cache.shape != v_cache.shape \
-            or k_cache.shape[2] != k.shape[1]:
+    shape, cache = k.shape, k_cache.shape
+    if shape != v.shape or shape[0] != N or cache != v_cache.shape or cache[2] != shape[1]:
         raise ValueError("keys and values must be of the same tokens, pages and heads")
-    if page_table.dim() != 2 or page_table.dtype != torch.int32 or page_table.shape[0] != B \
-            or (page_table.numel() and page_table.stride(1) != 1):
+    table = page_table.shape
+    if len(table) != 2 or page_table.dtype is not torch.int32 or table[0] != B:
         raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
-    pages, page, _, _ = k_cache.shape
-    room = page_table.shape[1] * page
+    row, col = page_table.stride()
+    if col != 1 and table[1] > 1:
+        raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
+    room = table[1] * cache[1]
     max_len = room if max_len is None else int(max_len)
     if max_len > room:
         raise ValueError("max_len is more than the page table's rows hold")
-    return _Tree(B, N, min(TT_MAX_TREE, max(N, 1)) if max_nodes is None else int(max_nodes),
-                 _TREE_DTYPES[q.dtype], Hq, k.shape[1], D, page,
-                 _given(tree_off, "tree_off", torch.int32, B + 1),
-                 _given(parents, "parents", torch.int32, N), _Heads(*_heads(q, "q", q, 3)),
-                 _Heads(*_heads(k, "k", q, 3)), _Heads(*_heads(v, "v", q, 3)),
-                 _Pages(*_heads(k_cache, "k_cache", q, 4)),
-                 _Pages(*_heads(v_cache, "v_cache", q, 4)), pages, _ptr(page_table),
-                 max(page_table.stride(0), page_table.shape[1]),
+    return _Tree(B, N, min(TT_MAX_TREE, max(N, 1)) if max_nodes is None else int(max_nodes), code,
+                 Hq, shape[1], D, cache[1], _given(tree_off, "tree_off", torch.int32, B + 1),
+                 _given(parents, "parents", torch.int32, N), _heads(q, "q", dtype, D, 3, _Heads),
+                 _heads(k, "k", dtype, D, 3, _Heads), _heads(v, "v", dtype, D, 3, _Heads),
+                 _heads(k_cache, "k_cache", dtype, D, 4, _Pages),
+                 _heads(v_cache, "v_cache", dtype, D, 4, _Pages), cache[0],
+                 page_table.data_ptr(), max(row, table[1]),
                  _given(cache_len, "cache_len", torch.int32, B), max_len,
-                 float(D ** -0.5 if scale is None else scale))
+                 D ** -0.5 if scale is None else float(scale))
 
 
 def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,

@@ -238,6 +238,9 @@ __global__ void __launch_bounds__(kThreads, 2)
   grid_launch_dependents();
 
   if (t == kRowThreads) {
+    prefetch_map(&p.q);
+    prefetch_map(&p.kc);
+    prefetch_map(&p.vc);
     mbar_init(&s.q_full, 1);
     mbar_init(&s.q_empty, 1);
     for (int i = 0; i < S::kStages; ++i) {
