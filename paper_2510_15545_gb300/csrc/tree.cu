@@ -522,22 +522,24 @@ __global__ void __launch_bounds__(kThreads, 2)
         auto sees = [&](int c) {
           return cache ? there(c) : valid ? s.seen[local][(base + c) >> 5] : 0u;
         };
-        // this thread's half of the row's scores, 32 at a time
-        const int c0 = 64 * half, c1 = min(n, c0 + 64);
+        // this thread's half of the row's scores: read once, weights in their registers
+        // (all of the 64 columns, whatever the tile holds: the rest is hidden)
+        const int c0 = 64 * half;
+        uint32_t v[2][32];
         float f = 1.f;
         bool raised = false;
         if (some) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) tmem_ld32(mine + c0 + 32 * h, v[h]);
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int c = c0; c < c1; c += 32) {
-            uint32_t v[32];
-            tmem_ld32(mine + c, v);
-            const uint32_t see = sees(c);
-            tmem_wait_ld(v);
-            if (see != 0xffffffffu) hide(v, see);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            tmem_wait_ld(v[h]);
+            const uint32_t see = sees(c0 + 32 * h);
+            if (see != 0xffffffffu) hide(v[h], see);
             __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[i]));
+            for (int i = 0; i < 32; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(v[h][i]));
           }
           float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
           high = fmaxf(high, other(high, it & 1));
@@ -550,30 +552,19 @@ __global__ void __launch_bounds__(kThreads, 2)
             m = to;
             l *= f;
           }
-        }
-        uint32_t w[32];  // the weights, two to a word
-        if (some) {
           const float shift = (m == -INFINITY ? 0.f : -m * p.scale2) + kOffset;
           const f32x2 scale2 = pair(p.scale2, p.scale2), shift2 = pair(shift, shift);
           f32x2 sum2 = 0;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const int c = c0 + 32 * h;
-            if (c >= c1) break;
-            uint32_t v[32];
-            tmem_ld32(mine + c, v);
-            const uint32_t see = sees(c);
-            tmem_wait_ld(v);
-            if (see != 0xffffffffu) hide(v, see);
-            __syncwarp();
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              const f32x2 e = exp2_pair(
-                  fma2(pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1])), scale2, shift2));
+              const f32x2 e = exp2_pair(fma2(
+                  pair(__uint_as_float(v[h][2 * i]), __uint_as_float(v[h][2 * i + 1])), scale2, shift2));
               sum2 = add2(sum2, e);
               float lo, hi;
               split(e, lo, hi);
-              w[16 * h + i] = pack2<F16>(lo, hi);
+              v[h][i] = pack2<F16>(lo, hi);
             }
           }
           l += sum_pair(sum2);
@@ -591,10 +582,8 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         if (some) {
           const uint32_t to = mine + S::weights(c0);
-          if (c0 + 32 < c1)
-            tmem_st32(to, w);
-          else if (c0 < c1)
-            tmem_st16(to, w);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) tmem_st16(to + 16 * h, v[h]);
           if (raised && j > x.tile) {
 #pragma unroll 1
             for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
