@@ -53,14 +53,16 @@ struct List {
   int status;
 };
 
-// What the CTAs of a row tell each other: sums relative to `base` (a share of
-// nothing but -inf: 0).
+// What the CTAs of a row tell each other. The columns outside the list have a
+// maximum of their own: a student may hold nearly all of its mass on the list, and
+// what is outside it still has a share of r. (Maxima of nothing are -inf.)
 struct Share {
-  float base;
-  float out;     // sum of 2^((z - base) scale) outside the list
-  float listed;  // the same on the list
-  float mass;    // sum of p on the list,
-  float cross;   // and of p (ln p - (z - base) / T)
+  float m;      // max z,
+  float all;    // and sum of 2^((z - m) scale)
+  float m_out;  // the same outside the list
+  float out;
+  float mass;   // sum of p on the list,
+  float cross;  // and of p (ln p - (z - m) / T), with 0 for an m of -inf
 };
 
 // One warp reads the list of row r for columns c0 .. c1 - 1: p = exp(logp),
@@ -203,24 +205,60 @@ __device__ __forceinline__ void store_elem(char* row, int x, float v) {
   }
 }
 
-// Gradient factors of a row: q_j = 2^((z_j - M) scale) / S.
+// The row's maximum and sums from its CTAs' shares, the same in every CTA:
+// q_j = 2^((z_j - M) scale) / all, t = 2^((m_out - M) scale) out / all.
+struct Row {
+  float M, all, m_out, out;
+};
+// 2^((m - M) scale) x for a sum x relative to m; one of nothing is 0, or NaN.
+__device__ __forceinline__ float relative(float x, float m, float M, float scale) {
+  return m > -INFINITY ? x * ex2_approx((m - M) * scale) : x;
+}
+// (by one warp, a share to a lane: by every thread, it was a tenth of a CTA's work)
+__device__ __forceinline__ Row row_sums(const DistillArgs& a, const Share* share, int S, int lane) {
+  static_assert(kMaxSplit <= 16, "shares of half a warp");
+  Share x{-INFINITY, 0.f, -INFINITY, 0.f, 0.f, 0.f};
+  if (lane < S) x = share[lane];
+  Row y{x.m, 0.f, x.m_out, 0.f};
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    y.M = fmaxf(y.M, __shfl_xor_sync(0xffffffffu, y.M, o));
+    y.m_out = fmaxf(y.m_out, __shfl_xor_sync(0xffffffffu, y.m_out, o));
+  }
+  y.all = relative(x.all, x.m, y.M, a.scale);
+  y.out = relative(x.out, x.m_out, y.m_out, a.scale);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) {
+    y.all += __shfl_xor_sync(0xffffffffu, y.all, o);
+    y.out += __shfl_xor_sync(0xffffffffu, y.out, o);
+  }
+  if (!a.tail) {  // (r = 0: not needed apart)
+    y.m_out = y.M;
+    y.out = y.all;
+  }
+  return y;  // (in the first half of the warp)
+}
+
+// Gradient factors of a row.
 struct Factors {
   float M;
-  float outside;  // (W - r / t) w / (T S): times 2^((z - M) scale), outside the list
-  float listed;   // W / S
+  float m_out;    // 0 where nothing is outside the list
+  float outside;  // times 2^((z - m_out) scale) outside the list: (W q - r q / t) w / T
+  float listed;   // W / all: times 2^((z - M) scale) on it, W q
   float wt;       // w / T
   bool none;      // gradient 0
 };
-__device__ __forceinline__ Factors factors(const DistillArgs& a, const List& L, int64_t r, float M,
-                                           float S, float S_out) {
+__device__ __forceinline__ Factors factors(const DistillArgs& a, const List& L, int64_t r,
+                                           const Row& y) {
   Factors f;
   f.wt = (a.weight ? a.weight[r] : 1.f) / a.temp;
   const float W = L.mass + L.rest;
-  f.M = M;
-  f.listed = W / S;
-  // (no mass outside the list: nothing there has a gradient)
-  f.outside = f.wt * (S_out > 0.f ? W / S - L.rest / S_out : 0.f);
-  f.none = f.wt == 0.f || !(S > 0.f && S < INFINITY) ||
+  f.M = y.M;
+  f.listed = W / y.all;
+  const bool some = y.out > 0.f;
+  f.m_out = some ? y.m_out : 0.f;
+  f.outside = some ? f.wt * (relative(f.listed, y.m_out, y.M, a.scale) - L.rest / y.out) : 0.f;
+  f.none = f.wt == 0.f || !(y.all > 0.f && y.all < INFINITY) ||
            (L.status & (TT_REQ_EMPTY | TT_REQ_NOT_FINITE)) != 0;
   return f;
 }
@@ -229,53 +267,49 @@ __device__ __forceinline__ float listed_grad(const DistillArgs& a, const Factors
   return f.none ? 0.f : f.wt * (f.listed * ex2_approx((z - f.M) * a.scale) - p);
 }
 
+template <int DT>
+__device__ __forceinline__ float smem_logit(const char* seg, int x) {
+  if constexpr (DT == TT_F32)
+    return reinterpret_cast<const float*>(seg)[x];
+  else
+    return bf16_to_f32(reinterpret_cast<const uint16_t*>(seg)[x]);
+}
+template <int DT>
+__device__ __forceinline__ void set_smem_logit(char* seg, int x, float z) {
+  if constexpr (DT == TT_F32)
+    reinterpret_cast<float*>(seg)[x] = z;
+  else
+    reinterpret_cast<uint16_t*>(seg)[x] = uint16_t(__float_as_uint(z) >> 16);
+}
+
 // One warp adds the list's columns (their logits in L.z) to the sums of the
 // CTA's warps (their maxima and sums outside the list).
 __device__ __forceinline__ Share cta_share(const DistillArgs& a, const List& L, const float2* s_ms,
                                            int lane) {
   const int n = L.count;
-  float top = lane < kWarps ? s_ms[lane].x : -INFINITY;
+  Share x{lane < kWarps ? s_ms[lane].x : -INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f};
+  x.m_out = warp_max_f(x.m);
   for (int e = lane; e < n; e += 32)
-    if (L.col[e] >= 0) top = fmaxf(top, L.z[e]);
-  top = warp_max_f(top);
-  Share x;
-  x.base = top > -INFINITY ? top : 0.f;
-  x.out = x.listed = x.mass = x.cross = 0.f;
-  if (lane < kWarps) {
-    const float2 ms = s_ms[lane];
-    x.out = ms.x > -INFINITY ? ms.y * ex2_approx((ms.x - x.base) * a.scale) : ms.y;
-  }
+    if (L.col[e] >= 0) x.m = fmaxf(x.m, L.z[e]);
+  x.m = warp_max_f(x.m);
+  if (lane < kWarps) x.out = relative(s_ms[lane].y, s_ms[lane].x, x.m_out, a.scale);
+  const float ref = x.m > -INFINITY ? x.m : 0.f;
   for (int e = lane; e < n; e += 32) {
     if (L.col[e] < 0) continue;
-    const float d = L.z[e] - x.base, p = L.p[e];
-    x.listed += ex2_approx(d * a.scale);
+    const float d = L.z[e] - ref, p = L.p[e];
+    x.all += ex2_approx(d * a.scale);
     x.mass += p;
     if (p > 0.f) x.cross += p * (logf(p) - d / a.temp);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     x.out += __shfl_xor_sync(0xffffffffu, x.out, o);
-    x.listed += __shfl_xor_sync(0xffffffffu, x.listed, o);
+    x.all += __shfl_xor_sync(0xffffffffu, x.all, o);
     x.mass += __shfl_xor_sync(0xffffffffu, x.mass, o);
     x.cross += __shfl_xor_sync(0xffffffffu, x.cross, o);
   }
+  x.all += relative(x.out, x.m_out, x.m, a.scale);
   return x;
-}
-
-// The row's maximum and sums from its CTAs' shares, the same in every CTA.
-struct Row {
-  float M, all, out;
-};
-__device__ __forceinline__ Row row_sums(const DistillArgs& a, const Share* share, int S) {
-  Row y{share[0].base, 0.f, 0.f};
-  for (int k = 1; k < S; ++k) y.M = fmaxf(y.M, share[k].base);
-  for (int k = 0; k < S; ++k) {
-    const float f = ex2_approx((share[k].base - y.M) * a.scale);
-    y.out += share[k].out * f;
-    y.all += share[k].listed * f;
-  }
-  y.all += y.out;
-  return y;
 }
 
 // One thread writes the row's loss, statistics and status.
@@ -284,11 +318,15 @@ __device__ __forceinline__ void report(const DistillArgs& a, int64_t r, const Li
   const float ln_s = logf(y.all);
   float loss = 0.f, mass = 0.f;
   for (int k = 0; k < S; ++k) {
+    if (!(share[k].mass > 0.f)) continue;
+    const float ref = share[k].m > -INFINITY ? share[k].m : 0.f;
     mass += share[k].mass;
-    loss += share[k].cross + share[k].mass * ((y.M - share[k].base) / a.temp);
+    loss += share[k].cross + share[k].mass * ((y.M - ref) / a.temp);
   }
   loss += mass * ln_s;
-  if (L.rest > 0.f) loss += L.rest * (logf(L.rest) - (logf(y.out) - ln_s));
+  if (L.rest > 0.f)
+    loss += L.rest * (logf(L.rest) -
+                      (y.out > 0.f ? (y.m_out - y.M) / a.temp + logf(y.out) - ln_s : -INFINITY));
   const bool finite = y.all > 0.f && y.all < INFINITY;
   const int st = L.status | (finite ? 0 : TT_REQ_NOT_FINITE) | (ok ? 0 : TT_REQ_TIMEOUT);
   a.status[r] = st;
@@ -296,7 +334,7 @@ __device__ __forceinline__ void report(const DistillArgs& a, int64_t r, const Li
     a.loss[r] = st & (TT_REQ_NOT_FINITE | TT_REQ_TIMEOUT) ? __int_as_float(0x7fffffff)
                 : st & TT_REQ_EMPTY                       ? 0.f
                                                           : loss;
-  if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(y.M, y.all, y.out, 0.f);
+  if (a.stats) reinterpret_cast<float4*>(a.stats)[r] = make_float4(y.M, y.all, y.m_out, y.out);
 }
 
 // A thread's running maximum and sum of 2^((z - m) scale).
@@ -340,21 +378,6 @@ __device__ __forceinline__ uint4 no_logits() {
 }
 
 template <int DT>
-__device__ __forceinline__ float smem_logit(const char* seg, int x) {
-  if constexpr (DT == TT_F32)
-    return reinterpret_cast<const float*>(seg)[x];
-  else
-    return bf16_to_f32(reinterpret_cast<const uint16_t*>(seg)[x]);
-}
-template <int DT>
-__device__ __forceinline__ void set_smem_logit(char* seg, int x, float z) {
-  if constexpr (DT == TT_F32)
-    reinterpret_cast<float*>(seg)[x] = z;
-  else
-    reinterpret_cast<uint16_t*>(seg)[x] = uint16_t(__float_as_uint(z) >> 16);
-}
-
-template <int DT>
 __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant__ DistillArgs a) {
   constexpr int VEC = DT == TT_F32 ? 4 : 8;
   constexpr int ESZ = 16 / VEC;
@@ -363,6 +386,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   __shared__ uint64_t full;
   __shared__ float2 s_ms[kWarps];
   __shared__ Share s_share[kMaxSplit];
+  __shared__ Factors s_factors;
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = a.split, rank = S > 1 ? int(cluster.block_rank()) : 0;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -424,10 +448,15 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
     cluster.sync();
   else
     __syncthreads();
-  const Row y = row_sums(a, s_share, S);
+  Row y;
+  if (warp == 0) {
+    y = row_sums(a, s_share, S, lane);
+    if (lane == 0) s_factors = factors(a, L, r, y);
+  }
+  __syncthreads();
   if (rank == 0 && t == 0) report(a, r, L, s_share, S, y, ok);
   if (!a.grad) return;
-  const Factors f = factors(a, L, r, y.M, y.all, y.out);
+  const Factors f = s_factors;
   char* grow = a.grad + r * a.grad_stride_bytes;
   uint4* out = reinterpret_cast<uint4*>(grow + int64_t(c0) * ESZ);
   if (f.none) {
@@ -435,13 +464,13 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   } else {
 #pragma unroll 4
     for (int v = t; v < whole; v += kThreads)
-      __stcs(out + v, scaled_exp<DT>(sv[v], f.M, a.scale, f.outside));
+      __stcs(out + v, scaled_exp<DT>(sv[v], f.m_out, a.scale, f.outside));
   }
   if (nvec > whole && t == whole % kThreads) {
     for (int x = whole * VEC; x < c1 - c0; ++x)
       store_elem<DT>(grow, c0 + x,
                      f.none ? 0.f
-                            : f.outside * ex2_approx((smem_logit<DT>(seg, x) - f.M) * a.scale));
+                            : f.outside * ex2_approx((smem_logit<DT>(seg, x) - f.m_out) * a.scale));
   }
   // the listed columns of this thread's vectors, after them
   for (int e = 0; e < n; ++e) {
@@ -542,7 +571,10 @@ __global__ void __launch_bounds__(kThreads, 8) distill_loss_kernel(
     cluster.barrier_wait();
   }
   if (S > 1) cluster.sync();
-  if (rank == 0 && t == 0) report(a, r, L, s_share, S, row_sums(a, s_share, S), true);
+  if (rank == 0 && warp == 0) {
+    const Row y = row_sums(a, s_share, S, lane);
+    if (lane == 0) report(a, r, L, s_share, S, y, true);
+  }
 }
 
 // The gradient alone, from the forward call's statistics: a CTA takes kGradVecs
@@ -557,6 +589,7 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(
   constexpr int VEC = DT == TT_F32 ? 4 : 8;
   constexpr int ESZ = 16 / VEC;
   __shared__ List L;
+  __shared__ Factors s_factors;
   const int t = threadIdx.x;
   const int parts = (a.V + kGradVecs * VEC - 1) / (kGradVecs * VEC);
   const int64_t r = blockIdx.x / parts;
@@ -582,22 +615,23 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(
     __syncwarp();
     for (int e = t; e < L.count; e += 32)
       if (L.col[e] >= 0) L.z[e] = load_logit<DT>(row, L.col[e]);
+    if (t == 0) s_factors = factors(a, L, r, Row{st.x, st.y, st.z, st.w});
   }
   __syncthreads();
-  const Factors f = factors(a, L, r, st.x, st.y, st.z);
+  const Factors f = s_factors;
   uint4* out = reinterpret_cast<uint4*>(grow + int64_t(c0) * ESZ);
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u) {
     const int v = u * kThreads + t;
     if (v < whole)
       __stcs(out + v,
-             f.none ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(w[u], f.M, a.scale, f.outside));
+             f.none ? make_uint4(0, 0, 0, 0) : scaled_exp<DT>(w[u], f.m_out, a.scale, f.outside));
   }
   if (ragged)
     for (int q = 0; q < VEC; ++q)
       if (c0 + whole * VEC + q < c1)
         store_elem<DT>(grow, c0 + whole * VEC + q,
-                       f.none ? 0.f : f.outside * ex2_approx((z_tail[q] - f.M) * a.scale));
+                       f.none ? 0.f : f.outside * ex2_approx((z_tail[q] - f.m_out) * a.scale));
   for (int e = 0; e < L.count; ++e) {
     const int x = L.col[e] - c0;
     if (x >= 0 && (x / VEC) % kThreads == t)

@@ -44,7 +44,8 @@ struct DistillArgs {
   const float* logp;    // [rows * K]
   const float* weight;  // [rows] or NULL
   float* loss;
-  float* stats;  // [rows * 4]: max z, sum of 2^((z - max) scale) over all columns and outside the list
+  float* stats;  // [rows * 4]: max z and sum of 2^((z - max) scale), of all columns and of
+                 // those outside the list
   int32_t* status;
   char* grad;  // NULL: the forward call alone
   int64_t grad_stride_bytes;

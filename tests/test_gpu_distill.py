@@ -192,6 +192,47 @@ def test_a_student_that_knows_its_teacher(dtype):
 
 
 @pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("lead", [60.0, 150.0, 1000.0])
+def test_a_student_sure_beyond_fp32(dtype, lead):
+    """The mass outside the list is below what fp32 holds; its logarithm and its
+    shares of the teacher's rest are not."""
+    gen = torch.Generator().manual_seed(16)
+    V = 5000
+    z = torch.randn((3, V), generator=gen)
+    ids, logp = teacher(3, V, 8, gen, unused=0.0, mass=0.9)
+    z.scatter_(1, ids.long(), z.gather(1, ids.long()) + lead)
+    rows = rows_of(z, dtype)
+    loss, grad, bound = expected(rows, ids, logp, 1.0, True, None)
+    out = torch.ones((3, V), dtype=torch.bool).scatter_(1, ids.long(), False)
+    # (t in 64 bits is 0 from a lead of 745 on: the shares of r outside the list, directly)
+    zo = rows.cpu().double().masked_fill(~out, -math.inf)
+    rest = 1 - torch.exp(logp.double()).sum(1, keepdim=True)
+    q = torch.softmax(rows.cpu().double(), 1)
+    want = torch.where(out, q - rest * torch.softmax(zo, 1), grad)
+    bound = torch.where(out, 1e-5 * (q + want.abs()), bound)
+    for g in (True, False):
+        o = tt.tt_distill(rows, ids.cuda(), logp.cuda(), tail=True, grad=g)
+        torch.testing.assert_close(o["loss"].cpu().double(), loss, rtol=1e-5, atol=2e-5)
+        back = tt.tt_distill_grad(rows, ids.cuda(), logp.cuda(), o["stats"], tail=True)
+        check_grad(back, want, bound, dtype)
+    check_grad(tt.tt_distill(rows, ids.cuda(), logp.cuda(), tail=True)["grad"], want, bound, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("level", [-500.0, 500.0])
+def test_columns_masked_in_a_run(dtype, level):
+    """Every column but the first few hundred masked, at a level far from 0: what
+    shares of a row hold nothing say nothing about its maximum."""
+    gen = torch.Generator().manual_seed(17)
+    V = 90000
+    z = torch.full((2, V), -math.inf)
+    z[:, :700] = torch.randn((2, 700), generator=gen) + level
+    ids, logp = teacher(2, 700, 6, gen, unused=0.0)
+    for tail in (False, True):
+        check(z, ids, logp, dtype, 1.0, tail)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
 @pytest.mark.parametrize("low", [-math.inf, "lowest"])
 @pytest.mark.parametrize("tail", [False, True])
 def test_masked_students(dtype, low, tail):
