@@ -62,7 +62,12 @@ constexpr float kLn2 = 0.693147180559945f;
 // A row's reference maximum follows its maximum once that is 2^kSlack above it:
 // weights stay below 2^(kSlack + offset), and the output is scaled rarely.
 constexpr float kSlack = 8.f;
-constexpr int kMinShare = 2;  // tiles of a CTA, where there are few
+constexpr int kMinShare = 2;  // places of a CTA, where there are few
+// What an item costs beyond its tiles (queries, ancestors, output), in tiles: it
+// takes as many places in the list before its first tile. Without them the CTAs that
+// hold requests with short caches took twice the mean time: 64-token trees over
+// ragged caches 65 us, 48 with 3 (49 with 2 or 5); a serving batch 186 and 175.
+constexpr int kItemCost = 3;
 
 struct TreeKernelArgs {
   CUtensorMap q, k, v, kc, vc;
@@ -78,7 +83,7 @@ struct TreeKernelArgs {
   // of one that begins in them at 2 c + 1
   float* part;        // [2 ctas * rows * D] outputs, not normalised
   float2* part_ml;    // [2 ctas * rows] their reference maximum (log2) and sum
-  int32_t* first;     // [B + 1] tiles before each request's, then the tiles per CTA
+  int32_t* first;     // [B + 1] places before each request's, then the places per CTA
 };
 
 // A request's usable range: its nodes and cache length, or why it has none.
@@ -107,27 +112,30 @@ __host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / 
 __device__ __forceinline__ int item_tiles(const TreeKernelArgs& p, const Request& r, int mt) {
   return cache_tiles(r.len) + tree_tiles(min(r.nodes, (mt + 1) * p.per_tile));
 }
-// The tiles of one key head of a request.
-__device__ __forceinline__ int head_tiles(const TreeKernelArgs& p, const Request& r) {
+// The place that one key head of a request takes in the list.
+__device__ __forceinline__ int head_places(const TreeKernelArgs& p, const Request& r) {
   int n = 0;
-  for (int mt = 0; mt * p.per_tile < r.nodes; ++mt) n += item_tiles(p, r, mt);
+  for (int mt = 0; mt * p.per_tile < r.nodes; ++mt) n += kItemCost + item_tiles(p, r, mt);
   return n;
 }
-// A place in the list of tiles.
+// An item of the list, the first of its tiles that is left, and the places before it.
 struct Place {
-  int b, hk, mt, tile;
+  int b, hk, mt, tile, lead;
   Request r;
   __device__ __forceinline__ void find(const TreeKernelArgs& p, int request_b, int offset) {
     b = request_b;
     r = request(p.a, b);
-    const int per_head = head_tiles(p, r);
+    const int per_head = head_places(p, r);
     hk = offset / per_head;
-    tile = offset % per_head;
+    offset %= per_head;
     mt = 0;
-    for (int n; tile >= (n = item_tiles(p, r, mt)); ++mt) tile -= n;
+    for (int n; offset >= (n = kItemCost + item_tiles(p, r, mt)); ++mt) offset -= n;
+    tile = max(0, offset - kItemCost);
+    lead = max(0, kItemCost - offset);
   }
   __device__ __forceinline__ void next_item(const TreeKernelArgs& p) {
     tile = 0;
+    lead = kItemCost;
     if (++mt * p.per_tile < r.nodes) return;
     mt = 0;
     if (++hk < p.a.Hkv) return;
@@ -178,8 +186,8 @@ struct Smem {
   uint32_t odd[kWords];          // drafted tokens with a value that is not finite
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t q_empty, s_full, s_free, p_full, o_done;
-  long long sums[kThreads / 32];  // tiles of the requests, by warps
-  int start_b, start_offset;      // where this CTA's tiles begin
+  long long sums[kThreads / 32];  // places of the requests, by warps
+  int start_b, start_offset;      // where this CTA's places begin
   Place place[kRowWarps];         // where the row warps are (their registers are dear)
   uint32_t tmem;
   int failed;
@@ -264,7 +272,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const int each = (a.B + kThreads - 1) / kThreads, b0 = min(a.B, t * each),
               b1 = min(a.B, b0 + each);
     long long mine = 0;
-    for (int b = b0; b < b1; ++b) mine += (long long)(head_tiles(p, request(a, b))) * a.Hkv;
+    for (int b = b0; b < b1; ++b) mine += (long long)(head_places(p, request(a, b))) * a.Hkv;
     long long upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -286,7 +294,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     long long at = upto - mine;
     if (todo > 0 && from >= at && from < upto) {
       for (int b = b0; b < b1; ++b) {
-        const long long n = (long long)(head_tiles(p, request(a, b))) * a.Hkv;
+        const long long n = (long long)(head_places(p, request(a, b))) * a.Hkv;
         if (from < at + n) {
           s.start_b = b;
           s.start_offset = int(from - at);
@@ -299,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 2)
       at = upto - mine;
       for (int b = b0; b < b1; ++b) {
         p.first[b] = int(at);
-        at += (long long)(head_tiles(p, request(a, b))) * a.Hkv;
+        at += (long long)(head_places(p, request(a, b))) * a.Hkv;
       }
       if (t == 0) p.first[a.B] = int(share);
     }
@@ -311,11 +319,13 @@ __global__ void __launch_bounds__(kThreads, 2)
   if (warp == kRowWarps) {
     // ------------------------------------------------------------ copies
     Place x;
+    x.lead = 0;
     if (todo > 0) x.find(p, s.start_b, s.start_offset);
     // lane i copies a tile's i-th box of slots
     const int per = kTile / p.box;
     int it = 0;
-    for (int seg = 0; todo > 0 && ok; ++seg) {
+    for (int seg = 0; todo > x.lead && ok; ++seg) {
+      todo -= x.lead;
       const int n_cache = cache_tiles(x.r.len);
       const int node0 = x.mt * p.per_tile, node1 = min(x.r.nodes, node0 + p.per_tile);
       const int tile1 = min(n_cache + tree_tiles(node1), x.tile + todo);
@@ -394,10 +404,12 @@ __global__ void __launch_bounds__(kThreads, 2)
     // ---------------------------------------------------------- products
     if (lane == 0) {
       Place x;
+      x.lead = 0;
       if (todo > 0) x.find(p, s.start_b, s.start_offset);
       const uint32_t idesc_o = umma_idesc(F16, D, true);
       int it = 0;
-      for (int seg = 0; todo > 0 && ok; ++seg) {
+      for (int seg = 0; todo > x.lead && ok; ++seg) {
+        todo -= x.lead;
         const int n_cache = cache_tiles(x.r.len);
         const int node1 = min(x.r.nodes, (x.mt + 1) * p.per_tile);
         const int tile1 = min(n_cache + tree_tiles(node1), x.tile + todo);
@@ -472,10 +484,14 @@ __global__ void __launch_bounds__(kThreads, 2)
       return s.half[turn][half ^ 1][row];
     };
     Place& x = s.place[warp];
-    if (todo > 0 && lane == 0) x.find(p, s.start_b, s.start_offset);
+    if (lane == 0) {
+      x.lead = 0;
+      if (todo > 0) x.find(p, s.start_b, s.start_offset);
+    }
     __syncwarp();
     int it = 0;
-    while (todo > 0) {
+    while (todo > x.lead) {
+      todo -= x.lead;
       const int n_cache = cache_tiles(x.r.len);
       const int node1 = min(x.r.nodes, (x.mt + 1) * p.per_tile);
       const int tile1 = min(n_cache + tree_tiles(node1), x.tile + todo);
@@ -736,8 +752,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   if (i >= r.nodes) return;
   const int hk = FEW ? head : head / p.group;
   const int mt = i / p.per_tile;
-  int before = hk * head_tiles(p, r);
-  for (int k = 0; k < mt; ++k) before += item_tiles(p, r, k);
+  int before = hk * head_places(p, r) + kItemCost;  // its first tile's place
+  for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles(p, r, k);
   const int last = before + item_tiles(p, r, mt) - 1;
   grid_dependency_wait();
   // the CTAs that the item lies in
@@ -821,7 +837,7 @@ Cut cut(const TreeArgs& a, int sm_count) {
   c.per_tile = kTile / c.group;
   const int64_t row_tiles = (a.max_nodes + c.per_tile - 1) / c.per_tile;
   const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
-  const int64_t all = int64_t(a.B) * a.Hkv * row_tiles * tiles;
+  const int64_t all = int64_t(a.B) * a.Hkv * row_tiles * (kItemCost + tiles);
   c.ctas = int(std::max<int64_t>(1, std::min<int64_t>(2 * int64_t(sm_count),
                                                       (all + kMinShare - 1) / kMinShare)));
   // (were all lengths the longest; fewer tiles make shares smaller and pieces more)
