@@ -77,7 +77,7 @@ __device__ __noinline__ void select_best(const char* row, int c0, int c1, int n,
     s_want = n;
   }
   for (int shift = 24; shift >= 0; shift -= 8) {
-    hist[t] = 0;
+    for (int i = t; i < 256; i += kThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t prefix = s_prefix;
     each_logit<DT>(row, c0, c1, [&](float z, int) {
@@ -140,20 +140,24 @@ __device__ __noinline__ void select_best(const char* row, int c0, int c1, int n,
   __syncthreads();
 }
 
-// The sums of some columns: their maximum z, sum of 2^d and of 2^d d with
-// d = (z - max) log2(e) / T, and how many come before the given column.
+// The sums of some columns: their maximum z, sum of 2^d over all but one column
+// of that maximum and of 2^d d over all, with d = (z - max) log2(e) / T, and how
+// many come before the given column. (The maximum's own 1 is kept apart: next to
+// it, the rest of a row that one column dominates would be rounded away, and that
+// is all of the column's log probability.)
 struct Sums {
   float m, s, e;
   int before;
 };
 __device__ __forceinline__ void join(Sums& a, const Sums& b, float scale) {
-  const float m = fmaxf(a.m, b.m);
+  const bool swap = b.m > a.m;
+  const float m = swap ? b.m : a.m, low = swap ? a.m : b.m;
+  const float ls = swap ? a.s : b.s, le = swap ? a.e : b.e;
   // (d of -inf, or of the type's whole range: the factor is 0)
-  const float da = a.m == m ? 0.f : fmaxf((a.m - m) * scale, -256.f);
-  const float db = b.m == m ? 0.f : fmaxf((b.m - m) * scale, -256.f);
-  const float fa = ex2_approx(da), fb = ex2_approx(db);
-  a.e = fa * fmaf(a.s, da, a.e) + fb * fmaf(b.s, db, b.e);
-  a.s = fa * a.s + fb * b.s;
+  const float d = low == m ? 0.f : fmaxf((low - m) * scale, -256.f), f = ex2_approx(d);
+  const float sum = (low > -INFINITY ? 1.f : 0.f) + ls;
+  a.s = fmaf(f, sum, swap ? b.s : a.s);
+  a.e = fmaf(f, fmaf(sum, d, le), swap ? b.e : a.e);
   a.m = m;
   a.before += b.before;
 }
@@ -233,6 +237,8 @@ struct Shared {
   float post[kWarps];
   unsigned int count;  // vectors that reached the bar
   unsigned int kept;   // columns that reach the last one
+  int holder;          // the thread of the maximum
+  float rest[kWarps];
   unsigned long long best[TT_MAX_TOP_K];
   int vecs[kVectors];
   unsigned long long found[kCandidates];
@@ -385,19 +391,6 @@ __global__ void __launch_bounds__(kThreads, 4)
     }
   }
 
-  // the CTA's sums
-  x.s = sum_pair(s2);
-  x.e = sum_pair(number(e2));
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    Sums y;
-    y.m = __shfl_xor_sync(0xffffffffu, x.m, o);
-    y.s = __shfl_xor_sync(0xffffffffu, x.s, o);
-    y.e = __shfl_xor_sync(0xffffffffu, x.e, o);
-    y.before = __shfl_xor_sync(0xffffffffu, x.before, o);
-    join(x, y, a.scale);
-  }
-  if (lane == 0) s.sums[warp] = x;
   // (the columns around the given one within its vector)
   int close = 0;
   if (warp == 0 && given && v_id >= 0 && v_id < nvec && lane < VEC) {
@@ -408,12 +401,52 @@ __global__ void __launch_bounds__(kThreads, 4)
     }
   }
   close = __popc(__ballot_sync(0xffffffffu, close));
-  __syncthreads();
-  if (t == 0) {
-    Sums y = s.sums[0];
-    y.before += close;
-    for (int j = 1; j < kWarps; ++j) join(y, s.sums[j], a.scale);
-    s.mine = y;
+  // the CTA's sums
+  x.s = sum_pair(s2) - (x.m > -INFINITY ? 1.f : 0.f);
+  x.e = sum_pair(number(e2));
+  for (int turn = 0; turn < 2; ++turn) {
+    Sums y = x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      Sums other;
+      other.m = __shfl_xor_sync(0xffffffffu, y.m, o);
+      other.s = __shfl_xor_sync(0xffffffffu, y.s, o);
+      other.e = __shfl_xor_sync(0xffffffffu, y.e, o);
+      other.before = __shfl_xor_sync(0xffffffffu, y.before, o);
+      join(y, other, a.scale);
+    }
+    if (lane == 0) s.sums[warp] = y;
+    __syncthreads();
+    if (t == 0) {
+      y = s.sums[0];
+      y.before += close;
+      for (int j = 1; j < kWarps; ++j) join(y, s.sums[j], a.scale);
+      s.mine = y;
+    }
+    __syncthreads();
+    const float m = s.mine.m;
+    if (turn == 1 || !(m > -INFINITY && s.mine.s < 0.5f)) break;
+    // One column dominates, and its thread has summed beside its 1: the thread's
+    // columns once more, by all threads, without it.
+    if (x.m == m) s.holder = t;
+    __syncthreads();
+    float rest = 0.f;
+    for (int v = s.holder + t * kThreads; v < nvec; v += kThreads * kThreads) {
+#pragma unroll
+      for (int q = 0; q < VEC; ++q) {
+        const int col = c0 + v * VEC + q;
+        const float z = col < c1 ? load_logit<DT>(row, col) : -INFINITY;
+        if (z != m) rest += ex2_approx((z - m) * a.scale);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) rest += __shfl_xor_sync(0xffffffffu, rest, o);
+    if (lane == 0) s.rest[warp] = rest;
+    __syncthreads();
+    if (x.m == m) {
+      x.s = s.rest[0];
+      for (int j = 1; j < kWarps; ++j) x.s += s.rest[j];
+    }
   }
   // and its best columns: the last bar leaves little more than them
   if (n > 0) {
@@ -460,13 +493,13 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
   __syncthreads();
   const Sums y = s.mine;
-  const bool ok = y.s > 0.f && y.s < INFINITY;  // neither empty nor NaN or +inf
-  const float nan = __int_as_float(0x7fffffff), ln_s = logf(y.s);
+  const bool ok = y.m > -INFINITY && y.s < INFINITY;  // neither empty nor NaN or +inf
+  const float nan = __int_as_float(0x7fffffff), ln_s = log1pf(y.s);
   if (t == 0) {
     a.out.status[r] = (ok ? 0 : TT_REQ_NOT_FINITE) |
                       (given || id == -1 ? 0 : TT_REQ_ID_OUT_OF_RANGE);
     if (a.out.lse) a.out.lse[r] = ok ? y.m / a.temp + ln_s : nan;
-    if (a.out.entropy) a.out.entropy[r] = ok ? ln_s - kLn2 * (y.e / y.s) : nan;
+    if (a.out.entropy) a.out.entropy[r] = ok ? ln_s - kLn2 * (y.e / (1.f + y.s)) : nan;
     if (a.out.logprob)
       a.out.logprob[r] =
           !ok || (!given && id != -1) ? nan : given ? (zt - y.m) / a.temp - ln_s : 0.f;

@@ -160,6 +160,33 @@ def test_masks(V, dtype, low):
 
 
 @pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("V", [3000, 70001])
+@pytest.mark.parametrize("lead", [8.0, 14.0, 20.0, 40.0])
+def test_rows_that_one_column_dominates(dtype, V, lead):
+    """The log probability of a column that holds nearly all of the mass is the
+    rest's, relative to its size: the terms' 2^-22 and |d| 2^-23, and the sums'
+    (1e-6); its entropy alike."""
+    gen = torch.Generator().manual_seed(V)
+    z = torch.randn((6, V), generator=gen)
+    at = torch.randint(V, (6,), generator=gen)
+    at[0], at[1] = 0, V - 1
+    z[torch.arange(6), at] = lead + math.log(V)
+    z[5, 10:20] = z[5, at[5]]  # (and one with equals)
+    rows, ids = rows_of(z, dtype), at.int().cuda()
+    g, o = tt.tt_logprobs(rows, ids, top_n=2), expected(rows, ids, 1.0, 2)
+    zd = rows.cpu().double()
+    for r in range(5):
+        rest = torch.exp(zd[r] - zd[r, at[r]])
+        rest[at[r]] = 0.0
+        want = -torch.log1p(rest.sum())
+        assert abs(g["logprob"][r].item() - want) <= 1e-5 * abs(want), r
+        assert g["top_logprobs"][r, 0].item() == g["logprob"][r].item()
+        h = -want + (rest * (zd[r, at[r]] - zd[r])).sum() / (1 + rest.sum())
+        assert abs(g["entropy"][r].item() - h) <= 1e-5 * h, r
+    torch.testing.assert_close(g["logprob"].cpu().double(), o["logprob"], rtol=REL, atol=ABS)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
 @pytest.mark.parametrize("temp", [1e-30, 1e-4, 0.01, 100.0, 1e30])
 @pytest.mark.parametrize("size", [1e-3, 1.0, 1e4, 1e30])
 def test_temperatures_and_sizes(dtype, temp, size):
