@@ -32,12 +32,16 @@ namespace tt {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kBatch = 8;           // vectors of a thread between two looks at the bar
 constexpr int kVectors = 2048;      // room for vectors that reach the bar
 constexpr int kCandidates = 1024;   // and for columns that reach the last one
 constexpr int kMaxSplit = 16;
+// CTAs have 256 threads while those of all rows fit the SMs at once, 4 to an SM, and
+// 128, 8 to an SM, for more rows: the end of a row, which has no loads of its own,
+// holds up fewer threads, and the last rows leave less idle. Narrow / wide, us: 4096
+// rows of 201,088 bf16 columns 327 / 342, 1000 of 32,000 fp32 28.9 / 31.3, 3000 of 4096
+// bf16 19.9 / 34.1; but 608 of 151,936 fp32 87 / 67, 310 of 128,256 bf16 47 / 33.
+constexpr int kWidePerSm = 4;
 constexpr float kLeast = -3.402823466e38f;  // -inf never reaches a bar
 constexpr float kLn2 = 0.693147180559945f;
 
@@ -53,7 +57,7 @@ __device__ __forceinline__ float key_value(uint32_t k) {
 }
 
 // The columns c0 .. c1 - 1 in steps of one per thread.
-template <int DT, typename F>
+template <int DT, int kThreads, typename F>
 __device__ __forceinline__ void each_logit(const char* row, int c0, int c1, F&& f) {
   for (int x = c0 + threadIdx.x; x < c1; x += kThreads) f(load_logit<DT>(row, x), x);
 }
@@ -62,9 +66,10 @@ __device__ __forceinline__ void each_logit(const char* row, int c0, int c1, F&& 
 // order of the logit above the complement of the column; 0 where there are
 // fewer): a radix search for the n-th largest logit, the columns above it, and
 // the first of those equal to it.
-template <int DT>
+template <int DT, int kThreads>
 __device__ __noinline__ void select_best(const char* row, int c0, int c1, int n,
                                          unsigned long long* best) {
+  constexpr int kWarps = kThreads / 32;
   __shared__ unsigned int hist[256];
   __shared__ unsigned int s_prefix, s_want, s_count;
   __shared__ unsigned int s_warp[kWarps];
@@ -80,7 +85,7 @@ __device__ __noinline__ void select_best(const char* row, int c0, int c1, int n,
     for (int i = t; i < 256; i += kThreads) hist[i] = 0;
     __syncthreads();
     const uint32_t prefix = s_prefix;
-    each_logit<DT>(row, c0, c1, [&](float z, int) {
+    each_logit<DT, kThreads>(row, c0, c1, [&](float z, int) {
       const uint32_t k = order_key(z);
       if (k > empty && (shift == 24 || (k >> (shift + 8)) == prefix >> (shift + 8)))
         atomicAdd(&hist[(k >> shift) & 255], 1u);
@@ -100,7 +105,7 @@ __device__ __noinline__ void select_best(const char* row, int c0, int c1, int n,
   const unsigned int equal = s_want;  // how many of its equals are taken, in column order
   if (t == 0) s_count = 0;
   __syncthreads();
-  each_logit<DT>(row, c0, c1, [&](float z, int x) {
+  each_logit<DT, kThreads>(row, c0, c1, [&](float z, int x) {
     const uint32_t k = order_key(z);
     if (k > tau && k > empty) {
       const unsigned int p = atomicAdd(&s_count, 1u);
@@ -231,6 +236,7 @@ __device__ __forceinline__ float logit_above(float z) {
   return __int_as_float(z == 0.f ? step : u > 0 ? u + step : u - step);
 }
 
+template <int kWarps>
 struct Shared {
   Sums sums[kWarps];
   Sums mine;  // the CTA's share
@@ -246,6 +252,7 @@ struct Shared {
 
 // The n best of `count` keys (n <= TT_MAX_TOP_K; 0 where there are fewer), by
 // counting those above each one: keys are distinct.
+template <int kThreads>
 __device__ __forceinline__ void rank_keys(const unsigned long long* key, int count, int n,
                                           unsigned long long* best) {
   if (threadIdx.x < n) best[threadIdx.x] = 0;
@@ -259,12 +266,13 @@ __device__ __forceinline__ void rank_keys(const unsigned long long* key, int cou
   __syncthreads();
 }
 
-template <int DT>
-__global__ void __launch_bounds__(kThreads, 4)
+template <int DT, int kThreads>
+__global__ void __launch_bounds__(kThreads, 256 * kWidePerSm / kThreads)
     logprob_kernel(const __grid_constant__ LogprobArgs a) {
   constexpr int VEC = DT == TT_F32 ? 4 : 8;
   constexpr int ESZ = 16 / VEC;
-  __shared__ Shared s;
+  constexpr int kWarps = kThreads / 32;
+  __shared__ Shared<kWarps> s;
   const cg::cluster_group cluster = cg::this_cluster();
   const int S = a.split, rank = S > 1 ? int(cluster.block_rank()) : 0;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
@@ -467,9 +475,9 @@ __global__ void __launch_bounds__(kThreads, 4)
     __syncthreads();
     const int kept = int(s.kept);
     if (count > kVectors || kept > kCandidates)
-      select_best<DT>(row, c0, c1, n, s.best);
+      select_best<DT, kThreads>(row, c0, c1, n, s.best);
     else
-      rank_keys(s.found, kept, n, s.best);
+      rank_keys<kThreads>(s.found, kept, n, s.best);
   }
   // the row's, by its first CTA
   if (S > 1) {
@@ -488,7 +496,7 @@ __global__ void __launch_bounds__(kThreads, 4)
       s.kept = 0;
     }
     cluster.sync();
-    if (n > 0) rank_keys(s.found, S * n, n, s.best);
+    if (n > 0) rank_keys<kThreads>(s.found, S * n, n, s.best);
     if (t == 0) s.mine = s.sums[0];
   }
   __syncthreads();
@@ -515,7 +523,7 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 }
 
-template <int DT>
+template <int DT, int kThreads>
 cudaError_t launch(LogprobArgs a, cudaStream_t stream, int sm_count) {
   constexpr int VEC = DT == TT_F32 ? 4 : 8;
   // CTAs of a row: enough to fill the SMs, each with a batch of vectors at least
@@ -536,19 +544,29 @@ cudaError_t launch(LogprobArgs a, cudaStream_t stream, int sm_count) {
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cfg.attrs = attr;
   cfg.numAttrs = S > 1 ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, logprob_kernel<DT>, a);
+  return cudaLaunchKernelEx(&cfg, logprob_kernel<DT, kThreads>, a);
 }
 
 template <int DT>
+cudaError_t choose(const LogprobArgs& a, cudaStream_t stream, int sm_count) {
+  return a.rows > kWidePerSm * sm_count ? launch<DT, 128>(a, stream, sm_count)
+                                          : launch<DT, 256>(a, stream, sm_count);
+}
+
+// (narrow CTAs are never in clusters)
+template <int DT>
 cudaError_t preload() {
-  return cudaFuncSetAttribute(logprob_kernel<DT>, cudaFuncAttributeNonPortableClusterSizeAllowed,
-                              1);
+  cudaFuncAttributes attr;
+  const cudaError_t e = cudaFuncGetAttributes(&attr, logprob_kernel<DT, 128>);
+  return e != cudaSuccess ? e
+                          : cudaFuncSetAttribute(logprob_kernel<DT, 256>,
+                                                 cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
 }
 
 }  // namespace
 
 cudaError_t launch_logprobs(const LogprobArgs& a, int dt, cudaStream_t stream, int sm_count) {
-  return dt == TT_F32 ? launch<TT_F32>(a, stream, sm_count) : launch<TT_BF16>(a, stream, sm_count);
+  return dt == TT_F32 ? choose<TT_F32>(a, stream, sm_count) : choose<TT_BF16>(a, stream, sm_count);
 }
 
 cudaError_t preload_logprobs() {

@@ -159,6 +159,26 @@ def test_masks(V, dtype, low):
     torch.testing.assert_close(g["lse"].cpu().double()[:5], o["lse"][:5], rtol=REL, atol=ABS)
 
 
+@pytest.mark.parametrize("V", [1, 9, 1025, 8200, 20011])
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("n", [1, 32])
+def test_rows_beyond_the_machine(V, dtype, n):
+    """More rows than are computed at once, every kind among them: ordinary ones,
+    masked ones, empty ones, ties beyond every list, single columns, NaN."""
+    gen = torch.Generator().manual_seed(V + n)
+    R = 1300
+    z = torch.randn((R, V), generator=gen) * 3
+    kind = torch.arange(R) % 7
+    z[kind == 1] = torch.where(torch.rand((R, V), generator=gen) < 0.9, -math.inf, z)[kind == 1]
+    z[kind == 2] = -math.inf
+    z[kind == 3] = 0.5
+    z[kind == 4] = (torch.arange(V) // 64).float()
+    z[kind == 5] = -math.inf
+    z[kind == 5, V // 2] = -2.0
+    z[5::70, V // 3] = math.nan  # (beside a single column)
+    check(rows_of(z, dtype), random_ids(R, V, gen), n=n)
+
+
 @pytest.mark.parametrize("dtype", [F, H])
 @pytest.mark.parametrize("V", [3000, 70001])
 @pytest.mark.parametrize("lead", [8.0, 14.0, 20.0, 40.0])
