@@ -153,7 +153,7 @@ tt_status tt_distill(const tt_logits* student, const tt_teacher* teacher, float 
   a.stats = stats;
   a.status = status;
   cudaError_t e = load_kernels();
-  if (e == cudaSuccess) 
+  if (e == cudaSuccess)
     e = launch_distill(a, student->dtype, static_cast<cudaStream_t>(stream), device_sms());
   return e == cudaSuccess ? TT_OK : record_cuda_error(e);
 }
