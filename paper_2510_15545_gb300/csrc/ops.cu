@@ -198,7 +198,7 @@ tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_by
   if (need > 0 && (!workspace || workspace_bytes < need ||
                    (reinterpret_cast<uintptr_t>(workspace) & 255) != 0))
     return TT_ERR_INVALID_ARG;
-  if (tree->B > 65535) return TT_ERR_UNSUPPORTED;
+  if (!tree_fits(a, device_sms())) return TT_ERR_UNSUPPORTED;
   a.ws = static_cast<char*>(workspace);
   a.out = static_cast<char*>(out);
   a.lse = lse;

@@ -828,6 +828,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
 // How a call is cut: tokens per tile of rows, CTAs, and the workspace.
 struct Cut {
   int group, per_tile, ctas, rows;
+  int64_t places;  // in the list, were all lengths the longest
   int64_t pieces;  // of one item, about
   size_t part_bytes, ml_bytes, bytes;
 };
@@ -837,7 +838,8 @@ Cut cut(const TreeArgs& a, int sm_count) {
   c.per_tile = kTile / c.group;
   const int64_t row_tiles = (a.max_nodes + c.per_tile - 1) / c.per_tile;
   const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
-  const int64_t all = int64_t(a.B) * a.Hkv * row_tiles * (kItemCost + tiles);
+  const int64_t all = c.places = int64_t(std::min(
+      1e18, double(a.B) * double(a.Hkv) * double(row_tiles) * double(kItemCost + tiles)));
   c.ctas = int(std::max<int64_t>(1, std::min<int64_t>(2 * int64_t(sm_count),
                                                       (all + kMinShare - 1) / kMinShare)));
   // (were all lengths the longest; fewer tiles make shares smaller and pieces more)
@@ -923,9 +925,14 @@ cudaError_t preload() {
 
 size_t tree_workspace_bytes(const TreeArgs& a, int sm_count) { return cut(a, sm_count).bytes; }
 
+// (places of the list, and blocks of the join, are 32-bit numbers)
+bool tree_fits(const TreeArgs& a, int sm_count) {
+  return cut(a, sm_count).places <= INT32_MAX &&
+         double(a.B) * a.max_nodes * double(a.Hq) <= INT32_MAX;
+}
+
 cudaError_t launch_tree(const TreeArgs& a, int dt, cudaStream_t stream, int sm_count) {
   const Cut c = cut(a, sm_count);
-  if (int64_t(a.B) * a.max_nodes * a.Hq > INT32_MAX) return cudaErrorInvalidConfiguration;
   TreeKernelArgs p;
   std::memset(&p, 0, sizeof p);
   p.a = a;

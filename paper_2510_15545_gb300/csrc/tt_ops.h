@@ -79,6 +79,7 @@ struct TreeArgs {
 };
 
 size_t tree_workspace_bytes(const TreeArgs& args, int sm_count);
+bool tree_fits(const TreeArgs& args, int sm_count);
 cudaError_t launch_tree(const TreeArgs& args, int dt, cudaStream_t stream, int sm_count);
 cudaError_t preload_tree();
 

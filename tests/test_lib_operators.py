@@ -167,7 +167,15 @@ def test_tree_refuses_outputs_and_workspace(lib):
 
 def test_tree_of_no_requests(lib):
     assert attend(lib, tree(B=0), status=None) == 0
-    assert attend(lib, tree(B=65536, n_nodes=0)) == UNSUPPORTED
+
+
+def test_tree_refuses_what_its_numbers_do_not_hold(lib):
+    """The list's places (one per tile of every request, key head and row tile, at
+    the longest) and the rows of the join are counted in 32 bits."""
+    big = tree(B=65535, max_nodes=512, max_len=1 << 20, table_stride=65536, n_pages=65536)
+    assert attend(lib, big) == UNSUPPORTED
+    assert attend(lib, tree(B=1 << 20, max_nodes=512)) == UNSUPPORTED
+    assert attend(lib, tree(B=2**31 - 1)) == UNSUPPORTED
 
 
 def test_status_bits_and_types():
