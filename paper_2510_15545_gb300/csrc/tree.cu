@@ -120,7 +120,7 @@ __device__ __forceinline__ int head_places(const TreeKernelArgs& p, const Reques
 }
 // An item of the list, the first of its tiles that is left, and the places before it.
 struct Place {
-  int b, hk, mt, tile, lead;
+  int b, hk, mt, tile, lead, start;
   Request r;
   __device__ __forceinline__ void find(const TreeKernelArgs& p, int request_b, int offset) {
     b = request_b;
@@ -132,6 +132,15 @@ struct Place {
     for (int n; offset >= (n = kItemCost + item_tiles(p, r, mt)); ++mt) offset -= n;
     tile = max(0, offset - kItemCost);
     lead = max(0, kItemCost - offset);
+  }
+  // How far into its n tiles of the item a CTA begins, to go round: row tiles of one
+  // head read the same keys, CTAs of the same share take them on, and all are to be
+  // at the same ones at a time, as those of the first row tile come to them in order.
+  __device__ __forceinline__ int turn(const TreeKernelArgs& p, int share, int n) const {
+    int shift = 0;
+    for (int k = 0; k < mt; ++k) shift += kItemCost + item_tiles(p, r, k);
+    shift %= share;
+    return shift < n ? shift : 0;
   }
   __device__ __forceinline__ void next_item(const TreeKernelArgs& p) {
     tile = 0;
@@ -188,6 +197,7 @@ struct Smem {
   uint64_t q_empty, s_full, s_free, p_full, o_done;
   long long sums[kThreads / 32];  // places of the requests, by warps
   int start_b, start_offset;      // where this CTA's places begin
+  int share;                      // and how many a CTA has
   Place place[kRowWarps];         // where the row warps are (their registers are dear)
   uint32_t tmem;
   int failed;
@@ -291,6 +301,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     const long long share = max((long long)(kMinShare), (all + p.ctas - 1) / p.ctas);
     const long long from = share * blockIdx.x;
     todo = int(max(0ll, min(share, all - from)));
+    if (t == 0) s.share = int(share);
     long long at = upto - mine;
     if (todo > 0 && from >= at && from < upto) {
       for (int b = b0; b < b1; ++b) {
@@ -335,7 +346,8 @@ __global__ void __launch_bounds__(kThreads, 2)
                    ? a.page_table[x.b * a.table_stride + slot / a.page_size]
                    : -1;
       };
-      int page = page_of(x.tile);
+      int j = x.tile + x.turn(p, s.share, tile1 - x.tile);
+      int page = page_of(j);
       // the queries, once the item before has been done with its own
       ok = __all_sync(0xffffffffu, mbar_wait(&s.q_empty, (seg & 1) ^ 1, limit));
       if (!ok) break;
@@ -346,10 +358,10 @@ __global__ void __launch_bounds__(kThreads, 2)
                       x.hk * p.group, x.r.first + node0);
       }
       __syncwarp();
-      for (int j = x.tile; j < tile1; ++j, ++it) {
+      for (int i = x.tile; i < tile1; ++i, ++it) {
         const int st = it % S::kStages;
         const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
-        const int next = page_of(j + 1);
+        const int next_j = j + 1 < tile1 ? j + 1 : x.tile, next = page_of(next_j);
         const bool cache = j < n_cache;
         bool mine;
         int bytes, at;
@@ -396,6 +408,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         if (!ok) break;
         copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
         page = next;
+        j = next_j;
       }
       todo -= tile1 - x.tile;
       x.next_item(p);
@@ -418,7 +431,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           const int left = j < n_cache ? x.r.len - j * kTile : node1 - (j - n_cache) * kTile;
           return min(kTile, (left + 31) & ~31);
         };
-        auto scores = [&](int j, int i) {
+        auto scores = [&](int j, int i, bool last) {
           const int st = i % S::kStages;
           if (!mbar_wait(&s.k_full[st], (i / S::kStages) & 1, limit)) return false;
           tc_fence_after();
@@ -431,17 +444,19 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
           umma_commit(&s.s_full);
           umma_commit(&s.k_empty[st]);
-          if (j + 1 == tile1) umma_commit(&s.q_empty);
+          if (last) umma_commit(&s.q_empty);
           return true;
         };
         ok = mbar_wait(&s.q_full, seg & 1, limit);
         // (scores read by all rows: the next ones may take their place)
         if (ok && S::kOwn && it > 0) ok = mbar_wait(&s.s_free, (it - 1) & 1, limit);
-        ok = ok && scores(x.tile, it);
-        for (int j = x.tile; j < tile1 && ok; ++j, ++it) {
+        int j = x.tile + x.turn(p, s.share, tile1 - x.tile);
+        ok = ok && scores(j, it, x.tile + 1 == tile1);
+        for (int i = x.tile; i < tile1 && ok; ++i, ++it) {
           const int st = it % S::kStages;
-          if (S::kOwn && j + 1 < tile1) {
-            ok = mbar_wait(&s.s_free, it & 1, limit) && scores(j + 1, it + 1);
+          const int next = j + 1 < tile1 ? j + 1 : x.tile;
+          if (S::kOwn && i + 1 < tile1) {
+            ok = mbar_wait(&s.s_free, it & 1, limit) && scores(next, it + 1, i + 2 == tile1);
             if (!ok) break;
           }
           ok = mbar_wait(&s.v_full[st], (it / S::kStages) & 1, limit) &&
@@ -452,10 +467,11 @@ __global__ void __launch_bounds__(kThreads, 2)
           const int steps = keys(j) / 16;
           for (int c = 0; c < steps; ++c)
             umma_ts(tmem + S::kOut, tmem + S::weights(16 * c), umma_desc(va + c * 2048, kBlock),
-                    idesc_o, j > x.tile || c > 0);
+                    idesc_o, i > x.tile || c > 0);
           umma_commit(&s.o_done);
           umma_commit(&s.v_empty[st]);
-          if (!S::kOwn && j + 1 < tile1) ok = scores(j + 1, it + 1);
+          if (!S::kOwn && i + 1 < tile1) ok = scores(next, it + 1, i + 2 == tile1);
+          j = next;
         }
         todo -= tile1 - x.tile;
         x.next_item(p);
@@ -516,7 +532,10 @@ __global__ void __launch_bounds__(kThreads, 2)
         asm volatile("bar.sync 5, 256;" ::: "memory");
       }
       float m = -INFINITY, l = 0.f;  // the reference maximum (of scores) and the sum
-      for (int j = x.tile; j < tile1; ++j, ++it) {
+      if (lane == 0) x.start = x.tile + x.turn(p, s.share, tile1 - x.tile);
+      __syncwarp();
+      int j = x.start;
+      do {
         const int st = it % S::kStages;
         const uint32_t parity = (it / S::kStages) & 1;
         const bool cache = j < n_cache;
@@ -600,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           const uint32_t to = mine + S::weights(c0);
 #pragma unroll
           for (int h = 0; h < 2; ++h) tmem_st16(to + 16 * h, v[h]);
-          if (raised && j > x.tile) {
+          if (raised && j != x.start) {
 #pragma unroll 1
             for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
               uint32_t o[32];
@@ -644,7 +663,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         }
         tc_fence_before();
         mbar_arrive(&s.p_full);
-      }
+        ++it;
+        if (++j == tile1) j = x.tile;
+      } while (j != x.start);
       if (!ok) {
         if (t == 0) a.status[x.b] = TT_REQ_TIMEOUT;
         break;
