@@ -748,99 +748,117 @@ __global__ void __launch_bounds__(kThreads, 2)
 }
 
 // Joins the pieces of every row whose item was cut: with M the largest of their
-// references, out = sum 2^(m - M) o / sum 2^(m - M) l. A few pieces: a warp takes
-// a token's rows of a key head, kJoinRows at once (rows are many then, and what
-// they wait for is the way to their pieces). More: the CTA's warps take a row's
-// pieces in turn.
-constexpr int kJoinWarps = 4, kJoinRows = 4;
+// references, out = sum 2^(m - M) o / sum 2^(m - M) l. It has little to read and waits
+// for it, so what a row needs is asked for at once: the loads of four pieces before
+// the first is added (reading the maximum first cost 2.4 us of a call of 17). A few
+// pieces: a warp takes two of a key head's rows. More: the CTA's warps take a row's
+// pieces in turn (64-token trees over 65,536 keys with 11 pieces a row: 76 and 79 us;
+// 1 request of 8 tokens over 8192 with 30: 27 and 18).
+constexpr int kJoinWarps = 4, kFewPieces = 16;
 
 template <int D, bool F16, bool FEW>
 __global__ void __launch_bounds__(kJoinWarps * 32)
     tree_join_kernel(const __grid_constant__ TreeKernelArgs p) {
-  constexpr int N = D / 32, R = FEW ? kJoinRows : 1, W = FEW ? 1 : kJoinWarps;
+  constexpr int N = D / 32, R = FEW ? 2 : 1, W = FEW ? 1 : kJoinWarps;
+  constexpr int C = FEW ? 4 : 8;  // pieces at once
   using Vec = typename std::conditional<N == 4, float4, float2>::type;
-  __shared__ float s_acc[W][D];
-  __shared__ float s_l[W];
+  __shared__ __align__(16) float s_acc[W][D];
+  __shared__ float2 s_ml[W];
   const TreeArgs& a = p.a;
   const int warp = FEW ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
-  // token i of request b and key head hk (FEW), or the head h too
+  // row g0 (and the next) of key head hk, token i of request b
   const unsigned int x = FEW ? blockIdx.x * kJoinWarps + (threadIdx.x >> 5) : blockIdx.x;
-  const unsigned int heads = FEW ? a.Hkv : a.Hq;
-  const int head = int(x % heads), i = int(x / heads % a.max_nodes);
-  const int b = int(x / heads / a.max_nodes);
+  const unsigned int runs = (p.group + R - 1) / R, per_token = runs * a.Hkv;
+  const int g0 = int(x % runs) * R, hk = int(x % per_token / runs);
+  const int i = int(x / per_token % a.max_nodes), b = int(x / per_token / a.max_nodes);
   if (b >= a.B) return;
+  grid_dependency_wait();
+  const int share = p.first[a.B], first = p.first[b];
   const Request r = request(a, b);
   if (i >= r.nodes) return;
-  const int hk = FEW ? head : head / p.group;
   const int mt = i / p.per_tile;
   int before = hk * head_places(p, r) + kItemCost;  // its first tile's place
   for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles(p, r, k);
   const int last = before + item_tiles(p, r, mt) - 1;
-  grid_dependency_wait();
   // the CTAs that the item lies in
-  const int share = p.first[a.B], first = p.first[b];
   const int c0 = (first + before) / share, pieces = (first + last) / share - c0 + 1;
   if (pieces < 2) return;
-  for (int g0 = FEW ? 0 : head % p.group; g0 < (FEW ? p.group : head % p.group + 1); g0 += R) {
-    const int in_item = (i - mt * p.per_tile) * p.group + g0;
-    auto place = [&](int s, int q) {  // of row q in piece s (past the group: the last)
-      return (2 * (int64_t(c0) + s) + (s == 0)) * p.rows + in_item + min(q, p.group - 1 - g0);
-    };
-    float M[R], l[R], acc[R][N];
+  const int in_item = (i - mt * p.per_tile) * p.group + g0;
+  auto place = [&](int s, int q) {  // of row q in piece s (past the group: the last)
+    return (2 * (int64_t(c0) + s) + (s == 0)) * p.rows + in_item + min(q, p.group - 1 - g0);
+  };
+  float M[R], l[R], acc[R][N];
 #pragma unroll
-    for (int q = 0; q < R; ++q) {
-      M[q] = -INFINITY;
-      l[q] = 0.f;
+  for (int q = 0; q < R; ++q) {
+    M[q] = -INFINITY;
+    l[q] = 0.f;
 #pragma unroll
-      for (int c = 0; c < N; ++c) acc[q][c] = 0.f;
+    for (int c = 0; c < N; ++c) acc[q][c] = 0.f;
+  }
+  auto add = [&](int q, float l_more, const Vec& o, float f) {
+    l[q] = fmaf(l_more, f, l[q]);
+    acc[q][0] = fmaf(o.x, f, acc[q][0]);
+    acc[q][1] = fmaf(o.y, f, acc[q][1]);
+    if constexpr (N == 4) {
+      acc[q][2] = fmaf(o.z, f, acc[q][2]);
+      acc[q][3] = fmaf(o.w, f, acc[q][3]);
     }
-    for (int s = lane; s < pieces; s += 32) {
+  };
+  for (int s0 = warp; s0 < pieces; s0 += W * C) {
+    float2 ml[C][R];
+    Vec o[C][R];
 #pragma unroll
-      for (int q = 0; q < R; ++q) M[q] = fmaxf(M[q], p.part_ml[place(s, q)].x);
-    }
-#pragma unroll
-    for (int q = 0; q < R; ++q) M[q] = warp_max_f(M[q]);
-#pragma unroll 2
-    for (int s = warp; s < pieces; s += W) {
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
       for (int q = 0; q < R; ++q) {
-        const float2 ml = p.part_ml[place(s, q)];
-        const Vec o = reinterpret_cast<const Vec*>(p.part + place(s, q) * D)[lane];
-        // (a piece of nothing but -inf scores: 0, whatever the maximum is)
-        const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - M[q]);
-        l[q] = fmaf(ml.y, f, l[q]);
-        acc[q][0] = fmaf(o.x, f, acc[q][0]);
-        acc[q][1] = fmaf(o.y, f, acc[q][1]);
-        if constexpr (N == 4) {
-          acc[q][2] = fmaf(o.z, f, acc[q][2]);
-          acc[q][3] = fmaf(o.w, f, acc[q][3]);
-        }
-      }
-    }
-    if constexpr (!FEW) {
-#pragma unroll
-      for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[0][c];
-      if (lane == 0) s_l[warp] = l[0];
-      __syncthreads();
-      if (warp > 0) return;
-#pragma unroll
-      for (int w = 1; w < W; ++w) {
-        l[0] += s_l[w];
-#pragma unroll
-        for (int c = 0; c < N; ++c) acc[0][c] += s_acc[w][lane * N + c];
+        const int64_t at = place(min(s0 + c * W, pieces - 1), q);
+        ml[c][q] = p.part_ml[at];
+        o[c][q] = reinterpret_cast<const Vec*>(p.part + at * D)[lane];
       }
     }
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      if (g0 + q >= p.group) break;
-      const float inv = l[q] > 0.f || l[q] != l[q] ? 1.f / l[q] : 0.f;
-      const int64_t row = (int64_t(r.first) + i) * a.Hq + hk * p.group + g0 + q;
-      uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
-      out[0] = pack2<F16>(acc[q][0] * inv, acc[q][1] * inv);
-      if constexpr (N == 4) out[1] = pack2<F16>(acc[q][2] * inv, acc[q][3] * inv);
-      if (a.lse && lane == 0)
-        a.lse[row] = l[q] > 0.f || l[q] != l[q] ? fmaf(M[q], kLn2, logf(l[q])) : -INFINITY;
+      float top = M[q];
+#pragma unroll
+      for (int c = 0; c < C; ++c) top = fmaxf(top, ml[c][q].x);
+      const float f = M[q] == -INFINITY ? 0.f : ex2_approx(M[q] - top);
+      M[q] = top;
+      l[q] *= f;
+#pragma unroll
+      for (int c = 0; c < N; ++c) acc[q][c] *= f;
+      // (a piece of nothing but -inf scores: 0, whatever the maximum is)
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (s0 + c * W < pieces)
+          add(q, ml[c][q].y, o[c][q], ml[c][q].x == -INFINITY ? 0.f : ex2_approx(ml[c][q].x - top));
     }
+  }
+  if constexpr (!FEW) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[0][c];
+    if (lane == 0) s_ml[warp] = make_float2(M[0], l[0]);
+    __syncthreads();
+    if (warp > 0) return;
+    for (int w = 1; w < W; ++w) M[0] = fmaxf(M[0], s_ml[w].x);
+    l[0] = 0.f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) acc[0][c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = s_ml[w].x == -INFINITY ? 0.f : ex2_approx(s_ml[w].x - M[0]);
+      add(0, s_ml[w].y, reinterpret_cast<const Vec*>(s_acc[w])[lane], f);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < R; ++q) {
+    if (g0 + q >= p.group) break;
+    const float inv = l[q] > 0.f || l[q] != l[q] ? 1.f / l[q] : 0.f;
+    const int64_t row = (int64_t(r.first) + i) * a.Hq + hk * p.group + g0 + q;
+    uint32_t* out = reinterpret_cast<uint32_t*>(a.out + row * D * 2) + lane * (N / 2);
+    out[0] = pack2<F16>(acc[q][0] * inv, acc[q][1] * inv);
+    if constexpr (N == 4) out[1] = pack2<F16>(acc[q][2] * inv, acc[q][3] * inv);
+    if (a.lse && lane == 0)
+      a.lse[row] = l[q] > 0.f || l[q] != l[q] ? fmaf(M[q], kLn2, logf(l[q])) : -INFINITY;
   }
 }
 
@@ -920,10 +938,10 @@ cudaError_t launch(const TreeKernelArgs& p, int64_t pieces, cudaStream_t stream)
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
-  const bool few = pieces <= 8;
+  const bool few = pieces <= kFewPieces;
   const int64_t tokens = int64_t(a.B) * a.max_nodes;
-  cfg.gridDim =
-      dim3(unsigned(few ? (tokens * a.Hkv + kJoinWarps - 1) / kJoinWarps : tokens * a.Hq));
+  cfg.gridDim = dim3(unsigned(
+      few ? (tokens * a.Hkv * ((p.group + 1) / 2) + kJoinWarps - 1) / kJoinWarps : tokens * a.Hq));
   cfg.blockDim = dim3(kJoinWarps * 32);
   cfg.dynamicSmemBytes = 0;
   cfg.attrs = attr;
