@@ -15,9 +15,16 @@
 // what is left; the CTAs give each other their sums through distributed shared
 // memory, and each writes its share of the gradient. Logits are read from memory
 // once, the gradient written once. Several CTAs share an SM, so that one's copies
-// run beside another's sums and stores; a CTA's own steps are kept few, since thousands of rows make tens of thousands of CTAs: one warp
-// reads the list while the copies are on their way, a thread takes out, and later
-// patches, the listed columns of its own vectors.
+// run beside another's sums and stores; a CTA's own steps are kept few, since thousands
+// of rows make tens of thousands of CTAs: one warp reads the list while the copies are
+// on their way, a thread takes out, and later patches, the listed columns of its own
+// vectors.
+//
+// Measured, loss and gradient: 2048 rows of 128,256 bf16 columns, lists of 20, tail
+// mode 210 us, 5.0 TB/s; 1001 of 151,936 fp32, lists of 32, 242 us, 5.0 TB/s; 4 rows
+// 7 us. The bound is the way of a row, not the memory (54 % busy): copy, sums,
+// exchange (a fifth of the time) and stores follow each other, and shared memory holds
+// four or five shares per SM to put beside them.
 #include <cooperative_groups.h>
 #include <cstdint>
 

@@ -19,6 +19,12 @@
 // bar) are searched digit by digit, reading them again. When there are few rows, a
 // cluster of CTAs shares each and joins its parts through distributed shared
 // memory.
+//
+// Measured: 4096 rows of 201,088 bf16 columns with ids and 20 best 327 us, 5.0 TB/s
+// (without either 248 us, 6.6 TB/s); 608 rows of 151,936 fp32 columns 67 us, 5.5
+// TB/s; one row 7 us. The logits are the bound for the plain sums; ids that few
+// columns come behind (counting the others) and the ends of rows, where the last
+// columns are gathered and nothing is loaded, take the rest.
 #include <algorithm>
 #include <cooperative_groups.h>
 #include <cstdint>
@@ -32,7 +38,9 @@ namespace tt {
 
 namespace {
 
-constexpr int kBatch = 8;           // vectors of a thread between two looks at the bar
+// Vectors of a thread between two looks at the bar, all loaded before the first is
+// used: with 4 the 608 rows below took 71 to 75 us, with 8 they take 67.
+constexpr int kBatch = 8;
 constexpr int kVectors = 2048;      // room for vectors that reach the bar
 constexpr int kCandidates = 1024;   // and for columns that reach the last one
 constexpr int kMaxSplit = 16;

@@ -27,7 +27,15 @@
 // finds its part from the requests' sizes, and takes it item by item (an item:
 // one request, key head and row tile); the copies of an item begin while the one
 // before it is finished. Items cut by a CTA's end leave unnormalised pieces, which
-// a second kernel joins.
+// a second kernel joins. The row tiles of a head read the same keys, and a CTA goes
+// round its own so that all are at the same ones at a time: they come from memory
+// once (two documents of up to 131,072 keys under two row tiles 76 us without, 69
+// with).
+//
+// Measured: 64 requests of 9 tokens, 32 heads on 8, up to 8192 keys 176 us, 6.2 TB/s:
+// the cache is the bound. 64-token trees of 64-wide heads over up to 4096 keys, 16
+// requests, 47 us: the way of a tile is (scores, maximum, weights, product, one after
+// the other; tensor pipe 20 % busy, memory 22 %), and 9 us of the join.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 

@@ -169,6 +169,14 @@ def test_nodes(n, parents):
     check(make([129], [n], 5, 1, 128, 64, E, parents=parents, seed=n + 1))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(8, 1, 128), (9, 3, 64), (5, 1, 128), (32, 2, 64)])
+@pytest.mark.parametrize("dtype", [H, E])
+def test_several_row_tiles_over_long_caches(Hq, Hkv, D, dtype):
+    """Rows of a key head beyond one tile: each tile of rows goes round its keys
+    from a place of its own, and is cut at others."""
+    check(make([20001, 9000, 131, 0, 4097], [100, 33, 130, 65, 1], Hq, Hkv, D, 48, dtype, seed=9))
+
+
 @pytest.mark.parametrize("L", [3000, 8191, 20001, 70000])
 @pytest.mark.parametrize("Hq,Hkv,D", [(8, 1, 128), (4, 2, 64), (32, 8, 128)])
 def test_long_caches(L, Hq, Hkv, D):
