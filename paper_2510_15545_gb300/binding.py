@@ -8,6 +8,7 @@ from __future__ import annotations
 import ctypes
 import dataclasses
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -744,7 +745,7 @@ def tt_logprobs(logits: torch.Tensor, ids: Optional[torch.Tensor] = None, *, tem
             ("top_ids", i32, R * n), ("top_logprobs", f32, R * n), ("status", i32, R))]
     else:
         # (an allocation for each output cost a call 12 us on the Grace host)
-        buf = torch.empty(5 * R + 2 * R * max(n, 0), dtype=torch.float32, device=logits.device)
+        buf = logits.new_empty(5 * R + 2 * R * max(n, 0), dtype=torch.float32)
         whole = buf.view(torch.int32)
         row, top = ((R,), (1,)), ((R, n), (n, 1))
         o = {"lse": buf.as_strided(*row, 0), "entropy": buf.as_strided(*row, R),
@@ -874,7 +875,12 @@ def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: 
 _TREE_DTYPES = {torch.bfloat16: TT_BF16, torch.float16: TT_F16}
 
 
-def _heads(t: torch.Tensor, name: str, dtype, D: int, dims: int, C):
+# _Tree's fields in order: filled in one step, since five nested structures and 22
+# arguments took a call 2 us more of the Grace host
+_TREE = struct.Struct("8i2P" + 3 * "P2q" + 2 * "P3q" + "qPqPif")
+
+
+def _heads(t: torch.Tensor, name: str, dtype, D: int, dims: int):
     """Pointer and strides of a tensor [..., heads, head_dim] of the queries' type."""
     stride = t.stride()
     if t.dtype is not dtype or len(stride) != dims or t.shape[-1] != D:
@@ -882,7 +888,7 @@ def _heads(t: torch.Tensor, name: str, dtype, D: int, dims: int, C):
                          % (name, dims, str(dtype).replace("torch.", "")))
     if stride[-1] != 1:
         raise ValueError("%s must have unit stride within a head" % name)
-    return C(t.data_ptr(), *stride[:-1])
+    return t.data_ptr(), *stride[:-1]
 
 
 def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
@@ -902,18 +908,23 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
     if col != 1 and table[1] > 1:
         raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
     room = table[1] * cache[1]
-    max_len = room if max_len is None else int(max_len)
+    max_len = min(room, 1 << 30) if max_len is None else int(max_len)
     if max_len > room:
         raise ValueError("max_len is more than the page table's rows hold")
-    return _Tree(B, N, min(TT_MAX_TREE, max(N, 1)) if max_nodes is None else int(max_nodes), code,
-                 Hq, shape[1], D, cache[1], _given(tree_off, "tree_off", torch.int32, B + 1),
-                 _given(parents, "parents", torch.int32, N), _heads(q, "q", dtype, D, 3, _Heads),
-                 _heads(k, "k", dtype, D, 3, _Heads), _heads(v, "v", dtype, D, 3, _Heads),
-                 _heads(k_cache, "k_cache", dtype, D, 4, _Pages),
-                 _heads(v_cache, "v_cache", dtype, D, 4, _Pages), cache[0],
-                 page_table.data_ptr(), max(row, table[1]),
-                 _given(cache_len, "cache_len", torch.int32, B), max_len,
-                 D ** -0.5 if scale is None else float(scale))
+    T = _Tree()
+    try:
+        _TREE.pack_into(
+            T, 0, B, N, min(TT_MAX_TREE, max(N, 1)) if max_nodes is None else int(max_nodes), code,
+            Hq, shape[1], D, cache[1], _given(tree_off, "tree_off", torch.int32, B + 1) or 0,
+            _given(parents, "parents", torch.int32, N) or 0, *_heads(q, "q", dtype, D, 3),
+            *_heads(k, "k", dtype, D, 3), *_heads(v, "v", dtype, D, 3),
+            *_heads(k_cache, "k_cache", dtype, D, 4), *_heads(v_cache, "v_cache", dtype, D, 4),
+            cache[0], page_table.data_ptr(), max(row, table[1]),
+            _given(cache_len, "cache_len", torch.int32, B), max_len,
+            D ** -0.5 if scale is None else float(scale))
+    except (struct.error, OverflowError) as e:
+        raise ValueError("tt_tree_attn: a size is beyond its type") from e
+    return T
 
 
 def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
@@ -951,14 +962,14 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
         ws_p, n = (_ptr(ws), ws.numel()) if ws is not None else (None, 0)
     else:
         # (one allocation: scratch, then lse and status)
-        buf = torch.empty(n // 4 + rows + B, dtype=torch.float32, device=q.device)
+        buf = q.new_empty(n // 4 + rows + B, dtype=torch.float32)
         o = {"lse": buf.as_strided((N, Hq), (Hq, 1), n // 4),
              "status": buf.view(torch.int32).as_strided((B,), (1,), n // 4 + rows)}
         ws_p = buf.data_ptr()
         if ws is not None:
             ws_p, n = ws.data_ptr(), ws.numel()
     if "out" not in o:
-        o["out"] = torch.empty((N, Hq, D), dtype=q.dtype, device=q.device)
+        o["out"] = q.new_empty((N, Hq, D))
     code = L.tt_tree_attn(ctypes.byref(T), ws_p, n, _given(o["out"], "out", q.dtype, rows * D),
                           _given(o["lse"], "lse", torch.float32, rows),
                           _given(o["status"], "status", torch.int32, B), _stream(None))

@@ -29,6 +29,7 @@ def test_struct_layouts():
     assert T.v.offset == 96 and T.k_cache.offset == 120 and T.v_cache.offset == 152
     assert T.n_pages.offset == 184 and T.table_stride.offset == 200
     assert T.max_len.offset == 216 and T.scale.offset == 220 and ctypes.sizeof(T) == 224
+    assert binding._TREE.size == ctypes.sizeof(T)
 
 
 def logits(**kw):
