@@ -367,11 +367,18 @@ __global__ void __launch_bounds__(kThreads, 256 * kWidePerSm / kThreads)
     }
     if (given && top >= zt) {
       uint32_t n_before = 0;
+      if (v0 + kBatch * kThreads <= whole && uint32_t(v_id - v0) >= kBatch * kThreads) {
+        // (all of the batch on one side of the given column)
+        const uint32_t threshold = v0 < v_id ? from : above;
 #pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int v = v0 + u * kThreads + t;
-        if (vm[u] >= zt && v != v_id && v < nvec)
-          count_at_least<DT>(w[u], v < v_id ? from : above, n_before);
+        for (int u = 0; u < kBatch; ++u) count_at_least<DT>(w[u], threshold, n_before);
+      } else {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int v = v0 + u * kThreads + t;
+          if (vm[u] >= zt && v != v_id && v < nvec)
+            count_at_least<DT>(w[u], v < v_id ? from : above, n_before);
+        }
       }
       x.before += count_of<DT>(n_before);
     }
