@@ -20,8 +20,8 @@
 // cluster of CTAs shares each and joins its parts through distributed shared
 // memory.
 //
-// Measured: 4096 rows of 201,088 bf16 columns with ids and 20 best 327 us, 5.0 TB/s
-// (without either 248 us, 6.6 TB/s); 608 rows of 151,936 fp32 columns 67 us, 5.5
+// Measured: 4096 rows of 201,088 bf16 columns with ids and 20 best 314 us, 5.2 TB/s
+// (without either 248 us, 6.6 TB/s); 608 rows of 151,936 fp32 columns 62 us, 5.9
 // TB/s; one row 7 us. The logits are the bound for the plain sums; ids that few
 // columns come behind (counting the others) and the ends of rows, where the last
 // columns are gathered and nothing is loaded, take the rest.
@@ -39,7 +39,8 @@ namespace tt {
 namespace {
 
 // Vectors of a thread between two looks at the bar, all loaded before the first is
-// used: with 4 the 608 rows below took 71 to 75 us, with 8 they take 67.
+// used: 4096 rows of 201,088 bf16 columns 349 us with 4, 319 with 6, 314 with 8 (3000
+// rows of 4096 16, 18 and 20).
 constexpr int kBatch = 8;
 constexpr int kVectors = 2048;      // room for vectors that reach the bar
 constexpr int kCandidates = 1024;   // and for columns that reach the last one
@@ -47,8 +48,8 @@ constexpr int kMaxSplit = 16;
 // CTAs have 256 threads while those of all rows fit the SMs at once, 4 to an SM, and
 // 128, 8 to an SM, for more rows: the end of a row, which has no loads of its own,
 // holds up fewer threads, and the last rows leave less idle. Narrow / wide, us: 4096
-// rows of 201,088 bf16 columns 327 / 342, 1000 of 32,000 fp32 28.9 / 31.3, 3000 of 4096
-// bf16 19.9 / 34.1; but 608 of 151,936 fp32 87 / 67, 310 of 128,256 bf16 47 / 33.
+// rows of 201,088 bf16 columns 312 / 328, 1000 of 32,000 fp32 26.9 / 30.2, 3000 of 4096
+// bf16 20.2 / 34.7; but 608 of 151,936 fp32 76 / 62, 310 of 128,256 bf16 44 / 31.
 constexpr int kWidePerSm = 4;
 constexpr float kLeast = -3.402823466e38f;  // -inf never reaches a bar
 constexpr float kLn2 = 0.693147180559945f;
