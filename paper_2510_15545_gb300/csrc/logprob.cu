@@ -21,10 +21,10 @@
 // memory.
 //
 // Measured: 4096 rows of 201,088 bf16 columns with ids and 20 best 314 us, 5.2 TB/s
-// (without either 248 us, 6.6 TB/s); 608 rows of 151,936 fp32 columns 62 us, 5.9
-// TB/s; one row 7 us. The logits are the bound for the plain sums; ids that few
-// columns come behind (counting the others) and the ends of rows, where the last
-// columns are gathered and nothing is loaded, take the rest.
+// (without either 254 us, 6.5 TB/s); 608 rows of 151,936 fp32 columns 62 us, 5.9
+// TB/s; one row 7 us. The logits are the bound for the plain sums; the
+// ends of rows, where the best columns are gathered and nothing is loaded, take most
+// of the rest (45 us), the count of the columns before the given ones 10.
 #include <algorithm>
 #include <cooperative_groups.h>
 #include <cstdint>
