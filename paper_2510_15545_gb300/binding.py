@@ -848,6 +848,20 @@ def tt_distill_grad(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_log
     return g
 
 
+class _DistillGrad(torch.autograd.Function):
+    """tt_distill_grad within a backward pass: it has no derivative of its own, and
+    says so when one is asked for."""
+
+    @staticmethod
+    def forward(ctx, logits, ids, logp, stats, up, temp, tail):
+        return tt_distill_grad(logits, ids, logp, stats, temp=temp, tail=tail,
+                               weight=up.float().contiguous())
+
+    @staticmethod
+    def backward(ctx, _):
+        raise RuntimeError("distill_loss has no second derivative")
+
+
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, teacher_ids, teacher_logp, temp, tail):
@@ -858,11 +872,7 @@ class _DistillLoss(torch.autograd.Function):
 
     @staticmethod
     def backward(ctx, up):
-        logits, ids, logp, stats = ctx.saved_tensors
-        temp, tail = ctx.args
-        g = tt_distill_grad(logits, ids, logp, stats, temp=temp, tail=tail,
-                            weight=up.float().contiguous())
-        return g, None, None, None, None
+        return _DistillGrad.apply(*ctx.saved_tensors, up, *ctx.args), None, None, None, None
 
 
 def distill_loss(logits: torch.Tensor, teacher_ids: torch.Tensor, teacher_logp: torch.Tensor, *,

@@ -329,6 +329,16 @@ def test_autograd():
     torch.testing.assert_close(head.grad, want, rtol=1e-4, atol=1e-6)
 
 
+def test_a_gradient_has_none_of_its_own():
+    """Second derivatives are refused, not taken for zero."""
+    gen = torch.Generator().manual_seed(12)
+    ids, logp = (x.cuda() for x in teacher(3, 512, 4, gen))
+    z = torch.randn((3, 512), generator=gen).cuda().requires_grad_()
+    g, = torch.autograd.grad(tt.distill_loss(z * z, ids, logp).sum(), z, create_graph=True)
+    with pytest.raises(RuntimeError):
+        g.sum().backward()
+
+
 def test_logprobs_lists_and_streams():
     """What tt_logprobs answers about the target's rows is the teacher's list; the
     calls take the stream they are given, and repeat to the bit."""
