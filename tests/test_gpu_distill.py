@@ -329,6 +329,23 @@ def test_autograd():
     torch.testing.assert_close(head.grad, want, rtol=1e-4, atol=1e-6)
 
 
+@pytest.mark.parametrize("dtype", [F, H])
+def test_rows_billions_of_bytes_apart(dtype):
+    """The same bits as rows that are close, in one call and in two."""
+    gen = torch.Generator().manual_seed(13)
+    R, V, step = 5, 3001, 2 ** 30 + 8
+    ids, logp = (x.cuda() for x in teacher(R, V, 6, gen))
+    near = rows_of(torch.randn((R, V), generator=gen), dtype)
+    far = torch.empty(R * step, dtype=dtype, device="cuda").as_strided((R, V), (step, 1))
+    far.copy_(near)
+    g, h = (tt.tt_distill(z, ids, logp, tail=True) for z in (near, far))
+    two = tt.tt_distill_grad(far, ids, logp, h["stats"], tail=True)
+    tt.tt_distill(far, ids, logp, tail=True, grad=far)
+    assert torch.equal(g["loss"], h["loss"])
+    for got in (h["grad"], two, far):
+        assert torch.equal(g["grad"], got)
+
+
 def test_a_gradient_has_none_of_its_own():
     """Second derivatives are refused, not taken for zero."""
     gen = torch.Generator().manual_seed(12)

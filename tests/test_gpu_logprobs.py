@@ -248,6 +248,14 @@ def test_rows_that_are_not_finite(V, dtype):
     check(rows_of(z[[3, 5]], dtype), ids[[3, 5]], n=4)
 
 
+def test_rows_billions_of_bytes_apart():
+    gen = torch.Generator().manual_seed(8)
+    step = 2 ** 29 + 8
+    rows = torch.empty(9 * step, device="cuda").as_strided((9, 3001), (step, 1))
+    rows.copy_(torch.randn((9, 3001), generator=gen))
+    check(rows, random_ids(9, 3001, gen), n=9)
+
+
 def test_ids_out_of_range():
     gen = torch.Generator().manual_seed(1)
     rows = rows_of(torch.randn((5, 1000), generator=gen), F)

@@ -299,6 +299,30 @@ def test_strides():
     assert torch.equal(check(dataclasses.replace(d, q=wide))["out"], g["out"])
 
 
+def test_keys_and_values_laid_out_differently():
+    """Slots outermost in one cache, heads in the other."""
+    c = make([300, 70], [6, 9], 8, 2, 64, 32, E, seed=18)
+    g = check(c)
+    for name in ("k_cache", "v_cache"):
+        turned = getattr(c, name).transpose(1, 2).contiguous().transpose(1, 2)
+        h = check(dataclasses.replace(c, **{name: turned}))
+        assert torch.equal(g["out"], h["out"]) and torch.equal(g["lse"], h["lse"])
+
+
+def test_offsets_beyond_32_bits():
+    """Pages that start billions of bytes apart."""
+    c = make([60, 40], [3, 2], 4, 2, 128, 32, H, seed=19, extra=0)
+    g = check(c)
+    pages, far = c.k_cache.shape[0], {}
+    for name in ("k_cache", "v_cache"):
+        step = 2 ** 30 + 64
+        buf = torch.empty(pages * step, dtype=H, device="cuda")
+        far[name] = buf.as_strided(c.k_cache.shape, (step, 256, 128, 1))
+        far[name].copy_(getattr(c, name))
+    h = check(dataclasses.replace(c, **far))
+    assert torch.equal(g["out"], h["out"]) and torch.equal(g["lse"], h["lse"])
+
+
 def test_bounds_above_what_is_there():
     """max_len and max_nodes may be larger than any request's."""
     c = make([300, 0, 70], [6, 1, 9], 8, 2, 128, 32, H, seed=16)
