@@ -683,7 +683,10 @@ __global__ void __launch_bounds__(kThreads, 2)
       const bool has_tree = tile1 > n_cache;
       if (has_tree) asm volatile("bar.sync 5, 256;" ::: "memory");  // (s.odd is whole)
       if (some) {
-        l += other(l, it & 1);
+        // (the slot of the last tile's maxima: all have read those, or that tile's product
+        // would not be done, and the slot's next maxima lie behind another barrier; the
+        // other slot is where the next item's first maxima go, with none between)
+        l += other(l, (it - 1) & 1);
         const bool whole = x.tile == 0 && tile1 == n_cache + tree_tiles(node1);
         // where the row goes: to the output, or to its place in the CTA's piece
         const int64_t to =

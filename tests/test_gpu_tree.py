@@ -195,6 +195,21 @@ def test_ragged_batches_with_empty_requests():
     check(make(lens, nodes, 16, 4, 64, 32, H, seed=4))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,n", [(8, 2, 128, 4), (16, 4, 64, 3), (32, 1, 64, 4)])
+@pytest.mark.parametrize("dtype", [H, E])
+def test_items_that_follow_each_other_within_caches(Hq, Hkv, D, n, dtype):
+    """CTAs that end one item and begin another, which they leave before its drafted
+    tokens: the two threads of a row add up the one's sum while the other's first
+    scores come. The same bits each time."""
+    gen = torch.Generator().manual_seed(31)
+    lens = torch.randint(500, 3500, (150,), generator=gen).tolist()
+    c = make(lens, [n] * 150, Hq, Hkv, D, 64, dtype, seed=32)
+    first = check(c)
+    for _ in range(30):
+        g = tt.tt_tree_attn(*c.args(), max_len=max(lens), max_nodes=n)
+        assert torch.equal(g["out"], first["out"]) and torch.equal(g["lse"], first["lse"])
+
+
 @pytest.mark.parametrize("size", [0.05, 6.0])
 def test_flat_and_sharp_softmax(size):
     for dtype in (H, E):
