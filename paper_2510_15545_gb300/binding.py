@@ -921,6 +921,10 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
     max_len = min(room, 1 << 30) if max_len is None else int(max_len)
     if max_len > room:
         raise ValueError("max_len is more than the page table's rows hold")
+    if B < 2:  # (the stride of a single row is any number)
+        row = max(row, table[1])
+    elif row < table[1] and max_len > 0 and row < (max_len - 1) // cache[1] + 1:
+        raise ValueError("page_table's rows share memory; give its .contiguous()")
     T = _Tree()
     try:
         _TREE.pack_into(
@@ -929,7 +933,7 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
             _given(parents, "parents", torch.int32, N) or 0, *_heads(q, "q", dtype, D, 3),
             *_heads(k, "k", dtype, D, 3), *_heads(v, "v", dtype, D, 3),
             *_heads(k_cache, "k_cache", dtype, D, 4), *_heads(v_cache, "v_cache", dtype, D, 4),
-            cache[0], page_table.data_ptr(), max(row, table[1]),
+            cache[0], page_table.data_ptr(), row,
             _given(cache_len, "cache_len", torch.int32, B), max_len,
             D ** -0.5 if scale is None else float(scale))
     except (struct.error, OverflowError) as e:

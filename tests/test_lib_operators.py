@@ -5,6 +5,7 @@ import ctypes
 import math
 
 import pytest
+import torch
 
 import paper_2510_15545_gb300 as tt
 from paper_2510_15545_gb300 import _build, binding
@@ -177,6 +178,36 @@ def test_tree_refuses_what_its_numbers_do_not_hold(lib):
     assert attend(lib, big) == UNSUPPORTED
     assert attend(lib, tree(B=1 << 20, max_nodes=512)) == UNSUPPORTED
     assert attend(lib, tree(B=2**31 - 1)) == UNSUPPORTED
+
+
+def described(table, B, **kw):
+    """The descriptor of a call with a page table, of pages of 16 slots."""
+    heads = torch.zeros((B, 2, 64), dtype=torch.bfloat16)
+    cache = torch.zeros((9, 16, 2, 64), dtype=torch.bfloat16)
+    lens, off = torch.zeros(B, dtype=torch.int32), torch.arange(B + 1, dtype=torch.int32)
+    a = dict(scale=None, max_len=None, max_nodes=None)
+    a.update(kw)
+    return binding._tree(heads, heads, heads, cache, cache, table, lens, off, None, **a)
+
+
+def test_page_tables_whose_rows_share_memory_are_refused():
+    """A stride of theirs, or one made up, would have the kernel read other entries
+    than the table's, or past its end."""
+    row = torch.arange(5, dtype=torch.int32)
+    for table in (row.expand(4, 5), row.repeat(2).unfold(0, 5, 1)[:4]):
+        with pytest.raises(ValueError):
+            described(table, 4)
+        with pytest.raises(ValueError):
+            described(table, 4, max_len=33)
+    # rows that share only what no request reaches keep their own stride
+    T = described(torch.arange(20, dtype=torch.int32).unfold(0, 5, 3)[:4], 4, max_len=48)
+    assert T.table_stride == 3 and T.max_len == 48
+    for B in (1, 4):
+        assert described(row.repeat(B, 1), B).table_stride == 5
+        assert described(torch.zeros((B, 12), dtype=torch.int32)[:, :5], B).table_stride == 12
+    # one row has any stride; no length needs no row
+    assert described(row.expand(1, 5).as_strided((1, 5), (0, 1)), 1).table_stride == 5
+    assert described(torch.zeros((4, 0), dtype=torch.int32), 4).max_len == 0
 
 
 def test_status_bits_and_types():
