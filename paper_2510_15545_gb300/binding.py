@@ -965,23 +965,21 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
     L = load()
     N, Hq, D = q.shape
     rows, B = N * Hq, T.B
-    n = int(L.tt_tree_workspace_bytes(ctypes.byref(T))) if ws is None else 0
+    if ws is None:
+        # (an allocation of its own, gone when the call returns: in one with lse, whoever
+        # keeps that would keep it too)
+        n = int(L.tt_tree_workspace_bytes(ctypes.byref(T)))
+        ws = q.new_empty(n, dtype=torch.uint8)
+    ws_p, n = ws.data_ptr(), ws.numel()
     if out:
         o = dict(out)
         if "lse" not in o:
             o["lse"] = torch.empty((N, Hq), dtype=torch.float32, device=q.device)
         _need(o, "status", B, torch.int32, q.device)
-        if n:
-            ws = torch.empty(n, dtype=torch.uint8, device=q.device)
-        ws_p, n = (_ptr(ws), ws.numel()) if ws is not None else (None, 0)
     else:
-        # (one allocation: scratch, then lse and status)
-        buf = q.new_empty(n // 4 + rows + B, dtype=torch.float32)
-        o = {"lse": buf.as_strided((N, Hq), (Hq, 1), n // 4),
-             "status": buf.view(torch.int32).as_strided((B,), (1,), n // 4 + rows)}
-        ws_p = buf.data_ptr()
-        if ws is not None:
-            ws_p, n = ws.data_ptr(), ws.numel()
+        buf = q.new_empty(rows + B, dtype=torch.float32)
+        o = {"lse": buf.as_strided((N, Hq), (Hq, 1), 0),
+             "status": buf.view(torch.int32).as_strided((B,), (1,), rows)}
     if "out" not in o:
         o["out"] = q.new_empty((N, Hq, D))
     code = L.tt_tree_attn(ctypes.byref(T), ws_p, n, _given(o["out"], "out", q.dtype, rows * D),

@@ -210,5 +210,39 @@ def test_page_tables_whose_rows_share_memory_are_refused():
     assert described(torch.zeros((4, 0), dtype=torch.int32), 4).max_len == 0
 
 
+class Calls:
+    """Stands for the library on the host: keeps the arguments of its calls, whose
+    sizes the real one gives, and answers that all went well."""
+
+    def __init__(self, monkeypatch, lib):
+        self.lib, self.args = lib, {}
+        monkeypatch.setattr(binding, "load", lambda: self)
+        monkeypatch.setattr(binding, "_stream", lambda stream: None)
+
+    def __getattr__(self, name):
+        if name.endswith("_bytes"):
+            return getattr(self.lib, name)
+
+        def call(*args):
+            self.args[name] = args
+            return 0
+        return call
+
+
+def test_results_of_tree_attention_hold_no_scratch(lib, monkeypatch):
+    calls = Calls(monkeypatch, lib)
+    heads = torch.zeros((8, 8, 128), dtype=torch.bfloat16)
+    cache = torch.zeros((4, 16, 8, 128), dtype=torch.bfloat16)
+    table = torch.zeros((2, 2), dtype=torch.int32)
+    lens, off = torch.zeros(2, dtype=torch.int32), torch.tensor([0, 4, 8], dtype=torch.int32)
+    status = torch.zeros(2, dtype=torch.int32)
+    for out in (None, dict(status=status), dict(out=torch.zeros_like(heads))):
+        o = tt.tt_tree_attn(heads, heads, heads, cache, cache, table, lens, off, out=out)
+        need = calls.args["tt_tree_attn"][2]
+        assert need >= lib.tt_tree_workspace_bytes(calls.args["tt_tree_attn"][0]) > 100000
+        for name, x in o.items():
+            assert x.untyped_storage().nbytes() < 20000, name
+
+
 def test_status_bits_and_types():
     assert (binding.TT_F32, binding.TT_BF16, binding.TT_F16) == (0, 1, 2)
