@@ -865,10 +865,14 @@ class _DistillGrad(torch.autograd.Function):
 class _DistillLoss(torch.autograd.Function):
     @staticmethod
     def forward(ctx, logits, teacher_ids, teacher_logp, temp, tail):
-        o = tt_distill(logits, teacher_ids, teacher_logp, temp=temp, tail=tail, grad=False)
+        # (a loss of its own: as a view beside the stats, which the backward pass reads, it
+        # could not be changed in place)
+        loss = logits.new_empty(logits.shape[:1], dtype=torch.float32)
+        o = tt_distill(logits, teacher_ids, teacher_logp, temp=temp, tail=tail, grad=False,
+                       out=dict(loss=loss))
         ctx.save_for_backward(logits, teacher_ids, teacher_logp, o["stats"])
         ctx.args = temp, tail
-        return o["loss"][:logits.shape[0]]
+        return loss
 
     @staticmethod
     def backward(ctx, up):

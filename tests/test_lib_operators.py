@@ -244,5 +244,18 @@ def test_results_of_tree_attention_hold_no_scratch(lib, monkeypatch):
             assert x.untyped_storage().nbytes() < 20000, name
 
 
+@pytest.mark.parametrize("change", [lambda x: x.mul_(2.0), lambda x: x.div_(4.0),
+                                    lambda x: x[0].zero_()])
+def test_losses_may_be_changed_in_place(lib, monkeypatch, change):
+    """As any loss may: what the backward pass keeps is no part of them."""
+    Calls(monkeypatch, lib)
+    z = torch.zeros((3, 8), requires_grad=True)
+    loss = tt.distill_loss(z, torch.zeros((3, 2), dtype=torch.int32), torch.zeros((3, 2)))
+    assert loss.shape == (3,) and loss.dtype is torch.float32
+    change(loss)
+    loss.sum().backward()
+    assert z.grad.shape == z.shape
+
+
 def test_status_bits_and_types():
     assert (binding.TT_F32, binding.TT_BF16, binding.TT_F16) == (0, 1, 2)
