@@ -430,8 +430,9 @@ typedef struct {
  *   tail = 0: the list is normalised, p = softmax(logp), and the loss is
  *     sum p (ln p - ln q) over it;
  *   tail = 1: p = exp(logp) as given, and the teacher's remaining mass
- *     r = max(0, 1 - sum p) is compared with the student's mass t outside the
- *     list: the loss gets r (ln r - ln t).
+ *     r = 1 - sum p is compared with the student's mass t outside the list: the
+ *     loss gets r (ln r - ln t). r is 0 up to 2^-20 sum p (1 + |ln p|), within
+ *     which 1 - sum p is rounding: a list that holds all of its teacher's mass.
  * loss [R] (optional) is not weighted; grad (optional; the student's type, width
  * and row count; may be the student's own memory) = weight[r] dloss[r] / dz, with
  * weight [R] fp32 or NULL for 1. stats [R * 4] (optional, 16-byte aligned) is what

@@ -52,6 +52,12 @@ constexpr int kSegmentGoal = 52 * 1024;
 constexpr int kSegmentMax = 200 * 1024;  // bytes of a row that a CTA holds
 constexpr int kHeldBytes = 48 * 1024;    // rows up to this are held for a loss alone, too
 constexpr int kStep = 4;  // vectors of a thread summed at once
+// 1 - P is no mass but rounding up to this much of sum p (1 + |ln p|): each ln p comes
+// rounded from a sum of rounded exponentials, and its own exponential is rounded (some
+// 16 roundings of 2^-24, of p or of p |ln p|). A list that holds all of its teacher's
+// mass (a mask leaves fewer columns than it has room for) would else have a rest of
+// 1e-7, and a student masked alike, which has nothing there, a loss of inf.
+constexpr float kRestRounding = 1.f / (1 << 20);
 
 // The list's entries within a CTA's columns, those of one column added up in the
 // first of them (the others have column -1), and the whole list's mass.
@@ -108,19 +114,25 @@ __device__ __forceinline__ void read_entries(const DistillArgs& a, int64_t r, in
   }
   const float lead = a.tail ? 0.f : warp_max_f(top);
   F2 mass = {0.f, 0.f};
+  float terms = 0.f;  // sum p (1 + |ln p|)
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    p[i] = id[i] >= 0 ? expf(p[i] - lead) : 0.f;
+    const float ln = p[i] - lead;
+    p[i] = id[i] >= 0 ? expf(ln) : 0.f;
     mass = f2_add(mass, F2{p[i], 0.f});
+    if (id[i] >= 0) terms = fmaf(p[i], 1.f + fabsf(ln), terms);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
-    if (a.tail)  // (1 - P is what it is needed for)
+    if (a.tail) {  // (1 - P is what they are needed for)
       mass = f2_add(mass, F2{__shfl_xor_sync(0xffffffffu, mass.hi, o),
                              __shfl_xor_sync(0xffffffffu, mass.lo, o)});
-    else
+      terms += __shfl_xor_sync(0xffffffffu, terms, o);
+    } else {
       mass.hi += __shfl_xor_sync(0xffffffffu, mass.hi, o);
+    }
   }
+  const float rest = (1.f - mass.hi) - mass.lo;
   const float inv = a.tail || !(mass.hi > 0.f) ? 1.f : 1.f / mass.hi;
   int n = 0;
 #pragma unroll
@@ -173,7 +185,7 @@ __device__ __forceinline__ void read_entries(const DistillArgs& a, int64_t r, in
   if (lane == 0) {
     L.count = n;
     L.mass = a.tail ? mass.hi : any ? 1.f : 0.f;
-    L.rest = a.tail && any ? fmaxf(0.f, (1.f - mass.hi) - mass.lo) : 0.f;
+    L.rest = a.tail && any && rest > kRestRounding * terms ? rest : 0.f;
     L.status = (any ? 0 : TT_REQ_EMPTY) | (odd ? TT_REQ_NOT_FINITE : 0) |
                (off ? TT_REQ_ID_OUT_OF_RANGE : 0);
   }

@@ -248,6 +248,49 @@ def test_masked_students(dtype, low, tail):
 
 
 @pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("low", [-math.inf, "lowest"])
+@pytest.mark.parametrize("V,R,left", [(3000, 300, 1), (3000, 300, 3), (3000, 300, 20), (70001, 40, 9)])
+def test_lists_that_hold_the_whole_mass(dtype, low, V, R, left):
+    """A mask leaves fewer columns than the teacher lists, and the student is masked
+    alike: nothing is outside the list on either side, and what 1 - P says is
+    rounding. (A list's log probabilities are off by 1e-5 at most, so p by that
+    relative amount and the loss by that much of sum p (1 + |ln p - ln q|).)"""
+    gen = torch.Generator().manual_seed(V + left)
+    keep = torch.zeros((R, V), dtype=torch.bool)
+    keep.scatter_(1, torch.stack([torch.randperm(V, generator=gen)[:left] for _ in range(R)]), True)
+    low = torch.finfo(dtype).min if low == "lowest" else low
+    target, student = (rows_of((torch.randn((R, V), generator=gen) * 3).masked_fill(~keep, low), dtype)
+                       for _ in range(2))
+    for temp in (0.6, 1.0):
+        o = tt.tt_logprobs(target, temp=temp, top_n=32)
+        logp = torch.log_softmax((target.cpu().double() / temp).masked_fill(~keep, -math.inf), 1)
+        logq = torch.log_softmax(student.cpu().double().masked_fill(~keep, -math.inf), 1)
+        p, q = torch.exp(logp), torch.exp(logq)
+        apart = torch.where(keep, logp - logq, 0.0)
+        loss = (p * apart).sum(1)
+        room = 1e-5 * ((p * (1 + apart.abs())).sum(1) + loss.abs()) + 2e-5
+        for grad in (True, False):
+            g = tt.tt_distill(student, o["top_ids"], o["top_logprobs"], tail=True, grad=grad)
+            assert (g["status"] == 0).all() and torch.isfinite(g["loss"]).all()
+            assert ((g["loss"].cpu().double() - loss).abs() <= room).all()
+            back = tt.tt_distill_grad(student, o["top_ids"], o["top_logprobs"], g["stats"], tail=True)
+            for x in (back, g.get("grad", back)):
+                check_grad(x, q - p, 2e-5 * (q + p), dtype)
+
+
+@pytest.mark.parametrize("missing", [0.0, 1e-7, 1e-5])
+def test_what_counts_as_a_rest(missing):
+    """A whole row's list: mass that is missing beyond rounding has no place in the
+    student, whose loss is inf; up to rounding there is none."""
+    gen = torch.Generator().manual_seed(18)
+    logp = torch.log_softmax(torch.randn((50, 16), generator=gen).double(), 1) + math.log1p(-missing)
+    ids = torch.arange(16).expand(50, 16).int().contiguous().cuda()
+    z = rows_of(torch.randn((50, 16), generator=gen), F)
+    loss = tt.tt_distill(z, ids, logp.float().cuda(), tail=True)["loss"]
+    assert (loss == math.inf).all() if missing > 1e-6 else torch.isfinite(loss).all()
+
+
+@pytest.mark.parametrize("dtype", [F, H])
 def test_rows_without_a_loss(dtype):
     """No usable entry: 0 and EMPTY. No normaliser or an entry that is no log
     probability: NaN, gradient 0, NOT_FINITE. An impossible column: loss inf, the
