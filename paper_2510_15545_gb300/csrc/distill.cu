@@ -228,6 +228,24 @@ __device__ __forceinline__ void store_elem(char* row, int x, float v) {
   }
 }
 
+// Logits that the gradient may be written over: loads that need not find the memory
+// unwritten while the kernel runs, as read-only ones do.
+template <int DT>
+__device__ __forceinline__ float row_logit(const char* row, int64_t x) {
+  if constexpr (DT == TT_F32)
+    return reinterpret_cast<const float*>(row)[x];
+  else
+    return bf16_to_f32(reinterpret_cast<const uint16_t*>(row)[x]);
+}
+__device__ __forceinline__ uint4 row_vector(const char* p) {
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(p)
+               : "memory");
+  return r;
+}
+
 // The row's maximum and sums from its CTAs' shares, the same in every CTA:
 // q_j = 2^((z_j - M) scale) / all, t = 2^((m_out - M) scale) out / all.
 struct Row {
@@ -432,7 +450,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   // the ragged tail (the row's last columns) with -inf behind it
   if (nvec > whole && t >= 32 && t < 32 + VEC) {
     const int x = whole * VEC + t - 32;
-    set_smem_logit<DT>(seg, x, c0 + x < c1 ? load_logit<DT>(row, c0 + x) : -INFINITY);
+    set_smem_logit<DT>(seg, x, c0 + x < c1 ? row_logit<DT>(row, c0 + x) : -INFINITY);
   }
   if (warp == 0) read_list(a, r, c0, c1, L, lane);
   __syncthreads();
@@ -625,19 +643,19 @@ __global__ void __launch_bounds__(kThreads) distill_grad_kernel(
 #pragma unroll
   for (int u = 0; u < kPerThread; ++u) {
     const int v = u * kThreads + t;
-    w[u] = v < whole ? ld_stream_v4(in + v * 16) : make_uint4(0, 0, 0, 0);
+    w[u] = v < whole ? row_vector(in + v * 16) : make_uint4(0, 0, 0, 0);
   }
   const bool ragged = t == whole % kThreads;  // the thread of the row's last columns
   float z_tail[VEC];
   if (ragged)
     for (int q = 0; q < VEC; ++q)
-      z_tail[q] = c0 + whole * VEC + q < c1 ? load_logit<DT>(row, c0 + whole * VEC + q) : 0.f;
+      z_tail[q] = c0 + whole * VEC + q < c1 ? row_logit<DT>(row, c0 + whole * VEC + q) : 0.f;
   const float4 st = reinterpret_cast<const float4*>(a.stats)[r];
   if (t < 32) {
     read_list(a, r, c0, c1, L, t);
     __syncwarp();
     for (int e = t; e < L.count; e += 32)
-      if (L.col[e] >= 0) L.z[e] = load_logit<DT>(row, L.col[e]);
+      if (L.col[e] >= 0) L.z[e] = row_logit<DT>(row, L.col[e]);
     if (t == 0) s_factors = factors(a, L, r, Row{st.x, st.y, st.z, st.w});
   }
   __syncthreads();

@@ -358,6 +358,23 @@ def test_gradient_in_the_logits_place(dtype):
     assert torch.equal(two, tt.tt_distill_grad(rows, ids, logp, want["stats"], tail=True))
 
 
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("R,V", [(3000, 2051), (700, 33001), (60, 151939)])
+def test_many_gradients_in_the_logits_place(dtype, R, V):
+    """More rows than run at once, ragged ends, lists at both ends of a row."""
+    gen = torch.Generator().manual_seed(R)
+    ids = torch.randint(V, (R, 8), generator=gen).int().cuda()
+    ids[:, 0], ids[:, 1] = 0, V - 1
+    logp = (torch.log_softmax(torch.randn((R, 8), generator=gen), 1) - 0.2).cuda()
+    rows = rows_of(torch.randn((R, V), generator=gen), dtype)
+    want = tt.tt_distill(rows, ids, logp, tail=True)
+    later = tt.tt_distill_grad(rows, ids, logp, want["stats"], tail=True)
+    one, two = rows_of(rows, dtype), rows_of(rows, dtype)
+    tt.tt_distill(one, ids, logp, tail=True, grad=one)
+    tt.tt_distill_grad(two, ids, logp, want["stats"], tail=True, grad=two)
+    assert torch.equal(one, want["grad"]) and torch.equal(two, later)
+
+
 def test_autograd():
     gen = torch.Generator().manual_seed(11)
     R, V = 7, 4096
