@@ -80,6 +80,7 @@ struct Share {
   float out;
   float mass;   // sum of p on the list,
   float cross;  // and of p (ln p - (z - m) / T), with 0 for an m of -inf
+  int late;     // its copies did not come in time: the sums are NaN
 };
 
 // One warp reads the list of row r for columns c0 .. c1 - 1: p = exp(logp),
@@ -258,7 +259,7 @@ __device__ __forceinline__ float relative(float x, float m, float M, float scale
 // (by one warp, a share to a lane: by every thread, it was a tenth of a CTA's work)
 __device__ __forceinline__ Row row_sums(const DistillArgs& a, const Share* share, int S, int lane) {
   static_assert(kMaxSplit <= 16, "shares of half a warp");
-  Share x{-INFINITY, 0.f, -INFINITY, 0.f, 0.f, 0.f};
+  Share x{-INFINITY, 0.f, -INFINITY, 0.f, 0.f, 0.f, 0};
   if (lane < S) x = share[lane];
   Row y{x.m, 0.f, x.m_out, 0.f};
 #pragma unroll
@@ -326,9 +327,9 @@ __device__ __forceinline__ void set_smem_logit(char* seg, int x, float z) {
 // One warp adds the list's columns (their logits in L.z) to the sums of the
 // CTA's warps (their maxima and sums outside the list).
 __device__ __forceinline__ Share cta_share(const DistillArgs& a, const List& L, const float2* s_ms,
-                                           int lane) {
+                                           int lane, bool late) {
   const int n = L.count;
-  Share x{lane < kWarps ? s_ms[lane].x : -INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f};
+  Share x{lane < kWarps ? s_ms[lane].x : -INFINITY, 0.f, 0.f, 0.f, 0.f, 0.f, late};
   x.m_out = warp_max_f(x.m);
   for (int e = lane; e < n; e += 32)
     if (L.col[e] >= 0) x.m = fmaxf(x.m, L.z[e]);
@@ -350,15 +351,18 @@ __device__ __forceinline__ Share cta_share(const DistillArgs& a, const List& L, 
     x.cross += __shfl_xor_sync(0xffffffffu, x.cross, o);
   }
   x.all += relative(x.out, x.m_out, x.m, a.scale);
+  if (late) x.all = __int_as_float(0x7fffffff);
   return x;
 }
 
 // One thread writes the row's loss, statistics and status.
 __device__ __forceinline__ void report(const DistillArgs& a, int64_t r, const List& L,
-                                       const Share* share, int S, const Row& y, bool ok) {
+                                       const Share* share, int S, const Row& y) {
   const float ln_s = logf(y.all);
   float loss = 0.f, mass = 0.f;
+  int late = 0;
   for (int k = 0; k < S; ++k) {
+    late |= share[k].late;
     if (!(share[k].mass > 0.f)) continue;
     const float ref = share[k].m > -INFINITY ? share[k].m : 0.f;
     mass += share[k].mass;
@@ -369,7 +373,7 @@ __device__ __forceinline__ void report(const DistillArgs& a, int64_t r, const Li
     loss += L.rest * (logf(L.rest) -
                       (y.out > 0.f ? (y.m_out - y.M) / a.temp + logf(y.out) - ln_s : -INFINITY));
   const bool finite = y.all > 0.f && y.all < INFINITY;
-  const int st = L.status | (finite ? 0 : TT_REQ_NOT_FINITE) | (ok ? 0 : TT_REQ_TIMEOUT);
+  const int st = L.status | (late ? TT_REQ_TIMEOUT : finite ? 0 : TT_REQ_NOT_FINITE);
   a.status[r] = st;
   if (a.loss)
     a.loss[r] = st & (TT_REQ_NOT_FINITE | TT_REQ_TIMEOUT) ? __int_as_float(0x7fffffff)
@@ -443,7 +447,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     if (whole > 0) {
       mbar_arrive_expect_tx(&full, whole * 16);
-      for (int at = 0; at < whole * 16; at += 32768)
+      for (int at = 0; at < whole * 16 && int(blockIdx.x) != a.stall; at += 32768)
         bulk_copy_g2s(seg + at, row + int64_t(c0) * ESZ + at, min(32768, whole * 16 - at), &full);
     }
   }
@@ -454,8 +458,10 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
   }
   if (warp == 0) read_list(a, r, c0, c1, L, lane);
   __syncthreads();
-  const uint64_t limit = kWaitLimitNs;
-  const bool ok = whole == 0 || mbar_wait(&full, 0, limit);
+  const bool landed = whole == 0 || mbar_wait(&full, 0, a.wait_ns);
+  // (late copies still come into this CTA's memory: it stays for them. At the kernel's
+  // end, the second wait cost every row: 218 us for 210.)
+  if (!landed) mbar_wait(&full, 0, a.wait_ns);
   // take the list's columns out of this thread's vectors
   const int n = L.count;
   for (int e = 0; e < n; ++e) {
@@ -474,12 +480,11 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
       w[u] = v0 + u * kThreads < nvec ? sv[v0 + u * kThreads] : no_logits<DT>();
     add_vectors<DT>(run, w, a.scale);
   }
-  float2 ms = warp_running(run, a.scale);
-  if (!ok) ms.y = __int_as_float(0x7fffffff);
+  const float2 ms = warp_running(run, a.scale);
   if (lane == 0) s_ms[warp] = ms;
-  __syncthreads();
+  const bool ok = __syncthreads_and(landed);
   if (warp == 0) {
-    const Share x = cta_share(a, L, s_ms, lane);
+    const Share x = cta_share(a, L, s_ms, lane, !ok);
     if (S > 1) cluster.barrier_wait();
     if (lane < S) (S > 1 ? cluster.map_shared_rank(s_share, lane) : s_share)[rank] = x;
   } else if (S > 1) {
@@ -495,7 +500,7 @@ __global__ void __launch_bounds__(kThreads) distill_kernel(const __grid_constant
     if (lane == 0) s_factors = factors(a, L, r, y);
   }
   __syncthreads();
-  if (rank == 0 && t == 0) report(a, r, L, s_share, S, y, ok);
+  if (rank == 0 && t == 0) report(a, r, L, s_share, S, y);
   if (!a.grad) return;
   const Factors f = s_factors;
   char* grow = a.grad + r * a.grad_stride_bytes;
@@ -604,7 +609,7 @@ __global__ void __launch_bounds__(kThreads, 8) distill_loss_kernel(
   if (lane == 0) s_ms[warp] = ms;
   __syncthreads();
   if (warp == 0) {
-    const Share x = cta_share(a, L, s_ms, lane);
+    const Share x = cta_share(a, L, s_ms, lane, false);
     if (S > 1) cluster.barrier_wait();
     if (lane == 0) (S > 1 ? cluster.map_shared_rank(s_share, 0) : s_share)[rank] = x;
     __syncwarp();
@@ -614,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 8) distill_loss_kernel(
   if (S > 1) cluster.sync();
   if (rank == 0 && warp == 0) {
     const Row y = row_sums(a, s_share, S, lane);
-    if (lane == 0) report(a, r, L, s_share, S, y, true);
+    if (lane == 0) report(a, r, L, s_share, S, y);
   }
 }
 
@@ -733,7 +738,9 @@ cudaError_t preload() {
 
 int distill_max_cols(int dt) { return kMaxSplit * kSegmentMax / (dt == TT_F32 ? 4 : 2); }
 
-cudaError_t launch_distill(const DistillArgs& a, int dt, cudaStream_t stream, int sm_count) {
+cudaError_t launch_distill(const DistillArgs& args, int dt, cudaStream_t stream, int sm_count) {
+  DistillArgs a = args;
+  next_launch_stall(&a.stall, &a.wait_ns);
   return dt == TT_F32 ? launch<TT_F32>(a, stream, sm_count) : launch<TT_BF16>(a, stream, sm_count);
 }
 

@@ -17,6 +17,9 @@ cudaError_t load_kernels();
 int device_sms();
 bool rows_usable(const tt_logits* L, int64_t rows);
 tt_status record_cuda_error(cudaError_t e);
+// Test hook of the bounded waits (rowpass.cu): the CTA to hold up and the wait limit
+// of the next launch; false (and the defaults) when off.
+bool next_launch_stall(int32_t* cta, uint64_t* wait_ns);
 
 struct LogprobArgs {
   const char* data;
@@ -49,7 +52,10 @@ struct DistillArgs {
   int32_t* status;
   char* grad;  // NULL: the forward call alone
   int64_t grad_stride_bytes;
-  int split, share;  // CTAs per row and columns of each (filled in by the launcher)
+  // filled in by the launcher:
+  int split, share;  // CTAs per row and columns of each
+  int stall;         // the CTA whose copies a test withholds, or -1
+  uint64_t wait_ns;  // limit of a wait
 };
 
 int distill_max_cols(int dt);
