@@ -68,8 +68,8 @@ typedef enum {
 #define TT_REQ_EMPTY 4           /* k == 0 or m == 0 */
 #define TT_REQ_BAD_OFFSETS 8     /* CSR offsets decreasing or outside [0, n_draft/n_target] */
 #define TT_REQ_NOT_FINITE 16     /* a logits row gave a non-finite normaliser */
-#define TT_REQ_TIMEOUT 32        /* a pipeline wait in the row pass gave up (bounded waits);
-                                    the step's results are not valid */
+#define TT_REQ_TIMEOUT 32        /* a wait inside a kernel gave up (all are bounded); the
+                                    step's results, or the row's or request's, are not valid */
 #define TT_REQ_INTERNAL 64       /* an internal bounds check in a kernel failed (the access
                                     was skipped); the step's results are not valid */
 #define TT_REQ_NO_MATCH 128      /* tt_encode: some position of the decoded draft string is
@@ -515,7 +515,8 @@ size_t tt_tree_workspace_bytes(const tt_tree* tree);
  * status [B]: BAD_OFFSETS and TOO_LONG (more nodes than max_nodes, a length that
  * is negative or above max_len) leave the request's outputs unwritten;
  * ID_OUT_OF_RANGE reports a parent or a page out of range (the node then counts
- * as a root, the page's slots are left out). Lengths of zero are fine. */
+ * as a root, the page's slots are left out); TIMEOUT marks every request that a
+ * CTA whose wait gave up left undone. Lengths of zero are fine. */
 tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_bytes, void* out,
                        float* lse, int32_t* status, void* stream);
 

@@ -92,6 +92,9 @@ struct TreeKernelArgs {
   float* part;        // [2 ctas * rows * D] outputs, not normalised
   float2* part_ml;    // [2 ctas * rows] their reference maximum (log2) and sum
   int32_t* first;     // [B + 1] places before each request's, then the places per CTA
+  int32_t* stop;      // [ctas] the place from which a CTA gave up, INT32_MAX if it did not
+  uint64_t wait_ns;   // limit of a wait
+  int stall;          // the CTA whose copies a test withholds from its second tile on, or -1
 };
 
 // A request's usable range: its nodes and cache length, or why it has none.
@@ -202,13 +205,13 @@ struct Smem {
   uint32_t left_out[4];          // boxes of the last tiles that were not copied
   uint32_t odd[kWords];          // drafted tokens with a value that is not finite
   uint64_t q_full, k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
-  uint64_t q_empty, s_full, s_free, p_full, o_done;
+  uint64_t q_empty, s_full, s_free, p_full, o_done, drained;
   long long sums[kThreads / 32];  // places of the requests, by warps
   int start_b, start_offset;      // where this CTA's places begin
   int share;                      // and how many a CTA has
   Place place[kRowWarps];         // where the row warps are (their registers are dear)
   uint32_t tmem;
-  int failed;
+  int end, stop;                  // the place behind this CTA's, and where it gave up
 };
 
 template <bool F16>
@@ -260,7 +263,7 @@ __global__ void __launch_bounds__(kThreads, 2)
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
   const TreeArgs& a = p.a;
   const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-  const uint64_t limit = kWaitLimitNs;
+  const uint64_t& limit = p.wait_ns;
   grid_launch_dependents();
 
   if (t == kRowThreads) {
@@ -279,7 +282,8 @@ __global__ void __launch_bounds__(kThreads, 2)
     mbar_init(&s.s_free, kRowThreads);
     mbar_init(&s.p_full, kRowThreads);
     mbar_init(&s.o_done, 1);
-    s.failed = 0;
+    mbar_init(&s.drained, 1);
+    s.stop = INT32_MAX;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kRowWarps + 1) tmem_alloc(&s.tmem, kTmemColumns);
@@ -309,7 +313,10 @@ __global__ void __launch_bounds__(kThreads, 2)
     const long long share = max((long long)(kMinShare), (all + p.ctas - 1) / p.ctas);
     const long long from = share * blockIdx.x;
     todo = int(max(0ll, min(share, all - from)));
-    if (t == 0) s.share = int(share);
+    if (t == 0) {
+      s.share = int(share);
+      s.end = int(min(all, from + share));
+    }
     long long at = upto - mine;
     if (todo > 0 && from >= at && from < upto) {
       for (int b = b0; b < b1; ++b) {
@@ -342,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, 2)
     if (todo > 0) x.find(p, s.start_b, s.start_offset);
     // lane i copies a tile's i-th box of slots
     const int per = kTile / p.box;
-    int it = 0;
+    int it = 0, q_copies = 0, k_copies = 0, v_copies = 0;
     for (int seg = 0; todo > x.lead && ok; ++seg) {
       todo -= x.lead;
       const int n_cache = cache_tiles(x.r.len);
@@ -366,6 +373,7 @@ __global__ void __launch_bounds__(kThreads, 2)
                       x.hk * p.group, x.r.first + node0);
       }
       __syncwarp();
+      ++q_copies;
       for (int i = x.tile; i < tile1; ++i, ++it) {
         const int st = it % S::kStages;
         const uint32_t parity = ((it / S::kStages) & 1) ^ 1;
@@ -404,7 +412,8 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
           __syncwarp();
         };
-        ok = __all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit));
+        ok = __all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit)) &&
+             (it != 1 || int(blockIdx.x) != p.stall);
         if (!ok) break;
         // boxes of slots in use whose page is out of range (told before the copy is)
         if (lane == 0)
@@ -412,14 +421,22 @@ __global__ void __launch_bounds__(kThreads, 2)
               cache ? ~copied & ((1u << (min(kTile, x.r.len - j * kTile) + p.box - 1) / p.box) - 1)
                     : 0u;
         copy(s.k[st], &s.k_full[st], &p.kc, &p.k);
+        ++k_copies;
         ok = __all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit));
         if (!ok) break;
         copy(s.v[st], &s.v_full[st], &p.vc, &p.v);
+        ++v_copies;
         page = next;
         j = next_j;
       }
       todo -= tile1 - x.tile;
       x.next_item(p);
+    }
+    // (the CTA's memory stays until its last copies have come)
+    if (q_copies > 0) mbar_wait(&s.q_full, (q_copies - 1) & 1, limit);
+    for (int st = 0; st < S::kStages; ++st) {
+      if (k_copies > st) mbar_wait(&s.k_full[st], ((k_copies - 1 - st) / S::kStages) & 1, limit);
+      if (v_copies > st) mbar_wait(&s.v_full[st], ((v_copies - 1 - st) / S::kStages) & 1, limit);
     }
   } else if (warp == kRowWarps + 1) {
     // ---------------------------------------------------------- products
@@ -484,6 +501,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         todo -= tile1 - x.tile;
         x.next_item(p);
       }
+      // (and until its last products and their arrivals are done)
+      umma_commit(&s.drained);
+      mbar_wait(&s.drained, 0, limit);
     }
   } else {
     // -------------------------------------------------------------- rows
@@ -506,6 +526,14 @@ __global__ void __launch_bounds__(kThreads, 2)
       s.half[turn][half][row] = y;
       asm volatile("bar.sync %0, 64;" ::"r"(1 + quarter) : "memory");
       return s.half[turn][half ^ 1][row];
+    };
+    // A warp goes on, or gives up, as one. One that gave up passes the barriers between
+    // the warps as often as the others, but waits and arrives no more and writes
+    // nothing: so the others give up, too, and all end.
+    auto wait_for = [&](uint64_t* bar, uint32_t parity) {
+      if (!ok) return;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+      if (!ok && lane == 0) atomicMin(&s.stop, s.end - todo);
     };
     Place& x = s.place[warp];
     if (lane == 0) {
@@ -550,8 +578,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         const int base = (j - n_cache) * kTile;  // first drafted token of a tree tile
         const int left = cache ? x.r.len - j * kTile : node1 - base;
         const int n = min(kTile, (left + 31) & ~31);
-        // (the warp goes on, or gives up, as one)
-        if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.s_full, it & 1, limit)))) break;
+        wait_for(&s.s_full, it & 1);
         tc_fence_after();
         const uint32_t bad_boxes = s.left_out[it & 3];
         // which of 32 keys from c on the row sees; `there`: which hold anything
@@ -617,9 +644,9 @@ __global__ void __launch_bounds__(kThreads, 2)
         // has to be done with the weights' place and in the output. (Every warp waits
         // for that, or one without rows would be a tile ahead on p_full.)
         if (S::kOwn) {
-          mbar_arrive(&s.s_free);
+          if (ok) mbar_arrive(&s.s_free);
           if (it > 0) {
-            if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
+            wait_for(&s.o_done, (it - 1) & 1);
             tc_fence_after();
           }
         }
@@ -644,7 +671,7 @@ __global__ void __launch_bounds__(kThreads, 2)
         // could be NaN), and of drafted tokens, what is not finite: a token outside
         // its branch would get NaN from it. (Its own branch gets it at the end.)
         if (left < n || bad_boxes || !cache) {
-          if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.v_full[st], parity, limit)))) break;
+          wait_for(&s.v_full[st], parity);
           for (int i = t; i < n * kHalves * 8; i += kRowThreads) {
             const int key = (i >> 3) % n, block = (i >> 3) / n;
             uint4* at = reinterpret_cast<uint4*>(s.v[st] + block * kBlock + key * 128 + (i & 7) * 16);
@@ -670,15 +697,11 @@ __global__ void __launch_bounds__(kThreads, 2)
           fence_proxy_async();
         }
         tc_fence_before();
-        mbar_arrive(&s.p_full);
+        if (ok) mbar_arrive(&s.p_full);
         ++it;
         if (++j == tile1) j = x.tile;
       } while (j != x.start);
-      if (!ok) {
-        if (t == 0) a.status[x.b] = TT_REQ_TIMEOUT;
-        break;
-      }
-      if (!(ok = __all_sync(0xffffffffu, mbar_wait(&s.o_done, (it - 1) & 1, limit)))) break;
+      wait_for(&s.o_done, (it - 1) & 1);
       tc_fence_after();
       const bool has_tree = tile1 > n_cache;
       if (has_tree) asm volatile("bar.sync 5, 256;" ::: "memory");  // (s.odd is whole)
@@ -698,7 +721,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           uint32_t v[32];
           tmem_ld32(mine + S::kOut + c, v);
           tmem_wait_ld(v);
-          if (valid) {
+          if (valid && ok) {
             if (has_tree) {
               for (int w = 0; w * 32 < node1; ++w)
                 for (uint32_t odd = s.odd[w] & s.seen[local][w]; odd; odd &= odd - 1) {
@@ -736,7 +759,7 @@ __global__ void __launch_bounds__(kThreads, 2)
           }
           __syncwarp();
         }
-        if (valid && half == 0) {
+        if (valid && ok && half == 0) {
           const float m2 = m == -INFINITY ? -INFINITY : m * p.scale2 - kOffset;
           if (!whole)
             p.part_ml[to] = make_float2(m2, l);
@@ -751,11 +774,10 @@ __global__ void __launch_bounds__(kThreads, 2)
       __syncwarp();
     }
   }
-  if (!ok) atomicOr(&s.failed, 1);
   tc_fence_before();
   __syncthreads();
   if (warp == kRowWarps + 1) tmem_free(tmem, kTmemColumns);
-  if (t == 0 && s.failed && todo > 0) a.status[s.place[0].b] = TT_REQ_TIMEOUT;
+  if (t == 0) p.stop[blockIdx.x] = s.stop;  // (the join tells the requests)
 }
 
 // Joins the pieces of every row whose item was cut: with M the largest of their
@@ -764,7 +786,8 @@ __global__ void __launch_bounds__(kThreads, 2)
 // the first is added (reading the maximum first cost 2.4 us of a call of 17). A few
 // pieces: a warp takes two of a key head's rows. More: the CTA's warps take a row's
 // pieces in turn (64-token trees over 65,536 keys with 11 pieces a row: 76 and 79 us;
-// 1 request of 8 tokens over 8192 with 30: 27 and 18).
+// 1 request of 8 tokens over 8192 with 30: 27 and 18). It also tells the requests that
+// lost places to a CTA that gave up.
 constexpr int kJoinWarps = 4, kFewPieces = 16;
 
 template <int D, bool F16, bool FEW>
@@ -787,8 +810,16 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   const int share = p.first[a.B], first = p.first[b];
   const Request r = request(a, b);
   if (i >= r.nodes) return;
+  const int per_head = head_places(p, r);
+  // (one warp of the request)
+  if (i == 0 && hk == 0 && g0 == 0 && (FEW || threadIdx.x < 32)) {
+    const int end = first + per_head * a.Hkv - 1;  // its last place
+    int stop = INT32_MAX;
+    for (int c = first / share + lane; c <= end / share; c += 32) stop = min(stop, p.stop[c]);
+    if (__any_sync(0xffffffffu, stop <= end) && lane == 0) a.status[b] |= TT_REQ_TIMEOUT;
+  }
   const int mt = i / p.per_tile;
-  int before = hk * head_places(p, r) + kItemCost;  // its first tile's place
+  int before = hk * per_head + kItemCost;  // its first tile's place
   for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles(p, r, k);
   const int last = before + item_tiles(p, r, mt) - 1;
   // the CTAs that the item lies in
@@ -880,7 +911,7 @@ struct Cut {
   int group, per_tile, ctas, rows;
   int64_t places;  // in the list, were all lengths the longest
   int64_t pieces;  // of one item, about
-  size_t part_bytes, ml_bytes, bytes;
+  size_t part_bytes, ml_bytes, first_bytes, bytes;
 };
 Cut cut(const TreeArgs& a, int sm_count) {
   Cut c;
@@ -899,7 +930,8 @@ Cut cut(const TreeArgs& a, int sm_count) {
   const size_t rows = 2 * size_t(c.ctas) * c.rows;
   c.part_bytes = align256(rows * a.D * sizeof(float));
   c.ml_bytes = align256(rows * sizeof(float2));
-  c.bytes = c.part_bytes + c.ml_bytes + align256((size_t(a.B) + 1) * sizeof(int32_t));
+  c.first_bytes = align256((size_t(a.B) + 1) * sizeof(int32_t));
+  c.bytes = c.part_bytes + c.ml_bytes + c.first_bytes + align256(c.ctas * sizeof(int32_t));
   return c;
 }
 
@@ -945,7 +977,7 @@ cudaError_t launch(const TreeKernelArgs& p, int64_t pieces, cudaStream_t stream)
   cfg.dynamicSmemBytes = sizeof(Smem<D>) + 1024;
   cfg.stream = stream;
   cudaError_t e = cudaLaunchKernelEx(&cfg, tree_kernel<D, F16>, p);
-  if (e != cudaSuccess || p.ctas == 1) return e;
+  if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -995,6 +1027,8 @@ cudaError_t launch_tree(const TreeArgs& a, int dt, cudaStream_t stream, int sm_c
   p.part = reinterpret_cast<float*>(a.ws);
   p.part_ml = reinterpret_cast<float2*>(a.ws + c.part_bytes);
   p.first = reinterpret_cast<int32_t*>(a.ws + c.part_bytes + c.ml_bytes);
+  p.stop = p.first + c.first_bytes / sizeof(int32_t);
+  next_launch_stall(&p.stall, &p.wait_ns);
   const bool f16 = dt == TT_F16;
   bool ok = true;
   if (a.n_nodes > 0) {

@@ -68,3 +68,76 @@ def _run_child(code, cta):
     (40, 151936, "float32", False, True, 47, 3)])
 def test_a_row_whose_logits_do_not_come(R, V, dtype, tail, grad, cta, row):
     _run_child(DISTILL % dict(root=ROOT, R=R, V=V, dtype=dtype, tail=tail, grad=grad, row=row), cta)
+
+
+TREE = r"""
+import sys, time
+sys.path.insert(0, %(root)r)
+import torch
+import paper_2510_15545_gb300 as tt
+from paper_2510_15545_gb300 import binding
+tt.load(build_if_missing=True)
+gen = torch.Generator(device="cuda").manual_seed(2)
+lens, n, Hq, Hkv, D, hit, may = %(lens)r, %(n)d, %(Hq)d, %(Hkv)d, %(D)d, %(hit)r, %(may)r
+B, page = len(lens), 64
+P = (max(lens) + page - 1) // page
+randn = lambda *s: torch.randn(s, generator=gen, device="cuda").to(torch.%(dtype)s)
+i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+args = (randn(B * n, Hq, D), randn(B * n, Hkv, D), randn(B * n, Hkv, D),
+        randn(B * P, page, Hkv, D), randn(B * P, page, Hkv, D),
+        torch.arange(B * P, device="cuda").int().view(B, P), i32(lens),
+        torch.arange(B + 1, device="cuda").int() * n)
+torch.cuda.synchronize()
+t0 = time.perf_counter()
+g = tt.tt_tree_attn(*args, max_len=max(lens), max_nodes=n)
+torch.cuda.synchronize()
+assert time.perf_counter() - t0 < 20.0
+assert binding.load().tt_last_cuda_error() == 0
+status = g["status"].tolist()
+late = [b for b in range(B) if status[b]]
+assert all(status[b] == 32 for b in late) and set(hit) <= set(late) <= set(may), (late, hit, may)
+h = tt.tt_tree_attn(*args, max_len=max(lens), max_nodes=n)
+assert h["status"].tolist() == [0] * B and torch.isfinite(h["out"]).all()
+for b in range(B):
+    if b not in late:
+        for key in ("out", "lse"):
+            assert torch.equal(g[key][b * n:(b + 1) * n], h[key][b * n:(b + 1) * n]), (b, key)
+print("child ok")
+"""
+
+
+def _list(lens, n, Hq, Hkv):
+    """The requests of the places of the list that the CTAs share, and a CTA's share."""
+    per_tile = 128 // (Hq // Hkv)
+    tiles = lambda x: (x + 127) // 128  # noqa: E731
+    places = []
+    for b, L in enumerate(lens):
+        for _ in range(Hkv):
+            for first in range(0, n, per_tile):
+                places += [b] * (3 + tiles(L) + tiles(min(n, first + per_tile)))
+    ctas = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    return places, max(2, -(-len(places) // ctas))
+
+
+# one row tile a head, and two; wide heads, and narrow ones, whose products run ahead
+@pytest.mark.parametrize("n,Hq,Hkv,D,dtype", [
+    (4, 8, 2, 128, "bfloat16"), (5, 4, 2, 64, "float16"), (32, 16, 2, 128, "bfloat16"),
+    (64, 8, 2, 64, "float16")])
+@pytest.mark.parametrize("two", [False, True])
+def test_requests_whose_keys_do_not_come(n, Hq, Hkv, D, dtype, two):
+    """A CTA that gives up within one request, or before it comes to the next one:
+    both are told, and no others."""
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    lens = [40000, 39000, 38500, 41000, 37777, 40001, 36000, 42000]
+    places, share = _list(lens, n, Hq, Hkv)
+    assert share >= 8
+    for cta in range(3, len(places) // share):
+        mine = places[cta * share:(cta + 1) * share]
+        # (two tiles at least before the next request begins)
+        if (mine[0] != mine[-1] and mine.count(mine[0]) >= 5) if two else mine[0] == mine[-1]:
+            break
+    else:
+        pytest.skip("no such CTA among these places")
+    _run_child(TREE % dict(root=ROOT, lens=lens, n=n, Hq=Hq, Hkv=Hkv, D=D, dtype=dtype,
+                           hit=sorted({mine[0], mine[-1]}), may=sorted(set(mine))), cta)
