@@ -22,7 +22,7 @@
 //
 // Measured, loss and gradient: 2048 rows of 128,256 bf16 columns, lists of 20, tail
 // mode 210 us, 5.0 TB/s; 1001 of 151,936 fp32, lists of 32, 242 us, 5.0 TB/s; 4 rows
-// 7 us. The bound is the way of a row, not the memory (54 % busy): copy, sums,
+// 7 us. The bound is the way of a row, not the memory (0.74 of a copy's rate): copy, sums,
 // exchange (a fifth of the time) and stores follow each other, and shared memory holds
 // four or five shares per SM to put beside them.
 #include <cooperative_groups.h>
@@ -48,6 +48,8 @@ constexpr int kMaxSplit = 16;
 // ones exchange more sums, larger ones leave fewer to run beside each other. Loss
 // and gradient of 2048 rows of 128,256 bf16 columns: 4 CTAs 230 us, 5 220, 6 210,
 // 7 225, 8 212; of 1001 rows of 151,936 fp32: 9 248, 12 243, 13 265, 14 247, 16 258.
+// (7 and 13 are behind their neighbours, 5 and 9 are not; whether by the cluster's size
+// or the share's was not told apart.)
 constexpr int kSegmentGoal = 52 * 1024;
 constexpr int kSegmentMax = 200 * 1024;  // bytes of a row that a CTA holds
 constexpr int kHeldBytes = 48 * 1024;    // rows up to this are held for a loss alone, too

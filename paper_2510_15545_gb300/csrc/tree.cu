@@ -32,10 +32,10 @@
 // once (two documents of up to 131,072 keys under two row tiles 76 us without, 69
 // with).
 //
-// Measured: 64 requests of 9 tokens, 32 heads on 8, up to 8192 keys 176 us, 6.2 TB/s:
+// Measured: 64 requests of 9 tokens, 32 heads on 8, up to 8192 keys 175 us, 6.3 TB/s:
 // the cache is the bound. 64-token trees of 64-wide heads over up to 4096 keys, 16
 // requests, 47 us: the way of a tile is (scores, maximum, weights, product, one after
-// the other; tensor pipe 20 % busy, memory 22 %), and 9 us of the join.
+// the other; tensor pipe 16 % busy, memory at a quarter of its rate), and 9 us of the join.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
