@@ -1085,9 +1085,7 @@ namespace {
 // TT_TEST_STALL_LAUNCHES row-pass launches (default 1) hold the stage of its
 // n-th consumer step, with every pipeline wait of those launches limited to
 // TT_TEST_WAIT_MS milliseconds, so that a test can watch the waits run out and
-// the call report TT_REQ_TIMEOUT, then see the next launches run normally. (The
-// operators' kernels that wait for copies count as such launches: there it is CTA n
-// whose copies do not come.)
+// the call report TT_REQ_TIMEOUT, then see the next launches run normally.
 struct StallHook {
   int stall_stage = -1;
   uint64_t wait_ns = kWaitLimitNs;

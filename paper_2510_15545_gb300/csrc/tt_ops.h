@@ -17,8 +17,9 @@ cudaError_t load_kernels();
 int device_sms();
 bool rows_usable(const tt_logits* L, int64_t rows);
 tt_status record_cuda_error(cudaError_t e);
-// Test hook of the bounded waits (rowpass.cu): the CTA to hold up and the wait limit
-// of the next launch; false (and the defaults) when off.
+// Test hook of the bounded waits (rowpass.cu, whose launches and those of the
+// operators that wait for copies are counted together): the CTA whose copies are
+// withheld and the wait limit of the next launch; false (and the defaults) when off.
 bool next_launch_stall(int32_t* cta, uint64_t* wait_ns);
 
 struct LogprobArgs {
