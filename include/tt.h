@@ -81,7 +81,7 @@ typedef enum {
 #define TT_MAX_DPOS_BINS 4096    /* most bins of tt_dpos_hist */
 #define TT_MAX_HISTORY 3072      /* longest repetition-penalty history per request */
 
-typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 /* tt_tree_attn only */ } tt_dtype;
+typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 /* heads only */ } tt_dtype;
 
 /* A token byte-string table: token id v spells bytes[offsets[v] .. offsets[v+1]). */
 typedef struct {
@@ -519,6 +519,66 @@ size_t tt_tree_workspace_bytes(const tt_tree* tree);
  * CTA whose wait gave up left undone. Lengths of zero are fine. */
 tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_bytes, void* out,
                        float* lse, int32_t* status, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Rotary positions.
+ */
+
+/* How the pairs of a head's first rot_dim elements turn. */
+typedef struct {
+  const uint64_t* turns; /* device, [rot_dim / 2] turns per position of each pair, as
+                            fractions of 2^64 (tt_rope_turns) */
+  int32_t rot_dim;       /* even, 2 .. head_dim; the other elements stay as they are */
+  int32_t interleaved;   /* pairs (i, i + rot_dim / 2) if 0, (2i, 2i + 1) if 1 */
+  float mscale;          /* factor of the turned elements (1; an attention factor of
+                            scaled contexts) */
+} tt_rope_plan;
+
+#define TT_ROPE_PLAIN 0  /* f_i = base ^ (-2i / rot_dim), i = 0 .. rot_dim / 2 - 1 */
+#define TT_ROPE_LINEAR 1 /* f_i / factor */
+#define TT_ROPE_BASE 2   /* base * factor ^ (rot_dim / (rot_dim - 2)) in place of base: the
+                            slowest pair turns factor times slower */
+#define TT_ROPE_PARTS 3  /* by parts (YaRN, arXiv 2309.00071): a pair that makes r turns in the
+                            original context gets f_i ((1 - g) / factor + g), g = (r - low) /
+                            (high - low) held within 0 .. 1 */
+
+typedef struct {
+  int32_t rot_dim; /* even, 2 .. 256 (TT_ROPE_BASE: from 4) */
+  int32_t scaling; /* TT_ROPE_* */
+  double base;     /* > 0 */
+  double factor;   /* > 0; how many times longer the context has become */
+  double original; /* > 0: positions of the original context (TT_ROPE_PARTS) */
+  double low, high; /* turns within it, low < high (TT_ROPE_PARTS) */
+} tt_rope_config;
+
+/* Angles per position, radians, [rot_dim / 2]. HOST memory, no GPU needed. */
+tt_status tt_rope_freqs(const tt_rope_config* config, double* freqs);
+
+/* n angles per position (any finite radians) as tt_rope_plan's turns. HOST memory in
+ * and out: the caller copies them to the device once. */
+tt_status tt_rope_turns(const double* freqs, int32_t n, uint64_t* turns);
+
+/* Query and key heads of n_tokens tokens to be rotated. An output may be its own
+ * input (same data and strides), else it shares no memory with the inputs. Inputs may
+ * have strides of 0; an output's heads must not overlap. */
+typedef struct {
+  int32_t n_tokens;
+  int32_t dtype;     /* tt_dtype: fp32, bf16 or fp16 */
+  int32_t head_dim;  /* a multiple of 8, 8 .. 256 */
+  int32_t n_q_heads; /* >= 1 */
+  int32_t n_k_heads; /* 0: no keys (k and k_out unused) */
+  int32_t transpose; /* 1: the transposed map (sines negated, mscale kept), which takes a
+                        gradient of the outputs to one of the inputs */
+  const int32_t* positions; /* device, [n_tokens]; any int32 */
+  tt_heads q, k;         /* read */
+  tt_heads q_out, k_out; /* written */
+  tt_rope_plan plan;
+} tt_rotate;
+
+/* Rotates every head by its token's position, in one launch. Angles are exact to
+ * 2^-32 turns at any position, sines and cosines and products fp32, the result is
+ * rounded once. Needs no workspace. */
+tt_status tt_rope(const tt_rotate* rotate, void* stream);
 
 /* Static text for a tt_status. */
 const char* tt_status_string(tt_status s);

@@ -97,13 +97,29 @@ class _Tree(ctypes.Structure):
                 ("cache_len", c_p), ("max_len", c_i32), ("scale", c_f32)]
 
 
+class _RopeConfig(ctypes.Structure):
+    _fields_ = [("rot_dim", c_i32), ("scaling", c_i32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original", ctypes.c_double),
+                ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class _RopePlan(ctypes.Structure):
+    _fields_ = [("turns", c_p), ("rot_dim", c_i32), ("interleaved", c_i32), ("mscale", c_f32)]
+
+
+class _Rotate(ctypes.Structure):
+    _fields_ = [("n_tokens", c_i32), ("dtype", c_i32), ("head_dim", c_i32), ("n_q_heads", c_i32),
+                ("n_k_heads", c_i32), ("transpose", c_i32), ("positions", c_p), ("q", _Heads),
+                ("k", _Heads), ("q_out", _Heads), ("k_out", _Heads), ("plan", _RopePlan)]
+
+
 _lib = None
 EXPORTS = ("tt_workspace_bytes", "tt_workspace_bytes_for", "tt_align", "tt_transfer", "tt_verify", "tt_step",
            "tt_step_noalloc", "tt_status_string", "tt_last_cuda_error", "tt_version",
            "tt_vocab_index_bytes", "tt_vocab_index_build", "tt_encode_workspace_bytes",
            "tt_encode", "tt_consistency", "tt_dpos_hist", "tt_sharded_workspace_bytes",
            "tt_verify_sharded", "tt_logprobs", "tt_distill", "tt_distill_grad",
-           "tt_tree_workspace_bytes", "tt_tree_attn")
+           "tt_tree_workspace_bytes", "tt_tree_attn", "tt_rope_freqs", "tt_rope_turns", "tt_rope")
 TT_MAX_SHARDS = 8
 TT_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -179,6 +195,12 @@ def load(build_if_missing: bool = False):
     L.tt_tree_workspace_bytes.restype = ctypes.c_size_t
     L.tt_tree_attn.argtypes = [P(_Tree), c_p, ctypes.c_size_t, c_p, c_p, c_p, c_p]
     L.tt_tree_attn.restype = c_i32
+    L.tt_rope_freqs.argtypes = [P(_RopeConfig), P(ctypes.c_double)]
+    L.tt_rope_freqs.restype = c_i32
+    L.tt_rope_turns.argtypes = [P(ctypes.c_double), c_i32, P(c_u64)]
+    L.tt_rope_turns.restype = c_i32
+    L.tt_rope.argtypes = [P(_Rotate), c_p]
+    L.tt_rope.restype = c_i32
     _lib = L
     return L
 
@@ -1001,3 +1023,152 @@ def tt_tree_workspace(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off
               max_nodes)
     return torch.empty(max(int(load().tt_tree_workspace_bytes(ctypes.byref(T))), 256),
                        dtype=torch.uint8, device=q.device)
+
+
+# ------------------------------------------------------------- rotary positions
+
+def _gpu_of(*tensors) -> int:
+    """The GPU that a call's tensors (None passes) are all on: a kernel reads what its
+    pointers say, whatever device they were made for."""
+    at = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != at:
+            raise ValueError("a call's tensors must be on one device")
+    if at < 0:
+        raise ValueError("a call's tensors must be on a GPU")
+    return at
+
+
+_ROPE_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
+
+
+def rope_freqs(rot_dim: int, *, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0,
+               original: float = 0.0, low: float = 1.0, high: float = 32.0) -> torch.Tensor:
+    """Angles per position (fp64 radians on the host, [rot_dim / 2]) of a head's
+    pairs: base ** (-2 i / rot_dim), for a context that became ``factor`` times as long
+    "linear" (slowed by it), "base" (a larger base), or by "parts": pairs with fewer
+    than ``low`` turns within the ``original`` context are slowed, those with more than
+    ``high`` left, a ramp between."""
+    if scaling not in _ROPE_SCALINGS:
+        raise ValueError("scaling must be one of %s" % ", ".join(sorted(_ROPE_SCALINGS)))
+    f = (ctypes.c_double * max(int(rot_dim) // 2, 1))()
+    c = _RopeConfig(int(rot_dim), _ROPE_SCALINGS[scaling], float(base), float(factor),
+                    float(original), float(low), float(high))
+    _check("tt_rope_freqs", load().tt_rope_freqs(ctypes.byref(c), f))
+    return torch.tensor(list(f), dtype=torch.float64)
+
+
+def rope_turns(freqs, device="cuda") -> torch.Tensor:
+    """What tt_rope takes: angles per position (rope_freqs', or any radians) as turns
+    per position, fractions of 2^64 in an int64 tensor; made once and kept."""
+    host = torch.as_tensor(freqs, dtype=torch.float64).reshape(-1).tolist()
+    n = len(host)
+    turns = (c_u64 * max(n, 1))()
+    _check("tt_rope_turns", load().tt_rope_turns((ctypes.c_double * max(n, 1))(*host), n, turns))
+    return torch.from_numpy(np.frombuffer(turns, np.int64, n).copy()).to(device)
+
+
+def _heads3(t: torch.Tensor, name: str, dtype, D: int):
+    """_heads of [tokens, heads, head_dim]; the stride of a single token or head is any
+    number, and 0 here."""
+    p, token, head = _heads(t, name, dtype, D, 3)
+    N, H, _ = t.shape
+    return p, token if N > 1 else 0, head if H > 1 else 0
+
+
+_HEAD_DTYPES = {torch.float32: TT_F32, torch.bfloat16: TT_BF16, torch.float16: TT_F16}
+_ROTATE = struct.Struct("6iP" + 4 * "P2q" + "P2if4x")
+_NO_HEADS = (0, 0, 0)
+
+
+def tt_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
+            turns: torch.Tensor, *, interleaved: bool = False, mscale: float = 1.0,
+            transpose: bool = False, out=None, stream=None) -> dict:
+    """Rotary positions: the heads q [N, q heads, head_dim] and k [N, kv heads,
+    head_dim] (None: none) of N tokens, fp32, bf16 or fp16 with unit innermost stride,
+    rotated by positions int32 [N]. The first 2 * len(turns) elements of a head turn,
+    pairs (i, i + half) or, interleaved, (2 i, 2 i + 1), and are scaled by mscale;
+    transpose: the map that takes gradients of the results to gradients of the heads.
+    Returns q and k; tensors given in ``out`` are written in place, and may be the
+    inputs."""
+    if stream is not None:
+        with _on(stream):
+            return tt_rope(q, k, positions, turns, interleaved=interleaved, mscale=mscale,
+                           transpose=transpose, out=out)
+    at = _gpu_of(q, k, positions, turns, *(out.values() if out else ()))
+    if at != torch.cuda.current_device():
+        with torch.cuda.device(at):
+            return tt_rope(q, k, positions, turns, interleaved=interleaved, mscale=mscale,
+                           transpose=transpose, out=out)
+    dtype = q.dtype
+    code = _HEAD_DTYPES.get(dtype)
+    if code is None:
+        raise TypeError("heads must be float32, bfloat16 or float16")
+    if q.dim() != 3 or (k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0])):
+        raise ValueError("q and k must be [tokens, heads, head_dim] of the same tokens")
+    N, Hq, D = q.shape
+    o = dict(out) if out else {}
+    for name, x in (("q", q), ("k", k)):
+        if x is None:
+            if name in o:
+                raise ValueError("out holds keys, but none are given")
+        elif name not in o:
+            o[name] = torch.empty(x.shape, dtype=dtype, device=x.device)
+        elif o[name].shape != x.shape:
+            raise ValueError("out's %s must have its input's shape" % name)
+    n = turns.numel()
+    if positions.numel() != N:
+        raise ValueError("positions must be int32 [tokens]")
+    R = _Rotate()
+    try:
+        _ROTATE.pack_into(
+            R, 0, N, code, D, Hq, 0 if k is None else k.shape[1], int(bool(transpose)),
+            _given(positions, "positions", torch.int32, N), *_heads3(q, "q", dtype, D),
+            *(_NO_HEADS if k is None else _heads3(k, "k", dtype, D)),
+            *_heads3(o["q"], "q out", dtype, D),
+            *(_NO_HEADS if k is None else _heads3(o["k"], "k out", dtype, D)),
+            _given(turns, "turns", torch.int64, n), 2 * n, int(bool(interleaved)), float(mscale))
+    except (struct.error, OverflowError) as e:
+        raise ValueError("tt_rope: a size is beyond its type") from e
+    code = load().tt_rope(ctypes.byref(R), _stream(None))
+    if code:
+        _check("tt_rope", code)
+    return o
+
+
+def _dense(t: torch.Tensor) -> torch.Tensor:
+    """Heads as the library takes them (gradients come with any strides)."""
+    if t.stride(-1) == 1 and t.stride(0) % 8 == 0 and t.stride(1) % 8 == 0 and \
+            t.data_ptr() % 16 == 0:
+        return t
+    return t.clone(memory_format=torch.contiguous_format)
+
+
+class _Rope(torch.autograd.Function):
+    """A linear map, whose derivative is its transpose, of any order."""
+
+    @staticmethod
+    def forward(ctx, q, k, positions, turns, interleaved, mscale, transpose):
+        o = tt_rope(q, k, positions, turns, interleaved=interleaved, mscale=mscale,
+                    transpose=transpose)
+        ctx.save_for_backward(positions, turns)
+        ctx.args = interleaved, mscale, not transpose
+        ctx.set_materialize_grads(False)
+        return (o["q"], o["k"]) if k is not None else o["q"]
+
+    @staticmethod
+    def backward(ctx, *ups):
+        args = *ctx.saved_tensors, *ctx.args
+        got = [_dense(u) for u in ups if u is not None]
+        if len(got) == 2:
+            grads = _Rope.apply(*got, *args)
+        else:
+            grads = [None if u is None else _Rope.apply(got[0], None, *args) for u in ups]
+        return (*grads, *(None,) * (7 - len(grads)))
+
+
+def rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, turns: torch.Tensor,
+         *, interleaved: bool = False, mscale: float = 1.0):
+    """tt_rope as differentiable q and k (k None: q alone); gradients flow to the
+    heads."""
+    return _Rope.apply(q, k, positions, turns, bool(interleaved), float(mscale), False)

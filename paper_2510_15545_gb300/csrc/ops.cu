@@ -1,5 +1,6 @@
 // ops.cu -- the extern "C" entry points of the operators around a verification
 // step: argument checks (before anything touches the GPU) and launches.
+#include <algorithm>
 #include <climits>
 #include <cmath>
 #include <cstdint>
@@ -13,6 +14,7 @@ using namespace tt;
 
 // (log2(e) / T and what it scales stay within fp32)
 bool temp_ok(float t) { return t >= 1e-36f && t <= 1e36f; }
+constexpr double kTwoPi = 6.283185307179586476925;
 float log2e_over(float t) { return float(1.4426950408889634 / double(t)); }
 
 int elem_size(const tt_logits* L) { return L->dtype == TT_F32 ? 4 : 2; }
@@ -111,6 +113,35 @@ TreeArgs tree_args(const tt_tree* t) {
   return a;
 }
 
+bool rope_plan_ok(const tt_rope_plan& p, int head_dim) {
+  return p.turns && (reinterpret_cast<uintptr_t>(p.turns) & 7) == 0 && p.rot_dim >= 2 &&
+         p.rot_dim <= head_dim && p.rot_dim % 2 == 0 && (p.interleaved == 0 || p.interleaved == 1) &&
+         std::isfinite(p.mscale);
+}
+
+// Heads that are written: none shares memory with another.
+bool heads_apart(const tt_heads& h, int64_t tokens, int64_t heads, int D) {
+  if (!heads_ok(h)) return false;
+  if (heads == 1) return tokens == 1 || h.token_stride >= D;
+  if (tokens == 1) return h.head_stride >= D;
+  const int64_t in = std::min(h.token_stride, h.head_stride);
+  const int64_t out = std::max(h.token_stride, h.head_stride);
+  // (equal strides would put head h of token i on head h + 1 of token i - 1)
+  const int64_t inner = h.token_stride < h.head_stride ? tokens : heads;
+  return in >= D && (out - D) / in >= inner - 1 && in != out;
+}
+
+// Whether an output is its input, or lies in memory of its own as far as its pointer
+// and strides tell.
+bool out_ok(const tt_heads& in, const tt_heads& out) {
+  return in.data != out.data ||
+         (in.token_stride == out.token_stride && in.head_stride == out.head_stride);
+}
+
+RopeTensor rope_tensor(const tt_heads& h) {
+  return {static_cast<char*>(const_cast<void*>(h.data)), h.token_stride, h.head_stride};
+}
+
 }  // namespace
 
 extern "C" {
@@ -206,6 +237,82 @@ tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_by
   cudaError_t e = load_kernels();
   if (e == cudaSuccess)
     e = launch_tree(a, tree->dtype, static_cast<cudaStream_t>(stream), device_sms());
+  return e == cudaSuccess ? TT_OK : record_cuda_error(e);
+}
+
+tt_status tt_rope_freqs(const tt_rope_config* c, double* freqs) {
+  if (!c || !freqs || c->rot_dim < 2 || c->rot_dim > 256 || c->rot_dim % 2 != 0)
+    return TT_ERR_INVALID_ARG;
+  if (!(c->base > 0.0) || !std::isfinite(c->base)) return TT_ERR_INVALID_ARG;
+  if (c->scaling < TT_ROPE_PLAIN || c->scaling > TT_ROPE_PARTS) return TT_ERR_INVALID_ARG;
+  if (c->scaling != TT_ROPE_PLAIN && (!(c->factor > 0.0) || !std::isfinite(c->factor)))
+    return TT_ERR_INVALID_ARG;
+  if (c->scaling == TT_ROPE_BASE && c->rot_dim < 4) return TT_ERR_INVALID_ARG;
+  if (c->scaling == TT_ROPE_PARTS &&
+      (!(c->original > 0.0) || !std::isfinite(c->original) || !std::isfinite(c->low) ||
+       !std::isfinite(c->high) || !(c->low < c->high)))
+    return TT_ERR_INVALID_ARG;
+  const double d = c->rot_dim;
+  const double base =
+      c->scaling == TT_ROPE_BASE ? c->base * std::pow(c->factor, d / (d - 2.0)) : c->base;
+  for (int i = 0; i < c->rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / d);
+    if (c->scaling == TT_ROPE_LINEAR) f /= c->factor;
+    if (c->scaling == TT_ROPE_PARTS) {
+      const double r = c->original * f / kTwoPi;
+      const double g = std::min(1.0, std::max(0.0, (r - c->low) / (c->high - c->low)));
+      f *= (1.0 - g) / c->factor + g;
+    }
+    freqs[i] = f;
+  }
+  return TT_OK;
+}
+
+tt_status tt_rope_turns(const double* freqs, int32_t n, uint64_t* turns) {
+  if (n < 0 || (n > 0 && (!freqs || !turns))) return TT_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i)
+    if (!std::isfinite(freqs[i])) return TT_ERR_INVALID_ARG;
+  for (int i = 0; i < n; ++i) {
+    const double t = freqs[i] / kTwoPi, part = t - std::floor(t);
+    // (a tiny negative angle's part may round to a whole turn: none)
+    turns[i] = part < 1.0 ? uint64_t(std::ldexp(part, 64)) : 0;
+  }
+  return TT_OK;
+}
+
+tt_status tt_rope(const tt_rotate* r, void* stream) {
+  if (!r || r->n_tokens < 0 || r->dtype < TT_F32 || r->dtype > TT_F16 || r->head_dim < 8 ||
+      r->head_dim > 256 || r->head_dim % 8 != 0 || r->n_q_heads < 1 || r->n_k_heads < 0 ||
+      (r->transpose != 0 && r->transpose != 1))
+    return TT_ERR_INVALID_ARG;
+  if (!rope_plan_ok(r->plan, r->head_dim)) return TT_ERR_INVALID_ARG;
+  if (r->n_tokens == 0) return TT_OK;
+  if (!r->positions || !heads_ok(r->q) || !out_ok(r->q, r->q_out) ||
+      !heads_apart(r->q_out, r->n_tokens, r->n_q_heads, r->head_dim))
+    return TT_ERR_INVALID_ARG;
+  if (r->n_k_heads > 0 && (!heads_ok(r->k) || !out_ok(r->k, r->k_out) ||
+                           !heads_apart(r->k_out, r->n_tokens, r->n_k_heads, r->head_dim)))
+    return TT_ERR_INVALID_ARG;
+  if (int64_t(r->n_q_heads) + r->n_k_heads > 65535) return TT_ERR_UNSUPPORTED;
+  RopeArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.n_tokens = r->n_tokens;
+  a.D = r->head_dim;
+  a.Hq = r->n_q_heads;
+  a.Hk = r->n_k_heads;
+  a.rot_dim = r->plan.rot_dim;
+  a.interleaved = r->plan.interleaved;
+  a.back = r->transpose;
+  a.mscale = r->plan.mscale;
+  a.positions = r->positions;
+  a.turns = r->plan.turns;
+  a.q = rope_tensor(r->q);
+  a.k = rope_tensor(r->k);
+  a.q_out = rope_tensor(r->q_out);
+  a.k_out = rope_tensor(r->k_out);
+  cudaError_t e = load_kernels();
+  if (e == cudaSuccess)
+    e = launch_rope(a, r->dtype, static_cast<cudaStream_t>(stream), device_sms());
   return e == cudaSuccess ? TT_OK : record_cuda_error(e);
 }
 

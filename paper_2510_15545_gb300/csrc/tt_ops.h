@@ -1,7 +1,7 @@
 // tt_ops.h -- arguments and launchers of the operators around a verification
 // step: log probabilities of logits rows (logprob.cu), a student's loss against a
 // teacher's top log probabilities (distill.cu), attention of drafted tokens over a
-// paged cache (tree.cu).
+// paged cache (tree.cu), rotary positions (rope.cu).
 #pragma once
 
 #include <cstdint>
@@ -89,5 +89,20 @@ size_t tree_workspace_bytes(const TreeArgs& args, int sm_count);
 bool tree_fits(const TreeArgs& args, int sm_count);
 cudaError_t launch_tree(const TreeArgs& args, int dt, cudaStream_t stream, int sm_count);
 cudaError_t preload_tree();
+
+struct RopeTensor {
+  char* data;  // strides in elements
+  int64_t token, head;
+};
+struct RopeArgs {
+  int n_tokens, D, Hq, Hk, rot_dim, interleaved, back;
+  float mscale;
+  const int32_t* positions;
+  const uint64_t* turns;
+  RopeTensor q, k, q_out, k_out;
+};
+
+cudaError_t launch_rope(const RopeArgs& args, int dt, cudaStream_t stream, int sm_count);
+cudaError_t preload_rope();
 
 }  // namespace tt
