@@ -81,7 +81,8 @@ typedef enum {
 #define TT_MAX_DPOS_BINS 4096    /* most bins of tt_dpos_hist */
 #define TT_MAX_HISTORY 3072      /* longest repetition-penalty history per request */
 
-typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 /* heads only */ } tt_dtype;
+typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 /* heads only */,
+               TT_E4M3 = 3 /* caches only, with tt_scales */ } tt_dtype;
 
 /* A token byte-string table: token id v spells bytes[offsets[v] .. offsets[v+1]). */
 typedef struct {
@@ -579,6 +580,67 @@ typedef struct {
  * 2^-32 turns at any position, sines and cosines and products fp32, the result is
  * rounded once. Needs no workspace. */
 tt_status tt_rope(const tt_rotate* rotate, void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Paged caches: appending, and caches in 8 bits.
+ */
+
+#define TT_SCALE_SLOTS 16 /* slots of a page that share a scale in a head */
+
+/* Scales of a cache of e4m3 elements: an element of slot x of page p, head h stands for
+ * its value times 2^(data[p * page_stride + x / 16 * group_stride + h * head_stride]
+ * - 127); the byte 255 stands for NaN. Strides in bytes, >= 0. */
+typedef struct {
+  uint8_t* data; /* device */
+  int64_t page_stride;
+  int64_t group_stride;
+  int64_t head_stride;
+} tt_scales;
+
+/* Keys and values of new tokens for the caches of B requests. Request b owns the
+ * tokens token_off[b] .. token_off[b+1]-1 of k and v. Its first keep[b] (or all) go,
+ * in order, to slots cache_len[b], cache_len[b] + 1, ... of its cache, slots and pages
+ * as in tt_tree; with a path, the i-th is the token numbered path[token_off[b] + i]
+ * within the request (of an accepted branch of a tree). Pages that are written belong
+ * to one request. */
+typedef struct {
+  int32_t B;
+  int32_t n_tokens;    /* of k and v; token_off[B] */
+  int32_t max_new;     /* bound on a request's tokens, >= 1 */
+  int32_t dtype;       /* TT_BF16 or TT_F16: of k and v */
+  int32_t cache_dtype; /* dtype, or TT_E4M3 */
+  int32_t n_heads;
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t page_size;   /* slots of a page, a multiple of 16 */
+  const int32_t* token_off; /* device, [B+1] */
+  const int32_t* keep;      /* device, [B], or NULL: every token */
+  const int32_t* path;      /* device, [n_tokens], or NULL: in order */
+  const int32_t* positions; /* device, [n_tokens], of tokens for the rotation, or NULL: the
+                               number of the slot that a token goes to */
+  tt_heads k, v;
+  tt_pages k_cache, v_cache;  /* written; of TT_E4M3, strides multiples of 16 elements */
+  tt_scales k_scale, v_scale; /* read and written (TT_E4M3) */
+  int64_t n_pages;            /* pages at k_cache and v_cache */
+  const int32_t* page_table;  /* device */
+  int64_t table_stride;       /* elements between its rows */
+  const int32_t* cache_len;   /* device, [B] slots in use before */
+  int32_t max_len;            /* bound on the slots in use after; the table's rows hold them */
+} tt_append;
+
+/* Appends, keys rotated by `rope` on the way (as tt_rope would; NULL: as they are),
+ * rounded once. In TT_E4M3 a group of 16 slots of a head gets the least scale from 2^-126
+ * on with which the largest finite element of its new slots fits 448; where slots
+ * before cache_len are in use in the group it is at least theirs, and if it is larger
+ * those are rounded again. Elements that are not finite are NaN there; finite ones
+ * are held within 1.875 2^15 (fp16) or 1.875 2^127 (bf16). Slots past the appended ones
+ * stay as they are. new_len [B] (optional; not cache_len's own memory) is the slots in
+ * use after. status [B]: BAD_OFFSETS (also: keep[b] beyond the request's tokens) and
+ * TOO_LONG (more tokens than max_new, a length that is negative or would pass
+ * max_len) append nothing; ID_OUT_OF_RANGE reports an entry of the path or a page out
+ * of range, whose tokens are left out, and new_len stays as it was in all these
+ * cases. Needs no workspace. */
+tt_status tt_cache_append(const tt_append* append, const tt_rope_plan* rope, int32_t* new_len,
+                          int32_t* status, void* stream);
 
 /* Static text for a tt_status. */
 const char* tt_status_string(tt_status s);

@@ -9,14 +9,14 @@ log probabilities. The names below are the library's entry points; the library
 is loaded on first use and a missing build raises."""
 from .binding import (AlignCall, Batch, Params, StepCall, TTError, VocabTable, device_inputs,
                      distill_loss, load, rope, rope_freqs, rope_turns, step_outputs, tt_align,
-                     tt_consistency, tt_distill, tt_distill_grad, tt_dpos_hist, tt_encode,
+                     tt_cache_append, tt_consistency, tt_distill, tt_distill_grad, tt_dpos_hist, tt_encode,
                      tt_encode_workspace_bytes, tt_logprobs, tt_rope, tt_status_string, tt_step,
                      tt_step_noalloc, tt_transfer, tt_tree_attn, tt_tree_workspace, tt_verify,
                      tt_verify_sharded, tt_version, tt_workspace_bytes, vocab_index, workspace)
 
 __all__ = ["AlignCall", "Batch", "Params", "StepCall", "TTError", "VocabTable", "device_inputs",
            "distill_loss", "load", "rope", "rope_freqs", "rope_turns", "step_outputs", "tt_align",
-           "tt_consistency", "tt_distill", "tt_distill_grad", "tt_dpos_hist", "tt_encode",
+           "tt_cache_append", "tt_consistency", "tt_distill", "tt_distill_grad", "tt_dpos_hist", "tt_encode",
            "tt_encode_workspace_bytes", "tt_logprobs", "tt_rope", "tt_status_string", "tt_step",
            "tt_step_noalloc", "tt_transfer", "tt_tree_attn", "tt_tree_workspace", "tt_verify",
            "tt_verify_sharded", "tt_version", "tt_workspace_bytes", "vocab_index", "workspace"]

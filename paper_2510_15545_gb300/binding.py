@@ -24,7 +24,8 @@ TT_REQ_ID_OUT_OF_RANGE, TT_REQ_TOO_LONG, TT_REQ_EMPTY, TT_REQ_BAD_OFFSETS, TT_RE
     1, 2, 4, 8, 16)
 TT_REQ_NO_MATCH, TT_REQ_INCONSISTENT = 128, 256
 TT_MAX_ENCODE_BYTES, TT_MAX_DPOS_BINS = 2048, 4096
-TT_F32, TT_BF16, TT_F16 = 0, 1, 2
+TT_F32, TT_BF16, TT_F16, TT_E4M3 = 0, 1, 2, 3
+TT_SCALE_SLOTS = 16
 TT_MAX_TOP_K, TT_MAX_DISTILL_K, TT_MAX_TREE = 32, 128, 512
 TT_MAX_K, TT_MAX_M, TT_MAX_TOKEN_BYTES = 256, 512, 256
 
@@ -113,13 +114,29 @@ class _Rotate(ctypes.Structure):
                 ("k", _Heads), ("q_out", _Heads), ("k_out", _Heads), ("plan", _RopePlan)]
 
 
+class _Scales(ctypes.Structure):
+    _fields_ = [("data", c_p), ("page_stride", c_i64), ("group_stride", c_i64),
+                ("head_stride", c_i64)]
+
+
+class _Append(ctypes.Structure):
+    _fields_ = [("B", c_i32), ("n_tokens", c_i32), ("max_new", c_i32), ("dtype", c_i32),
+                ("cache_dtype", c_i32), ("n_heads", c_i32), ("head_dim", c_i32),
+                ("page_size", c_i32), ("token_off", c_p), ("keep", c_p), ("path", c_p),
+                ("positions", c_p), ("k", _Heads), ("v", _Heads), ("k_cache", _Pages),
+                ("v_cache", _Pages), ("k_scale", _Scales), ("v_scale", _Scales),
+                ("n_pages", c_i64), ("page_table", c_p), ("table_stride", c_i64),
+                ("cache_len", c_p), ("max_len", c_i32)]
+
+
 _lib = None
 EXPORTS = ("tt_workspace_bytes", "tt_workspace_bytes_for", "tt_align", "tt_transfer", "tt_verify", "tt_step",
            "tt_step_noalloc", "tt_status_string", "tt_last_cuda_error", "tt_version",
            "tt_vocab_index_bytes", "tt_vocab_index_build", "tt_encode_workspace_bytes",
            "tt_encode", "tt_consistency", "tt_dpos_hist", "tt_sharded_workspace_bytes",
            "tt_verify_sharded", "tt_logprobs", "tt_distill", "tt_distill_grad",
-           "tt_tree_workspace_bytes", "tt_tree_attn", "tt_rope_freqs", "tt_rope_turns", "tt_rope")
+           "tt_tree_workspace_bytes", "tt_tree_attn", "tt_rope_freqs", "tt_rope_turns", "tt_rope",
+           "tt_cache_append")
 TT_MAX_SHARDS = 8
 TT_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -201,6 +218,8 @@ def load(build_if_missing: bool = False):
     L.tt_rope_turns.restype = c_i32
     L.tt_rope.argtypes = [P(_Rotate), c_p]
     L.tt_rope.restype = c_i32
+    L.tt_cache_append.argtypes = [P(_Append), P(_RopePlan), c_p, c_p, c_p]
+    L.tt_cache_append.restype = c_i32
     _lib = L
     return L
 
@@ -927,6 +946,25 @@ def _heads(t: torch.Tensor, name: str, dtype, D: int, dims: int):
     return t.data_ptr(), *stride[:-1]
 
 
+def _table(page_table: torch.Tensor, B: int, page_size: int, max_len: Optional[int]):
+    """Distance of a page table's rows, and the bound on a request's slots."""
+    table = page_table.shape
+    if len(table) != 2 or page_table.dtype is not torch.int32 or table[0] != B:
+        raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
+    row, col = page_table.stride()
+    if col != 1 and table[1] > 1:
+        raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
+    room = table[1] * page_size
+    max_len = min(room, 1 << 30) if max_len is None else int(max_len)
+    if max_len > room:
+        raise ValueError("max_len is more than the page table's rows hold")
+    if B < 2:  # (the stride of a single row is any number)
+        row = max(row, table[1])
+    elif row < table[1] and max_len > 0 and row < (max_len - 1) // page_size + 1:
+        raise ValueError("page_table's rows share memory; give its .contiguous()")
+    return row, max_len
+
+
 def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
           max_nodes) -> _Tree:
     dtype = q.dtype
@@ -937,20 +975,7 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
     shape, cache = k.shape, k_cache.shape
     if shape != v.shape or shape[0] != N or cache != v_cache.shape or cache[2] != shape[1]:
         raise ValueError("keys and values must be of the same tokens, pages and heads")
-    table = page_table.shape
-    if len(table) != 2 or page_table.dtype is not torch.int32 or table[0] != B:
-        raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
-    row, col = page_table.stride()
-    if col != 1 and table[1] > 1:
-        raise ValueError("page_table must be int32 [requests, pages] with unit column stride")
-    room = table[1] * cache[1]
-    max_len = min(room, 1 << 30) if max_len is None else int(max_len)
-    if max_len > room:
-        raise ValueError("max_len is more than the page table's rows hold")
-    if B < 2:  # (the stride of a single row is any number)
-        row = max(row, table[1])
-    elif row < table[1] and max_len > 0 and row < (max_len - 1) // cache[1] + 1:
-        raise ValueError("page_table's rows share memory; give its .contiguous()")
+    row, max_len = _table(page_table, B, cache[1], max_len)
     T = _Tree()
     try:
         _TREE.pack_into(
@@ -1172,3 +1197,96 @@ def rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, tu
     """tt_rope as differentiable q and k (k None: q alone); gradients flow to the
     heads."""
     return _Rope.apply(q, k, positions, turns, bool(interleaved), float(mscale), False)
+
+
+# ------------------------------------------------------ appending to paged caches
+
+_APPEND = struct.Struct("8i4P" + 2 * "P2q" + 4 * "P3q" + "qPqPi4x")
+_NO_SCALES = (0, 0, 0, 0)
+
+
+def _scales(t: Optional[torch.Tensor], name: str, cache):
+    """Pointer and strides of the scales of a cache's e4m3 elements."""
+    want = (cache[0], cache[1] // TT_SCALE_SLOTS, cache[2])
+    if t is None or t.dtype not in (torch.float8_e8m0fnu, torch.uint8) or tuple(t.shape) != want:
+        raise ValueError("%s must be float8_e8m0fnu (or its bytes) [pages, page_size / 16, heads]"
+                         % name)
+    return t.data_ptr(), *t.stride()
+
+
+def tt_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,
+                    page_table: torch.Tensor, cache_len: torch.Tensor, token_off: torch.Tensor, *,
+                    k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                    keep: Optional[torch.Tensor] = None, path: Optional[torch.Tensor] = None,
+                    turns: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                    interleaved: bool = False, mscale: float = 1.0, max_len: Optional[int] = None,
+                    max_new: Optional[int] = None, out=None, stream=None) -> dict:
+    """Appends keys and values k, v [N, kv heads, head_dim] of B requests (tokens
+    token_off[b] .. token_off[b+1]-1) to their paged caches k_cache, v_cache [pages,
+    page_size, kv heads, head_dim] behind the cache_len[b] slots in use: of the tokens'
+    type, or float8_e4m3fn with k_scale and v_scale float8_e8m0fnu [pages,
+    page_size / 16, kv heads]. keep int32 [B]: only a request's first so many; path
+    int32 [N]: the i-th one appended is the token of that number within the request
+    (an accepted branch). turns (rope_turns): keys are rotated on the way, by positions
+    int32 [N] or by their slots' numbers. Returns new_len and status int32 [B]; tensors
+    given in ``out`` are written in place. max_len bounds the slots in use after, max_new
+    the tokens of a request (default: what the table and N allow)."""
+    if stream is not None:
+        with _on(stream):
+            return tt_cache_append(k, v, k_cache, v_cache, page_table, cache_len, token_off,
+                                   k_scale=k_scale, v_scale=v_scale, keep=keep, path=path,
+                                   turns=turns, positions=positions, interleaved=interleaved,
+                                   mscale=mscale, max_len=max_len, max_new=max_new, out=out)
+    at = _gpu_of(k, v, k_cache, v_cache, page_table, cache_len, token_off, k_scale, v_scale, keep,
+                 path, turns, positions, *(out.values() if out else ()))
+    if at != torch.cuda.current_device():
+        with torch.cuda.device(at):
+            return tt_cache_append(k, v, k_cache, v_cache, page_table, cache_len, token_off,
+                                   k_scale=k_scale, v_scale=v_scale, keep=keep, path=path,
+                                   turns=turns, positions=positions, interleaved=interleaved,
+                                   mscale=mscale, max_len=max_len, max_new=max_new, out=out)
+    dtype, cache, held = k.dtype, k_cache.shape, k_cache.dtype
+    code = _TREE_DTYPES.get(dtype)
+    if code is None:
+        raise TypeError("keys must be bfloat16 or float16")
+    if k.dim() != 3 or k.shape != v.shape or len(cache) != 4 or cache != v_cache.shape or \
+            cache[2] != k.shape[1] or v_cache.dtype is not held:
+        raise ValueError("keys and values must be of the same tokens, pages and heads")
+    (N, H, D), B, i32 = k.shape, cache_len.numel(), torch.int32
+    in8 = held is torch.float8_e4m3fn
+    if not in8 and (k_scale is not None or v_scale is not None):
+        raise ValueError("scales belong to caches of float8_e4m3fn")
+    row, max_len = _table(page_table, B, cache[1], max_len)
+    n = None if turns is None else turns.numel()
+    if n is None and positions is not None:
+        raise ValueError("positions are for a rotation, which turns give")
+    A = _Append()
+    try:
+        _APPEND.pack_into(
+            A, 0, B, N, max(N, 1) if max_new is None else int(max_new), code,
+            TT_E4M3 if in8 else code, H, D, cache[1],
+            _given(token_off, "token_off", i32, B + 1), _given(keep, "keep", i32, B) or 0,
+            _given(path, "path", i32, N) or 0, _given(positions, "positions", i32, N) or 0,
+            *_heads3(k, "k", dtype, D), *_heads3(v, "v", dtype, D),
+            *_heads(k_cache, "k_cache", held if in8 else dtype, D, 4),
+            *_heads(v_cache, "v_cache", held if in8 else dtype, D, 4),
+            *(_scales(k_scale, "k_scale", cache) if in8 else _NO_SCALES),
+            *(_scales(v_scale, "v_scale", cache) if in8 else _NO_SCALES),
+            cache[0], page_table.data_ptr(), row, _given(cache_len, "cache_len", i32, B), max_len)
+        plan = None if n is None else _RopePlan(_given(turns, "turns", torch.int64, n), 2 * n,
+                                                int(bool(interleaved)), float(mscale))
+    except (struct.error, OverflowError) as e:
+        raise ValueError("tt_cache_append: a size is beyond its type") from e
+    if out:
+        o = dict(out)
+        _need(o, "new_len", B, i32, k.device)
+        _need(o, "status", B, i32, k.device)
+    else:
+        buf = cache_len.new_empty(2 * B)
+        o = {"new_len": buf.as_strided((B,), (1,), 0), "status": buf.as_strided((B,), (1,), B)}
+    code = load().tt_cache_append(ctypes.byref(A), None if plan is None else ctypes.byref(plan),
+                                  _given(o["new_len"], "new_len", i32, B),
+                                  _given(o["status"], "status", i32, B), _stream(None))
+    if code:
+        _check("tt_cache_append", code)
+    return o

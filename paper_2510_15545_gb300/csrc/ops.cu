@@ -138,8 +138,22 @@ bool out_ok(const tt_heads& in, const tt_heads& out) {
          (in.token_stride == out.token_stride && in.head_stride == out.head_stride);
 }
 
+bool scales_ok(const tt_scales& s) {
+  return s.data && s.page_stride >= 0 && s.group_stride >= 0 && s.head_stride >= 0;
+}
+// Pages of e4m3 elements.
+bool pages8_ok(const tt_pages& p, const tt_scales& s) {
+  return pages_ok(p) && p.page_stride % 16 == 0 && p.slot_stride % 16 == 0 &&
+         p.head_stride % 16 == 0 && scales_ok(s);
+}
+
 RopeTensor rope_tensor(const tt_heads& h) {
   return {static_cast<char*>(const_cast<void*>(h.data)), h.token_stride, h.head_stride};
+}
+
+AppendCache append_cache(const tt_pages& p, const tt_scales& s) {
+  return {static_cast<char*>(const_cast<void*>(p.data)), p.page_stride, p.slot_stride,
+          p.head_stride, s.data, s.page_stride, s.group_stride, s.head_stride};
 }
 
 }  // namespace
@@ -313,6 +327,62 @@ tt_status tt_rope(const tt_rotate* r, void* stream) {
   cudaError_t e = load_kernels();
   if (e == cudaSuccess)
     e = launch_rope(a, r->dtype, static_cast<cudaStream_t>(stream), device_sms());
+  return e == cudaSuccess ? TT_OK : record_cuda_error(e);
+}
+
+tt_status tt_cache_append(const tt_append* p, const tt_rope_plan* rope, int32_t* new_len,
+                          int32_t* status, void* stream) {
+  if (!p || p->B < 0 || p->n_tokens < 0 || p->max_new < 1 ||
+      (p->dtype != TT_BF16 && p->dtype != TT_F16) ||
+      (p->cache_dtype != p->dtype && p->cache_dtype != TT_E4M3) || p->n_heads < 1 ||
+      (p->head_dim != 64 && p->head_dim != 128) || p->page_size < 16 || p->page_size % 16 != 0 ||
+      p->page_size > 1 << 20 || p->max_len < 0 || p->max_len > 1 << 30)
+    return TT_ERR_INVALID_ARG;
+  if (rope && !rope_plan_ok(*rope, p->head_dim)) return TT_ERR_INVALID_ARG;
+  if (p->B == 0) return TT_OK;
+  if (!p->token_off || !p->cache_len || !status || new_len == p->cache_len) return TT_ERR_INVALID_ARG;
+  if (p->n_tokens > 0 && (!heads_ok(p->k) || !heads_ok(p->v))) return TT_ERR_INVALID_ARG;
+  const bool held8 = p->cache_dtype == TT_E4M3;
+  const int64_t pages = (int64_t(p->max_len) + p->page_size - 1) / p->page_size;
+  if (p->max_len > 0) {
+    if (held8 ? !pages8_ok(p->k_cache, p->k_scale) || !pages8_ok(p->v_cache, p->v_scale)
+              : !pages_ok(p->k_cache) || !pages_ok(p->v_cache))
+      return TT_ERR_INVALID_ARG;
+    if (p->n_pages < 1 || p->n_pages > INT32_MAX || !p->page_table || p->table_stride < pages)
+      return TT_ERR_INVALID_ARG;
+  }
+  AppendArgs a;
+  std::memset(&a, 0, sizeof a);
+  a.B = p->B;
+  a.n_tokens = p->n_tokens;
+  a.max_new = p->max_new;
+  a.H = p->n_heads;
+  a.D = p->head_dim;
+  a.page_size = p->page_size;
+  a.max_len = p->max_len;
+  a.token_off = p->token_off;
+  a.keep = p->keep;
+  a.path = p->path;
+  a.positions = p->positions;
+  a.cache_len = p->cache_len;
+  a.page_table = p->page_table;
+  a.n_pages = p->n_pages;
+  a.table_stride = p->table_stride;
+  a.k = rope_tensor(p->k);
+  a.v = rope_tensor(p->v);
+  a.k_cache = append_cache(p->k_cache, p->k_scale);
+  a.v_cache = append_cache(p->v_cache, p->v_scale);
+  if (rope) {
+    a.rot_dim = rope->rot_dim;
+    a.interleaved = rope->interleaved;
+    a.mscale = rope->mscale;
+    a.turns = rope->turns;
+  }
+  a.new_len = new_len;
+  a.status = status;
+  cudaError_t e = load_kernels();
+  if (e == cudaSuccess)
+    e = launch_append(a, p->dtype, held8, static_cast<cudaStream_t>(stream), device_sms());
   return e == cudaSuccess ? TT_OK : record_cuda_error(e);
 }
 

@@ -1,7 +1,8 @@
 // tt_ops.h -- arguments and launchers of the operators around a verification
 // step: log probabilities of logits rows (logprob.cu), a student's loss against a
 // teacher's top log probabilities (distill.cu), attention of drafted tokens over a
-// paged cache (tree.cu), rotary positions (rope.cu).
+// paged cache (tree.cu), rotary positions (rope.cu), appending to
+// paged caches (append.cu).
 #pragma once
 
 #include <cstdint>
@@ -104,5 +105,27 @@ struct RopeArgs {
 
 cudaError_t launch_rope(const RopeArgs& args, int dt, cudaStream_t stream, int sm_count);
 cudaError_t preload_rope();
+
+struct AppendCache {
+  char* data;  // strides in elements
+  int64_t page, slot, head;
+  uint8_t* scale;  // strides in bytes
+  int64_t scale_page, scale_group, scale_head;
+};
+struct AppendArgs {
+  int B, n_tokens, max_new, H, D, page_size, max_len;
+  const int32_t *token_off, *keep, *path, *positions, *cache_len, *page_table;
+  int64_t n_pages, table_stride;
+  RopeTensor k, v;
+  AppendCache k_cache, v_cache;
+  int rot_dim, interleaved;  // rot_dim 0: no rotation
+  float mscale;
+  const uint64_t* turns;
+  int32_t *new_len, *status;
+};
+
+cudaError_t launch_append(const AppendArgs& args, int dt, bool held8, cudaStream_t stream,
+                          int sm_count);
+cudaError_t preload_append();
 
 }  // namespace tt
