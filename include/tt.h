@@ -642,6 +642,19 @@ typedef struct {
 tt_status tt_cache_append(const tt_append* append, const tt_rope_plan* rope, int32_t* new_len,
                           int32_t* status, void* stream);
 
+/* Scratch bytes of tt_tree_attn8 for these sizes (0: none needed, or invalid sizes). */
+size_t tt_tree8_workspace_bytes(const tt_tree* tree);
+
+/* tt_tree_attn over caches in 8 bits: tree's k_cache and v_cache hold e4m3 elements
+ * (strides multiples of 16) with the given scales, as tt_cache_append leaves them;
+ * q, k, v and the output are of tree's dtype. Keys count as they are; values are
+ * rounded to that type, which holds them exactly within its range (fp16: multiples of
+ * 2^-24 below 65,520). A slot whose scale is NaN makes its rows NaN. Everything else is as for
+ * tt_tree_attn. */
+tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_scales* v_scale,
+                        void* workspace, size_t workspace_bytes, void* out, float* lse,
+                        int32_t* status, void* stream);
+
 /* Static text for a tt_status. */
 const char* tt_status_string(tt_status s);
 

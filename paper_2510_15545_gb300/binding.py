@@ -136,7 +136,7 @@ EXPORTS = ("tt_workspace_bytes", "tt_workspace_bytes_for", "tt_align", "tt_trans
            "tt_encode", "tt_consistency", "tt_dpos_hist", "tt_sharded_workspace_bytes",
            "tt_verify_sharded", "tt_logprobs", "tt_distill", "tt_distill_grad",
            "tt_tree_workspace_bytes", "tt_tree_attn", "tt_rope_freqs", "tt_rope_turns", "tt_rope",
-           "tt_cache_append")
+           "tt_cache_append", "tt_tree8_workspace_bytes", "tt_tree_attn8")
 TT_MAX_SHARDS = 8
 TT_NOALLOC_SCRATCH_BYTES = 16 << 20
 
@@ -220,6 +220,11 @@ def load(build_if_missing: bool = False):
     L.tt_rope.restype = c_i32
     L.tt_cache_append.argtypes = [P(_Append), P(_RopePlan), c_p, c_p, c_p]
     L.tt_cache_append.restype = c_i32
+    L.tt_tree8_workspace_bytes.argtypes = [P(_Tree)]
+    L.tt_tree8_workspace_bytes.restype = ctypes.c_size_t
+    L.tt_tree_attn8.argtypes = [P(_Tree), P(_Scales), P(_Scales), c_p, ctypes.c_size_t, c_p, c_p,
+                                c_p, c_p]
+    L.tt_tree_attn8.restype = c_i32
     _lib = L
     return L
 
@@ -976,6 +981,7 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
     if shape != v.shape or shape[0] != N or cache != v_cache.shape or cache[2] != shape[1]:
         raise ValueError("keys and values must be of the same tokens, pages and heads")
     row, max_len = _table(page_table, B, cache[1], max_len)
+    held = k_cache.dtype if k_cache.dtype is torch.float8_e4m3fn else dtype
     T = _Tree()
     try:
         _TREE.pack_into(
@@ -983,7 +989,7 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
             Hq, shape[1], D, cache[1], _given(tree_off, "tree_off", torch.int32, B + 1) or 0,
             _given(parents, "parents", torch.int32, N) or 0, *_heads(q, "q", dtype, D, 3),
             *_heads(k, "k", dtype, D, 3), *_heads(v, "v", dtype, D, 3),
-            *_heads(k_cache, "k_cache", dtype, D, 4), *_heads(v_cache, "v_cache", dtype, D, 4),
+            *_heads(k_cache, "k_cache", held, D, 4), *_heads(v_cache, "v_cache", held, D, 4),
             cache[0], page_table.data_ptr(), row,
             _given(cache_len, "cache_len", torch.int32, B), max_len,
             D ** -0.5 if scale is None else float(scale))
@@ -992,12 +998,32 @@ def _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, s
     return T
 
 
+def _scales(t: Optional[torch.Tensor], name: str, cache):
+    """Pointer and strides of the scales of a cache's e4m3 elements."""
+    want = (cache[0], cache[1] // TT_SCALE_SLOTS, cache[2])
+    if t is None or t.dtype not in (torch.float8_e8m0fnu, torch.uint8) or tuple(t.shape) != want:
+        raise ValueError("%s must be float8_e8m0fnu (or its bytes) [pages, page_size / 16, heads]"
+                         % name)
+    return t.data_ptr(), *t.stride()
+
+
+def _cache_scales(k_cache: torch.Tensor, k_scale, v_scale):
+    """The scales' descriptors of caches in 8 bits, None for others."""
+    if k_cache.dtype is not torch.float8_e4m3fn:
+        if k_scale is not None or v_scale is not None:
+            raise ValueError("scales belong to caches of float8_e4m3fn")
+        return None
+    return (ctypes.byref(_Scales(*_scales(k_scale, "k_scale", k_cache.shape))),
+            ctypes.byref(_Scales(*_scales(v_scale, "v_scale", k_cache.shape))))
+
+
 def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor,
                  v_cache: torch.Tensor, page_table: torch.Tensor, cache_len: torch.Tensor,
                  tree_off: torch.Tensor, parents: Optional[torch.Tensor] = None, *,
                  scale: Optional[float] = None, max_len: Optional[int] = None,
                  max_nodes: Optional[int] = None, ws: Optional[torch.Tensor] = None, out=None,
-                 stream=None) -> dict:
+                 stream=None, k_scale: Optional[torch.Tensor] = None,
+                 v_scale: Optional[torch.Tensor] = None) -> dict:
     """Attention of the drafted tokens q [N, q heads, head_dim] of B requests
     (nodes tree_off[b] .. tree_off[b+1]-1, k and v [N, kv heads, head_dim] their own
     keys and values, parents [N] numbered within the request, None for chains) over
@@ -1005,21 +1031,33 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
     head_dim] (any strides with unit innermost), page_table int32 [B, pages per
     request], cache_len int32 [B]. Returns out [N, q heads, head_dim], lse
     [N, q heads] and status [B]; tensors given in ``out`` are written in place.
-    max_len and max_nodes bound the lengths and the nodes of a request and size the
+    Caches in 8 bits are float8_e4m3fn with k_scale and v_scale float8_e8m0fnu [pages,
+    page_size / 16, kv heads], as tt_cache_append leaves them. max_len and max_nodes bound the lengths and the nodes of a request and size the
     launch (default: what the table and N allow)."""
     if stream is not None:
         with _on(stream):
             return tt_tree_attn(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents,
-                                scale=scale, max_len=max_len, max_nodes=max_nodes, ws=ws, out=out)
+                                scale=scale, max_len=max_len, max_nodes=max_nodes, ws=ws, out=out,
+                                k_scale=k_scale, v_scale=v_scale)
     T = _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, scale, max_len,
               max_nodes)
+    scales = _cache_scales(k_cache, k_scale, v_scale)
+    if scales:
+        at = _gpu_of(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, k_scale,
+                     v_scale, ws, *(out.values() if out else ()))
+        if at != torch.cuda.current_device():
+            with torch.cuda.device(at):
+                return tt_tree_attn(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off,
+                                    parents, scale=scale, max_len=max_len, max_nodes=max_nodes,
+                                    ws=ws, out=out, k_scale=k_scale, v_scale=v_scale)
     L = load()
     N, Hq, D = q.shape
     rows, B = N * Hq, T.B
     if ws is None:
         # (an allocation of its own, gone when the call returns: in one with lse, whoever
         # keeps that would keep it too)
-        n = int(L.tt_tree_workspace_bytes(ctypes.byref(T)))
+        size = L.tt_tree8_workspace_bytes if scales else L.tt_tree_workspace_bytes
+        n = int(size(ctypes.byref(T)))
         ws = q.new_empty(n, dtype=torch.uint8)
     ws_p, n = ws.data_ptr(), ws.numel()
     if out:
@@ -1033,11 +1071,15 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
              "status": buf.view(torch.int32).as_strided((B,), (1,), rows)}
     if "out" not in o:
         o["out"] = q.new_empty((N, Hq, D))
-    code = L.tt_tree_attn(ctypes.byref(T), ws_p, n, _given(o["out"], "out", q.dtype, rows * D),
-                          _given(o["lse"], "lse", torch.float32, rows),
-                          _given(o["status"], "status", torch.int32, B), _stream(None))
+    args = (ws_p, n, _given(o["out"], "out", q.dtype, rows * D),
+            _given(o["lse"], "lse", torch.float32, rows),
+            _given(o["status"], "status", torch.int32, B), _stream(None))
+    if scales:
+        code = L.tt_tree_attn8(ctypes.byref(T), *scales, *args)
+    else:
+        code = L.tt_tree_attn(ctypes.byref(T), *args)
     if code:
-        _check("tt_tree_attn", code)
+        _check("tt_tree_attn8" if scales else "tt_tree_attn", code)
     return o
 
 
@@ -1046,8 +1088,9 @@ def tt_tree_workspace(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off
     """Scratch that tt_tree_attn calls of these sizes can share, one at a time."""
     T = _tree(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents, None, max_len,
               max_nodes)
-    return torch.empty(max(int(load().tt_tree_workspace_bytes(ctypes.byref(T))), 256),
-                       dtype=torch.uint8, device=q.device)
+    in8 = k_cache.dtype is torch.float8_e4m3fn
+    size = load().tt_tree8_workspace_bytes if in8 else load().tt_tree_workspace_bytes
+    return torch.empty(max(int(size(ctypes.byref(T))), 256), dtype=torch.uint8, device=q.device)
 
 
 # ------------------------------------------------------------- rotary positions
@@ -1203,15 +1246,6 @@ def rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, tu
 
 _APPEND = struct.Struct("8i4P" + 2 * "P2q" + 4 * "P3q" + "qPqPi4x")
 _NO_SCALES = (0, 0, 0, 0)
-
-
-def _scales(t: Optional[torch.Tensor], name: str, cache):
-    """Pointer and strides of the scales of a cache's e4m3 elements."""
-    want = (cache[0], cache[1] // TT_SCALE_SLOTS, cache[2])
-    if t is None or t.dtype not in (torch.float8_e8m0fnu, torch.uint8) or tuple(t.shape) != want:
-        raise ValueError("%s must be float8_e8m0fnu (or its bytes) [pages, page_size / 16, heads]"
-                         % name)
-    return t.data_ptr(), *t.stride()
 
 
 def tt_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor,

@@ -48,6 +48,7 @@ cudaError_t ensure_loaded() {
   if ((e = preload_tree()) != cudaSuccess) return e;
   if ((e = preload_rope()) != cudaSuccess) return e;
   if ((e = preload_append()) != cudaSuccess) return e;
+  if ((e = preload_tree8()) != cudaSuccess) return e;
   if (dev >= 0 && dev < 64) done[dev].store(true, std::memory_order_release);
   return cudaSuccess;
 }

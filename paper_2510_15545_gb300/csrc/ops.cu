@@ -147,6 +147,27 @@ bool pages8_ok(const tt_pages& p, const tt_scales& s) {
          p.head_stride % 16 == 0 && scales_ok(s);
 }
 
+// What both tree calls check beyond the sizes, but for their caches.
+tt_status tree_ok(const tt_tree* tree, const void* out, const int32_t* status) {
+  if (tree->dtype != TT_BF16 && tree->dtype != TT_F16) return TT_ERR_INVALID_ARG;
+  if (!(tree->scale > 0.f) || !std::isfinite(tree->scale)) return TT_ERR_INVALID_ARG;
+  if (tree->B == 0) return TT_OK;
+  if (!tree->tree_off || !tree->cache_len || !status) return TT_ERR_INVALID_ARG;
+  if (tree->n_nodes > 0 && (!heads_ok(tree->q) || !heads_ok(tree->k) || !heads_ok(tree->v) ||
+                            !aligned16(out)))
+    return TT_ERR_INVALID_ARG;
+  const int64_t pages = (int64_t(tree->max_len) + tree->page_size - 1) / tree->page_size;
+  if (tree->max_len > 0 && (tree->n_pages < 1 || tree->n_pages > INT32_MAX || !tree->page_table ||
+                            tree->table_stride < pages))
+    return TT_ERR_INVALID_ARG;
+  return TT_OK;
+}
+
+bool workspace_ok(const void* workspace, size_t bytes, size_t need) {
+  return need == 0 || (workspace && bytes >= need &&
+                       (reinterpret_cast<uintptr_t>(workspace) & 255) == 0);
+}
+
 RopeTensor rope_tensor(const tt_heads& h) {
   return {static_cast<char*>(const_cast<void*>(h.data)), h.token_stride, h.head_stride};
 }
@@ -226,22 +247,12 @@ size_t tt_tree_workspace_bytes(const tt_tree* tree) {
 tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_bytes, void* out,
                        float* lse, int32_t* status, void* stream) {
   if (!tree_sizes_ok(tree)) return TT_ERR_INVALID_ARG;
-  if (tree->dtype != TT_BF16 && tree->dtype != TT_F16) return TT_ERR_INVALID_ARG;
-  if (!(tree->scale > 0.f) || !std::isfinite(tree->scale)) return TT_ERR_INVALID_ARG;
-  if (tree->B == 0) return TT_OK;
-  if (!tree->tree_off || !tree->cache_len || !status) return TT_ERR_INVALID_ARG;
-  if (tree->n_nodes > 0 && (!heads_ok(tree->q) || !heads_ok(tree->k) || !heads_ok(tree->v) ||
-                            !aligned16(out)))
-    return TT_ERR_INVALID_ARG;
-  const int64_t pages = (int64_t(tree->max_len) + tree->page_size - 1) / tree->page_size;
-  if (tree->max_len > 0 &&
-      (!pages_ok(tree->k_cache) || !pages_ok(tree->v_cache) || tree->n_pages < 1 ||
-       tree->n_pages > INT32_MAX || !tree->page_table || tree->table_stride < pages))
+  const tt_status st = tree_ok(tree, out, status);
+  if (st != TT_OK || tree->B == 0) return st;
+  if (tree->max_len > 0 && (!pages_ok(tree->k_cache) || !pages_ok(tree->v_cache)))
     return TT_ERR_INVALID_ARG;
   TreeArgs a = tree_args(tree);
-  const size_t need = tree_workspace_bytes(a, device_sms());
-  if (need > 0 && (!workspace || workspace_bytes < need ||
-                   (reinterpret_cast<uintptr_t>(workspace) & 255) != 0))
+  if (!workspace_ok(workspace, workspace_bytes, tree_workspace_bytes(a, device_sms())))
     return TT_ERR_INVALID_ARG;
   if (!tree_fits(a, device_sms())) return TT_ERR_UNSUPPORTED;
   a.ws = static_cast<char*>(workspace);
@@ -251,6 +262,36 @@ tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_by
   cudaError_t e = load_kernels();
   if (e == cudaSuccess)
     e = launch_tree(a, tree->dtype, static_cast<cudaStream_t>(stream), device_sms());
+  return e == cudaSuccess ? TT_OK : record_cuda_error(e);
+}
+
+size_t tt_tree8_workspace_bytes(const tt_tree* tree) {
+  return tree_sizes_ok(tree) ? tree8_workspace_bytes(tree_args(tree), device_sms()) : 0;
+}
+
+tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_scales* v_scale,
+                        void* workspace, size_t workspace_bytes, void* out, float* lse,
+                        int32_t* status, void* stream) {
+  if (!tree_sizes_ok(tree) || !k_scale || !v_scale) return TT_ERR_INVALID_ARG;
+  const tt_status st = tree_ok(tree, out, status);
+  if (st != TT_OK || tree->B == 0) return st;
+  if (tree->max_len > 0 &&
+      (!pages8_ok(tree->k_cache, *k_scale) || !pages8_ok(tree->v_cache, *v_scale)))
+    return TT_ERR_INVALID_ARG;
+  TreeArgs a = tree_args(tree);
+  if (!workspace_ok(workspace, workspace_bytes, tree8_workspace_bytes(a, device_sms())))
+    return TT_ERR_INVALID_ARG;
+  if (!tree8_fits(a, device_sms())) return TT_ERR_UNSUPPORTED;
+  a.ws = static_cast<char*>(workspace);
+  a.out = static_cast<char*>(out);
+  a.lse = lse;
+  a.status = status;
+  const TreeScales sc = {
+      {k_scale->data, k_scale->page_stride, k_scale->group_stride, k_scale->head_stride},
+      {v_scale->data, v_scale->page_stride, v_scale->group_stride, v_scale->head_stride}};
+  cudaError_t e = load_kernels();
+  if (e == cudaSuccess)
+    e = launch_tree8(a, sc, tree->dtype, static_cast<cudaStream_t>(stream), device_sms());
   return e == cudaSuccess ? TT_OK : record_cuda_error(e);
 }
 

@@ -1,7 +1,7 @@
 // tt_ops.h -- arguments and launchers of the operators around a verification
 // step: log probabilities of logits rows (logprob.cu), a student's loss against a
 // teacher's top log probabilities (distill.cu), attention of drafted tokens over a
-// paged cache (tree.cu), rotary positions (rope.cu), appending to
+// paged cache (tree.cu; in 8 bits, tree8.cu), rotary positions (rope.cu), appending to
 // paged caches (append.cu).
 #pragma once
 
@@ -127,5 +127,19 @@ struct AppendArgs {
 cudaError_t launch_append(const AppendArgs& args, int dt, bool held8, cudaStream_t stream,
                           int sm_count);
 cudaError_t preload_append();
+
+struct TreeScale {
+  const uint8_t* data;  // strides in bytes
+  int64_t page, group, head;
+};
+struct TreeScales {
+  TreeScale k, v;
+};
+
+size_t tree8_workspace_bytes(const TreeArgs& args, int sm_count);
+bool tree8_fits(const TreeArgs& args, int sm_count);
+cudaError_t launch_tree8(const TreeArgs& args, const TreeScales& scales, int dt,
+                         cudaStream_t stream, int sm_count);
+cudaError_t preload_tree8();
 
 }  // namespace tt
