@@ -3,135 +3,1250 @@
 //
 // Token i of request b sees the L_b keys of the request's cache, its ancestors
 // i, parent(i), parent(parent(i)), ... and nothing else; its output in a head is
-// sum_x softmax_x(scale q.k_x) v_x over them, held in the running form.
+// sum_x softmax_x(scale q.k_x) v_x over them, held in the running form: with
+// m = max s_x and l = sum 2^(s_x - m), a larger m scales what was summed before.
+//
+// The bound is the cache, half of what 16 bits take, so half the time for each of its
+// tiles, and few rows: the tokens of a request times the query heads that share a key
+// head, often under 64. So keys take the rows of the matrix products and tokens the
+// columns: scores S^T = K Q^T and outputs O^T = V^T P^T, of 128 keys and up to 64
+// columns, cost what the columns cost. A thread then holds one key's scores of many
+// tokens: its scale is one number, its mask one bit, and the sums of the weights stay
+// in registers until an item ends. Only a row's maximum goes across threads, and it is
+// asked for only where a score passes the reference by 2^kSlack, which a vote tells.
+//
+// Keys are multiplied as they are, e4m3 by e4m3: a query is the sum of two (bf16) or
+// three (fp16) e4m3 pieces, sixteen times finer each, of a power of two of its row:
+// its 8 or 11 digits exactly, but for elements 2^-17 below the row's largest, whose
+// digits end at 2^-22 of it. Values are turned into the inputs' type, exactly, by four
+// warps of their own, since weights in pieces would cost the rows' warps more than the
+// whole conversion takes. The request's own drafted tokens are a tile of 16-bit keys.
+//
+// One CTA per SM: a warp copies tiles (a page at a time) and their scales, four convert,
+// one thread issues products, eight warps hold the scores, two for 32 keys each. Tiles
+// of all requests, key heads and 64 rows form one list, which the CTAs share evenly:
+// lengths are known on the device alone. Items cut by a CTA's end leave unnormalised
+// pieces, which a second kernel joins.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <algorithm>
+#include <atomic>
 #include <cstdint>
 #include <cstring>
+#include <numeric>
+#include <type_traits>
 
+#include "tt_device.cuh"
 #include "tt_e4m3.cuh"
 #include "tt_f2.cuh"
 #include "tt_ops.h"
+#include "tt_ring.cuh"
 #include "tt_rope.cuh"
+#include "tt_umma.cuh"
 
 namespace tt {
 
 namespace {
 
-constexpr int kWarps = 4;
+constexpr int kTile = 128;                     // keys of a tile
+constexpr int kRowWarps = 8, kConvWarps = 4;   // hold scores, convert values
+constexpr int kRowThreads = kRowWarps * 32, kConvThreads = kConvWarps * 32;
+constexpr int kThreads = kRowThreads + kConvThreads + 64;
+constexpr int kWords = TT_MAX_TREE / 32;
+constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
+constexpr int kScaleRing = 8;                    // tiles' scales, items' facts that are kept
+constexpr int kItemRing = 4;
+constexpr float kLn2 = 0.693147180559945f;
+// A row's reference maximum follows its maximum once that is 2^kSlack above it:
+// weights stay below 2^(kSlack + offset), and the output is scaled rarely.
+constexpr float kSlack = 8.f;
+constexpr int kMinShare = 2;  // places of a CTA, where there are few
+// What an item costs beyond its tiles (queries, ancestors, output), in tiles: it
+// takes as many places in the list before its first tile.
+constexpr int kItemCost = 2;
 
-// One warp per row (token, head): lane l holds elements l D / 32 .. of the head.
-template <int D, int DT>
-__global__ void __launch_bounds__(kWarps * 32) tree8_kernel(const TreeArgs a, const TreeScales sc) {
-  constexpr int E = D / 32;
-  const int lane = threadIdx.x & 31;
-  const int64_t row = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
-  const int h = int(row % a.Hq), hk = h / (a.Hq / a.Hkv);
-  const int i = int(row / a.Hq % a.max_nodes), b = int(row / a.Hq / a.max_nodes);
-  if (b >= a.B) return;
-  int status = 0;
-  const int first = a.tree_off[b], end = a.tree_off[b + 1], len = a.cache_len[b];
-  if (first < 0 || end < first || end > a.n_nodes)
-    status = TT_REQ_BAD_OFFSETS;
-  else if (end - first > a.max_nodes || len < 0 || len > a.max_len)
-    status = TT_REQ_TOO_LONG;
-  const int nodes = status ? 0 : end - first;
-  if (i == 0 && h == 0) {
-    bool bad = false;
-    if (a.parents)
-      for (int j = lane; j < nodes; j += 32) {
-        const int up = a.parents[first + j];
-        bad |= up < -1 || up >= j;
-      }
-    if (!status)
-      for (int x = lane; x < (len + a.page_size - 1) / a.page_size; x += 32) {
-        const int page = a.page_table[b * a.table_stride + x];
-        bad |= page < 0 || page >= a.n_pages;
-      }
-    bad = __any_sync(0xffffffffu, bad);
-    if (lane == 0) a.status[b] = status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
+struct Tree8Args {
+  CUtensorMap kc, vc;
+  TreeArgs a;
+  TreeScales sc;
+  float scale2;       // scale * log2(e)
+  int group;          // G
+  int ctas;           // of the launch
+  int box;            // slots of one copy: they lie within a page
+  int slots_inner;    // the cache maps' second dimension is the slot, the third the head
+  // pieces: CTA c leaves that of an item that began before its tiles at 2 c, that
+  // of one that begins in them at 2 c + 1
+  float* part;        // [2 ctas * R * D] outputs, not normalised
+  float2* part_ml;    // [2 ctas * R] their reference maximum (log2) and sum
+  int32_t* first;     // [B + 1] places before each request's, then the places per CTA
+  int32_t* stop;      // [ctas] the place from which a CTA gave up, INT32_MAX if it did not
+  uint64_t wait_ns;   // limit of a wait
+  int stall;          // the CTA whose copies a test withholds from its second tile on, or -1
+};
+
+// A request's usable range: its nodes and cache length, or why it has none.
+struct Request {
+  int first, nodes, len, status;
+};
+__device__ __forceinline__ Request request(const TreeArgs& a, int b) {
+  Request r{a.tree_off[b], 0, a.cache_len[b], 0};
+  const int end = a.tree_off[b + 1];
+  if (r.first < 0 || end < r.first || end > a.n_nodes) {
+    r.status = TT_REQ_BAD_OFFSETS;
+    return r;
   }
-  if (i >= nodes) return;
-  float q[E];
-  double acc[E] = {}, l = 0.0;  // (sums of many terms, one after the other)
-  for (int e = 0; e < E; ++e)
-    q[e] = load_elem<DT>(a.q + ((first + i) * a.q_token + h * a.q_head + lane * E + e) * 2);
-  float m = -INFINITY;
-  auto add = [&](float (&k)[E], float (&v)[E]) {
-    float s = 0.f;
-    for (int e = 0; e < E; ++e) s = fmaf(q[e], k[e], s);
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    s *= a.scale;
-    if (s == -INFINITY) return;  // (no weight)
-    const float to = fmaxf(m, s), f = m == -INFINITY ? 0.f : expf(m - to);
-    const float w = s != s ? s : expf(s - to);
-    m = to;
-    l = l * f + w;
-    for (int e = 0; e < E; ++e) acc[e] = acc[e] * f + double(w) * v[e];
-  };
-  for (int x = 0; x < len; ++x) {
-    const int page = a.page_table[b * a.table_stride + x / a.page_size], slot = x % a.page_size;
-    if (page < 0 || page >= a.n_pages) continue;
-    auto read = [&](const char* data, int64_t ps, int64_t ss, int64_t hs, const TreeScale& s,
-                    float (&y)[E]) {
-      const float f = e8m0(s.data[page * s.page + slot / TT_SCALE_SLOTS * s.group + hk * s.head]);
-      const char* at = data + page * ps + slot * ss + hk * hs + lane * E;
-      for (int e = 0; e < E; e += 2) {
-        const uint32_t two = e4m3x2_to_f16x2(*reinterpret_cast<const uint16_t*>(at + e));
-        const float2 g = __half22float2(*reinterpret_cast<const __half2*>(&two));
-        y[e] = g.x * f;
-        y[e + 1] = g.y * f;
-      }
-    };
-    float k[E], v[E];
-    read(a.kc, a.kc_page, a.kc_slot, a.kc_head, sc.k, k);
-    read(a.vc, a.vc_page, a.vc_slot, a.vc_head, sc.v, v);
-    add(k, v);
+  r.nodes = end - r.first;
+  if (r.nodes > a.max_nodes || r.len < 0 || r.len > a.max_len) {
+    r.status = TT_REQ_TOO_LONG;
+    r.nodes = 0;
   }
-  for (int j = i, up; j >= 0; j = up) {
-    up = a.parents ? a.parents[first + j] : j - 1;
-    if (up < -1 || up >= j) up = -1;
-    float k[E], v[E];
-    for (int e = 0; e < E; ++e) {
-      k[e] = load_elem<DT>(a.k + ((first + j) * a.k_token + hk * a.k_head + lane * E + e) * 2);
-      v[e] = load_elem<DT>(a.v + ((first + j) * a.v_token + hk * a.v_head + lane * E + e) * 2);
-    }
-    add(k, v);
-  }
-  const int64_t to = int64_t(first + i) * a.Hq + h;
-  const double inv = l > 0.0 || l != l ? 1.0 / l : 0.0;
-  for (int e = 0; e < E; ++e)
-    store_elem<DT>(a.out + (to * D + lane * E + e) * 2, float(acc[e] * inv));
-  if (a.lse && lane == 0) a.lse[to] = l > 0.0 || l != l ? m + float(log(l)) : -INFINITY;
+  return r;
 }
 
-template <int D, int DT>
-cudaError_t launch(const TreeArgs& a, const TreeScales& sc, cudaStream_t stream) {
+// Rows of a request and key head are (token, query head of the group), in order; an
+// item is R of them. The tiles that its rows see: the cache's, then those of drafted
+// tokens up to its last row's.
+__host__ __device__ inline int cache_tiles(int len) { return len / kTile + (len % kTile != 0); }
+__host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / kTile; }
+template <int R>
+__host__ __device__ inline int items(int nodes, int group) {
+  return (nodes * group + R - 1) / R;
+}
+template <int R>
+__device__ __forceinline__ int item_end(const Request& r, int group, int mt) {  // its last token + 1
+  return (min(r.nodes * group, (mt + 1) * R) - 1) / group + 1;
+}
+template <int R>
+__device__ __forceinline__ int item_tiles(const Request& r, int group, int mt) {
+  return cache_tiles(r.len) + tree_tiles(item_end<R>(r, group, mt));
+}
+// The places that one key head of a request takes in the list.
+template <int R>
+__device__ __forceinline__ int head_places(const Request& r, int group) {
+  const int n = items<R>(r.nodes, group);
+  int sum = n * (kItemCost + cache_tiles(r.len));
+  for (int mt = 0; mt < n; ++mt) sum += tree_tiles(item_end<R>(r, group, mt));
+  return sum;
+}
+// An item of the list, the first of its tiles that is left, and the places before it.
+template <int R>
+struct Place {
+  int b, hk, mt, tile, lead;
+  Request r;
+  __device__ __forceinline__ void find(const Tree8Args& p, int request_b, int offset) {
+    b = request_b;
+    r = request(p.a, b);
+    const int per_head = head_places<R>(r, p.group);
+    hk = offset / per_head;
+    offset %= per_head;
+    mt = 0;
+    for (int n; offset >= (n = kItemCost + item_tiles<R>(r, p.group, mt)); ++mt) offset -= n;
+    tile = max(0, offset - kItemCost);
+    lead = max(0, kItemCost - offset);
+  }
+  __device__ __forceinline__ void next_item(const Tree8Args& p) {
+    tile = 0;
+    lead = kItemCost;
+    if (++mt * R < r.nodes * p.group) return;
+    mt = 0;
+    if (++hk < p.a.Hkv) return;
+    hk = 0;
+    do {
+      if (++b >= p.a.B) return;
+      r = request(p.a, b);
+    } while (r.nodes == 0);
+  }
+};
+// The part of an item that a CTA takes.
+template <int R>
+struct Item {
+  int n_cache, rows, tile0, tile1, end;
+  __device__ __forceinline__ Item(const Tree8Args& p, const Place<R>& x, int todo) {
+    n_cache = cache_tiles(x.r.len);
+    rows = min(R, x.r.nodes * p.group - x.mt * R);
+    end = item_end<R>(x.r, p.group, x.mt);
+    tile0 = x.tile;
+    tile1 = min(n_cache + tree_tiles(end), x.tile + todo);
+  }
+  // keys of tile j in use
+  __device__ __forceinline__ int keys(const Place<R>& x, int j) const {
+    return min(kTile, j < n_cache ? x.r.len - j * kTile : end - (j - n_cache) * kTile);
+  }
+};
+
+// Whether every parent and page of the request is in range (the row threads).
+__device__ bool out_of_range(const TreeArgs& a, int b, const Request& r, int t) {
+  bool bad = false;
+  if (a.parents)
+    for (int i = t; i < r.nodes; i += kRowThreads) {
+      const int p = a.parents[r.first + i];
+      bad |= p < -1 || p >= i;
+    }
+  const int pages = r.len / a.page_size + (r.len % a.page_size != 0);
+  for (int x = t; x < pages; x += kRowThreads) {
+    const int p = a.page_table[b * a.table_stride + x];
+    bad |= p < 0 || p >= a.n_pages;
+  }
+  return bad;
+}
+
+template <int D, int R, bool F16>
+struct Smem8 {
+  static constexpr int kPieces = F16 ? 3 : 2;
+  // Tensor memory: two tiles' scores (a column for each piece and row), the output.
+  static constexpr int kScores = kPieces * R, kOut = 2 * kScores;
+  static constexpr int kColumns = kOut + R <= 64 ? 64 : kOut + R <= 128 ? 128 : kOut + R <= 256 ? 256 : 512;
+  static constexpr int kStages = D == 64 ? 6 : R >= 32 ? 3 : 4;  // what 227 KB hold
+  char w[2][kTile * D * 2];           // values of 16 bits; a drafted tile's keys too
+  char p[kTile * 128];                // weights, the rows of a key side by side
+  char k[kStages][kTile * D];         // keys and values as they come
+  char q16[R * D * 2];                // queries for drafted keys,
+  char q8[kPieces * R * D];           // and in pieces for the cache's
+  char v[kStages][kTile * D];
+  uint32_t seen[R][kWords];           // a token's ancestors and itself
+  int16_t up[TT_MAX_TREE];            // parents, -1 for roots
+  uint8_t token[R];                   // of a row, from the item's first
+  float k_scale[kScaleRing][kGroups], v_scale[kScaleRing][kGroups];
+  uint32_t left_out[kScaleRing];      // groups whose page is out of range
+  float factor[kItemRing][R];         // a row's pieces times it and a key's scale: log2 scores
+  uint32_t odd[kItemRing][kWords];    // drafted tokens with a value that is not finite
+  float ref[R], shift[R], fall[R];    // reference maximum, what is added to scores, last change
+  float part[4][R];                   // what the warps of 32 keys each tell
+  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
+  uint64_t q_full, q_empty, p_full, o_done, o_free, drained;
+  long long sums[kThreads / 32];      // places of the requests, by warps
+  int start_b, start_offset;          // where this CTA's places begin
+  int share;                          // and how many a CTA has
+  int unset[2];                       // rows of a half without a reference yet
+  uint32_t tmem;
+  int end, stop;                      // the place behind this CTA's, and where it gave up
+};
+
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+      : "r"(addr)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+      : "memory");
+}
+// (The registers pass through, so that nothing reads them before.)
+__device__ __forceinline__ void tmem_wait8(uint32_t (&r)[8]) {
+  asm volatile("tcgen05.wait::ld.sync.aligned;"
+               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
+                 "+r"(r[7])
+               :
+               : "memory");
+}
+// D[tmem] (+)= A[smem] B[smem] over 32 of K, both e4m3.
+__device__ __forceinline__ void umma8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.u32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
+      : "memory");
+}
+// Operand of e4m3 elements in rows of D bytes along K, swizzled by as many.
+template <int D>
+__device__ __forceinline__ uint64_t umma8_desc(uint32_t addr) {
+  return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(1) << 16 | uint64_t(8 * D >> 4) << 32 | uint64_t(1) << 46 |
+         uint64_t(D == 128 ? 2 : 4) << 61;
+}
+// Byte `at` of row r of such an operand.
+template <int D>
+__device__ __forceinline__ int swizzled8(int r, int at) {
+  return r * D + (at ^ (D == 128 ? (r & 7) << 4 : (r >> 1 & 3) << 4));
+}
+// 16-byte unit u of row r in 128-byte swizzled rows.
+__device__ __forceinline__ int swizzled16(int r, int u) { return r * 128 + ((u ^ (r & 7)) << 4); }
+// Instruction descriptors, fp32 accumulators, M = 128: e4m3 operands; and 16-bit ones that
+// both lie along M and N.
+__device__ __forceinline__ uint32_t idesc_e4m3(int n) {
+  return 1u << 4 | uint32_t(n >> 3) << 17 | uint32_t(128 >> 4) << 24;
+}
+__device__ __forceinline__ uint32_t idesc_mn(bool f16, int n) {
+  return umma_idesc(f16, n, true) | 1u << 15;
+}
+// Whether any of `threads` threads says so; all of them come to the barrier.
+__device__ __forceinline__ bool any_of(int barrier, int threads, bool x) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\t"
+      "setp.ne.u32 q, %3, 0;\n\t"
+      "bar.red.or.pred p, %1, %2, q;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"(barrier), "r"(threads), "r"(uint32_t(x))
+      : "memory");
+  return r != 0;
+}
+__device__ __forceinline__ void sync_of(int barrier, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+}
+// The largest of a warp's numbers (NaN: none).
+__device__ __forceinline__ float warp_max(float x) {
+  const int i = x != x ? int(0x807fffff) : __float_as_int(x);  // (-inf)
+  const int top = __reduce_max_sync(0xffffffffu, i ^ ((i >> 31) & 0x7fffffff));
+  return __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
+}
+// Sums of N numbers over the lanes: lane i gets that of the i-th (mod N).
+template <int N>
+__device__ __forceinline__ float warp_sums(float (&x)[N], int lane) {
+#pragma unroll
+  for (int s = N / 2; s > 0; s /= 2)
+#pragma unroll
+    for (int i = 0; i < s; ++i) {
+      const float give = lane & s ? x[i] : x[i + s], keep = lane & s ? x[i + s] : x[i];
+      x[i] = keep + __shfl_xor_sync(0xffffffffu, give, s);
+    }
+#pragma unroll
+  for (int s = N; s < 32; s *= 2) x[0] += __shfl_xor_sync(0xffffffffu, x[0], s);
+  return x[0];
+}
+
+template <int D, int R, bool F16>
+__global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
+  using S = Smem8<D, R, F16>;
+  constexpr int DT = F16 ? TT_F16 : TT_BF16;
+  constexpr int kPieces = S::kPieces, kStages = S::kStages;
+  constexpr int kBlock = kTile * 128;         // distance of the 64-element blocks of a 16-bit tile
+  constexpr int kChunks = R / 16;             // of 8 rows, of a row warp
+  constexpr float kOffset = F16 ? 7.f : 0.f;  // fp16 weights: away from its small end
+  extern __shared__ char raw[];
+  S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
+  const TreeArgs& a = p.a;
+  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  const uint64_t& limit = p.wait_ns;
+  grid_launch_dependents();
+
+  if (t == kRowThreads) {
+    for (int i = 0; i < kStages; ++i) {
+      mbar_init(&s.k_full[i], 1);
+      mbar_init(&s.k_empty[i], 1);
+      mbar_init(&s.v_full[i], 1);
+      mbar_init(&s.v_empty[i], kConvThreads);
+    }
+    for (int i = 0; i < kScaleRing; ++i) mbar_init(&s.scale_full[i], 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&s.w_full[i], kConvThreads);
+      mbar_init(&s.w_empty[i], 1);
+      mbar_init(&s.s_full[i], 1);
+      mbar_init(&s.s_free[i], kRowThreads);
+    }
+    mbar_init(&s.q_full, kConvThreads);
+    mbar_init(&s.q_empty, 1);
+    mbar_init(&s.p_full, kRowThreads);
+    mbar_init(&s.o_done, 1);
+    mbar_init(&s.o_free, kRowThreads);
+    mbar_init(&s.drained, 1);
+    s.stop = INT32_MAX;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == kRowWarps + kConvWarps + 1) tmem_alloc(&s.tmem, S::kColumns);
+  // The list: each thread adds up a run of requests, and the one whose run holds
+  // this CTA's first place tells the request.
+  int todo;
+  {
+    const int each = (a.B + kThreads - 1) / kThreads, b0 = min(a.B, t * each),
+              b1 = min(a.B, b0 + each);
+    long long mine = 0;
+    for (int b = b0; b < b1; ++b) mine += (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
+    long long upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    if (lane == 31) s.sums[warp] = upto;
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    long long all = 0;
+    for (int w = 0; w < kThreads / 32; ++w) {
+      if (w < warp) upto += s.sums[w];
+      all += s.sums[w];
+    }
+    const long long share = max((long long)(kMinShare), (all + p.ctas - 1) / p.ctas);
+    const long long from = share * blockIdx.x;
+    todo = int(max(0ll, min(share, all - from)));
+    if (t == 0) {
+      s.share = int(share);
+      s.end = int(min(all, from + share));
+    }
+    long long at = upto - mine;
+    if (todo > 0 && from >= at && from < upto) {
+      for (int b = b0; b < b1; ++b) {
+        const long long n = (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
+        if (from < at + n) {
+          s.start_b = b;
+          s.start_offset = int(from - at);
+          break;
+        }
+        at += n;
+      }
+    }
+    if (blockIdx.x == 0) {  // for the join
+      at = upto - mine;
+      for (int b = b0; b < b1; ++b) {
+        p.first[b] = int(at);
+        at += (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
+      }
+      if (t == 0) p.first[a.B] = int(share);
+    }
+  }
+  __syncthreads();
+  const uint32_t tmem = s.tmem;
+  bool ok = true;
+  Place<R> x;
+  x.lead = 0;
+  if (todo > 0) x.find(p, s.start_b, s.start_offset);
+
+  if (warp == kRowWarps + kConvWarps) {
+    // ------------------------------------------------------------ copies
+    // Lane i copies a tile's i-th box of slots, lane g reads its g-th scales. Pages are
+    // asked for two tiles ahead, scales one.
+    struct Ahead {
+      int hk, tile, len, page, b;  // page: of the lane's box
+      bool there;
+      uint32_t k, v;               // scale bytes
+    };
+    const int per = kTile / p.box;
+    int j = 0, j1 = 0, used = 0;
+    bool open = false;
+    auto next = [&]() {
+      Ahead y;
+      y.there = false;
+      y.page = -1;
+      y.b = y.hk = y.tile = y.len = 0;
+      y.k = y.v = 0;
+      for (;;) {
+        if (!open) {
+          if (todo <= x.lead) return y;
+          todo -= x.lead;
+          const Item<R> it(p, x, todo);
+          j = it.tile0;
+          j1 = min(it.tile1, it.n_cache);
+          used = it.tile1 - it.tile0;
+          open = true;
+        }
+        if (j < j1) break;
+        todo -= used;
+        x.next_item(p);
+        open = false;
+      }
+      y.there = true;
+      y.b = x.b;
+      y.hk = x.hk;
+      y.tile = j++;
+      y.len = x.r.len;
+      const int slot = y.tile * kTile + lane * p.box;
+      if (lane < per && slot < y.len) y.page = a.page_table[x.b * a.table_stride + slot / a.page_size];
+      return y;
+    };
+    auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
+    auto scales = [&](Ahead& y) {
+      if (!y.there) return;
+      const int page = __shfl_sync(0xffffffffu, y.page, (lane % kGroups) * TT_SCALE_SLOTS / p.box);
+      const int slot = y.tile * kTile + lane * TT_SCALE_SLOTS;
+      if (lane < kGroups && slot < y.len && usable(page)) {
+        const int64_t g = slot % a.page_size / TT_SCALE_SLOTS;
+        y.k = p.sc.k.data[page * p.sc.k.page + g * p.sc.k.group + y.hk * p.sc.k.head];
+        y.v = p.sc.v.data[page * p.sc.v.page + g * p.sc.v.group + y.hk * p.sc.v.head];
+      }
+    };
+    Ahead one = next(), two = next();
+    scales(one);
+    int n = 0, k_copies = 0, v_copies = 0;
+    for (; one.there && ok; ++n) {
+      const Ahead c = one;
+      one = two;
+      scales(one);
+      two = next();
+      const int st = n % kStages, ring = n % kScaleRing;
+      const uint32_t parity = ((n / kStages) & 1) ^ 1;
+      const int slot = c.tile * kTile + lane * p.box;
+      const bool mine = usable(c.page);
+      const unsigned int copied = __ballot_sync(0xffffffffu, mine);
+      const int boxes = __popc(copied);
+      auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* map) {
+        if (lane == 0) mbar_arrive_expect_tx(bar, boxes * p.box * D);
+        __syncwarp();
+        if (mine) {
+          const int in_page = slot % a.page_size;
+          tma_load_4d(smem_u32(dst) + lane * p.box * D, map, smem_u32(bar), 0,
+                      p.slots_inner ? in_page : c.hk, p.slots_inner ? c.hk : in_page, c.page);
+        }
+        __syncwarp();
+      };
+      ok = __all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit)) &&
+           (n != 1 || int(blockIdx.x) != p.stall);
+      if (!ok) break;
+      // (the scales of kScaleRing tiles ago: rows read them before they free scores of
+      // a tile that this stage's last products came two after)
+      if (lane < kGroups) {
+        s.k_scale[ring][lane] = e8m0(c.k);
+        s.v_scale[ring][lane] = e8m0(c.v);
+      }
+      const int box_of = (lane % kGroups) * TT_SCALE_SLOTS / p.box;
+      const unsigned int lost = __ballot_sync(0xffffffffu, lane < kGroups && !(copied >> box_of & 1));
+      if (lane == 0) s.left_out[ring] = lost;
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&s.scale_full[ring]);
+      copy(s.k[st], &s.k_full[st], &p.kc);
+      ++k_copies;
+      ok = __all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit));
+      if (!ok) break;
+      copy(s.v[st], &s.v_full[st], &p.vc);
+      ++v_copies;
+    }
+    // (the CTA's memory stays until its last copies have come)
+    for (int st = 0; st < kStages; ++st) {
+      if (k_copies > st) mbar_wait(&s.k_full[st], ((k_copies - 1 - st) / kStages) & 1, limit);
+      if (v_copies > st) mbar_wait(&s.v_full[st], ((v_copies - 1 - st) / kStages) & 1, limit);
+    }
+  } else if (warp == kRowWarps + kConvWarps + 1) {
+    // ---------------------------------------------------------- products
+    if (lane == 0) {
+      int n = 0, kt = 0, w = 0;  // tiles, the cache's among them, 16-bit operands
+      for (int seg = 0; todo > x.lead && ok; ++seg) {
+        todo -= x.lead;
+        const Item<R> it(p, x, todo);
+        // scores of tile j, the n-th; its drafted keys are operand w_at
+        auto scores = [&](int j, int tile, int w_at) {
+          const int buf = tile & 1;
+          if (!mbar_wait(&s.s_free[buf], ((tile >> 1) & 1) ^ 1, limit)) return false;
+          const uint32_t to = tmem + buf * S::kScores;
+          if (j < it.n_cache) {
+            const int st = kt % kStages;
+            if (!mbar_wait(&s.k_full[st], (kt / kStages) & 1, limit)) return false;
+            tc_fence_after();
+            const uint32_t ka = smem_u32(s.k[st]), qa = smem_u32(s.q8);
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c)
+              umma8_ss(to, umma8_desc<D>(ka + 32 * c), umma8_desc<D>(qa + 32 * c),
+                       idesc_e4m3(S::kScores), c > 0);
+            umma_commit(&s.k_empty[st]);
+            ++kt;
+          } else {
+            if (!mbar_wait(&s.w_full[w_at & 1], (w_at >> 1) & 1, limit)) return false;
+            tc_fence_after();
+            const uint32_t ka = smem_u32(s.w[w_at & 1]), qa = smem_u32(s.q16);
+#pragma unroll
+            for (int c = 0; c < D / 16; ++c)
+              umma_ss(to, umma_desc(ka + (c / 4) * kBlock + (c % 4) * 32, 16),
+                      umma_desc(qa + (c / 4) * (R * 128) + (c % 4) * 32, 16), umma_idesc(F16, R, false),
+                      c > 0);
+            umma_commit(&s.w_empty[w_at & 1]);
+          }
+          umma_commit(&s.s_full[buf]);
+          if (j + 1 == it.tile1) umma_commit(&s.q_empty);
+          return true;
+        };
+        ok = mbar_wait(&s.q_full, seg & 1, limit) && scores(it.tile0, n, w);
+        for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n) {
+          if (j >= it.n_cache) ++w;  // (behind the keys)
+          if (j + 1 < it.tile1) {
+            ok = scores(j + 1, n + 1, w + 1);
+            if (!ok) break;
+          }
+          ok = mbar_wait(&s.w_full[w & 1], (w >> 1) & 1, limit) &&
+               mbar_wait(&s.p_full, n & 1, limit) &&
+               (j > it.tile0 || mbar_wait(&s.o_free, (seg & 1) ^ 1, limit));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t va = smem_u32(s.w[w & 1]), pa = smem_u32(s.p);
+          const int steps = (it.keys(x, j) + 15) / 16;
+          // (heads of 64: the other half of the 128 rows is of what lies behind the
+          // operand, the other one or the weights, and nobody reads it)
+          for (int c = 0; c < steps; ++c)
+            umma_ss(tmem + S::kOut, umma_desc(va + c * 2048, kBlock),
+                    umma_desc(pa + c * 2048, 16), idesc_mn(F16, R), j > it.tile0 || c > 0);
+          umma_commit(&s.w_empty[w & 1]);
+          umma_commit(&s.o_done);
+          ++w;
+        }
+        todo -= it.tile1 - it.tile0;
+        x.next_item(p);
+      }
+      // (and until its last products and their arrivals are done)
+      umma_commit(&s.drained);
+      mbar_wait(&s.drained, 0, limit);
+    }
+  } else if (warp >= kRowWarps) {
+    // -------------------------------------------------- queries and values
+    const int ct = t - kRowThreads;
+    auto wait_for = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+      return ok;
+    };
+    int vt = 0, w = 0;
+    for (int seg = 0; todo > x.lead && ok; ++seg) {
+      todo -= x.lead;
+      const Item<R> it(p, x, todo);
+      // Queries: kEach threads to a row.
+      {
+        constexpr int kEach = kConvThreads / R, kVecs = D / 8 / kEach;
+        const int r = ct / kEach, sub = ct % kEach;
+        const int row = x.mt * R + r, token = row / p.group, head = x.hk * p.group + row % p.group;
+        uint4 q[kVecs];
+        const bool valid = r < it.rows;
+        const char* from = a.q + ((int64_t(x.r.first) + token) * a.q_token + int64_t(head) * a.q_head) * 2;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i)
+          q[i] = valid ? reinterpret_cast<const uint4*>(from)[sub * kVecs + i] : make_uint4(0, 0, 0, 0);
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+          float e[8];
+          unpack16<DT>(q[i], e);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
+        }
+#pragma unroll
+        for (int o = 1; o < kEach; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const uint32_t code = e8m0_for(top);
+        const float inverse = e8m0_inverse(code);
+        if (!wait_for(&s.q_empty, (seg & 1) ^ 1)) break;
+        if (sub == 0) s.factor[seg % kItemRing][r] = p.scale2 * e8m0(code);
+        if (ct < kWords) s.odd[seg % kItemRing][ct] = 0;
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+          const int u = sub * kVecs + i;  // 16-byte unit of the row
+          *reinterpret_cast<uint4*>(s.q16 + (u / 8) * (R * 128) + swizzled16(r, u % 8)) = q[i];
+          float e[8];
+          unpack16<DT>(q[i], e);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
+            e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
+#pragma unroll
+          for (int piece = 0; piece < kPieces; ++piece) {
+            uint32_t two[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
+              const uint32_t half = e4m3x2_to_f16x2(two[k]);
+              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
+              e[2 * k] = (e[2 * k] - f.x) * 16.f;
+              e[2 * k + 1] = (e[2 * k + 1] - f.y) * 16.f;
+            }
+            *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) =
+                make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
+          }
+        }
+        fence_proxy_async();
+        mbar_arrive(&s.q_full);
+      }
+      for (int j = it.tile0; j < it.tile1 && ok; ++j) {
+        const int keys = it.keys(x, j), steps = (keys + 15) / 16;  // (others are not multiplied)
+        constexpr int kUnits = D / 8;  // of 8 elements, of a key
+        if (j < it.n_cache) {
+          const int st = vt % kStages, ring = vt % kScaleRing;
+          if (!wait_for(&s.v_full[st], (vt / kStages) & 1)) break;
+          if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
+          const uint32_t lost = s.left_out[ring];
+#pragma unroll 4
+          for (int i = ct; i < steps * 16 * kUnits; i += kConvThreads) {
+            const int key = i / kUnits, u = i % kUnits;
+            uint4 o = make_uint4(0, 0, 0, 0);
+            if (key < keys && !(lost >> (key / TT_SCALE_SLOTS) & 1)) {
+              const uint2 in = *reinterpret_cast<const uint2*>(s.v[st] + key * D + u * 8);
+              const float f = s.v_scale[ring][key / TT_SCALE_SLOTS];
+              float e[8];
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t half = e4m3x2_to_f16x2((k < 2 ? in.x : in.y) >> (k & 1) * 16 & 0xffff);
+                const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&half));
+                e[2 * k] = y.x * f;
+                e[2 * k + 1] = y.y * f;
+              }
+              o = pack16<DT>(e);
+            }
+            *reinterpret_cast<uint4*>(s.w[w & 1] + (u / 8) * kBlock + swizzled16(key, u % 8)) = o;
+          }
+          mbar_arrive(&s.v_empty[st]);
+          ++vt;
+        } else {
+          // Drafted tokens: keys as they are, then values without what is not finite (a
+          // token outside its branch would get NaN from it; its own gets it at the end).
+          const int base = (j - it.n_cache) * kTile;
+          for (int kv = 0; kv < 2; ++kv) {
+            if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
+            const char* from = kv ? a.v : a.k;
+            const int64_t ts = kv ? a.v_token : a.k_token, hs = kv ? a.v_head : a.k_head;
+            for (int i = ct; i < steps * 16 * kUnits; i += kConvThreads) {
+              const int key = i / kUnits, u = i % kUnits;
+              uint4 o = make_uint4(0, 0, 0, 0);
+              if (key < keys) {
+                o = *reinterpret_cast<const uint4*>(
+                    from + ((int64_t(x.r.first) + base + key) * ts + x.hk * hs + u * 8) * 2);
+                if (kv) {
+                  constexpr uint32_t kExp = F16 ? 0x7c00 : 0x7f80;
+                  bool odd = false;
+#pragma unroll
+                  for (int q = 0; q < 4; ++q) {
+                    uint32_t y = q == 0 ? o.x : q == 1 ? o.y : q == 2 ? o.z : o.w;
+                    if ((y & kExp) == kExp) {
+                      y &= 0xffff0000u;
+                      odd = true;
+                    }
+                    if ((y >> 16 & kExp) == kExp) {
+                      y &= 0xffffu;
+                      odd = true;
+                    }
+                    (q == 0 ? o.x : q == 1 ? o.y : q == 2 ? o.z : o.w) = y;
+                  }
+                  if (odd)
+                    atomicOr(&s.odd[seg % kItemRing][(base + key) >> 5], 1u << ((base + key) & 31));
+                }
+              }
+              *reinterpret_cast<uint4*>(s.w[w & 1] + (u / 8) * kBlock + swizzled16(key, u % 8)) = o;
+            }
+            if (kv == 0) {
+              fence_proxy_async();
+              mbar_arrive(&s.w_full[w & 1]);
+              ++w;
+            }
+          }
+          if (!ok) break;
+        }
+        fence_proxy_async();
+        mbar_arrive(&s.w_full[w & 1]);
+        ++w;
+      }
+      todo -= it.tile1 - it.tile0;
+      x.next_item(p);
+    }
+  } else {
+    // -------------------------------------------------------------- rows
+    // (while the first copies are on their way: the requests' statuses)
+    for (int b = blockIdx.x; b < a.B; b += p.ctas) {
+      const Request r = request(a, b);
+      const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t));
+      if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
+    }
+    const int quarter = warp & 3, half = warp >> 2, key = quarter * 32 + lane;
+    const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
+    const int barrier = 1 + half;  // of the four warps that hold the same rows
+    // This warp's j-th chunk of rows: 8 c .. 8 c + 7.
+    auto chunk = [&](int j) { return 2 * j + half; };
+    // A warp goes on, or gives up, as one. One that gave up passes the barriers between
+    // the warps as often as the others, but waits and arrives no more and writes
+    // nothing: so the others give up, too, and all end.
+    auto wait_for = [&](uint64_t* bar, uint32_t parity) {
+      if (!ok) return;
+      ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+      if (!ok && lane == 0) atomicMin(&s.stop, s.end - todo);
+    };
+    int n = 0, ct = 0;
+    for (int seg = 0; todo > x.lead; ++seg) {
+      todo -= x.lead;
+      const Item<R> it(p, x, todo);
+      const int ring = seg % kItemRing, row0 = x.mt * R, token0 = row0 / p.group;
+      const int chunks = (it.rows + 7) / 8;
+      if (it.tile1 > it.n_cache) {
+        // a token's ancestors: one thread walks up from each token
+        sync_of(5, kRowThreads);  // (done with the last ones)
+        for (int i = t; i < it.end; i += kRowThreads) {
+          const int up = a.parents ? a.parents[x.r.first + i] : i - 1;
+          s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
+        }
+        if (t < R) s.token[t] = uint8_t((row0 + t) / p.group - token0);
+        sync_of(5, kRowThreads);
+        if (t < it.end - token0) {
+          const int words = tree_tiles(it.end) * (kTile / 32);
+          for (int w = 0; w < words; ++w) s.seen[t][w] = 0;
+          for (int i = token0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
+        }
+        sync_of(5, kRowThreads);
+      }
+      float l[kChunks][8];
+#pragma unroll
+      for (int j = 0; j < kChunks; ++j)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) l[j][i] = 0.f;
+      bool unset = true;
+      for (int j = it.tile0; j < it.tile1; ++j, ++n) {
+        const bool cache = j < it.n_cache;
+        const int keys = it.keys(x, j);
+        bool there = key < keys;
+        float scale = 1.f;
+        if (cache) {
+          const int e = ct % kScaleRing;
+          wait_for(&s.scale_full[e], (ct / kScaleRing) & 1);
+          scale = s.k_scale[e][key / TT_SCALE_SLOTS];
+          there = there && !(s.left_out[e] >> (key / TT_SCALE_SLOTS) & 1);
+          ++ct;
+        }
+        wait_for(&s.s_full[n & 1], (n >> 1) & 1);
+        tc_fence_after();
+        const uint32_t at = mine + (n & 1) * S::kScores;
+        // the scores of this thread's key, as log2
+        float y[kChunks][8];
+        float over = -INFINITY;
+#pragma unroll
+        for (int j2 = 0; j2 < kChunks; ++j2) {
+          const int c = chunk(j2);
+          if (c >= chunks) break;
+          if (cache) {
+            uint32_t v[kPieces][8];
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) tmem_ld8(at + q * R + 8 * c, v[q]);
+            const float* factor = s.factor[ring] + 8 * c;
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q) tmem_wait8(v[q]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              float z = __uint_as_float(v[kPieces - 1][i]);
+#pragma unroll
+              for (int q = kPieces - 2; q >= 0; --q) z = fmaf(z, 1.f / 16, __uint_as_float(v[q][i]));
+              y[j2][i] = there ? z * scale * factor[i] : -INFINITY;
+            }
+          } else {
+            uint32_t v[8];
+            tmem_ld8(at + 8 * c, v);
+            tmem_wait8(v);
+            const int word = ((j - it.n_cache) * kTile + key) >> 5;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const bool sees = there && s.seen[s.token[8 * c + i]][word] >> lane & 1;
+              y[j2][i] = sees ? __uint_as_float(v[i]) * p.scale2 : -INFINITY;
+            }
+          }
+          if (!unset) {
+            const float* shift = s.shift + 8 * c;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) over = fmaxf(over, y[j2][i] + shift[i]);
+          }
+        }
+        tc_fence_before();
+        if (ok) mbar_arrive(&s.s_free[n & 1]);
+        // the references follow the maxima, and with them the sums
+        const bool raised = unset || any_of(barrier, 128, over > kSlack + kOffset);
+        if (raised) {
+          float top = -INFINITY;
+#pragma unroll
+          for (int j2 = 0; j2 < kChunks; ++j2) {
+            if (chunk(j2) >= chunks) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const float m = warp_max(y[j2][i]);
+              if (lane == 8 * j2 + i) top = m;
+            }
+          }
+          // (lane: the row's number among this half's)
+          const int row = 8 * chunk(lane / 8) + lane % 8;
+          const bool has = lane < 8 * kChunks && row < it.rows;
+          if (has) s.part[quarter][row] = top;
+          sync_of(barrier, 128);
+          if (quarter == 0) {
+            bool none = false;
+            if (has) {
+              top = fmaxf(fmaxf(s.part[0][row], s.part[1][row]), fmaxf(s.part[2][row], s.part[3][row]));
+              const float old = j == it.tile0 ? -INFINITY : s.ref[row];
+              const float to = top - old > kSlack || old == -INFINITY ? fmaxf(old, top) : old;
+              s.ref[row] = to;
+              s.shift[row] = (to == -INFINITY ? 0.f : -to) + kOffset;
+              s.fall[row] = old == -INFINITY ? 0.f : ex2_approx(old - to);
+              none = to == -INFINITY;
+            } else if (lane < 8 * kChunks) {  // (rows that a chunk has too many)
+              s.shift[row] = -INFINITY;
+              s.fall[row] = 0.f;
+            }
+            none = __any_sync(0xffffffffu, none);
+            if (lane == 0) s.unset[half] = none;
+          }
+          sync_of(barrier, 128);
+          unset = s.unset[half];
+#pragma unroll
+          for (int j2 = 0; j2 < kChunks; ++j2) {
+            if (chunk(j2) >= chunks) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) l[j2][i] *= s.fall[8 * chunk(j2) + i];
+          }
+        }
+        // weights, and their sums
+        uint4 out[kChunks];
+#pragma unroll
+        for (int j2 = 0; j2 < kChunks; ++j2) {
+          const int c = chunk(j2);
+          if (c >= chunks) break;
+          const float* shift = s.shift + 8 * c;
+          float e[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            e[i] = ex2_approx(y[j2][i] + shift[i]);
+            l[j2][i] += e[i];
+          }
+          out[j2] = pack16<DT>(e);
+        }
+        // (the last tile's product is done with the weights' place and with the output)
+        if (n > 0) wait_for(&s.o_done, (n - 1) & 1);
+        tc_fence_after();
+#pragma unroll
+        for (int j2 = 0; j2 < kChunks; ++j2) {
+          const int c = chunk(j2);
+          if (c >= chunks) break;
+          if (ok) *reinterpret_cast<uint4*>(s.p + swizzled16(key, c)) = out[j2];
+          if (raised && j > it.tile0) {
+            uint32_t v[8];
+            tmem_ld8(mine + S::kOut + 8 * c, v);
+            tmem_wait8(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              v[i] = __float_as_uint(__uint_as_float(v[i]) * s.fall[8 * c + i]);
+            tmem_st8(mine + S::kOut + 8 * c, v);
+          }
+        }
+        tmem_wait_st();
+        fence_proxy_async();
+        tc_fence_before();
+        if (ok) mbar_arrive(&s.p_full);
+      }
+      // the sums of all keys, a row to a lane
+      {
+        float sums[8 * kChunks];
+#pragma unroll
+        for (int j2 = 0; j2 < kChunks; ++j2)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sums[8 * j2 + i] = l[j2][i];
+        const float sum = warp_sums(sums, lane);
+        const int row = 8 * chunk(lane / 8 % kChunks) + lane % 8;
+        sync_of(barrier, 128);  // (done with s.part and s.fall)
+        if (lane < 8 * kChunks && row < it.rows) s.part[quarter][row] = sum;
+        sync_of(barrier, 128);
+        const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
+        const bool has_tree = it.tile1 > it.n_cache;
+        // where a row goes: to the output, or to its place in the CTA's piece
+        auto place = [&](int r) {
+          return whole ? (int64_t(x.r.first) + (row0 + r) / p.group) * a.Hq + x.hk * p.group +
+                             (row0 + r) % p.group
+                       : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + r;
+        };
+        if (quarter == 0 && lane < 8 * kChunks && row < it.rows && ok) {
+          const float all = s.part[0][row] + s.part[1][row] + (s.part[2][row] + s.part[3][row]);
+          const float m2 = s.ref[row] == -INFINITY ? -INFINITY : s.ref[row] - kOffset;
+          s.fall[row] = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
+          if (!whole)
+            p.part_ml[place(row)] = make_float2(m2, all);
+          else if (a.lse)
+            a.lse[place(row)] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
+        }
+        sync_of(barrier, 128);
+        wait_for(&s.o_done, (n - 1) & 1);
+        tc_fence_after();
+        if (D == 128 || quarter < 2) {
+#pragma unroll 1
+          for (int j2 = 0; j2 < kChunks; ++j2) {
+            const int c = chunk(j2);
+            if (c >= chunks) break;
+            uint32_t v[8];
+            tmem_ld8(mine + S::kOut + 8 * c, v);
+            tmem_wait8(v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const int r = 8 * c + i;
+              if (r >= it.rows || !ok) continue;
+              float y = __uint_as_float(v[i]);
+              if (has_tree)
+                for (int w = 0; w * 32 < it.end; ++w)
+                  for (uint32_t odd = s.odd[ring][w] & s.seen[s.token[r]][w]; odd; odd &= odd - 1) {
+                    const int64_t peer = int64_t(x.r.first) + w * 32 + __ffs(odd) - 1;
+                    const float z =
+                        load_elem<DT>(a.v + (peer * a.v_token + x.hk * a.v_head + key) * 2);
+                    if (!(fabsf(z) < INFINITY)) y += z;
+                  }
+              const int64_t to = place(r) * D + key;
+              if (whole)
+                store_elem<DT>(a.out + to * 2, y * s.fall[r]);
+              else
+                p.part[to] = y;
+            }
+          }
+        }
+        tc_fence_before();
+        if (ok) mbar_arrive(&s.o_free);
+      }
+      todo -= it.tile1 - it.tile0;
+      x.next_item(p);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kRowWarps + kConvWarps + 1) tmem_free(tmem, S::kColumns);
+  if (t == 0) p.stop[blockIdx.x] = s.stop;  // (the join tells the requests)
+}
+
+// Joins the pieces of every row whose item was cut: with M the largest of their
+// references, out = sum 2^(m - M) o / sum 2^(m - M) l. A CTA takes a row; its warps take
+// the pieces in turn, the loads of eight before the first is added. It also tells the
+// requests that lost places to a CTA that gave up.
+constexpr int kJoinWarps = 4, kFewPieces = 16;
+
+template <int D, int R, bool F16, bool FEW>
+__global__ void __launch_bounds__(kJoinWarps * 32)
+    tree8_join_kernel(const __grid_constant__ Tree8Args p) {
+  constexpr int DT = F16 ? TT_F16 : TT_BF16;
+  constexpr int N = D / 32, W = FEW ? 1 : kJoinWarps;
+  constexpr int C = FEW ? 4 : 8;  // pieces at once
+  using Vec = typename std::conditional<N == 4, float4, float2>::type;
+  __shared__ __align__(16) float s_acc[W][D];
+  __shared__ float2 s_ml[W];
+  const TreeArgs& a = p.a;
+  const int warp = FEW ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const unsigned int at = FEW ? blockIdx.x * kJoinWarps + (threadIdx.x >> 5) : blockIdx.x;
+  const int h = int(at % a.Hq), hk = h / p.group;
+  const int i = int(at / a.Hq % a.max_nodes), b = int(at / a.Hq / a.max_nodes);
+  if (b >= a.B) return;
+  grid_dependency_wait();
+  const int share = p.first[a.B], first = p.first[b];
+  const Request r = request(a, b);
+  if (i >= r.nodes) return;
+  const int per_head = head_places<R>(r, p.group);
+  // (one warp of the request)
+  if (i == 0 && h == 0 && (FEW || threadIdx.x < 32)) {
+    const int end = first + per_head * a.Hkv - 1;  // its last place
+    int stop = INT32_MAX;
+    for (int c = first / share + lane; c <= end / share; c += 32) stop = min(stop, p.stop[c]);
+    if (__any_sync(0xffffffffu, stop <= end) && lane == 0) a.status[b] |= TT_REQ_TIMEOUT;
+  }
+  const int row = i * p.group + h % p.group, mt = row / R;
+  int before = hk * per_head + kItemCost;  // its first tile's place
+  for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles<R>(r, p.group, k);
+  const int last = before + item_tiles<R>(r, p.group, mt) - 1;
+  // the CTAs that the item lies in
+  const int c0 = (first + before) / share, pieces = (first + last) / share - c0 + 1;
+  if (pieces < 2) return;
+  auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * R + row % R; };
+  float M = -INFINITY, l = 0.f, acc[N];
+#pragma unroll
+  for (int c = 0; c < N; ++c) acc[c] = 0.f;
+  auto add = [&](float l_more, const Vec& o, float f) {
+    l = fmaf(l_more, f, l);
+    acc[0] = fmaf(o.x, f, acc[0]);
+    acc[1] = fmaf(o.y, f, acc[1]);
+    if constexpr (N == 4) {
+      acc[2] = fmaf(o.z, f, acc[2]);
+      acc[3] = fmaf(o.w, f, acc[3]);
+    }
+  };
+  for (int k0 = warp; k0 < pieces; k0 += W * C) {
+    float2 ml[C];
+    Vec o[C];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int64_t from = place(min(k0 + c * W, pieces - 1));
+      ml[c] = p.part_ml[from];
+      o[c] = reinterpret_cast<const Vec*>(p.part + from * D)[lane];
+    }
+    float top = M;
+#pragma unroll
+    for (int c = 0; c < C; ++c) top = fmaxf(top, ml[c].x);
+    const float f = M == -INFINITY ? 0.f : ex2_approx(M - top);
+    M = top;
+    l *= f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) acc[c] *= f;
+    // (a piece without a reference: of NaN, or of nothing, which adds 0)
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+      if (k0 + c * W < pieces)
+        add(ml[c].y, o[c],
+            ml[c].x == -INFINITY ? (ml[c].y != ml[c].y ? 1.f : 0.f) : ex2_approx(ml[c].x - top));
+  }
+  if constexpr (!FEW) {
+#pragma unroll
+    for (int c = 0; c < N; ++c) s_acc[warp][lane * N + c] = acc[c];
+    if (lane == 0) s_ml[warp] = make_float2(M, l);
+    __syncthreads();
+    if (warp > 0) return;
+    for (int w = 1; w < W; ++w) M = fmaxf(M, s_ml[w].x);
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < N; ++c) acc[c] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float f = s_ml[w].x == -INFINITY ? (s_ml[w].y != s_ml[w].y ? 1.f : 0.f)
+                                             : ex2_approx(s_ml[w].x - M);
+      add(s_ml[w].y, reinterpret_cast<const Vec*>(s_acc[w])[lane], f);
+    }
+  }
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const int64_t to = (int64_t(r.first) + i) * a.Hq + h;
+  uint32_t* out = reinterpret_cast<uint32_t*>(a.out + to * D * 2) + lane * (N / 2);
+  out[0] = pack_pair<DT>(acc[0] * inv, acc[1] * inv);
+  if constexpr (N == 4) out[1] = pack_pair<DT>(acc[2] * inv, acc[3] * inv);
+  if (a.lse && lane == 0) a.lse[to] = l > 0.f || l != l ? fmaf(M, kLn2, logf(l)) : -INFINITY;
+}
+
+// ------------------------------------------------------------------- host
+
+// How a call is cut: CTAs, and the workspace.
+struct Cut8 {
+  int rows;        // R
+  int ctas;
+  int64_t places;  // in the list, were all lengths the longest
+  int64_t pieces;  // of one item, about
+  size_t part_bytes, ml_bytes, first_bytes, bytes;
+};
+Cut8 cut8(const TreeArgs& a, int sm_count) {
+  Cut8 c;
+  const int group = a.Hq / a.Hkv;
+  const int64_t rows = int64_t(a.max_nodes) * group;
+  c.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  const int64_t row_tiles = (rows + c.rows - 1) / c.rows;
+  const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
+  const int64_t all = c.places = int64_t(std::min(
+      1e18, double(a.B) * double(a.Hkv) * double(row_tiles) * double(kItemCost + tiles)));
+  c.ctas = int(std::max<int64_t>(
+      1, std::min<int64_t>(sm_count, (all + kMinShare - 1) / kMinShare)));
+  // (were all lengths the longest; fewer tiles make shares smaller and pieces more)
+  const int64_t share = std::max<int64_t>(kMinShare, (all + c.ctas - 1) / c.ctas);
+  c.pieces = tiles / share + 2;
+  const size_t held = 2 * size_t(c.ctas) * c.rows;
+  c.part_bytes = align256(held * a.D * sizeof(float));
+  c.ml_bytes = align256(held * sizeof(float2));
+  c.first_bytes = align256((size_t(a.B) + 1) * sizeof(int32_t));
+  c.bytes = c.part_bytes + c.ml_bytes + c.first_bytes + align256(c.ctas * sizeof(int32_t));
+  return c;
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+  static std::atomic<void*> found{nullptr};
+  void* f = found.load(std::memory_order_acquire);
+  if (!f) {
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault,
+                                         &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess)
+      return nullptr;
+    found.store(f, std::memory_order_release);
+  }
+  return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(f);
+}
+
+// A map of a cache's bytes, in boxes of one head's elements of some slots. Dimensions by
+// rising stride: heads within slots, or slots within heads.
+bool encode(CUtensorMap* map, const TreeArgs& a, const char* data, int64_t page, int64_t slot,
+            int64_t head, int box, bool slots_inner, CUtensorMapSwizzle swizzle) {
+  const int64_t size[4] = {a.D, slots_inner ? a.page_size : a.Hkv, slots_inner ? a.Hkv : a.page_size,
+                           a.n_pages};
+  const int64_t stride[4] = {1, slots_inner ? slot : head, slots_inner ? head : slot, page};
+  const cuuint32_t boxes[4] = {cuuint32_t(a.D), cuuint32_t(slots_inner ? box : 1),
+                               cuuint32_t(slots_inner ? 1 : box), 1},
+                   ones[4] = {1, 1, 1, 1};
+  cuuint64_t dims[4], strides[3];
+  for (int i = 0; i < 4; ++i) {
+    dims[i] = cuuint64_t(size[i]);
+    // (a dimension of one entry takes any valid stride)
+    if (i > 0) strides[i - 1] = cuuint64_t(size[i] > 1 ? stride[i] : size[0]);
+  }
+  const auto f = encoder();
+  return f && f(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<char*>(data), dims, strides, boxes,
+                ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, int R, bool F16>
+cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
+  const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned((int64_t(a.B) * a.max_nodes * a.Hq + kWarps - 1) / kWarps));
-  cfg.blockDim = dim3(kWarps * 32);
+  cfg.gridDim = dim3(unsigned(p.ctas));
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
   cfg.stream = stream;
-  return cudaLaunchKernelEx(&cfg, tree8_kernel<D, DT>, a, sc);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, R, F16>, p);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  const bool few = pieces <= kFewPieces;
+  const int64_t rows = int64_t(a.B) * a.max_nodes * a.Hq;
+  cfg.gridDim = dim3(unsigned(few ? (rows + kJoinWarps - 1) / kJoinWarps : rows));
+  cfg.blockDim = dim3(kJoinWarps * 32);
+  cfg.dynamicSmemBytes = 0;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return few ? cudaLaunchKernelEx(&cfg, tree8_join_kernel<D, R, F16, true>, p)
+             : cudaLaunchKernelEx(&cfg, tree8_join_kernel<D, R, F16, false>, p);
+}
+
+template <int D, int R, bool F16>
+cudaError_t preload() {
+  cudaFuncAttributes fa;
+  cudaError_t e = cudaFuncGetAttributes(&fa, tree8_join_kernel<D, R, F16, true>);
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree8_join_kernel<D, R, F16, false>);
+  if (e != cudaSuccess) return e;
+  static_assert(sizeof(Smem8<D, R, F16>) + 1024 <= 227 * 1024, "shared memory of a CTA");
+  return cudaFuncSetAttribute(tree8_kernel<D, R, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              int(sizeof(Smem8<D, R, F16>)) + 1024);
+}
+template <int D, bool F16>
+cudaError_t preload_all() {
+  cudaError_t e = preload<D, 16, F16>();
+  if (e == cudaSuccess) e = preload<D, 32, F16>();
+  if (e == cudaSuccess) e = preload<D, 64, F16>();
+  return e;
 }
 
 }  // namespace
 
-size_t tree8_workspace_bytes(const TreeArgs&, int) { return 256; }
+size_t tree8_workspace_bytes(const TreeArgs& a, int sm_count) { return cut8(a, sm_count).bytes; }
 
-bool tree8_fits(const TreeArgs& a, int) {
-  return double(a.B) * a.max_nodes * double(a.Hq) <= INT32_MAX;
+// (places of the list, and blocks of the join, are 32-bit numbers)
+bool tree8_fits(const TreeArgs& a, int sm_count) {
+  return cut8(a, sm_count).places <= INT32_MAX &&
+         double(a.B) * a.max_nodes * double(a.Hq) <= INT32_MAX;
 }
 
-cudaError_t launch_tree8(const TreeArgs& a, const TreeScales& sc, int dt, cudaStream_t stream, int) {
-  if (a.D == 128)
-    return dt == TT_F16 ? launch<128, TT_F16>(a, sc, stream) : launch<128, TT_BF16>(a, sc, stream);
-  return dt == TT_F16 ? launch<64, TT_F16>(a, sc, stream) : launch<64, TT_BF16>(a, sc, stream);
+cudaError_t launch_tree8(const TreeArgs& a, const TreeScales& sc, int dt, cudaStream_t stream,
+                         int sm_count) {
+  const Cut8 c = cut8(a, sm_count);
+  Tree8Args p;
+  std::memset(&p, 0, sizeof p);
+  p.a = a;
+  p.sc = sc;
+  p.scale2 = float(double(a.scale) * 1.4426950408889634);
+  p.group = a.Hq / a.Hkv;
+  p.ctas = c.ctas;
+  p.box = std::gcd(a.page_size, kTile);
+  p.part = reinterpret_cast<float*>(a.ws);
+  p.part_ml = reinterpret_cast<float2*>(a.ws + c.part_bytes);
+  p.first = reinterpret_cast<int32_t*>(a.ws + c.part_bytes + c.ml_bytes);
+  p.stop = p.first + c.first_bytes / sizeof(int32_t);
+  next_launch_stall(&p.stall, &p.wait_ns);
+  if (a.max_len > 0) {
+    // (one order for both, so that a copy's coordinates are the same)
+    p.slots_inner = a.kc_slot < a.kc_head && a.page_size > 1 && a.Hkv > 1;
+    if (!encode(&p.kc, a, a.kc, a.kc_page, a.kc_slot, a.kc_head, p.box, p.slots_inner,
+                a.D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !encode(&p.vc, a, a.vc, a.vc_page, a.vc_slot, a.vc_head, p.box, p.slots_inner,
+                CU_TENSOR_MAP_SWIZZLE_NONE))
+      return cudaErrorInvalidValue;
+  }
+  auto go = [&](auto dim, auto f16) {
+    constexpr int D = decltype(dim)::value;
+    constexpr bool F16 = decltype(f16)::value;
+    return c.rows == 16   ? launch<D, 16, F16>(p, c.pieces, stream)
+           : c.rows == 32 ? launch<D, 32, F16>(p, c.pieces, stream)
+                          : launch<D, 64, F16>(p, c.pieces, stream);
+  };
+  auto of = [&](auto dim) { return dt == TT_F16 ? go(dim, std::true_type()) : go(dim, std::false_type()); };
+  return a.D == 128 ? of(std::integral_constant<int, 128>()) : of(std::integral_constant<int, 64>());
 }
 
 cudaError_t preload_tree8() {
-  cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, tree8_kernel<128, TT_F16>);
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree8_kernel<128, TT_BF16>);
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree8_kernel<64, TT_F16>);
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree8_kernel<64, TT_BF16>);
+  cudaError_t e = preload_all<128, true>();
+  if (e == cudaSuccess) e = preload_all<128, false>();
+  if (e == cudaSuccess) e = preload_all<64, true>();
+  if (e == cudaSuccess) e = preload_all<64, false>();
   return e;
 }
 
