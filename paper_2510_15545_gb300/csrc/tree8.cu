@@ -18,9 +18,11 @@
 // Keys are multiplied as they are, e4m3 by e4m3: a query is the sum of two (bf16) or
 // three (fp16) e4m3 pieces, sixteen times finer each, of a power of two of its row:
 // its 8 or 11 digits exactly, but for elements 2^-17 below the row's largest, whose
-// digits end at 2^-22 of it. Values are turned into the inputs' type, exactly, by four
-// warps of their own, since weights in pieces would cost the rows' warps more than the
-// whole conversion takes. The request's own drafted tokens are a tile of 16-bit keys.
+// digits end at 2^-22 of it. Values become fp16, which holds every e4m3 value, by four
+// warps of their own (weights in pieces would cost the rows' warps more); their scale
+// goes to the weights, of the largest scale so far, so that fp16 holds those of scales
+// 2^-20 below it as well as the largest's. The request's own drafted tokens are a tile
+// of keys and values of the inputs' type.
 //
 // One CTA per SM: a warp copies tiles (a page at a time) and their scales, four convert,
 // one thread issues products, eight warps hold the scores, two for 32 keys each. Tiles
@@ -44,15 +46,22 @@
 #include "tt_ring.cuh"
 #include "tt_rope.cuh"
 #include "tt_umma.cuh"
+#include "tt_x2.cuh"
 
 namespace tt {
 
 namespace {
 
 constexpr int kTile = 128;                     // keys of a tile
-constexpr int kRowWarps = 8, kConvWarps = 4;   // hold scores, convert values
-constexpr int kRowThreads = kRowWarps * 32, kConvThreads = kConvWarps * 32;
-constexpr int kThreads = kRowThreads + kConvThreads + 64;
+constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
+// The warps that hold the scores of R rows: twice four, of 32 keys each.
+template <int R>
+struct Rows {
+  static constexpr int kSubs = 2;                         // fours of warps
+  static constexpr int kChunks = R / 8 / kSubs;           // of 8 rows, of a warp
+  static constexpr int kWarps = 4 * kSubs, kThreads = kWarps * 32;
+  static constexpr int kAll = kThreads + kConvThreads + 96;  // threads of a CTA
+};
 constexpr int kWords = TT_MAX_TREE / 32;
 constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
 constexpr int kScaleRing = 8;                    // tiles' scales, items' facts that are kept
@@ -65,6 +74,18 @@ constexpr int kMinShare = 2;  // places of a CTA, where there are few
 // What an item costs beyond its tiles (queries, ancestors, output), in tiles: it
 // takes as many places in the list before its first tile.
 constexpr int kItemCost = 2;
+
+// mbar_wait in few instructions: the roles wait in some thirty places, and what they
+// do in between has to stay in the instruction caches.
+__device__ __forceinline__ bool wait8(uint64_t* bar, uint32_t parity, const uint64_t& limit_ns) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint64_t t0 = global_ns();
+#pragma unroll 1
+  do {
+    if (mbar_try_wait(bar, parity)) return true;
+  } while (global_ns() - t0 <= limit_ns);
+  return false;
+}
 
 struct Tree8Args {
   CUtensorMap kc, vc;
@@ -123,46 +144,56 @@ __device__ __forceinline__ int item_tiles(const Request& r, int group, int mt) {
 }
 // The places that one key head of a request takes in the list.
 template <int R>
-__device__ __forceinline__ int head_places(const Request& r, int group) {
+__device__ __noinline__ int head_places(const Request r, int group) {
   const int n = items<R>(r.nodes, group);
   int sum = n * (kItemCost + cache_tiles(r.len));
+#pragma unroll 1
   for (int mt = 0; mt < n; ++mt) sum += tree_tiles(item_end<R>(r, group, mt));
   return sum;
 }
 // An item of the list, the first of its tiles that is left, and the places before it.
-template <int R>
+// (Finding it and stepping on are calls: each role does it, and inlined in all of them
+// they made 180 KB of code, whose misses cost more than the work; with them and the
+// slow side of a wait apart it is TODO.)
 struct Place {
   int b, hk, mt, tile, lead;
   Request r;
-  __device__ __forceinline__ void find(const Tree8Args& p, int request_b, int offset) {
-    b = request_b;
-    r = request(p.a, b);
-    const int per_head = head_places<R>(r, p.group);
-    hk = offset / per_head;
-    offset %= per_head;
-    mt = 0;
-    for (int n; offset >= (n = kItemCost + item_tiles<R>(r, p.group, mt)); ++mt) offset -= n;
-    tile = max(0, offset - kItemCost);
-    lead = max(0, kItemCost - offset);
-  }
-  __device__ __forceinline__ void next_item(const Tree8Args& p) {
-    tile = 0;
-    lead = kItemCost;
-    if (++mt * R < r.nodes * p.group) return;
-    mt = 0;
-    if (++hk < p.a.Hkv) return;
-    hk = 0;
-    do {
-      if (++b >= p.a.B) return;
-      r = request(p.a, b);
-    } while (r.nodes == 0);
-  }
 };
+template <int R>
+__device__ __noinline__ Place find_place(const TreeArgs& a, int group, int request_b, int offset) {
+  Place x;
+  x.b = request_b;
+  x.r = request(a, request_b);
+  const int per_head = head_places<R>(x.r, group);
+  x.hk = offset / per_head;
+  offset %= per_head;
+  x.mt = 0;
+#pragma unroll 1
+  for (int n; offset >= (n = kItemCost + item_tiles<R>(x.r, group, x.mt)); ++x.mt) offset -= n;
+  x.tile = max(0, offset - kItemCost);
+  x.lead = max(0, kItemCost - offset);
+  return x;
+}
+template <int R>
+__device__ __noinline__ Place next_place(const TreeArgs& a, int group, Place x) {
+  x.tile = 0;
+  x.lead = kItemCost;
+  if (++x.mt * R < x.r.nodes * group) return x;
+  x.mt = 0;
+  if (++x.hk < a.Hkv) return x;
+  x.hk = 0;
+#pragma unroll 1
+  do {
+    if (++x.b >= a.B) return x;
+    x.r = request(a, x.b);
+  } while (x.r.nodes == 0);
+  return x;
+}
 // The part of an item that a CTA takes.
 template <int R>
 struct Item {
   int n_cache, rows, tile0, tile1, end;
-  __device__ __forceinline__ Item(const Tree8Args& p, const Place<R>& x, int todo) {
+  __device__ __forceinline__ Item(const Tree8Args& p, const Place& x, int todo) {
     n_cache = cache_tiles(x.r.len);
     rows = min(R, x.r.nodes * p.group - x.mt * R);
     end = item_end<R>(x.r, p.group, x.mt);
@@ -170,21 +201,23 @@ struct Item {
     tile1 = min(n_cache + tree_tiles(end), x.tile + todo);
   }
   // keys of tile j in use
-  __device__ __forceinline__ int keys(const Place<R>& x, int j) const {
+  __device__ __forceinline__ int keys(const Place& x, int j) const {
     return min(kTile, j < n_cache ? x.r.len - j * kTile : end - (j - n_cache) * kTile);
   }
 };
 
 // Whether every parent and page of the request is in range (the row threads).
-__device__ bool out_of_range(const TreeArgs& a, int b, const Request& r, int t) {
+__device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Request r, int t, int threads) {
   bool bad = false;
   if (a.parents)
-    for (int i = t; i < r.nodes; i += kRowThreads) {
+#pragma unroll 1
+    for (int i = t; i < r.nodes; i += threads) {
       const int p = a.parents[r.first + i];
       bad |= p < -1 || p >= i;
     }
   const int pages = r.len / a.page_size + (r.len % a.page_size != 0);
-  for (int x = t; x < pages; x += kRowThreads) {
+#pragma unroll 1
+  for (int x = t; x < pages; x += threads) {
     const int p = a.page_table[b * a.table_stride + x];
     bad |= p < 0 || p >= a.n_pages;
   }
@@ -208,22 +241,30 @@ struct Smem8 {
   int16_t up[TT_MAX_TREE];            // parents, -1 for roots
   uint8_t token[R];                   // of a row, from the item's first
   float k_scale[kScaleRing][kGroups], v_scale[kScaleRing][kGroups];
-  uint32_t left_out[kScaleRing];      // groups whose page is out of range
-  float factor[kItemRing][R];         // a row's pieces times it and a key's scale: log2 scores
+  uint32_t left_out[2][kScaleRing];   // groups whose page is out of range: keys, values
+  int top_code[kScaleRing];           // the largest of the values' scales
+  alignas(16) float factor[kItemRing][R];         // a row's pieces times it and a key's scale: log2 scores
+  alignas(16) float own_factor[8];                // the same of drafted keys
   uint32_t odd[kItemRing][kWords];    // drafted tokens with a value that is not finite
-  float ref[R], shift[R], fall[R];    // reference maximum, what is added to scores, last change
+  alignas(16) float shift[R];         // what is added to log2 scores
+  alignas(16) float fall[R];          // a reference's last change
+  float ref[R];                       // reference maximum (log2)
   float part[4][R];                   // what the warps of 32 keys each tell
   uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
   uint64_t q_full, q_empty, p_full, o_done, o_free, drained;
-  long long sums[kThreads / 32];      // places of the requests, by warps
+  long long sums[Rows<R>::kAll / 32];  // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
-  int unset[2];                       // rows of a half without a reference yet
+  int unset[4];                       // rows of four warps without a reference yet
   uint32_t tmem;
   int end, stop;                      // the place behind this CTA's, and where it gave up
 };
 
+// Numbers 2 i and 2 i + 1.
+__device__ __forceinline__ f32x2 both(const uint32_t (&v)[8], int i) {
+  return pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+}
 __device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
   asm volatile(
       "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -312,14 +353,36 @@ __device__ __forceinline__ float warp_sums(float (&x)[N], int lane) {
   return x[0];
 }
 
+// What drafted tokens with a value that is not finite add to element d of a row that
+// sees them.
+template <int DT>
+__device__ __noinline__ float odd_values(const TreeArgs& a, const uint32_t* odd, const uint32_t* seen,
+                                         int end, int first, int hk, int d) {
+  float sum = 0.f;
+#pragma unroll 1
+  for (int w = 0; w * 32 < end; ++w)
+#pragma unroll 1
+    for (uint32_t both = odd[w] & seen[w]; both; both &= both - 1) {
+      const int64_t peer = int64_t(first) + w * 32 + __ffs(both) - 1;
+      const float z = load_elem<DT>(a.v + (peer * a.v_token + hk * a.v_head + d) * 2);
+      if (!(fabsf(z) < INFINITY)) sum += z;
+    }
+  return sum;
+}
+
 template <int D, int R, bool F16>
-__global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
+__global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
   constexpr int kPieces = S::kPieces, kStages = S::kStages;
+  // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
+  // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
+  constexpr int kOwnCode = F16 ? 127 : 67;
   constexpr int kBlock = kTile * 128;         // distance of the 64-element blocks of a 16-bit tile
-  constexpr int kChunks = R / 16;             // of 8 rows, of a row warp
-  constexpr float kOffset = F16 ? 7.f : 0.f;  // fp16 weights: away from its small end
+  constexpr int kSubs = Rows<R>::kSubs, kChunks = Rows<R>::kChunks;
+  constexpr int kRowWarps = Rows<R>::kWarps, kRowThreads = Rows<R>::kThreads;
+  constexpr int kThreads = Rows<R>::kAll;
+  constexpr float kOffset = 7.f;              // fp16 weights: away from its small end
   extern __shared__ char raw[];
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
   const TreeArgs& a = p.a;
@@ -334,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       mbar_init(&s.v_full[i], 1);
       mbar_init(&s.v_empty[i], kConvThreads);
     }
-    for (int i = 0; i < kScaleRing; ++i) mbar_init(&s.scale_full[i], 1);
+    for (int i = 0; i < kScaleRing; ++i) mbar_init(&s.scale_full[i], 2);
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.w_full[i], kConvThreads);
       mbar_init(&s.w_empty[i], 1);
@@ -348,9 +411,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     mbar_init(&s.o_free, kRowThreads);
     mbar_init(&s.drained, 1);
     s.stop = INT32_MAX;
+    for (int i = 0; i < 8; ++i) s.own_factor[i] = p.scale2;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == kRowWarps + kConvWarps + 1) tmem_alloc(&s.tmem, S::kColumns);
+  if (warp == kRowWarps + kConvWarps) tmem_alloc(&s.tmem, S::kColumns);
   // The list: each thread adds up a run of requests, and the one whose run holds
   // this CTA's first place tells the request.
   int todo;
@@ -358,6 +422,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     const int each = (a.B + kThreads - 1) / kThreads, b0 = min(a.B, t * each),
               b1 = min(a.B, b0 + each);
     long long mine = 0;
+#pragma unroll 1
     for (int b = b0; b < b1; ++b) mine += (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
     long long upto = mine;
 #pragma unroll
@@ -383,6 +448,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     }
     long long at = upto - mine;
     if (todo > 0 && from >= at && from < upto) {
+#pragma unroll 1
       for (int b = b0; b < b1; ++b) {
         const long long n = (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
         if (from < at + n) {
@@ -395,6 +461,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     }
     if (blockIdx.x == 0) {  // for the join
       at = upto - mine;
+#pragma unroll 1
       for (int b = b0; b < b1; ++b) {
         p.first[b] = int(at);
         at += (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
@@ -405,28 +472,31 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
   __syncthreads();
   const uint32_t tmem = s.tmem;
   bool ok = true;
-  Place<R> x;
+  Place x;
   x.lead = 0;
-  if (todo > 0) x.find(p, s.start_b, s.start_offset);
+  if (todo > 0) x = find_place<R>(p.a, p.group, s.start_b, s.start_offset);
 
-  if (warp == kRowWarps + kConvWarps) {
+  if (warp > kRowWarps + kConvWarps) {
     // ------------------------------------------------------------ copies
-    // Lane i copies a tile's i-th box of slots, lane g reads its g-th scales. Pages are
-    // asked for two tiles ahead, scales one.
+    // One warp for keys, one for values. Lane g < 8 has to do with a tile's g-th 16 slots:
+    // it reads their scale, and copies the box that begins with them. Pages are asked
+    // for two tiles ahead, scales one.
+    const bool values = warp != kRowWarps + kConvWarps + 1;
+    const TreeScale& sc = values ? p.sc.v : p.sc.k;
+    char* const dst = values ? &s.v[0][0] : &s.k[0][0];
+    uint64_t* const full = values ? s.v_full : s.k_full;
+    uint64_t* const empty = values ? s.v_empty : s.k_empty;
+    const CUtensorMap* const map = values ? &p.vc : &p.kc;
+    const int per_tile = kTile / a.page_size, rest = kTile % a.page_size;
     struct Ahead {
-      int hk, tile, len, page, b;  // page: of the lane's box
+      int hk, page, in_page;  // of the lane's slots
+      uint32_t code;
       bool there;
-      uint32_t k, v;               // scale bytes
     };
-    const int per = kTile / p.box;
-    int j = 0, j1 = 0, used = 0;
+    int j = 0, j1 = 0, used = 0, index = 0, in_page = 0;  // index: of the table's row
     bool open = false;
     auto next = [&]() {
-      Ahead y;
-      y.there = false;
-      y.page = -1;
-      y.b = y.hk = y.tile = y.len = 0;
-      y.k = y.v = 0;
+      Ahead y{0, -1, 0, 0, false};
       for (;;) {
         if (!open) {
           if (todo <= x.lead) return y;
@@ -435,84 +505,75 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           j = it.tile0;
           j1 = min(it.tile1, it.n_cache);
           used = it.tile1 - it.tile0;
+          const int slot = j * kTile + lane * TT_SCALE_SLOTS;
+          index = slot / a.page_size;
+          in_page = slot % a.page_size;
           open = true;
         }
         if (j < j1) break;
         todo -= used;
-        x.next_item(p);
+        x = next_place<R>(p.a, p.group, x);
         open = false;
       }
       y.there = true;
-      y.b = x.b;
       y.hk = x.hk;
-      y.tile = j++;
-      y.len = x.r.len;
-      const int slot = y.tile * kTile + lane * p.box;
-      if (lane < per && slot < y.len) y.page = a.page_table[x.b * a.table_stride + slot / a.page_size];
+      y.in_page = in_page;
+      if (lane < kGroups && j * kTile + lane * TT_SCALE_SLOTS < x.r.len)
+        y.page = a.page_table[x.b * a.table_stride + index];
+      ++j;
+      index += per_tile;
+      in_page += rest;
+      if (in_page >= a.page_size) {
+        in_page -= a.page_size;
+        ++index;
+      }
       return y;
     };
     auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
-    auto scales = [&](Ahead& y) {
-      if (!y.there) return;
-      const int page = __shfl_sync(0xffffffffu, y.page, (lane % kGroups) * TT_SCALE_SLOTS / p.box);
-      const int slot = y.tile * kTile + lane * TT_SCALE_SLOTS;
-      if (lane < kGroups && slot < y.len && usable(page)) {
-        const int64_t g = slot % a.page_size / TT_SCALE_SLOTS;
-        y.k = p.sc.k.data[page * p.sc.k.page + g * p.sc.k.group + y.hk * p.sc.k.head];
-        y.v = p.sc.v.data[page * p.sc.v.page + g * p.sc.v.group + y.hk * p.sc.v.head];
-      }
-    };
-    Ahead one = next(), two = next();
-    scales(one);
-    int n = 0, k_copies = 0, v_copies = 0;
-    for (; one.there && ok; ++n) {
+    Ahead one, two;
+    one.there = two.there = false;
+    int n = 0;
+#pragma unroll 1
+    for (int k = 0; ok && (k < 2 || one.there); ++k) {
       const Ahead c = one;
       one = two;
-      scales(one);
+      if (one.there && usable(one.page))
+        one.code = sc.data[one.page * sc.page + (one.in_page / TT_SCALE_SLOTS) * sc.group +
+                           one.hk * sc.head];
       two = next();
+      if (!c.there) continue;
       const int st = n % kStages, ring = n % kScaleRing;
-      const uint32_t parity = ((n / kStages) & 1) ^ 1;
-      const int slot = c.tile * kTile + lane * p.box;
       const bool mine = usable(c.page);
-      const unsigned int copied = __ballot_sync(0xffffffffu, mine);
-      const int boxes = __popc(copied);
-      auto copy = [&](char* dst, uint64_t* bar, const CUtensorMap* map) {
-        if (lane == 0) mbar_arrive_expect_tx(bar, boxes * p.box * D);
-        __syncwarp();
-        if (mine) {
-          const int in_page = slot % a.page_size;
-          tma_load_4d(smem_u32(dst) + lane * p.box * D, map, smem_u32(bar), 0,
-                      p.slots_inner ? in_page : c.hk, p.slots_inner ? c.hk : in_page, c.page);
-        }
-        __syncwarp();
-      };
-      ok = __all_sync(0xffffffffu, mbar_wait(&s.k_empty[st], parity, limit)) &&
+      ok = __all_sync(0xffffffffu, wait8(&empty[st], ((n / kStages) & 1) ^ 1, limit)) &&
            (n != 1 || int(blockIdx.x) != p.stall);
       if (!ok) break;
-      // (the scales of kScaleRing tiles ago: rows read them before they free scores of
-      // a tile that this stage's last products came two after)
-      if (lane < kGroups) {
-        s.k_scale[ring][lane] = e8m0(c.k);
-        s.v_scale[ring][lane] = e8m0(c.v);
+      // (The scales in this place are of kScaleRing tiles ago. Keys': a stage's last
+      // products came after rows had freed the scores of two tiles before its own, for
+      // which they had read the scale. Values': they came to be converted after the
+      // product of two tiles before, for which rows and converters had read theirs.)
+      if (lane < kGroups) (values ? s.v_scale : s.k_scale)[ring][lane] = e8m0(c.code);
+      const unsigned int lost = __ballot_sync(0xffffffffu, lane < kGroups && !mine);
+      const int top = __reduce_max_sync(0xffffffffu, c.code != 255 ? int(c.code) : 0);
+      const bool begins = mine && lane * TT_SCALE_SLOTS % p.box == 0;
+      const int boxes = __popc(__ballot_sync(0xffffffffu, begins));
+      if (lane == 0) {
+        s.left_out[values][ring] = lost;
+        if (values) s.top_code[ring] = top;
+        mbar_arrive_expect_tx(&full[st], boxes * p.box * D);
       }
-      const int box_of = (lane % kGroups) * TT_SCALE_SLOTS / p.box;
-      const unsigned int lost = __ballot_sync(0xffffffffu, lane < kGroups && !(copied >> box_of & 1));
-      if (lane == 0) s.left_out[ring] = lost;
       __syncwarp();
+      if (begins)
+        tma_load_4d(smem_u32(dst) + st * (kTile * D) + lane * TT_SCALE_SLOTS * D, map,
+                    smem_u32(&full[st]), 0, p.slots_inner ? c.in_page : c.hk,
+                    p.slots_inner ? c.hk : c.in_page, c.page);
       if (lane == 0) mbar_arrive(&s.scale_full[ring]);
-      copy(s.k[st], &s.k_full[st], &p.kc);
-      ++k_copies;
-      ok = __all_sync(0xffffffffu, mbar_wait(&s.v_empty[st], parity, limit));
-      if (!ok) break;
-      copy(s.v[st], &s.v_full[st], &p.vc);
-      ++v_copies;
+      ++n;
     }
     // (the CTA's memory stays until its last copies have come)
-    for (int st = 0; st < kStages; ++st) {
-      if (k_copies > st) mbar_wait(&s.k_full[st], ((k_copies - 1 - st) / kStages) & 1, limit);
-      if (v_copies > st) mbar_wait(&s.v_full[st], ((v_copies - 1 - st) / kStages) & 1, limit);
-    }
-  } else if (warp == kRowWarps + kConvWarps + 1) {
+#pragma unroll 1
+    for (int st = 0; st < kStages; ++st)
+      if (n > st) wait8(&full[st], ((n - 1 - st) / kStages) & 1, limit);
+  } else if (warp == kRowWarps + kConvWarps) {
     // ---------------------------------------------------------- products
     if (lane == 0) {
       int n = 0, kt = 0, w = 0;  // tiles, the cache's among them, 16-bit operands
@@ -522,21 +583,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         // scores of tile j, the n-th; its drafted keys are operand w_at
         auto scores = [&](int j, int tile, int w_at) {
           const int buf = tile & 1;
-          if (!mbar_wait(&s.s_free[buf], ((tile >> 1) & 1) ^ 1, limit)) return false;
+          if (!wait8(&s.s_free[buf], ((tile >> 1) & 1) ^ 1, limit)) return false;
           const uint32_t to = tmem + buf * S::kScores;
           if (j < it.n_cache) {
             const int st = kt % kStages;
-            if (!mbar_wait(&s.k_full[st], (kt / kStages) & 1, limit)) return false;
+            if (!wait8(&s.k_full[st], (kt / kStages) & 1, limit)) return false;
             tc_fence_after();
             const uint32_t ka = smem_u32(s.k[st]), qa = smem_u32(s.q8);
+            const uint64_t kd = umma8_desc<D>(ka), qd = umma8_desc<D>(qa);
 #pragma unroll
             for (int c = 0; c < D / 32; ++c)
-              umma8_ss(to, umma8_desc<D>(ka + 32 * c), umma8_desc<D>(qa + 32 * c),
-                       idesc_e4m3(S::kScores), c > 0);
+              umma8_ss(to, kd + 2 * c, qd + 2 * c, idesc_e4m3(S::kScores), c > 0);
             umma_commit(&s.k_empty[st]);
             ++kt;
           } else {
-            if (!mbar_wait(&s.w_full[w_at & 1], (w_at >> 1) & 1, limit)) return false;
+            if (!wait8(&s.w_full[w_at & 1], (w_at >> 1) & 1, limit)) return false;
             tc_fence_after();
             const uint32_t ka = smem_u32(s.w[w_at & 1]), qa = smem_u32(s.q16);
 #pragma unroll
@@ -550,41 +611,48 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           if (j + 1 == it.tile1) umma_commit(&s.q_empty);
           return true;
         };
-        ok = mbar_wait(&s.q_full, seg & 1, limit) && scores(it.tile0, n, w);
-        for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n) {
-          if (j >= it.n_cache) ++w;  // (behind the keys)
-          if (j + 1 < it.tile1) {
-            ok = scores(j + 1, n + 1, w + 1);
+        ok = wait8(&s.q_full, seg & 1, limit);
+        // a tile's scores before the product of the one before it, but for the first of
+        // an item, whose queries may not be there yet
+#pragma unroll 1
+        for (int j = it.tile0; j <= it.tile1 && ok; ++j) {
+          if (j < it.tile1) {
+            ok = scores(j, n + (j > it.tile0), w + (j > it.tile0 && j - 1 < it.n_cache ? 1 : j > it.tile0 ? 2 : 0));
             if (!ok) break;
           }
-          ok = mbar_wait(&s.w_full[w & 1], (w >> 1) & 1, limit) &&
-               mbar_wait(&s.p_full, n & 1, limit) &&
-               (j > it.tile0 || mbar_wait(&s.o_free, (seg & 1) ^ 1, limit));
+          if (j == it.tile0) continue;
+          const int i = j - 1;
+          if (i >= it.n_cache) ++w;  // (behind the keys)
+          ok = wait8(&s.w_full[w & 1], (w >> 1) & 1, limit) && wait8(&s.p_full, n & 1, limit) &&
+               (i > it.tile0 || wait8(&s.o_free, (seg & 1) ^ 1, limit));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t va = smem_u32(s.w[w & 1]), pa = smem_u32(s.p);
-          const int steps = (it.keys(x, j) + 15) / 16;
+          const uint64_t vd = umma_desc(smem_u32(s.w[w & 1]), kBlock), pd = umma_desc(smem_u32(s.p), 16);
+          const uint32_t idesc = idesc_mn(F16 || i < it.n_cache, R);
+          const int steps = (it.keys(x, i) + 15) / 16;
           // (heads of 64: the other half of the 128 rows is of what lies behind the
           // operand, the other one or the weights, and nobody reads it)
-          for (int c = 0; c < steps; ++c)
-            umma_ss(tmem + S::kOut, umma_desc(va + c * 2048, kBlock),
-                    umma_desc(pa + c * 2048, 16), idesc_mn(F16, R), j > it.tile0 || c > 0);
+#pragma unroll
+          for (int c = 0; c < kTile / 16; ++c)
+            if (c < steps)
+              umma_ss(tmem + S::kOut, vd + 128 * c, pd + 128 * c, idesc, i > it.tile0 || c > 0);
           umma_commit(&s.w_empty[w & 1]);
           umma_commit(&s.o_done);
           ++w;
+          ++n;
         }
         todo -= it.tile1 - it.tile0;
-        x.next_item(p);
+        x = next_place<R>(p.a, p.group, x);
       }
       // (and until its last products and their arrivals are done)
       umma_commit(&s.drained);
-      mbar_wait(&s.drained, 0, limit);
+      wait8(&s.drained, 0, limit);
     }
   } else if (warp >= kRowWarps) {
     // -------------------------------------------------- queries and values
     const int ct = t - kRowThreads;
     auto wait_for = [&](uint64_t* bar, uint32_t parity) {
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+      if (ok) ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       return ok;
     };
     int vt = 0, w = 0;
@@ -651,25 +719,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           const int st = vt % kStages, ring = vt % kScaleRing;
           if (!wait_for(&s.v_full[st], (vt / kStages) & 1)) break;
           if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
-          const uint32_t lost = s.left_out[ring];
+          // (a thread takes 8 elements of either half of a key: stores of 16 bytes without
+          // bank conflicts)
+          const uint32_t lost = s.left_out[1][ring];
+          constexpr int kPairs = D / 64;
 #pragma unroll 4
-          for (int i = ct; i < steps * 16 * kUnits; i += kConvThreads) {
-            const int key = i / kUnits, u = i % kUnits;
-            uint4 o = make_uint4(0, 0, 0, 0);
-            if (key < keys && !(lost >> (key / TT_SCALE_SLOTS) & 1)) {
-              const uint2 in = *reinterpret_cast<const uint2*>(s.v[st] + key * D + u * 8);
-              const float f = s.v_scale[ring][key / TT_SCALE_SLOTS];
-              float e[8];
+          for (int k = 0; k < kTile * 8 / kConvThreads; ++k) {
+            const int i = k * kConvThreads + ct, key = i / 8, u = i % 8;
+            const bool there = key < keys && !(lost >> (key / TT_SCALE_SLOTS) & 1);
 #pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const uint32_t half = e4m3x2_to_f16x2((k < 2 ? in.x : in.y) >> (k & 1) * 16 & 0xffff);
-                const float2 y = __half22float2(*reinterpret_cast<const __half2*>(&half));
-                e[2 * k] = y.x * f;
-                e[2 * k + 1] = y.y * f;
-              }
-              o = pack16<DT>(e);
+            for (int h = 0; h < kPairs; ++h) {
+              uint2 in = make_uint2(0, 0);
+              if (there) in = *reinterpret_cast<const uint2*>(s.v[st] + key * D + h * 64 + u * 8);
+              *reinterpret_cast<uint4*>(s.w[w & 1] + h * kBlock + swizzled16(key, u)) =
+                  make_uint4(e4m3x2_to_f16x2(in.x & 0xffff), e4m3x2_to_f16x2(in.x >> 16),
+                             e4m3x2_to_f16x2(in.y & 0xffff), e4m3x2_to_f16x2(in.y >> 16));
             }
-            *reinterpret_cast<uint4*>(s.w[w & 1] + (u / 8) * kBlock + swizzled16(key, u % 8)) = o;
           }
           mbar_arrive(&s.v_empty[st]);
           ++vt;
@@ -677,10 +742,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           // Drafted tokens: keys as they are, then values without what is not finite (a
           // token outside its branch would get NaN from it; its own gets it at the end).
           const int base = (j - it.n_cache) * kTile;
+#pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
             const char* from = kv ? a.v : a.k;
             const int64_t ts = kv ? a.v_token : a.k_token, hs = kv ? a.v_head : a.k_head;
+#pragma unroll 1
             for (int i = ct; i < steps * 16 * kUnits; i += kConvThreads) {
               const int key = i / kUnits, u = i % kUnits;
               uint4 o = make_uint4(0, 0, 0, 0);
@@ -722,27 +789,28 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         ++w;
       }
       todo -= it.tile1 - it.tile0;
-      x.next_item(p);
+      x = next_place<R>(p.a, p.group, x);
     }
   } else {
     // -------------------------------------------------------------- rows
     // (while the first copies are on their way: the requests' statuses)
+#pragma unroll 1
     for (int b = blockIdx.x; b < a.B; b += p.ctas) {
       const Request r = request(a, b);
-      const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t));
+      const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t, kRowThreads));
       if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
-    const int quarter = warp & 3, half = warp >> 2, key = quarter * 32 + lane;
+    const int quarter = warp & 3, rows_of = warp >> 2, key = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-    const int barrier = 1 + half;  // of the four warps that hold the same rows
+    const int barrier = 1 + rows_of;  // of the four warps that hold the same rows
     // This warp's j-th chunk of rows: 8 c .. 8 c + 7.
-    auto chunk = [&](int j) { return 2 * j + half; };
+    auto chunk = [&](int j) { return kSubs * j + rows_of; };
     // A warp goes on, or gives up, as one. One that gave up passes the barriers between
     // the warps as often as the others, but waits and arrives no more and writes
     // nothing: so the others give up, too, and all end.
     auto wait_for = [&](uint64_t* bar, uint32_t parity) {
       if (!ok) return;
-      ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, limit));
+      ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       if (!ok && lane == 0) atomicMin(&s.stop, s.end - todo);
     };
     int n = 0, ct = 0;
@@ -754,6 +822,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       if (it.tile1 > it.n_cache) {
         // a token's ancestors: one thread walks up from each token
         sync_of(5, kRowThreads);  // (done with the last ones)
+#pragma unroll 1
         for (int i = t; i < it.end; i += kRowThreads) {
           const int up = a.parents ? a.parents[x.r.first + i] : i - 1;
           s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
@@ -762,34 +831,44 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         sync_of(5, kRowThreads);
         if (t < it.end - token0) {
           const int words = tree_tiles(it.end) * (kTile / 32);
+#pragma unroll 1
           for (int w = 0; w < words; ++w) s.seen[t][w] = 0;
+#pragma unroll 1
           for (int i = token0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
         }
         sync_of(5, kRowThreads);
       }
-      float l[kChunks][8];
+      f32x2 l[kChunks][4];  // sums of the weights, as the scores
 #pragma unroll
       for (int j = 0; j < kChunks; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) l[j][i] = 0.f;
+        for (int i = 0; i < 4; ++i) l[j][i] = 0;
       bool unset = true;
+      int code = 0;  // the output is in units of 2^(code - 127)
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
         const bool cache = j < it.n_cache;
         const int keys = it.keys(x, j);
         bool there = key < keys;
-        float scale = 1.f;
+        float scale = 1.f, value = 1.f;
+        int top_code = kOwnCode;
         if (cache) {
           const int e = ct % kScaleRing;
           wait_for(&s.scale_full[e], (ct / kScaleRing) & 1);
           scale = s.k_scale[e][key / TT_SCALE_SLOTS];
-          there = there && !(s.left_out[e] >> (key / TT_SCALE_SLOTS) & 1);
+          value = s.v_scale[e][key / TT_SCALE_SLOTS];
+          top_code = max(1, s.top_code[e]);
+          there = there && !(s.left_out[0][e] >> (key / TT_SCALE_SLOTS) & 1);
           ++ct;
         }
         wait_for(&s.s_full[n & 1], (n >> 1) & 1);
         tc_fence_after();
         const uint32_t at = mine + (n & 1) * S::kScores;
-        // the scores of this thread's key, as log2
-        float y[kChunks][8];
+        // The scores of this thread's key, two rows to a number; times its row's factor and
+        // with its row's shift they are exponents of weights.
+        const float* factors = cache ? s.factor[ring] : s.own_factor;
+        const int factor_step = cache ? 8 : 0;
+        const bool all_there = __all_sync(0xffffffffu, there);
+        f32x2 z[kChunks][4];
         float over = -INFINITY;
 #pragma unroll
         for (int j2 = 0; j2 < kChunks; ++j2) {
@@ -799,15 +878,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             uint32_t v[kPieces][8];
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) tmem_ld8(at + q * R + 8 * c, v[q]);
-            const float* factor = s.factor[ring] + 8 * c;
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) tmem_wait8(v[q]);
+            const f32x2 sixteenth = pair(1.f / 16, 1.f / 16), scale2 = pair(scale, scale);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float z = __uint_as_float(v[kPieces - 1][i]);
+            for (int i = 0; i < 4; ++i) {
+              f32x2 y = both(v[kPieces - 1], i);
 #pragma unroll
-              for (int q = kPieces - 2; q >= 0; --q) z = fmaf(z, 1.f / 16, __uint_as_float(v[q][i]));
-              y[j2][i] = there ? z * scale * factor[i] : -INFINITY;
+              for (int q = kPieces - 2; q >= 0; --q) y = fma2(y, sixteenth, both(v[q], i));
+              z[j2][i] = mul2(y, scale2);
+            }
+            if (!all_there) {
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                if (!there) z[j2][i] = pair(-INFINITY, -INFINITY);
             }
           } else {
             uint32_t v[8];
@@ -815,15 +899,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             tmem_wait8(v);
             const int word = ((j - it.n_cache) * kTile + key) >> 5;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const bool sees = there && s.seen[s.token[8 * c + i]][word] >> lane & 1;
-              y[j2][i] = sees ? __uint_as_float(v[i]) * p.scale2 : -INFINITY;
-            }
+            for (int i = 0; i < 8; ++i)
+              if (!(there && s.seen[s.token[8 * c + i]][word] >> lane & 1)) v[i] = 0xff800000u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[j2][i] = both(v, i);
           }
           if (!unset) {
-            const float* shift = s.shift + 8 * c;
+            const f32x2* factor = reinterpret_cast<const f32x2*>(factors + factor_step * c);
+            const f32x2* shift = reinterpret_cast<const f32x2*>(s.shift + 8 * c);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) over = fmaxf(over, y[j2][i] + shift[i]);
+            for (int i = 0; i < 4; ++i) {
+              float lo, hi;
+              split(fma2(z[j2][i], factor[i], shift[i]), lo, hi);
+              over = fmaxf(over, fmaxf(lo, hi));
+            }
           }
         }
         tc_fence_before();
@@ -835,13 +924,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
 #pragma unroll
           for (int j2 = 0; j2 < kChunks; ++j2) {
             if (chunk(j2) >= chunks) break;
+            const f32x2* factor =
+                reinterpret_cast<const f32x2*>(factors + factor_step * chunk(j2));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const float m = warp_max(y[j2][i]);
-              if (lane == 8 * j2 + i) top = m;
+            for (int i = 0; i < 4; ++i) {
+              float lo, hi;
+              split(mul2(z[j2][i], factor[i]), lo, hi);
+              lo = warp_max(lo);
+              hi = warp_max(hi);
+              if (lane == 8 * j2 + 2 * i) top = lo;
+              if (lane == 8 * j2 + 2 * i + 1) top = hi;
             }
           }
-          // (lane: the row's number among this half's)
+          // (lane: the row's number among these warps')
           const int row = 8 * chunk(lane / 8) + lane % 8;
           const bool has = lane < 8 * kChunks && row < it.rows;
           if (has) s.part[quarter][row] = top;
@@ -861,31 +956,41 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
               s.fall[row] = 0.f;
             }
             none = __any_sync(0xffffffffu, none);
-            if (lane == 0) s.unset[half] = none;
+            if (lane == 0) s.unset[rows_of] = none;
           }
           sync_of(barrier, 128);
-          unset = s.unset[half];
+          unset = s.unset[rows_of];
 #pragma unroll
           for (int j2 = 0; j2 < kChunks; ++j2) {
             if (chunk(j2) >= chunks) break;
+            const f32x2* fall = reinterpret_cast<const f32x2*>(s.fall + 8 * chunk(j2));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) l[j2][i] *= s.fall[8 * chunk(j2) + i];
+            for (int i = 0; i < 4; ++i) l[j2][i] = mul2(l[j2][i], fall[i]);
           }
         }
-        // weights, and their sums
+        // Weights, and their sums. What the values' scale makes of them is in units of the
+        // largest scale so far; when that rises the output falls.
+        float output_fall = 1.f;
+        if (top_code > code) {
+          output_fall = code > 0 ? e8m0(code) * e8m0_inverse(top_code) : 0.f;
+          code = top_code;
+        }
+        value *= e8m0_inverse(code);
         uint4 out[kChunks];
 #pragma unroll
         for (int j2 = 0; j2 < kChunks; ++j2) {
           const int c = chunk(j2);
           if (c >= chunks) break;
-          const float* shift = s.shift + 8 * c;
+          const f32x2* factor = reinterpret_cast<const f32x2*>(factors + factor_step * c);
+          const f32x2* shift = reinterpret_cast<const f32x2*>(s.shift + 8 * c);
           float e[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            e[i] = ex2_approx(y[j2][i] + shift[i]);
-            l[j2][i] += e[i];
+          for (int i = 0; i < 4; ++i) {
+            const f32x2 y = exp2_pair(fma2(z[j2][i], factor[i], shift[i]));
+            l[j2][i] = add2(l[j2][i], y);
+            split(mul2(y, pair(value, value)), e[2 * i], e[2 * i + 1]);
           }
-          out[j2] = pack16<DT>(e);
+          out[j2] = F16 || cache ? pack16<TT_F16>(e) : pack16<TT_BF16>(e);
         }
         // (the last tile's product is done with the weights' place and with the output)
         if (n > 0) wait_for(&s.o_done, (n - 1) & 1);
@@ -895,13 +1000,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           const int c = chunk(j2);
           if (c >= chunks) break;
           if (ok) *reinterpret_cast<uint4*>(s.p + swizzled16(key, c)) = out[j2];
-          if (raised && j > it.tile0) {
+          if ((raised || output_fall != 1.f) && j > it.tile0) {
             uint32_t v[8];
             tmem_ld8(mine + S::kOut + 8 * c, v);
             tmem_wait8(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              v[i] = __float_as_uint(__uint_as_float(v[i]) * s.fall[8 * c + i]);
+              v[i] = __float_as_uint(__uint_as_float(v[i]) *
+                                     (raised ? s.fall[8 * c + i] * output_fall : output_fall));
             tmem_st8(mine + S::kOut + 8 * c, v);
           }
         }
@@ -916,7 +1022,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
 #pragma unroll
         for (int j2 = 0; j2 < kChunks; ++j2)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sums[8 * j2 + i] = l[j2][i];
+          for (int i = 0; i < 4; ++i) split(l[j2][i], sums[8 * j2 + 2 * i], sums[8 * j2 + 2 * i + 1]);
         const float sum = warp_sums(sums, lane);
         const int row = 8 * chunk(lane / 8 % kChunks) + lane % 8;
         sync_of(barrier, 128);  // (done with s.part and s.fall)
@@ -926,22 +1032,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         const bool has_tree = it.tile1 > it.n_cache;
         // where a row goes: to the output, or to its place in the CTA's piece
         auto place = [&](int r) {
-          return whole ? (int64_t(x.r.first) + (row0 + r) / p.group) * a.Hq + x.hk * p.group +
-                             (row0 + r) % p.group
+          const int token = (row0 + r) / p.group;
+          return whole ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + r - token * p.group
                        : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + r;
         };
         if (quarter == 0 && lane < 8 * kChunks && row < it.rows && ok) {
           const float all = s.part[0][row] + s.part[1][row] + (s.part[2][row] + s.part[3][row]);
           const float m2 = s.ref[row] == -INFINITY ? -INFINITY : s.ref[row] - kOffset;
           s.fall[row] = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
+          const int64_t to = place(row);
           if (!whole)
-            p.part_ml[place(row)] = make_float2(m2, all);
+            p.part_ml[to] = make_float2(m2, all);
           else if (a.lse)
-            a.lse[place(row)] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
+            a.lse[to] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
         }
         sync_of(barrier, 128);
         wait_for(&s.o_done, (n - 1) & 1);
         tc_fence_after();
+        const float unit = e8m0(code);
+        bool odd = false;
+        if (has_tree) odd = lane < kWords && s.odd[ring][lane];
+        odd = __any_sync(0xffffffffu, odd);
         if (D == 128 || quarter < 2) {
 #pragma unroll 1
           for (int j2 = 0; j2 < kChunks; ++j2) {
@@ -950,24 +1061,26 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             uint32_t v[8];
             tmem_ld8(mine + S::kOut + 8 * c, v);
             tmem_wait8(v);
+            // (rows lie side by side, but for where a token ends)
+            int g = (row0 + 8 * c) % p.group;
+            int64_t to = place(8 * c) * D + key;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
               const int r = 8 * c + i;
-              if (r >= it.rows || !ok) continue;
-              float y = __uint_as_float(v[i]);
-              if (has_tree)
-                for (int w = 0; w * 32 < it.end; ++w)
-                  for (uint32_t odd = s.odd[ring][w] & s.seen[s.token[r]][w]; odd; odd &= odd - 1) {
-                    const int64_t peer = int64_t(x.r.first) + w * 32 + __ffs(odd) - 1;
-                    const float z =
-                        load_elem<DT>(a.v + (peer * a.v_token + x.hk * a.v_head + key) * 2);
-                    if (!(fabsf(z) < INFINITY)) y += z;
-                  }
-              const int64_t to = place(r) * D + key;
-              if (whole)
-                store_elem<DT>(a.out + to * 2, y * s.fall[r]);
-              else
-                p.part[to] = y;
+              if (r < it.rows && ok) {
+                float y = __uint_as_float(v[i]) * unit;
+                if (odd)
+                  y += odd_values<DT>(a, s.odd[ring], s.seen[s.token[r]], it.end, x.r.first, x.hk, key);
+                if (whole)
+                  store_elem<DT>(a.out + to * 2, y * s.fall[r]);
+                else
+                  p.part[to] = y;
+              }
+              to += D;
+              if (++g == p.group) {
+                g = 0;
+                if (whole) to += int64_t(a.Hq - p.group) * D;
+              }
             }
           }
         }
@@ -975,12 +1088,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         if (ok) mbar_arrive(&s.o_free);
       }
       todo -= it.tile1 - it.tile0;
-      x.next_item(p);
+      x = next_place<R>(p.a, p.group, x);
     }
   }
   tc_fence_before();
   __syncthreads();
-  if (warp == kRowWarps + kConvWarps + 1) tmem_free(tmem, S::kColumns);
+  if (warp == kRowWarps + kConvWarps) tmem_free(tmem, S::kColumns);
   if (t == 0) p.stop[blockIdx.x] = s.stop;  // (the join tells the requests)
 }
 
@@ -1159,7 +1272,7 @@ cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Rows<R>::kAll);
   cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
   cfg.stream = stream;
   cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, R, F16>, p);

@@ -4,8 +4,10 @@ as for caches of 16 bits.
 
 Tolerances. As there (scores, weights, output), with two additions. Queries meet the
 e4m3 keys as sums of e4m3 pieces, exact but for what lies 2^-21 below a row's largest
-element: that times the keys' sizes joins a score's error. Values are numbers of the
-inputs' type whatever the scale, so they add nothing."""
+element: that times the keys' sizes joins a score's error. Weights of cached keys are
+fp16 numbers in units of the largest scale 2^k of the values, the largest weight at 2^7
+or more: beyond 2^-11 of each, they are off by half of fp16's least number, 2^-25, so 2^-32
+of the largest; times 448 2^k, at most twice the largest value, for every key."""
 import ctypes
 import dataclasses
 import math
@@ -109,6 +111,8 @@ def expected(c, b, scale, skip_pages=()):
     every = every.repeat_interleave(G, 1)
     bound = (1.02 * u * (mean + out.abs()) + (2 * order(es[..., None]) + 2e-5) * mean
              + 2.0 ** -30 * every + 2.0 ** -25)
+    if len(x):
+        bound = bound + 2.0 ** -31 * len(x) * torch.nan_to_num(v[:len(x)].abs()).amax()
     flat = lambda y: y.permute(2, 0, 1).reshape(n, Hkv * G)  # noqa: E731
     return out, bound, flat(lse), flat(es) + 1e-5
 
