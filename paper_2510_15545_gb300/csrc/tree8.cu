@@ -54,10 +54,10 @@ namespace {
 
 constexpr int kTile = 128;                     // keys of a tile
 constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
-// The warps that hold the scores of R rows: twice four, of 32 keys each.
+// The warps that turn scores of R rows into weights: fours, of 32 keys each.
 template <int R>
 struct Rows {
-  static constexpr int kSubs = 2;                         // fours of warps
+  static constexpr int kSubs = R == 64 ? 4 : 2;           // fours of warps
   static constexpr int kChunks = R / 8 / kSubs;           // of 8 rows, of a warp
   static constexpr int kWarps = 4 * kSubs, kThreads = kWarps * 32;
   static constexpr int kAll = kThreads + kConvThreads + 96;  // threads of a CTA
@@ -227,16 +227,19 @@ __device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Reques
 template <int D, int R, bool F16>
 struct Smem8 {
   static constexpr int kPieces = F16 ? 3 : 2;
-  // Tensor memory: two tiles' scores (a column for each piece and row), the output.
-  static constexpr int kScores = kPieces * R, kOut = 2 * kScores;
-  static constexpr int kColumns = kOut + R <= 64 ? 64 : kOut + R <= 128 ? 128 : kOut + R <= 256 ? 256 : 512;
-  static constexpr int kStages = D == 64 ? 6 : R >= 32 ? 3 : 4;  // what 227 KB hold
+  // Tensor memory: two tiles' scores (a column for each piece and row), the output, the
+  // sums of the weights.
+  static constexpr int kScores = kPieces * R, kOut = 2 * kScores, kSums = kOut + R;
+  static constexpr int kColumns = kSums + R <= 128 ? 128 : kSums + R <= 256 ? 256 : 512;
+  // what 227 KB hold
+  static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : 3;
+  static constexpr int kStagesV = D == 64 ? 6 : R == 64 ? 2 : 3;
   char w[2][kTile * D * 2];           // values of 16 bits; a drafted tile's keys too
-  char p[kTile * 128];                // weights, the rows of a key side by side
-  char k[kStages][kTile * D];         // keys and values as they come
+  char p[2][kTile * 128];             // weights, the rows of a key side by side
+  char k[kStagesK][kTile * D];        // keys and values as they come
   char q16[R * D * 2];                // queries for drafted keys,
   char q8[kPieces * R * D];           // and in pieces for the cache's
-  char v[kStages][kTile * D];
+  char v[kStagesV][kTile * D];
   uint32_t seen[R][kWords];           // a token's ancestors and itself
   int16_t up[TT_MAX_TREE];            // parents, -1 for roots
   uint8_t token[R];                   // of a row, from the item's first
@@ -250,9 +253,9 @@ struct Smem8 {
   alignas(16) float fall[R];          // a reference's last change
   float ref[R];                       // reference maximum (log2)
   float part[4][R];                   // what the warps of 32 keys each tell
-  uint64_t k_full[kStages], k_empty[kStages], v_full[kStages], v_empty[kStages];
+  uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
-  uint64_t q_full, q_empty, p_full, o_done, o_free, drained;
+  uint64_t p_full[2], o_done[2], q_full, q_empty, o_free, drained;
   long long sums[Rows<R>::kAll / 32];  // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
@@ -332,6 +335,15 @@ __device__ __forceinline__ bool any_of(int barrier, int threads, bool x) {
 __device__ __forceinline__ void sync_of(int barrier, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
 }
+__device__ __forceinline__ bool elect_one() {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "elect.sync _|p, 0xffffffff;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r));
+  return r != 0;
+}
 // The largest of a warp's numbers (NaN: none).
 __device__ __forceinline__ float warp_max(float x) {
   const int i = x != x ? int(0x807fffff) : __float_as_int(x);  // (-inf)
@@ -374,7 +386,7 @@ template <int D, int R, bool F16>
 __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
-  constexpr int kPieces = S::kPieces, kStages = S::kStages;
+  constexpr int kPieces = S::kPieces;
   // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
   // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
   constexpr int kOwnCode = F16 ? 127 : 67;
@@ -386,14 +398,17 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
   extern __shared__ char raw[];
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
   const TreeArgs& a = p.a;
-  const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+  // (a number that is the same in all lanes, and known to be)
+  const int t = threadIdx.x, warp = __shfl_sync(0xffffffffu, t >> 5, 0), lane = t & 31;
   const uint64_t& limit = p.wait_ns;
   grid_launch_dependents();
 
   if (t == kRowThreads) {
-    for (int i = 0; i < kStages; ++i) {
+    for (int i = 0; i < S::kStagesK; ++i) {
       mbar_init(&s.k_full[i], 1);
       mbar_init(&s.k_empty[i], 1);
+    }
+    for (int i = 0; i < S::kStagesV; ++i) {
       mbar_init(&s.v_full[i], 1);
       mbar_init(&s.v_empty[i], kConvThreads);
     }
@@ -403,11 +418,11 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
       mbar_init(&s.w_empty[i], 1);
       mbar_init(&s.s_full[i], 1);
       mbar_init(&s.s_free[i], kRowThreads);
+      mbar_init(&s.p_full[i], kRowThreads);
+      mbar_init(&s.o_done[i], 1);
     }
     mbar_init(&s.q_full, kConvThreads);
     mbar_init(&s.q_empty, 1);
-    mbar_init(&s.p_full, kRowThreads);
-    mbar_init(&s.o_done, 1);
     mbar_init(&s.o_free, kRowThreads);
     mbar_init(&s.drained, 1);
     s.stop = INT32_MAX;
@@ -486,6 +501,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
     char* const dst = values ? &s.v[0][0] : &s.k[0][0];
     uint64_t* const full = values ? s.v_full : s.k_full;
     uint64_t* const empty = values ? s.v_empty : s.k_empty;
+    const int stages = values ? S::kStagesV : S::kStagesK;
     const CUtensorMap* const map = values ? &p.vc : &p.kc;
     const int per_tile = kTile / a.page_size, rest = kTile % a.page_size;
     struct Ahead {
@@ -532,7 +548,8 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
     auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
     Ahead one, two;
     one.there = two.there = false;
-    int n = 0;
+    int n = 0, st = 0;
+    uint32_t parity = 1;
 #pragma unroll 1
     for (int k = 0; ok && (k < 2 || one.there); ++k) {
       const Ahead c = one;
@@ -542,9 +559,9 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
                            one.hk * sc.head];
       two = next();
       if (!c.there) continue;
-      const int st = n % kStages, ring = n % kScaleRing;
+      const int ring = n % kScaleRing;
       const bool mine = usable(c.page);
-      ok = __all_sync(0xffffffffu, wait8(&empty[st], ((n / kStages) & 1) ^ 1, limit)) &&
+      ok = __all_sync(0xffffffffu, wait8(&empty[st], parity, limit)) &&
            (n != 1 || int(blockIdx.x) != p.stall);
       if (!ok) break;
       // (The scales in this place are of kScaleRing tiles ago. Keys': a stage's last
@@ -568,86 +585,105 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
                     p.slots_inner ? c.hk : c.in_page, c.page);
       if (lane == 0) mbar_arrive(&s.scale_full[ring]);
       ++n;
+      if (++st == stages) {
+        st = 0;
+        parity ^= 1;
+      }
     }
     // (the CTA's memory stays until its last copies have come)
 #pragma unroll 1
-    for (int st = 0; st < kStages; ++st)
-      if (n > st) wait8(&full[st], ((n - 1 - st) / kStages) & 1, limit);
+    for (int i = 0; i < stages; ++i)
+      if (n > i) wait8(&full[i], ((n - 1 - i) / stages) & 1, limit);
   } else if (warp == kRowWarps + kConvWarps) {
     // ---------------------------------------------------------- products
-    if (lane == 0) {
-      int n = 0, kt = 0, w = 0;  // tiles, the cache's among them, 16-bit operands
-      for (int seg = 0; todo > x.lead && ok; ++seg) {
-        todo -= x.lead;
-        const Item<R> it(p, x, todo);
-        // scores of tile j, the n-th; its drafted keys are operand w_at
-        auto scores = [&](int j, int tile, int w_at) {
-          const int buf = tile & 1;
-          if (!wait8(&s.s_free[buf], ((tile >> 1) & 1) ^ 1, limit)) return false;
+    // (the whole warp goes along, one lane issues: operands then are uniform registers)
+    const uint64_t kd = umma8_desc<D>(smem_u32(s.k)), qd = umma8_desc<D>(smem_u32(s.q8)),
+                   od = umma_desc(smem_u32(s.q16), 16), wk = umma_desc(smem_u32(s.w), 16),
+                   wv = umma_desc(smem_u32(s.w), kBlock), pd = umma_desc(smem_u32(s.p), 16);
+    constexpr uint32_t kWStep = kTile * D * 2 / 16, kKStep = kTile * D / 16, kPStep = kTile * 128 / 16;
+    auto on = [&](uint64_t* bar, uint32_t parity) {
+      return __all_sync(0xffffffffu, wait8(bar, parity, limit)) != 0;
+    };
+    int n = 0, kt = 0, kst = 0, w = 0;  // tiles, the cache's among them, 16-bit operands
+#pragma unroll 1
+    for (int seg = 0; todo > x.lead && ok; ++seg) {
+      todo -= x.lead;
+      const Item<R> it(p, x, todo);
+      ok = on(&s.q_full, seg & 1);
+      // A tile's scores before the product of the one before it, but for the first of an
+      // item, whose queries may not be there yet.
+#pragma unroll 1
+      for (int j = it.tile0; j <= it.tile1 && ok; ++j) {
+        const int i = j - 1;
+        if (j < it.tile1) {
+          const int tile = n + (j > it.tile0), buf = tile & 1;
+          ok = on(&s.s_free[buf], ((tile >> 1) & 1) ^ 1);
+          if (!ok) break;
           const uint32_t to = tmem + buf * S::kScores;
           if (j < it.n_cache) {
-            const int st = kt % kStages;
-            if (!wait8(&s.k_full[st], (kt / kStages) & 1, limit)) return false;
-            tc_fence_after();
-            const uint32_t ka = smem_u32(s.k[st]), qa = smem_u32(s.q8);
-            const uint64_t kd = umma8_desc<D>(ka), qd = umma8_desc<D>(qa);
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c)
-              umma8_ss(to, kd + 2 * c, qd + 2 * c, idesc_e4m3(S::kScores), c > 0);
-            umma_commit(&s.k_empty[st]);
-            ++kt;
-          } else {
-            if (!wait8(&s.w_full[w_at & 1], (w_at >> 1) & 1, limit)) return false;
-            tc_fence_after();
-            const uint32_t ka = smem_u32(s.w[w_at & 1]), qa = smem_u32(s.q16);
-#pragma unroll
-            for (int c = 0; c < D / 16; ++c)
-              umma_ss(to, umma_desc(ka + (c / 4) * kBlock + (c % 4) * 32, 16),
-                      umma_desc(qa + (c / 4) * (R * 128) + (c % 4) * 32, 16), umma_idesc(F16, R, false),
-                      c > 0);
-            umma_commit(&s.w_empty[w_at & 1]);
-          }
-          umma_commit(&s.s_full[buf]);
-          if (j + 1 == it.tile1) umma_commit(&s.q_empty);
-          return true;
-        };
-        ok = wait8(&s.q_full, seg & 1, limit);
-        // a tile's scores before the product of the one before it, but for the first of
-        // an item, whose queries may not be there yet
-#pragma unroll 1
-        for (int j = it.tile0; j <= it.tile1 && ok; ++j) {
-          if (j < it.tile1) {
-            ok = scores(j, n + (j > it.tile0), w + (j > it.tile0 && j - 1 < it.n_cache ? 1 : j > it.tile0 ? 2 : 0));
+            ok = on(&s.k_full[kst], kt & 1);
             if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int c = 0; c < D / 32; ++c)
+                umma8_ss(to, kd + kst * kKStep + 2 * c, qd + 2 * c, idesc_e4m3(S::kScores), c > 0);
+              umma_commit(&s.s_full[buf]);
+              umma_commit(&s.k_empty[kst]);
+              if (j + 1 == it.tile1) umma_commit(&s.q_empty);
+            }
+            if (++kst == S::kStagesK) {
+              kst = 0;
+              ++kt;
+            }
+          } else {
+            // (its drafted keys lie behind the last tile's values, and behind its keys)
+            const int at = w + (j > it.tile0) + (j > it.tile0 && i >= it.n_cache);
+            ok = on(&s.w_full[at & 1], (at >> 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+#pragma unroll
+              for (int c = 0; c < D / 16; ++c)
+                umma_ss(to, wk + (at & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
+                        od + (c / 4) * (R * 128 / 16) + (c % 4) * 2, umma_idesc(F16, R, false), c > 0);
+              umma_commit(&s.s_full[buf]);
+              umma_commit(&s.w_empty[at & 1]);
+              if (j + 1 == it.tile1) umma_commit(&s.q_empty);
+            }
           }
-          if (j == it.tile0) continue;
-          const int i = j - 1;
-          if (i >= it.n_cache) ++w;  // (behind the keys)
-          ok = wait8(&s.w_full[w & 1], (w >> 1) & 1, limit) && wait8(&s.p_full, n & 1, limit) &&
-               (i > it.tile0 || wait8(&s.o_free, (seg & 1) ^ 1, limit));
-          if (!ok) break;
-          tc_fence_after();
-          const uint64_t vd = umma_desc(smem_u32(s.w[w & 1]), kBlock), pd = umma_desc(smem_u32(s.p), 16);
-          const uint32_t idesc = idesc_mn(F16 || i < it.n_cache, R);
-          const int steps = (it.keys(x, i) + 15) / 16;
-          // (heads of 64: the other half of the 128 rows is of what lies behind the
-          // operand, the other one or the weights, and nobody reads it)
+          __syncwarp();
+        }
+        if (j == it.tile0) continue;
+        if (i >= it.n_cache) ++w;  // (behind the keys)
+        ok = on(&s.w_full[w & 1], (w >> 1) & 1) && on(&s.p_full[n & 1], (n >> 1) & 1) &&
+             (i > it.tile0 || on(&s.o_free, (seg & 1) ^ 1));
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t idesc = idesc_mn(F16 || i < it.n_cache, R);
+        const int steps = (it.keys(x, i) + 15) / 16;
+        // (heads of 64: the other half of the 128 rows is of what lies behind the operand,
+        // the other one or the weights, and nobody reads it)
+        if (elect_one()) {
 #pragma unroll
           for (int c = 0; c < kTile / 16; ++c)
             if (c < steps)
-              umma_ss(tmem + S::kOut, vd + 128 * c, pd + 128 * c, idesc, i > it.tile0 || c > 0);
+              umma_ss(tmem + S::kOut, wv + (w & 1) * kWStep + 128 * c, pd + (n & 1) * kPStep + 128 * c,
+                      idesc, i > it.tile0 || c > 0);
+          umma_commit(&s.o_done[n & 1]);
           umma_commit(&s.w_empty[w & 1]);
-          umma_commit(&s.o_done);
-          ++w;
-          ++n;
         }
-        todo -= it.tile1 - it.tile0;
-        x = next_place<R>(p.a, p.group, x);
+        __syncwarp();
+        ++w;
+        ++n;
       }
-      // (and until its last products and their arrivals are done)
-      umma_commit(&s.drained);
-      wait8(&s.drained, 0, limit);
+      todo -= it.tile1 - it.tile0;
+      x = next_place<R>(p.a, p.group, x);
     }
+    // (and until its last products and their arrivals are done)
+    if (elect_one()) umma_commit(&s.drained);
+    __syncwarp();
+    on(&s.drained, 0);
   } else if (warp >= kRowWarps) {
     // -------------------------------------------------- queries and values
     const int ct = t - kRowThreads;
@@ -655,7 +691,8 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
       if (ok) ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       return ok;
     };
-    int vt = 0, w = 0;
+    int vt = 0, st = 0, w = 0;
+    uint32_t parity = 0;
     for (int seg = 0; todo > x.lead && ok; ++seg) {
       todo -= x.lead;
       const Item<R> it(p, x, todo);
@@ -716,8 +753,8 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         const int keys = it.keys(x, j), steps = (keys + 15) / 16;  // (others are not multiplied)
         constexpr int kUnits = D / 8;  // of 8 elements, of a key
         if (j < it.n_cache) {
-          const int st = vt % kStages, ring = vt % kScaleRing;
-          if (!wait_for(&s.v_full[st], (vt / kStages) & 1)) break;
+          const int ring = vt % kScaleRing;
+          if (!wait_for(&s.v_full[st], parity)) break;
           if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
           // (a thread takes 8 elements of either half of a key: stores of 16 bytes without
           // bank conflicts)
@@ -738,6 +775,10 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
           }
           mbar_arrive(&s.v_empty[st]);
           ++vt;
+          if (++st == S::kStagesV) {
+            st = 0;
+            parity ^= 1;
+          }
         } else {
           // Drafted tokens: keys as they are, then values without what is not finite (a
           // token outside its branch would get NaN from it; its own gets it at the end).
@@ -803,8 +844,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
     const int quarter = warp & 3, rows_of = warp >> 2, key = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
     const int barrier = 1 + rows_of;  // of the four warps that hold the same rows
-    // This warp's j-th chunk of rows: 8 c .. 8 c + 7.
-    auto chunk = [&](int j) { return kSubs * j + rows_of; };
+    // This warp's chunks of rows, 8 c .. 8 c + 7: c = rows_of, rows_of + kSubs, ...
     // A warp goes on, or gives up, as one. One that gave up passes the barriers between
     // the warps as often as the others, but waits and arrives no more and writes
     // nothing: so the others give up, too, and all end.
@@ -838,17 +878,19 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         }
         sync_of(5, kRowThreads);
       }
-      f32x2 l[kChunks][4];  // sums of the weights, as the scores
-#pragma unroll
-      for (int j = 0; j < kChunks; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) l[j][i] = 0;
+      // sums of the weights, from nothing
+#pragma unroll 1
+      for (int c = rows_of; c < chunks; c += kSubs) {
+        const uint32_t zero[8] = {};
+        tmem_st8(mine + S::kSums + 8 * c, zero);
+      }
+      tmem_wait_st();
       bool unset = true;
       int code = 0;  // the output is in units of 2^(code - 127)
+#pragma unroll 1
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
         const bool cache = j < it.n_cache;
-        const int keys = it.keys(x, j);
-        bool there = key < keys;
+        bool there = key < it.keys(x, j);
         float scale = 1.f, value = 1.f;
         int top_code = kOwnCode;
         if (cache) {
@@ -863,35 +905,32 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         wait_for(&s.s_full[n & 1], (n >> 1) & 1);
         tc_fence_after();
         const uint32_t at = mine + (n & 1) * S::kScores;
-        // The scores of this thread's key, two rows to a number; times its row's factor and
-        // with its row's shift they are exponents of weights.
-        const float* factors = cache ? s.factor[ring] : s.own_factor;
-        const int factor_step = cache ? 8 : 0;
+        const f32x2 scale2 = pair(scale, scale);
         const bool all_there = __all_sync(0xffffffffu, there);
-        f32x2 z[kChunks][4];
-        float over = -INFINITY;
-#pragma unroll
-        for (int j2 = 0; j2 < kChunks; ++j2) {
-          const int c = chunk(j2);
-          if (c >= chunks) break;
+        // The scores of this thread's key with the rows of chunk c, two to a number; times
+        // its row's factor and with its row's shift they are exponents of weights. (They
+        // are read again where they are needed again: the loops over chunks are rolled, as
+        // unrolled code of this size came from beyond the instruction caches: TODO.)
+        const float* const factors = cache ? s.factor[ring] : s.own_factor;
+        const int factor_step = cache ? 4 : 0;
+        auto scores = [&](int c, f32x2 (&z)[4]) {
           if (cache) {
             uint32_t v[kPieces][8];
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) tmem_ld8(at + q * R + 8 * c, v[q]);
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) tmem_wait8(v[q]);
-            const f32x2 sixteenth = pair(1.f / 16, 1.f / 16), scale2 = pair(scale, scale);
+            const f32x2 sixteenth = pair(1.f / 16, 1.f / 16);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               f32x2 y = both(v[kPieces - 1], i);
 #pragma unroll
               for (int q = kPieces - 2; q >= 0; --q) y = fma2(y, sixteenth, both(v[q], i));
-              z[j2][i] = mul2(y, scale2);
+              z[i] = mul2(y, scale2);
             }
-            if (!all_there) {
+            if (!all_there && !there) {
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (!there) z[j2][i] = pair(-INFINITY, -INFINITY);
+              for (int i = 0; i < 4; ++i) z[i] = pair(-INFINITY, -INFINITY);
             }
           } else {
             uint32_t v[8];
@@ -902,49 +941,38 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
             for (int i = 0; i < 8; ++i)
               if (!(there && s.seen[s.token[8 * c + i]][word] >> lane & 1)) v[i] = 0xff800000u;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[j2][i] = both(v, i);
+            for (int i = 0; i < 4; ++i) z[i] = both(v, i);
           }
-          if (!unset) {
-            const f32x2* factor = reinterpret_cast<const f32x2*>(factors + factor_step * c);
-            const f32x2* shift = reinterpret_cast<const f32x2*>(s.shift + 8 * c);
+        };
+        auto factor = [&](int c) { return reinterpret_cast<const f32x2*>(factors) + factor_step * c; };
+        auto shift = [&](int c) { return reinterpret_cast<const f32x2*>(s.shift + 8 * c); };
+        // New references, where a row's maximum is above its own by more than kSlack (or it
+        // has none), and what that makes of the output.
+        auto raise = [&] {
+#pragma unroll 1
+          for (int c = rows_of; c < chunks; c += kSubs) {
+            f32x2 z[4];
+            scores(c, z);
+            float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               float lo, hi;
-              split(fma2(z[j2][i], factor[i], shift[i]), lo, hi);
-              over = fmaxf(over, fmaxf(lo, hi));
-            }
-          }
-        }
-        tc_fence_before();
-        if (ok) mbar_arrive(&s.s_free[n & 1]);
-        // the references follow the maxima, and with them the sums
-        const bool raised = unset || any_of(barrier, 128, over > kSlack + kOffset);
-        if (raised) {
-          float top = -INFINITY;
-#pragma unroll
-          for (int j2 = 0; j2 < kChunks; ++j2) {
-            if (chunk(j2) >= chunks) break;
-            const f32x2* factor =
-                reinterpret_cast<const f32x2*>(factors + factor_step * chunk(j2));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float lo, hi;
-              split(mul2(z[j2][i], factor[i]), lo, hi);
+              split(mul2(z[i], factor(c)[i]), lo, hi);
               lo = warp_max(lo);
               hi = warp_max(hi);
-              if (lane == 8 * j2 + 2 * i) top = lo;
-              if (lane == 8 * j2 + 2 * i + 1) top = hi;
+              if (lane == 2 * i) top = lo;
+              if (lane == 2 * i + 1) top = hi;
             }
+            if (lane < 8) s.part[quarter][8 * c + lane] = top;
           }
-          // (lane: the row's number among these warps')
-          const int row = 8 * chunk(lane / 8) + lane % 8;
-          const bool has = lane < 8 * kChunks && row < it.rows;
-          if (has) s.part[quarter][row] = top;
           sync_of(barrier, 128);
           if (quarter == 0) {
+            // (lane: the row's number among these warps')
+            const int row = 8 * (kSubs * (lane / 8) + rows_of) + lane % 8;
             bool none = false;
-            if (has) {
-              top = fmaxf(fmaxf(s.part[0][row], s.part[1][row]), fmaxf(s.part[2][row], s.part[3][row]));
+            if (lane < 8 * kChunks && row < it.rows) {
+              const float top = fmaxf(fmaxf(s.part[0][row], s.part[1][row]),
+                                      fmaxf(s.part[2][row], s.part[3][row]));
               const float old = j == it.tile0 ? -INFINITY : s.ref[row];
               const float to = top - old > kSlack || old == -INFINITY ? fmaxf(old, top) : old;
               s.ref[row] = to;
@@ -960,73 +988,118 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
           }
           sync_of(barrier, 128);
           unset = s.unset[rows_of];
-#pragma unroll
-          for (int j2 = 0; j2 < kChunks; ++j2) {
-            if (chunk(j2) >= chunks) break;
-            const f32x2* fall = reinterpret_cast<const f32x2*>(s.fall + 8 * chunk(j2));
-#pragma unroll
-            for (int i = 0; i < 4; ++i) l[j2][i] = mul2(l[j2][i], fall[i]);
-          }
-        }
-        // Weights, and their sums. What the values' scale makes of them is in units of the
-        // largest scale so far; when that rises the output falls.
+        };
+        // What the values' scale makes of weights is in units of the largest scale so far;
+        // when that rises the output falls.
         float output_fall = 1.f;
         if (top_code > code) {
           output_fall = code > 0 ? e8m0(code) * e8m0_inverse(top_code) : 0.f;
           code = top_code;
         }
         value *= e8m0_inverse(code);
-        uint4 out[kChunks];
-#pragma unroll
-        for (int j2 = 0; j2 < kChunks; ++j2) {
-          const int c = chunk(j2);
-          if (c >= chunks) break;
-          const f32x2* factor = reinterpret_cast<const f32x2*>(factors + factor_step * c);
-          const f32x2* shift = reinterpret_cast<const f32x2*>(s.shift + 8 * c);
-          float e[8];
+        const f32x2 value2 = pair(value, value);
+        char* const weights = s.p[n & 1] + key * 128;
+        const bool early = unset;
+        if (early) raise();
+        // (the product of two tiles ago is done with the weights' place)
+        wait_for(&s.o_done[n & 1], ((n >> 1) & 1) ^ 1);
+        float over = -INFINITY;
+#pragma unroll 1
+        for (int c = rows_of; c < chunks; c += kSubs) {
+          f32x2 z[4];
+          uint32_t l[8];
+          tmem_ld8(mine + S::kSums + 8 * c, l);
+          scores(c, z);
+          tmem_wait8(l);
+          uint32_t out[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const f32x2 y = exp2_pair(fma2(z[j2][i], factor[i], shift[i]));
-            l[j2][i] = add2(l[j2][i], y);
-            split(mul2(y, pair(value, value)), e[2 * i], e[2 * i + 1]);
+            const f32x2 y = fma2(z[i], factor(c)[i], shift(c)[i]);
+            float lo, hi;
+            split(y, lo, hi);
+            over = fmaxf(over, fmaxf(lo, hi));
+            f32x2 e = exp2_pair(y), sum = both(l, i);
+            if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(s.fall + 8 * c)[i]);
+            sum = add2(sum, e);
+            split(sum, lo, hi);
+            l[2 * i] = __float_as_uint(lo);
+            l[2 * i + 1] = __float_as_uint(hi);
+            split(mul2(e, value2), lo, hi);
+            out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
           }
-          out[j2] = F16 || cache ? pack16<TT_F16>(e) : pack16<TT_BF16>(e);
+          tmem_st8(mine + S::kSums + 8 * c, l);
+          *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
+              make_uint4(out[0], out[1], out[2], out[3]);
         }
-        // (the last tile's product is done with the weights' place and with the output)
-        if (n > 0) wait_for(&s.o_done, (n - 1) & 1);
-        tc_fence_after();
+        // A weight that is too large, seldom: new references, weights again. (The sums were
+        // added to in 32 bits, which hold them, or the old ones are nothing to the new.)
+        const bool raised = !early && any_of(barrier, 128, over > kSlack + kOffset);
+        if (raised) {
+          raise();
+#pragma unroll 1
+          for (int c = rows_of; c < chunks; c += kSubs) {
+            f32x2 z[4];
+            uint32_t l[8];
+            tmem_wait_st();
+            tmem_ld8(mine + S::kSums + 8 * c, l);
+            scores(c, z);
+            tmem_wait8(l);
+            uint32_t out[4];
 #pragma unroll
-        for (int j2 = 0; j2 < kChunks; ++j2) {
-          const int c = chunk(j2);
-          if (c >= chunks) break;
-          if (ok) *reinterpret_cast<uint4*>(s.p + swizzled16(key, c)) = out[j2];
-          if ((raised || output_fall != 1.f) && j > it.tile0) {
+            for (int i = 0; i < 4; ++i) {
+              float e[2], lo, hi;
+              split(exp2_pair(fma2(z[i], factor(c)[i], shift(c)[i])), e[0], e[1]);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const float fall = s.fall[8 * c + 2 * i + k];
+                l[2 * i + k] = __float_as_uint(
+                    fall > 0x1p-60f ? __uint_as_float(l[2 * i + k]) * fall : e[k]);
+              }
+              split(mul2(pair(e[0], e[1]), value2), lo, hi);
+              out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
+            }
+            tmem_st8(mine + S::kSums + 8 * c, l);
+            *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
+                make_uint4(out[0], out[1], out[2], out[3]);
+          }
+        }
+        tc_fence_before();
+        if (ok) mbar_arrive(&s.s_free[n & 1]);
+        if ((raised || early || output_fall != 1.f) && j > it.tile0) {
+          wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = rows_of; c < chunks; c += kSubs) {
             uint32_t v[8];
             tmem_ld8(mine + S::kOut + 8 * c, v);
             tmem_wait8(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              v[i] = __float_as_uint(__uint_as_float(v[i]) *
-                                     (raised ? s.fall[8 * c + i] * output_fall : output_fall));
+              v[i] = __float_as_uint(__uint_as_float(v[i]) * output_fall *
+                                     (raised || early ? s.fall[8 * c + i] : 1.f));
             tmem_st8(mine + S::kOut + 8 * c, v);
           }
         }
         tmem_wait_st();
         fence_proxy_async();
         tc_fence_before();
-        if (ok) mbar_arrive(&s.p_full);
+        if (ok) mbar_arrive(&s.p_full[n & 1]);
       }
-      // the sums of all keys, a row to a lane
+      // the sums of all keys
       {
-        float sums[8 * kChunks];
-#pragma unroll
-        for (int j2 = 0; j2 < kChunks; ++j2)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) split(l[j2][i], sums[8 * j2 + 2 * i], sums[8 * j2 + 2 * i + 1]);
-        const float sum = warp_sums(sums, lane);
-        const int row = 8 * chunk(lane / 8 % kChunks) + lane % 8;
+        const int row = 8 * (kSubs * (lane / 8) + rows_of) + lane % 8;
         sync_of(barrier, 128);  // (done with s.part and s.fall)
-        if (lane < 8 * kChunks && row < it.rows) s.part[quarter][row] = sum;
+#pragma unroll 1
+        for (int c = rows_of; c < chunks; c += kSubs) {
+          uint32_t l[8];
+          tmem_ld8(mine + S::kSums + 8 * c, l);
+          tmem_wait8(l);
+          float sums[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
+          const float sum = warp_sums(sums, lane);
+          if (lane < 8) s.part[quarter][8 * c + lane] = sum;
+        }
         sync_of(barrier, 128);
         const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
         const bool has_tree = it.tile1 > it.n_cache;
@@ -1047,7 +1120,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
             a.lse[to] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
         }
         sync_of(barrier, 128);
-        wait_for(&s.o_done, (n - 1) & 1);
+        wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
         tc_fence_after();
         const float unit = e8m0(code);
         bool odd = false;
@@ -1055,9 +1128,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         odd = __any_sync(0xffffffffu, odd);
         if (D == 128 || quarter < 2) {
 #pragma unroll 1
-          for (int j2 = 0; j2 < kChunks; ++j2) {
-            const int c = chunk(j2);
-            if (c >= chunks) break;
+          for (int c = rows_of; c < chunks; c += kSubs) {
             uint32_t v[8];
             tmem_ld8(mine + S::kOut + 8 * c, v);
             tmem_wait8(v);
