@@ -54,12 +54,16 @@ namespace {
 
 constexpr int kTile = 128;                     // keys of a tile
 constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
-// The warps that turn scores of R rows into weights: fours, of 32 keys each.
-template <int R>
+// The warps that turn scores of R rows into weights: fours, of 32 keys each. Where tensor
+// memory has room for two outputs, half of them takes the even tiles and half the odd
+// ones, each with references, sums and an output of its own: what a tile takes from its
+// scores to its weights is mostly waiting, and so two are on their way.
+template <int R, bool F16>
 struct Rows {
-  static constexpr int kSubs = R == 64 ? 4 : 2;           // fours of warps
-  static constexpr int kChunks = R / 8 / kSubs;           // of 8 rows, of a warp
-  static constexpr int kWarps = 4 * kSubs, kThreads = kWarps * 32;
+  static constexpr int kSets = F16 && R == 64 ? 1 : 2;
+  static constexpr int kSubs = R == 16 ? 1 : 4 / kSets;    // fours of a set, which share its rows
+  static constexpr int kChunks = R / 8 / kSubs;            // of 8 rows, of a warp, at most
+  static constexpr int kFours = kSets * kSubs, kWarps = 4 * kFours, kThreads = kWarps * 32;
   static constexpr int kAll = kThreads + kConvThreads + 96;  // threads of a CTA
 };
 constexpr int kWords = TT_MAX_TREE / 32;
@@ -227,10 +231,13 @@ __device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Reques
 template <int D, int R, bool F16>
 struct Smem8 {
   static constexpr int kPieces = F16 ? 3 : 2;
-  // Tensor memory: two tiles' scores (a column for each piece and row), the output, the
+  // Tensor memory: two tiles' scores (a column for each piece and row), the outputs, the
   // sums of the weights.
-  static constexpr int kScores = kPieces * R, kOut = 2 * kScores, kSums = kOut + R;
-  static constexpr int kColumns = kSums + R <= 128 ? 128 : kSums + R <= 256 ? 256 : 512;
+  static constexpr int kSets = Rows<R, F16>::kSets;
+  static constexpr int kScores = kPieces * R, kOut = 2 * kScores, kSums = kOut + kSets * R;
+  static constexpr int kUsed = kSums + kSets * R;
+  static constexpr int kColumns = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+  static_assert(kUsed <= 512, "tensor memory");
   // what 227 KB hold
   static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : 3;
   static constexpr int kStagesV = D == 64 ? 6 : R == 64 ? 2 : 3;
@@ -249,14 +256,15 @@ struct Smem8 {
   alignas(16) float factor[kItemRing][R];         // a row's pieces times it and a key's scale: log2 scores
   alignas(16) float own_factor[8];                // the same of drafted keys
   uint32_t odd[kItemRing][kWords];    // drafted tokens with a value that is not finite
-  alignas(16) float shift[R];         // what is added to log2 scores
-  alignas(16) float fall[R];          // a reference's last change
-  float ref[R];                       // reference maximum (log2)
-  float part[4][R];                   // what the warps of 32 keys each tell
+  alignas(16) float shift[kSets][R];  // what is added to log2 scores
+  alignas(16) float fall[kSets][R];   // a reference's last change; at the end, outputs' factors
+  float ref[kSets][R];                // reference maximum (log2)
+  float part[kSets][4][R];            // what the warps of 32 keys each tell
+  int code[kSets];                    // units of the outputs, 0: no tile
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
   uint64_t p_full[2], o_done[2], q_full, q_empty, o_free, drained;
-  long long sums[Rows<R>::kAll / 32];  // places of the requests, by warps
+  long long sums[Rows<R, F16>::kAll / 32];  // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
   int unset[4];                       // rows of four warps without a reference yet
@@ -383,7 +391,7 @@ __device__ __noinline__ float odd_values(const TreeArgs& a, const uint32_t* odd,
 }
 
 template <int D, int R, bool F16>
-__global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
+__global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
   constexpr int kPieces = S::kPieces;
@@ -391,9 +399,10 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
   // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
   constexpr int kOwnCode = F16 ? 127 : 67;
   constexpr int kBlock = kTile * 128;         // distance of the 64-element blocks of a 16-bit tile
-  constexpr int kSubs = Rows<R>::kSubs, kChunks = Rows<R>::kChunks;
-  constexpr int kRowWarps = Rows<R>::kWarps, kRowThreads = Rows<R>::kThreads;
-  constexpr int kThreads = Rows<R>::kAll;
+  constexpr int kSets = Rows<R, F16>::kSets, kSubs = Rows<R, F16>::kSubs;
+  constexpr int kChunks = Rows<R, F16>::kChunks, kFours = Rows<R, F16>::kFours;
+  constexpr int kRowWarps = Rows<R, F16>::kWarps, kRowThreads = Rows<R, F16>::kThreads;
+  constexpr int kThreads = Rows<R, F16>::kAll;
   constexpr float kOffset = 7.f;              // fp16 weights: away from its small end
   extern __shared__ char raw[];
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
@@ -417,8 +426,8 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
       mbar_init(&s.w_full[i], kConvThreads);
       mbar_init(&s.w_empty[i], 1);
       mbar_init(&s.s_full[i], 1);
-      mbar_init(&s.s_free[i], kRowThreads);
-      mbar_init(&s.p_full[i], kRowThreads);
+      mbar_init(&s.s_free[i], kRowThreads / kSets);
+      mbar_init(&s.p_full[i], kRowThreads / kSets);
       mbar_init(&s.o_done[i], 1);
     }
     mbar_init(&s.q_full, kConvThreads);
@@ -506,13 +515,16 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
     const int per_tile = kTile / a.page_size, rest = kTile % a.page_size;
     struct Ahead {
       int hk, page, in_page;  // of the lane's slots
+      const uint8_t* scales;
       uint32_t code;
       bool there;
     };
-    int j = 0, j1 = 0, used = 0, index = 0, in_page = 0;  // index: of the table's row
+    int j = 0, j1 = 0, used = 0, left = 0, in_page = 0;
+    const int32_t* pages = nullptr;    // from this tile's on
+    const uint8_t* scales = nullptr;   // of the key head
     bool open = false;
     auto next = [&]() {
-      Ahead y{0, -1, 0, 0, false};
+      Ahead y{0, -1, 0, nullptr, 0, false};
       for (;;) {
         if (!open) {
           if (todo <= x.lead) return y;
@@ -522,8 +534,10 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
           j1 = min(it.tile1, it.n_cache);
           used = it.tile1 - it.tile0;
           const int slot = j * kTile + lane * TT_SCALE_SLOTS;
-          index = slot / a.page_size;
+          pages = a.page_table + x.b * a.table_stride + slot / a.page_size;
           in_page = slot % a.page_size;
+          left = x.r.len - slot;
+          scales = sc.data + x.hk * sc.head;
           open = true;
         }
         if (j < j1) break;
@@ -534,14 +548,15 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
       y.there = true;
       y.hk = x.hk;
       y.in_page = in_page;
-      if (lane < kGroups && j * kTile + lane * TT_SCALE_SLOTS < x.r.len)
-        y.page = a.page_table[x.b * a.table_stride + index];
+      y.scales = scales;
+      if (lane < kGroups && left > 0) y.page = *pages;
       ++j;
-      index += per_tile;
+      left -= kTile;
+      pages += per_tile;
       in_page += rest;
       if (in_page >= a.page_size) {
         in_page -= a.page_size;
-        ++index;
+        ++pages;
       }
       return y;
     };
@@ -555,8 +570,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
       const Ahead c = one;
       one = two;
       if (one.there && usable(one.page))
-        one.code = sc.data[one.page * sc.page + (one.in_page / TT_SCALE_SLOTS) * sc.group +
-                           one.hk * sc.head];
+        one.code = one.scales[one.page * sc.page + (one.in_page / TT_SCALE_SLOTS) * sc.group];
       two = next();
       if (!c.there) continue;
       const int ring = n % kScaleRing;
@@ -657,7 +671,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         if (j == it.tile0) continue;
         if (i >= it.n_cache) ++w;  // (behind the keys)
         ok = on(&s.w_full[w & 1], (w >> 1) & 1) && on(&s.p_full[n & 1], (n >> 1) & 1) &&
-             (i > it.tile0 || on(&s.o_free, (seg & 1) ^ 1));
+             (i - it.tile0 >= kSets || on(&s.o_free, (seg & 1) ^ 1));
         if (!ok) break;
         tc_fence_after();
         const uint32_t idesc = idesc_mn(F16 || i < it.n_cache, R);
@@ -668,8 +682,8 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
 #pragma unroll
           for (int c = 0; c < kTile / 16; ++c)
             if (c < steps)
-              umma_ss(tmem + S::kOut, wv + (w & 1) * kWStep + 128 * c, pd + (n & 1) * kPStep + 128 * c,
-                      idesc, i > it.tile0 || c > 0);
+              umma_ss(tmem + S::kOut + (kSets == 2 ? (n & 1) * R : 0), wv + (w & 1) * kWStep + 128 * c, pd + (n & 1) * kPStep + 128 * c,
+                      idesc, i - it.tile0 >= kSets || c > 0);
           umma_commit(&s.o_done[n & 1]);
           umma_commit(&s.w_empty[w & 1]);
         }
@@ -759,18 +773,36 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
           // (a thread takes 8 elements of either half of a key: stores of 16 bytes without
           // bank conflicts)
           const uint32_t lost = s.left_out[1][ring];
-          constexpr int kPairs = D / 64;
-#pragma unroll 4
-          for (int k = 0; k < kTile * 8 / kConvThreads; ++k) {
-            const int i = k * kConvThreads + ct, key = i / 8, u = i % 8;
-            const bool there = key < keys && !(lost >> (key / TT_SCALE_SLOTS) & 1);
+          constexpr int kPairs = D / 64, kEach = kTile * 8 / kConvThreads;
+          const int u = ct % 8, key0 = ct / 8;  // (its keys are 16 apart)
+          const char* const from = s.v[st] + key0 * D + u * 8;
+          char* const to = s.w[w & 1] + swizzled16(key0, u);
+          auto convert = [](const uint2& in) {
+            return make_uint4(e4m3x2_to_f16x2(in.x & 0xffff), e4m3x2_to_f16x2(in.x >> 16),
+                              e4m3x2_to_f16x2(in.y & 0xffff), e4m3x2_to_f16x2(in.y >> 16));
+          };
+          if (keys == kTile && lost == 0) {
 #pragma unroll
             for (int h = 0; h < kPairs; ++h) {
-              uint2 in = make_uint2(0, 0);
-              if (there) in = *reinterpret_cast<const uint2*>(s.v[st] + key * D + h * 64 + u * 8);
-              *reinterpret_cast<uint4*>(s.w[w & 1] + h * kBlock + swizzled16(key, u)) =
-                  make_uint4(e4m3x2_to_f16x2(in.x & 0xffff), e4m3x2_to_f16x2(in.x >> 16),
-                             e4m3x2_to_f16x2(in.y & 0xffff), e4m3x2_to_f16x2(in.y >> 16));
+              uint2 in[kEach];
+#pragma unroll
+              for (int k = 0; k < kEach; ++k)
+                in[k] = *reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64);
+#pragma unroll
+              for (int k = 0; k < kEach; ++k)
+                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in[k]);
+            }
+          } else {
+#pragma unroll 1
+            for (int k = 0; k < kEach; ++k) {
+              const int key = key0 + 16 * k;
+              const bool there = key < keys && !(lost >> (key / TT_SCALE_SLOTS) & 1);
+#pragma unroll
+              for (int h = 0; h < kPairs; ++h) {
+                uint2 in = make_uint2(0, 0);
+                if (there) in = *reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64);
+                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in);
+              }
             }
           }
           mbar_arrive(&s.v_empty[st]);
@@ -841,9 +873,13 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
       const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t, kRowThreads));
       if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
-    const int quarter = warp & 3, rows_of = warp >> 2, key = quarter * 32 + lane;
+    const int quarter = warp & 3, four = warp >> 2, key = quarter * 32 + lane;
+    const int set = four / kSubs, rows_of = four % kSubs;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-    const int barrier = 1 + rows_of;  // of the four warps that hold the same rows
+    const int barrier = 1 + four;  // of its four warps
+    const uint32_t output = mine + S::kOut + set * R, my_sums = mine + S::kSums + set * R;
+    float* const my_shift = s.shift[set];
+    float* const my_fall = s.fall[set];
     // This warp's chunks of rows, 8 c .. 8 c + 7: c = rows_of, rows_of + kSubs, ...
     // A warp goes on, or gives up, as one. One that gave up passes the barriers between
     // the warps as often as the others, but waits and arrives no more and writes
@@ -882,7 +918,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
 #pragma unroll 1
       for (int c = rows_of; c < chunks; c += kSubs) {
         const uint32_t zero[8] = {};
-        tmem_st8(mine + S::kSums + 8 * c, zero);
+        tmem_st8(my_sums + 8 * c, zero);
       }
       tmem_wait_st();
       bool unset = true;
@@ -890,6 +926,11 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
 #pragma unroll 1
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
         const bool cache = j < it.n_cache;
+        if (kSets == 2 && (n & 1) != set) {
+          ct += cache;
+          continue;
+        }
+        const bool first = code == 0;
         bool there = key < it.keys(x, j);
         float scale = 1.f, value = 1.f;
         int top_code = kOwnCode;
@@ -945,7 +986,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
           }
         };
         auto factor = [&](int c) { return reinterpret_cast<const f32x2*>(factors) + factor_step * c; };
-        auto shift = [&](int c) { return reinterpret_cast<const f32x2*>(s.shift + 8 * c); };
+        auto shift = [&](int c) { return reinterpret_cast<const f32x2*>(my_shift + 8 * c); };
         // New references, where a row's maximum is above its own by more than kSlack (or it
         // has none), and what that makes of the output.
         auto raise = [&] {
@@ -963,7 +1004,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
               if (lane == 2 * i) top = lo;
               if (lane == 2 * i + 1) top = hi;
             }
-            if (lane < 8) s.part[quarter][8 * c + lane] = top;
+            if (lane < 8) s.part[set][quarter][8 * c + lane] = top;
           }
           sync_of(barrier, 128);
           if (quarter == 0) {
@@ -971,23 +1012,23 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
             const int row = 8 * (kSubs * (lane / 8) + rows_of) + lane % 8;
             bool none = false;
             if (lane < 8 * kChunks && row < it.rows) {
-              const float top = fmaxf(fmaxf(s.part[0][row], s.part[1][row]),
-                                      fmaxf(s.part[2][row], s.part[3][row]));
-              const float old = j == it.tile0 ? -INFINITY : s.ref[row];
+              const float top = fmaxf(fmaxf(s.part[set][0][row], s.part[set][1][row]),
+                                      fmaxf(s.part[set][2][row], s.part[set][3][row]));
+              const float old = first ? -INFINITY : s.ref[set][row];
               const float to = top - old > kSlack || old == -INFINITY ? fmaxf(old, top) : old;
-              s.ref[row] = to;
-              s.shift[row] = (to == -INFINITY ? 0.f : -to) + kOffset;
-              s.fall[row] = old == -INFINITY ? 0.f : ex2_approx(old - to);
+              s.ref[set][row] = to;
+              my_shift[row] = (to == -INFINITY ? 0.f : -to) + kOffset;
+              my_fall[row] = old == -INFINITY ? 0.f : ex2_approx(old - to);
               none = to == -INFINITY;
             } else if (lane < 8 * kChunks) {  // (rows that a chunk has too many)
-              s.shift[row] = -INFINITY;
-              s.fall[row] = 0.f;
+              my_shift[row] = -INFINITY;
+              my_fall[row] = 0.f;
             }
             none = __any_sync(0xffffffffu, none);
-            if (lane == 0) s.unset[rows_of] = none;
+            if (lane == 0) s.unset[four] = none;
           }
           sync_of(barrier, 128);
-          unset = s.unset[rows_of];
+          unset = s.unset[four];
         };
         // What the values' scale makes of weights is in units of the largest scale so far;
         // when that rises the output falls.
@@ -1008,7 +1049,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         for (int c = rows_of; c < chunks; c += kSubs) {
           f32x2 z[4];
           uint32_t l[8];
-          tmem_ld8(mine + S::kSums + 8 * c, l);
+          tmem_ld8(my_sums + 8 * c, l);
           scores(c, z);
           tmem_wait8(l);
           uint32_t out[4];
@@ -1019,7 +1060,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
             split(y, lo, hi);
             over = fmaxf(over, fmaxf(lo, hi));
             f32x2 e = exp2_pair(y), sum = both(l, i);
-            if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(s.fall + 8 * c)[i]);
+            if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(my_fall + 8 * c)[i]);
             sum = add2(sum, e);
             split(sum, lo, hi);
             l[2 * i] = __float_as_uint(lo);
@@ -1027,7 +1068,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
             split(mul2(e, value2), lo, hi);
             out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
           }
-          tmem_st8(mine + S::kSums + 8 * c, l);
+          tmem_st8(my_sums + 8 * c, l);
           *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
               make_uint4(out[0], out[1], out[2], out[3]);
         }
@@ -1041,7 +1082,7 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
             f32x2 z[4];
             uint32_t l[8];
             tmem_wait_st();
-            tmem_ld8(mine + S::kSums + 8 * c, l);
+            tmem_ld8(my_sums + 8 * c, l);
             scores(c, z);
             tmem_wait8(l);
             uint32_t out[4];
@@ -1051,33 +1092,35 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
               split(exp2_pair(fma2(z[i], factor(c)[i], shift(c)[i])), e[0], e[1]);
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
-                const float fall = s.fall[8 * c + 2 * i + k];
+                const float fall = my_fall[8 * c + 2 * i + k];
                 l[2 * i + k] = __float_as_uint(
                     fall > 0x1p-60f ? __uint_as_float(l[2 * i + k]) * fall : e[k]);
               }
               split(mul2(pair(e[0], e[1]), value2), lo, hi);
               out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
             }
-            tmem_st8(mine + S::kSums + 8 * c, l);
+            tmem_st8(my_sums + 8 * c, l);
             *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
                 make_uint4(out[0], out[1], out[2], out[3]);
           }
         }
         tc_fence_before();
         if (ok) mbar_arrive(&s.s_free[n & 1]);
-        if ((raised || early || output_fall != 1.f) && j > it.tile0) {
-          wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
+        if ((raised || early || output_fall != 1.f) && !first) {
+          // (its last product is done: that of two tiles ago, for which this warp has waited,
+          // or the last one)
+          if (kSets == 1) wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
           tc_fence_after();
 #pragma unroll 1
           for (int c = rows_of; c < chunks; c += kSubs) {
             uint32_t v[8];
-            tmem_ld8(mine + S::kOut + 8 * c, v);
+            tmem_ld8(output + 8 * c, v);
             tmem_wait8(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
               v[i] = __float_as_uint(__uint_as_float(v[i]) * output_fall *
-                                     (raised || early ? s.fall[8 * c + i] : 1.f));
-            tmem_st8(mine + S::kOut + 8 * c, v);
+                                     (raised || early ? my_fall[8 * c + i] : 1.f));
+            tmem_st8(output + 8 * c, v);
           }
         }
         tmem_wait_st();
@@ -1086,78 +1129,97 @@ __global__ void __launch_bounds__(Rows<R>::kAll, 1) tree8_kernel(const __grid_co
         if (ok) mbar_arrive(&s.p_full[n & 1]);
       }
       // the sums of all keys
-      {
-        const int row = 8 * (kSubs * (lane / 8) + rows_of) + lane % 8;
-        sync_of(barrier, 128);  // (done with s.part and s.fall)
 #pragma unroll 1
-        for (int c = rows_of; c < chunks; c += kSubs) {
-          uint32_t l[8];
-          tmem_ld8(mine + S::kSums + 8 * c, l);
-          tmem_wait8(l);
-          float sums[8];
+      for (int c = rows_of; c < chunks; c += kSubs) {
+        uint32_t l[8];
+        tmem_ld8(my_sums + 8 * c, l);
+        tmem_wait8(l);
+        float sums[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
-          const float sum = warp_sums(sums, lane);
-          if (lane < 8) s.part[quarter][8 * c + lane] = sum;
+        for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
+        const float sum = warp_sums(sums, lane);
+        if (c == rows_of) sync_of(barrier, 128);  // (done with s.part and s.fall)
+        if (lane < 8) s.part[set][quarter][8 * c + lane] = sum;
+      }
+      if (rows_of == 0 && quarter == 0 && lane == 0) s.code[set] = code;
+      sync_of(5, kRowThreads);
+      const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
+      // where a row goes: to the output, or to its place in the CTA's piece
+      auto place = [&](int r) {
+        const int token = (row0 + r) / p.group;
+        return whole ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + r - token * p.group
+                     : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + r;
+      };
+      if (t < it.rows) {
+        // the sets' sums and outputs relative to the larger of their references
+        float top = -INFINITY, all = 0.f, l[kSets], f[kSets];
+#pragma unroll
+        for (int k = 0; k < kSets; ++k)
+          if (s.code[k]) top = fmaxf(top, s.ref[k][t]);
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) {
+          l[k] = f[k] = 0.f;
+          if (s.code[k]) {
+            l[k] = s.part[k][0][t] + s.part[k][1][t] + (s.part[k][2][t] + s.part[k][3][t]);
+            f[k] = s.ref[k][t] == -INFINITY ? (l[k] != l[k] ? 1.f : 0.f) : ex2_approx(s.ref[k][t] - top);
+            all = fmaf(l[k], f[k], all);
+          }
         }
-        sync_of(barrier, 128);
-        const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
-        const bool has_tree = it.tile1 > it.n_cache;
-        // where a row goes: to the output, or to its place in the CTA's piece
-        auto place = [&](int r) {
-          const int token = (row0 + r) / p.group;
-          return whole ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + r - token * p.group
-                       : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + r;
-        };
-        if (quarter == 0 && lane < 8 * kChunks && row < it.rows && ok) {
-          const float all = s.part[0][row] + s.part[1][row] + (s.part[2][row] + s.part[3][row]);
-          const float m2 = s.ref[row] == -INFINITY ? -INFINITY : s.ref[row] - kOffset;
-          s.fall[row] = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
-          const int64_t to = place(row);
-          if (!whole)
-            p.part_ml[to] = make_float2(m2, all);
-          else if (a.lse)
-            a.lse[to] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
-        }
-        sync_of(barrier, 128);
-        wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
-        tc_fence_after();
-        const float unit = e8m0(code);
-        bool odd = false;
-        if (has_tree) odd = lane < kWords && s.odd[ring][lane];
-        odd = __any_sync(0xffffffffu, odd);
-        if (D == 128 || quarter < 2) {
+        const float m2 = top == -INFINITY ? -INFINITY : top - kOffset;
+        const float inverse = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
+#pragma unroll
+        for (int k = 0; k < kSets; ++k) s.fall[k][t] = f[k] * inverse * (s.code[k] ? e8m0(s.code[k]) : 0.f);
+        const int64_t to = place(t);
+        if (ok && !whole)
+          p.part_ml[to] = make_float2(m2, all);
+        else if (ok && a.lse)
+          a.lse[to] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
+      }
+      sync_of(5, kRowThreads);
+      wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
+      if (kSets == 2 && n > 1) wait_for(&s.o_done[n & 1], ((n - 2) >> 1) & 1);
+      tc_fence_after();
+      bool odd = false;
+      if (it.tile1 > it.n_cache) odd = lane < kWords && s.odd[ring][lane];
+      odd = __any_sync(0xffffffffu, odd);
+      if (D == 128 || quarter < 2) {
 #pragma unroll 1
-          for (int c = rows_of; c < chunks; c += kSubs) {
+        for (int c = four; c < chunks; c += kFours) {
+          float y[8] = {};
+#pragma unroll
+          for (int k = 0; k < kSets; ++k) {
+            if (!s.code[k]) continue;
             uint32_t v[8];
-            tmem_ld8(mine + S::kOut + 8 * c, v);
+            tmem_ld8(mine + S::kOut + k * R + 8 * c, v);
             tmem_wait8(v);
-            // (rows lie side by side, but for where a token ends)
-            int g = (row0 + 8 * c) % p.group;
-            int64_t to = place(8 * c) * D + key;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const int r = 8 * c + i;
-              if (r < it.rows && ok) {
-                float y = __uint_as_float(v[i]) * unit;
-                if (odd)
-                  y += odd_values<DT>(a, s.odd[ring], s.seen[s.token[r]], it.end, x.r.first, x.hk, key);
-                if (whole)
-                  store_elem<DT>(a.out + to * 2, y * s.fall[r]);
-                else
-                  p.part[to] = y;
-              }
-              to += D;
-              if (++g == p.group) {
-                g = 0;
-                if (whole) to += int64_t(a.Hq - p.group) * D;
-              }
+            for (int i = 0; i < 8; ++i) y[i] = fmaf(__uint_as_float(v[i]), s.fall[k][8 * c + i], y[i]);
+          }
+          // (rows lie side by side, but for where a token ends)
+          int g = (row0 + 8 * c) % p.group;
+          int64_t to = place(8 * c) * D + key;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int r = 8 * c + i;
+            if (r < it.rows && ok) {
+              if (odd)
+                y[i] += odd_values<DT>(a, s.odd[ring], s.seen[s.token[r]], it.end, x.r.first, x.hk, key);
+              if (whole)
+                store_elem<DT>(a.out + to * 2, y[i]);
+              else
+                p.part[to] = y[i];
+            }
+            to += D;
+            if (++g == p.group) {
+              g = 0;
+              if (whole) to += int64_t(a.Hq - p.group) * D;
             }
           }
         }
-        tc_fence_before();
-        if (ok) mbar_arrive(&s.o_free);
       }
+      tc_fence_before();
+      if (ok) mbar_arrive(&s.o_free);
+      sync_of(5, kRowThreads);  // (done with the sets' facts)
       todo -= it.tile1 - it.tile0;
       x = next_place<R>(p.a, p.group, x);
     }
@@ -1343,7 +1405,7 @@ cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(Rows<R>::kAll);
+  cfg.blockDim = dim3(Rows<R, F16>::kAll);
   cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
   cfg.stream = stream;
   cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, R, F16>, p);
