@@ -64,7 +64,7 @@ struct Rows {
   static constexpr int kSubs = R == 16 ? 1 : 4 / kSets;    // fours of a set, which share its rows
   static constexpr int kChunks = R / 8 / kSubs;            // of 8 rows, of a warp, at most
   static constexpr int kFours = kSets * kSubs, kWarps = 4 * kFours, kThreads = kWarps * 32;
-  static constexpr int kAll = kThreads + kConvThreads + 96;  // threads of a CTA
+  static constexpr int kAll = kThreads + kConvThreads + 128;  // threads of a CTA
 };
 constexpr int kWords = TT_MAX_TREE / 32;
 constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
@@ -263,7 +263,7 @@ struct Smem8 {
   int code[kSets];                    // units of the outputs, 0: no tile
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
-  uint64_t p_full[2], o_done[2], q_full, q_empty, o_free, drained;
+  uint64_t p_full[2], o_done[2], q_full, q_empty, own_full, o_free, drained[2];
   long long sums[Rows<R, F16>::kAll / 32];  // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
@@ -390,6 +390,14 @@ __device__ __noinline__ float odd_values(const TreeArgs& a, const uint32_t* odd,
   return sum;
 }
 
+// Which of 8 rows see the drafted token of bit `lane` of a word.
+__device__ __noinline__ uint32_t tree_sees(const uint32_t* seen, const uint8_t* tokens, int word, int lane) {
+  uint32_t see = 0;
+#pragma unroll 1
+  for (int i = 0; i < 8; ++i) see |= (seen[tokens[i] * kWords + word] >> lane & 1) << i;
+  return see;
+}
+
 template <int D, int R, bool F16>
 __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
@@ -433,7 +441,9 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
     mbar_init(&s.q_full, kConvThreads);
     mbar_init(&s.q_empty, 1);
     mbar_init(&s.o_free, kRowThreads);
-    mbar_init(&s.drained, 1);
+    mbar_init(&s.own_full, kConvThreads);
+    mbar_init(&s.drained[0], 1);
+    mbar_init(&s.drained[1], 1);
     s.stop = INT32_MAX;
     for (int i = 0; i < 8; ++i) s.own_factor[i] = p.scale2;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -500,12 +510,12 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
   x.lead = 0;
   if (todo > 0) x = find_place<R>(p.a, p.group, s.start_b, s.start_offset);
 
-  if (warp > kRowWarps + kConvWarps) {
+  if (warp > kRowWarps + kConvWarps + 1) {
     // ------------------------------------------------------------ copies
     // One warp for keys, one for values. Lane g < 8 has to do with a tile's g-th 16 slots:
     // it reads their scale, and copies the box that begins with them. Pages are asked
     // for two tiles ahead, scales one.
-    const bool values = warp != kRowWarps + kConvWarps + 1;
+    const bool values = warp != kRowWarps + kConvWarps + 2;
     const TreeScale& sc = values ? p.sc.v : p.sc.k;
     char* const dst = values ? &s.v[0][0] : &s.k[0][0];
     uint64_t* const full = values ? s.v_full : s.k_full;
@@ -608,96 +618,105 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
 #pragma unroll 1
     for (int i = 0; i < stages; ++i)
       if (n > i) wait8(&full[i], ((n - 1 - i) / stages) & 1, limit);
-  } else if (warp == kRowWarps + kConvWarps) {
+  } else if (warp >= kRowWarps + kConvWarps) {
     // ---------------------------------------------------------- products
-    // (the whole warp goes along, one lane issues: operands then are uniform registers)
-    const uint64_t kd = umma8_desc<D>(smem_u32(s.k)), qd = umma8_desc<D>(smem_u32(s.q8)),
-                   od = umma_desc(smem_u32(s.q16), 16), wk = umma_desc(smem_u32(s.w), 16),
-                   wv = umma_desc(smem_u32(s.w), kBlock), pd = umma_desc(smem_u32(s.p), 16);
-    constexpr uint32_t kWStep = kTile * D * 2 / 16, kKStep = kTile * D / 16, kPStep = kTile * 128 / 16;
+    // One warp issues those that give scores, one those with values. (Warps go along as a
+    // whole, one lane issues: operands then are uniform registers.)
     auto on = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, wait8(bar, parity, limit)) != 0;
     };
-    int n = 0, kt = 0, kst = 0, w = 0;  // tiles, the cache's among them, 16-bit operands
+    constexpr uint32_t kWStep = kTile * D * 2 / 16, kKStep = kTile * D / 16, kPStep = kTile * 128 / 16;
+    int n = 0, w = 0;  // tiles, 16-bit operands
+    if (warp == kRowWarps + kConvWarps) {
+      const uint64_t kd = umma8_desc<D>(smem_u32(s.k)), qd = umma8_desc<D>(smem_u32(s.q8)),
+                     od = umma_desc(smem_u32(s.q16), 16), wk = umma_desc(smem_u32(s.w), 16);
+      int turn = 0, st = 0, drafted = 0;
 #pragma unroll 1
-    for (int seg = 0; todo > x.lead && ok; ++seg) {
-      todo -= x.lead;
-      const Item<R> it(p, x, todo);
-      ok = on(&s.q_full, seg & 1);
-      // A tile's scores before the product of the one before it, but for the first of an
-      // item, whose queries may not be there yet.
+      for (int seg = 0; todo > x.lead && ok; ++seg) {
+        todo -= x.lead;
+        const Item<R> it(p, x, todo);
+        ok = on(&s.q_full, seg & 1);
 #pragma unroll 1
-      for (int j = it.tile0; j <= it.tile1 && ok; ++j) {
-        const int i = j - 1;
-        if (j < it.tile1) {
-          const int tile = n + (j > it.tile0), buf = tile & 1;
-          ok = on(&s.s_free[buf], ((tile >> 1) & 1) ^ 1);
-          if (!ok) break;
+        for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
+          const int buf = n & 1;
           const uint32_t to = tmem + buf * S::kScores;
           if (j < it.n_cache) {
-            ok = on(&s.k_full[kst], kt & 1);
+            ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
               for (int c = 0; c < D / 32; ++c)
-                umma8_ss(to, kd + kst * kKStep + 2 * c, qd + 2 * c, idesc_e4m3(S::kScores), c > 0);
+                umma8_ss(to, kd + st * kKStep + 2 * c, qd + 2 * c, idesc_e4m3(S::kScores), c > 0);
               umma_commit(&s.s_full[buf]);
-              umma_commit(&s.k_empty[kst]);
+              umma_commit(&s.k_empty[st]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
             }
-            if (++kst == S::kStagesK) {
-              kst = 0;
-              ++kt;
+            if (++st == S::kStagesK) {
+              st = 0;
+              ++turn;
             }
           } else {
-            // (its drafted keys lie behind the last tile's values, and behind its keys)
-            const int at = w + (j > it.tile0) + (j > it.tile0 && i >= it.n_cache);
-            ok = on(&s.w_full[at & 1], (at >> 1) & 1);
+            // (a barrier of their own: on w_full's, this warp could be two phases ahead, where
+            // a parity says nothing)
+            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
               for (int c = 0; c < D / 16; ++c)
-                umma_ss(to, wk + (at & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
+                umma_ss(to, wk + (w & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
                         od + (c / 4) * (R * 128 / 16) + (c % 4) * 2, umma_idesc(F16, R, false), c > 0);
               umma_commit(&s.s_full[buf]);
-              umma_commit(&s.w_empty[at & 1]);
+              umma_commit(&s.w_empty[w & 1]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
             }
+            ++w;  // (behind its keys, its values)
           }
           __syncwarp();
         }
-        if (j == it.tile0) continue;
-        if (i >= it.n_cache) ++w;  // (behind the keys)
-        ok = on(&s.w_full[w & 1], (w >> 1) & 1) && on(&s.p_full[n & 1], (n >> 1) & 1) &&
-             (i - it.tile0 >= kSets || on(&s.o_free, (seg & 1) ^ 1));
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t idesc = idesc_mn(F16 || i < it.n_cache, R);
-        const int steps = (it.keys(x, i) + 15) / 16;
-        // (heads of 64: the other half of the 128 rows is of what lies behind the operand,
-        // the other one or the weights, and nobody reads it)
-        if (elect_one()) {
-#pragma unroll
-          for (int c = 0; c < kTile / 16; ++c)
-            if (c < steps)
-              umma_ss(tmem + S::kOut + (kSets == 2 ? (n & 1) * R : 0), wv + (w & 1) * kWStep + 128 * c, pd + (n & 1) * kPStep + 128 * c,
-                      idesc, i - it.tile0 >= kSets || c > 0);
-          umma_commit(&s.o_done[n & 1]);
-          umma_commit(&s.w_empty[w & 1]);
-        }
-        __syncwarp();
-        ++w;
-        ++n;
+        todo -= it.tile1 - it.tile0;
+        x = next_place<R>(p.a, p.group, x);
       }
-      todo -= it.tile1 - it.tile0;
-      x = next_place<R>(p.a, p.group, x);
+    } else {
+      const uint64_t wv = umma_desc(smem_u32(s.w), kBlock), pd = umma_desc(smem_u32(s.p), 16);
+#pragma unroll 1
+      for (int seg = 0; todo > x.lead && ok; ++seg) {
+        todo -= x.lead;
+        const Item<R> it(p, x, todo);
+#pragma unroll 1
+        for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
+          if (j >= it.n_cache) ++w;
+          const int keys = it.keys(x, j), buf = n & 1;
+          ok = on(&s.w_full[w & 1], (w >> 1) & 1) && on(&s.p_full[buf], (n >> 1) & 1) &&
+               (j - it.tile0 >= kSets || on(&s.o_free, (seg & 1) ^ 1));
+          if (!ok) break;
+          tc_fence_after();
+          const uint32_t idesc = idesc_mn(F16 || j < it.n_cache, R);
+          const uint32_t to = tmem + S::kOut + (kSets == 2 ? buf * R : 0);
+          const bool more = j - it.tile0 >= kSets;
+          // (heads of 64: the other half of the 128 rows is of what lies behind the operand,
+          // the other one or the weights, and nobody reads it)
+          if (elect_one()) {
+#pragma unroll
+            for (int c = 0; c < kTile / 16; ++c)
+              if (16 * c < keys)
+                umma_ss(to, wv + (w & 1) * kWStep + 128 * c, pd + buf * kPStep + 128 * c, idesc,
+                        more || c > 0);
+            umma_commit(&s.o_done[buf]);
+            umma_commit(&s.w_empty[w & 1]);
+          }
+          __syncwarp();
+        }
+        todo -= it.tile1 - it.tile0;
+        x = next_place<R>(p.a, p.group, x);
+      }
     }
-    // (and until its last products and their arrivals are done)
-    if (elect_one()) umma_commit(&s.drained);
+    // (and until their last products and the arrivals for them are done)
+    uint64_t* const drained = &s.drained[warp - kRowWarps - kConvWarps];
+    if (elect_one()) umma_commit(drained);
     __syncwarp();
-    on(&s.drained, 0);
+    on(drained, 0);
   } else if (warp >= kRowWarps) {
     // -------------------------------------------------- queries and values
     const int ct = t - kRowThreads;
@@ -852,6 +871,7 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
             if (kv == 0) {
               fence_proxy_async();
               mbar_arrive(&s.w_full[w & 1]);
+              mbar_arrive(&s.own_full);
               ++w;
             }
           }
@@ -947,7 +967,6 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         tc_fence_after();
         const uint32_t at = mine + (n & 1) * S::kScores;
         const f32x2 scale2 = pair(scale, scale);
-        const bool all_there = __all_sync(0xffffffffu, there);
         // The scores of this thread's key with the rows of chunk c, two to a number; times
         // its row's factor and with its row's shift they are exponents of weights. (They
         // are read again where they are needed again: the loops over chunks are rolled, as
@@ -955,10 +974,11 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         const float* const factors = cache ? s.factor[ring] : s.own_factor;
         const int factor_step = cache ? 4 : 0;
         auto scores = [&](int c, f32x2 (&z)[4]) {
+          uint32_t v[kPieces][8], seen = there ? 0xff : 0;
+          tmem_ld8(at + 8 * c, v[0]);
           if (cache) {
-            uint32_t v[kPieces][8];
 #pragma unroll
-            for (int q = 0; q < kPieces; ++q) tmem_ld8(at + q * R + 8 * c, v[q]);
+            for (int q = 1; q < kPieces; ++q) tmem_ld8(at + q * R + 8 * c, v[q]);
 #pragma unroll
             for (int q = 0; q < kPieces; ++q) tmem_wait8(v[q]);
             const f32x2 sixteenth = pair(1.f / 16, 1.f / 16);
@@ -969,20 +989,19 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
               for (int q = kPieces - 2; q >= 0; --q) y = fma2(y, sixteenth, both(v[q], i));
               z[i] = mul2(y, scale2);
             }
-            if (!all_there && !there) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) z[i] = pair(-INFINITY, -INFINITY);
-            }
           } else {
-            uint32_t v[8];
-            tmem_ld8(at + 8 * c, v);
-            tmem_wait8(v);
-            const int word = ((j - it.n_cache) * kTile + key) >> 5;
+            tmem_wait8(v[0]);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (!(there && s.seen[s.token[8 * c + i]][word] >> lane & 1)) v[i] = 0xff800000u;
+            for (int i = 0; i < 4; ++i) z[i] = both(v[0], i);
+            seen &= tree_sees(s.seen[0], s.token + 8 * c, ((j - it.n_cache) * kTile + key) >> 5, lane);
+          }
+          if (!__all_sync(0xffffffffu, seen == 0xff)) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[i] = both(v, i);
+            for (int i = 0; i < 4; ++i) {
+              float lo, hi;
+              split(z[i], lo, hi);
+              z[i] = pair(seen >> (2 * i) & 1 ? lo : -INFINITY, seen >> (2 * i + 1) & 1 ? hi : -INFINITY);
+            }
           }
         };
         auto factor = [&](int c) { return reinterpret_cast<const f32x2*>(factors) + factor_step * c; };
@@ -1041,69 +1060,76 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         const f32x2 value2 = pair(value, value);
         char* const weights = s.p[n & 1] + key * 128;
         const bool early = unset;
-        if (early) raise();
         // (the product of two tiles ago is done with the weights' place)
         wait_for(&s.o_done[n & 1], ((n >> 1) & 1) ^ 1);
-        float over = -INFINITY;
+        // 0: references, then weights; 1: weights. One that is too large, seldom: 2, new
+        // references, weights again. (The sums were added to in 32 bits, which hold them, or
+        // the old ones are nothing to the new.)
+        int pass = early ? 0 : 1;
 #pragma unroll 1
-        for (int c = rows_of; c < chunks; c += kSubs) {
-          f32x2 z[4];
-          uint32_t l[8];
-          tmem_ld8(my_sums + 8 * c, l);
-          scores(c, z);
-          tmem_wait8(l);
-          uint32_t out[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const f32x2 y = fma2(z[i], factor(c)[i], shift(c)[i]);
-            float lo, hi;
-            split(y, lo, hi);
-            over = fmaxf(over, fmaxf(lo, hi));
-            f32x2 e = exp2_pair(y), sum = both(l, i);
-            if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(my_fall + 8 * c)[i]);
-            sum = add2(sum, e);
-            split(sum, lo, hi);
-            l[2 * i] = __float_as_uint(lo);
-            l[2 * i + 1] = __float_as_uint(hi);
-            split(mul2(e, value2), lo, hi);
-            out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
-          }
-          tmem_st8(my_sums + 8 * c, l);
-          *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
-              make_uint4(out[0], out[1], out[2], out[3]);
-        }
-        // A weight that is too large, seldom: new references, weights again. (The sums were
-        // added to in 32 bits, which hold them, or the old ones are nothing to the new.)
-        const bool raised = !early && any_of(barrier, 128, over > kSlack + kOffset);
-        if (raised) {
-          raise();
+        do {
+          if (pass != 1) raise();
+          if (pass < 2) {
+            float over = -INFINITY;
 #pragma unroll 1
-          for (int c = rows_of; c < chunks; c += kSubs) {
-            f32x2 z[4];
-            uint32_t l[8];
-            tmem_wait_st();
-            tmem_ld8(my_sums + 8 * c, l);
-            scores(c, z);
-            tmem_wait8(l);
-            uint32_t out[4];
+            for (int c = rows_of; c < chunks; c += kSubs) {
+              f32x2 z[4];
+              uint32_t l[8];
+              tmem_ld8(my_sums + 8 * c, l);
+              scores(c, z);
+              tmem_wait8(l);
+              uint32_t out[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float e[2], lo, hi;
-              split(exp2_pair(fma2(z[i], factor(c)[i], shift(c)[i])), e[0], e[1]);
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const float fall = my_fall[8 * c + 2 * i + k];
-                l[2 * i + k] = __float_as_uint(
-                    fall > 0x1p-60f ? __uint_as_float(l[2 * i + k]) * fall : e[k]);
+              for (int i = 0; i < 4; ++i) {
+                const f32x2 y = fma2(z[i], factor(c)[i], shift(c)[i]);
+                float lo, hi;
+                split(y, lo, hi);
+                over = fmaxf(over, fmaxf(lo, hi));
+                f32x2 e = exp2_pair(y), sum = both(l, i);
+                if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(my_fall + 8 * c)[i]);
+                sum = add2(sum, e);
+                split(sum, lo, hi);
+                l[2 * i] = __float_as_uint(lo);
+                l[2 * i + 1] = __float_as_uint(hi);
+                split(mul2(e, value2), lo, hi);
+                out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
               }
-              split(mul2(pair(e[0], e[1]), value2), lo, hi);
-              out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
+              tmem_st8(my_sums + 8 * c, l);
+              *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
+                  make_uint4(out[0], out[1], out[2], out[3]);
             }
-            tmem_st8(my_sums + 8 * c, l);
-            *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
-                make_uint4(out[0], out[1], out[2], out[3]);
+            pass = !early && any_of(barrier, 128, over > kSlack + kOffset) ? 2 : 3;
+          } else {
+#pragma unroll 1
+            for (int c = rows_of; c < chunks; c += kSubs) {
+              f32x2 z[4];
+              uint32_t l[8];
+              tmem_wait_st();
+              tmem_ld8(my_sums + 8 * c, l);
+              scores(c, z);
+              tmem_wait8(l);
+              uint32_t out[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                float e[2], lo, hi;
+                split(exp2_pair(fma2(z[i], factor(c)[i], shift(c)[i])), e[0], e[1]);
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                  const float fall = my_fall[8 * c + 2 * i + k];
+                  l[2 * i + k] = __float_as_uint(
+                      fall > 0x1p-60f ? __uint_as_float(l[2 * i + k]) * fall : e[k]);
+                }
+                split(mul2(pair(e[0], e[1]), value2), lo, hi);
+                out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
+              }
+              tmem_st8(my_sums + 8 * c, l);
+              *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
+                  make_uint4(out[0], out[1], out[2], out[3]);
+            }
+            pass = 4;
           }
-        }
+        } while (pass < 3);
+        const bool raised = pass == 4;
         tc_fence_before();
         if (ok) mbar_arrive(&s.s_free[n & 1]);
         if ((raised || early || output_fall != 1.f) && !first) {
