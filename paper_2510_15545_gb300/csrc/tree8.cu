@@ -54,18 +54,11 @@ namespace {
 
 constexpr int kTile = 128;                     // keys of a tile
 constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
-// The warps that turn scores of R rows into weights: fours, of 32 keys each. Where tensor
-// memory has room for two outputs, half of them takes the even tiles and half the odd
-// ones, each with references, sums and an output of its own: what a tile takes from its
-// scores to its weights is mostly waiting, and so two are on their way.
-template <int R, bool F16>
-struct Rows {
-  static constexpr int kSets = F16 && R == 64 ? 1 : 2;
-  static constexpr int kSubs = R == 16 ? 1 : 4 / kSets;    // fours of a set, which share its rows
-  static constexpr int kChunks = R / 8 / kSubs;            // of 8 rows, of a warp, at most
-  static constexpr int kFours = kSets * kSubs, kWarps = 4 * kFours, kThreads = kWarps * 32;
-  static constexpr int kAll = kThreads + kConvThreads + 128;  // threads of a CTA
-};
+// Eight warps turn scores into weights, 32 keys each: four take the even tiles and four
+// the odd ones, each with references, sums and an output of their own. What a tile takes
+// from its scores to its weights is mostly waiting, and so two are on their way.
+constexpr int kSets = 2, kRowWarps = 4 * kSets, kRowThreads = kRowWarps * 32;
+constexpr int kThreads = kRowThreads + kConvThreads + 128;
 constexpr int kWords = TT_MAX_TREE / 32;
 constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
 constexpr int kScaleRing = 8;                    // tiles' scales, items' facts that are kept
@@ -230,16 +223,12 @@ __device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Reques
 
 template <int D, int R, bool F16>
 struct Smem8 {
-  static constexpr int kPieces = F16 ? 3 : 2;
-  // Tensor memory: two tiles' scores (a column for each piece and row), the outputs, the
-  // sums of the weights.
-  static constexpr int kSets = Rows<R, F16>::kSets;
-  static constexpr int kScores = kPieces * R, kOut = 2 * kScores, kSums = kOut + kSets * R;
-  static constexpr int kUsed = kSums + kSets * R;
+  static constexpr int kPieces = F16 ? 3 : 2;  // of queries
+  // Tensor memory: of each set the scores of its tile, its output, the sums of its weights.
+  static constexpr int kOut = kSets * R, kSums = 2 * kOut, kUsed = 3 * kOut;
   static constexpr int kColumns = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
-  static_assert(kUsed <= 512, "tensor memory");
   // what 227 KB hold
-  static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : 3;
+  static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : R == 64 && F16 ? 2 : 3;
   static constexpr int kStagesV = D == 64 ? 6 : R == 64 ? 2 : 3;
   char w[2][kTile * D * 2];           // values of 16 bits; a drafted tile's keys too
   char p[2][kTile * 128];             // weights, the rows of a key side by side
@@ -257,17 +246,19 @@ struct Smem8 {
   alignas(16) float own_factor[8];                // the same of drafted keys
   uint32_t odd[kItemRing][kWords];    // drafted tokens with a value that is not finite
   alignas(16) float shift[kSets][R];  // what is added to log2 scores
-  alignas(16) float fall[kSets][R];   // a reference's last change; at the end, outputs' factors
   float ref[kSets][R];                // reference maximum (log2)
   float part[kSets][4][R];            // what the warps of 32 keys each tell
-  int code[kSets];                    // units of the outputs, 0: no tile
+  // of this item and the one before, whose output may be on its way still
+  alignas(16) float fall[2][kSets][R];  // a reference's last change; at the end, outputs' factors
+  int code[2][kSets];                 // units of the outputs, 0: no tile
+  int64_t row_to[2][R];               // row of the output, or of the CTA's pieces
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
   uint64_t p_full[2], o_done[2], q_full, q_empty, own_full, o_free, drained[2];
-  long long sums[Rows<R, F16>::kAll / 32];  // places of the requests, by warps
+  long long sums[kThreads / 32];  // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
-  int unset[4];                       // rows of four warps without a reference yet
+  int unset[kSets];                   // rows without a reference yet
   uint32_t tmem;
   int end, stop;                      // the place behind this CTA's, and where it gave up
 };
@@ -343,6 +334,11 @@ __device__ __forceinline__ bool any_of(int barrier, int threads, bool x) {
 __device__ __forceinline__ void sync_of(int barrier, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
 }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
 __device__ __forceinline__ bool elect_one() {
   uint32_t r;
   asm volatile(
@@ -399,7 +395,7 @@ __device__ __noinline__ uint32_t tree_sees(const uint32_t* seen, const uint8_t* 
 }
 
 template <int D, int R, bool F16>
-__global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
+__global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
   constexpr int kPieces = S::kPieces;
@@ -407,10 +403,6 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
   // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
   constexpr int kOwnCode = F16 ? 127 : 67;
   constexpr int kBlock = kTile * 128;         // distance of the 64-element blocks of a 16-bit tile
-  constexpr int kSets = Rows<R, F16>::kSets, kSubs = Rows<R, F16>::kSubs;
-  constexpr int kChunks = Rows<R, F16>::kChunks, kFours = Rows<R, F16>::kFours;
-  constexpr int kRowWarps = Rows<R, F16>::kWarps, kRowThreads = Rows<R, F16>::kThreads;
-  constexpr int kThreads = Rows<R, F16>::kAll;
   constexpr float kOffset = 7.f;              // fp16 weights: away from its small end
   extern __shared__ char raw[];
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
@@ -434,8 +426,8 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
       mbar_init(&s.w_full[i], kConvThreads);
       mbar_init(&s.w_empty[i], 1);
       mbar_init(&s.s_full[i], 1);
-      mbar_init(&s.s_free[i], kRowThreads / kSets);
-      mbar_init(&s.p_full[i], kRowThreads / kSets);
+      mbar_init(&s.s_free[i], 128);
+      mbar_init(&s.p_full[i], 128);
       mbar_init(&s.o_done[i], 1);
     }
     mbar_init(&s.q_full, kConvThreads);
@@ -639,15 +631,18 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
           const int buf = n & 1;
-          const uint32_t to = tmem + buf * S::kScores;
+          const uint32_t to = tmem + buf * R;
           if (j < it.n_cache) {
             ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
-              for (int c = 0; c < D / 32; ++c)
-                umma8_ss(to, kd + st * kKStep + 2 * c, qd + 2 * c, idesc_e4m3(S::kScores), c > 0);
+              for (int q = 0; q < kPieces; ++q)
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c)
+                  umma8_ss(to, kd + st * kKStep + 2 * c, qd + q * (R * D / 16) + 2 * c, idesc_e4m3(R),
+                           q > 0 || c > 0);
               umma_commit(&s.s_full[buf]);
               umma_commit(&s.k_empty[st]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
@@ -693,7 +688,7 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
           if (!ok) break;
           tc_fence_after();
           const uint32_t idesc = idesc_mn(F16 || j < it.n_cache, R);
-          const uint32_t to = tmem + S::kOut + (kSets == 2 ? buf * R : 0);
+          const uint32_t to = tmem + S::kOut + buf * R;
           const bool more = j - it.tile0 >= kSets;
           // (heads of 64: the other half of the 128 rows is of what lies behind the operand,
           // the other one or the weights, and nobody reads it)
@@ -772,8 +767,8 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
               two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
               const uint32_t half = e4m3x2_to_f16x2(two[k]);
               const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
-              e[2 * k] = (e[2 * k] - f.x) * 16.f;
-              e[2 * k + 1] = (e[2 * k + 1] - f.y) * 16.f;
+              e[2 * k] -= f.x;
+              e[2 * k + 1] -= f.y;
             }
             *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) =
                 make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
@@ -893,14 +888,11 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
       const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t, kRowThreads));
       if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
-    const int quarter = warp & 3, four = warp >> 2, key = quarter * 32 + lane;
-    const int set = four / kSubs, rows_of = four % kSubs;
+    const int quarter = warp & 3, set = warp >> 2, key = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-    const int barrier = 1 + four;  // of its four warps
-    const uint32_t output = mine + S::kOut + set * R, my_sums = mine + S::kSums + set * R;
-    float* const my_shift = s.shift[set];
-    float* const my_fall = s.fall[set];
-    // This warp's chunks of rows, 8 c .. 8 c + 7: c = rows_of, rows_of + kSubs, ...
+    const uint32_t at = mine + set * R, output = at + S::kOut, my_sums = at + S::kSums;
+    const int barrier = 1 + set;  // of the set's four warps
+    char* const weights = s.p[set] + key * 128;
     // A warp goes on, or gives up, as one. One that gave up passes the barriers between
     // the warps as often as the others, but waits and arrives no more and writes
     // nothing: so the others give up, too, and all end.
@@ -934,9 +926,19 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         }
         sync_of(5, kRowThreads);
       }
+      float* const my_shift = s.shift[set];
+      float* const my_fall = s.fall[seg & 1][set];
+      const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
+      // where a row goes: to the output, or to its place in the CTA's piece
+      if (t < R) {
+        const int token = (row0 + t) / p.group;
+        s.row_to[seg & 1][t] =
+            whole ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + t - token * p.group
+                  : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + t;
+      }
       // sums of the weights, from nothing
 #pragma unroll 1
-      for (int c = rows_of; c < chunks; c += kSubs) {
+      for (int c = 0; c < chunks; ++c) {
         const uint32_t zero[8] = {};
         tmem_st8(my_sums + 8 * c, zero);
       }
@@ -946,7 +948,7 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
 #pragma unroll 1
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
         const bool cache = j < it.n_cache;
-        if (kSets == 2 && (n & 1) != set) {
+        if ((n & 1) != set) {
           ct += cache;
           continue;
         }
@@ -963,45 +965,29 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
           there = there && !(s.left_out[0][e] >> (key / TT_SCALE_SLOTS) & 1);
           ++ct;
         }
-        wait_for(&s.s_full[n & 1], (n >> 1) & 1);
+        wait_for(&s.s_full[set], (n >> 1) & 1);
         tc_fence_after();
-        const uint32_t at = mine + (n & 1) * S::kScores;
         const f32x2 scale2 = pair(scale, scale);
         // The scores of this thread's key with the rows of chunk c, two to a number; times
-        // its row's factor and with its row's shift they are exponents of weights. (They
-        // are read again where they are needed again: the loops over chunks are rolled, as
-        // unrolled code of this size came from beyond the instruction caches: TODO.)
+        // the key's scale and its row's factor and with its row's shift they are exponents of
+        // weights. (They are read again where they are needed again: the loops over chunks
+        // are rolled, as unrolled code of this size came from beyond the instruction caches.)
         const float* const factors = cache ? s.factor[ring] : s.own_factor;
         const int factor_step = cache ? 4 : 0;
-        auto scores = [&](int c, f32x2 (&z)[4]) {
-          uint32_t v[kPieces][8], seen = there ? 0xff : 0;
-          tmem_ld8(at + 8 * c, v[0]);
-          if (cache) {
+        const uint32_t mask = there ? 0xff : 0;
+        const bool plain = cache && __all_sync(0xffffffffu, there);
+        auto scores = [&](int c, const uint32_t (&v)[8], f32x2 (&z)[4]) {
 #pragma unroll
-            for (int q = 1; q < kPieces; ++q) tmem_ld8(at + q * R + 8 * c, v[q]);
+          for (int i = 0; i < 4; ++i) z[i] = mul2(both(v, i), scale2);
+          if (plain) return;
+          const uint32_t seen =
+              cache ? mask
+                    : mask & tree_sees(s.seen[0], s.token + 8 * c, ((j - it.n_cache) * kTile + key) >> 5, lane);
 #pragma unroll
-            for (int q = 0; q < kPieces; ++q) tmem_wait8(v[q]);
-            const f32x2 sixteenth = pair(1.f / 16, 1.f / 16);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              f32x2 y = both(v[kPieces - 1], i);
-#pragma unroll
-              for (int q = kPieces - 2; q >= 0; --q) y = fma2(y, sixteenth, both(v[q], i));
-              z[i] = mul2(y, scale2);
-            }
-          } else {
-            tmem_wait8(v[0]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) z[i] = both(v[0], i);
-            seen &= tree_sees(s.seen[0], s.token + 8 * c, ((j - it.n_cache) * kTile + key) >> 5, lane);
-          }
-          if (!__all_sync(0xffffffffu, seen == 0xff)) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float lo, hi;
-              split(z[i], lo, hi);
-              z[i] = pair(seen >> (2 * i) & 1 ? lo : -INFINITY, seen >> (2 * i + 1) & 1 ? hi : -INFINITY);
-            }
+          for (int i = 0; i < 4; ++i) {
+            float lo, hi;
+            split(z[i], lo, hi);
+            z[i] = pair(seen >> (2 * i) & 1 ? lo : -INFINITY, seen >> (2 * i + 1) & 1 ? hi : -INFINITY);
           }
         };
         auto factor = [&](int c) { return reinterpret_cast<const f32x2*>(factors) + factor_step * c; };
@@ -1010,9 +996,12 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         // has none), and what that makes of the output.
         auto raise = [&] {
 #pragma unroll 1
-          for (int c = rows_of; c < chunks; c += kSubs) {
+          for (int c = 0; c < chunks; ++c) {
+            uint32_t v[8];
+            tmem_ld8(at + 8 * c, v);
+            tmem_wait8(v);
             f32x2 z[4];
-            scores(c, z);
+            scores(c, v, z);
             float top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -1026,28 +1015,22 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
             if (lane < 8) s.part[set][quarter][8 * c + lane] = top;
           }
           sync_of(barrier, 128);
-          if (quarter == 0) {
-            // (lane: the row's number among these warps')
-            const int row = 8 * (kSubs * (lane / 8) + rows_of) + lane % 8;
-            bool none = false;
-            if (lane < 8 * kChunks && row < it.rows) {
-              const float top = fmaxf(fmaxf(s.part[set][0][row], s.part[set][1][row]),
-                                      fmaxf(s.part[set][2][row], s.part[set][3][row]));
-              const float old = first ? -INFINITY : s.ref[set][row];
-              const float to = top - old > kSlack || old == -INFINITY ? fmaxf(old, top) : old;
-              s.ref[set][row] = to;
-              my_shift[row] = (to == -INFINITY ? 0.f : -to) + kOffset;
-              my_fall[row] = old == -INFINITY ? 0.f : ex2_approx(old - to);
-              none = to == -INFINITY;
-            } else if (lane < 8 * kChunks) {  // (rows that a chunk has too many)
-              my_shift[row] = -INFINITY;
-              my_fall[row] = 0.f;
-            }
-            none = __any_sync(0xffffffffu, none);
-            if (lane == 0) s.unset[four] = none;
+          bool none = false;
+          const int row = quarter * 32 + lane;
+          if (row < it.rows) {
+            const auto& part = s.part[set];
+            const float top = fmaxf(fmaxf(part[0][row], part[1][row]), fmaxf(part[2][row], part[3][row]));
+            const float old = first ? -INFINITY : s.ref[set][row];
+            const float to = top - old > kSlack || old == -INFINITY ? fmaxf(old, top) : old;
+            s.ref[set][row] = to;
+            my_shift[row] = (to == -INFINITY ? 0.f : -to) + kOffset;
+            my_fall[row] = old == -INFINITY ? 0.f : ex2_approx(old - to);
+            none = to == -INFINITY;
+          } else if (row < R) {  // (rows that a chunk has too many)
+            my_shift[row] = -INFINITY;
+            my_fall[row] = 0.f;
           }
-          sync_of(barrier, 128);
-          unset = s.unset[four];
+          unset = any_of(barrier, 128, none);
         };
         // What the values' scale makes of weights is in units of the largest scale so far;
         // when that rises the output falls.
@@ -1058,10 +1041,9 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         }
         value *= e8m0_inverse(code);
         const f32x2 value2 = pair(value, value);
-        char* const weights = s.p[n & 1] + key * 128;
         const bool early = unset;
         // (the product of two tiles ago is done with the weights' place)
-        wait_for(&s.o_done[n & 1], ((n >> 1) & 1) ^ 1);
+        wait_for(&s.o_done[set], ((n >> 1) & 1) ^ 1);
         // 0: references, then weights; 1: weights. One that is too large, seldom: 2, new
         // references, weights again. (The sums were added to in 32 bits, which hold them, or
         // the old ones are nothing to the new.)
@@ -1071,20 +1053,20 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
           if (pass != 1) raise();
           if (pass < 2) {
             float over = -INFINITY;
-#pragma unroll 1
-            for (int c = rows_of; c < chunks; c += kSubs) {
-              f32x2 z[4];
-              uint32_t l[8];
+            auto fetch = [&](int c, uint32_t (&v)[8], uint32_t (&l)[8]) {
+              tmem_ld8(at + 8 * c, v);
               tmem_ld8(my_sums + 8 * c, l);
-              scores(c, z);
-              tmem_wait8(l);
+            };
+            auto weigh = [&](int c, const uint32_t (&v)[8], uint32_t (&l)[8]) {
+              f32x2 z[4];
+              scores(c, v, z);
               uint32_t out[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 const f32x2 y = fma2(z[i], factor(c)[i], shift(c)[i]);
                 float lo, hi;
                 split(y, lo, hi);
-                over = fmaxf(over, fmaxf(lo, hi));
+                over = max3(over, lo, hi);
                 f32x2 e = exp2_pair(y), sum = both(l, i);
                 if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(my_fall + 8 * c)[i]);
                 sum = add2(sum, e);
@@ -1097,17 +1079,34 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
               tmem_st8(my_sums + 8 * c, l);
               *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
                   make_uint4(out[0], out[1], out[2], out[3]);
+            };
+            // (a chunk is fetched while the one before it is weighed)
+            uint32_t v0[8], l0[8], v1[8], l1[8];
+            fetch(0, v0, l0);
+#pragma unroll 1
+            for (int c = 0; c < chunks; c += 2) {
+              tmem_wait8(v0);
+              tmem_wait8(l0);
+              if (c + 1 < chunks) fetch(c + 1, v1, l1);
+              weigh(c, v0, l0);
+              if (c + 1 >= chunks) break;
+              tmem_wait8(v1);
+              tmem_wait8(l1);
+              if (c + 2 < chunks) fetch(c + 2, v0, l0);
+              weigh(c + 1, v1, l1);
             }
             pass = !early && any_of(barrier, 128, over > kSlack + kOffset) ? 2 : 3;
           } else {
 #pragma unroll 1
-            for (int c = rows_of; c < chunks; c += kSubs) {
+            for (int c = 0; c < chunks; ++c) {
               f32x2 z[4];
-              uint32_t l[8];
+              uint32_t v[8], l[8];
               tmem_wait_st();
+              tmem_ld8(at + 8 * c, v);
               tmem_ld8(my_sums + 8 * c, l);
-              scores(c, z);
+              tmem_wait8(v);
               tmem_wait8(l);
+              scores(c, v, z);
               uint32_t out[4];
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
@@ -1131,14 +1130,12 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         } while (pass < 3);
         const bool raised = pass == 4;
         tc_fence_before();
-        if (ok) mbar_arrive(&s.s_free[n & 1]);
+        if (ok) mbar_arrive(&s.s_free[set]);
         if ((raised || early || output_fall != 1.f) && !first) {
-          // (its last product is done: that of two tiles ago, for which this warp has waited,
-          // or the last one)
-          if (kSets == 1) wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
+          // (its last product is done: that of two tiles ago, for which this warp has waited)
           tc_fence_after();
 #pragma unroll 1
-          for (int c = rows_of; c < chunks; c += kSubs) {
+          for (int c = 0; c < chunks; ++c) {
             uint32_t v[8];
             tmem_ld8(output + 8 * c, v);
             tmem_wait8(v);
@@ -1152,50 +1149,49 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
         tmem_wait_st();
         fence_proxy_async();
         tc_fence_before();
-        if (ok) mbar_arrive(&s.p_full[n & 1]);
+        if (ok) mbar_arrive(&s.p_full[set]);
       }
       // the sums of all keys
+      if (code) {
+        sync_of(barrier, 128);  // (done with s.part and s.fall)
 #pragma unroll 1
-      for (int c = rows_of; c < chunks; c += kSubs) {
-        uint32_t l[8];
-        tmem_ld8(my_sums + 8 * c, l);
-        tmem_wait8(l);
-        float sums[8];
+        for (int c = 0; c < chunks; ++c) {
+          uint32_t l[8];
+          tmem_ld8(my_sums + 8 * c, l);
+          tmem_wait8(l);
+          float sums[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
-        const float sum = warp_sums(sums, lane);
-        if (c == rows_of) sync_of(barrier, 128);  // (done with s.part and s.fall)
-        if (lane < 8) s.part[set][quarter][8 * c + lane] = sum;
+          for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
+          const float sum = warp_sums(sums, lane);
+          if (lane < 8) s.part[set][quarter][8 * c + lane] = sum;
+        }
       }
-      if (rows_of == 0 && quarter == 0 && lane == 0) s.code[set] = code;
+      if (quarter == 0 && lane == 0) s.code[seg & 1][set] = code;
       sync_of(5, kRowThreads);
-      const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
-      // where a row goes: to the output, or to its place in the CTA's piece
-      auto place = [&](int r) {
-        const int token = (row0 + r) / p.group;
-        return whole ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + r - token * p.group
-                     : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + r;
-      };
       if (t < it.rows) {
         // the sets' sums and outputs relative to the larger of their references
         float top = -INFINITY, all = 0.f, l[kSets], f[kSets];
+        const int* const codes = s.code[seg & 1];
 #pragma unroll
         for (int k = 0; k < kSets; ++k)
-          if (s.code[k]) top = fmaxf(top, s.ref[k][t]);
+          if (codes[k]) top = fmaxf(top, s.ref[k][t]);
 #pragma unroll
         for (int k = 0; k < kSets; ++k) {
           l[k] = f[k] = 0.f;
-          if (s.code[k]) {
-            l[k] = s.part[k][0][t] + s.part[k][1][t] + (s.part[k][2][t] + s.part[k][3][t]);
-            f[k] = s.ref[k][t] == -INFINITY ? (l[k] != l[k] ? 1.f : 0.f) : ex2_approx(s.ref[k][t] - top);
+          if (codes[k]) {
+            const auto& part = s.part[k];
+            const float ref = s.ref[k][t];
+            l[k] = part[0][t] + part[1][t] + (part[2][t] + part[3][t]);
+            f[k] = ref == -INFINITY ? (l[k] != l[k] ? 1.f : 0.f) : ex2_approx(ref - top);
             all = fmaf(l[k], f[k], all);
           }
         }
         const float m2 = top == -INFINITY ? -INFINITY : top - kOffset;
         const float inverse = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
 #pragma unroll
-        for (int k = 0; k < kSets; ++k) s.fall[k][t] = f[k] * inverse * (s.code[k] ? e8m0(s.code[k]) : 0.f);
-        const int64_t to = place(t);
+        for (int k = 0; k < kSets; ++k)
+          s.fall[seg & 1][k][t] = f[k] * inverse * (codes[k] ? e8m0(codes[k]) : 0.f);
+        const int64_t to = s.row_to[seg & 1][t];
         if (ok && !whole)
           p.part_ml[to] = make_float2(m2, all);
         else if (ok && a.lse)
@@ -1203,49 +1199,42 @@ __global__ void __launch_bounds__(Rows<R, F16>::kAll, 1) tree8_kernel(const __gr
       }
       sync_of(5, kRowThreads);
       wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
-      if (kSets == 2 && n > 1) wait_for(&s.o_done[n & 1], ((n - 2) >> 1) & 1);
+      if (n > 1) wait_for(&s.o_done[n & 1], ((n - 2) >> 1) & 1);
       tc_fence_after();
       bool odd = false;
       if (it.tile1 > it.n_cache) odd = lane < kWords && s.odd[ring][lane];
       odd = __any_sync(0xffffffffu, odd);
       if (D == 128 || quarter < 2) {
 #pragma unroll 1
-        for (int c = four; c < chunks; c += kFours) {
+        for (int c = set; c < chunks; c += kSets) {
           float y[8] = {};
 #pragma unroll
           for (int k = 0; k < kSets; ++k) {
-            if (!s.code[k]) continue;
+            if (!s.code[seg & 1][k]) continue;
             uint32_t v[8];
             tmem_ld8(mine + S::kOut + k * R + 8 * c, v);
             tmem_wait8(v);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = fmaf(__uint_as_float(v[i]), s.fall[k][8 * c + i], y[i]);
+            for (int i = 0; i < 8; ++i)
+              y[i] = fmaf(__uint_as_float(v[i]), s.fall[seg & 1][k][8 * c + i], y[i]);
           }
-          // (rows lie side by side, but for where a token ends)
-          int g = (row0 + 8 * c) % p.group;
-          int64_t to = place(8 * c) * D + key;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int r = 8 * c + i;
             if (r < it.rows && ok) {
               if (odd)
                 y[i] += odd_values<DT>(a, s.odd[ring], s.seen[s.token[r]], it.end, x.r.first, x.hk, key);
+              const int64_t to = s.row_to[seg & 1][r] * D + key;
               if (whole)
                 store_elem<DT>(a.out + to * 2, y[i]);
               else
                 p.part[to] = y[i];
-            }
-            to += D;
-            if (++g == p.group) {
-              g = 0;
-              if (whole) to += int64_t(a.Hq - p.group) * D;
             }
           }
         }
       }
       tc_fence_before();
       if (ok) mbar_arrive(&s.o_free);
-      sync_of(5, kRowThreads);  // (done with the sets' facts)
       todo -= it.tile1 - it.tile0;
       x = next_place<R>(p.a, p.group, x);
     }
@@ -1431,7 +1420,7 @@ cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(Rows<R, F16>::kAll);
+  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
   cfg.stream = stream;
   cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, R, F16>, p);
