@@ -54,15 +54,21 @@ namespace {
 
 constexpr int kTile = 128;                     // keys of a tile
 constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
-// Eight warps turn scores into weights, 32 keys each: four take the even tiles and four
-// the odd ones, each with references, sums and an output of their own. What a tile takes
-// from its scores to its weights is mostly waiting, and so two are on their way.
-constexpr int kSets = 2, kRowWarps = 4 * kSets, kRowThreads = kRowWarps * 32;
-constexpr int kThreads = kRowThreads + kConvThreads + 128;
+// Eight warps turn scores into weights, 32 keys each, for 64 rows sixteen: half of them
+// take the even tiles and half the odd ones, each with references, sums and an output of
+// their own. What a tile takes from its scores to its weights is mostly waiting, and so
+// two are on their way.
+constexpr int kSets = 2;
+template <int R>
+struct Warps {
+  static constexpr int kSubs = R == 64 ? 2 : 1;  // fours of a set, which share the rows
+  static constexpr int kRow = 4 * kSets * kSubs, kRowThreads = kRow * 32;
+  static constexpr int kThreads = kRowThreads + kConvThreads + 128;  // of a CTA
+};
 constexpr int kWords = TT_MAX_TREE / 32;
 constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
-constexpr int kScaleRing = 8;                    // tiles' scales, items' facts that are kept
-constexpr int kItemRing = 4;
+constexpr int kScaleRing = 16;                   // tiles' scales that are kept
+constexpr int kBatch = 4;                        // tiles whose pages are asked for together
 constexpr float kLn2 = 0.693147180559945f;
 // A row's reference maximum follows its maximum once that is 2^kSlack above it:
 // weights stay below 2^(kSlack + offset), and the output is scaled rarely.
@@ -186,21 +192,26 @@ __device__ __noinline__ Place next_place(const TreeArgs& a, int group, Place x) 
   } while (x.r.nodes == 0);
   return x;
 }
-// The part of an item that a CTA takes.
+// The part of an item that a CTA takes: tiles of drafted tokens, which have to come from
+// further away, first, then the cache's.
 template <int R>
 struct Item {
-  int n_cache, rows, tile0, tile1, end;
+  int n_tree, rows, tile0, tile1, end;
   __device__ __forceinline__ Item(const Tree8Args& p, const Place& x, int todo) {
-    n_cache = cache_tiles(x.r.len);
     rows = min(R, x.r.nodes * p.group - x.mt * R);
     end = item_end<R>(x.r, p.group, x.mt);
+    n_tree = tree_tiles(end);
     tile0 = x.tile;
-    tile1 = min(n_cache + tree_tiles(end), x.tile + todo);
+    tile1 = min(n_tree + cache_tiles(x.r.len), x.tile + todo);
   }
-  // keys of tile j in use
-  __device__ __forceinline__ int keys(const Place& x, int j) const {
-    return min(kTile, j < n_cache ? x.r.len - j * kTile : end - (j - n_cache) * kTile);
-  }
+};
+// Keys in use of tile j of an item.
+__device__ __forceinline__ int tile_keys(int j, int n_tree, int end, int len) {
+  return min(kTile, j < n_tree ? end - j * kTile : len - (j - n_tree) * kTile);
+}
+// What the converting warps, which come to an item first, tell the others of it.
+struct Facts {
+  int n_tree, rows, tile0, tile1, end, len, first, hk, at;  // at: the place of its first tile
 };
 
 // Whether every parent and page of the request is in range (the row threads).
@@ -224,41 +235,43 @@ __device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Reques
 template <int D, int R, bool F16>
 struct Smem8 {
   static constexpr int kPieces = F16 ? 3 : 2;  // of queries
-  // Tensor memory: of each set the scores of its tile, its output, the sums of its weights.
-  static constexpr int kOut = kSets * R, kSums = 2 * kOut, kUsed = 3 * kOut;
+  // Tensor memory: scores of four tiles, of each set its output and the sums of its weights.
+  static constexpr int kOut = 4 * R, kSums = kOut + kSets * R, kUsed = kSums + kSets * R;
   static constexpr int kColumns = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
   // what 227 KB hold
   static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : R == 64 && F16 ? 2 : 3;
   static constexpr int kStagesV = D == 64 ? 6 : R == 64 ? 2 : 3;
+  static constexpr int kThreads = Warps<R>::kThreads;
   char w[2][kTile * D * 2];           // values of 16 bits; a drafted tile's keys too
   char p[2][kTile * 128];             // weights, the rows of a key side by side
   char k[kStagesK][kTile * D];        // keys and values as they come
   char q16[R * D * 2];                // queries for drafted keys,
   char q8[kPieces * R * D];           // and in pieces for the cache's
   char v[kStagesV][kTile * D];
-  uint32_t seen[R][kWords];           // a token's ancestors and itself
+  // of this item and the next one
+  uint32_t seen[2][R][kWords];        // a token's ancestors and itself
+  alignas(16) float factor[2][R];     // a row's pieces times it and a key's scale: log2 scores
+  uint32_t odd[2][kWords];            // drafted tokens with a value that is not finite
+  int64_t row_to[2][R];               // row of the output, or of the CTA's pieces
+  uint8_t token[2][R];                // of a row, from the item's first
+  Facts facts[2];
   int16_t up[TT_MAX_TREE];            // parents, -1 for roots
-  uint8_t token[R];                   // of a row, from the item's first
   float k_scale[kScaleRing][kGroups], v_scale[kScaleRing][kGroups];
   uint32_t left_out[2][kScaleRing];   // groups whose page is out of range: keys, values
   int top_code[kScaleRing];           // the largest of the values' scales
-  alignas(16) float factor[kItemRing][R];         // a row's pieces times it and a key's scale: log2 scores
-  alignas(16) float own_factor[8];                // the same of drafted keys
-  uint32_t odd[kItemRing][kWords];    // drafted tokens with a value that is not finite
+  alignas(16) float own_factor[8];    // the factor of drafted keys
   alignas(16) float shift[kSets][R];  // what is added to log2 scores
+  alignas(16) float fall[kSets][R];   // a reference's last change
+  alignas(16) float share_of[kSets][R];  // of the output, at an item's end
   float ref[kSets][R];                // reference maximum (log2)
   float part[kSets][4][R];            // what the warps of 32 keys each tell
-  // of this item and the one before, whose output may be on its way still
-  alignas(16) float fall[2][kSets][R];  // a reference's last change; at the end, outputs' factors
-  int code[2][kSets];                 // units of the outputs, 0: no tile
-  int64_t row_to[2][R];               // row of the output, or of the CTA's pieces
+  int code[kSets];                    // units of the outputs, 0: no tile
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
-  uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
-  uint64_t p_full[2], o_done[2], q_full, q_empty, own_full, o_free, drained[2];
-  long long sums[kThreads / 32];  // places of the requests, by warps
+  uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[4], s_free[4];
+  uint64_t p_full[2], o_done[2], item_full[2], o_free[2], q_full, q_empty, own_full, drained[2];
+  long long sums[kThreads / 32];      // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
-  int unset[kSets];                   // rows without a reference yet
   uint32_t tmem;
   int end, stop;                      // the place behind this CTA's, and where it gave up
 };
@@ -389,16 +402,18 @@ __device__ __noinline__ float odd_values(const TreeArgs& a, const uint32_t* odd,
 // Which of 8 rows see the drafted token of bit `lane` of a word.
 __device__ __noinline__ uint32_t tree_sees(const uint32_t* seen, const uint8_t* tokens, int word, int lane) {
   uint32_t see = 0;
-#pragma unroll 1
+#pragma unroll
   for (int i = 0; i < 8; ++i) see |= (seen[tokens[i] * kWords + word] >> lane & 1) << i;
   return see;
 }
 
 template <int D, int R, bool F16>
-__global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
+__global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
-  constexpr int kPieces = S::kPieces;
+  constexpr int kPieces = S::kPieces, kSubs = Warps<R>::kSubs;
+  constexpr int kRowWarps = Warps<R>::kRow, kRowThreads = Warps<R>::kRowThreads;
+  constexpr int kThreads = Warps<R>::kThreads;
   // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
   // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
   constexpr int kOwnCode = F16 ? 127 : 67;
@@ -425,14 +440,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.w_full[i], kConvThreads);
       mbar_init(&s.w_empty[i], 1);
-      mbar_init(&s.s_full[i], 1);
-      mbar_init(&s.s_free[i], 128);
-      mbar_init(&s.p_full[i], 128);
+      mbar_init(&s.p_full[i], 128 * kSubs);
       mbar_init(&s.o_done[i], 1);
+      mbar_init(&s.item_full[i], kConvThreads);
+      mbar_init(&s.o_free[i], kRowThreads);
+    }
+    for (int i = 0; i < 4; ++i) {
+      mbar_init(&s.s_full[i], 1);
+      mbar_init(&s.s_free[i], 128 * kSubs);
     }
     mbar_init(&s.q_full, kConvThreads);
     mbar_init(&s.q_empty, 1);
-    mbar_init(&s.o_free, kRowThreads);
     mbar_init(&s.own_full, kConvThreads);
     mbar_init(&s.drained[0], 1);
     mbar_init(&s.drained[1], 1);
@@ -500,13 +518,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
   bool ok = true;
   Place x;
   x.lead = 0;
-  if (todo > 0) x = find_place<R>(p.a, p.group, s.start_b, s.start_offset);
+  if (todo > 0 && warp >= kRowWarps) x = find_place<R>(p.a, p.group, s.start_b, s.start_offset);
 
   if (warp > kRowWarps + kConvWarps + 1) {
     // ------------------------------------------------------------ copies
-    // One warp for keys, one for values. Lane g < 8 has to do with a tile's g-th 16 slots:
-    // it reads their scale, and copies the box that begins with them. Pages are asked
-    // for two tiles ahead, scales one.
+    // One warp for keys, one for values. Pages of four tiles are asked for at once, two
+    // batches ahead, and their scales one: lane 8 k + g has to do with the g-th 16 slots of
+    // a batch's k-th tile. It reads their scale, and copies the box that begins with them.
     const bool values = warp != kRowWarps + kConvWarps + 2;
     const TreeScale& sc = values ? p.sc.v : p.sc.k;
     char* const dst = values ? &s.v[0][0] : &s.k[0][0];
@@ -514,32 +532,23 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     uint64_t* const empty = values ? s.v_empty : s.k_empty;
     const int stages = values ? S::kStagesV : S::kStagesK;
     const CUtensorMap* const map = values ? &p.vc : &p.kc;
-    const int per_tile = kTile / a.page_size, rest = kTile % a.page_size;
-    struct Ahead {
+    struct Batch {
       int hk, page, in_page;  // of the lane's slots
-      const uint8_t* scales;
+      int tiles;              // 0: no more
       uint32_t code;
-      bool there;
     };
-    int j = 0, j1 = 0, used = 0, left = 0, in_page = 0;
-    const int32_t* pages = nullptr;    // from this tile's on
-    const uint8_t* scales = nullptr;   // of the key head
+    int j = 0, j1 = 0, used = 0;
     bool open = false;
     auto next = [&]() {
-      Ahead y{0, -1, 0, nullptr, 0, false};
+      Batch y{0, -1, 0, 0, 0};
       for (;;) {
         if (!open) {
           if (todo <= x.lead) return y;
           todo -= x.lead;
           const Item<R> it(p, x, todo);
-          j = it.tile0;
-          j1 = min(it.tile1, it.n_cache);
+          j = max(0, it.tile0 - it.n_tree);
+          j1 = it.tile1 - it.n_tree;
           used = it.tile1 - it.tile0;
-          const int slot = j * kTile + lane * TT_SCALE_SLOTS;
-          pages = a.page_table + x.b * a.table_stride + slot / a.page_size;
-          in_page = slot % a.page_size;
-          left = x.r.len - slot;
-          scales = sc.data + x.hk * sc.head;
           open = true;
         }
         if (j < j1) break;
@@ -547,63 +556,64 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         x = next_place<R>(p.a, p.group, x);
         open = false;
       }
-      y.there = true;
+      y.tiles = min(kBatch, j1 - j);
       y.hk = x.hk;
-      y.in_page = in_page;
-      y.scales = scales;
-      if (lane < kGroups && left > 0) y.page = *pages;
-      ++j;
-      left -= kTile;
-      pages += per_tile;
-      in_page += rest;
-      if (in_page >= a.page_size) {
-        in_page -= a.page_size;
-        ++pages;
-      }
+      const int slot = j * kTile + lane * TT_SCALE_SLOTS;
+      y.in_page = slot % a.page_size;
+      if (lane < y.tiles * kGroups && slot < x.r.len)
+        y.page = a.page_table[x.b * a.table_stride + slot / a.page_size];
+      j += y.tiles;
       return y;
     };
     auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
-    Ahead one, two;
-    one.there = two.there = false;
+    Batch one, two;
+    one.tiles = two.tiles = 0;
     int n = 0, st = 0;
     uint32_t parity = 1;
 #pragma unroll 1
-    for (int k = 0; ok && (k < 2 || one.there); ++k) {
-      const Ahead c = one;
+    for (int k = 0; ok && (k < 2 || one.tiles); ++k) {
+      const Batch c = one;
       one = two;
-      if (one.there && usable(one.page))
-        one.code = one.scales[one.page * sc.page + (one.in_page / TT_SCALE_SLOTS) * sc.group];
+      const bool mine = c.tiles && usable(c.page), then = one.tiles && usable(one.page);
+      if (then)
+        one.code = sc.data[one.page * sc.page + (one.in_page / TT_SCALE_SLOTS) * sc.group +
+                           one.hk * sc.head];
       two = next();
-      if (!c.there) continue;
-      const int ring = n % kScaleRing;
-      const bool mine = usable(c.page);
-      ok = __all_sync(0xffffffffu, wait8(&empty[st], parity, limit)) &&
-           (n != 1 || int(blockIdx.x) != p.stall);
-      if (!ok) break;
-      // (The scales in this place are of kScaleRing tiles ago. Keys': a stage's last
-      // products came after rows had freed the scores of two tiles before its own, for
-      // which they had read the scale. Values': they came to be converted after the
-      // product of two tiles before, for which rows and converters had read theirs.)
-      if (lane < kGroups) (values ? s.v_scale : s.k_scale)[ring][lane] = e8m0(c.code);
-      const unsigned int lost = __ballot_sync(0xffffffffu, lane < kGroups && !mine);
-      const int top = __reduce_max_sync(0xffffffffu, c.code != 255 ? int(c.code) : 0);
-      const bool begins = mine && lane * TT_SCALE_SLOTS % p.box == 0;
-      const int boxes = __popc(__ballot_sync(0xffffffffu, begins));
-      if (lane == 0) {
-        s.left_out[values][ring] = lost;
-        if (values) s.top_code[ring] = top;
-        mbar_arrive_expect_tx(&full[st], boxes * p.box * D);
-      }
-      __syncwarp();
-      if (begins)
-        tma_load_4d(smem_u32(dst) + st * (kTile * D) + lane * TT_SCALE_SLOTS * D, map,
-                    smem_u32(&full[st]), 0, p.slots_inner ? c.in_page : c.hk,
-                    p.slots_inner ? c.hk : c.in_page, c.page);
-      if (lane == 0) mbar_arrive(&s.scale_full[ring]);
-      ++n;
-      if (++st == stages) {
-        st = 0;
-        parity ^= 1;
+      if (!c.tiles) continue;
+      const bool begins = mine && lane % kGroups * TT_SCALE_SLOTS % p.box == 0;
+      const unsigned int lost = __ballot_sync(0xffffffffu, !mine);
+      const unsigned int boxes = __ballot_sync(0xffffffffu, begins);
+      const float scale = e8m0(c.code);
+      int top = c.code != 255 ? int(c.code) : 0;
+#pragma unroll
+      for (int o = 1; o < kGroups; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      const int at1 = p.slots_inner ? c.in_page : c.hk, at2 = p.slots_inner ? c.hk : c.in_page;
+#pragma unroll 1
+      for (int i = 0; i < c.tiles; ++i) {
+        ok = __all_sync(0xffffffffu, wait8(&empty[st], parity, limit)) &&
+             (n != 1 || int(blockIdx.x) != p.stall);
+        if (!ok) break;
+        // (The scales in this place are of kScaleRing tiles ago, which is further back than
+        // the stages and the tiles on their way behind them reach.)
+        const int ring = n % kScaleRing;
+        if (lane / kGroups == i) {
+          (values ? s.v_scale : s.k_scale)[ring][lane % kGroups] = scale;
+          if (lane % kGroups == 0) {
+            s.left_out[values][ring] = lost >> (kGroups * i) & 0xff;
+            if (values) s.top_code[ring] = top;
+            mbar_arrive_expect_tx(&full[st], __popc(boxes >> (kGroups * i) & 0xff) * p.box * D);
+          }
+        }
+        __syncwarp();
+        if (begins && lane / kGroups == i)
+          tma_load_4d(smem_u32(dst) + st * (kTile * D) + lane % kGroups * TT_SCALE_SLOTS * D, map,
+                      smem_u32(&full[st]), 0, at1, at2, c.page);
+        if (lane == 0) mbar_arrive(&s.scale_full[ring]);
+        ++n;
+        if (++st == stages) {
+          st = 0;
+          parity ^= 1;
+        }
       }
     }
     // (the CTA's memory stays until its last copies have come)
@@ -630,10 +640,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         ok = on(&s.q_full, seg & 1);
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
-          const int buf = n & 1;
+          const int buf = n & 3;
           const uint32_t to = tmem + buf * R;
-          if (j < it.n_cache) {
-            ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
+          if (j >= it.n_tree) {
+            ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 2) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -654,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           } else {
             // (a barrier of their own: on w_full's, this warp could be two phases ahead, where
             // a parity says nothing)
-            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
+            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 2) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -681,13 +691,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         const Item<R> it(p, x, todo);
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
-          if (j >= it.n_cache) ++w;
-          const int keys = it.keys(x, j), buf = n & 1;
+          if (j < it.n_tree) ++w;
+          const int keys = tile_keys(j, it.n_tree, it.end, x.r.len), buf = n & 1;
           ok = on(&s.w_full[w & 1], (w >> 1) & 1) && on(&s.p_full[buf], (n >> 1) & 1) &&
-               (j - it.tile0 >= kSets || on(&s.o_free, (seg & 1) ^ 1));
+               (j - it.tile0 >= kSets || seg == 0 || on(&s.o_free[(seg - 1) & 1], ((seg - 1) >> 1) & 1));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t idesc = idesc_mn(F16 || j < it.n_cache, R);
+          const uint32_t idesc = idesc_mn(F16 || j >= it.n_tree, R);
           const uint32_t to = tmem + S::kOut + buf * R;
           const bool more = j - it.tile0 >= kSets;
           // (heads of 64: the other half of the 128 rows is of what lies behind the operand,
@@ -719,11 +729,44 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       if (ok) ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       return ok;
     };
-    int vt = 0, st = 0, w = 0;
+    int vt = 0, st = 0, w = 0, seg = 0;
     uint32_t parity = 0;
-    for (int seg = 0; todo > x.lead && ok; ++seg) {
+#pragma unroll 1
+    for (; todo > x.lead && ok; ++seg) {
       todo -= x.lead;
       const Item<R> it(p, x, todo);
+      const int side = seg & 1, row0 = x.mt * R, token0 = row0 / p.group;
+      // (the item before the last one is over)
+      if (!wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1)) break;
+      // Its facts, and a token's ancestors: one thread walks up from each token.
+      if (ct == 0)
+        s.facts[side] = Facts{it.n_tree, it.rows, it.tile0, it.tile1, it.end,
+                              x.r.len,   x.r.first, x.hk,   s.end - todo};
+      if (ct < R) {
+        const int token = (row0 + ct) / p.group;
+        s.token[side][ct] = uint8_t(token - token0);
+        s.row_to[side][ct] =
+            it.tile0 == 0 && it.tile1 == it.n_tree + cache_tiles(x.r.len)
+                ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + ct - token * p.group
+                : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + ct;
+      }
+      if (ct < kWords) s.odd[side][ct] = 0;
+      if (it.tile0 < it.n_tree) {
+        sync_of(6, kConvThreads);  // (done with the last ones)
+#pragma unroll 1
+        for (int i = ct; i < it.end; i += kConvThreads) {
+          const int up = a.parents ? a.parents[x.r.first + i] : i - 1;
+          s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
+        }
+        sync_of(6, kConvThreads);
+        if (ct < it.end - token0) {
+          const int words = it.n_tree * (kTile / 32);
+#pragma unroll 1
+          for (int k = 0; k < words; ++k) s.seen[side][ct][k] = 0;
+#pragma unroll 1
+          for (int i = token0 + ct; i >= 0; i = s.up[i]) s.seen[side][ct][i >> 5] |= 1u << (i & 31);
+        }
+      }
       // Queries: kEach threads to a row.
       {
         constexpr int kEach = kConvThreads / R, kVecs = D / 8 / kEach;
@@ -748,8 +791,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         const uint32_t code = e8m0_for(top);
         const float inverse = e8m0_inverse(code);
         if (!wait_for(&s.q_empty, (seg & 1) ^ 1)) break;
-        if (sub == 0) s.factor[seg % kItemRing][r] = p.scale2 * e8m0(code);
-        if (ct < kWords) s.odd[seg % kItemRing][ct] = 0;
+        if (sub == 0) s.factor[side][r] = p.scale2 * e8m0(code);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
           const int u = sub * kVecs + i;  // 16-byte unit of the row
@@ -776,11 +818,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         }
         fence_proxy_async();
         mbar_arrive(&s.q_full);
+        mbar_arrive(&s.item_full[side]);
       }
       for (int j = it.tile0; j < it.tile1 && ok; ++j) {
-        const int keys = it.keys(x, j), steps = (keys + 15) / 16;  // (others are not multiplied)
+        const int keys = tile_keys(j, it.n_tree, it.end, x.r.len);
+        const int steps = (keys + 15) / 16;  // (others are not multiplied)
         constexpr int kUnits = D / 8;  // of 8 elements, of a key
-        if (j < it.n_cache) {
+        if (j >= it.n_tree) {
           const int ring = vt % kScaleRing;
           if (!wait_for(&s.v_full[st], parity)) break;
           if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
@@ -828,7 +872,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         } else {
           // Drafted tokens: keys as they are, then values without what is not finite (a
           // token outside its branch would get NaN from it; its own gets it at the end).
-          const int base = (j - it.n_cache) * kTile;
+          const int base = j * kTile;
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
@@ -858,7 +902,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
                     (q == 0 ? o.x : q == 1 ? o.y : q == 2 ? o.z : o.w) = y;
                   }
                   if (odd)
-                    atomicOr(&s.odd[seg % kItemRing][(base + key) >> 5], 1u << ((base + key) & 31));
+                    atomicOr(&s.odd[side][(base + key) >> 5], 1u << ((base + key) & 31));
                 }
               }
               *reinterpret_cast<uint4*>(s.w[w & 1] + (u / 8) * kBlock + swizzled16(key, u % 8)) = o;
@@ -879,6 +923,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       todo -= it.tile1 - it.tile0;
       x = next_place<R>(p.a, p.group, x);
     }
+    // (no more)
+    if (ok && wait_for(&s.o_free[seg & 1], ((seg >> 1) & 1) ^ 1)) {
+      if (ct == 0) s.facts[seg & 1].tile1 = -1;
+      mbar_arrive(&s.item_full[seg & 1]);
+    }
   } else {
     // -------------------------------------------------------------- rows
     // (while the first copies are on their way: the requests' statuses)
@@ -888,57 +937,37 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t, kRowThreads));
       if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
-    const int quarter = warp & 3, set = warp >> 2, key = quarter * 32 + lane;
+    const int quarter = warp & 3, four = warp >> 2, key = quarter * 32 + lane;
+    const int set = four / kSubs, sub = four % kSubs;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-    const uint32_t at = mine + set * R, output = at + S::kOut, my_sums = at + S::kSums;
-    const int barrier = 1 + set;  // of the set's four warps
+    const uint32_t output = mine + S::kOut + set * R, my_sums = mine + S::kSums + set * R;
+    const int barrier = 1 + four;  // of its four warps
+    float* const my_shift = s.shift[set];
+    float* const my_fall = s.fall[set];
     char* const weights = s.p[set] + key * 128;
     // A warp goes on, or gives up, as one. One that gave up passes the barriers between
-    // the warps as often as the others, but waits and arrives no more and writes
-    // nothing: so the others give up, too, and all end.
+    // the warps as often as the others until the item's end, where all give up, but waits
+    // and arrives no more and writes nothing: so the others give up, too, and all end.
+    int at_place = s.end - todo;
     auto wait_for = [&](uint64_t* bar, uint32_t parity) {
       if (!ok) return;
       ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
-      if (!ok && lane == 0) atomicMin(&s.stop, s.end - todo);
+      if (!ok && lane == 0) atomicMin(&s.stop, at_place);
     };
     int n = 0, ct = 0;
-    for (int seg = 0; todo > x.lead; ++seg) {
-      todo -= x.lead;
-      const Item<R> it(p, x, todo);
-      const int ring = seg % kItemRing, row0 = x.mt * R, token0 = row0 / p.group;
+#pragma unroll 1
+    for (int seg = 0; todo > 0; ++seg) {
+      const int side = seg & 1;
+      wait_for(&s.item_full[side], (seg >> 1) & 1);
+      if (any_of(5, kRowThreads, !ok)) break;
+      const Facts it = s.facts[side];
+      if (it.tile1 < 0) break;
+      at_place = it.at;
       const int chunks = (it.rows + 7) / 8;
-      if (it.tile1 > it.n_cache) {
-        // a token's ancestors: one thread walks up from each token
-        sync_of(5, kRowThreads);  // (done with the last ones)
-#pragma unroll 1
-        for (int i = t; i < it.end; i += kRowThreads) {
-          const int up = a.parents ? a.parents[x.r.first + i] : i - 1;
-          s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
-        }
-        if (t < R) s.token[t] = uint8_t((row0 + t) / p.group - token0);
-        sync_of(5, kRowThreads);
-        if (t < it.end - token0) {
-          const int words = tree_tiles(it.end) * (kTile / 32);
-#pragma unroll 1
-          for (int w = 0; w < words; ++w) s.seen[t][w] = 0;
-#pragma unroll 1
-          for (int i = token0 + t; i >= 0; i = s.up[i]) s.seen[t][i >> 5] |= 1u << (i & 31);
-        }
-        sync_of(5, kRowThreads);
-      }
-      float* const my_shift = s.shift[set];
-      float* const my_fall = s.fall[seg & 1][set];
-      const bool whole = it.tile0 == 0 && it.tile1 == it.n_cache + tree_tiles(it.end);
-      // where a row goes: to the output, or to its place in the CTA's piece
-      if (t < R) {
-        const int token = (row0 + t) / p.group;
-        s.row_to[seg & 1][t] =
-            whole ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + t - token * p.group
-                  : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + t;
-      }
+      const bool whole = it.tile0 == 0 && it.tile1 == it.n_tree + cache_tiles(it.len);
       // sums of the weights, from nothing
 #pragma unroll 1
-      for (int c = 0; c < chunks; ++c) {
+      for (int c = sub; c < chunks; c += kSubs) {
         const uint32_t zero[8] = {};
         tmem_st8(my_sums + 8 * c, zero);
       }
@@ -947,13 +976,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       int code = 0;  // the output is in units of 2^(code - 127)
 #pragma unroll 1
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
-        const bool cache = j < it.n_cache;
+        const bool cache = j >= it.n_tree;
         if ((n & 1) != set) {
           ct += cache;
           continue;
         }
         const bool first = code == 0;
-        bool there = key < it.keys(x, j);
+        bool there = key < tile_keys(j, it.n_tree, it.end, it.len);
         float scale = 1.f, value = 1.f;
         int top_code = kOwnCode;
         if (cache) {
@@ -965,14 +994,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           there = there && !(s.left_out[0][e] >> (key / TT_SCALE_SLOTS) & 1);
           ++ct;
         }
-        wait_for(&s.s_full[set], (n >> 1) & 1);
+        wait_for(&s.s_full[n & 3], (n >> 2) & 1);
         tc_fence_after();
+        const uint32_t at = mine + (n & 3) * R;
         const f32x2 scale2 = pair(scale, scale);
         // The scores of this thread's key with the rows of chunk c, two to a number; times
         // the key's scale and its row's factor and with its row's shift they are exponents of
         // weights. (They are read again where they are needed again: the loops over chunks
         // are rolled, as unrolled code of this size came from beyond the instruction caches.)
-        const float* const factors = cache ? s.factor[ring] : s.own_factor;
+        const float* const factors = cache ? s.factor[side] : s.own_factor;
         const int factor_step = cache ? 4 : 0;
         const uint32_t mask = there ? 0xff : 0;
         const bool plain = cache && __all_sync(0xffffffffu, there);
@@ -982,7 +1012,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           if (plain) return;
           const uint32_t seen =
               cache ? mask
-                    : mask & tree_sees(s.seen[0], s.token + 8 * c, ((j - it.n_cache) * kTile + key) >> 5, lane);
+                    : mask & tree_sees(s.seen[side][0], s.token[side] + 8 * c, (j * kTile + key) >> 5, lane);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float lo, hi;
@@ -996,7 +1026,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         // has none), and what that makes of the output.
         auto raise = [&] {
 #pragma unroll 1
-          for (int c = 0; c < chunks; ++c) {
+          for (int c = sub; c < chunks; c += kSubs) {
             uint32_t v[8];
             tmem_ld8(at + 8 * c, v);
             tmem_wait8(v);
@@ -1015,8 +1045,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             if (lane < 8) s.part[set][quarter][8 * c + lane] = top;
           }
           sync_of(barrier, 128);
+          // (a thread to each of these warps' rows, as far as there are so many)
           bool none = false;
-          const int row = quarter * 32 + lane;
+          const int row = 8 * (sub + kSubs * (key / 8)) + key % 8;
           if (row < it.rows) {
             const auto& part = s.part[set];
             const float top = fmaxf(fmaxf(part[0][row], part[1][row]), fmaxf(part[2][row], part[3][row]));
@@ -1080,25 +1111,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
               *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
                   make_uint4(out[0], out[1], out[2], out[3]);
             };
-            // (a chunk is fetched while the one before it is weighed)
-            uint32_t v0[8], l0[8], v1[8], l1[8];
-            fetch(0, v0, l0);
+            if constexpr (kSubs == 1) {
+              // (a chunk is fetched while the one before it is weighed)
+              uint32_t v0[8], l0[8], v1[8], l1[8];
+              fetch(0, v0, l0);
 #pragma unroll 1
-            for (int c = 0; c < chunks; c += 2) {
-              tmem_wait8(v0);
-              tmem_wait8(l0);
-              if (c + 1 < chunks) fetch(c + 1, v1, l1);
-              weigh(c, v0, l0);
-              if (c + 1 >= chunks) break;
-              tmem_wait8(v1);
-              tmem_wait8(l1);
-              if (c + 2 < chunks) fetch(c + 2, v0, l0);
-              weigh(c + 1, v1, l1);
+              for (int c = 0; c < chunks; c += 2) {
+                tmem_wait8(v0);
+                tmem_wait8(l0);
+                if (c + 1 < chunks) fetch(c + 1, v1, l1);
+                weigh(c, v0, l0);
+                if (c + 1 >= chunks) break;
+                tmem_wait8(v1);
+                tmem_wait8(l1);
+                if (c + 2 < chunks) fetch(c + 2, v0, l0);
+                weigh(c + 1, v1, l1);
+              }
+            } else {
+#pragma unroll 1
+              for (int c = sub; c < chunks; c += kSubs) {
+                uint32_t v[8], l[8];
+                fetch(c, v, l);
+                tmem_wait8(v);
+                tmem_wait8(l);
+                weigh(c, v, l);
+              }
             }
             pass = !early && any_of(barrier, 128, over > kSlack + kOffset) ? 2 : 3;
           } else {
 #pragma unroll 1
-            for (int c = 0; c < chunks; ++c) {
+            for (int c = sub; c < chunks; c += kSubs) {
               f32x2 z[4];
               uint32_t v[8], l[8];
               tmem_wait_st();
@@ -1130,12 +1172,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         } while (pass < 3);
         const bool raised = pass == 4;
         tc_fence_before();
-        if (ok) mbar_arrive(&s.s_free[set]);
+        if (ok) mbar_arrive(&s.s_free[n & 3]);
         if ((raised || early || output_fall != 1.f) && !first) {
           // (its last product is done: that of two tiles ago, for which this warp has waited)
           tc_fence_after();
 #pragma unroll 1
-          for (int c = 0; c < chunks; ++c) {
+          for (int c = sub; c < chunks; c += kSubs) {
             uint32_t v[8];
             tmem_ld8(output + 8 * c, v);
             tmem_wait8(v);
@@ -1153,9 +1195,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       }
       // the sums of all keys
       if (code) {
-        sync_of(barrier, 128);  // (done with s.part and s.fall)
 #pragma unroll 1
-        for (int c = 0; c < chunks; ++c) {
+        for (int c = sub; c < chunks; c += kSubs) {
           uint32_t l[8];
           tmem_ld8(my_sums + 8 * c, l);
           tmem_wait8(l);
@@ -1163,68 +1204,69 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
 #pragma unroll
           for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
           const float sum = warp_sums(sums, lane);
+          if (c == sub) sync_of(barrier, 128);  // (done with s.part)
           if (lane < 8) s.part[set][quarter][8 * c + lane] = sum;
         }
       }
-      if (quarter == 0 && lane == 0) s.code[seg & 1][set] = code;
+      if (sub == 0 && quarter == 0 && lane == 0) s.code[set] = code;
       sync_of(5, kRowThreads);
       if (t < it.rows) {
         // the sets' sums and outputs relative to the larger of their references
-        float top = -INFINITY, all = 0.f, l[kSets], f[kSets];
-        const int* const codes = s.code[seg & 1];
+        float top = -INFINITY, all = 0.f, f[kSets];
 #pragma unroll
         for (int k = 0; k < kSets; ++k)
-          if (codes[k]) top = fmaxf(top, s.ref[k][t]);
+          if (s.code[k]) top = fmaxf(top, s.ref[k][t]);
 #pragma unroll
         for (int k = 0; k < kSets; ++k) {
-          l[k] = f[k] = 0.f;
-          if (codes[k]) {
-            const auto& part = s.part[k];
+          f[k] = 0.f;
+          if (s.code[k]) {
             const float ref = s.ref[k][t];
-            l[k] = part[0][t] + part[1][t] + (part[2][t] + part[3][t]);
-            f[k] = ref == -INFINITY ? (l[k] != l[k] ? 1.f : 0.f) : ex2_approx(ref - top);
-            all = fmaf(l[k], f[k], all);
+            const float l = s.part[k][0][t] + s.part[k][1][t] + (s.part[k][2][t] + s.part[k][3][t]);
+            f[k] = ref == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(ref - top);
+            all = fmaf(l, f[k], all);
           }
         }
         const float m2 = top == -INFINITY ? -INFINITY : top - kOffset;
         const float inverse = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
 #pragma unroll
         for (int k = 0; k < kSets; ++k)
-          s.fall[seg & 1][k][t] = f[k] * inverse * (codes[k] ? e8m0(codes[k]) : 0.f);
-        const int64_t to = s.row_to[seg & 1][t];
+          s.share_of[k][t] = f[k] * inverse * (s.code[k] ? e8m0(s.code[k]) : 0.f);
+        const int64_t to = s.row_to[side][t];
         if (ok && !whole)
           p.part_ml[to] = make_float2(m2, all);
         else if (ok && a.lse)
           a.lse[to] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
       }
+      const bool used[kSets] = {s.code[0] != 0, s.code[1] != 0};
+      bool odd = false;
+      if (it.tile0 < it.n_tree) odd = lane < kWords && s.odd[side][lane];
+      odd = __any_sync(0xffffffffu, odd);
       sync_of(5, kRowThreads);
       wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
       if (n > 1) wait_for(&s.o_done[n & 1], ((n - 2) >> 1) & 1);
       tc_fence_after();
-      bool odd = false;
-      if (it.tile1 > it.n_cache) odd = lane < kWords && s.odd[ring][lane];
-      odd = __any_sync(0xffffffffu, odd);
       if (D == 128 || quarter < 2) {
 #pragma unroll 1
-        for (int c = set; c < chunks; c += kSets) {
+        for (int c = four; c < chunks; c += kSets * kSubs) {
           float y[8] = {};
 #pragma unroll
           for (int k = 0; k < kSets; ++k) {
-            if (!s.code[seg & 1][k]) continue;
+            if (!used[k]) continue;
             uint32_t v[8];
             tmem_ld8(mine + S::kOut + k * R + 8 * c, v);
             tmem_wait8(v);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-              y[i] = fmaf(__uint_as_float(v[i]), s.fall[seg & 1][k][8 * c + i], y[i]);
+              y[i] = fmaf(__uint_as_float(v[i]), s.share_of[k][8 * c + i], y[i]);
           }
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const int r = 8 * c + i;
             if (r < it.rows && ok) {
               if (odd)
-                y[i] += odd_values<DT>(a, s.odd[ring], s.seen[s.token[r]], it.end, x.r.first, x.hk, key);
-              const int64_t to = s.row_to[seg & 1][r] * D + key;
+                y[i] += odd_values<DT>(a, s.odd[side], s.seen[side][s.token[side][r]], it.end, it.first,
+                                       it.hk, key);
+              const int64_t to = s.row_to[side][r] * D + key;
               if (whole)
                 store_elem<DT>(a.out + to * 2, y[i]);
               else
@@ -1234,9 +1276,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         }
       }
       tc_fence_before();
-      if (ok) mbar_arrive(&s.o_free);
-      todo -= it.tile1 - it.tile0;
-      x = next_place<R>(p.a, p.group, x);
+      if (ok) mbar_arrive(&s.o_free[side]);
     }
   }
   tc_fence_before();
@@ -1420,7 +1460,7 @@ cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(kThreads);
+  cfg.blockDim = dim3(Warps<R>::kThreads);
   cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
   cfg.stream = stream;
   cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, R, F16>, p);
