@@ -7,28 +7,27 @@
 // m = max s_x and l = sum 2^(s_x - m), a larger m scales what was summed before.
 //
 // The bound is the cache, half of what 16 bits take, so half the time for each of its
-// tiles, and few rows: the tokens of a request times the query heads that share a key
-// head, often under 64. So keys take the rows of the matrix products and tokens the
-// columns: scores S^T = K Q^T and outputs O^T = V^T P^T, of 128 keys and up to 64
-// columns, cost what the columns cost. A thread then holds one key's scores of many
-// tokens: its scale is one number, its mask one bit, and the sums of the weights stay
-// in registers until an item ends. Only a row's maximum goes across threads, and it is
-// asked for only where a score passes the reference by 2^kSlack, which a vote tells.
+// tiles. Their products are matrix products: 128 rows (token, head of the group) against
+// tiles of 128 keys. Keys are multiplied as they are, e4m3 by e4m3: a query is the sum of
+// two (bf16) or three (fp16) e4m3 pieces of a power of two of its row, its 8 or 11 digits
+// exactly for elements down to 2^-10 of the row's largest, and within 2^-19 of that below;
+// the products add the pieces up. Values become fp16, which holds every e4m3 value, by four
+// warps of their own, in units of the largest scale so far (2^-24 of that unit is the
+// finest); when a larger one comes the sums fall. The request's own drafted tokens are
+// tiles of keys and values of the inputs' type.
 //
-// Keys are multiplied as they are, e4m3 by e4m3: a query is the sum of two (bf16) or
-// three (fp16) e4m3 pieces, sixteen times finer each, of a power of two of its row:
-// its 8 or 11 digits exactly, but for elements 2^-17 below the row's largest, whose
-// digits end at 2^-22 of it. Values become fp16, which holds every e4m3 value, by four
-// warps of their own (weights in pieces would cost the rows' warps more); their scale
-// goes to the weights, of the largest scale so far, so that fp16 holds those of scales
-// 2^-20 below it as well as the largest's. The request's own drafted tokens are a tile
-// of keys and values of the inputs' type.
+// One CTA per SM: two warps copy (a page's slots at a time) keys and values with their
+// scales, four convert, two issue the products, eight hold the rows, two threads each.
+// While rows turn a tile's scores into weights, the next tile's scores and the last one's
+// product with values are under way: tensor memory holds two tiles' scores, two tiles'
+// weights and the output. Tiles of all requests, key heads and 128 rows form one list,
+// which the CTAs share evenly: lengths are known on the device alone. Items cut by a CTA's
+// end leave unnormalised pieces, which a second kernel joins.
 //
-// One CTA per SM: a warp copies tiles (a page at a time) and their scales, four convert,
-// one thread issues products, eight warps hold the scores, two for 32 keys each. Tiles
-// of all requests, key heads and 64 rows form one list, which the CTAs share evenly:
-// lengths are known on the device alone. Items cut by a CTA's end leave unnormalised
-// pieces, which a second kernel joins.
+// Built and taken back: keys as the rows of the products and tokens as their columns, so
+// that they cost what the columns cost. A thread then has a key, and a row's factor,
+// maximum and sum come from shared memory or go across threads: 12 instructions a score
+// for 4 here, and a serving batch took 199 us.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
@@ -54,17 +53,9 @@ namespace {
 
 constexpr int kTile = 128;                     // keys of a tile
 constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
-// Eight warps turn scores into weights, 32 keys each, for 64 rows sixteen: half of them
-// take the even tiles and half the odd ones, each with references, sums and an output of
-// their own. What a tile takes from its scores to its weights is mostly waiting, and so
-// two are on their way.
-constexpr int kSets = 2;
-template <int R>
-struct Warps {
-  static constexpr int kSubs = R == 64 ? 2 : 1;  // fours of a set, which share the rows
-  static constexpr int kRow = 4 * kSets * kSubs, kRowThreads = kRow * 32;
-  static constexpr int kThreads = kRowThreads + kConvThreads + 128;  // of a CTA
-};
+constexpr int kRows = 128;                     // of an item
+constexpr int kRowWarps = 8, kRowThreads = kRowWarps * 32;  // two for each 32 rows
+constexpr int kThreads = kRowThreads + kConvThreads + 128;
 constexpr int kWords = TT_MAX_TREE / 32;
 constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
 constexpr int kScaleRing = 16;                   // tiles' scales that are kept
@@ -101,8 +92,8 @@ struct Tree8Args {
   int slots_inner;    // the cache maps' second dimension is the slot, the third the head
   // pieces: CTA c leaves that of an item that began before its tiles at 2 c, that
   // of one that begins in them at 2 c + 1
-  float* part;        // [2 ctas * R * D] outputs, not normalised
-  float2* part_ml;    // [2 ctas * R] their reference maximum (log2) and sum
+  float* part;        // [2 ctas * kRows * D] outputs, not normalised
+  float2* part_ml;    // [2 ctas * kRows] their reference maximum (log2) and sum
   int32_t* first;     // [B + 1] places before each request's, then the places per CTA
   int32_t* stop;      // [ctas] the place from which a CTA gave up, INT32_MAX if it did not
   uint64_t wait_ns;   // limit of a wait
@@ -133,25 +124,21 @@ __device__ __forceinline__ Request request(const TreeArgs& a, int b) {
 // tokens up to its last row's.
 __host__ __device__ inline int cache_tiles(int len) { return len / kTile + (len % kTile != 0); }
 __host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / kTile; }
-template <int R>
 __host__ __device__ inline int items(int nodes, int group) {
-  return (nodes * group + R - 1) / R;
+  return (nodes * group + kRows - 1) / kRows;
 }
-template <int R>
 __device__ __forceinline__ int item_end(const Request& r, int group, int mt) {  // its last token + 1
-  return (min(r.nodes * group, (mt + 1) * R) - 1) / group + 1;
+  return (min(r.nodes * group, (mt + 1) * kRows) - 1) / group + 1;
 }
-template <int R>
 __device__ __forceinline__ int item_tiles(const Request& r, int group, int mt) {
-  return cache_tiles(r.len) + tree_tiles(item_end<R>(r, group, mt));
+  return cache_tiles(r.len) + tree_tiles(item_end(r, group, mt));
 }
 // The places that one key head of a request takes in the list.
-template <int R>
 __device__ __noinline__ int head_places(const Request r, int group) {
-  const int n = items<R>(r.nodes, group);
+  const int n = items(r.nodes, group);
   int sum = n * (kItemCost + cache_tiles(r.len));
 #pragma unroll 1
-  for (int mt = 0; mt < n; ++mt) sum += tree_tiles(item_end<R>(r, group, mt));
+  for (int mt = 0; mt < n; ++mt) sum += tree_tiles(item_end(r, group, mt));
   return sum;
 }
 // An item of the list, the first of its tiles that is left, and the places before it.
@@ -162,26 +149,24 @@ struct Place {
   int b, hk, mt, tile, lead;
   Request r;
 };
-template <int R>
 __device__ __noinline__ Place find_place(const TreeArgs& a, int group, int request_b, int offset) {
   Place x;
   x.b = request_b;
   x.r = request(a, request_b);
-  const int per_head = head_places<R>(x.r, group);
+  const int per_head = head_places(x.r, group);
   x.hk = offset / per_head;
   offset %= per_head;
   x.mt = 0;
 #pragma unroll 1
-  for (int n; offset >= (n = kItemCost + item_tiles<R>(x.r, group, x.mt)); ++x.mt) offset -= n;
+  for (int n; offset >= (n = kItemCost + item_tiles(x.r, group, x.mt)); ++x.mt) offset -= n;
   x.tile = max(0, offset - kItemCost);
   x.lead = max(0, kItemCost - offset);
   return x;
 }
-template <int R>
 __device__ __noinline__ Place next_place(const TreeArgs& a, int group, Place x) {
   x.tile = 0;
   x.lead = kItemCost;
-  if (++x.mt * R < x.r.nodes * group) return x;
+  if (++x.mt * kRows < x.r.nodes * group) return x;
   x.mt = 0;
   if (++x.hk < a.Hkv) return x;
   x.hk = 0;
@@ -194,12 +179,11 @@ __device__ __noinline__ Place next_place(const TreeArgs& a, int group, Place x) 
 }
 // The part of an item that a CTA takes: tiles of drafted tokens, which have to come from
 // further away, first, then the cache's.
-template <int R>
 struct Item {
   int n_tree, rows, tile0, tile1, end;
   __device__ __forceinline__ Item(const Tree8Args& p, const Place& x, int todo) {
-    rows = min(R, x.r.nodes * p.group - x.mt * R);
-    end = item_end<R>(x.r, p.group, x.mt);
+    rows = min(kRows, x.r.nodes * p.group - x.mt * kRows);
+    end = item_end(x.r, p.group, x.mt);
     n_tree = tree_tiles(end);
     tile0 = x.tile;
     tile1 = min(n_tree + cache_tiles(x.r.len), x.tile + todo);
@@ -211,7 +195,7 @@ __device__ __forceinline__ int tile_keys(int j, int n_tree, int end, int len) {
 }
 // What the converting warps, which come to an item first, tell the others of it.
 struct Facts {
-  int n_tree, rows, tile0, tile1, end, len, first, hk, at;  // at: the place of its first tile
+  int n_tree, rows, tile0, tile1, end, len, first, hk, row0, at;  // at: the place of its first tile
 };
 
 // Whether every parent and page of the request is in range (the row threads).
@@ -232,43 +216,33 @@ __device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Reques
   return bad;
 }
 
-template <int D, int R, bool F16>
+template <int D, bool F16>
 struct Smem8 {
   static constexpr int kPieces = F16 ? 3 : 2;  // of queries
-  // Tensor memory: scores of four tiles, of each set its output and the sums of its weights.
-  static constexpr int kOut = 4 * R, kSums = kOut + kSets * R, kUsed = kSums + kSets * R;
-  static constexpr int kColumns = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+  // Tensor memory: scores of two tiles, weights of two (a column holds two keys'), the output.
+  static constexpr int kWeights = 2 * kTile, kOut = 3 * kTile, kColumns = 512;
   // what 227 KB hold
-  static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : R == 64 && F16 ? 2 : 3;
-  static constexpr int kStagesV = D == 64 ? 6 : R == 64 ? 2 : 3;
-  static constexpr int kThreads = Warps<R>::kThreads;
+  static constexpr int kStagesK = D == 64 ? 5 : F16 ? 2 : 3, kStagesV = D == 64 ? 5 : 2;
   char w[2][kTile * D * 2];           // values of 16 bits; a drafted tile's keys too
-  char p[2][kTile * 128];             // weights, the rows of a key side by side
+  char q16[kRows * D * 2];            // queries for drafted keys,
+  char q8[kPieces * kRows * D];       // and in pieces for the cache's
   char k[kStagesK][kTile * D];        // keys and values as they come
-  char q16[R * D * 2];                // queries for drafted keys,
-  char q8[kPieces * R * D];           // and in pieces for the cache's
   char v[kStagesV][kTile * D];
+  uint32_t seen[kRows][kWords];       // a token's ancestors and itself
   // of this item and the next one
-  uint32_t seen[2][R][kWords];        // a token's ancestors and itself
-  alignas(16) float factor[2][R];     // a row's pieces times it and a key's scale: log2 scores
+  float factor[2][kRows];             // a row's pieces times it and a key's scale: log2 scores
   uint32_t odd[2][kWords];            // drafted tokens with a value that is not finite
-  int64_t row_to[2][R];               // row of the output, or of the CTA's pieces
-  uint8_t token[2][R];                // of a row, from the item's first
   Facts facts[2];
-  int16_t up[TT_MAX_TREE];            // parents, -1 for roots
-  float k_scale[kScaleRing][kGroups], v_scale[kScaleRing][kGroups];
+  // of the tiles under way
+  alignas(16) float k_scale[kScaleRing][kGroups];
+  uint32_t v_scale[kScaleRing][kGroups];  // two fp16 numbers, of the tile's unit
   uint32_t left_out[2][kScaleRing];   // groups whose page is out of range: keys, values
-  int top_code[kScaleRing];           // the largest of the values' scales
-  alignas(16) float own_factor[8];    // the factor of drafted keys
-  alignas(16) float shift[kSets][R];  // what is added to log2 scores
-  alignas(16) float fall[kSets][R];   // a reference's last change
-  alignas(16) float share_of[kSets][R];  // of the output, at an item's end
-  float ref[kSets][R];                // reference maximum (log2)
-  float part[kSets][4][R];            // what the warps of 32 keys each tell
-  int code[kSets];                    // units of the outputs, 0: no tile
+  int unit[kScaleRing];               // largest scale of the item's values so far
+  float half[2][2][kRows];            // what the two threads of a row tell each other
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
-  uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[4], s_free[4];
-  uint64_t p_full[2], o_done[2], item_full[2], o_free[2], q_full, q_empty, own_full, drained[2];
+  uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
+  uint64_t p_full[2], o_done[2], item_full[2], o_free[2], seen_free, q_full, q_empty, own_full,
+      drained[2];
   long long sums[kThreads / 32];      // places of the requests, by warps
   int start_b, start_offset;          // where this CTA's places begin
   int share;                          // and how many a CTA has
@@ -276,31 +250,6 @@ struct Smem8 {
   int end, stop;                      // the place behind this CTA's, and where it gave up
 };
 
-// Numbers 2 i and 2 i + 1.
-__device__ __forceinline__ f32x2 both(const uint32_t (&v)[8], int i) {
-  return pair(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
-}
-__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t (&r)[8]) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-      : "r"(addr)
-      : "memory");
-}
-__device__ __forceinline__ void tmem_st8(uint32_t addr, const uint32_t (&r)[8]) {
-  asm volatile(
-      "tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(addr),
-      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-      : "memory");
-}
-// (The registers pass through, so that nothing reads them before.)
-__device__ __forceinline__ void tmem_wait8(uint32_t (&r)[8]) {
-  asm volatile("tcgen05.wait::ld.sync.aligned;"
-               : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]),
-                 "+r"(r[7])
-               :
-               : "memory");
-}
 // D[tmem] (+)= A[smem] B[smem] over 32 of K, both e4m3.
 __device__ __forceinline__ void umma8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile(
@@ -323,13 +272,9 @@ __device__ __forceinline__ int swizzled8(int r, int at) {
 }
 // 16-byte unit u of row r in 128-byte swizzled rows.
 __device__ __forceinline__ int swizzled16(int r, int u) { return r * 128 + ((u ^ (r & 7)) << 4); }
-// Instruction descriptors, fp32 accumulators, M = 128: e4m3 operands; and 16-bit ones that
-// both lie along M and N.
+// Instruction descriptor: fp32 accumulators, M = 128, N columns, e4m3 operands.
 __device__ __forceinline__ uint32_t idesc_e4m3(int n) {
   return 1u << 4 | uint32_t(n >> 3) << 17 | uint32_t(128 >> 4) << 24;
-}
-__device__ __forceinline__ uint32_t idesc_mn(bool f16, int n) {
-  return umma_idesc(f16, n, true) | 1u << 15;
 }
 // Whether any of `threads` threads says so; all of them come to the barrier.
 __device__ __forceinline__ bool any_of(int barrier, int threads, bool x) {
@@ -347,6 +292,19 @@ __device__ __forceinline__ bool any_of(int barrier, int threads, bool x) {
 __device__ __forceinline__ void sync_of(int barrier, int threads) {
   asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
 }
+// -inf in place of the scores whose bit is not set.
+__device__ __forceinline__ void hide(uint32_t (&v)[32], uint32_t see) {
+#pragma unroll
+  for (int i = 0; i < 32; ++i)
+    if (!(see >> i & 1)) v[i] = 0xff800000u;
+}
+// A product that may have become too small for a number, which -inf may be multiplied
+// by; NaN stays.
+__device__ __forceinline__ float not_zero(float x) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(0x1p-120f));
+  return r;
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -361,59 +319,54 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(r));
   return r != 0;
 }
-// The largest of a warp's numbers (NaN: none).
-__device__ __forceinline__ float warp_max(float x) {
-  const int i = x != x ? int(0x807fffff) : __float_as_int(x);  // (-inf)
-  const int top = __reduce_max_sync(0xffffffffu, i ^ ((i >> 31) & 0x7fffffff));
-  return __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
-}
-// Sums of N numbers over the lanes: lane i gets that of the i-th (mod N).
-template <int N>
-__device__ __forceinline__ float warp_sums(float (&x)[N], int lane) {
-#pragma unroll
-  for (int s = N / 2; s > 0; s /= 2)
-#pragma unroll
-    for (int i = 0; i < s; ++i) {
-      const float give = lane & s ? x[i] : x[i + s], keep = lane & s ? x[i + s] : x[i];
-      x[i] = keep + __shfl_xor_sync(0xffffffffu, give, s);
-    }
-#pragma unroll
-  for (int s = N; s < 32; s *= 2) x[0] += __shfl_xor_sync(0xffffffffu, x[0], s);
-  return x[0];
-}
-
-// What drafted tokens with a value that is not finite add to element d of a row that
-// sees them.
+// What drafted tokens with a value that is not finite add to elements d .. d + 31 of token
+// i's row: it walks up from there.
 template <int DT>
-__device__ __noinline__ float odd_values(const TreeArgs& a, const uint32_t* odd, const uint32_t* seen,
-                                         int end, int first, int hk, int d) {
-  float sum = 0.f;
+__device__ __noinline__ void odd_values(const TreeArgs& a, const uint32_t* odd, int first, int i, int hk,
+                                        int d, float (&sum)[32]) {
 #pragma unroll 1
-  for (int w = 0; w * 32 < end; ++w)
+  for (int e = 0; e < 32; ++e) sum[e] = 0.f;
 #pragma unroll 1
-    for (uint32_t both = odd[w] & seen[w]; both; both &= both - 1) {
-      const int64_t peer = int64_t(first) + w * 32 + __ffs(both) - 1;
-      const float z = load_elem<DT>(a.v + (peer * a.v_token + hk * a.v_head + d) * 2);
-      if (!(fabsf(z) < INFINITY)) sum += z;
+  for (int up; i >= 0; i = up) {
+    up = a.parents ? a.parents[first + i] : i - 1;
+    if (up < -1 || up >= i) up = -1;
+    if (!(odd[i >> 5] >> (i & 31) & 1)) continue;
+#pragma unroll 1
+    for (int e = 0; e < 32; ++e) {
+      const float z = load_elem<DT>(a.v + ((int64_t(first) + i) * a.v_token + hk * a.v_head + d + e) * 2);
+      if (!(fabsf(z) < INFINITY)) sum[e] += z;
     }
-  return sum;
+  }
+}
+// 2^-k as two fp16 numbers, k >= 0.
+__device__ __forceinline__ uint32_t half_power(int k) {
+  const uint32_t x = k <= 14 ? uint32_t(15 - k) << 10 : k <= 24 ? 1u << (24 - k) : 0u;
+  return x | x << 16;
+}
+__device__ __forceinline__ uint32_t half_mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// 32 bytes to memory: one store where they are known to start on 32 bytes (pieces), two
+// of 16 for the caller's output.
+template <bool TWO>
+__device__ __forceinline__ void store_sector(char* to, const uint32_t (&o)[8]) {
+  if constexpr (TWO) {
+    reinterpret_cast<uint4*>(to)[0] = make_uint4(o[0], o[1], o[2], o[3]);
+    reinterpret_cast<uint4*>(to)[1] = make_uint4(o[4], o[5], o[6], o[7]);
+  } else {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(o[0]),
+                 "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7])
+                 : "memory");
+  }
 }
 
-// Which of 8 rows see the drafted token of bit `lane` of a word.
-__device__ __noinline__ uint32_t tree_sees(const uint32_t* seen, const uint8_t* tokens, int word, int lane) {
-  uint32_t see = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) see |= (seen[tokens[i] * kWords + word] >> lane & 1) << i;
-  return see;
-}
-
-template <int D, int R, bool F16>
-__global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
-  using S = Smem8<D, R, F16>;
+template <int D, bool F16>
+__global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constant__ Tree8Args p) {
+  using S = Smem8<D, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
-  constexpr int kPieces = S::kPieces, kSubs = Warps<R>::kSubs;
-  constexpr int kRowWarps = Warps<R>::kRow, kRowThreads = Warps<R>::kRowThreads;
-  constexpr int kThreads = Warps<R>::kThreads;
+  constexpr int kPieces = S::kPieces;
   // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
   // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
   constexpr int kOwnCode = F16 ? 127 : 67;
@@ -440,22 +393,20 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.w_full[i], kConvThreads);
       mbar_init(&s.w_empty[i], 1);
-      mbar_init(&s.p_full[i], 128 * kSubs);
+      mbar_init(&s.s_full[i], 1);
+      mbar_init(&s.s_free[i], kRowThreads);
+      mbar_init(&s.p_full[i], kRowThreads);
       mbar_init(&s.o_done[i], 1);
       mbar_init(&s.item_full[i], kConvThreads);
       mbar_init(&s.o_free[i], kRowThreads);
     }
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(&s.s_full[i], 1);
-      mbar_init(&s.s_free[i], 128 * kSubs);
-    }
     mbar_init(&s.q_full, kConvThreads);
     mbar_init(&s.q_empty, 1);
     mbar_init(&s.own_full, kConvThreads);
+    mbar_init(&s.seen_free, kRowThreads);
     mbar_init(&s.drained[0], 1);
     mbar_init(&s.drained[1], 1);
     s.stop = INT32_MAX;
-    for (int i = 0; i < 8; ++i) s.own_factor[i] = p.scale2;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == kRowWarps + kConvWarps) tmem_alloc(&s.tmem, S::kColumns);
@@ -467,7 +418,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
               b1 = min(a.B, b0 + each);
     long long mine = 0;
 #pragma unroll 1
-    for (int b = b0; b < b1; ++b) mine += (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
+    for (int b = b0; b < b1; ++b) mine += (long long)(head_places(request(a, b), p.group)) * a.Hkv;
     long long upto = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -494,7 +445,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
     if (todo > 0 && from >= at && from < upto) {
 #pragma unroll 1
       for (int b = b0; b < b1; ++b) {
-        const long long n = (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
+        const long long n = (long long)(head_places(request(a, b), p.group)) * a.Hkv;
         if (from < at + n) {
           s.start_b = b;
           s.start_offset = int(from - at);
@@ -508,7 +459,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
 #pragma unroll 1
       for (int b = b0; b < b1; ++b) {
         p.first[b] = int(at);
-        at += (long long)(head_places<R>(request(a, b), p.group)) * a.Hkv;
+        at += (long long)(head_places(request(a, b), p.group)) * a.Hkv;
       }
       if (t == 0) p.first[a.B] = int(share);
     }
@@ -518,7 +469,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
   bool ok = true;
   Place x;
   x.lead = 0;
-  if (todo > 0 && warp >= kRowWarps) x = find_place<R>(p.a, p.group, s.start_b, s.start_offset);
+  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, p.group, s.start_b, s.start_offset);
 
   if (warp > kRowWarps + kConvWarps + 1) {
     // ------------------------------------------------------------ copies
@@ -535,25 +486,27 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
     struct Batch {
       int hk, page, in_page;  // of the lane's slots
       int tiles;              // 0: no more
+      int unit;               // of values, where an item begins, else -1
       uint32_t code;
     };
     int j = 0, j1 = 0, used = 0;
     bool open = false;
     auto next = [&]() {
-      Batch y{0, -1, 0, 0, 0};
+      Batch y{0, -1, 0, 0, -1, 0};
       for (;;) {
         if (!open) {
           if (todo <= x.lead) return y;
           todo -= x.lead;
-          const Item<R> it(p, x, todo);
+          const Item it(p, x, todo);
           j = max(0, it.tile0 - it.n_tree);
           j1 = it.tile1 - it.n_tree;
           used = it.tile1 - it.tile0;
+          y.unit = it.tile0 < it.n_tree ? kOwnCode : 1;
           open = true;
         }
         if (j < j1) break;
         todo -= used;
-        x = next_place<R>(p.a, p.group, x);
+        x = next_place(p.a, p.group, x);
         open = false;
       }
       y.tiles = min(kBatch, j1 - j);
@@ -568,7 +521,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
     auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
     Batch one, two;
     one.tiles = two.tiles = 0;
-    int n = 0, st = 0;
+    int n = 0, st = 0, unit = 1;
     uint32_t parity = 1;
 #pragma unroll 1
     for (int k = 0; ok && (k < 2 || one.tiles); ++k) {
@@ -583,7 +536,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
       const bool begins = mine && lane % kGroups * TT_SCALE_SLOTS % p.box == 0;
       const unsigned int lost = __ballot_sync(0xffffffffu, !mine);
       const unsigned int boxes = __ballot_sync(0xffffffffu, begins);
-      const float scale = e8m0(c.code);
+      if (c.unit > 0) unit = c.unit;
       int top = c.code != 255 ? int(c.code) : 0;
 #pragma unroll
       for (int o = 1; o < kGroups; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -596,19 +549,26 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
         // (The scales in this place are of kScaleRing tiles ago, which is further back than
         // the stages and the tiles on their way behind them reach.)
         const int ring = n % kScaleRing;
+        unit = max(unit, __shfl_sync(0xffffffffu, top, kGroups * i));
         if (lane / kGroups == i) {
-          (values ? s.v_scale : s.k_scale)[ring][lane % kGroups] = scale;
-          if (lane % kGroups == 0) {
-            s.left_out[values][ring] = lost >> (kGroups * i) & 0xff;
-            if (values) s.top_code[ring] = top;
-            mbar_arrive_expect_tx(&full[st], __popc(boxes >> (kGroups * i) & 0xff) * p.box * D);
-          }
+          if (values)
+            s.v_scale[ring][lane % kGroups] = c.code == 255 ? 0x7e007e00u : half_power(unit - int(c.code));
+          else
+            s.k_scale[ring][lane % kGroups] = e8m0(c.code);
+        }
+        if (lane == 0) {
+          s.left_out[values][ring] = lost >> (kGroups * i) & 0xff;
+          if (values) s.unit[ring] = unit;
+        }
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive_expect_tx(&full[st], __popc(boxes >> (kGroups * i) & 0xff) * p.box * D);
+          mbar_arrive(&s.scale_full[ring]);
         }
         __syncwarp();
         if (begins && lane / kGroups == i)
           tma_load_4d(smem_u32(dst) + st * (kTile * D) + lane % kGroups * TT_SCALE_SLOTS * D, map,
                       smem_u32(&full[st]), 0, at1, at2, c.page);
-        if (lane == 0) mbar_arrive(&s.scale_full[ring]);
         ++n;
         if (++st == stages) {
           st = 0;
@@ -627,7 +587,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
     auto on = [&](uint64_t* bar, uint32_t parity) {
       return __all_sync(0xffffffffu, wait8(bar, parity, limit)) != 0;
     };
-    constexpr uint32_t kWStep = kTile * D * 2 / 16, kKStep = kTile * D / 16, kPStep = kTile * 128 / 16;
+    constexpr uint32_t kWStep = kTile * D * 2 / 16, kKStep = kTile * D / 16;
     int n = 0, w = 0;  // tiles, 16-bit operands
     if (warp == kRowWarps + kConvWarps) {
       const uint64_t kd = umma8_desc<D>(smem_u32(s.k)), qd = umma8_desc<D>(smem_u32(s.q8)),
@@ -636,14 +596,14 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
 #pragma unroll 1
       for (int seg = 0; todo > x.lead && ok; ++seg) {
         todo -= x.lead;
-        const Item<R> it(p, x, todo);
+        const Item it(p, x, todo);
         ok = on(&s.q_full, seg & 1);
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
-          const int buf = n & 3;
-          const uint32_t to = tmem + buf * R;
+          const int buf = n & 1;
+          const uint32_t to = tmem + buf * kTile;
           if (j >= it.n_tree) {
-            ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 2) & 1) ^ 1);
+            ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -651,8 +611,8 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
               for (int q = 0; q < kPieces; ++q)
 #pragma unroll
                 for (int c = 0; c < D / 32; ++c)
-                  umma8_ss(to, kd + st * kKStep + 2 * c, qd + q * (R * D / 16) + 2 * c, idesc_e4m3(R),
-                           q > 0 || c > 0);
+                  umma8_ss(to, qd + q * (kRows * D / 16) + 2 * c, kd + st * kKStep + 2 * c,
+                           idesc_e4m3(kTile), q > 0 || c > 0);
               umma_commit(&s.s_full[buf]);
               umma_commit(&s.k_empty[st]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
@@ -664,14 +624,15 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
           } else {
             // (a barrier of their own: on w_full's, this warp could be two phases ahead, where
             // a parity says nothing)
-            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 2) & 1) ^ 1);
+            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
 #pragma unroll
               for (int c = 0; c < D / 16; ++c)
-                umma_ss(to, wk + (w & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
-                        od + (c / 4) * (R * 128 / 16) + (c % 4) * 2, umma_idesc(F16, R, false), c > 0);
+                umma_ss(to, od + (c / 4) * (kBlock / 16) + (c % 4) * 2,
+                        wk + (w & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
+                        umma_idesc(F16, kTile, false), c > 0);
               umma_commit(&s.s_full[buf]);
               umma_commit(&s.w_empty[w & 1]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
@@ -681,32 +642,30 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
           __syncwarp();
         }
         todo -= it.tile1 - it.tile0;
-        x = next_place<R>(p.a, p.group, x);
+        x = next_place(p.a, p.group, x);
       }
     } else {
-      const uint64_t wv = umma_desc(smem_u32(s.w), kBlock), pd = umma_desc(smem_u32(s.p), 16);
+      const uint64_t wv = umma_desc(smem_u32(s.w), kBlock);
 #pragma unroll 1
       for (int seg = 0; todo > x.lead && ok; ++seg) {
         todo -= x.lead;
-        const Item<R> it(p, x, todo);
+        const Item it(p, x, todo);
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
           if (j < it.n_tree) ++w;
           const int keys = tile_keys(j, it.n_tree, it.end, x.r.len), buf = n & 1;
           ok = on(&s.w_full[w & 1], (w >> 1) & 1) && on(&s.p_full[buf], (n >> 1) & 1) &&
-               (j - it.tile0 >= kSets || seg == 0 || on(&s.o_free[(seg - 1) & 1], ((seg - 1) >> 1) & 1));
+               (j > it.tile0 || seg == 0 || on(&s.o_free[(seg - 1) & 1], ((seg - 1) >> 1) & 1));
           if (!ok) break;
           tc_fence_after();
-          const uint32_t idesc = idesc_mn(F16 || j >= it.n_tree, R);
-          const uint32_t to = tmem + S::kOut + buf * R;
-          const bool more = j - it.tile0 >= kSets;
-          // (heads of 64: the other half of the 128 rows is of what lies behind the operand,
-          // the other one or the weights, and nobody reads it)
+          const uint32_t idesc = umma_idesc(F16 || j >= it.n_tree, D, true);
+          const uint32_t weights = tmem + S::kWeights + buf * (kTile / 2);
+          const bool more = j > it.tile0;
           if (elect_one()) {
 #pragma unroll
             for (int c = 0; c < kTile / 16; ++c)
               if (16 * c < keys)
-                umma_ss(to, wv + (w & 1) * kWStep + 128 * c, pd + buf * kPStep + 128 * c, idesc,
+                umma_ts(tmem + S::kOut, weights + 8 * c, wv + (w & 1) * kWStep + 128 * c, idesc,
                         more || c > 0);
             umma_commit(&s.o_done[buf]);
             umma_commit(&s.w_empty[w & 1]);
@@ -714,7 +673,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
           __syncwarp();
         }
         todo -= it.tile1 - it.tile0;
-        x = next_place<R>(p.a, p.group, x);
+        x = next_place(p.a, p.group, x);
       }
     }
     // (and until their last products and the arrivals for them are done)
@@ -729,75 +688,66 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
       if (ok) ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       return ok;
     };
-    int vt = 0, st = 0, w = 0, seg = 0;
+    int vt = 0, st = 0, w = 0, seg = 0, drafted = 0;
     uint32_t parity = 0;
 #pragma unroll 1
     for (; todo > x.lead && ok; ++seg) {
       todo -= x.lead;
-      const Item<R> it(p, x, todo);
-      const int side = seg & 1, row0 = x.mt * R, token0 = row0 / p.group;
+      const Item it(p, x, todo);
+      const int side = seg & 1, row0 = x.mt * kRows, token0 = row0 / p.group;
       // (the item before the last one is over)
       if (!wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1)) break;
       // Its facts, and a token's ancestors: one thread walks up from each token.
       if (ct == 0)
         s.facts[side] = Facts{it.n_tree, it.rows, it.tile0, it.tile1, it.end,
-                              x.r.len,   x.r.first, x.hk,   s.end - todo};
-      if (ct < R) {
-        const int token = (row0 + ct) / p.group;
-        s.token[side][ct] = uint8_t(token - token0);
-        s.row_to[side][ct] =
-            it.tile0 == 0 && it.tile1 == it.n_tree + cache_tiles(x.r.len)
-                ? (int64_t(x.r.first) + token) * a.Hq + x.hk * p.group + row0 + ct - token * p.group
-                : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * R + ct;
-      }
+                              x.r.len,   x.r.first, x.hk,   row0,     s.end - todo};
       if (ct < kWords) s.odd[side][ct] = 0;
       if (it.tile0 < it.n_tree) {
-        sync_of(6, kConvThreads);  // (done with the last ones)
+        // (the parents in the place of the values to come, the ancestors once rows are done
+        // with the last ones)
+        if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1) ||
+            !wait_for(&s.seen_free, (drafted++ & 1) ^ 1))
+          break;
+        int16_t* const ups = reinterpret_cast<int16_t*>(s.w[w & 1]);
 #pragma unroll 1
         for (int i = ct; i < it.end; i += kConvThreads) {
           const int up = a.parents ? a.parents[x.r.first + i] : i - 1;
-          s.up[i] = int16_t(up < -1 || up >= i ? -1 : up);
+          ups[i] = int16_t(up < -1 || up >= i ? -1 : up);
         }
         sync_of(6, kConvThreads);
         if (ct < it.end - token0) {
           const int words = it.n_tree * (kTile / 32);
 #pragma unroll 1
-          for (int k = 0; k < words; ++k) s.seen[side][ct][k] = 0;
+          for (int k = 0; k < words; ++k) s.seen[ct][k] = 0;
 #pragma unroll 1
-          for (int i = token0 + ct; i >= 0; i = s.up[i]) s.seen[side][ct][i >> 5] |= 1u << (i & 31);
+          for (int i = token0 + ct; i >= 0; i = ups[i]) s.seen[ct][i >> 5] |= 1u << (i & 31);
         }
+        sync_of(6, kConvThreads);
       }
-      // Queries: kEach threads to a row.
+      // Queries: a thread to a row.
       {
-        constexpr int kEach = kConvThreads / R, kVecs = D / 8 / kEach;
-        const int r = ct / kEach, sub = ct % kEach;
-        const int row = x.mt * R + r, token = row / p.group, head = x.hk * p.group + row % p.group;
-        uint4 q[kVecs];
-        const bool valid = r < it.rows;
-        const char* from = a.q + ((int64_t(x.r.first) + token) * a.q_token + int64_t(head) * a.q_head) * 2;
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-          q[i] = valid ? reinterpret_cast<const uint4*>(from)[sub * kVecs + i] : make_uint4(0, 0, 0, 0);
+        const int row = row0 + ct, token = row / p.group, head = x.hk * p.group + row % p.group;
+        const bool valid = ct < it.rows;
+        const uint4* from = reinterpret_cast<const uint4*>(
+            a.q + ((int64_t(x.r.first) + token) * a.q_token + int64_t(head) * a.q_head) * 2);
         float top = 0.f;
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
+#pragma unroll 4
+        for (int u = 0; u < D / 8; ++u) {
           float e[8];
-          unpack16<DT>(q[i], e);
+          unpack16<DT>(valid ? from[u] : make_uint4(0, 0, 0, 0), e);
 #pragma unroll
           for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
         }
-#pragma unroll
-        for (int o = 1; o < kEach; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const uint32_t code = e8m0_for(top);
         const float inverse = e8m0_inverse(code);
         if (!wait_for(&s.q_empty, (seg & 1) ^ 1)) break;
-        if (sub == 0) s.factor[side][r] = p.scale2 * e8m0(code);
-#pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-          const int u = sub * kVecs + i;  // 16-byte unit of the row
-          *reinterpret_cast<uint4*>(s.q16 + (u / 8) * (R * 128) + swizzled16(r, u % 8)) = q[i];
+        s.factor[side][ct] = p.scale2 * e8m0(code);
+#pragma unroll 2
+        for (int u = 0; u < D / 8; ++u) {  // (read again: from L1 or L2)
+          const uint4 q = valid ? from[u] : make_uint4(0, 0, 0, 0);
+          *reinterpret_cast<uint4*>(s.q16 + (u / 8) * kBlock + swizzled16(ct, u % 8)) = q;
           float e[8];
-          unpack16<DT>(q[i], e);
+          unpack16<DT>(q, e);
 #pragma unroll
           for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
             e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
@@ -812,7 +762,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
               e[2 * k] -= f.x;
               e[2 * k + 1] -= f.y;
             }
-            *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) =
+            *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * kRows + ct, u * 8)) =
                 make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
           }
         }
@@ -835,10 +785,14 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
           const int u = ct % 8, key0 = ct / 8;  // (its keys are 16 apart)
           const char* const from = s.v[st] + key0 * D + u * 8;
           char* const to = s.w[w & 1] + swizzled16(key0, u);
-          auto convert = [](const uint2& in) {
-            return make_uint4(e4m3x2_to_f16x2(in.x & 0xffff), e4m3x2_to_f16x2(in.x >> 16),
-                              e4m3x2_to_f16x2(in.y & 0xffff), e4m3x2_to_f16x2(in.y >> 16));
+          auto convert = [](const uint2& in, uint32_t scale) {
+            return make_uint4(half_mul2(e4m3x2_to_f16x2(in.x & 0xffff), scale),
+                              half_mul2(e4m3x2_to_f16x2(in.x >> 16), scale),
+                              half_mul2(e4m3x2_to_f16x2(in.y & 0xffff), scale),
+                              half_mul2(e4m3x2_to_f16x2(in.y >> 16), scale));
           };
+          // (its k-th key is one of the k-th 16 slots)
+          const uint32_t* const scales = s.v_scale[ring];
           if (keys == kTile && lost == 0) {
 #pragma unroll
             for (int h = 0; h < kPairs; ++h) {
@@ -848,7 +802,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
                 in[k] = *reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64);
 #pragma unroll
               for (int k = 0; k < kEach; ++k)
-                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in[k]);
+                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in[k], scales[k]);
             }
           } else {
 #pragma unroll 1
@@ -859,7 +813,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
               for (int h = 0; h < kPairs; ++h) {
                 uint2 in = make_uint2(0, 0);
                 if (there) in = *reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64);
-                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in);
+                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = there ? convert(in, scales[k]) : make_uint4(0, 0, 0, 0);
               }
             }
           }
@@ -921,7 +875,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
         ++w;
       }
       todo -= it.tile1 - it.tile0;
-      x = next_place<R>(p.a, p.group, x);
+      x = next_place(p.a, p.group, x);
     }
     // (no more)
     if (ok && wait_for(&s.o_free[seg & 1], ((seg >> 1) & 1) ^ 1)) {
@@ -937,14 +891,15 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
       const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t, kRowThreads));
       if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
-    const int quarter = warp & 3, four = warp >> 2, key = quarter * 32 + lane;
-    const int set = four / kSubs, sub = four % kSubs;
+    const int quarter = warp & 3, half = warp >> 2, row = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
-    const uint32_t output = mine + S::kOut + set * R, my_sums = mine + S::kSums + set * R;
-    const int barrier = 1 + four;  // of its four warps
-    float* const my_shift = s.shift[set];
-    float* const my_fall = s.fall[set];
-    char* const weights = s.p[set] + key * 128;
+    const int c0 = 64 * half;                                     // its first key of a tile
+    // tells the row's other thread x, and returns what that told (turn: of two)
+    auto other = [&](float y, int turn) {
+      s.half[turn][half][row] = y;
+      sync_of(1 + quarter, 64);
+      return s.half[turn][half ^ 1][row];
+    };
     // A warp goes on, or gives up, as one. One that gave up passes the barriers between
     // the warps as often as the others until the item's end, where all give up, but waits
     // and arrives no more and writes nothing: so the others give up, too, and all end.
@@ -963,316 +918,195 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
       const Facts it = s.facts[side];
       if (it.tile1 < 0) break;
       at_place = it.at;
-      const int chunks = (it.rows + 7) / 8;
-      const bool whole = it.tile0 == 0 && it.tile1 == it.n_tree + cache_tiles(it.len);
-      // sums of the weights, from nothing
-#pragma unroll 1
-      for (int c = sub; c < chunks; c += kSubs) {
-        const uint32_t zero[8] = {};
-        tmem_st8(my_sums + 8 * c, zero);
-      }
-      tmem_wait_st();
-      bool unset = true;
-      int code = 0;  // the output is in units of 2^(code - 127)
+      const bool valid = row < it.rows;
+      const bool some = __any_sync(0xffffffffu, valid);  // (others only keep step)
+      const int token = (it.row0 + row) / p.group, local = token - it.row0 / p.group;
+      const float factor = s.factor[side][row];
+      float m = -INFINITY, l = 0.f;  // the reference maximum (log2) and the sum
+      int code = 0;                  // the output is in units of 2^(code - 127)
 #pragma unroll 1
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
-        const bool cache = j >= it.n_tree;
-        if ((n & 1) != set) {
-          ct += cache;
-          continue;
-        }
-        const bool first = code == 0;
-        bool there = key < tile_keys(j, it.n_tree, it.end, it.len);
-        float scale = 1.f, value = 1.f;
-        int top_code = kOwnCode;
+        const bool cache = j >= it.n_tree, first = j == it.tile0;
+        const int keys = tile_keys(j, it.n_tree, it.end, it.len), e = ct % kScaleRing;
+        float f[4];  // what makes a score of each 16 keys its log2
+        int unit = kOwnCode;
+        uint32_t lost = 0;
         if (cache) {
-          const int e = ct % kScaleRing;
           wait_for(&s.scale_full[e], (ct / kScaleRing) & 1);
-          scale = s.k_scale[e][key / TT_SCALE_SLOTS];
-          value = s.v_scale[e][key / TT_SCALE_SLOTS];
-          top_code = max(1, s.top_code[e]);
-          there = there && !(s.left_out[0][e] >> (key / TT_SCALE_SLOTS) & 1);
+          const float4 scale = *reinterpret_cast<const float4*>(s.k_scale[e] + 4 * half);
+          f[0] = not_zero(scale.x * factor);
+          f[1] = not_zero(scale.y * factor);
+          f[2] = not_zero(scale.z * factor);
+          f[3] = not_zero(scale.w * factor);
+          unit = s.unit[e];
+          lost = s.left_out[0][e] >> (4 * half);
           ++ct;
+        } else {
+          f[0] = f[1] = f[2] = f[3] = p.scale2;
         }
-        wait_for(&s.s_full[n & 3], (n >> 2) & 1);
+        wait_for(&s.s_full[n & 1], (n >> 1) & 1);
         tc_fence_after();
-        const uint32_t at = mine + (n & 3) * R;
-        const f32x2 scale2 = pair(scale, scale);
-        // The scores of this thread's key with the rows of chunk c, two to a number; times
-        // the key's scale and its row's factor and with its row's shift they are exponents of
-        // weights. (They are read again where they are needed again: the loops over chunks
-        // are rolled, as unrolled code of this size came from beyond the instruction caches.)
-        const float* const factors = cache ? s.factor[side] : s.own_factor;
-        const int factor_step = cache ? 4 : 0;
-        const uint32_t mask = there ? 0xff : 0;
-        const bool plain = cache && __all_sync(0xffffffffu, there);
-        auto scores = [&](int c, const uint32_t (&v)[8], f32x2 (&z)[4]) {
+        uint32_t v[2][32];
+        float high = -INFINITY;
+        if (some) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) z[i] = mul2(both(v, i), scale2);
-          if (plain) return;
-          const uint32_t seen =
-              cache ? mask
-                    : mask & tree_sees(s.seen[side][0], s.token[side] + 8 * c, (j * kTile + key) >> 5, lane);
+          for (int h = 0; h < 2; ++h) tmem_ld32(mine + (n & 1) * kTile + c0 + 32 * h, v[h]);
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float lo, hi;
-            split(z[i], lo, hi);
-            z[i] = pair(seen >> (2 * i) & 1 ? lo : -INFINITY, seen >> (2 * i + 1) & 1 ? hi : -INFINITY);
-          }
-        };
-        auto factor = [&](int c) { return reinterpret_cast<const f32x2*>(factors) + factor_step * c; };
-        auto shift = [&](int c) { return reinterpret_cast<const f32x2*>(my_shift + 8 * c); };
-        // New references, where a row's maximum is above its own by more than kSlack (or it
-        // has none), and what that makes of the output.
-        auto raise = [&] {
-#pragma unroll 1
-          for (int c = sub; c < chunks; c += kSubs) {
-            uint32_t v[8];
-            tmem_ld8(at + 8 * c, v);
-            tmem_wait8(v);
-            f32x2 z[4];
-            scores(c, v, z);
-            float top = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float lo, hi;
-              split(mul2(z[i], factor(c)[i]), lo, hi);
-              lo = warp_max(lo);
-              hi = warp_max(hi);
-              if (lane == 2 * i) top = lo;
-              if (lane == 2 * i + 1) top = hi;
+          for (int h = 0; h < 2; ++h) {
+            tmem_wait_ld(v[h]);
+            // which of 32 keys the row sees
+            if (!cache || keys < kTile || lost) {
+              const int left = keys - c0 - 32 * h;
+              uint32_t see = left >= 32 ? 0xffffffffu : (1u << max(0, left)) - 1;
+              if (lost >> (2 * h) & 1) see &= 0xffff0000u;
+              if (lost >> (2 * h) & 2) see &= 0xffffu;
+              if (!cache) see &= valid ? s.seen[local][(j * kTile + c0) / 32 + h] : 0u;
+              hide(v[h], see);
+              __syncwarp();
             }
-            if (lane < 8) s.part[set][quarter][8 * c + lane] = top;
-          }
-          sync_of(barrier, 128);
-          // (a thread to each of these warps' rows, as far as there are so many)
-          bool none = false;
-          const int row = 8 * (sub + kSubs * (key / 8)) + key % 8;
-          if (row < it.rows) {
-            const auto& part = s.part[set];
-            const float top = fmaxf(fmaxf(part[0][row], part[1][row]), fmaxf(part[2][row], part[3][row]));
-            const float old = first ? -INFINITY : s.ref[set][row];
-            const float to = top - old > kSlack || old == -INFINITY ? fmaxf(old, top) : old;
-            s.ref[set][row] = to;
-            my_shift[row] = (to == -INFINITY ? 0.f : -to) + kOffset;
-            my_fall[row] = old == -INFINITY ? 0.f : ex2_approx(old - to);
-            none = to == -INFINITY;
-          } else if (row < R) {  // (rows that a chunk has too many)
-            my_shift[row] = -INFINITY;
-            my_fall[row] = 0.f;
-          }
-          unset = any_of(barrier, 128, none);
-        };
-        // What the values' scale makes of weights is in units of the largest scale so far;
-        // when that rises the output falls.
-        float output_fall = 1.f;
-        if (top_code > code) {
-          output_fall = code > 0 ? e8m0(code) * e8m0_inverse(top_code) : 0.f;
-          code = top_code;
-        }
-        value *= e8m0_inverse(code);
-        const f32x2 value2 = pair(value, value);
-        const bool early = unset;
-        // (the product of two tiles ago is done with the weights' place)
-        wait_for(&s.o_done[set], ((n >> 1) & 1) ^ 1);
-        // 0: references, then weights; 1: weights. One that is too large, seldom: 2, new
-        // references, weights again. (The sums were added to in 32 bits, which hold them, or
-        // the old ones are nothing to the new.)
-        int pass = early ? 0 : 1;
-#pragma unroll 1
-        do {
-          if (pass != 1) raise();
-          if (pass < 2) {
-            float over = -INFINITY;
-            auto fetch = [&](int c, uint32_t (&v)[8], uint32_t (&l)[8]) {
-              tmem_ld8(at + 8 * c, v);
-              tmem_ld8(my_sums + 8 * c, l);
-            };
-            auto weigh = [&](int c, const uint32_t (&v)[8], uint32_t (&l)[8]) {
-              f32x2 z[4];
-              scores(c, v, z);
-              uint32_t out[4];
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const f32x2 y = fma2(z[i], factor(c)[i], shift(c)[i]);
+            for (int g = 0; g < 2; ++g) {
+              float top = __uint_as_float(v[h][16 * g]);
+#pragma unroll
+              for (int i = 1; i < 15; i += 2)
+                top = max3(top, __uint_as_float(v[h][16 * g + i]), __uint_as_float(v[h][16 * g + i + 1]));
+              top = fmaxf(top, __uint_as_float(v[h][16 * g + 15]));
+              high = fmaxf(high, top * f[2 * h + g]);
+            }
+          }
+        }
+        tc_fence_before();
+        if (ok) mbar_arrive(&s.s_free[n & 1]);
+        // (all ancestors are read)
+        if (j + 1 == min(it.n_tree, it.tile1) && ok) mbar_arrive(&s.seen_free);
+        // what the values' scale makes of the sums, and a larger maximum of the row's
+        float fall = 1.f;
+        if (unit > code) {
+          if (code > 0) fall = e8m0(code) * e8m0_inverse(unit);
+          code = unit;
+        }
+        bool falls = fall != 1.f;
+        if (some) {
+          high = fmaxf(high, other(high, n & 1));
+          if (high - m > kSlack || (m == -INFINITY && high > -INFINITY)) {
+            const float to = fmaxf(m, high), less = m == -INFINITY ? 0.f : ex2_approx(m - to);
+            m = to;
+            l *= less;
+            fall *= less;
+          }
+          falls = __any_sync(0xffffffffu, fall != 1.f);
+          const float shift = (m == -INFINITY ? 0.f : -m) + kOffset;
+          const f32x2 shift2 = pair(shift, shift);
+          f32x2 sum2 = 0;
+          auto weigh = [&](auto own) {
+            const float value = e8m0_inverse(code);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const float g = f[2 * h + i / 8];
+                const f32x2 y = exp2_pair(
+                    fma2(pair(__uint_as_float(v[h][2 * i]), __uint_as_float(v[h][2 * i + 1])), pair(g, g),
+                         shift2));
+                sum2 = add2(sum2, y);
                 float lo, hi;
                 split(y, lo, hi);
-                over = max3(over, lo, hi);
-                f32x2 e = exp2_pair(y), sum = both(l, i);
-                if (early) sum = mul2(sum, reinterpret_cast<const f32x2*>(my_fall + 8 * c)[i]);
-                sum = add2(sum, e);
-                split(sum, lo, hi);
-                l[2 * i] = __float_as_uint(lo);
-                l[2 * i + 1] = __float_as_uint(hi);
-                split(mul2(e, value2), lo, hi);
-                out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
-              }
-              tmem_st8(my_sums + 8 * c, l);
-              *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
-                  make_uint4(out[0], out[1], out[2], out[3]);
-            };
-            if constexpr (kSubs == 1) {
-              // (a chunk is fetched while the one before it is weighed)
-              uint32_t v0[8], l0[8], v1[8], l1[8];
-              fetch(0, v0, l0);
-#pragma unroll 1
-              for (int c = 0; c < chunks; c += 2) {
-                tmem_wait8(v0);
-                tmem_wait8(l0);
-                if (c + 1 < chunks) fetch(c + 1, v1, l1);
-                weigh(c, v0, l0);
-                if (c + 1 >= chunks) break;
-                tmem_wait8(v1);
-                tmem_wait8(l1);
-                if (c + 2 < chunks) fetch(c + 2, v0, l0);
-                weigh(c + 1, v1, l1);
-              }
-            } else {
-#pragma unroll 1
-              for (int c = sub; c < chunks; c += kSubs) {
-                uint32_t v[8], l[8];
-                fetch(c, v, l);
-                tmem_wait8(v);
-                tmem_wait8(l);
-                weigh(c, v, l);
+                if constexpr (decltype(own)::value)
+                  v[h][i] = pack_pair<DT>(lo * value, hi * value);
+                else
+                  v[h][i] = pack_pair<TT_F16>(lo, hi);
               }
             }
-            pass = !early && any_of(barrier, 128, over > kSlack + kOffset) ? 2 : 3;
-          } else {
+          };
+          if (cache)
+            weigh(std::false_type());
+          else
+            weigh(std::true_type());
+          l += sum_pair(sum2);
+        }
+        // (the product of two tiles ago is done with the weights' place)
+        wait_for(&s.o_done[n & 1], ((n >> 1) & 1) ^ 1);
+        tc_fence_after();
+        if (some) {
+          const uint32_t to = mine + S::kWeights + (n & 1) * (kTile / 2) + 32 * half;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) tmem_st16(to + 16 * h, v[h]);
+          if (falls && !first) {
+            wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
+            tc_fence_after();
 #pragma unroll 1
-            for (int c = sub; c < chunks; c += kSubs) {
-              f32x2 z[4];
-              uint32_t v[8], l[8];
-              tmem_wait_st();
-              tmem_ld8(at + 8 * c, v);
-              tmem_ld8(my_sums + 8 * c, l);
-              tmem_wait8(v);
-              tmem_wait8(l);
-              scores(c, v, z);
-              uint32_t out[4];
+            for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+              uint32_t o[32];
+              tmem_ld32(mine + S::kOut + c, o);
+              tmem_wait_ld(o);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                float e[2], lo, hi;
-                split(exp2_pair(fma2(z[i], factor(c)[i], shift(c)[i])), e[0], e[1]);
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  const float fall = my_fall[8 * c + 2 * i + k];
-                  l[2 * i + k] = __float_as_uint(
-                      fall > 0x1p-60f ? __uint_as_float(l[2 * i + k]) * fall : e[k]);
-                }
-                split(mul2(pair(e[0], e[1]), value2), lo, hi);
-                out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);
-              }
-              tmem_st8(my_sums + 8 * c, l);
-              *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
-                  make_uint4(out[0], out[1], out[2], out[3]);
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * fall);
+              tmem_st32(mine + S::kOut + c, o);
             }
-            pass = 4;
           }
-        } while (pass < 3);
-        const bool raised = pass == 4;
+          tmem_wait_st();
+        }
         tc_fence_before();
-        if (ok) mbar_arrive(&s.s_free[n & 3]);
-        if ((raised || early || output_fall != 1.f) && !first) {
-          // (its last product is done: that of two tiles ago, for which this warp has waited)
-          tc_fence_after();
-#pragma unroll 1
-          for (int c = sub; c < chunks; c += kSubs) {
-            uint32_t v[8];
-            tmem_ld8(output + 8 * c, v);
-            tmem_wait8(v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              v[i] = __float_as_uint(__uint_as_float(v[i]) * output_fall *
-                                     (raised || early ? my_fall[8 * c + i] : 1.f));
-            tmem_st8(output + 8 * c, v);
-          }
-        }
-        tmem_wait_st();
-        fence_proxy_async();
-        tc_fence_before();
-        if (ok) mbar_arrive(&s.p_full[set]);
+        if (ok) mbar_arrive(&s.p_full[n & 1]);
       }
-      // the sums of all keys
-      if (code) {
-#pragma unroll 1
-        for (int c = sub; c < chunks; c += kSubs) {
-          uint32_t l[8];
-          tmem_ld8(my_sums + 8 * c, l);
-          tmem_wait8(l);
-          float sums[8];
-#pragma unroll
-          for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
-          const float sum = warp_sums(sums, lane);
-          if (c == sub) sync_of(barrier, 128);  // (done with s.part)
-          if (lane < 8) s.part[set][quarter][8 * c + lane] = sum;
-        }
-      }
-      if (sub == 0 && quarter == 0 && lane == 0) s.code[set] = code;
-      sync_of(5, kRowThreads);
-      if (t < it.rows) {
-        // the sets' sums and outputs relative to the larger of their references
-        float top = -INFINITY, all = 0.f, f[kSets];
-#pragma unroll
-        for (int k = 0; k < kSets; ++k)
-          if (s.code[k]) top = fmaxf(top, s.ref[k][t]);
-#pragma unroll
-        for (int k = 0; k < kSets; ++k) {
-          f[k] = 0.f;
-          if (s.code[k]) {
-            const float ref = s.ref[k][t];
-            const float l = s.part[k][0][t] + s.part[k][1][t] + (s.part[k][2][t] + s.part[k][3][t]);
-            f[k] = ref == -INFINITY ? (l != l ? 1.f : 0.f) : ex2_approx(ref - top);
-            all = fmaf(l, f[k], all);
-          }
-        }
-        const float m2 = top == -INFINITY ? -INFINITY : top - kOffset;
-        const float inverse = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
-#pragma unroll
-        for (int k = 0; k < kSets; ++k)
-          s.share_of[k][t] = f[k] * inverse * (s.code[k] ? e8m0(s.code[k]) : 0.f);
-        const int64_t to = s.row_to[side][t];
-        if (ok && !whole)
-          p.part_ml[to] = make_float2(m2, all);
-        else if (ok && a.lse)
-          a.lse[to] = all > 0.f || all != all ? fmaf(m2, kLn2, logf(all)) : -INFINITY;
-      }
-      const bool used[kSets] = {s.code[0] != 0, s.code[1] != 0};
       bool odd = false;
       if (it.tile0 < it.n_tree) odd = lane < kWords && s.odd[side][lane];
       odd = __any_sync(0xffffffffu, odd);
-      sync_of(5, kRowThreads);
       wait_for(&s.o_done[(n - 1) & 1], ((n - 1) >> 1) & 1);
-      if (n > 1) wait_for(&s.o_done[n & 1], ((n - 2) >> 1) & 1);
       tc_fence_after();
-      if (D == 128 || quarter < 2) {
+      if (some) {
+        l += other(l, n & 1);
+        const bool whole = it.tile0 == 0 && it.tile1 == it.n_tree + cache_tiles(it.len);
+        // where the row goes: to the output, or to its place in the CTA's piece
+        const int64_t to = whole ? (int64_t(it.first) + token) * a.Hq + it.hk * p.group + it.row0 + row -
+                                       token * p.group
+                                 : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * kRows + row;
+        const float unit = e8m0(code);
+        const float by = whole ? (l > 0.f || l != l ? unit / l : 0.f) : unit;
 #pragma unroll 1
-        for (int c = four; c < chunks; c += kSets * kSubs) {
-          float y[8] = {};
+        for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
+          uint32_t v[32];
+          tmem_ld32(mine + S::kOut + c, v);
+          tmem_wait_ld(v);
+          if (valid && ok) {
 #pragma unroll
-          for (int k = 0; k < kSets; ++k) {
-            if (!used[k]) continue;
-            uint32_t v[8];
-            tmem_ld8(mine + S::kOut + k * R + 8 * c, v);
-            tmem_wait8(v);
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * by);
+            if (odd) {
+              float more[32];
+              odd_values<DT>(a, s.odd[side], it.first, token, it.hk, c, more);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-              y[i] = fmaf(__uint_as_float(v[i]), s.share_of[k][8 * c + i], y[i]);
-          }
+              for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + more[i]);
+            }
+            if (whole) {
+              char* out = a.out + (to * D + c) * 2;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int r = 8 * c + i;
-            if (r < it.rows && ok) {
-              if (odd)
-                y[i] += odd_values<DT>(a, s.odd[side], s.seen[side][s.token[side][r]], it.end, it.first,
-                                       it.hk, key);
-              const int64_t to = s.row_to[side][r] * D + key;
-              if (whole)
-                store_elem<DT>(a.out + to * 2, y[i]);
-              else
-                p.part[to] = y[i];
+              for (int i = 0; i < 2; ++i) {
+                uint32_t o[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q)
+                  o[q] = pack_pair<DT>(__uint_as_float(v[16 * i + 2 * q]),
+                                       __uint_as_float(v[16 * i + 2 * q + 1]));
+                store_sector<true>(out + 32 * i, o);
+              }
+            } else {
+              char* out = reinterpret_cast<char*>(p.part + to * D + c);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t o[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) o[q] = v[8 * i + q];
+                store_sector<false>(out + 32 * i, o);
+              }
             }
           }
+          __syncwarp();
+        }
+        if (valid && ok && half == 0) {
+          const float m2 = m == -INFINITY ? -INFINITY : m - kOffset;
+          if (!whole)
+            p.part_ml[to] = make_float2(m2, l);
+          else if (a.lse)
+            a.lse[to] = l > 0.f || l != l ? fmaf(m2, kLn2, logf(l)) : -INFINITY;
         }
       }
       tc_fence_before();
@@ -1291,7 +1125,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_kernel(const __gr
 // requests that lost places to a CTA that gave up.
 constexpr int kJoinWarps = 4, kFewPieces = 16;
 
-template <int D, int R, bool F16, bool FEW>
+template <int D, bool F16, bool FEW>
 __global__ void __launch_bounds__(kJoinWarps * 32)
     tree8_join_kernel(const __grid_constant__ Tree8Args p) {
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
@@ -1310,7 +1144,7 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   const int share = p.first[a.B], first = p.first[b];
   const Request r = request(a, b);
   if (i >= r.nodes) return;
-  const int per_head = head_places<R>(r, p.group);
+  const int per_head = head_places(r, p.group);
   // (one warp of the request)
   if (i == 0 && h == 0 && (FEW || threadIdx.x < 32)) {
     const int end = first + per_head * a.Hkv - 1;  // its last place
@@ -1318,14 +1152,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
     for (int c = first / share + lane; c <= end / share; c += 32) stop = min(stop, p.stop[c]);
     if (__any_sync(0xffffffffu, stop <= end) && lane == 0) a.status[b] |= TT_REQ_TIMEOUT;
   }
-  const int row = i * p.group + h % p.group, mt = row / R;
+  const int row = i * p.group + h % p.group, mt = row / kRows;
   int before = hk * per_head + kItemCost;  // its first tile's place
-  for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles<R>(r, p.group, k);
-  const int last = before + item_tiles<R>(r, p.group, mt) - 1;
+  for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles(r, p.group, k);
+  const int last = before + item_tiles(r, p.group, mt) - 1;
   // the CTAs that the item lies in
   const int c0 = (first + before) / share, pieces = (first + last) / share - c0 + 1;
   if (pieces < 2) return;
-  auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * R + row % R; };
+  auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * kRows + row % kRows; };
   float M = -INFINITY, l = 0.f, acc[N];
 #pragma unroll
   for (int c = 0; c < N; ++c) acc[c] = 0.f;
@@ -1391,7 +1225,6 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
 
 // How a call is cut: CTAs, and the workspace.
 struct Cut8 {
-  int rows;        // R
   int ctas;
   int64_t places;  // in the list, were all lengths the longest
   int64_t pieces;  // of one item, about
@@ -1401,8 +1234,7 @@ Cut8 cut8(const TreeArgs& a, int sm_count) {
   Cut8 c;
   const int group = a.Hq / a.Hkv;
   const int64_t rows = int64_t(a.max_nodes) * group;
-  c.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-  const int64_t row_tiles = (rows + c.rows - 1) / c.rows;
+  const int64_t row_tiles = (rows + kRows - 1) / kRows;
   const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
   const int64_t all = c.places = int64_t(std::min(
       1e18, double(a.B) * double(a.Hkv) * double(row_tiles) * double(kItemCost + tiles)));
@@ -1411,7 +1243,7 @@ Cut8 cut8(const TreeArgs& a, int sm_count) {
   // (were all lengths the longest; fewer tiles make shares smaller and pieces more)
   const int64_t share = std::max<int64_t>(kMinShare, (all + c.ctas - 1) / c.ctas);
   c.pieces = tiles / share + 2;
-  const size_t held = 2 * size_t(c.ctas) * c.rows;
+  const size_t held = 2 * size_t(c.ctas) * kRows;
   c.part_bytes = align256(held * a.D * sizeof(float));
   c.ml_bytes = align256(held * sizeof(float2));
   c.first_bytes = align256((size_t(a.B) + 1) * sizeof(int32_t));
@@ -1455,15 +1287,15 @@ bool encode(CUtensorMap* map, const TreeArgs& a, const char* data, int64_t page,
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, int R, bool F16>
+template <int D, bool F16>
 cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(Warps<R>::kThreads);
-  cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
+  cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = sizeof(Smem8<D, F16>) + 1024;
   cfg.stream = stream;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, R, F16>, p);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, F16>, p);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1475,28 +1307,20 @@ cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   cfg.dynamicSmemBytes = 0;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return few ? cudaLaunchKernelEx(&cfg, tree8_join_kernel<D, R, F16, true>, p)
-             : cudaLaunchKernelEx(&cfg, tree8_join_kernel<D, R, F16, false>, p);
+  return few ? cudaLaunchKernelEx(&cfg, tree8_join_kernel<D, F16, true>, p)
+             : cudaLaunchKernelEx(&cfg, tree8_join_kernel<D, F16, false>, p);
 }
 
-template <int D, int R, bool F16>
+template <int D, bool F16>
 cudaError_t preload() {
   cudaFuncAttributes fa;
-  cudaError_t e = cudaFuncGetAttributes(&fa, tree8_join_kernel<D, R, F16, true>);
-  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree8_join_kernel<D, R, F16, false>);
+  cudaError_t e = cudaFuncGetAttributes(&fa, tree8_join_kernel<D, F16, true>);
+  if (e == cudaSuccess) e = cudaFuncGetAttributes(&fa, tree8_join_kernel<D, F16, false>);
   if (e != cudaSuccess) return e;
-  static_assert(sizeof(Smem8<D, R, F16>) + 1024 <= 227 * 1024, "shared memory of a CTA");
-  return cudaFuncSetAttribute(tree8_kernel<D, R, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              int(sizeof(Smem8<D, R, F16>)) + 1024);
+  static_assert(sizeof(Smem8<D, F16>) + 1024 <= 227 * 1024, "shared memory of a CTA");
+  return cudaFuncSetAttribute(tree8_kernel<D, F16>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              int(sizeof(Smem8<D, F16>)) + 1024);
 }
-template <int D, bool F16>
-cudaError_t preload_all() {
-  cudaError_t e = preload<D, 16, F16>();
-  if (e == cudaSuccess) e = preload<D, 32, F16>();
-  if (e == cudaSuccess) e = preload<D, 64, F16>();
-  return e;
-}
-
 }  // namespace
 
 size_t tree8_workspace_bytes(const TreeArgs& a, int sm_count) { return cut8(a, sm_count).bytes; }
@@ -1535,19 +1359,17 @@ cudaError_t launch_tree8(const TreeArgs& a, const TreeScales& sc, int dt, cudaSt
   auto go = [&](auto dim, auto f16) {
     constexpr int D = decltype(dim)::value;
     constexpr bool F16 = decltype(f16)::value;
-    return c.rows == 16   ? launch<D, 16, F16>(p, c.pieces, stream)
-           : c.rows == 32 ? launch<D, 32, F16>(p, c.pieces, stream)
-                          : launch<D, 64, F16>(p, c.pieces, stream);
+    return launch<D, F16>(p, c.pieces, stream);
   };
   auto of = [&](auto dim) { return dt == TT_F16 ? go(dim, std::true_type()) : go(dim, std::false_type()); };
   return a.D == 128 ? of(std::integral_constant<int, 128>()) : of(std::integral_constant<int, 64>());
 }
 
 cudaError_t preload_tree8() {
-  cudaError_t e = preload_all<128, true>();
-  if (e == cudaSuccess) e = preload_all<128, false>();
-  if (e == cudaSuccess) e = preload_all<64, true>();
-  if (e == cudaSuccess) e = preload_all<64, false>();
+  cudaError_t e = preload<128, true>();
+  if (e == cudaSuccess) e = preload<128, false>();
+  if (e == cudaSuccess) e = preload<64, true>();
+  if (e == cudaSuccess) e = preload<64, false>();
   return e;
 }
 
