@@ -18,10 +18,10 @@ LIB = os.path.join(PKG, "libtt.so")
 SOURCES = ["api.cu", "align.cu", "rowpass.cu", "decide.cu", "noalloc.cu", "encode.cu", "shard.cu",
            "filter.cu", "nucleus.cu", "nucrow.cu", "pen.cu", "ops.cu", "logprob.cu",
            "distill.cu", "tree.cu", "rope.cu", "append.cu",
-           "tree8.cu"]
+           "tree8.cu", "tree8_few.cu"]
 HEADERS = ["tt_device.cuh", "tt_launch.h", "tt_shard.h", "tt_f2.cuh",
            "tt_ring.cuh", "tt_ops.h", "tt_umma.cuh", "tt_x2.cuh",
-           "tt_rope.cuh", "tt_e4m3.cuh"]
+           "tt_rope.cuh", "tt_e4m3.cuh", "tt_tree8.cuh"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -24,197 +24,31 @@
 // which the CTAs share evenly: lengths are known on the device alone. Items cut by a CTA's
 // end leave unnormalised pieces, which a second kernel joins.
 //
-// Built and taken back: keys as the rows of the products and tokens as their columns, so
-// that they cost what the columns cost. A thread then has a key, and a row's factor,
-// maximum and sum come from shared memory or go across threads: 12 instructions a score
-// for 4 here, and a serving batch took 199 us.
+// Requests of few rows go to tree8_few.cu, whose products have them as columns; how both
+// compare stands at the rule that chooses.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 
 #include <algorithm>
 #include <atomic>
-#include <cstdint>
 #include <cstring>
 #include <numeric>
 #include <type_traits>
 
-#include "tt_device.cuh"
-#include "tt_e4m3.cuh"
-#include "tt_f2.cuh"
-#include "tt_ops.h"
-#include "tt_ring.cuh"
-#include "tt_rope.cuh"
-#include "tt_umma.cuh"
-#include "tt_x2.cuh"
+#include "tt_tree8.cuh"
 
 namespace tt {
 
 namespace {
 
-constexpr int kTile = 128;                     // keys of a tile
-constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
-constexpr int kRows = 128;                     // of an item
+constexpr int kRows = kManyRows;
 constexpr int kRowWarps = 8, kRowThreads = kRowWarps * 32;  // two for each 32 rows
 constexpr int kThreads = kRowThreads + kConvThreads + 128;
-constexpr int kWords = TT_MAX_TREE / 32;
-constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
-constexpr int kScaleRing = 16;                   // tiles' scales that are kept
-constexpr int kBatch = 4;                        // tiles whose pages are asked for together
-constexpr float kLn2 = 0.693147180559945f;
-// A row's reference maximum follows its maximum once that is 2^kSlack above it:
-// weights stay below 2^(kSlack + offset), and the output is scaled rarely.
-constexpr float kSlack = 8.f;
-constexpr int kMinShare = 2;  // places of a CTA, where there are few
-// What an item costs beyond its tiles (queries, ancestors, output), in tiles: it
-// takes as many places in the list before its first tile.
-constexpr int kItemCost = 2;
 
-// mbar_wait in few instructions: the roles wait in some thirty places, and what they
-// do in between has to stay in the instruction caches.
-__device__ __forceinline__ bool wait8(uint64_t* bar, uint32_t parity, const uint64_t& limit_ns) {
-  if (mbar_try_wait(bar, parity)) return true;
-  const uint64_t t0 = global_ns();
-#pragma unroll 1
-  do {
-    if (mbar_try_wait(bar, parity)) return true;
-  } while (global_ns() - t0 <= limit_ns);
-  return false;
-}
-
-struct Tree8Args {
-  CUtensorMap kc, vc;
-  TreeArgs a;
-  TreeScales sc;
-  float scale2;       // scale * log2(e)
-  int group;          // G
-  int ctas;           // of the launch
-  int box;            // slots of one copy: they lie within a page
-  int slots_inner;    // the cache maps' second dimension is the slot, the third the head
-  // pieces: CTA c leaves that of an item that began before its tiles at 2 c, that
-  // of one that begins in them at 2 c + 1
-  float* part;        // [2 ctas * kRows * D] outputs, not normalised
-  float2* part_ml;    // [2 ctas * kRows] their reference maximum (log2) and sum
-  int32_t* first;     // [B + 1] places before each request's, then the places per CTA
-  int32_t* stop;      // [ctas] the place from which a CTA gave up, INT32_MAX if it did not
-  uint64_t wait_ns;   // limit of a wait
-  int stall;          // the CTA whose copies a test withholds from its second tile on, or -1
-};
-
-// A request's usable range: its nodes and cache length, or why it has none.
-struct Request {
-  int first, nodes, len, status;
-};
-__device__ __forceinline__ Request request(const TreeArgs& a, int b) {
-  Request r{a.tree_off[b], 0, a.cache_len[b], 0};
-  const int end = a.tree_off[b + 1];
-  if (r.first < 0 || end < r.first || end > a.n_nodes) {
-    r.status = TT_REQ_BAD_OFFSETS;
-    return r;
-  }
-  r.nodes = end - r.first;
-  if (r.nodes > a.max_nodes || r.len < 0 || r.len > a.max_len) {
-    r.status = TT_REQ_TOO_LONG;
-    r.nodes = 0;
-  }
-  return r;
-}
-
-// Rows of a request and key head are (token, query head of the group), in order; an
-// item is R of them. The tiles that its rows see: the cache's, then those of drafted
-// tokens up to its last row's.
-__host__ __device__ inline int cache_tiles(int len) { return len / kTile + (len % kTile != 0); }
-__host__ __device__ inline int tree_tiles(int end) { return (end + kTile - 1) / kTile; }
-__host__ __device__ inline int items(int nodes, int group) {
-  return (nodes * group + kRows - 1) / kRows;
-}
-__device__ __forceinline__ int item_end(const Request& r, int group, int mt) {  // its last token + 1
-  return (min(r.nodes * group, (mt + 1) * kRows) - 1) / group + 1;
-}
-__device__ __forceinline__ int item_tiles(const Request& r, int group, int mt) {
-  return cache_tiles(r.len) + tree_tiles(item_end(r, group, mt));
-}
-// The places that one key head of a request takes in the list.
-__device__ __noinline__ int head_places(const Request r, int group) {
-  const int n = items(r.nodes, group);
-  int sum = n * (kItemCost + cache_tiles(r.len));
-#pragma unroll 1
-  for (int mt = 0; mt < n; ++mt) sum += tree_tiles(item_end(r, group, mt));
-  return sum;
-}
-// An item of the list, the first of its tiles that is left, and the places before it.
-// (Finding it and stepping on are calls: each role does it, and inlined in all of them
-// they made 180 KB of code, whose misses cost more than the work; with them and the
-// slow side of a wait apart it is TODO.)
-struct Place {
-  int b, hk, mt, tile, lead;
-  Request r;
-};
-__device__ __noinline__ Place find_place(const TreeArgs& a, int group, int request_b, int offset) {
-  Place x;
-  x.b = request_b;
-  x.r = request(a, request_b);
-  const int per_head = head_places(x.r, group);
-  x.hk = offset / per_head;
-  offset %= per_head;
-  x.mt = 0;
-#pragma unroll 1
-  for (int n; offset >= (n = kItemCost + item_tiles(x.r, group, x.mt)); ++x.mt) offset -= n;
-  x.tile = max(0, offset - kItemCost);
-  x.lead = max(0, kItemCost - offset);
-  return x;
-}
-__device__ __noinline__ Place next_place(const TreeArgs& a, int group, Place x) {
-  x.tile = 0;
-  x.lead = kItemCost;
-  if (++x.mt * kRows < x.r.nodes * group) return x;
-  x.mt = 0;
-  if (++x.hk < a.Hkv) return x;
-  x.hk = 0;
-#pragma unroll 1
-  do {
-    if (++x.b >= a.B) return x;
-    x.r = request(a, x.b);
-  } while (x.r.nodes == 0);
-  return x;
-}
-// The part of an item that a CTA takes: tiles of drafted tokens, which have to come from
-// further away, first, then the cache's.
-struct Item {
-  int n_tree, rows, tile0, tile1, end;
-  __device__ __forceinline__ Item(const Tree8Args& p, const Place& x, int todo) {
-    rows = min(kRows, x.r.nodes * p.group - x.mt * kRows);
-    end = item_end(x.r, p.group, x.mt);
-    n_tree = tree_tiles(end);
-    tile0 = x.tile;
-    tile1 = min(n_tree + cache_tiles(x.r.len), x.tile + todo);
-  }
-};
-// Keys in use of tile j of an item.
-__device__ __forceinline__ int tile_keys(int j, int n_tree, int end, int len) {
-  return min(kTile, j < n_tree ? end - j * kTile : len - (j - n_tree) * kTile);
-}
 // What the converting warps, which come to an item first, tell the others of it.
 struct Facts {
   int n_tree, rows, tile0, tile1, end, len, first, hk, row0, at;  // at: the place of its first tile
 };
-
-// Whether every parent and page of the request is in range (the row threads).
-__device__ __noinline__ bool out_of_range(const TreeArgs& a, int b, const Request r, int t, int threads) {
-  bool bad = false;
-  if (a.parents)
-#pragma unroll 1
-    for (int i = t; i < r.nodes; i += threads) {
-      const int p = a.parents[r.first + i];
-      bad |= p < -1 || p >= i;
-    }
-  const int pages = r.len / a.page_size + (r.len % a.page_size != 0);
-#pragma unroll 1
-  for (int x = t; x < pages; x += threads) {
-    const int p = a.page_table[b * a.table_stride + x];
-    bad |= p < 0 || p >= a.n_pages;
-  }
-  return bad;
-}
 
 template <int D, bool F16>
 struct Smem8 {
@@ -250,75 +84,6 @@ struct Smem8 {
   int end, stop;                      // the place behind this CTA's, and where it gave up
 };
 
-// D[tmem] (+)= A[smem] B[smem] over 32 of K, both e4m3.
-__device__ __forceinline__ void umma8_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "setp.ne.u32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(uint32_t(add))
-      : "memory");
-}
-// Operand of e4m3 elements in rows of D bytes along K, swizzled by as many.
-template <int D>
-__device__ __forceinline__ uint64_t umma8_desc(uint32_t addr) {
-  return uint64_t((addr & 0x3ffffu) >> 4) | uint64_t(1) << 16 | uint64_t(8 * D >> 4) << 32 | uint64_t(1) << 46 |
-         uint64_t(D == 128 ? 2 : 4) << 61;
-}
-// Byte `at` of row r of such an operand.
-template <int D>
-__device__ __forceinline__ int swizzled8(int r, int at) {
-  return r * D + (at ^ (D == 128 ? (r & 7) << 4 : (r >> 1 & 3) << 4));
-}
-// 16-byte unit u of row r in 128-byte swizzled rows.
-__device__ __forceinline__ int swizzled16(int r, int u) { return r * 128 + ((u ^ (r & 7)) << 4); }
-// Instruction descriptor: fp32 accumulators, M = 128, N columns, e4m3 operands.
-__device__ __forceinline__ uint32_t idesc_e4m3(int n) {
-  return 1u << 4 | uint32_t(n >> 3) << 17 | uint32_t(128 >> 4) << 24;
-}
-// Whether any of `threads` threads says so; all of them come to the barrier.
-__device__ __forceinline__ bool any_of(int barrier, int threads, bool x) {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 q, %3, 0;\n\t"
-      "bar.red.or.pred p, %1, %2, q;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r)
-      : "r"(barrier), "r"(threads), "r"(uint32_t(x))
-      : "memory");
-  return r != 0;
-}
-__device__ __forceinline__ void sync_of(int barrier, int threads) {
-  asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
-}
-// -inf in place of the scores whose bit is not set.
-__device__ __forceinline__ void hide(uint32_t (&v)[32], uint32_t see) {
-#pragma unroll
-  for (int i = 0; i < 32; ++i)
-    if (!(see >> i & 1)) v[i] = 0xff800000u;
-}
-// A product that may have become too small for a number, which -inf may be multiplied
-// by; NaN stays.
-__device__ __forceinline__ float not_zero(float x) {
-  float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(x), "f"(0x1p-120f));
-  return r;
-}
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
-  return r;
-}
-__device__ __forceinline__ bool elect_one() {
-  uint32_t r;
-  asm volatile(
-      "{\n\t.reg .pred p;\n\t"
-      "elect.sync _|p, 0xffffffff;\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(r));
-  return r != 0;
-}
 // What drafted tokens with a value that is not finite add to elements d .. d + 31 of token
 // i's row: it walks up from there.
 template <int DT>
@@ -375,6 +140,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
   extern __shared__ char raw[];
   S& s = *reinterpret_cast<S*>(raw + ((1024 - (smem_u32(raw) & 1023)) & 1023));
   const TreeArgs& a = p.a;
+  const Shape shape{p.group, kRows};
   // (a number that is the same in all lanes, and known to be)
   const int t = threadIdx.x, warp = __shfl_sync(0xffffffffu, t >> 5, 0), lane = t & 31;
   const uint64_t& limit = p.wait_ns;
@@ -412,64 +178,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
   if (warp == kRowWarps + kConvWarps) tmem_alloc(&s.tmem, S::kColumns);
   // The list: each thread adds up a run of requests, and the one whose run holds
   // this CTA's first place tells the request.
-  int todo;
-  {
-    const int each = (a.B + kThreads - 1) / kThreads, b0 = min(a.B, t * each),
-              b1 = min(a.B, b0 + each);
-    long long mine = 0;
-#pragma unroll 1
-    for (int b = b0; b < b1; ++b) mine += (long long)(head_places(request(a, b), p.group)) * a.Hkv;
-    long long upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long y = __shfl_up_sync(0xffffffffu, upto, o);
-      if (lane >= o) upto += y;
-    }
-    if (lane == 31) s.sums[warp] = upto;
-    tc_fence_before();
-    __syncthreads();
-    tc_fence_after();
-    long long all = 0;
-    for (int w = 0; w < kThreads / 32; ++w) {
-      if (w < warp) upto += s.sums[w];
-      all += s.sums[w];
-    }
-    const long long share = max((long long)(kMinShare), (all + p.ctas - 1) / p.ctas);
-    const long long from = share * blockIdx.x;
-    todo = int(max(0ll, min(share, all - from)));
-    if (t == 0) {
-      s.share = int(share);
-      s.end = int(min(all, from + share));
-    }
-    long long at = upto - mine;
-    if (todo > 0 && from >= at && from < upto) {
-#pragma unroll 1
-      for (int b = b0; b < b1; ++b) {
-        const long long n = (long long)(head_places(request(a, b), p.group)) * a.Hkv;
-        if (from < at + n) {
-          s.start_b = b;
-          s.start_offset = int(from - at);
-          break;
-        }
-        at += n;
-      }
-    }
-    if (blockIdx.x == 0) {  // for the join
-      at = upto - mine;
-#pragma unroll 1
-      for (int b = b0; b < b1; ++b) {
-        p.first[b] = int(at);
-        at += (long long)(head_places(request(a, b), p.group)) * a.Hkv;
-      }
-      if (t == 0) p.first[a.B] = int(share);
-    }
-  }
+  int todo = begin_list<kThreads>(p, shape, s, t, warp, lane);
   __syncthreads();
   const uint32_t tmem = s.tmem;
   bool ok = true;
   Place x;
   x.lead = 0;
-  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, p.group, s.start_b, s.start_offset);
+  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, shape, s.start_b, s.start_offset);
 
   if (warp > kRowWarps + kConvWarps + 1) {
     // ------------------------------------------------------------ copies
@@ -497,7 +212,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         if (!open) {
           if (todo <= x.lead) return y;
           todo -= x.lead;
-          const Item it(p, x, todo);
+          const Item it(shape, x, todo);
           j = max(0, it.tile0 - it.n_tree);
           j1 = it.tile1 - it.n_tree;
           used = it.tile1 - it.tile0;
@@ -506,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         }
         if (j < j1) break;
         todo -= used;
-        x = next_place(p.a, p.group, x);
+        x = next_place(p.a, shape, x);
         open = false;
       }
       y.tiles = min(kBatch, j1 - j);
@@ -596,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
 #pragma unroll 1
       for (int seg = 0; todo > x.lead && ok; ++seg) {
         todo -= x.lead;
-        const Item it(p, x, todo);
+        const Item it(shape, x, todo);
         ok = on(&s.q_full, seg & 1);
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
@@ -642,14 +357,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           __syncwarp();
         }
         todo -= it.tile1 - it.tile0;
-        x = next_place(p.a, p.group, x);
+        x = next_place(p.a, shape, x);
       }
     } else {
       const uint64_t wv = umma_desc(smem_u32(s.w), kBlock);
 #pragma unroll 1
       for (int seg = 0; todo > x.lead && ok; ++seg) {
         todo -= x.lead;
-        const Item it(p, x, todo);
+        const Item it(shape, x, todo);
 #pragma unroll 1
         for (int j = it.tile0; j < it.tile1 && ok; ++j, ++n, ++w) {
           if (j < it.n_tree) ++w;
@@ -673,7 +388,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           __syncwarp();
         }
         todo -= it.tile1 - it.tile0;
-        x = next_place(p.a, p.group, x);
+        x = next_place(p.a, shape, x);
       }
     }
     // (and until their last products and the arrivals for them are done)
@@ -693,7 +408,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
 #pragma unroll 1
     for (; todo > x.lead && ok; ++seg) {
       todo -= x.lead;
-      const Item it(p, x, todo);
+      const Item it(shape, x, todo);
       const int side = seg & 1, row0 = x.mt * kRows, token0 = row0 / p.group;
       // (the item before the last one is over)
       if (!wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1)) break;
@@ -875,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         ++w;
       }
       todo -= it.tile1 - it.tile0;
-      x = next_place(p.a, p.group, x);
+      x = next_place(p.a, shape, x);
     }
     // (no more)
     if (ok && wait_for(&s.o_free[seg & 1], ((seg >> 1) & 1) ^ 1)) {
@@ -1144,7 +859,8 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   const int share = p.first[a.B], first = p.first[b];
   const Request r = request(a, b);
   if (i >= r.nodes) return;
-  const int per_head = head_places(r, p.group);
+  const Shape shape{p.group, p.rows};
+  const int per_head = head_places(r, shape);
   // (one warp of the request)
   if (i == 0 && h == 0 && (FEW || threadIdx.x < 32)) {
     const int end = first + per_head * a.Hkv - 1;  // its last place
@@ -1152,14 +868,14 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
     for (int c = first / share + lane; c <= end / share; c += 32) stop = min(stop, p.stop[c]);
     if (__any_sync(0xffffffffu, stop <= end) && lane == 0) a.status[b] |= TT_REQ_TIMEOUT;
   }
-  const int row = i * p.group + h % p.group, mt = row / kRows;
+  const int row = i * p.group + h % p.group, mt = row / p.rows;
   int before = hk * per_head + kItemCost;  // its first tile's place
-  for (int k = 0; k < mt; ++k) before += kItemCost + item_tiles(r, p.group, k);
-  const int last = before + item_tiles(r, p.group, mt) - 1;
+  for (int k = 0; k < mt; ++k) before += kItemCost + shape.tiles(r, k);
+  const int last = before + shape.tiles(r, mt) - 1;
   // the CTAs that the item lies in
   const int c0 = (first + before) / share, pieces = (first + last) / share - c0 + 1;
   if (pieces < 2) return;
-  auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * kRows + row % kRows; };
+  auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * p.rows + row % p.rows; };
   float M = -INFINITY, l = 0.f, acc[N];
 #pragma unroll
   for (int c = 0; c < N; ++c) acc[c] = 0.f;
@@ -1225,16 +941,24 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
 
 // How a call is cut: CTAs, and the workspace.
 struct Cut8 {
+  int rows;        // of an item
   int ctas;
   int64_t places;  // in the list, were all lengths the longest
   int64_t pieces;  // of one item, about
   size_t part_bytes, ml_bytes, first_bytes, bytes;
 };
-Cut8 cut8(const TreeArgs& a, int sm_count) {
+Cut8 cut8(const TreeArgs& a, int dt, int sm_count) {
   Cut8 c;
   const int group = a.Hq / a.Hkv;
   const int64_t rows = int64_t(a.max_nodes) * group;
-  const int64_t row_tiles = (rows + kRows - 1) / kRows;
+  // Few rows go to the kernel whose products have them as columns, which costs what they
+  // cost: 64 caches of 8192 and 8 heads took, with that one and with this,
+  //   heads of 128, bf16:  158 and 211 us at 16 rows, 191 and 231 at 32, 237 and 252 at 48,
+  //                        259 and 256 at 64 (fp16: 245 and 243 at 40);
+  //   heads of 64:         137 and 163 us at 16, 174 and 174 at 32, 215 and 181 at 48.
+  const bool bf16_128 = a.D == 128 && dt == TT_BF16;
+  c.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 && bf16_128 ? 64 : kManyRows;
+  const int64_t row_tiles = (rows + c.rows - 1) / c.rows;
   const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
   const int64_t all = c.places = int64_t(std::min(
       1e18, double(a.B) * double(a.Hkv) * double(row_tiles) * double(kItemCost + tiles)));
@@ -1243,7 +967,7 @@ Cut8 cut8(const TreeArgs& a, int sm_count) {
   // (were all lengths the longest; fewer tiles make shares smaller and pieces more)
   const int64_t share = std::max<int64_t>(kMinShare, (all + c.ctas - 1) / c.ctas);
   c.pieces = tiles / share + 2;
-  const size_t held = 2 * size_t(c.ctas) * kRows;
+  const size_t held = 2 * size_t(c.ctas) * c.rows;
   c.part_bytes = align256(held * a.D * sizeof(float));
   c.ml_bytes = align256(held * sizeof(float2));
   c.first_bytes = align256((size_t(a.B) + 1) * sizeof(int32_t));
@@ -1291,11 +1015,16 @@ template <int D, bool F16>
 cudaError_t launch(const Tree8Args& p, int64_t pieces, cudaStream_t stream) {
   const TreeArgs& a = p.a;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = sizeof(Smem8<D, F16>) + 1024;
   cfg.stream = stream;
-  cudaError_t e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, F16>, p);
+  cudaError_t e;
+  if (p.rows < kManyRows) {
+    e = launch_tree8_few(p, F16 ? TT_F16 : TT_BF16, stream);
+  } else {
+    cfg.gridDim = dim3(unsigned(p.ctas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(Smem8<D, F16>) + 1024;
+    e = cudaLaunchKernelEx(&cfg, tree8_kernel<D, F16>, p);
+  }
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -1323,23 +1052,26 @@ cudaError_t preload() {
 }
 }  // namespace
 
-size_t tree8_workspace_bytes(const TreeArgs& a, int sm_count) { return cut8(a, sm_count).bytes; }
+size_t tree8_workspace_bytes(const TreeArgs& a, int dt, int sm_count) {
+  return cut8(a, dt, sm_count).bytes;
+}
 
 // (places of the list, and blocks of the join, are 32-bit numbers)
-bool tree8_fits(const TreeArgs& a, int sm_count) {
-  return cut8(a, sm_count).places <= INT32_MAX &&
+bool tree8_fits(const TreeArgs& a, int dt, int sm_count) {
+  return cut8(a, dt, sm_count).places <= INT32_MAX &&
          double(a.B) * a.max_nodes * double(a.Hq) <= INT32_MAX;
 }
 
 cudaError_t launch_tree8(const TreeArgs& a, const TreeScales& sc, int dt, cudaStream_t stream,
                          int sm_count) {
-  const Cut8 c = cut8(a, sm_count);
+  const Cut8 c = cut8(a, dt, sm_count);
   Tree8Args p;
   std::memset(&p, 0, sizeof p);
   p.a = a;
   p.sc = sc;
   p.scale2 = float(double(a.scale) * 1.4426950408889634);
   p.group = a.Hq / a.Hkv;
+  p.rows = c.rows;
   p.ctas = c.ctas;
   p.box = std::gcd(a.page_size, kTile);
   p.part = reinterpret_cast<float*>(a.ws);
@@ -1366,7 +1098,8 @@ cudaError_t launch_tree8(const TreeArgs& a, const TreeScales& sc, int dt, cudaSt
 }
 
 cudaError_t preload_tree8() {
-  cudaError_t e = preload<128, true>();
+  cudaError_t e = preload_tree8_few();
+  if (e == cudaSuccess) e = preload<128, true>();
   if (e == cudaSuccess) e = preload<128, false>();
   if (e == cudaSuccess) e = preload<64, true>();
   if (e == cudaSuccess) e = preload<64, false>();

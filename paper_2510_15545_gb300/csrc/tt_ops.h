@@ -1,8 +1,8 @@
 // tt_ops.h -- arguments and launchers of the operators around a verification
 // step: log probabilities of logits rows (logprob.cu), a student's loss against a
 // teacher's top log probabilities (distill.cu), attention of drafted tokens over a
-// paged cache (tree.cu; in 8 bits, tree8.cu), rotary positions (rope.cu), appending to
-// paged caches (append.cu).
+// paged cache (tree.cu; in 8 bits, tree8.cu and tree8_few.cu), rotary positions
+// (rope.cu), appending to paged caches (append.cu).
 #pragma once
 
 #include <cstdint>
@@ -136,8 +136,8 @@ struct TreeScales {
   TreeScale k, v;
 };
 
-size_t tree8_workspace_bytes(const TreeArgs& args, int sm_count);
-bool tree8_fits(const TreeArgs& args, int sm_count);
+size_t tree8_workspace_bytes(const TreeArgs& args, int dt, int sm_count);
+bool tree8_fits(const TreeArgs& args, int dt, int sm_count);
 cudaError_t launch_tree8(const TreeArgs& args, const TreeScales& scales, int dt,
                          cudaStream_t stream, int sm_count);
 cudaError_t preload_tree8();
