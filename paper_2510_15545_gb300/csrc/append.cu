@@ -190,7 +190,16 @@ __global__ void __launch_bounds__(kThreads, 2)
     };
     // (the first head's keys are on their way while the sines are formed)
     Raw raw;
-    if (some && in_set < a.H) load(a.k, in_set, raw);
+    if (some && in_set < a.H) {
+      load(a.k, in_set, raw);
+      // (and values come nearer)
+      if (l % 4 == 0)
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i)
+          if (rows[i] >= 0)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(
+                a.v.data + (int64_t(rows[i]) * a.v.token + int64_t(in_set) * a.v.head) * 2 + 32 * l));
+    }
     if constexpr (ROT != kNone) {
       float4* const table = tables + ((it & 1) * p.sets + (busy ? set : 0)) * kSet;
       if (some) {
