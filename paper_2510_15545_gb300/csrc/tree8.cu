@@ -9,11 +9,11 @@
 // The bound is the cache, half of what 16 bits take, so half the time for each of its
 // tiles. Their products are matrix products: 128 rows (token, head of the group) against
 // tiles of 128 keys. Keys are multiplied as they are, e4m3 by e4m3: a query is the sum of
-// two (bf16) or three (fp16) e4m3 pieces of a power of two of its row, its 8 or 11 digits
-// exactly for elements down to 2^-10 of the row's largest, and within 2^-19 of that below;
-// the products add the pieces up. Values become fp16, which holds every e4m3 value, by four
-// warps of their own, in units of the largest scale so far (2^-24 of that unit is the
-// finest); when a larger one comes the sums fall. The request's own drafted tokens are
+// two (bf16) or three (fp16) e4m3 pieces of a power of two of its row, which the products
+// add up: its 8 or 11 digits, but for what is below 2^-17 of the row's largest element (the
+// distance of the smallest e4m3 numbers). Values become fp16, which holds every e4m3 value,
+// by four warps of their own, in units of the largest scale so far (2^-24 of that unit is
+// the finest); when a larger one comes the sums fall. The request's own drafted tokens are
 // tiles of keys and values of the inputs' type.
 //
 // One CTA per SM: two warps copy (a page's slots at a time) keys and values with their
@@ -406,12 +406,17 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     int vt = 0, st = 0, w = 0, seg = 0, drafted = 0;
     uint32_t parity = 0;
 #pragma unroll 1
-    for (; todo > x.lead && ok; ++seg) {
+    for (; todo > x.lead; ++seg) {
       todo -= x.lead;
       const Item it(shape, x, todo);
       const int side = seg & 1, row0 = x.mt * kRows, token0 = row0 / p.group;
-      // (the item before the last one is over)
-      if (!wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1)) break;
+      // (The item before the last one is over. The four warps meet at barriers: they give up
+      // as one, here.)
+      wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1);
+      if (any_of(6, kConvThreads, !ok)) {
+        ok = false;
+        break;
+      }
       // Its facts, and a token's ancestors: one thread walks up from each token.
       if (ct == 0)
         s.facts[side] = Facts{it.n_tree, it.rows, it.tile0, it.tile1, it.end,
@@ -420,9 +425,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       if (it.tile0 < it.n_tree) {
         // (the parents in the place of the values to come, the ancestors once rows are done
         // with the last ones)
-        if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1) ||
-            !wait_for(&s.seen_free, (drafted++ & 1) ^ 1))
+        wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1);
+        wait_for(&s.seen_free, (drafted++ & 1) ^ 1);
+        if (any_of(6, kConvThreads, !ok)) {
+          ok = false;
           break;
+        }
         int16_t* const ups = reinterpret_cast<int16_t*>(s.w[w & 1]);
 #pragma unroll 1
         for (int i = ct; i < it.end; i += kConvThreads) {
@@ -455,35 +463,36 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         }
         const uint32_t code = e8m0_for(top);
         const float inverse = e8m0_inverse(code);
-        if (!wait_for(&s.q_empty, (seg & 1) ^ 1)) break;
-        s.factor[side][ct] = p.scale2 * e8m0(code);
+        if (wait_for(&s.q_empty, (seg & 1) ^ 1)) {
+          s.factor[side][ct] = p.scale2 * e8m0(code);
 #pragma unroll 2
-        for (int u = 0; u < D / 8; ++u) {  // (read again: from L1 or L2)
-          const uint4 q = valid ? from[u] : make_uint4(0, 0, 0, 0);
-          *reinterpret_cast<uint4*>(s.q16 + (u / 8) * kBlock + swizzled16(ct, u % 8)) = q;
-          float e[8];
-          unpack16<DT>(q, e);
+          for (int u = 0; u < D / 8; ++u) {  // (read again: from L1 or L2)
+            const uint4 q = valid ? from[u] : make_uint4(0, 0, 0, 0);
+            *reinterpret_cast<uint4*>(s.q16 + (u / 8) * kBlock + swizzled16(ct, u % 8)) = q;
+            float e[8];
+            unpack16<DT>(q, e);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
-            e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
+            for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
+              e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
 #pragma unroll
-          for (int piece = 0; piece < kPieces; ++piece) {
-            uint32_t two[4];
+            for (int piece = 0; piece < kPieces; ++piece) {
+              uint32_t two[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
-              const uint32_t half = e4m3x2_to_f16x2(two[k]);
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
-              e[2 * k] -= f.x;
-              e[2 * k + 1] -= f.y;
+              for (int k = 0; k < 4; ++k) {
+                two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
+                const uint32_t half = e4m3x2_to_f16x2(two[k]);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
+                e[2 * k] -= f.x;
+                e[2 * k + 1] -= f.y;
+              }
+              *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * kRows + ct, u * 8)) =
+                  make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
             }
-            *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * kRows + ct, u * 8)) =
-                make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
           }
+          fence_proxy_async();
+          mbar_arrive(&s.q_full);
+          mbar_arrive(&s.item_full[side]);
         }
-        fence_proxy_async();
-        mbar_arrive(&s.q_full);
-        mbar_arrive(&s.item_full[side]);
       }
       for (int j = it.tile0; j < it.tile1 && ok; ++j) {
         const int keys = tile_keys(j, it.n_tree, it.end, x.r.len);

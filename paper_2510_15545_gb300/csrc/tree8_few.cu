@@ -438,12 +438,17 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
     int vt = 0, st = 0, w = 0, seg = 0;
     uint32_t parity = 0;
 #pragma unroll 1
-    for (; todo > x.lead && ok; ++seg) {
+    for (; todo > x.lead; ++seg) {
       todo -= x.lead;
       const Item it(shape, x, todo);
       const int side = seg & 1, row0 = x.mt * R, token0 = row0 / p.group;
-      // (the item before the last one is over)
-      if (!wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1)) break;
+      // (The item before the last one is over. The four warps meet at barriers: they give up
+      // as one, here.)
+      wait_for(&s.o_free[side], ((seg >> 1) & 1) ^ 1);
+      if (any_of(6, kConvThreads, !ok)) {
+        ok = false;
+        break;
+      }
       // Its facts, and a token's ancestors: one thread walks up from each token.
       if (ct == 0)
         s.facts[side] = Facts{it.n_tree, it.rows, it.tile0, it.tile1, it.end,
@@ -496,35 +501,36 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
         for (int o = 1; o < kEach; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const uint32_t code = e8m0_for(top);
         const float inverse = e8m0_inverse(code);
-        if (!wait_for(&s.q_empty, (seg & 1) ^ 1)) break;
-        if (sub == 0) s.factor[side][r] = not_zero(p.scale2 * e8m0(code));
+        if (wait_for(&s.q_empty, (seg & 1) ^ 1)) {
+          if (sub == 0) s.factor[side][r] = not_zero(p.scale2 * e8m0(code));
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-          const int u = sub * kVecs + i;  // 16-byte unit of the row
-          *reinterpret_cast<uint4*>(s.q16 + (u / 8) * (R * 128) + swizzled16(r, u % 8)) = q[i];
-          float e[8];
-          unpack16<DT>(q[i], e);
+          for (int i = 0; i < kVecs; ++i) {
+            const int u = sub * kVecs + i;  // 16-byte unit of the row
+            *reinterpret_cast<uint4*>(s.q16 + (u / 8) * (R * 128) + swizzled16(r, u % 8)) = q[i];
+            float e[8];
+            unpack16<DT>(q[i], e);
 #pragma unroll
-          for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
-            e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
+            for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
+              e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
 #pragma unroll
-          for (int piece = 0; piece < kPieces; ++piece) {
-            uint32_t two[4];
+            for (int piece = 0; piece < kPieces; ++piece) {
+              uint32_t two[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
-              const uint32_t half = e4m3x2_to_f16x2(two[k]);
-              const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
-              e[2 * k] -= f.x;
-              e[2 * k + 1] -= f.y;
+              for (int k = 0; k < 4; ++k) {
+                two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
+                const uint32_t half = e4m3x2_to_f16x2(two[k]);
+                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
+                e[2 * k] -= f.x;
+                e[2 * k + 1] -= f.y;
+              }
+              *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) =
+                  make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
             }
-            *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) =
-                make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
           }
+          fence_proxy_async();
+          mbar_arrive(&s.q_full);
+          mbar_arrive(&s.item_full[side]);
         }
-        fence_proxy_async();
-        mbar_arrive(&s.q_full);
-        mbar_arrive(&s.item_full[side]);
       }
       for (int j = it.tile0; j < it.tile1 && ok; ++j) {
         const int keys = tile_keys(j, it.n_tree, it.end, x.r.len);
