@@ -2,12 +2,19 @@
 elements and scales stand for, as numbers of 64 bits, goes through the same reference
 as for caches of 16 bits.
 
-Tolerances. As there (scores, weights, output), with two additions. Queries meet the
-e4m3 keys as sums of e4m3 pieces, exact but for what lies 2^-21 below a row's largest
-element: that times the keys' sizes joins a score's error. Weights of cached keys are
-fp16 numbers in units of the largest scale 2^k of the values, the largest weight at 2^7
-or more: beyond 2^-11 of each, they are off by half of fp16's least number, 2^-25, so 2^-32
-of the largest; times 448 2^k, at most twice the largest value, for every key."""
+Tolerances. As there (scores, weights, output), with three additions.
+Queries meet the e4m3 keys as sums of e4m3 pieces of q 2^-e, e the least with which the
+row's largest element is 448 or less, so that it is over 224. Each piece takes four binary
+digits off what is left, until that is below 2^-9, the distance of the smallest e4m3
+numbers: then it is off by half of that, 2^-10, which is less than 2^-17 of the largest
+element. That times the keys' sizes joins a score's error.
+Weights of cached keys are fp16 numbers, of a row's sum in units in which its largest is
+2^7 or more; with few rows they take the values' scales, relative to the largest scale 2^k so
+far. Beyond 2^-11 of each they are off by half of fp16's least number, 2^-25, so by 2^-32 of
+the largest; times 448 2^k, at most twice the largest value, for every key: 2^-31.
+With many rows the values take the scales: they are off by 2^-25 2^k, k of the largest scale
+so far, so by 2^-32 of the largest value, and their mean by no more.
+"""
 import ctypes
 import dataclasses
 import math
@@ -98,7 +105,7 @@ def expected(c, b, scale, skip_pages=()):
     q = c.q[lo:lo + n].double().view(n, Hkv, G, D)
     s = torch.einsum("nhgd,lhd->hgnl", q, k) * scale
     sizes = torch.einsum("nhgd,lhd->hgnl", q.abs(), k.abs()) * 2.0 ** -20
-    sizes += torch.einsum("nhg,lh->hgnl", q.abs().amax(-1), k.abs().sum(-1)) * 2.0 ** -21
+    sizes += torch.einsum("nhg,lh->hgnl", q.abs().amax(-1), k.abs().sum(-1)) * 2.0 ** -17
     es = (sizes * scale).masked_fill(~seen, 0).amax(-1)
     s = s.masked_fill(~seen, -math.inf)
     lse = torch.logsumexp(s, -1)
