@@ -1032,8 +1032,9 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
     request], cache_len int32 [B]. Returns out [N, q heads, head_dim], lse
     [N, q heads] and status [B]; tensors given in ``out`` are written in place.
     Caches in 8 bits are float8_e4m3fn with k_scale and v_scale float8_e8m0fnu [pages,
-    page_size / 16, kv heads], as tt_cache_append leaves them. max_len and max_nodes bound the lengths and the nodes of a request and size the
-    launch (default: what the table and N allow)."""
+    page_size / 16, kv heads], as tt_cache_append leaves them. max_len and max_nodes
+    bound the lengths and the nodes of a request and size the launch (default: what the
+    table and N allow)."""
     if stream is not None:
         with _on(stream):
             return tt_tree_attn(q, k, v, k_cache, v_cache, page_table, cache_len, tree_off, parents,
@@ -1058,7 +1059,7 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
         # keeps that would keep it too)
         size = L.tt_tree8_workspace_bytes if scales else L.tt_tree_workspace_bytes
         n = int(size(ctypes.byref(T)))
-        ws = q.new_empty(n, dtype=torch.uint8)
+        ws = torch.empty(n, dtype=torch.uint8, device=q.device)
     ws_p, n = ws.data_ptr(), ws.numel()
     if out:
         o = dict(out)
@@ -1066,11 +1067,10 @@ def tt_tree_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, k_cache: tor
             o["lse"] = torch.empty((N, Hq), dtype=torch.float32, device=q.device)
         _need(o, "status", B, torch.int32, q.device)
     else:
-        buf = q.new_empty(rows + B, dtype=torch.float32)
-        o = {"lse": buf.as_strided((N, Hq), (Hq, 1), 0),
-             "status": buf.view(torch.int32).as_strided((B,), (1,), rows)}
+        o = {"lse": torch.empty((N, Hq), dtype=torch.float32, device=q.device),
+             "status": torch.empty(B, dtype=torch.int32, device=q.device)}
     if "out" not in o:
-        o["out"] = q.new_empty((N, Hq, D))
+        o["out"] = torch.empty((N, Hq, D), dtype=q.dtype, device=q.device)
     args = (ws_p, n, _given(o["out"], "out", q.dtype, rows * D),
             _given(o["lse"], "lse", torch.float32, rows),
             _given(o["status"], "status", torch.int32, B), _stream(None))
@@ -1181,7 +1181,8 @@ def tt_rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor,
             if name in o:
                 raise ValueError("out holds keys, but none are given")
         elif name not in o:
-            o[name] = torch.empty(x.shape, dtype=dtype, device=x.device)
+            o[name] = (torch.empty_like(x) if x.is_contiguous() else
+                       torch.empty(x.shape, dtype=dtype, device=x.device))
         elif o[name].shape != x.shape:
             raise ValueError("out's %s must have its input's shape" % name)
     n = turns.numel()
@@ -1228,7 +1229,12 @@ class _Rope(torch.autograd.Function):
     def backward(ctx, *ups):
         args = *ctx.saved_tensors, *ctx.args
         got = [_dense(u) for u in ups if u is not None]
-        if len(got) == 2:
+        if not torch.is_grad_enabled():  # (no graph of the gradients: half the host's time)
+            positions, turns, interleaved, mscale, transpose = args
+            o = tt_rope(got[0], got[1] if len(got) == 2 else None, positions, turns,
+                        interleaved=interleaved, mscale=mscale, transpose=transpose)
+            grads = [o["q"], o["k"]] if len(got) == 2 else [None if u is None else o["q"] for u in ups]
+        elif len(got) == 2:
             grads = _Rope.apply(*got, *args)
         else:
             grads = [None if u is None else _Rope.apply(got[0], None, *args) for u in ups]
@@ -1316,7 +1322,7 @@ def tt_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_c
         _need(o, "new_len", B, i32, k.device)
         _need(o, "status", B, i32, k.device)
     else:
-        buf = cache_len.new_empty(2 * B)
+        buf = torch.empty(2 * B, dtype=i32, device=k.device)
         o = {"new_len": buf.as_strided((B,), (1,), 0), "status": buf.as_strided((B,), (1,), B)}
     code = load().tt_cache_append(ctypes.byref(A), None if plan is None else ctypes.byref(plan),
                                   _given(o["new_len"], "new_len", i32, B),
