@@ -13,7 +13,7 @@ Each round, for a batch of requests:
    target's top alternatives at every position that was reached;
 5. ``tt_distill`` is the draft's loss against those, and its gradient to the draft
    logits; plain products carry it into the draft's weights;
-6. keys and values of the accepted tokens enter the cache.
+6. ``tt_cache_append`` puts keys and values of the accepted tokens into the cache.
 
     python examples/online_draft.py [--rounds N]
 """
@@ -65,13 +65,9 @@ class Cache:
     def append(self, k, v, counts):
         """The first counts[b] of request b's n tokens, k and v [B, n, heads, head]."""
         B, n = k.shape[:2]
-        i = torch.arange(n, device="cuda")
-        slot = self.len[:, None].long() + i
-        page = self.table.long().gather(1, (slot // PAGE).clamp(max=self.table.shape[1] - 1))
-        take = i < counts[:, None]
-        self.k[page[take], slot[take] % PAGE] = k[take]
-        self.v[page[take], slot[take] % PAGE] = v[take]
-        self.len += counts
+        off = torch.arange(B + 1, dtype=torch.int32, device="cuda") * n
+        self.len = tt.tt_cache_append(k.flatten(0, 1), v.flatten(0, 1), self.k, self.v, self.table,
+                                      self.len, off, keep=counts, max_new=n)["new_len"]
 
 
 def run(rounds=60, B=32, k=4, rate=3.0, seed=0, report=None):

@@ -647,10 +647,9 @@ size_t tt_tree8_workspace_bytes(const tt_tree* tree);
 
 /* tt_tree_attn over caches in 8 bits: tree's k_cache and v_cache hold e4m3 elements
  * (strides multiples of 16) with the given scales, as tt_cache_append leaves them;
- * q, k, v and the output are of tree's dtype. Keys count as they are; values are
- * rounded to that type, which holds them exactly within its range (fp16: multiples of
- * 2^-24 below 65,520). A slot whose scale is NaN makes its rows NaN. Everything else is as for
- * tt_tree_attn. */
+ * q, k, v and the output are of tree's dtype. Keys count as they are; queries to 2^-17 of
+ * a row's largest element, values to 2^-24 of the largest scale of the request's head. A
+ * slot whose scale is NaN makes its rows NaN. Everything else is as for tt_tree_attn. */
 tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_scales* v_scale,
                         void* workspace, size_t workspace_bytes, void* out, float* lse,
                         int32_t* status, void* stream);

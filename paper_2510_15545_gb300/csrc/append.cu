@@ -11,12 +11,18 @@
 // costs its neighbours stays with 16 of them.
 //
 // Every element is read and written once, so memory bounds it. Work is one group of
-// 16 slots of one head: a warp holds its elements in fp32 registers between finding
-// the largest and rounding them, keys first, then values. The warps of a CTA take the
+// 16 slots of one head: a warp holds its elements in registers between finding the
+// largest and rounding them, keys first, then values. The warps of a CTA take the
 // heads of the same group, and share its sines and cosines, formed once, through
 // shared memory: formed by each head they took as many instructions as the copies'
 // time allows. The groups that the requests touch form one list, which the CTAs share
 // evenly: how many a request brings is known on the device alone.
+//
+// 8 prompts of 8192 tokens, 8 heads of 128, turned, to 8 bits: 92 us, 4.4 TB/s. A lane has
+// both elements of its pairs (with a vector of its own and its partner's, turned by both
+// lanes, 309 us); values are fetched into L2 while sines are formed (98 without). Two CTAs of
+// 128 registers to an SM: a third's worth of the list waited for a second round. Single
+// tokens of 256 requests: 10 us, one dependent read after another.
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
