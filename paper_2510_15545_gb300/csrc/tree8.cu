@@ -153,23 +153,23 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     }
     for (int i = 0; i < S::kStagesV; ++i) {
       mbar_init(&s.v_full[i], 1);
-      mbar_init(&s.v_empty[i], kConvThreads);
+      mbar_init(&s.v_empty[i], kConvWarps);
     }
     for (int i = 0; i < kScaleRing; ++i) mbar_init(&s.scale_full[i], 2);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&s.w_full[i], kConvThreads);
+      mbar_init(&s.w_full[i], kConvWarps);
       mbar_init(&s.w_empty[i], 1);
-      mbar_init(&s.s_full[i], 1);
-      mbar_init(&s.s_free[i], kRowThreads);
-      mbar_init(&s.p_full[i], kRowThreads);
+      mbar_init(&s.s_full[i], 2);
+      mbar_init(&s.s_free[i], kRowWarps);
+      mbar_init(&s.p_full[i], kRowWarps);
       mbar_init(&s.o_done[i], 1);
-      mbar_init(&s.item_full[i], kConvThreads);
-      mbar_init(&s.o_free[i], kRowThreads);
+      mbar_init(&s.item_full[i], kConvWarps);
+      mbar_init(&s.o_free[i], kRowWarps);
     }
-    mbar_init(&s.q_full, kConvThreads);
+    mbar_init(&s.q_full, kConvWarps);
     mbar_init(&s.q_empty, 1);
-    mbar_init(&s.own_full, kConvThreads);
-    mbar_init(&s.seen_free, kRowThreads);
+    mbar_init(&s.own_full, kConvWarps);
+    mbar_init(&s.seen_free, kRowWarps);
     mbar_init(&s.drained[0], 1);
     mbar_init(&s.drained[1], 1);
     s.stop = INT32_MAX;
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     if (warp == kRowWarps + kConvWarps) {
       const uint64_t kd = umma8_desc<D>(smem_u32(s.k)), qd = umma8_desc<D>(smem_u32(s.q8)),
                      od = umma_desc(smem_u32(s.q16), 16), wk = umma_desc(smem_u32(s.w), 16);
-      int turn = 0, st = 0, drafted = 0;
+      int turn = 0, st = 0, drafted = 0, ct = 0;
 #pragma unroll 1
       for (int seg = 0; todo > x.lead && ok; ++seg) {
         todo -= x.lead;
@@ -318,7 +318,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           const int buf = n & 1;
           const uint32_t to = tmem + buf * kTile;
           if (j >= it.n_tree) {
-            ok = on(&s.k_full[st], turn & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
+            ok = on(&s.k_full[st], turn & 1) && on(&s.scale_full[ct % kScaleRing], (ct / kScaleRing) & 1) &&
+                 on(&s.s_free[buf], ((n >> 1) & 1) ^ 1) && on(&s.o_done[buf], ((n >> 1) & 1) ^ 1);
+            ++ct;
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -329,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
                   umma8_ss(to, qd + q * (kRows * D / 16) + 2 * c, kd + st * kKStep + 2 * c,
                            idesc_e4m3(kTile), q > 0 || c > 0);
               umma_commit(&s.s_full[buf]);
+              mbar_arrive(&s.s_full[buf]);
               umma_commit(&s.k_empty[st]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
             }
@@ -339,7 +342,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           } else {
             // (a barrier of their own: on w_full's, this warp could be two phases ahead, where
             // a parity says nothing)
-            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1);
+            ok = on(&s.own_full, drafted++ & 1) && on(&s.s_free[buf], ((n >> 1) & 1) ^ 1) &&
+                 on(&s.o_done[buf], ((n >> 1) & 1) ^ 1);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -349,6 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
                         wk + (w & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
                         umma_idesc(F16, kTile, false), c > 0);
               umma_commit(&s.s_full[buf]);
+              mbar_arrive(&s.s_full[buf]);
               umma_commit(&s.w_empty[w & 1]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
             }
@@ -402,6 +407,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     auto wait_for = [&](uint64_t* bar, uint32_t parity) {
       if (ok) ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       return ok;
+    };
+    auto arrive = [&](uint64_t* bar) {  // of the warp
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
     };
     int vt = 0, st = 0, w = 0, seg = 0, drafted = 0;
     uint32_t parity = 0;
@@ -490,8 +499,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             }
           }
           fence_proxy_async();
-          mbar_arrive(&s.q_full);
-          mbar_arrive(&s.item_full[side]);
+          arrive(&s.q_full);
+          arrive(&s.item_full[side]);
         }
       }
       for (int j = it.tile0; j < it.tile1 && ok; ++j) {
@@ -541,7 +550,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
               }
             }
           }
-          mbar_arrive(&s.v_empty[st]);
+          arrive(&s.v_empty[st]);
           ++vt;
           if (++st == S::kStagesV) {
             st = 0;
@@ -587,15 +596,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             }
             if (kv == 0) {
               fence_proxy_async();
-              mbar_arrive(&s.w_full[w & 1]);
-              mbar_arrive(&s.own_full);
+              arrive(&s.w_full[w & 1]);
+              arrive(&s.own_full);
               ++w;
             }
           }
           if (!ok) break;
         }
         fence_proxy_async();
-        mbar_arrive(&s.w_full[w & 1]);
+        arrive(&s.w_full[w & 1]);
         ++w;
       }
       todo -= it.tile1 - it.tile0;
@@ -604,7 +613,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
     // (no more)
     if (ok && wait_for(&s.o_free[seg & 1], ((seg >> 1) & 1) ^ 1)) {
       if (ct == 0) s.facts[seg & 1].tile1 = -1;
-      mbar_arrive(&s.item_full[seg & 1]);
+      arrive(&s.item_full[seg & 1]);
     }
   } else {
     // -------------------------------------------------------------- rows
@@ -633,6 +642,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       ok = __all_sync(0xffffffffu, wait8(bar, parity, limit));
       if (!ok && lane == 0) atomicMin(&s.stop, at_place);
     };
+    auto arrive = [&](uint64_t* bar) {  // of the warp
+      __syncwarp();
+      if (ok && lane == 0) mbar_arrive(bar);
+    };
     int n = 0, ct = 0;
 #pragma unroll 1
     for (int seg = 0; todo > 0; ++seg) {
@@ -652,11 +665,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       for (int j = it.tile0; j < it.tile1; ++j, ++n) {
         const bool cache = j >= it.n_tree, first = j == it.tile0;
         const int keys = tile_keys(j, it.n_tree, it.end, it.len), e = ct % kScaleRing;
+        // (with the scores, the scales are there, the ancestors, and the weights' place: the
+        // product of two tiles ago is done)
+        wait_for(&s.s_full[n & 1], (n >> 1) & 1);
+        tc_fence_after();
         float f[4];  // what makes a score of each 16 keys its log2
         int unit = kOwnCode;
         uint32_t lost = 0;
         if (cache) {
-          wait_for(&s.scale_full[e], (ct / kScaleRing) & 1);
           const float4 scale = *reinterpret_cast<const float4*>(s.k_scale[e] + 4 * half);
           f[0] = not_zero(scale.x * factor);
           f[1] = not_zero(scale.y * factor);
@@ -668,8 +684,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         } else {
           f[0] = f[1] = f[2] = f[3] = p.scale2;
         }
-        wait_for(&s.s_full[n & 1], (n >> 1) & 1);
-        tc_fence_after();
         uint32_t v[2][32];
         float high = -INFINITY;
         if (some) {
@@ -700,9 +714,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           }
         }
         tc_fence_before();
-        if (ok) mbar_arrive(&s.s_free[n & 1]);
+        arrive(&s.s_free[n & 1]);
         // (all ancestors are read)
-        if (j + 1 == min(it.n_tree, it.tile1) && ok) mbar_arrive(&s.seen_free);
+        if (j + 1 == min(it.n_tree, it.tile1)) arrive(&s.seen_free);
         // what the values' scale makes of the sums, and a larger maximum of the row's
         float fall = 1.f;
         if (unit > code) {
@@ -748,9 +762,6 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
             weigh(std::true_type());
           l += sum_pair(sum2);
         }
-        // (the product of two tiles ago is done with the weights' place)
-        wait_for(&s.o_done[n & 1], ((n >> 1) & 1) ^ 1);
-        tc_fence_after();
         if (some) {
           const uint32_t to = mine + S::kWeights + (n & 1) * (kTile / 2) + 32 * half;
 #pragma unroll
@@ -771,7 +782,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           tmem_wait_st();
         }
         tc_fence_before();
-        if (ok) mbar_arrive(&s.p_full[n & 1]);
+        arrive(&s.p_full[n & 1]);
       }
       bool odd = false;
       if (it.tile0 < it.n_tree) odd = lane < kWords && s.odd[side][lane];
@@ -834,7 +845,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         }
       }
       tc_fence_before();
-      if (ok) mbar_arrive(&s.o_free[side]);
+      arrive(&s.o_free[side]);
     }
   }
   tc_fence_before();
