@@ -462,42 +462,32 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         const bool valid = ct < it.rows;
         const uint4* from = reinterpret_cast<const uint4*>(
             a.q + ((int64_t(x.r.first) + token) * a.q_token + int64_t(head) * a.q_head) * 2);
-        float top = 0.f;
-#pragma unroll 4
-        for (int u = 0; u < D / 8; ++u) {
-          float e[8];
-          unpack16<DT>(valid ? from[u] : make_uint4(0, 0, 0, 0), e);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
-        }
-        const uint32_t code = e8m0_for(top);
-        const float inverse = e8m0_inverse(code);
+        auto place = [&](int u) {  // 16-byte unit of the row
+          return reinterpret_cast<uint4*>(s.q16 + (u / 8) * kBlock + swizzled16(ct, u % 8));
+        };
+        // (The last loop is rolled, over what waits in the place for drafted keys: code that is
+        // run once an item comes from beyond the instruction caches, line by line.)
         if (wait_for(&s.q_empty, (seg & 1) ^ 1)) {
-          s.factor[side][ct] = p.scale2 * e8m0(code);
-#pragma unroll 2
-          for (int u = 0; u < D / 8; ++u) {  // (read again: from L1 or L2)
-            const uint4 q = valid ? from[u] : make_uint4(0, 0, 0, 0);
-            *reinterpret_cast<uint4*>(s.q16 + (u / 8) * kBlock + swizzled16(ct, u % 8)) = q;
-            float e[8];
-            unpack16<DT>(q, e);
+          float top = 0.f;
+#pragma unroll 1
+          for (int u = 0; u < D / 8; u += 4) {
+            uint4 q[4];
 #pragma unroll
-            for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
-              e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
+            for (int i = 0; i < 4; ++i) q[i] = valid ? from[u + i] : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int piece = 0; piece < kPieces; ++piece) {
-              uint32_t two[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
-                const uint32_t half = e4m3x2_to_f16x2(two[k]);
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
-                e[2 * k] -= f.x;
-                e[2 * k + 1] -= f.y;
-              }
-              *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * kRows + ct, u * 8)) =
-                  make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
+            for (int i = 0; i < 4; ++i) {
+              *place(u + i) = q[i];
+              top = largest<DT>(q[i], top);
             }
           }
+          const uint32_t code = e8m0_for(top);
+          const float inverse = e8m0_inverse(code);
+          s.factor[side][ct] = p.scale2 * e8m0(code);
+#pragma unroll 1
+          for (int u = 0; u < D / 8; ++u)
+            in_pieces<DT, kPieces>(*place(u), inverse, [&](int piece, uint2 two) {
+              *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * kRows + ct, u * 8)) = two;
+            });
           fence_proxy_async();
           arrive(&s.q_full);
           arrive(&s.item_full[side]);

@@ -483,20 +483,15 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
         constexpr int kEach = kConvThreads / R, kVecs = D / 8 / kEach;
         const int r = ct / kEach, sub = ct % kEach;
         const int row = x.mt * R + r, token = row / p.group, head = x.hk * p.group + row % p.group;
-        uint4 q[kVecs];
         const bool valid = r < it.rows;
-        const char* from = a.q + ((int64_t(x.r.first) + token) * a.q_token + int64_t(head) * a.q_head) * 2;
+        const uint4* from = reinterpret_cast<const uint4*>(
+            a.q + ((int64_t(x.r.first) + token) * a.q_token + int64_t(head) * a.q_head) * 2) + sub * kVecs;
+        uint4 q[kVecs];
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i)
-          q[i] = valid ? reinterpret_cast<const uint4*>(from)[sub * kVecs + i] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < kVecs; ++i) q[i] = valid ? from[i] : make_uint4(0, 0, 0, 0);
         float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < kVecs; ++i) {
-          float e[8];
-          unpack16<DT>(q[i], e);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
-        }
+        for (int i = 0; i < kVecs; ++i) top = largest<DT>(q[i], top);
 #pragma unroll
         for (int o = 1; o < kEach; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
         const uint32_t code = e8m0_for(top);
@@ -507,25 +502,9 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
           for (int i = 0; i < kVecs; ++i) {
             const int u = sub * kVecs + i;  // 16-byte unit of the row
             *reinterpret_cast<uint4*>(s.q16 + (u / 8) * (R * 128) + swizzled16(r, u % 8)) = q[i];
-            float e[8];
-            unpack16<DT>(q[i], e);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)  // (what is not finite has no pieces but NaN)
-              e[k] = fabsf(e[k]) < INFINITY ? e[k] * inverse : __uint_as_float(0x7fc00000u);
-#pragma unroll
-            for (int piece = 0; piece < kPieces; ++piece) {
-              uint32_t two[4];
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
-                const uint32_t half = e4m3x2_to_f16x2(two[k]);
-                const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
-                e[2 * k] -= f.x;
-                e[2 * k + 1] -= f.y;
-              }
-              *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) =
-                  make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16);
-            }
+            in_pieces<DT, kPieces>(q[i], inverse, [&](int piece, uint2 two) {
+              *reinterpret_cast<uint2*>(s.q8 + swizzled8<D>(piece * R + r, u * 8)) = two;
+            });
           }
           fence_proxy_async();
           mbar_arrive(&s.q_full);

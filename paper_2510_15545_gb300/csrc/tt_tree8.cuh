@@ -249,6 +249,38 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(r));
   return r != 0;
 }
+// The size of the largest of 8 elements that is finite, or `top`.
+template <int DT>
+__device__ __forceinline__ float largest(const uint4& q, float top) {
+  float e[8];
+  unpack16<DT>(q, e);
+#pragma unroll
+  for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
+  return top;
+}
+// 8 elements times `by` as sums of e4m3 pieces, each what the ones before leave (of what is
+// not finite NaN): put(piece, its 8 bytes).
+template <int DT, int PIECES, class Put>
+__device__ __forceinline__ void in_pieces(const uint4& q, float by, Put put) {
+  float e[8];
+  unpack16<DT>(q, e);
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    e[k] = fabsf(e[k]) < INFINITY ? e[k] * by : __uint_as_float(0x7fc00000u);
+#pragma unroll
+  for (int piece = 0; piece < PIECES; ++piece) {
+    uint32_t two[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      two[k] = to_e4m3x2(e[2 * k], e[2 * k + 1]);
+      const uint32_t half = e4m3x2_to_f16x2(two[k]);
+      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&half));
+      e[2 * k] -= f.x;
+      e[2 * k + 1] -= f.y;
+    }
+    put(piece, make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16));
+  }
+}
 // What a CTA finds of the list: it adds up the requests' places, each thread those of a run
 // of them, and the one whose run holds the CTA's first place tells the request. Returns
 // the CTA's places. (Every thread comes; a barrier behind it makes s.start_* known.)
