@@ -633,8 +633,9 @@ typedef struct {
  * before cache_len are in use in the group it is at least theirs, and if it is larger
  * those are rounded again. Elements that are not finite are NaN there; finite ones
  * are held within 1.875 2^15 (fp16) or 1.875 2^127 (bf16). Slots past the appended ones
- * stay as they are. new_len [B] (optional; not cache_len's own memory) is the slots in
- * use after. status [B]: BAD_OFFSETS (also: keep[b] beyond the request's tokens) and
+ * stay as they are. new_len [B] (optional) is the slots in use after; it and status share
+ * no memory with each other or the inputs, nor do the two caches (or their scales) begin at
+ * one place. status [B]: BAD_OFFSETS (also: keep[b] beyond the request's tokens) and
  * TOO_LONG (more tokens than max_new, a length that is negative or would pass
  * max_len) append nothing; ID_OUT_OF_RANGE reports an entry of the path or a page out
  * of range, whose tokens are left out, and new_len stays as it was in all these
@@ -648,8 +649,9 @@ size_t tt_tree8_workspace_bytes(const tt_tree* tree);
 /* tt_tree_attn over caches in 8 bits: tree's k_cache and v_cache hold e4m3 elements
  * (strides multiples of 16) with the given scales, as tt_cache_append leaves them;
  * q, k, v and the output are of tree's dtype. Keys count as they are; queries to 2^-17 of
- * a row's largest element, values to 2^-24 of the largest scale of the request's head. A
- * slot whose scale is NaN makes its rows NaN. Everything else is as for tt_tree_attn. */
+ * a row's largest element; values to 2^-24 of the largest scale of the request's head, or
+ * of 1 (fp16) or 2^-60 (bf16) if that is larger. A slot whose scale is NaN makes its rows
+ * NaN. Everything else is as for tt_tree_attn. */
 tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_scales* v_scale,
                         void* workspace, size_t workspace_bytes, void* out, float* lse,
                         int32_t* status, void* stream);

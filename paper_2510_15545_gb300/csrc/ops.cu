@@ -172,6 +172,12 @@ RopeTensor rope_tensor(const tt_heads& h) {
   return {static_cast<char*>(const_cast<void*>(h.data)), h.token_stride, h.head_stride};
 }
 
+// Whether n numbers at a and m at b (NULL: none) share memory.
+bool meet(const int32_t* a, int64_t n, const int32_t* b, int64_t m) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return b && x < y + uintptr_t(m) * 4 && y < x + uintptr_t(n) * 4;
+}
+
 AppendCache append_cache(const tt_pages& p, const tt_scales& s) {
   return {static_cast<char*>(const_cast<void*>(p.data)), p.page_stride, p.slot_stride,
           p.head_stride, s.data, s.page_stride, s.group_stride, s.head_stride};
@@ -381,13 +387,22 @@ tt_status tt_cache_append(const tt_append* p, const tt_rope_plan* rope, int32_t*
     return TT_ERR_INVALID_ARG;
   if (rope && !rope_plan_ok(*rope, p->head_dim)) return TT_ERR_INVALID_ARG;
   if (p->B == 0) return TT_OK;
-  if (!p->token_off || !p->cache_len || !status || new_len == p->cache_len) return TT_ERR_INVALID_ARG;
+  if (!p->token_off || !p->cache_len || !status) return TT_ERR_INVALID_ARG;
+  // (what some CTAs write, others still read)
+  const int64_t B = p->B;
+  for (const int32_t* out : {static_cast<const int32_t*>(new_len), static_cast<const int32_t*>(status)})
+    if (out && (meet(out, B, p->cache_len, B) || meet(out, B, p->token_off, B + 1) ||
+                meet(out, B, p->keep, B) || meet(out, B, p->path, p->n_tokens)))
+      return TT_ERR_INVALID_ARG;
+  if (new_len && meet(new_len, B, status, B)) return TT_ERR_INVALID_ARG;
   if (p->n_tokens > 0 && (!heads_ok(p->k) || !heads_ok(p->v))) return TT_ERR_INVALID_ARG;
   const bool held8 = p->cache_dtype == TT_E4M3;
   const int64_t pages = (int64_t(p->max_len) + p->page_size - 1) / p->page_size;
   if (p->max_len > 0) {
     if (held8 ? !pages8_ok(p->k_cache, p->k_scale) || !pages8_ok(p->v_cache, p->v_scale)
               : !pages_ok(p->k_cache) || !pages_ok(p->v_cache))
+      return TT_ERR_INVALID_ARG;
+    if (p->k_cache.data == p->v_cache.data || (held8 && p->k_scale.data == p->v_scale.data))
       return TT_ERR_INVALID_ARG;
     if (p->n_pages < 1 || p->n_pages > INT32_MAX || !p->page_table || p->table_stride < pages)
       return TT_ERR_INVALID_ARG;

@@ -24,6 +24,10 @@
 // which the CTAs share evenly: lengths are known on the device alone. Items cut by a CTA's
 // end leave unnormalised pieces, which a second kernel joins.
 //
+// Two documents of 131,072 keys with 32 tokens each, 16 heads on 2: 85.5 us, 2200 cycles a
+// tile and CTA, most of them a row's way from its scores to its weights (780 of exponentials).
+// Four threads to a row took 109 us: its barriers cost more than its shares saved.
+//
 // Requests of few rows go to tree8_few.cu, whose products have them as columns; how both
 // compare stands at the rule that chooses.
 #include <cuda.h>

@@ -14,9 +14,10 @@
 //
 // One CTA per SM: two warps copy, four convert, two issue products, eight or sixteen turn
 // scores into weights: half of them the even tiles and half the odd ones, each with
-// references, sums and an output of their own. What bounds it is how long a tile takes from
-// its scores to its weights, not the cache: 12 instructions a score, 1.07 GB of caches for
-// 256 single tokens in 321 us, 3.3 TB/s (at 4 rows the products' other columns are empty).
+// references, sums and an output of their own. 1.07 GB of caches for 256 single tokens take
+// 314 us, 3.4 TB/s: a fifth of it is items' beginnings and ends, and values are on their way
+// in three stages only. Of 36 rows what bounds it is how long a tile takes from its scores to
+// its weights, 12 instructions a score: 202 us for 64 requests of 9 tokens, 2.7 TB/s.
 // The loops over the rows are rolled: unrolled, their code came from beyond the instruction
 // caches.
 #include <algorithm>

@@ -30,13 +30,14 @@ def test_struct_layouts():
     assert binding.TT_E4M3 == 3 and binding.TT_SCALE_SLOTS == 16
 
 
-def append(lib, plan=None, new_len=3 * MEMORY, status=MEMORY, **kw):
+def append(lib, plan=None, new_len=3 * MEMORY, status=4 * MEMORY, **kw):
     heads = binding._Heads(MEMORY, 1024, 128)
     pages = binding._Pages(MEMORY, 16 * 1024, 1024, 128)
-    scales = binding._Scales(MEMORY, 8, 8, 1)
+    more = binding._Pages(8 * MEMORY, 16 * 1024, 1024, 128)
+    scales, scales_too = binding._Scales(MEMORY, 8, 8, 1), binding._Scales(2 * MEMORY, 8, 8, 1)
     f = dict(B=2, n_tokens=8, max_new=4, dtype=1, cache_dtype=3, n_heads=8, head_dim=128,
-             page_size=16, token_off=MEMORY, k=heads, v=heads, k_cache=pages, v_cache=pages,
-             k_scale=scales, v_scale=scales, n_pages=100, page_table=MEMORY, table_stride=8,
+             page_size=16, token_off=MEMORY, k=heads, v=heads, k_cache=pages, v_cache=more,
+             k_scale=scales, v_scale=scales_too, n_pages=100, page_table=MEMORY, table_stride=8,
              cache_len=2 * MEMORY, max_len=100)
     f.update(kw)
     return lib.tt_cache_append(P(binding._Append(**f)), P(plan) if plan else None, new_len, status,
@@ -75,6 +76,20 @@ def test_tensors_refused(lib):
     for bad in (binding._Scales(None, 8, 8, 1), binding._Scales(MEMORY, -8, 8, 1),
                 binding._Scales(MEMORY, 8, -8, 1), binding._Scales(MEMORY, 8, 8, -1)):
         assert append(lib, k_scale=bad) == INVALID and append(lib, v_scale=bad) == INVALID
+
+
+def test_memory_that_is_read_and_written_refused(lib):
+    for at in (MEMORY, MEMORY + 8, MEMORY - 4, 2 * MEMORY, 2 * MEMORY + 4):
+        assert append(lib, new_len=at) == INVALID and append(lib, status=at) == INVALID
+    for name in ("keep", "path"):
+        for at in (16 * MEMORY, 16 * MEMORY - 4, 16 * MEMORY + 4):
+            for out in ("new_len", "status"):
+                assert append(lib, **{name: 16 * MEMORY, out: at}) == INVALID
+    assert append(lib, new_len=4 * MEMORY) == INVALID
+    one = binding._Pages(MEMORY, 16384, 1024, 128)
+    for cache in (1, 3):
+        assert append(lib, cache_dtype=cache, k_cache=one, v_cache=one) == INVALID
+    assert append(lib, v_scale=binding._Scales(MEMORY, 8, 8, 1)) == INVALID
 
 
 def test_no_requests_need_nothing(lib):
