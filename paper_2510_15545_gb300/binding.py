@@ -1229,6 +1229,8 @@ class _Rope(torch.autograd.Function):
     def backward(ctx, *ups):
         args = *ctx.saved_tensors, *ctx.args
         got = [_dense(u) for u in ups if u is not None]
+        if not got:
+            return (None,) * 7
         if not torch.is_grad_enabled():  # (no graph of the gradients: half the host's time)
             positions, turns, interleaved, mscale, transpose = args
             o = tt_rope(got[0], got[1] if len(got) == 2 else None, positions, turns,
@@ -1244,7 +1246,8 @@ class _Rope(torch.autograd.Function):
 def rope(q: torch.Tensor, k: Optional[torch.Tensor], positions: torch.Tensor, turns: torch.Tensor,
          *, interleaved: bool = False, mscale: float = 1.0):
     """tt_rope as differentiable q and k (k None: q alone); gradients flow to the
-    heads."""
+    heads. (To capture a backward pass into a CUDA graph, as with any function of autograd,
+    let go of eager graphs of the same leaves first.)"""
     return _Rope.apply(q, k, positions, turns, bool(interleaved), float(mscale), False)
 
 

@@ -268,6 +268,32 @@ def test_leaves_that_need_no_gradient():
     assert k.grad.shape == k.shape
 
 
+class _Nothing(torch.autograd.Function):
+    """A function that gives no gradient."""
+
+    @staticmethod
+    def forward(ctx, x):
+        return x.clone()
+
+    @staticmethod
+    def backward(ctx, up):
+        return None
+
+
+def test_results_whose_gradients_do_not_come():
+    q, k, at = make(5, 4, 2, 64, F, seed=21)
+    turns = turns_of(64)
+    q, k = (x.detach().clone().requires_grad_() for x in (q, k))
+    a, b = tt.rope(q, k, at, turns)
+    (_Nothing.apply(a).sum() + _Nothing.apply(b).sum()).backward()
+    assert q.grad is None and k.grad is None
+    a, b = tt.rope(q, k, at, turns)
+    (_Nothing.apply(a).sum() + b.sum()).backward()
+    assert q.grad is None
+    want, bound = expected(torch.ones_like(k), at, turns, False, transpose=True)
+    assert ((k.grad.double() - want).abs() <= bound).all()
+
+
 def test_captured_in_a_graph():
     q, k, at = make(9, 4, 2, 128, H, seed=12)
     turns = turns_of(128)
