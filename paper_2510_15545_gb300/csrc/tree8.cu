@@ -81,8 +81,8 @@ struct Smem8 {
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
   uint64_t p_full[2], o_done[2], item_full[2], o_free[2], seen_free, q_full, q_empty, own_full,
       drained[2];
-  long long sums[kThreads / 32];      // places of the requests, by warps
-  int start_b, start_offset;          // where this CTA's places begin
+  int sums[kThreads / 32];            // places of the requests, by warps
+  int start_b, start_hk, start_offset;  // where this CTA's places begin
   int share;                          // and how many a CTA has
   uint32_t tmem;
   int end, stop;                      // the place behind this CTA's, and where it gave up
@@ -188,7 +188,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
   bool ok = true;
   Place x;
   x.lead = 0;
-  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, shape, s.start_b, s.start_offset);
+  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, shape, s.start_b, s.start_hk, s.start_offset);
 
   if (warp > kRowWarps + kConvWarps + 1) {
     // ------------------------------------------------------------ copies
@@ -870,24 +870,28 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   const int i = int(at / a.Hq % a.max_nodes), b = int(at / a.Hq / a.max_nodes);
   if (b >= a.B) return;
   grid_dependency_wait();
-  const int share = p.first[a.B], first = p.first[b];
+  const int share = p.first[a.B], head = p.first[a.B + 1], first = p.first[b];
   const Request r = request(a, b);
   if (i >= r.nodes) return;
   const Shape shape{p.group, p.rows};
-  const int per_head = head_places(r, shape);
   // (one warp of the request)
   if (i == 0 && h == 0 && (FEW || threadIdx.x < 32)) {
-    const int end = first + per_head * a.Hkv - 1;  // its last place
-    int stop = INT32_MAX;
-    for (int c = first / share + lane; c <= end / share; c += 32) stop = min(stop, p.stop[c]);
-    if (__any_sync(0xffffffffu, stop <= end) && lane == 0) a.status[b] |= TT_REQ_TIMEOUT;
+    const int per_head = head_places(r, shape);
+    const int most = per_head / share + 2;  // CTAs that a head of it lies in, at most
+    bool lost = false;
+    for (int x = lane; x < a.Hkv * most; x += 32) {
+      const int k = x / most, from = k * head + first, end = from + per_head - 1;
+      const int c = from / share + x % most;
+      if (c <= end / share) lost |= p.stop[c] <= end;
+    }
+    if (__any_sync(0xffffffffu, lost) && lane == 0) a.status[b] |= TT_REQ_TIMEOUT;
   }
   const int row = i * p.group + h % p.group, mt = row / p.rows;
-  int before = hk * per_head + kItemCost;  // its first tile's place
+  int before = hk * head + first + kItemCost;  // its first tile's place
   for (int k = 0; k < mt; ++k) before += kItemCost + shape.tiles(r, k);
   const int last = before + shape.tiles(r, mt) - 1;
   // the CTAs that the item lies in
-  const int c0 = (first + before) / share, pieces = (first + last) / share - c0 + 1;
+  const int c0 = before / share, pieces = last / share - c0 + 1;
   if (pieces < 2) return;
   auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * p.rows + row % p.rows; };
   float M = -INFINITY, l = 0.f, acc[N];
@@ -984,7 +988,7 @@ Cut8 cut8(const TreeArgs& a, int dt, int sm_count) {
   const size_t held = 2 * size_t(c.ctas) * c.rows;
   c.part_bytes = align256(held * a.D * sizeof(float));
   c.ml_bytes = align256(held * sizeof(float2));
-  c.first_bytes = align256((size_t(a.B) + 1) * sizeof(int32_t));
+  c.first_bytes = align256((size_t(a.B) + 2) * sizeof(int32_t));
   c.bytes = c.part_bytes + c.ml_bytes + c.first_bytes + align256(c.ctas * sizeof(int32_t));
   return c;
 }

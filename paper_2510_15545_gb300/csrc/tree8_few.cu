@@ -82,8 +82,8 @@ struct Smem8 {
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[4], s_free[4];
   uint64_t p_full[2], o_done[2], item_full[2], o_free[2], q_full, q_empty, own_full, drained[2];
-  long long sums[kThreads / 32];      // places of the requests, by warps
-  int start_b, start_offset;          // where this CTA's places begin
+  int sums[kThreads / 32];            // places of the requests, by warps
+  int start_b, start_hk, start_offset;  // where this CTA's places begin
   int share;                          // and how many a CTA has
   uint32_t tmem;
   int end, stop;                      // the place behind this CTA's, and where it gave up
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
   bool ok = true;
   Place x;
   x.lead = 0;
-  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, shape, s.start_b, s.start_offset);
+  if (todo > 0 && warp >= kRowWarps) x = find_place(p.a, shape, s.start_b, s.start_hk, s.start_offset);
 
   if (warp > kRowWarps + kConvWarps + 1) {
     // ------------------------------------------------------------ copies

@@ -52,8 +52,8 @@ def _list(lens, n, Hq, Hkv, rows):
     group = Hq // Hkv
     tiles = lambda x: (x + 127) // 128  # noqa: E731
     places = []
-    for b, L in enumerate(lens):
-        for _ in range(Hkv):
+    for _ in range(Hkv):
+        for b, L in enumerate(lens):
             for row in range(0, n * group, rows):
                 end = (min(n * group, row + rows) - 1) // group + 1
                 places += [b] * (2 + tiles(L) + tiles(end))
