@@ -30,8 +30,10 @@ constexpr float kLn2 = 0.693147180559945f;
 constexpr float kSlack = 8.f;
 constexpr int kMinShare = 2;  // places of a CTA, where there are few
 // What an item costs beyond its tiles (queries, ancestors, output), in tiles: it
-// takes as many places in the list before its first tile.
-constexpr int kItemCost = 2;
+// takes as many places in the list before its first tile. (8500 cycles beside 1500 of a
+// tile of single tokens; with 2 places those took 273 us, the serving batch 188, for 266 and
+// 179; with 8 they take 263 and 179, but a single chain 18.5 for 16.5.)
+constexpr int kItemCost = 5;
 
 // mbar_wait in few instructions: the roles wait in some thirty places, and what they
 // do in between has to stay in the instruction caches.

@@ -56,7 +56,7 @@ def _list(lens, n, Hq, Hkv, rows):
         for b, L in enumerate(lens):
             for row in range(0, n * group, rows):
                 end = (min(n * group, row + rows) - 1) // group + 1
-                places += [b] * (2 + tiles(L) + tiles(end))
+                places += [b] * (5 + tiles(L) + tiles(end))
     ctas = torch.cuda.get_device_properties(0).multi_processor_count
     return places, max(2, -(-len(places) // ctas))
 
@@ -73,11 +73,12 @@ def test_requests_whose_keys_do_not_come(n, Hq, Hkv, D, dtype, rows, two):
         pytest.skip("needs a GPU")
     lens = [40000, 39000, 38500, 41000, 37777, 40001, 36000, 42000]
     places, share = _list(lens, n, Hq, Hkv, rows)
-    assert share >= 8
+    assert share >= 16
     for cta in range(3, len(places) // share):
         mine = places[cta * share:(cta + 1) * share]
-        # (two tiles at least before the next request begins, and one of that)
-        if (mine[0] != mine[-1] and mine.count(mine[0]) >= 5 and mine.count(mine[-1]) >= 5
+        # (two tiles at least before the next request begins, and two of that, each behind what
+        # an item costs)
+        if (mine[0] != mine[-1] and mine.count(mine[0]) >= 8 and mine.count(mine[-1]) >= 8
                 if two else mine[0] == mine[-1]):
             break
     else:
