@@ -272,7 +272,7 @@ tt_status tt_tree_attn(const tt_tree* tree, void* workspace, size_t workspace_by
 }
 
 size_t tt_tree8_workspace_bytes(const tt_tree* tree) {
-  return tree_sizes_ok(tree) ? tree8_workspace_bytes(tree_args(tree), tree->dtype, device_sms()) : 0;
+  return tree_sizes_ok(tree) ? tree8_workspace_bytes(tree_args(tree), device_sms()) : 0;
 }
 
 tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_scales* v_scale,
@@ -285,9 +285,9 @@ tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_
       (!pages8_ok(tree->k_cache, *k_scale) || !pages8_ok(tree->v_cache, *v_scale)))
     return TT_ERR_INVALID_ARG;
   TreeArgs a = tree_args(tree);
-  if (!workspace_ok(workspace, workspace_bytes, tree8_workspace_bytes(a, tree->dtype, device_sms())))
+  if (!workspace_ok(workspace, workspace_bytes, tree8_workspace_bytes(a, device_sms())))
     return TT_ERR_INVALID_ARG;
-  if (!tree8_fits(a, tree->dtype, device_sms())) return TT_ERR_UNSUPPORTED;
+  if (!tree8_fits(a, device_sms())) return TT_ERR_UNSUPPORTED;
   a.ws = static_cast<char*>(workspace);
   a.out = static_cast<char*>(out);
   a.lse = lse;

@@ -24,7 +24,7 @@
 // which the CTAs share evenly: lengths are known on the device alone. Items cut by a CTA's
 // end leave unnormalised pieces, which a second kernel joins.
 //
-// Two documents of 131,072 keys with 32 tokens each, 16 heads on 2: 85.5 us, 2200 cycles a
+// Two documents of 131,072 keys with 32 tokens each, 16 heads on 2: 82 us, 2200 cycles a
 // tile and CTA, most of them a row's way from its scores to its weights (780 of exponentials).
 // Four threads to a row took 109 us: its barriers cost more than its shares saved.
 //
@@ -965,17 +965,15 @@ struct Cut8 {
   int64_t pieces;  // of one item, about
   size_t part_bytes, ml_bytes, first_bytes, bytes;
 };
-Cut8 cut8(const TreeArgs& a, int dt, int sm_count) {
+Cut8 cut8(const TreeArgs& a, int sm_count) {
   Cut8 c;
   const int group = a.Hq / a.Hkv;
   const int64_t rows = int64_t(a.max_nodes) * group;
   // Few rows go to the kernel whose products have them as columns, which costs what they
   // cost: 64 caches of 8192 and 8 heads took, with that one and with this,
-  //   heads of 128, bf16:  158 and 211 us at 16 rows, 191 and 231 at 32, 237 and 252 at 48,
-  //                        259 and 256 at 64 (fp16: 245 and 243 at 40);
-  //   heads of 64:         137 and 163 us at 16, 174 and 174 at 32, 215 and 181 at 48.
-  const bool bf16_128 = a.D == 128 && dt == TT_BF16;
-  c.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 48 && bf16_128 ? 64 : kManyRows;
+  //   heads of 128: 128 and 172 us at 16 rows, 174 and 179 at 32, 218 and 189 at 48;
+  //   heads of 64:  117 and 146 us at 16, 148 and 150 at 32.
+  c.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kManyRows;
   const int64_t row_tiles = (rows + c.rows - 1) / c.rows;
   const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item
   const int64_t all = c.places = int64_t(std::min(
@@ -1070,19 +1068,17 @@ cudaError_t preload() {
 }
 }  // namespace
 
-size_t tree8_workspace_bytes(const TreeArgs& a, int dt, int sm_count) {
-  return cut8(a, dt, sm_count).bytes;
-}
+size_t tree8_workspace_bytes(const TreeArgs& a, int sm_count) { return cut8(a, sm_count).bytes; }
 
 // (places of the list, and blocks of the join, are 32-bit numbers)
-bool tree8_fits(const TreeArgs& a, int dt, int sm_count) {
-  return cut8(a, dt, sm_count).places <= INT32_MAX &&
+bool tree8_fits(const TreeArgs& a, int sm_count) {
+  return cut8(a, sm_count).places <= INT32_MAX &&
          double(a.B) * a.max_nodes * double(a.Hq) <= INT32_MAX;
 }
 
 cudaError_t launch_tree8(const TreeArgs& a, const TreeScales& sc, int dt, cudaStream_t stream,
                          int sm_count) {
-  const Cut8 c = cut8(a, dt, sm_count);
+  const Cut8 c = cut8(a, sm_count);
   Tree8Args p;
   std::memset(&p, 0, sizeof p);
   p.a = a;

@@ -2,7 +2,7 @@
 // query heads that share a key head).
 //
 // Keys take the rows of the matrix products and tokens the columns: scores S^T = K Q^T and
-// outputs O^T = V^T P^T, of 128 keys and 16, 32 or 64 columns, cost what the columns cost. A
+// outputs O^T = V^T P^T, of 128 keys and 16 or 32 columns, cost what the columns cost. A
 // thread then holds one key's scores of many tokens: its scale is one number, its mask one
 // bit. Only a row's maximum goes across threads, and it is asked for only where a score
 // passes the reference by 2^kSlack, which a vote tells; the sums of the weights stay with the
@@ -12,12 +12,12 @@
 // their scale goes to the weights, in units of the largest scale so far, so that fp16 holds
 // those of scales 2^-20 below it as well as the largest's.
 //
-// One CTA per SM: two warps copy, four convert, two issue products, eight or sixteen turn
-// scores into weights: half of them the even tiles and half the odd ones, each with
-// references, sums and an output of their own. 1.07 GB of caches for 256 single tokens take
-// 314 us, 3.4 TB/s: a fifth of it is items' beginnings and ends, and values are on their way
-// in three stages only. Of 36 rows what bounds it is how long a tile takes from its scores to
-// its weights, 12 instructions a score: 202 us for 64 requests of 9 tokens, 2.7 TB/s.
+// One CTA per SM: two warps copy, four convert, two issue products, eight turn scores into
+// weights: half of them the even tiles and half the odd ones, each with references, sums and
+// an output of their own. 1.07 GB of caches for 256 single tokens take 259 us, 4.2 TB/s: a
+// fifth of it is items' beginnings and ends. Of 32 rows (64 requests, caches up to 8192, 174
+// us) what bounds it is how long a tile takes from its scores to its weights, 12 instructions
+// a score.
 // The loops over the rows are rolled: unrolled, their code came from beyond the instruction
 // caches.
 #include <algorithm>
@@ -29,17 +29,12 @@ namespace tt {
 
 namespace {
 
-// Eight warps turn scores into weights, 32 keys each, for 64 rows sixteen: half of them
-// take the even tiles and half the odd ones, each with references, sums and an output of
-// their own. What a tile takes from its scores to its weights is mostly waiting, and so
-// two are on their way.
+// Eight warps turn scores into weights, 32 keys each: half of them take the even tiles and
+// half the odd ones, each with references, sums and an output of their own. What a tile takes
+// from its scores to its weights is mostly waiting, and so two are on their way.
 constexpr int kSets = 2;
-template <int R>
-struct Warps {
-  static constexpr int kSubs = R == 64 ? 2 : 1;  // fours of a set, which share the rows
-  static constexpr int kRow = 4 * kSets * kSubs, kRowThreads = kRow * 32;
-  static constexpr int kThreads = kRowThreads + kConvThreads + 128;  // of a CTA
-};
+constexpr int kRowWarps = 4 * kSets, kRowThreads = kRowWarps * 32;
+constexpr int kThreads = kRowThreads + kConvThreads + 128;
 // What the converting warps, which come to an item first, tell the others of it.
 struct Facts {
   int n_tree, rows, tile0, tile1, end, len, first, hk, at;  // at: the place of its first tile
@@ -52,9 +47,8 @@ struct Smem8 {
   static constexpr int kOut = 4 * R, kSums = kOut + kSets * R, kUsed = kSums + kSets * R;
   static constexpr int kColumns = kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
   // what 227 KB hold
-  static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : R == 64 && F16 ? 2 : 3;
-  static constexpr int kStagesV = D == 64 ? 6 : R == 64 ? 2 : 3;
-  static constexpr int kThreads = Warps<R>::kThreads;
+  static constexpr int kStagesK = D == 64 ? 6 : R == 16 ? 4 : 3;
+  static constexpr int kStagesV = D == 64 ? 6 : 3;
   char w[2][kTile * D * 2];           // values of 16 bits; a drafted tile's keys too
   char p[2][kTile * 128];             // weights, the rows of a key side by side
   char k[kStagesK][kTile * D];        // keys and values as they come
@@ -165,12 +159,10 @@ __device__ __noinline__ uint32_t tree_sees(const uint32_t* seen, const uint8_t* 
 }
 
 template <int D, int R, bool F16>
-__global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const __grid_constant__ Tree8Args p) {
+__global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_constant__ Tree8Args p) {
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
-  constexpr int kPieces = S::kPieces, kSubs = Warps<R>::kSubs;
-  constexpr int kRowWarps = Warps<R>::kRow, kRowThreads = Warps<R>::kRowThreads;
-  constexpr int kThreads = Warps<R>::kThreads;
+  constexpr int kPieces = S::kPieces;
   // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
   // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
   constexpr int kOwnCode = F16 ? 127 : 67;
@@ -198,14 +190,14 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
     for (int i = 0; i < 2; ++i) {
       mbar_init(&s.w_full[i], kConvThreads);
       mbar_init(&s.w_empty[i], 1);
-      mbar_init(&s.p_full[i], 128 * kSubs);
+      mbar_init(&s.p_full[i], 128);
       mbar_init(&s.o_done[i], 1);
       mbar_init(&s.item_full[i], kConvThreads);
       mbar_init(&s.o_free[i], kRowThreads);
     }
     for (int i = 0; i < 4; ++i) {
       mbar_init(&s.s_full[i], 1);
-      mbar_init(&s.s_free[i], 128 * kSubs);
+      mbar_init(&s.s_free[i], 128);
     }
     mbar_init(&s.q_full, kConvThreads);
     mbar_init(&s.q_empty, 1);
@@ -629,11 +621,10 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
       const bool bad = any_of(5, kRowThreads, !r.status && out_of_range(a, b, r, t, kRowThreads));
       if (t == 0) a.status[b] = r.status | (bad ? TT_REQ_ID_OUT_OF_RANGE : 0);
     }
-    const int quarter = warp & 3, four = warp >> 2, key = quarter * 32 + lane;
-    const int set = four / kSubs, sub = four % kSubs;
+    const int quarter = warp & 3, set = warp >> 2, key = quarter * 32 + lane;
     const uint32_t mine = tmem + (uint32_t(quarter * 32) << 16);  // this warp's lanes
     const uint32_t output = mine + S::kOut + set * R, my_sums = mine + S::kSums + set * R;
-    const int barrier = 1 + four;  // of its four warps
+    const int barrier = 1 + set;  // of its four warps
     float* const my_shift = s.shift[set];
     float* const my_fall = s.fall[set];
     char* const weights = s.p[set] + key * 128;
@@ -659,7 +650,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
       const bool whole = it.tile0 == 0 && it.tile1 == it.n_tree + cache_tiles(it.len);
       // sums of the weights, from nothing
 #pragma unroll 1
-      for (int c = sub; c < chunks; c += kSubs) {
+      for (int c = 0; c < chunks; ++c) {
         const uint32_t zero[8] = {};
         tmem_st8(my_sums + 8 * c, zero);
       }
@@ -718,7 +709,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
         // has none), and what that makes of the output.
         auto raise = [&] {
 #pragma unroll 1
-          for (int c = sub; c < chunks; c += kSubs) {
+          for (int c = 0; c < chunks; ++c) {
             uint32_t v[8];
             tmem_ld8(at + 8 * c, v);
             tmem_wait8(v);
@@ -737,9 +728,9 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
             if (lane < 8) s.part[set][quarter][8 * c + lane] = top;
           }
           sync_of(barrier, 128);
-          // (a thread to each of these warps' rows, as far as there are so many)
+          // (a thread to each row)
           bool none = false;
-          const int row = 8 * (sub + kSubs * (key / 8)) + key % 8;
+          const int row = key;
           if (row < it.rows) {
             const auto& part = s.part[set];
             const float top = fmaxf(fmaxf(part[0][row], part[1][row]), fmaxf(part[2][row], part[3][row]));
@@ -803,36 +794,25 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
               *reinterpret_cast<uint4*>(weights + ((c ^ (key & 7)) << 4)) =
                   make_uint4(out[0], out[1], out[2], out[3]);
             };
-            if constexpr (kSubs == 1) {
-              // (a chunk is fetched while the one before it is weighed)
-              uint32_t v0[8], l0[8], v1[8], l1[8];
-              fetch(0, v0, l0);
+            // (a chunk is fetched while the one before it is weighed)
+            uint32_t v0[8], l0[8], v1[8], l1[8];
+            fetch(0, v0, l0);
 #pragma unroll 1
-              for (int c = 0; c < chunks; c += 2) {
-                tmem_wait8(v0);
-                tmem_wait8(l0);
-                if (c + 1 < chunks) fetch(c + 1, v1, l1);
-                weigh(c, v0, l0);
-                if (c + 1 >= chunks) break;
-                tmem_wait8(v1);
-                tmem_wait8(l1);
-                if (c + 2 < chunks) fetch(c + 2, v0, l0);
-                weigh(c + 1, v1, l1);
-              }
-            } else {
-#pragma unroll 1
-              for (int c = sub; c < chunks; c += kSubs) {
-                uint32_t v[8], l[8];
-                fetch(c, v, l);
-                tmem_wait8(v);
-                tmem_wait8(l);
-                weigh(c, v, l);
-              }
+            for (int c = 0; c < chunks; c += 2) {
+              tmem_wait8(v0);
+              tmem_wait8(l0);
+              if (c + 1 < chunks) fetch(c + 1, v1, l1);
+              weigh(c, v0, l0);
+              if (c + 1 >= chunks) break;
+              tmem_wait8(v1);
+              tmem_wait8(l1);
+              if (c + 2 < chunks) fetch(c + 2, v0, l0);
+              weigh(c + 1, v1, l1);
             }
             pass = !early && any_of(barrier, 128, over > kSlack + kOffset) ? 2 : 3;
           } else {
 #pragma unroll 1
-            for (int c = sub; c < chunks; c += kSubs) {
+            for (int c = 0; c < chunks; ++c) {
               f32x2 z[4];
               uint32_t v[8], l[8];
               tmem_wait_st();
@@ -869,7 +849,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
           // (its last product is done: that of two tiles ago, for which this warp has waited)
           tc_fence_after();
 #pragma unroll 1
-          for (int c = sub; c < chunks; c += kSubs) {
+          for (int c = 0; c < chunks; ++c) {
             uint32_t v[8];
             tmem_ld8(output + 8 * c, v);
             tmem_wait8(v);
@@ -888,7 +868,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
       // the sums of all keys
       if (code) {
 #pragma unroll 1
-        for (int c = sub; c < chunks; c += kSubs) {
+        for (int c = 0; c < chunks; ++c) {
           uint32_t l[8];
           tmem_ld8(my_sums + 8 * c, l);
           tmem_wait8(l);
@@ -896,11 +876,11 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
 #pragma unroll
           for (int i = 0; i < 8; ++i) sums[i] = __uint_as_float(l[i]);
           const float sum = warp_sums(sums, lane);
-          if (c == sub) sync_of(barrier, 128);  // (done with s.part)
+          if (c == 0) sync_of(barrier, 128);  // (done with s.part)
           if (lane < 8) s.part[set][quarter][8 * c + lane] = sum;
         }
       }
-      if (sub == 0 && quarter == 0 && lane == 0) s.code[set] = code;
+      if (quarter == 0 && lane == 0) s.code[set] = code;
       sync_of(5, kRowThreads);
       if (t < it.rows) {
         // the sets' sums and outputs relative to the larger of their references
@@ -939,7 +919,7 @@ __global__ void __launch_bounds__(Warps<R>::kThreads, 1) tree8_few_kernel(const 
       tc_fence_after();
       if (D == 128 || quarter < 2) {
 #pragma unroll 1
-        for (int c = four; c < chunks; c += kSets * kSubs) {
+        for (int c = set; c < chunks; c += kSets) {
           float y[8] = {};
 #pragma unroll
           for (int k = 0; k < kSets; ++k) {
@@ -981,7 +961,7 @@ template <int D, int R, bool F16>
 cudaError_t launch(const Tree8Args& p, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(unsigned(p.ctas));
-  cfg.blockDim = dim3(Warps<R>::kThreads);
+  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = sizeof(Smem8<D, R, F16>) + 1024;
   cfg.stream = stream;
   return cudaLaunchKernelEx(&cfg, tree8_few_kernel<D, R, F16>, p);
@@ -1000,9 +980,6 @@ cudaError_t of_call(int D, int rows, bool f16, Go go) {
   auto type = [&](auto dim, auto r) {
     return f16 ? go(dim, r, std::true_type()) : go(dim, r, std::false_type());
   };
-  // (33 to 64 rows: heads of 128 in bf16 alone)
-  if (rows == 64)
-    return go(std::integral_constant<int, 128>(), std::integral_constant<int, 64>(), std::false_type());
   auto row = [&](auto dim) {
     return rows == 16 ? type(dim, std::integral_constant<int, 16>())
                       : type(dim, std::integral_constant<int, 32>());
@@ -1020,7 +997,7 @@ cudaError_t launch_tree8_few(const Tree8Args& p, int dt, cudaStream_t stream) {
 
 cudaError_t preload_tree8_few() {
   for (int D : {64, 128})
-    for (int rows : {16, 32, 64})
+    for (int rows : {16, 32})
       for (bool f16 : {false, true}) {
         const cudaError_t e = of_call(D, rows, f16, [](auto dim, auto r, auto f) {
           return preload<decltype(dim)::value, decltype(r)::value, decltype(f)::value>();

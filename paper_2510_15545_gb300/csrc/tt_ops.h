@@ -136,8 +136,8 @@ struct TreeScales {
   TreeScale k, v;
 };
 
-size_t tree8_workspace_bytes(const TreeArgs& args, int dt, int sm_count);
-bool tree8_fits(const TreeArgs& args, int dt, int sm_count);
+size_t tree8_workspace_bytes(const TreeArgs& args, int sm_count);
+bool tree8_fits(const TreeArgs& args, int sm_count);
 cudaError_t launch_tree8(const TreeArgs& args, const TreeScales& scales, int dt,
                          cudaStream_t stream, int sm_count);
 cudaError_t preload_tree8();
