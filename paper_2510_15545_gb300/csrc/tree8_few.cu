@@ -829,8 +829,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                   const float fall = my_fall[8 * c + 2 * i + k];
-                  l[2 * i + k] = __float_as_uint(
-                      fall > 0x1p-60f ? __uint_as_float(l[2 * i + k]) * fall : e[k]);
+                  const float sum = __uint_as_float(l[2 * i + k]);
+                  // (NaN stays: one of the scores so far is)
+                  l[2 * i + k] = __float_as_uint(fall > 0x1p-60f || sum != sum ? sum * fall : e[k]);
                 }
                 split(mul2(pair(e[0], e[1]), value2), lo, hi);
                 out[i] = F16 || cache ? pack_pair<TT_F16>(lo, hi) : pack_pair<TT_BF16>(lo, hi);

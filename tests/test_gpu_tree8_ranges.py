@@ -1,0 +1,115 @@
+"""tt_tree_attn over caches in 8 bits at the ends of its numbers: NaN under scores that
+jump, values far smaller than what scales them, and the largest ones.
+
+Tolerances. A score's error is that of the tests beside this one (fp32 products, pieces of
+queries). Weights of cached keys are fp16 numbers of a row's sum in units in which its
+largest is 2^7 or more: beyond 2^-11 of each they are off by 2^-25, so by 2^-32 of the
+largest, times the sizes of all values. Cached values are fp16 numbers in units of the
+largest scale so far: off by 2^-25 of it, and their mean by no more. Weights of drafted keys
+have the inputs' type (in fp16 off by 2^-32 of the largest, too), the output is rounded to it
+once (in fp16 to 2^-25 at least)."""
+import math
+
+import pytest
+import torch
+
+import paper_2510_15545_gb300 as tt
+from test_gpu_tree import ancestors
+from test_gpu_tree8 import E, H, call, hold, make8, power
+
+pytestmark = pytest.mark.gpu
+
+NAN = float("nan")
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("needs a GPU")
+    tt.load(build_if_missing=True)
+
+
+def where(c, b):
+    """Pages and slots of request b's cached keys, in order."""
+    page = c.k_cache.shape[1]
+    x = torch.arange(c.lens[b], device="cuda")
+    return c.table[b].long()[x // page], x % page
+
+
+def expected(c, b, scale, unit):
+    """Output, its error bound and lse of request b's nodes; values are held in units of
+    `unit`."""
+    Hkv, D = c.k.shape[1:]
+    G = c.q.shape[1] // Hkv
+    lo, n = sum(c.nodes[:b]), c.nodes[b]
+    at, slot = where(c, b)
+    number = lambda y, s: (y.view(torch.uint8)[at, slot].view(torch.float8_e4m3fn).double()  # noqa: E731
+                           * power(s[at, slot // 16].int())[..., None])
+    k = torch.cat([number(c.k_cache, c.ks), c.k[lo:lo + n].double()])
+    v = torch.cat([number(c.v_cache, c.vs), c.v[lo:lo + n].double()])
+    seen = torch.cat([torch.ones((n, len(at)), dtype=torch.bool),
+                      ancestors(n, None if c.parents is None else c.parents[b])], 1).cuda()
+    q = c.q[lo:lo + n].double().view(n, Hkv, G, D)
+    s = torch.einsum("nhgd,lhd->hgnl", q, k) * scale
+    es = torch.einsum("nhgd,lhd->hgnl", q.abs(), k.abs()) * 2.0 ** -20
+    es += torch.einsum("nhg,lh->hgnl", q.abs().amax(-1), k.abs().sum(-1)) * 2.0 ** -17
+    es = (es * scale).masked_fill(~seen, 0).amax(-1)
+    s = s.masked_fill(~seen, -math.inf)
+    lse = torch.logsumexp(s, -1)
+    p = torch.exp(s - lse[..., None])
+    u = 2.0 ** -8 if c.q.dtype == H else 2.0 ** -11
+    order = lambda y: y.permute(2, 0, 1, 3).reshape(n, Hkv * G, -1)  # noqa: E731
+    out = order(torch.einsum("hgnl,lhd->hgnd", p, v))
+    mean = order(torch.einsum("hgnl,lhd->hgnd", p, v.abs()))
+    every = torch.einsum("nl,lhd->hnd", seen.double(), v.abs()).permute(1, 0, 2).repeat_interleave(G, 1)
+    bound = (1.02 * u * (mean + out.abs()) + (2 * order(es[..., None]) + 2e-5) * mean
+             + 2.0 ** -32 * every + 2.0 ** -25 * unit)
+    if c.q.dtype == E:
+        bound = bound + 2.0 ** -25
+    flat = lambda y: y.permute(2, 0, 1).reshape(n, Hkv * G)  # noqa: E731
+    return out, bound, flat(lse), flat(es) + 1e-5
+
+
+def check(c, requests, unit, scale=None, **kw):
+    kw.setdefault("max_len", max(c.lens))
+    kw.setdefault("max_nodes", max(c.nodes))
+    g = call(c, scale=scale, **kw)
+    scale = c.q.shape[2] ** -0.5 if scale is None else scale
+    assert g["status"].tolist() == [0] * len(c.lens)
+    for b in requests:
+        lo, n = sum(c.nodes[:b]), c.nodes[b]
+        out, bound, lse, el = expected(c, b, scale, unit)
+        off = (g["out"][lo:lo + n].double() - out).abs() / bound
+        assert off.max() <= 1, (b, off.max())  # (NaN fails, too)
+        off = (g["lse"][lo:lo + n].double() - lse).abs() / el
+        assert off.max() <= 1, (b, "lse", off.max())
+    return g
+
+
+@pytest.mark.parametrize("n", [1, 9, 40])  # of few rows, and of many
+@pytest.mark.parametrize("D,dtype", [(64, H), (128, E)])
+@pytest.mark.parametrize("what", ["key", "scale", "drafted"])
+def test_rows_stay_nan_when_scores_jump(n, D, dtype, what):
+    """A NaN key comes early, scores that make what came before it nothing later: the row's
+    sum is NaN, not that of what came later."""
+    B, L = 150, 128 * 7
+    c = make8([L] * B, [n] * B, 2, 1, D, 64, dtype, seed=1, parents=None)
+    c.q.fill_(8.0)
+    keys = torch.zeros(c.k_cache.shape, device="cuda")
+    for b in range(B):
+        at, slot = where(c, b)
+        keys[at[128 * 5:], slot[128 * 5:]] = 8.0  # (scores of 8 * 8 * sqrt(D), base e)
+    c.k_cache, c.ks = hold(keys)
+    clean = call(c, max_len=L, max_nodes=n)
+    assert torch.isfinite(clean["out"]).all() and torch.isfinite(clean["lse"]).all()
+    if what == "drafted":
+        c.k[0::n] = NAN  # (every token's first ancestor)
+    for b in range(B if what != "drafted" else 0):
+        at, slot = where(c, b)
+        for x in (5, 128 + 7):  # (of tiles one after the other)
+            if what == "key":
+                c.k_cache.view(torch.uint8)[at[x], slot[x], 0, 3] = 0x7f
+            else:
+                c.ks[at[x], slot[x] // 16] = 255
+    g = call(c, max_len=L, max_nodes=n)
+    assert torch.isnan(g["out"]).all() and torch.isnan(g["lse"]).all()
