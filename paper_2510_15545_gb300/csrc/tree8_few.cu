@@ -114,7 +114,7 @@ __device__ __forceinline__ uint32_t idesc_mn(bool f16, int n) {
 }
 // The largest of a warp's numbers (NaN: none).
 __device__ __forceinline__ float warp_max(float x) {
-  const int i = x != x ? int(0x807fffff) : __float_as_int(x);  // (-inf)
+  const int i = x != x ? int(0xff800000) : __float_as_int(x);  // (-inf)
   const int top = __reduce_max_sync(0xffffffffu, i ^ ((i >> 31) & 0x7fffffff));
   return __int_as_float(top ^ ((top >> 31) & 0x7fffffff));
 }

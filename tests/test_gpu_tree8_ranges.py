@@ -113,3 +113,21 @@ def test_rows_stay_nan_when_scores_jump(n, D, dtype, what):
                 c.ks[at[x], slot[x] // 16] = 255
     g = call(c, max_len=L, max_nodes=n)
     assert torch.isnan(g["out"]).all() and torch.isnan(g["lse"]).all()
+
+
+@pytest.mark.parametrize("n", [1, 9, 40])
+def test_rows_of_nan_and_scores_far_below_zero(n):
+    """A NaN key beside keys whose scores are all negative."""
+    B, L = 150, 128 * 5
+    c = make8([L] * B, [n] * B, 2, 1, 64, 64, H, seed=2, parents=None)
+    c.q.fill_(8.0)
+    c.k.fill_(-8.0)
+    c.k_cache, c.ks = hold(torch.full(c.k_cache.shape, -8.0, device="cuda"))
+    check(c, range(0, B, 37), 1.0)
+    for b in range(0, B, 2):
+        at, slot = where(c, b)
+        c.k_cache.view(torch.uint8)[at[200], slot[200], 0, 3] = 0x7f
+    g = call(c, max_len=L, max_nodes=n)
+    bad = (torch.arange(B, device="cuda") % 2 == 0).repeat_interleave(n)
+    assert torch.isnan(g["out"][bad]).all() and torch.isnan(g["lse"][bad]).all()
+    assert torch.isfinite(g["out"][~bad]).all() and torch.isfinite(g["lse"][~bad]).all()
