@@ -107,16 +107,6 @@ __device__ __noinline__ void odd_values(const TreeArgs& a, const uint32_t* odd, 
     }
   }
 }
-// 2^-k as two fp16 numbers, k >= 0.
-__device__ __forceinline__ uint32_t half_power(int k) {
-  const uint32_t x = k <= 14 ? uint32_t(15 - k) << 10 : k <= 24 ? 1u << (24 - k) : 0u;
-  return x | x << 16;
-}
-__device__ __forceinline__ uint32_t half_mul2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 // 32 bytes to memory: one store where they are known to start on 32 bytes (pieces), two
 // of 16 for the caller's output.
 template <bool TWO>

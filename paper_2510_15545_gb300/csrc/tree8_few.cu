@@ -8,13 +8,14 @@
 // passes the reference by 2^kSlack, which a vote tells; the sums of the weights stay with the
 // keys, in tensor memory, until an item ends.
 //
-// Keys, queries and drafted tokens are multiplied as there. Values become fp16 as they are;
-// their scale goes to the weights, in units of the largest scale so far, so that fp16 holds
-// those of scales 2^-20 below it as well as the largest's.
+// Keys, queries, values and drafted tokens are multiplied as there. (The values' scales
+// could go to the weights instead, before those are rounded to fp16: single tokens took 259
+// us so for 266. But weights 2^-14 below the largest then come to nothing where the scales
+// are 2^-18 below theirs, and thousands of such may be what a row has.)
 //
 // One CTA per SM: two warps copy, four convert, two issue products, eight turn scores into
 // weights: half of them the even tiles and half the odd ones, each with references, sums and
-// an output of their own. 1.07 GB of caches for 256 single tokens take 259 us, 4.2 TB/s: a
+// an output of their own. 1.07 GB of caches for 256 single tokens take 266 us, 4.1 TB/s: a
 // fifth of it is items' beginnings and ends. Of 32 rows (64 requests, caches up to 8192, 174
 // us) what bounds it is how long a tile takes from its scores to its weights, 12 instructions
 // a score.
@@ -63,9 +64,10 @@ struct Smem8 {
   uint8_t token[2][R];                // of a row, from the item's first
   Facts facts[2];
   int16_t up[TT_MAX_TREE];            // parents, -1 for roots
-  float k_scale[kScaleRing][kGroups], v_scale[kScaleRing][kGroups];
+  float k_scale[kScaleRing][kGroups];
+  alignas(16) uint32_t v_scale[kScaleRing][kGroups];  // two fp16 numbers, of the tile's unit
   uint32_t left_out[2][kScaleRing];   // groups whose page is out of range: keys, values
-  int top_code[kScaleRing];           // the largest of the values' scales
+  int unit[kScaleRing];               // largest scale of the item's values so far
   alignas(16) float own_factor[8];    // the factor of drafted keys
   alignas(16) float shift[kSets][R];  // what is added to log2 scores
   alignas(16) float fall[kSets][R];   // a reference's last change
@@ -234,12 +236,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
     struct Batch {
       int hk, page, in_page;  // of the lane's slots
       int tiles;              // 0: no more
+      int unit;               // of values, where an item begins, else -1
       uint32_t code;
     };
     int j = 0, j1 = 0, used = 0;
     bool open = false;
     auto next = [&]() {
-      Batch y{0, -1, 0, 0, 0};
+      Batch y{0, -1, 0, 0, -1, 0};
       for (;;) {
         if (!open) {
           if (todo <= x.lead) return y;
@@ -248,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           j = max(0, it.tile0 - it.n_tree);
           j1 = it.tile1 - it.n_tree;
           used = it.tile1 - it.tile0;
+          y.unit = it.tile0 < it.n_tree ? kOwnCode : 1;
           open = true;
         }
         if (j < j1) break;
@@ -267,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
     auto usable = [&](int page) { return page >= 0 && page < a.n_pages; };
     Batch one, two;
     one.tiles = two.tiles = 0;
-    int n = 0, st = 0;
+    int n = 0, st = 0, unit = 1;
     uint32_t parity = 1;
 #pragma unroll 1
     for (int k = 0; ok && (k < 2 || one.tiles); ++k) {
@@ -282,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
       const bool begins = mine && lane % kGroups * TT_SCALE_SLOTS % p.box == 0;
       const unsigned int lost = __ballot_sync(0xffffffffu, !mine);
       const unsigned int boxes = __ballot_sync(0xffffffffu, begins);
-      const float scale = e8m0(c.code);
+      if (c.unit > 0) unit = c.unit;
       int top = c.code != 255 ? int(c.code) : 0;
 #pragma unroll
       for (int o = 1; o < kGroups; o <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
@@ -295,14 +299,19 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
         // (The scales in this place are of kScaleRing tiles ago, which is further back than
         // the stages and the tiles on their way behind them reach.)
         const int ring = n % kScaleRing;
+        unit = max(unit, __shfl_sync(0xffffffffu, top, kGroups * i));
         if (lane / kGroups == i) {
-          (values ? s.v_scale : s.k_scale)[ring][lane % kGroups] = scale;
-          if (lane % kGroups == 0) {
-            s.left_out[values][ring] = lost >> (kGroups * i) & 0xff;
-            if (values) s.top_code[ring] = top;
-            mbar_arrive_expect_tx(&full[st], __popc(boxes >> (kGroups * i) & 0xff) * p.box * D);
-          }
+          if (values)
+            s.v_scale[ring][lane % kGroups] = c.code == 255 ? 0x7e007e00u : half_power(unit - int(c.code));
+          else
+            s.k_scale[ring][lane % kGroups] = e8m0(c.code);
         }
+        if (lane == 0) {
+          s.left_out[values][ring] = lost >> (kGroups * i) & 0xff;
+          if (values) s.unit[ring] = unit;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive_expect_tx(&full[st], __popc(boxes >> (kGroups * i) & 0xff) * p.box * D);
         __syncwarp();
         if (begins && lane / kGroups == i)
           tma_load_4d(smem_u32(dst) + st * (kTile * D) + lane % kGroups * TT_SCALE_SLOTS * D, map,
@@ -519,20 +528,29 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           const int u = ct % 8, key0 = ct / 8;  // (its keys are 16 apart)
           const char* const from = s.v[st] + key0 * D + u * 8;
           char* const to = s.w[w & 1] + swizzled16(key0, u);
-          auto convert = [](const uint2& in) {
-            return make_uint4(e4m3x2_to_f16x2(in.x & 0xffff), e4m3x2_to_f16x2(in.x >> 16),
-                              e4m3x2_to_f16x2(in.y & 0xffff), e4m3x2_to_f16x2(in.y >> 16));
+          auto convert = [](const uint2& in, uint32_t scale) {
+            return make_uint4(half_mul2(e4m3x2_to_f16x2(in.x & 0xffff), scale),
+                              half_mul2(e4m3x2_to_f16x2(in.x >> 16), scale),
+                              half_mul2(e4m3x2_to_f16x2(in.y & 0xffff), scale),
+                              half_mul2(e4m3x2_to_f16x2(in.y >> 16), scale));
           };
+          // (its k-th key is one of the k-th 16 slots)
+          const uint32_t* const scales = s.v_scale[ring];
           if (keys == kTile && lost == 0) {
+            // Four keys' halves at a time, rolled: single tokens took 301 us with all
+            // unrolled, 268 with eight at a time, 266 with four.
+            const uint4* const fours = reinterpret_cast<const uint4*>(scales);
+#pragma unroll 1
+            for (int i = 0; i < 2 * kPairs; ++i) {
+              const char* const from4 = from + (i & 1) * 64 * D + (i >> 1) * 64;
+              char* const to4 = to + (i & 1) * 8192 + (i >> 1) * kBlock;
+              const uint4 f = fours[i & 1];
+              const uint32_t by[4] = {f.x, f.y, f.z, f.w};
+              uint2 in[4];
 #pragma unroll
-            for (int h = 0; h < kPairs; ++h) {
-              uint2 in[kEach];
+              for (int k = 0; k < 4; ++k) in[k] = *reinterpret_cast<const uint2*>(from4 + k * 16 * D);
 #pragma unroll
-              for (int k = 0; k < kEach; ++k)
-                in[k] = *reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64);
-#pragma unroll
-              for (int k = 0; k < kEach; ++k)
-                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in[k]);
+              for (int k = 0; k < 4; ++k) *reinterpret_cast<uint4*>(to4 + k * 2048) = convert(in[k], by[k]);
             }
           } else {
 #pragma unroll 1
@@ -541,9 +559,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
               const bool there = key < keys && !(lost >> (key / TT_SCALE_SLOTS) & 1);
 #pragma unroll
               for (int h = 0; h < kPairs; ++h) {
-                uint2 in = make_uint2(0, 0);
-                if (there) in = *reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64);
-                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = convert(in);
+                uint4 out = make_uint4(0, 0, 0, 0);
+                if (there) out = convert(*reinterpret_cast<const uint2*>(from + k * 16 * D + h * 64), scales[k]);
+                *reinterpret_cast<uint4*>(to + h * kBlock + k * 2048) = out;
               }
             }
           }
@@ -666,14 +684,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
         }
         const bool first = code == 0;
         bool there = key < tile_keys(j, it.n_tree, it.end, it.len);
-        float scale = 1.f, value = 1.f;
-        int top_code = kOwnCode;
+        float scale = 1.f;
+        int unit = kOwnCode;
         if (cache) {
           const int e = ct % kScaleRing;
           wait_for(&s.scale_full[e], (ct / kScaleRing) & 1);
           scale = s.k_scale[e][key / TT_SCALE_SLOTS];
-          value = s.v_scale[e][key / TT_SCALE_SLOTS];
-          top_code = max(1, s.top_code[e]);
+          unit = s.unit[e];
           there = there && !(s.left_out[0][e] >> (key / TT_SCALE_SLOTS) & 1);
           ++ct;
         }
@@ -746,14 +763,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           }
           unset = any_of(barrier, 128, none);
         };
-        // What the values' scale makes of weights is in units of the largest scale so far;
-        // when that rises the output falls.
+        // Values are in units of the largest scale so far; when that rises the output falls.
         float output_fall = 1.f;
-        if (top_code > code) {
-          output_fall = code > 0 ? e8m0(code) * e8m0_inverse(top_code) : 0.f;
-          code = top_code;
+        if (unit > code) {
+          output_fall = code > 0 ? e8m0(code) * e8m0_inverse(unit) : 0.f;
+          code = unit;
         }
-        value *= e8m0_inverse(code);
+        const float value = cache ? 1.f : e8m0_inverse(code);
         const f32x2 value2 = pair(value, value);
         const bool early = unset;
         // (the product of two tiles ago is done with the weights' place)

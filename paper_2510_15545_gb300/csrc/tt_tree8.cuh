@@ -288,6 +288,16 @@ __device__ __forceinline__ void in_pieces(const uint4& q, float by, Put put) {
     put(piece, make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16));
   }
 }
+// 2^-k as two fp16 numbers, k >= 0.
+__device__ __forceinline__ uint32_t half_power(int k) {
+  const uint32_t x = k <= 14 ? uint32_t(15 - k) << 10 : k <= 24 ? 1u << (24 - k) : 0u;
+  return x | x << 16;
+}
+__device__ __forceinline__ uint32_t half_mul2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // What a CTA finds of the list: it adds up the requests' places of one head, each thread those
 // of a run of them, and the one whose run holds the CTA's first place tells the request.
 // Returns the CTA's places. (Every thread comes; a barrier behind it makes s.start_* known.)

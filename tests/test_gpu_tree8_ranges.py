@@ -131,3 +131,50 @@ def test_rows_of_nan_and_scores_far_below_zero(n):
     bad = (torch.arange(B, device="cuda") % 2 == 0).repeat_interleave(n)
     assert torch.isnan(g["out"][bad]).all() and torch.isnan(g["lse"][bad]).all()
     assert torch.isfinite(g["out"][~bad]).all() and torch.isfinite(g["lse"][~bad]).all()
+
+
+def strong_and_weak(c, D, lift):
+    """Keys: one in each of the first four tiles whose weight is e^lift of all others'."""
+    c.q.fill_(1.0)
+    c.k.fill_(0.0)
+    keys = torch.zeros(c.k_cache.shape, device="cuda")
+    for b in range(len(c.lens)):
+        at, slot = where(c, b)
+        for x in range(3, 512, 128):
+            keys[at[x], slot[x]] = lift / math.sqrt(D)
+    c.k_cache, c.ks = hold(keys)
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+@pytest.mark.parametrize("D,dtype", [(64, E), (128, E), (64, H)])
+def test_small_values_of_many_weak_keys(n, D, dtype):
+    """Thousands of keys whose weights are e^-10 of the largest, with values far below
+    what the drafted ones' may be: together they count."""
+    B, L = 304, 4096 + 77
+    c = make8([L] * B, [n] * B, 2, 1, D, 64, dtype, seed=3, parents=None)
+    strong_and_weak(c, D, 10.0)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    values = torch.randn(c.v_cache.shape, generator=gen, device="cuda").abs_().mul_(2.0 ** -11)
+    c.v_cache, c.vs = hold(values)
+    c.v.mul_(2.0 ** -11)
+    check(c, (0, 1, 150, 303), 1.0 if dtype == E else 2.0 ** -17)
+
+
+@pytest.mark.parametrize("n", [1, 8, 40])
+@pytest.mark.parametrize("dtype", [H, E])
+def test_scales_far_apart(n, dtype):
+    """Values of 1 in keys that do not count beside values of 2^-14 in those that do."""
+    B, L, D = 304, 4096 + 77, 64
+    c = make8([L] * B, [n] * B, 2, 1, D, 64, dtype, seed=4, parents=None)
+    strong_and_weak(c, D, 10.0)
+    keys, values = c.numbers()
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    values = torch.randn(c.v_cache.shape, generator=gen, device="cuda").abs_().mul_(2.0 ** -14)
+    for b in range(B):
+        at, slot = where(c, b)
+        keys[at[16:32], slot[16:32]] = -8.0  # (64 below the weak ones)
+        values[at[16:32], slot[16:32]] = 1.0
+    c.k_cache, c.ks = hold(keys)
+    c.v_cache, c.vs = hold(values)
+    c.v.mul_(2.0 ** -14)
+    check(c, (0, 1, 150, 303), 1.0 if dtype == E else 2.0 ** -8)
