@@ -22,7 +22,7 @@
 // product with values are under way: tensor memory holds two tiles' scores, two tiles'
 // weights and the output. Tiles of all requests, key heads and 128 rows form one list,
 // which the CTAs share evenly: lengths are known on the device alone. Items cut by a CTA's
-// end leave unnormalised pieces, which a second kernel joins.
+// end leave pieces, each with its sum and maximum, which a second kernel joins.
 //
 // Two documents of 131,072 keys with 32 tokens each, 16 heads on 2: 82 us, 2200 cycles a
 // tile and CTA, most of them a row's way from its scores to its weights (780 of exponentials).
@@ -781,7 +781,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
                                        token * p.group
                                  : (2 * int64_t(blockIdx.x) + (it.tile0 == 0)) * kRows + row;
         const float unit = e8m0(code);
-        const float by = whole ? (l > 0.f || l != l ? unit / l : 0.f) : unit;
+        const float by = l > 0.f || l != l ? unit / l : 0.f;
 #pragma unroll 1
         for (int c = half * (D / 2); c < (half + 1) * (D / 2); c += 32) {
           uint32_t v[32];
@@ -839,7 +839,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
 }
 
 // Joins the pieces of every row whose item was cut: with M the largest of their
-// references, out = sum 2^(m - M) o / sum 2^(m - M) l. A CTA takes a row; its warps take
+// references, out = sum 2^(m - M) l o / sum 2^(m - M) l. A CTA takes a row; its warps take
 // the pieces in turn, the loads of eight before the first is added. It also tells the
 // requests that lost places to a CTA that gave up.
 constexpr int kJoinWarps = 4, kFewPieces = 16;
@@ -884,11 +884,13 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
   const int c0 = before / share, pieces = last / share - c0 + 1;
   if (pieces < 2) return;
   auto place = [&](int k) { return (2 * (int64_t(c0) + k) + (k == 0)) * p.rows + row % p.rows; };
+  // (outputs are added up times 2^-46 l, which is below 1: sums are weights of up to 2^15
+  // for fewer than 2^31 keys)
+  constexpr float kBelowOne = 0x1p-46f;
   float M = -INFINITY, l = 0.f, acc[N];
 #pragma unroll
   for (int c = 0; c < N; ++c) acc[c] = 0.f;
-  auto add = [&](float l_more, const Vec& o, float f) {
-    l = fmaf(l_more, f, l);
+  auto add = [&](const Vec& o, float f) {
     acc[0] = fmaf(o.x, f, acc[0]);
     acc[1] = fmaf(o.y, f, acc[1]);
     if constexpr (N == 4) {
@@ -916,9 +918,12 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
     // (a piece without a reference: of NaN, or of nothing, which adds 0)
 #pragma unroll
     for (int c = 0; c < C; ++c)
-      if (k0 + c * W < pieces)
-        add(ml[c].y, o[c],
-            ml[c].x == -INFINITY ? (ml[c].y != ml[c].y ? 1.f : 0.f) : ex2_approx(ml[c].x - top));
+      if (k0 + c * W < pieces) {
+        const float part = ml[c].x == -INFINITY ? (ml[c].y != ml[c].y ? ml[c].y : 0.f)
+                                                : ml[c].y * ex2_approx(ml[c].x - top);
+        l += part;
+        add(o[c], part * kBelowOne);
+      }
   }
   if constexpr (!FEW) {
 #pragma unroll
@@ -934,10 +939,11 @@ __global__ void __launch_bounds__(kJoinWarps * 32)
     for (int w = 0; w < W; ++w) {
       const float f = s_ml[w].x == -INFINITY ? (s_ml[w].y != s_ml[w].y ? 1.f : 0.f)
                                              : ex2_approx(s_ml[w].x - M);
-      add(s_ml[w].y, reinterpret_cast<const Vec*>(s_acc[w])[lane], f);
+      l = fmaf(s_ml[w].y, f, l);
+      add(reinterpret_cast<const Vec*>(s_acc[w])[lane], f);
     }
   }
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;
+  const float inv = l > 0.f || l != l ? 1.f / (l * kBelowOne) : 0.f;
   const int64_t to = (int64_t(r.first) + i) * a.Hq + h;
   uint32_t* out = reinterpret_cast<uint32_t*>(a.out + to * D * 2) + lane * (N / 2);
   out[0] = pack_pair<DT>(acc[0] * inv, acc[1] * inv);

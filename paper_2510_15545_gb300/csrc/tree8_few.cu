@@ -916,7 +916,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           }
         }
         const float m2 = top == -INFINITY ? -INFINITY : top - kOffset;
-        const float inverse = whole ? (all > 0.f || all != all ? 1.f / all : 0.f) : 1.f;
+        const float inverse = all > 0.f || all != all ? 1.f / all : 0.f;
 #pragma unroll
         for (int k = 0; k < kSets; ++k)
           s.share_of[k][t] = f[k] * inverse * (s.code[k] ? e8m0(s.code[k]) : 0.f);

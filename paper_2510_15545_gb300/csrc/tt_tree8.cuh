@@ -59,7 +59,8 @@ struct Tree8Args {
   int slots_inner;    // the cache maps' second dimension is the slot, the third the head
   // pieces: CTA c leaves that of an item that began before its tiles at 2 c, that
   // of one that begins in them at 2 c + 1
-  float* part;        // [2 ctas * R * D] outputs, not normalised
+  float* part;        // [2 ctas * R * D] outputs, each over its piece's own sum (before that
+                      // is taken out, means near the largest number would pass it)
   float2* part_ml;    // [2 ctas * R] their reference maximum (log2) and sum
   int32_t* first;     // [B + 2] a head's places before each request's, the places per CTA,
                       // the places of a head

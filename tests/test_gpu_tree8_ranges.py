@@ -178,3 +178,17 @@ def test_scales_far_apart(n, dtype):
     c.v_cache, c.vs = hold(values)
     c.v.mul_(2.0 ** -14)
     check(c, (0, 1, 150, 303), 1.0 if dtype == E else 2.0 ** -8)
+
+
+@pytest.mark.parametrize("n", [1, 3, 60])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("B,L", [(1, 20001), (3, 3000), (2, 130), (200, 700)])
+def test_the_largest_values_of_bf16(n, D, B, L):
+    """Cached values up to the type's largest, in items that are cut and in whole ones."""
+    c = make8([L] * B, [n] * B, 4, 2, D, 16, H, seed=5)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    values = torch.rand(c.v_cache.shape, generator=gen, device="cuda").double() * 2 - 1
+    values.sign_().mul_(1.875 * 2.0 ** 127)
+    values[..., ::2] = values[..., ::2].abs()  # (means near the largest as well)
+    c.v_cache, c.vs = hold(values)
+    check(c, range(0, B, 67), 2.0 ** 120)
