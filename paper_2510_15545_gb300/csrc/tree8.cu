@@ -71,6 +71,7 @@ struct Smem8 {
   float factor[2][kRows];             // a row's pieces times it and a key's scale: log2 scores
   uint32_t odd[2][kWords];            // drafted tokens with a value that is not finite
   Facts facts[2];
+  int own_code[2][kOwnTiles];         // the unit that a drafted tile's values need
   // of the tiles under way
   alignas(16) float k_scale[kScaleRing][kGroups];
   uint32_t v_scale[kScaleRing][kGroups];  // two fp16 numbers, of the tile's unit
@@ -126,9 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
   using S = Smem8<D, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
   constexpr int kPieces = S::kPieces;
-  // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
-  // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
-  constexpr int kOwnCode = F16 ? 127 : 67;
+  constexpr int kOwnCode = own_code(F16);
   constexpr int kBlock = kTile * 128;         // distance of the 64-element blocks of a 16-bit tile
   constexpr float kOffset = 7.f;              // fp16 weights: away from its small end
   extern __shared__ char raw[];
@@ -424,6 +423,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
       if (ct == 0)
         s.facts[side] = Facts{it.n_tree, it.rows, it.tile0, it.tile1, it.end,
                               x.r.len,   x.r.first, x.hk,   row0,     s.end - todo};
+      if (ct < kOwnTiles) s.own_code[side][ct] = kOwnCode;
       if (ct < kWords) s.odd[side][ct] = 0;
       if (it.tile0 < it.n_tree) {
         // (the parents in the place of the values to come, the ancestors once rows are done
@@ -544,6 +544,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           // Drafted tokens: keys as they are, then values without what is not finite (a
           // token outside its branch would get NaN from it; its own gets it at the end).
           const int base = j * kTile;
+          uint32_t top = 0;  // of even and odd elements of values, the largest sizes' bits
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
@@ -556,6 +557,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
               if (key < keys) {
                 o = *reinterpret_cast<const uint4*>(
                     from + ((int64_t(x.r.first) + base + key) * ts + x.hk * hs + u * 8) * 2);
+                // (values are looked at beside the keys: with the scores rows know their unit)
+                if (!F16 && kv == 0) {
+                  const uint4 y = *reinterpret_cast<const uint4*>(
+                      a.v + ((int64_t(x.r.first) + base + key) * a.v_token + x.hk * a.v_head + u * 8) * 2);
+                  top = __vmaxu2(__vmaxu2(__vmaxu2(top, y.x & 0x7fff7fffu), y.y & 0x7fff7fffu),
+                                 __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu));
+                }
                 if (kv) {
                   constexpr uint32_t kExp = F16 ? 0x7c00 : 0x7f80;
                   bool odd = false;
@@ -579,6 +587,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
               *reinterpret_cast<uint4*>(s.w[w & 1] + (u / 8) * kBlock + swizzled16(key, u % 8)) = o;
             }
             if (kv == 0) {
+              if (!F16 && own_code_for(max(top & 0xffffu, top >> 16)) > kOwnCode)
+                large_values<D>(a, x.r.first + base, x.hk, ct, keys, &s.own_code[side][j]);
               fence_proxy_async();
               arrive(&s.w_full[w & 1]);
               arrive(&s.own_full);
@@ -667,6 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           ++ct;
         } else {
           f[0] = f[1] = f[2] = f[3] = p.scale2;
+          if (!F16) unit = s.own_code[side][j];
         }
         uint32_t v[2][32];
         float high = -INFINITY;
@@ -745,6 +756,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           else
             weigh(std::true_type());
           l += sum_pair(sum2);
+          // (in the unit that large drafted values need)
+          if constexpr (!F16)
+            if (cache && unit < code) {
+              const uint32_t by = half_power(code - unit);
+#pragma unroll
+              for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[h][i] = half_mul2(v[h][i], by);
+            }
         }
         if (some) {
           const uint32_t to = mine + S::kWeights + (n & 1) * (kTile / 2) + 32 * half;

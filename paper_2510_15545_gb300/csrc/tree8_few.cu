@@ -15,7 +15,7 @@
 //
 // One CTA per SM: two warps copy, four convert, two issue products, eight turn scores into
 // weights: half of them the even tiles and half the odd ones, each with references, sums and
-// an output of their own. 1.07 GB of caches for 256 single tokens take 266 us, 4.1 TB/s: a
+// an output of their own. 1.07 GB of caches for 256 single tokens take 272 us, 4.0 TB/s: a
 // fifth of it is items' beginnings and ends. Of 32 rows (64 requests, caches up to 8192, 174
 // us) what bounds it is how long a tile takes from its scores to its weights, 12 instructions
 // a score.
@@ -63,6 +63,7 @@ struct Smem8 {
   int64_t row_to[2][R];               // row of the output, or of the CTA's pieces
   uint8_t token[2][R];                // of a row, from the item's first
   Facts facts[2];
+  int own_code[2][kOwnTiles];         // the unit that a drafted tile's values need
   int16_t up[TT_MAX_TREE];            // parents, -1 for roots
   float k_scale[kScaleRing][kGroups];
   alignas(16) uint32_t v_scale[kScaleRing][kGroups];  // two fp16 numbers, of the tile's unit
@@ -165,9 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
   using S = Smem8<D, R, F16>;
   constexpr int DT = F16 ? TT_F16 : TT_BF16;
   constexpr int kPieces = S::kPieces;
-  // Drafted values have no scale, 2^0, which their weights in the inputs' type take: fp16
-  // holds them beside scales of 2^0 or more, bf16 beside any that are not below 2^-60.
-  constexpr int kOwnCode = F16 ? 127 : 67;
+  constexpr int kOwnCode = own_code(F16);
   constexpr int kBlock = kTile * 128;         // distance of the 64-element blocks of a 16-bit tile
   constexpr float kOffset = 7.f;              // fp16 weights: away from its small end
   extern __shared__ char raw[];
@@ -198,7 +197,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
       mbar_init(&s.o_free[i], kRowThreads);
     }
     for (int i = 0; i < 4; ++i) {
-      mbar_init(&s.s_full[i], 1);
+      mbar_init(&s.s_full[i], 2);
       mbar_init(&s.s_free[i], 128);
     }
     mbar_init(&s.q_full, kConvThreads);
@@ -362,6 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
                   umma8_ss(to, kd + st * kKStep + 2 * c, qd + q * (R * D / 16) + 2 * c, idesc_e4m3(R),
                            q > 0 || c > 0);
               umma_commit(&s.s_full[buf]);
+              mbar_arrive(&s.s_full[buf]);
               umma_commit(&s.k_empty[st]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
             }
@@ -381,6 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
                 umma_ss(to, wk + (w & 1) * kWStep + (c / 4) * (kBlock / 16) + (c % 4) * 2,
                         od + (c / 4) * (R * 128 / 16) + (c % 4) * 2, umma_idesc(F16, R, false), c > 0);
               umma_commit(&s.s_full[buf]);
+              mbar_arrive(&s.s_full[buf]);
               umma_commit(&s.w_empty[w & 1]);
               if (j + 1 == it.tile1) umma_commit(&s.q_empty);
             }
@@ -455,6 +456,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
       if (ct == 0)
         s.facts[side] = Facts{it.n_tree, it.rows, it.tile0, it.tile1, it.end,
                               x.r.len,   x.r.first, x.hk,   s.end - todo};
+      if (ct < kOwnTiles) s.own_code[side][ct] = kOwnCode;
       if (ct < R) {
         const int token = (row0 + ct) / p.group;
         s.token[side][ct] = uint8_t(token - token0);
@@ -575,6 +577,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           // Drafted tokens: keys as they are, then values without what is not finite (a
           // token outside its branch would get NaN from it; its own gets it at the end).
           const int base = j * kTile;
+          uint32_t top = 0;  // of even and odd elements of values, the largest sizes' bits
 #pragma unroll 1
           for (int kv = 0; kv < 2; ++kv) {
             if (!wait_for(&s.w_empty[w & 1], ((w >> 1) & 1) ^ 1)) break;
@@ -587,6 +590,13 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
               if (key < keys) {
                 o = *reinterpret_cast<const uint4*>(
                     from + ((int64_t(x.r.first) + base + key) * ts + x.hk * hs + u * 8) * 2);
+                // (values are looked at beside the keys: with the scores rows know their unit)
+                if (!F16 && kv == 0) {
+                  const uint4 y = *reinterpret_cast<const uint4*>(
+                      a.v + ((int64_t(x.r.first) + base + key) * a.v_token + x.hk * a.v_head + u * 8) * 2);
+                  top = __vmaxu2(__vmaxu2(__vmaxu2(top, y.x & 0x7fff7fffu), y.y & 0x7fff7fffu),
+                                 __vmaxu2(y.z & 0x7fff7fffu, y.w & 0x7fff7fffu));
+                }
                 if (kv) {
                   constexpr uint32_t kExp = F16 ? 0x7c00 : 0x7f80;
                   bool odd = false;
@@ -610,6 +620,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
               *reinterpret_cast<uint4*>(s.w[w & 1] + (u / 8) * kBlock + swizzled16(key, u % 8)) = o;
             }
             if (kv == 0) {
+              if (!F16 && own_code_for(max(top & 0xffffu, top >> 16)) > kOwnCode)
+                large_values<D>(a, x.r.first + base, x.hk, ct, keys, &s.own_code[side][j]);
               fence_proxy_async();
               mbar_arrive(&s.w_full[w & 1]);
               mbar_arrive(&s.own_full);
@@ -695,6 +707,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           ++ct;
         }
         wait_for(&s.s_full[n & 3], (n >> 2) & 1);
+        // (known before the scores' product was issued)
+        if (!F16 && j < it.n_tree) unit = s.own_code[side][j];
         tc_fence_after();
         const uint32_t at = mine + (n & 3) * R;
         const f32x2 scale2 = pair(scale, scale);
@@ -764,12 +778,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           unset = any_of(barrier, 128, none);
         };
         // Values are in units of the largest scale so far; when that rises the output falls.
+        // (Where large drafted values need a larger unit, the weights of cached keys take what
+        // is between.)
         float output_fall = 1.f;
         if (unit > code) {
           output_fall = code > 0 ? e8m0(code) * e8m0_inverse(unit) : 0.f;
           code = unit;
         }
-        const float value = cache ? 1.f : e8m0_inverse(code);
+        const float value = __uint_as_float(max(0, 127 + (cache ? unit : 127) - code) << 23);
         const f32x2 value2 = pair(value, value);
         const bool early = unset;
         // (the product of two tiles ago is done with the weights' place)

@@ -21,6 +21,7 @@ constexpr int kTile = 128;                     // keys of a tile
 constexpr int kConvWarps = 4, kConvThreads = kConvWarps * 32;  // that convert values
 constexpr int kManyRows = 128;                 // of an item of the kernel for many
 constexpr int kWords = TT_MAX_TREE / 32;
+constexpr int kOwnTiles = TT_MAX_TREE / kTile;  // of drafted tokens, of an item
 constexpr int kGroups = kTile / TT_SCALE_SLOTS;  // scales of a tile
 constexpr int kScaleRing = 16;                   // tiles' scales that are kept
 constexpr int kBatch = 4;                        // tiles whose pages are asked for together
@@ -265,6 +266,35 @@ __device__ __forceinline__ float largest(const uint4& q, float top) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
   return top;
+}
+// The unit (as a scale's byte) of sums that hold drafted values. Their weights have the
+// inputs' type, and take it: fp16 holds them beside scales of 2^0 or more, bf16 beside any that
+// are not below 2^-60. In that unit weights of up to 2^15 for 2^9 drafted tokens stay within
+// fp32 with values below 2^43; larger ones need a unit of 2^-102 times their power of two. So
+// the converting warps look at a drafted tile's values beside its keys: rows know the unit with
+// the scores (single tokens 272 us for 266, a serving batch 185 for 180; with the rows waiting
+// for the values that are fetched behind the keys, 295 and 195).
+__host__ __device__ constexpr int own_code(bool f16) { return f16 ? 127 : 67; }
+// (of the bits of the largest, a bf16 number)
+__device__ __forceinline__ int own_code_for(uint32_t top) { return int(top >> 7) - 102; }
+// Where a tile of drafted tokens has larger ones: the unit that the finite ones of a
+// converting thread's vectors of 8 need.
+template <int D>
+static __device__ __noinline__ void large_values(const TreeArgs& a, int first, int hk, int thread, int keys,
+                                                 int* code) {
+  constexpr int kUnits = D / 8;
+  uint32_t top = 0;
+#pragma unroll 1
+  for (int i = thread; i < keys * kUnits; i += kConvThreads) {
+    const uint16_t* y = reinterpret_cast<const uint16_t*>(a.v) + (int64_t(first) + i / kUnits) * a.v_token +
+                        hk * a.v_head + i % kUnits * 8;
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t size = y[e] & 0x7fffu;
+      if (size < 0x7f80u) top = max(top, size);
+    }
+  }
+  atomicMax(code, own_code_for(top));
 }
 // 8 elements times `by` as sums of e4m3 pieces, each what the ones before leave (of what is
 // not finite NaN): put(piece, its 8 bytes).

@@ -192,3 +192,36 @@ def test_the_largest_values_of_bf16(n, D, B, L):
     values[..., ::2] = values[..., ::2].abs()  # (means near the largest as well)
     c.v_cache, c.vs = hold(values)
     check(c, range(0, B, 67), 2.0 ** 120)
+
+
+@pytest.mark.parametrize("n", [1, 3, 60, 200])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power_of_2", [41, 53, 60, 100, 127])
+def test_large_drafted_values_of_bf16(n, D, power_of_2):
+    """Drafted values far above any usual ones, alone and beside cached ones of their
+    size."""
+    for B, L in ((1, 0), (4, 300), (160, 130)):
+        c = make8([L] * B, [n] * B, 4, 2, D, 16, H, seed=6, parents="forest")
+        gen = torch.Generator(device="cuda").manual_seed(6)
+        c.v[:] = ((torch.rand(c.v.shape, generator=gen, device="cuda").double() * 2 - 1)
+                  * 1.875 * 2.0 ** power_of_2).to(H)
+        c.v[..., ::2] = c.v[..., ::2].abs()
+        # (numbers of up to 2^E make the unit 2^(E - 102) at the most)
+        check(c, range(0, B, 53), max(1.0, 2.0 ** (power_of_2 - 102)))
+        values = torch.randn(c.v_cache.shape, generator=gen, device="cuda").clamp_(-3, 3).double()
+        c.v_cache, c.vs = hold(values * 2.0 ** (power_of_2 - 2))
+        check(c, range(0, B, 53), 2.0 ** (power_of_2 - 8))
+
+
+def test_large_drafted_values_stay_in_their_branch_and_item():
+    """Rows that do not see them keep their digits, those of other requests every bit."""
+    up = [-1, 0, 0, 1, 2]
+    lens, nodes = [300, 150, 700], [4, 5, 6]
+    c = make8(lens, nodes, 4, 2, 64, 32, H, seed=7)
+    c.parents[1] = up
+    clean = call(c, max_len=700, max_nodes=6)
+    c.v[4 + 2] *= 2.0 ** 90
+    g = check(c, (1,), 1.0, max_len=700, max_nodes=6)
+    rest = torch.ones(15, dtype=torch.bool, device="cuda")
+    rest[4:9] = False
+    assert torch.equal(g["out"][rest], clean["out"][rest]) and torch.equal(g["lse"], clean["lse"])
