@@ -635,8 +635,9 @@ typedef struct {
  * are held within 1.875 2^15 (fp16) or 1.875 2^127 (bf16). Slots past the appended ones
  * stay as they are. new_len [B] (optional) is the slots in use after; it and status share
  * no memory with each other or the inputs, nor do the two caches (or their scales) begin at
- * one place. status [B]: BAD_OFFSETS (also: keep[b] beyond the request's tokens) and
- * TOO_LONG (more tokens than max_new, a length that is negative or would pass
+ * one place, nor the entries of one share memory (its strides are those of nested
+ * dimensions, in any order). status [B]: BAD_OFFSETS (also: keep[b] beyond the request's
+ * tokens) and TOO_LONG (more tokens than max_new, a length that is negative or would pass
  * max_len) append nothing; ID_OUT_OF_RANGE reports an entry of the path or a page out
  * of range, whose tokens are left out, and new_len stays as it was in all these
  * cases. Needs no workspace. */

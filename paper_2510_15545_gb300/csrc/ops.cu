@@ -1,10 +1,12 @@
 // ops.cu -- the extern "C" entry points of the operators around a verification
 // step: argument checks (before anything touches the GPU) and launches.
 #include <algorithm>
+#include <array>
 #include <climits>
 #include <cmath>
 #include <cstdint>
 #include <cstring>
+#include <utility>
 
 #include "tt_ops.h"
 
@@ -145,6 +147,28 @@ bool scales_ok(const tt_scales& s) {
 bool pages8_ok(const tt_pages& p, const tt_scales& s) {
   return pages_ok(p) && p.page_stride % 16 == 0 && p.slot_stride % 16 == 0 &&
          p.head_stride % 16 == 0 && scales_ok(s);
+}
+
+// Whether runs of `one` elements, at every sum of multiples of three strides (>= 0) up to
+// their counts, share no memory, as those of nested dimensions do.
+bool entries_apart(int64_t one, std::array<std::pair<int64_t, int64_t>, 3> stride_count) {
+  std::sort(stride_count.begin(), stride_count.end());
+  int64_t extent = one;  // of what the strides so far reach
+  for (const auto& [stride, count] : stride_count) {
+    if (count < 2) continue;
+    if (stride < extent) return false;
+    extent = stride > (INT64_MAX - extent) / (count - 1) ? INT64_MAX : extent + stride * (count - 1);
+  }
+  return true;
+}
+// Caches that are written, and their scales.
+bool pages_apart(const tt_append* p, const tt_pages& c) {
+  return entries_apart(p->head_dim, {{{c.page_stride, p->n_pages}, {c.slot_stride, p->page_size},
+                                      {c.head_stride, p->n_heads}}});
+}
+bool scales_apart(const tt_append* p, const tt_scales& c) {
+  return entries_apart(1, {{{c.page_stride, p->n_pages}, {c.group_stride, p->page_size / TT_SCALE_SLOTS},
+                            {c.head_stride, p->n_heads}}});
 }
 
 // What both tree calls check beyond the sizes, but for their caches.
@@ -405,6 +429,9 @@ tt_status tt_cache_append(const tt_append* p, const tt_rope_plan* rope, int32_t*
     if (p->k_cache.data == p->v_cache.data || (held8 && p->k_scale.data == p->v_scale.data))
       return TT_ERR_INVALID_ARG;
     if (p->n_pages < 1 || p->n_pages > INT32_MAX || !p->page_table || p->table_stride < pages)
+      return TT_ERR_INVALID_ARG;
+    if (!pages_apart(p, p->k_cache) || !pages_apart(p, p->v_cache) ||
+        (held8 && (!scales_apart(p, p->k_scale) || !scales_apart(p, p->v_scale))))
       return TT_ERR_INVALID_ARG;
   }
   AppendArgs a;
