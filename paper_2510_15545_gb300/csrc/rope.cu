@@ -40,8 +40,8 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
   constexpr int P = VEC ? (PAIRS ? VE / 2 : VE) : 1;  // pairs of a unit
   const RopeArgs& a = p.a;
   const int u = threadIdx.x % p.units, in_cta = threadIdx.x / p.units;
-  const int token = blockIdx.x * p.tokens + in_cta;
-  if (in_cta >= p.tokens || token >= a.n_tokens) return;
+  const uint32_t token = blockIdx.x * p.tokens + in_cta;  // (the last CTA's may pass 2^31)
+  if (in_cta >= p.tokens || token >= uint32_t(a.n_tokens)) return;
   const int H = a.Hq + a.Hk;
   const int h0 = blockIdx.y * p.chunk, h1 = min(H, h0 + p.chunk);
   const bool turns = u < p.turning;
