@@ -604,7 +604,7 @@ typedef struct {
  * within the request (of an accepted branch of a tree). Pages that are written belong
  * to one request. */
 typedef struct {
-  int32_t B;
+  int32_t B;           /* at most 2^30 */
   int32_t n_tokens;    /* of k and v; token_off[B] */
   int32_t max_new;     /* bound on a request's tokens, >= 1 */
   int32_t dtype;       /* TT_BF16 or TT_F16: of k and v */

@@ -434,6 +434,8 @@ tt_status tt_cache_append(const tt_append* p, const tt_rope_plan* rope, int32_t*
         (held8 && (!scales_apart(p, p->k_scale) || !scales_apart(p, p->v_scale))))
       return TT_ERR_INVALID_ARG;
   }
+  // (a CTA's threads share the requests out by numbers of 32 bits)
+  if (p->B > 1 << 30) return TT_ERR_UNSUPPORTED;
   AppendArgs a;
   std::memset(&a, 0, sizeof a);
   a.B = p->B;
