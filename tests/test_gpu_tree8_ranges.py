@@ -225,3 +225,23 @@ def test_large_drafted_values_stay_in_their_branch_and_item():
     rest = torch.ones(15, dtype=torch.bool, device="cuda")
     rest[4:9] = False
     assert torch.equal(g["out"][rest], clean["out"][rest]) and torch.equal(g["lse"], clean["lse"])
+
+
+@pytest.mark.parametrize("n", [3, 60])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("power_of_2", [60, 100, 126])
+def test_rows_beside_large_drafted_values(n, D, power_of_2):
+    """The first token of a request is large, the others do not see it: what their cached
+    keys give counts to 2^-125 of it for each key (weights of 2^-25 in units of 2^-102 of it,
+    of elements of up to 448, over sums of 2^7), and no more is lost."""
+    B, L = 40, 300
+    c = make8([L] * B, [n] * B, 4, 2, D, 16, H, seed=8)
+    c.parents = [[-1] * n for _ in range(B)]
+    c.v[0::n] = 2.0 ** power_of_2
+    g = call(c, max_len=L, max_nodes=n)
+    for b in (0, 39):
+        out, bound, lse, el = expected(c, b, D ** -0.5, 1.0)
+        bound = bound + L * 2.0 ** (power_of_2 - 125)
+        off = (g["out"][b * n:b * n + n].double() - out).abs() / bound
+        assert off.max() <= 1, (b, off.max())
+        assert ((g["lse"][b * n:b * n + n].double() - lse).abs() <= el).all()
