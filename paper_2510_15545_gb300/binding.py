@@ -1271,8 +1271,9 @@ def tt_cache_append(k: torch.Tensor, v: torch.Tensor, k_cache: torch.Tensor, v_c
     page_size / 16, kv heads]. keep int32 [B]: only a request's first so many; path
     int32 [N]: the i-th one appended is the token of that number within the request
     (an accepted branch). turns (rope_turns): keys are rotated on the way, by positions
-    int32 [N] or by their slots' numbers. Returns new_len and status int32 [B]; tensors
-    given in ``out`` are written in place. max_len bounds the slots in use after, max_new
+    int32 [N] or by their slots' numbers. The caches and scales are written: their entries
+    share no memory (expanded ones are refused). Returns new_len and status int32 [B];
+    tensors given in ``out`` are written in place. max_len bounds the slots in use after, max_new
     the tokens of a request (default: what the table and N allow)."""
     if stream is not None:
         with _on(stream):

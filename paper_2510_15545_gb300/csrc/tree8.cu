@@ -987,8 +987,9 @@ Cut8 cut8(const TreeArgs& a, int sm_count) {
   const int64_t rows = int64_t(a.max_nodes) * group;
   // Few rows go to the kernel whose products have them as columns, which costs what they
   // cost: 64 caches of 8192 and 8 heads took, with that one and with this,
-  //   heads of 128: 128 and 172 us at 16 rows, 174 and 179 at 32, 218 and 189 at 48;
-  //   heads of 64:  117 and 146 us at 16, 148 and 150 at 32.
+  //   heads of 128: 131 and 178 us at 16 rows, 176 and 183 at 32;
+  //   heads of 64:  120 and 148 us at 16, 156 and 153 at 32
+  // (and with 64 columns, which are no longer there, 218 and 189 at 48).
   c.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : kManyRows;
   const int64_t row_tiles = (rows + c.rows - 1) / c.rows;
   const int64_t tiles = cache_tiles(a.max_len) + tree_tiles(a.max_nodes);  // of an item

@@ -16,7 +16,7 @@
 // One CTA per SM: two warps copy, four convert, two issue products, eight turn scores into
 // weights: half of them the even tiles and half the odd ones, each with references, sums and
 // an output of their own. 1.07 GB of caches for 256 single tokens take 272 us, 4.0 TB/s: a
-// fifth of it is items' beginnings and ends. Of 32 rows (64 requests, caches up to 8192, 174
+// fifth of it is items' beginnings and ends. Of 32 rows (64 requests, caches up to 8192, 176
 // us) what bounds it is how long a tile takes from its scores to its weights, 12 instructions
 // a score.
 // The loops over the rows are rolled: unrolled, their code came from beyond the instruction

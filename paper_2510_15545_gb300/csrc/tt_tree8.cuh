@@ -32,8 +32,8 @@ constexpr float kSlack = 8.f;
 constexpr int kMinShare = 2;  // places of a CTA, where there are few
 // What an item costs beyond its tiles (queries, ancestors, output), in tiles: it
 // takes as many places in the list before its first tile. (8500 cycles beside 1500 of a
-// tile of single tokens; with 2 places those took 273 us, a serving batch 188, for 266 and
-// 179; with 8 they took 263 and 179, but a single chain 18.5 for 16.5.)
+// tile of single tokens; with 2 places those took 281 us, a serving batch 200, for 273 and
+// 185; with 8 they took 271 and 185, but a single chain 17.7 for 16.6.)
 constexpr int kItemCost = 5;
 
 // mbar_wait in few instructions: the roles wait in some thirty places, and what they
