@@ -650,11 +650,11 @@ size_t tt_tree8_workspace_bytes(const tt_tree* tree);
 /* tt_tree_attn over caches in 8 bits: tree's k_cache and v_cache hold e4m3 elements
  * (strides multiples of 16) with the given scales, as tt_cache_append leaves them;
  * q, k, v and the output are of tree's dtype. Keys count as they are; queries to 2^-17 of
- * a row's largest element; values to 2^-24 of the largest scale of the request's head, or
- * of 1 (fp16) or 2^-60 (bf16) if that is larger. Weights of cached keys are rounded to fp16:
- * by 2^-11 of each, or 2^-32 of the row's largest if that is more. Where drafted values reach
- * 2^43 in size (bf16), what cached keys give counts to 2^-95 of the largest. A slot whose scale
- * is NaN makes its rows NaN. Everything else is as for tt_tree_attn. */
+ * a row's largest element; values to 2^-23 of the largest scale of the request's head, or to
+ * 2^-76 if that is more. Weights of cached keys are rounded to fp16: by 2^-11 of each, or 2^-32
+ * of the row's largest if that is more. Where drafted values reach 2^43 in size (bf16), what
+ * cached keys give counts to 2^-88 of the largest. A slot whose scale is NaN makes its rows
+ * NaN. Everything else is as for tt_tree_attn. */
 tt_status tt_tree_attn8(const tt_tree* tree, const tt_scales* k_scale, const tt_scales* v_scale,
                         void* workspace, size_t workspace_bytes, void* out, float* lse,
                         int32_t* status, void* stream);

@@ -12,7 +12,7 @@
 // two (bf16) or three (fp16) e4m3 pieces of a power of two of its row, which the products
 // add up: its 8 or 11 digits, but for what is below 2^-17 of the row's largest element (the
 // distance of the smallest e4m3 numbers). Values become fp16, which holds every e4m3 value,
-// by four warps of their own, in units of the largest scale so far (2^-24 of that unit is
+// by four warps of their own, in units that follow the largest scale so far (2^-32 of it is
 // the finest); when a larger one comes the sums fall. The request's own drafted tokens are
 // tiles of keys and values of the inputs' type.
 //
@@ -76,7 +76,7 @@ struct Smem8 {
   alignas(16) float k_scale[kScaleRing][kGroups];
   uint32_t v_scale[kScaleRing][kGroups];  // two fp16 numbers, of the tile's unit
   uint32_t left_out[2][kScaleRing];   // groups whose page is out of range: keys, values
-  int unit[kScaleRing];               // largest scale of the item's values so far
+  int unit[kScaleRing];               // of the item's values so far
   float half[2][2][kRows];            // what the two threads of a row tell each other
   uint64_t k_full[kStagesK], k_empty[kStagesK], v_full[kStagesV], v_empty[kStagesV];
   uint64_t scale_full[kScaleRing], w_full[2], w_empty[2], s_full[2], s_free[2];
@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
           j = max(0, it.tile0 - it.n_tree);
           j1 = it.tile1 - it.n_tree;
           used = it.tile1 - it.tile0;
-          y.unit = it.tile0 < it.n_tree ? kOwnCode : 1;
+          y.unit = it.tile0 < it.n_tree ? kLeastUnit : 1;
           open = true;
         }
         if (j < j1) break;
@@ -257,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         // (The scales in this place are of kScaleRing tiles ago, which is further back than
         // the stages and the tiles on their way behind them reach.)
         const int ring = n % kScaleRing;
-        unit = max(unit, __shfl_sync(0xffffffffu, top, kGroups * i));
+        unit = max(unit, __shfl_sync(0xffffffffu, top, kGroups * i) - kFiner);
         if (lane / kGroups == i) {
           if (values)
             s.v_scale[ring][lane % kGroups] = c.code == 255 ? 0x7e007e00u : half_power(unit - int(c.code));
@@ -714,7 +714,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_kernel(const __grid_constan
         if (j + 1 == min(it.n_tree, it.tile1)) arrive(&s.seen_free);
         // what the values' scale makes of the sums, and a larger maximum of the row's
         float fall = 1.f;
-        if (unit > code) {
+        if (F16 ? unit != code : unit > code) {
           if (code > 0) fall = e8m0(code) * e8m0_inverse(unit);
           code = unit;
         }

@@ -68,7 +68,7 @@ struct Smem8 {
   float k_scale[kScaleRing][kGroups];
   alignas(16) uint32_t v_scale[kScaleRing][kGroups];  // two fp16 numbers, of the tile's unit
   uint32_t left_out[2][kScaleRing];   // groups whose page is out of range: keys, values
-  int unit[kScaleRing];               // largest scale of the item's values so far
+  int unit[kScaleRing];               // of the item's values so far
   alignas(16) float own_factor[8];    // the factor of drafted keys
   alignas(16) float shift[kSets][R];  // what is added to log2 scores
   alignas(16) float fall[kSets][R];   // a reference's last change
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           j = max(0, it.tile0 - it.n_tree);
           j1 = it.tile1 - it.n_tree;
           used = it.tile1 - it.tile0;
-          y.unit = it.tile0 < it.n_tree ? kOwnCode : 1;
+          y.unit = it.tile0 < it.n_tree ? kLeastUnit : 1;
           open = true;
         }
         if (j < j1) break;
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
         // (The scales in this place are of kScaleRing tiles ago, which is further back than
         // the stages and the tiles on their way behind them reach.)
         const int ring = n % kScaleRing;
-        unit = max(unit, __shfl_sync(0xffffffffu, top, kGroups * i));
+        unit = max(unit, __shfl_sync(0xffffffffu, top, kGroups * i) - kFiner);
         if (lane / kGroups == i) {
           if (values)
             s.v_scale[ring][lane % kGroups] = c.code == 255 ? 0x7e007e00u : half_power(unit - int(c.code));
@@ -777,11 +777,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree8_few_kernel(const __grid_con
           }
           unset = any_of(barrier, 128, none);
         };
-        // Values are in units of the largest scale so far; when that rises the output falls.
+        // Values are in units that follow the largest scale so far; when that rises the output
+        // falls (fp16: it rises where the drafted ones' unit ends).
         // (Where large drafted values need a larger unit, the weights of cached keys take what
         // is between.)
         float output_fall = 1.f;
-        if (unit > code) {
+        if (F16 ? unit != code : unit > code) {
           output_fall = code > 0 ? e8m0(code) * e8m0_inverse(unit) : 0.f;
           code = unit;
         }

@@ -267,14 +267,20 @@ __device__ __forceinline__ float largest(const uint4& q, float top) {
   for (int k = 0; k < 8; ++k) top = fabsf(e[k]) < INFINITY ? fmaxf(top, fabsf(e[k])) : top;
   return top;
 }
+// Values of the cache are fp16 numbers in units of 2^-kFiner of the largest scale so far: its
+// own are up to 448 2^7 = 57344 then, and of scales down to 2^-31 of it every digit stays that
+// is 2^-32 of it or more (in units of itself, values of scales from 2^-25 of it on, up to
+// 448 2^-25, came to nothing).
+constexpr int kFiner = 7;
+constexpr int kLeastUnit = 67;  // (its byte) of sums that drafted values and the cache's share
 // The unit (as a scale's byte) of sums that hold drafted values. Their weights have the
-// inputs' type, and take it: fp16 holds them beside scales of 2^0 or more, bf16 beside any that
-// are not below 2^-60. In that unit weights of up to 2^15 for 2^9 drafted tokens stay within
+// inputs' type, and take it: fp16 holds them in units of 2^0, and the sums go to the cache's
+// unit when its tiles begin; bf16 in any that are not below 2^-60. In that unit weights of up to 2^15 for 2^9 drafted tokens stay within
 // fp32 with values below 2^43; larger ones need a unit of 2^-102 times their power of two. So
 // the converting warps look at a drafted tile's values beside its keys: rows know the unit with
 // the scores (single tokens 272 us for 266, a serving batch 185 for 180; with the rows waiting
 // for the values that are fetched behind the keys, 295 and 195).
-__host__ __device__ constexpr int own_code(bool f16) { return f16 ? 127 : 67; }
+__host__ __device__ constexpr int own_code(bool f16) { return f16 ? 127 : kLeastUnit; }
 // (of the bits of the largest, a bf16 number)
 __device__ __forceinline__ int own_code_for(uint32_t top) { return int(top >> 7) - 102; }
 // Where a tile of drafted tokens has larger ones: the unit that the finite ones of a
@@ -319,7 +325,7 @@ __device__ __forceinline__ void in_pieces(const uint4& q, float by, Put put) {
     put(piece, make_uint2(two[0] | two[1] << 16, two[2] | two[3] << 16));
   }
 }
-// 2^-k as two fp16 numbers, k >= 0.
+// 2^-k as two fp16 numbers, k >= -15; 0 where there is none, from k = 25 on.
 __device__ __forceinline__ uint32_t half_power(int k) {
   const uint32_t x = k <= 14 ? uint32_t(15 - k) << 10 : k <= 24 ? 1u << (24 - k) : 0u;
   return x | x << 16;

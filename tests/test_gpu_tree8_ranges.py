@@ -4,8 +4,9 @@ jump, values far smaller than what scales them, and the largest ones.
 Tolerances. A score's error is that of the tests beside this one (fp32 products, pieces of
 queries). Weights of cached keys are fp16 numbers of a row's sum in units in which its
 largest is 2^7 or more: beyond 2^-11 of each they are off by 2^-25, so by 2^-32 of the
-largest, times the sizes of all values. Cached values are fp16 numbers in units of the
-largest scale so far: off by 2^-25 of it, and their mean by no more. Weights of drafted keys
+largest, times the sizes of all values. Cached values are fp16 numbers in units of 2^-7 of the
+largest scale so far: off by 2^-32 of it; those of scales from 2^-32 of it on, which are at most
+448 times theirs, are none: off by 2^-23. Their mean is off by no more. Weights of drafted keys
 have the inputs' type (in fp16 off by 2^-32 of the largest, too), the output is rounded to it
 once (in fp16 to 2^-25 at least)."""
 import math
@@ -37,8 +38,8 @@ def where(c, b):
 
 
 def expected(c, b, scale, unit):
-    """Output, its error bound and lse of request b's nodes; values are held in units of
-    `unit`."""
+    """Output, its error bound and lse of request b's nodes; cached values are off by 2^-25
+    of `unit` at most."""
     Hkv, D = c.k.shape[1:]
     G = c.q.shape[1] // Hkv
     lo, n = sum(c.nodes[:b]), c.nodes[b]
@@ -232,8 +233,8 @@ def test_large_drafted_values_stay_in_their_branch_and_item():
 @pytest.mark.parametrize("power_of_2", [60, 100, 126])
 def test_rows_beside_large_drafted_values(n, D, power_of_2):
     """The first token of a request is large, the others do not see it: what their cached
-    keys give counts to 2^-125 of it for each key (weights of 2^-25 in units of 2^-102 of it,
-    of elements of up to 448, over sums of 2^7), and no more is lost."""
+    keys give counts to 2^-118 of it for each key (weights of 2^-25 in units of 2^-102 of it,
+    of elements of up to 448 2^7 < 2^16, over sums of 2^7), and no more is lost."""
     B, L = 40, 300
     c = make8([L] * B, [n] * B, 4, 2, D, 16, H, seed=8)
     c.parents = [[-1] * n for _ in range(B)]
@@ -241,7 +242,31 @@ def test_rows_beside_large_drafted_values(n, D, power_of_2):
     g = call(c, max_len=L, max_nodes=n)
     for b in (0, 39):
         out, bound, lse, el = expected(c, b, D ** -0.5, 1.0)
-        bound = bound + L * 2.0 ** (power_of_2 - 125)
+        bound = bound + L * 2.0 ** (power_of_2 - 118)
         off = (g["out"][b * n:b * n + n].double() - out).abs() / bound
         assert off.max() <= 1, (b, off.max())
         assert ((g["lse"][b * n:b * n + n].double() - lse).abs() <= el).all()
+
+
+@pytest.mark.parametrize("n", [1, 9, 40])
+@pytest.mark.parametrize("D,dtype", [(64, E), (128, E), (64, H), (128, H)])
+@pytest.mark.parametrize("L", [100, 128 * 9])
+def test_scales_at_the_end_of_their_units(n, D, dtype, L):
+    """Scales of 2^-20 to 2^-36, and of that times the largest one of the head."""
+    B = 34
+    c = make8([L] * B, [n] * B, 2, 1, D, 16, dtype, seed=9)
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    values = torch.randn(c.v_cache.shape, generator=gen, device="cuda").double().clamp(-3, 3)
+    values[..., 1] = 3.0  # (between 224 and 448 times 2^-7)
+    for b in range(B):
+        at, slot = where(c, b)
+        if dtype == E:
+            values[at, slot] *= 2.0 ** (7 - 20 - b % 17)
+        else:  # (16 keys have a scale of 2^-7, for one of their elements)
+            values[at[16:], slot[16:]] *= 2.0 ** (-20 - b % 17)
+            values[at[:16], slot[:16]] = 0.0
+            values[at[:16], slot[:16], 0, 0] = 3.0
+    c.v_cache, c.vs = hold(values)
+    c.v.zero_()
+    for b in range(B):
+        check(c, (b,), 2.0 ** (-20 - b % 17) if dtype == E else 2.0 ** (2 - 7))
